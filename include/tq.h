@@ -39,6 +39,12 @@ extern "C" {
 #define TQ_STATUS_BAD_CODE 1u      /* a code of 0 or > K was met; it decoded as four zero bytes */
 #define TQ_STATUS_BAD_ROW 2u       /* a row segment did not hold exactly cols/4 groups          */
 #define TQ_STATUS_WAIT_EXPIRED 4u  /* a bounded wait inside a kernel ran out                    */
+#define TQ_STATUS_BAD_PAGE 8u      /* a page id or slot outside the cache was met: not touched  */
+#define TQ_STATUS_BAD_POSITION 16u /* a position outside the rotary table was met               */
+
+/* Element types of the operators that take more than one. */
+#define TQ_TYPE_BF16 0
+#define TQ_TYPE_F32 1
 
 typedef struct tq_dict tq_dict;   /* HOST: the compression table                                */
 typedef struct tq_ddict tq_ddict; /* handle of a table resident in DEVICE memory                */
@@ -383,6 +389,127 @@ void tq_test_withhold_table_chunk(int on);
 int tq_device_status(const tq_dmat* m, void* cuda_stream, uint32_t* status);
 
 void tq_dmat_free(tq_dmat* m); /* host handle only */
+
+/* ------------------------------------------------------------------------------------------
+ * Between the linear layers of a decoder: normalisation, rotary positions and the key-value cache,
+ * attention of one new token over that cache, attention to an encoder's states.  The products above
+ * write fp32 and read bf16, and so do these calls: every fp32 output of a product is an input here as
+ * it stands, every bf16 output here is an input of a product.  Sums, statistics and softmax are held
+ * in 32 bits; a bf16 result is rounded once, to nearest even.  All calls are asynchronous on
+ * cuda_stream, and so are their errors on the device: an index that is out of range is not followed,
+ * it leaves a bit in a status word.  Strides are in elements; a row's own elements are contiguous.
+ * ---------------------------------------------------------------------------------------- */
+
+/* Root-mean-square norm of the residual stream, with the addition of a layer's output:
+ *   s = h + delta (delta may be NULL: s = h),  h_out = s rounded to h's type,
+ *   out = s / sqrt(mean_c s_c^2 + eps) * w     (of s in 32 bits, before it is rounded to h_out).
+ * h, h_out: DEVICE, rows x cols of h_type, h_stride elements from row to row; h_out may be h (in place)
+ * and may be NULL (the sum is not kept).  delta: DEVICE, rows x cols of delta_type, delta_stride.
+ * d_weight: DEVICE fp32 [cols].  d_out: DEVICE bf16 [rows][cols].  cols: 1..TQ_NORM_MAX_COLS.
+ * Any alignment of the elements' own size is accepted; 16-byte aligned rows (cols a multiple of 8) are
+ * read and written in 16-byte pieces.  rows == 0 is a call that does nothing. */
+#define TQ_NORM_MAX_COLS 16384u
+int tq_rmsnorm(const void* d_h, int h_type, int64_t h_stride, const void* d_delta, int delta_type,
+               int64_t delta_stride, const float* d_weight, float eps, uint32_t rows, uint32_t cols,
+               void* d_h_out, void* d_out_bf16, void* cuda_stream);
+
+/* The same with the result in 8 bits and a scale for each row, by the rule of tq_quantize_rows:
+ * scale_r = max_c |n_c| / 127 (1 for a row of zeros), q = clamp(round(n / scale_r), -127, 127), n the
+ * normalised row in 32 bits.  A row with a NaN in n has scale NaN and levels 0.
+ * d_q: DEVICE int8 [rows][cols]; d_scale: DEVICE fp32 [rows]. */
+int tq_rmsnorm_q8(const void* d_h, int h_type, int64_t h_stride, const void* d_delta, int delta_type,
+                  int64_t delta_stride, const float* d_weight, float eps, uint32_t rows, uint32_t cols,
+                  void* d_h_out, int8_t* d_q, float* d_scale, void* cuda_stream);
+
+/* A pool of pages of bf16 keys and values.  Slot i of page p of head h starts at element
+ * p * page_stride + h * head_stride + i * slot_stride of d_k and of d_v: [page][head][slot][dim] and
+ * [page][slot][head][dim] are both such pools.  d_k, d_v: DEVICE, 16-byte aligned, the strides
+ * multiples of 8; head_dim 64 or 128.  d_status: DEVICE word that collects TQ_STATUS_BAD_PAGE and
+ * TQ_STATUS_BAD_POSITION, or NULL. */
+typedef struct tq_kv_cache {
+  void* d_k;
+  void* d_v;
+  uint32_t n_pages, page_size, n_kv_heads, head_dim;
+  int64_t page_stride, head_stride, slot_stride;
+  uint32_t* d_status;
+} tq_kv_cache;
+
+/* Rotary positions of new tokens' queries and keys, and the write of keys and values to the cache.
+ * Pair i of a head (elements i and i + rot_dim/2, or 2i and 2i+1 if interleaved) is turned by the
+ * angle whose cosine and sine are table[p][i] and table[p][rot_dim/2 + i], p the token's position on
+ * the axis that pair i belongs to: the first sections[0] pairs go by axis 0, the next sections[1] by
+ * axis 1 and so on (time, height and width of a patch; text has one axis).  Elements from rot_dim on
+ * pass unchanged.  q goes to d_q_out, k and v to slot slots[t] of the cache (slot / page_size is the
+ * page); a slot of -1 writes nothing (padding of a batch).  No two tokens of a call may share a slot.
+ * d_q, d_k, d_v: DEVICE, tokens of n_q_heads, n_kv_heads, n_kv_heads heads of head_dim elements of
+ * x_type, 16-byte aligned; q_stride, k_stride, v_stride: from token to token, multiples of 8.
+ * d_table: DEVICE fp32 [n_positions][rot_dim]; rot_dim: multiple of 8, 8..head_dim.
+ * d_positions: DEVICE int32 [n_axes][n_tokens]; n_axes: 1..TQ_ROPE_MAX_AXES; sections: HOST
+ * [n_axes], adding up to rot_dim/2.  d_slots: DEVICE int32 [n_tokens].  d_q_out: DEVICE bf16
+ * [n_tokens][n_q_heads][head_dim].  A token with a position outside the table sets
+ * TQ_STATUS_BAD_POSITION: its q_out is NaN and nothing of it is written to the cache.  A slot outside
+ * the pool (other than -1) sets TQ_STATUS_BAD_PAGE and writes nothing to the cache. */
+#define TQ_ROPE_MAX_AXES 3u
+int tq_rope_append(const void* d_q, const void* d_k, const void* d_v, int x_type, int64_t q_stride,
+                   int64_t k_stride, int64_t v_stride, uint32_t n_tokens, uint32_t n_q_heads,
+                   const float* d_table, uint32_t n_positions, uint32_t rot_dim,
+                   const int32_t* d_positions, const uint32_t* sections, uint32_t n_axes,
+                   int interleaved, const int32_t* d_slots, const tq_kv_cache* cache, void* d_q_out,
+                   void* cuda_stream);
+
+/* Workspace of the two attention calls below: what the parts of a split hand to one another, the
+ * counters that find the last part, a status word.  tq_attn_workspace_size: bytes for the current
+ * device, whatever the sizes of the calls.  d_ws: DEVICE, 256-byte aligned; tq_attn_workspace_init
+ * clears it once, and every call leaves its counters cleared for the next.  Calls that share a
+ * workspace must not overlap on the GPU (calls on one stream never do). */
+int tq_attn_workspace_size(uint64_t* device_bytes);
+int tq_attn_workspace_init(void* d_ws, uint64_t ws_bytes, void* cuda_stream);
+
+/* Attention of one new token per sequence over a paged cache:
+ *   out[b][h] = sum_s softmax_s(scale * q[b][h] . k_s) v_s,  s = 0 .. lens[b]-1,
+ * k_s and v_s those of key-value head h / (n_q_heads / n_kv_heads) in slot s % page_size of page
+ * page_table[b][s / page_size].  The length is split over the GPU and the parts are joined in a fixed
+ * order: the same call gives the same bits.
+ * d_q: DEVICE bf16, n_seqs rows of [n_q_heads][head_dim], q_stride elements from row to row (multiple
+ * of 8), 16-byte aligned.  d_page_table: DEVICE int32, n_seqs rows of max_pages entries, of which a row's first
+ * ceil(lens[b] / page_size) are read.  d_lens: DEVICE int32 [n_seqs].  d_out: DEVICE bf16
+ * [n_seqs][n_q_heads][head_dim]; d_lse: DEVICE fp32 [n_seqs][n_q_heads] or NULL: the natural logarithm
+ * of the softmax's denominator.  A sequence of length 0 (or less) gives zeros and lse -inf.  Slots that
+ * no length reaches may hold anything.  A length beyond max_pages * page_size is cut there and a page
+ * id outside the pool hides its page; both set TQ_STATUS_BAD_PAGE. */
+int tq_paged_attention(const tq_kv_cache* cache, const void* d_q, int64_t q_stride, uint32_t n_seqs,
+                       uint32_t n_q_heads, const int32_t* d_page_table, uint32_t max_pages,
+                       const int32_t* d_lens, float scale, void* d_out, float* d_lse, void* d_ws,
+                       uint64_t ws_bytes, void* cuda_stream);
+
+/* Keys and values of an encoder's states: bf16, state s of head h of sequence b at element
+ * b * batch_stride + s * state_stride + h * head_stride of d_k and of d_v.  16-byte aligned, strides
+ * multiples of 8; batch_stride 0 gives every sequence the same states.  head_dim 64 or 128. */
+typedef struct tq_encoder_kv {
+  const void* d_k;
+  const void* d_v;
+  uint32_t n_seqs, n_states, n_kv_heads, head_dim;
+  int64_t batch_stride, state_stride, head_stride;
+} tq_encoder_kv;
+
+/* Attention of n_tokens queries per sequence to an encoder's states (no order between the two):
+ *   out[b][t][h] = sum_s softmax_s(scale * q[b][t][h] . k_s) v_s
+ * over the states s < kv_len[b] whose block the token sees: mask[b][t][s / block_len] != 0 (image
+ * tiles; block_len 1 is a mask of single states).  A token that sees nothing gives zeros and lse -inf.
+ * States at or past kv_len and states that a token does not see may hold anything, Inf and NaN included.
+ * d_q: DEVICE bf16, [n_q_heads][head_dim] for each sequence and token, q_batch_stride and q_token_stride
+ * elements apart (multiples of 8), 16-byte aligned.  d_kv_len: DEVICE int32 [n_seqs] or NULL (all states); values are
+ * clamped to 0..n_states.  d_mask: DEVICE uint8 [n_seqs][n_tokens][ceil(n_states / block_len)] or NULL.
+ * d_out: DEVICE bf16 [n_seqs][n_tokens][n_q_heads][head_dim]; d_lse: DEVICE fp32
+ * [n_seqs][n_tokens][n_q_heads] or NULL. */
+int tq_cross_attention(const tq_encoder_kv* kv, const void* d_q, int64_t q_batch_stride,
+                       int64_t q_token_stride, uint32_t n_tokens, uint32_t n_q_heads,
+                       const int32_t* d_kv_len, const uint8_t* d_mask, uint32_t block_len, float scale,
+                       void* d_out, float* d_lse, void* d_ws, uint64_t ws_bytes, void* cuda_stream);
+
+/* Read and clear the workspace's status word (TQ_STATUS_WAIT_EXPIRED: the call's outputs are not
+ * valid); synchronises cuda_stream. */
+int tq_attn_status(void* d_ws, void* cuda_stream, uint32_t* status);
 
 #ifdef __cplusplus
 }

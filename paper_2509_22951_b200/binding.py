@@ -30,6 +30,12 @@ TQ_TILES_MAX_COLS = 65536
 TQ_STATUS_BAD_CODE = 1
 TQ_STATUS_BAD_ROW = 2
 TQ_STATUS_WAIT_EXPIRED = 4
+TQ_STATUS_BAD_PAGE = 8
+TQ_STATUS_BAD_POSITION = 16
+TQ_TYPE_BF16 = 0
+TQ_TYPE_F32 = 1
+TQ_NORM_MAX_COLS = 16384
+TQ_ROPE_MAX_AXES = 3
 
 EXPORTS = [
     "tq_strerror", "tq_last_cuda_error", "tq_set_num_threads", "tq_quantize_tensor", "tq_quantize_tensor_bits", "tq_quantize_rows",
@@ -40,6 +46,8 @@ EXPORTS = [
     "tq_fused_gemm_ws", "tq_decode_bf16", "tq_gemm_bf16_ws", "tq_decode_bf16_stack", "tq_gemm_plan_size", "tq_gemm_plan_create", "tq_gemm_plan_run",
     "tq_gemm_plan_status", "tq_gemm_plan_free", "tq_stack_size", "tq_stack_plan_host", "tq_stack_create",
     "tq_fused_gemv_stack", "tq_fused_gemv_stack_host", "tq_stack_launches", "tq_test_withhold_table_chunk", "tq_decompress_stack", "tq_stack_free", "tq_device_status", "tq_dmat_free",
+    "tq_rmsnorm", "tq_rmsnorm_q8", "tq_rope_append", "tq_attn_workspace_size", "tq_attn_workspace_init", "tq_paged_attention",
+    "tq_cross_attention", "tq_attn_status",
 ]
 
 
@@ -56,6 +64,18 @@ class _Info(C.Structure):
                 ("layout", C.c_int32), ("levels_signed", C.c_int32),
                 ("n_hits", C.c_uint64), ("n_miss", C.c_uint64), ("stream_bytes", C.c_uint64),
                 ("payload_bytes", C.c_uint64), ("device_bytes", C.c_uint64), ("n_raw_words", C.c_uint64)]
+
+
+class _KvCache(C.Structure):
+    _fields_ = [("d_k", C.c_void_p), ("d_v", C.c_void_p), ("n_pages", C.c_uint32), ("page_size", C.c_uint32),
+                ("n_kv_heads", C.c_uint32), ("head_dim", C.c_uint32), ("page_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("slot_stride", C.c_int64), ("d_status", C.c_void_p)]
+
+
+class _EncoderKv(C.Structure):
+    _fields_ = [("d_k", C.c_void_p), ("d_v", C.c_void_p), ("n_seqs", C.c_uint32), ("n_states", C.c_uint32),
+                ("n_kv_heads", C.c_uint32), ("head_dim", C.c_uint32), ("batch_stride", C.c_int64), ("state_stride", C.c_int64),
+                ("head_stride", C.c_int64)]
 
 
 def _load() -> C.CDLL:
@@ -119,6 +139,18 @@ def _load() -> C.CDLL:
         "tq_stack_free": (None, [vp]),
         "tq_device_status": (C.c_int, [vp, vp, u32p]),
         "tq_dmat_free": (None, [vp]),
+        "tq_rmsnorm": (C.c_int, [vp, C.c_int, C.c_int64, vp, C.c_int, C.c_int64, vp, C.c_float, C.c_uint32, C.c_uint32, vp, vp, vp]),
+        "tq_rmsnorm_q8": (C.c_int, [vp, C.c_int, C.c_int64, vp, C.c_int, C.c_int64, vp, C.c_float, C.c_uint32, C.c_uint32, vp, vp,
+                                    vp, vp]),
+        "tq_rope_append": (C.c_int, [vp, vp, vp, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_uint32, C.c_uint32, vp, C.c_uint32,
+                                     C.c_uint32, vp, u32p, C.c_uint32, C.c_int, vp, C.POINTER(_KvCache), vp, vp]),
+        "tq_attn_workspace_size": (C.c_int, [u64p]),
+        "tq_attn_workspace_init": (C.c_int, [vp, C.c_uint64, vp]),
+        "tq_paged_attention": (C.c_int, [C.POINTER(_KvCache), vp, C.c_int64, C.c_uint32, C.c_uint32, vp, C.c_uint32, vp, C.c_float,
+                                         vp, vp, vp, C.c_uint64, vp]),
+        "tq_cross_attention": (C.c_int, [C.POINTER(_EncoderKv), vp, C.c_int64, C.c_int64, C.c_uint32, C.c_uint32, vp, vp, C.c_uint32,
+                                         C.c_float, vp, vp, vp, C.c_uint64, vp]),
+        "tq_attn_status": (C.c_int, [vp, vp, u32p]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -662,3 +694,226 @@ def tq_device_status(m: DeviceMatrix, stream=None) -> int:
     st = C.c_uint32()
     _check(_lib.tq_device_status(m._h, _stream_ptr(stream), C.byref(st)), "tq_device_status")
     return st.value
+
+
+# ------------------------------------------------------------------------------ between the linear layers
+_TYPES = {torch.bfloat16: TQ_TYPE_BF16, torch.float32: TQ_TYPE_F32}
+
+
+class _On:
+    """Device and stream of a call: a call on a stream that is not the current one gets its results from that stream's memory."""
+
+    __slots__ = ("ptr", "ctx")
+
+    def __init__(self, device: torch.device, stream):
+        index = device.index
+        if stream is None and torch.cuda.current_device() == index:  # the usual case, without a context manager
+            self.ptr, self.ctx = torch._C._cuda_getCurrentRawStream(index), None
+        elif stream is None:
+            self.ctx = torch.cuda.device(index)
+            self.ptr = torch.cuda.current_stream(index).cuda_stream
+        else:
+            self.ctx = torch.cuda.stream(stream)
+            self.ptr = stream.cuda_stream
+
+    def __enter__(self):
+        if self.ctx is not None:
+            self.ctx.__enter__()
+        return self.ptr
+
+    def __exit__(self, *exc):
+        if self.ctx is not None:
+            self.ctx.__exit__(*exc)
+
+
+def _strides(x: torch.Tensor):
+    """Strides, with 0 for dimensions of size 1, whose stride means nothing."""
+    return tuple(st if n > 1 else 0 for n, st in zip(x.shape, x.stride()))
+
+
+def _norm_args(h, weight, delta, h_out):
+    assert h.is_cuda and h.dtype in _TYPES and h.dim() == 2 and (h.stride(1) == 1 or h.shape[1] == 1)
+    rows, cols = h.shape
+    assert weight.is_cuda and weight.dtype == torch.float32 and weight.is_contiguous() and weight.numel() == cols
+    dp, dt, ds = None, 0, 0
+    if delta is not None:
+        assert delta.is_cuda and delta.dtype in _TYPES and delta.shape == h.shape and (delta.stride(1) == 1 or cols == 1)
+        dp, dt, ds = delta.data_ptr(), _TYPES[delta.dtype], delta.stride(0)
+        if h_out is None:
+            h_out = h
+    if h_out is not None:
+        assert h_out.is_cuda and h_out.dtype == h.dtype and h_out.shape == h.shape and _strides(h_out) == _strides(h)
+    return rows, cols, (h.data_ptr(), _TYPES[h.dtype], h.stride(0), dp, dt, ds, weight.data_ptr()), None if h_out is None else h_out.data_ptr()
+
+
+def tq_rmsnorm(h: torch.Tensor, weight: torch.Tensor, delta: torch.Tensor | None = None, eps: float = 1e-5,
+               out: torch.Tensor | None = None, h_out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """h: CUDA bf16 / fp32 [rows][cols] (rows may be strided); delta: bf16 / fp32 of the same shape; weight: fp32 [cols].
+    With a delta the sum h + delta goes to h_out (a tensor like h), or to h itself when h_out is None.  -> bf16 [rows][cols]."""
+    rows, cols, args, h_out = _norm_args(h, weight, delta, h_out)
+    with _On(h.device, stream) as st:
+        if out is None:
+            out = torch.empty((rows, cols), dtype=torch.bfloat16, device=h.device)
+        assert out.is_cuda and out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() == rows * cols
+        _check(_lib.tq_rmsnorm(*args, eps, rows, cols, h_out, out.data_ptr(), st), "tq_rmsnorm")
+    return out
+
+
+def tq_rmsnorm_q8(h: torch.Tensor, weight: torch.Tensor, delta: torch.Tensor | None = None, eps: float = 1e-5,
+                  q: torch.Tensor | None = None, scale: torch.Tensor | None = None, h_out: torch.Tensor | None = None, stream=None):
+    """tq_rmsnorm with the result in 8 bits: -> (int8 [rows][cols], fp32 [rows] scales)."""
+    rows, cols, args, h_out = _norm_args(h, weight, delta, h_out)
+    with _On(h.device, stream) as st:
+        if q is None:
+            q = torch.empty((rows, cols), dtype=torch.int8, device=h.device)
+        if scale is None:
+            scale = torch.empty(rows, dtype=torch.float32, device=h.device)
+        assert q.is_cuda and q.dtype == torch.int8 and q.is_contiguous() and q.numel() == rows * cols
+        assert scale.is_cuda and scale.dtype == torch.float32 and scale.is_contiguous() and scale.numel() == rows
+        _check(_lib.tq_rmsnorm_q8(*args, eps, rows, cols, h_out, q.data_ptr(), scale.data_ptr(), st), "tq_rmsnorm_q8")
+    return q, scale
+
+
+class KvCache:
+    """A pool of pages of keys and values: keeps the tensors and a status word alive."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor):
+        assert k.is_cuda and k.dtype == torch.bfloat16 and k.dim() == 4 and k.stride(3) == 1
+        assert v.device == k.device and v.dtype == k.dtype and v.shape == k.shape and _strides(v) == _strides(k)
+        self.k, self.v = k, v
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
+        self.status = torch.zeros(1, dtype=torch.int32, device=k.device)
+        self._c = _KvCache(k.data_ptr(), v.data_ptr(), self.n_pages, self.page_size, self.n_kv_heads, self.head_dim,
+                           *_strides(k)[:3], self.status.data_ptr())
+        self._ref = C.byref(self._c)
+
+
+def tq_kv_cache(k: torch.Tensor, v: torch.Tensor) -> KvCache:
+    """k, v: CUDA bf16 [pages][kv heads][page size][head dim] with any strides (a pool laid out as [pages][page size][kv heads][head
+    dim] is passed as pool.transpose(1, 2))."""
+    return KvCache(k, v)
+
+
+def tq_kv_cache_status(cache: KvCache) -> int:
+    """Reads and clears the cache's status word (TQ_STATUS_BAD_PAGE, TQ_STATUS_BAD_POSITION); synchronises the current stream."""
+    st = int(cache.status.item())
+    cache.status.zero_()
+    return st
+
+
+def _heads(x: torch.Tensor, n: int, dim: int):
+    """Token stride of x, [tokens][n * dim] or [tokens][n][dim]."""
+    assert x.dim() in (2, 3) and x.stride(-1) == 1
+    assert (x.shape[1] == n * dim) if x.dim() == 2 else (x.shape[1] == n and x.shape[2] == dim and (n == 1 or x.stride(1) == dim))
+    return x.stride(0)
+
+
+def tq_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, positions: torch.Tensor,
+                   slots: torch.Tensor, cache: KvCache, sections=None, interleaved: bool = False, out: torch.Tensor | None = None,
+                   stream=None) -> torch.Tensor:
+    """q, k, v: CUDA bf16 or fp32 [tokens][heads * head dim] or [tokens][heads][head dim] (tokens may be strided); table: fp32
+    [positions][rot dim], cosines then sines; positions: int32 [axes][tokens] or [tokens]; slots: int32 [tokens], -1 for none;
+    sections: pairs of each axis (one axis: all).  -> rotated q, bf16 [tokens][q heads][head dim]; k and v are in the cache."""
+    D, K, T = cache.head_dim, cache.n_kv_heads, q.shape[0]
+    assert q.is_cuda and q.dtype in _TYPES and k.dtype == q.dtype and v.dtype == q.dtype and k.shape[0] == T and v.shape[0] == T
+    assert k.device == q.device and v.device == q.device and cache.k.device == q.device
+    H = q.shape[1] if q.dim() == 3 else q.shape[1] // D
+    qs, ks, vs = _heads(q, H, D), _heads(k, K, D), _heads(v, K, D)
+    assert table.is_cuda and table.dtype == torch.float32 and table.is_contiguous() and table.dim() == 2
+    assert positions.is_cuda and positions.dtype == torch.int32 and positions.is_contiguous() and slots.is_cuda
+    assert slots.dtype == torch.int32 and slots.is_contiguous() and slots.numel() == T
+    axes = 1 if positions.dim() == 1 else positions.shape[0]
+    assert positions.numel() == axes * T
+    rot = table.shape[1]
+    sec = (rot // 2,) if sections is None else sections
+    assert len(sec) == axes
+    with _On(q.device, stream) as st:
+        if out is None:
+            out = torch.empty((T, H, D), dtype=torch.bfloat16, device=q.device)
+        assert out.is_cuda and out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() == T * H * D
+        _check(_lib.tq_rope_append(q.data_ptr(), k.data_ptr(), v.data_ptr(), _TYPES[q.dtype], qs, ks, vs, T, H, table.data_ptr(),
+                                   table.shape[0], rot, positions.data_ptr(), (C.c_uint32 * axes)(*sec), axes, int(interleaved),
+                                   slots.data_ptr(), cache._ref, out.data_ptr(), st), "tq_rope_append")
+    return out
+
+
+class AttnWorkspace:
+    """Workspace of tq_paged_attention and tq_cross_attention: one for each stream that makes such calls."""
+
+    def __init__(self, buf: torch.Tensor):
+        self.buf = buf
+        self.ptr, self.bytes = buf.data_ptr(), buf.numel()
+
+
+def tq_attn_workspace(device="cuda", stream=None) -> AttnWorkspace:
+    dev = torch.empty(0, device=device).device
+    need = C.c_uint64()
+    with torch.cuda.device(dev), _On(dev, stream) as st:
+        _check(_lib.tq_attn_workspace_size(C.byref(need)), "tq_attn_workspace_size")
+        buf = torch.empty(need.value, dtype=torch.uint8, device=dev)
+        _check(_lib.tq_attn_workspace_init(buf.data_ptr(), buf.numel(), st), "tq_attn_workspace_init")
+    return AttnWorkspace(buf)
+
+
+def tq_attn_status(workspace: AttnWorkspace, stream=None) -> int:
+    st = C.c_uint32()
+    with _On(workspace.buf.device, stream) as sp:
+        _check(_lib.tq_attn_status(workspace.ptr, sp, C.byref(st)), "tq_attn_status")
+    return st.value
+
+
+def _attn_out(shape, device, out, lse):
+    if out is None:
+        out = torch.empty(shape, dtype=torch.bfloat16, device=device)
+    assert out.is_cuda and out.dtype == torch.bfloat16 and out.is_contiguous() and out.shape == shape
+    if lse is not None:
+        assert lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == shape[:-1]
+    return out
+
+
+def tq_paged_attention(q: torch.Tensor, cache: KvCache, page_table: torch.Tensor, lens: torch.Tensor, workspace: AttnWorkspace,
+                       scale: float | None = None, out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                       stream=None) -> torch.Tensor:
+    """q: CUDA bf16 [sequences][q heads][head dim] (sequences may be strided); page_table: int32 [sequences][max pages]; lens: int32
+    [sequences]; scale: 1 / sqrt(head dim) when None; lse: fp32 [sequences][q heads], filled when given.  -> bf16 like q."""
+    D = cache.head_dim
+    assert q.is_cuda and q.dtype == torch.bfloat16 and q.dim() == 3 and q.shape[2] == D and q.stride(2) == 1
+    B, H = q.shape[0], q.shape[1]
+    assert (H == 1 or q.stride(1) == D) and cache.k.device == q.device and workspace.buf.device == q.device
+    assert page_table.is_cuda and page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.is_contiguous()
+    assert lens.is_cuda and lens.dtype == torch.int32 and lens.is_contiguous() and lens.numel() == B and page_table.shape[0] == B
+    with _On(q.device, stream) as st:
+        out = _attn_out((B, H, D), q.device, out, lse)
+        _check(_lib.tq_paged_attention(cache._ref, q.data_ptr(), q.stride(0) if B > 1 else 0, B, H, page_table.data_ptr(), page_table.shape[1],
+                                       lens.data_ptr(), D ** -0.5 if scale is None else scale, out.data_ptr(),
+                                       None if lse is None else lse.data_ptr(), workspace.ptr, workspace.bytes, st),
+               "tq_paged_attention")
+    return out
+
+
+def tq_cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, workspace: AttnWorkspace, kv_len: torch.Tensor | None = None,
+                       mask: torch.Tensor | None = None, block_len: int = 1, scale: float | None = None,
+                       out: torch.Tensor | None = None, lse: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """q: CUDA bf16 [sequences][tokens][q heads][head dim]; k, v: bf16 [sequences][states][kv heads][head dim], any strides (an
+    expanded batch has the same states for every sequence); kv_len: int32 [sequences]; mask: uint8 / bool
+    [sequences][tokens][ceil(states / block_len)], nonzero where a token sees the block; lse: fp32 [sequences][tokens][q heads],
+    filled when given.  -> bf16 [sequences][tokens][q heads][head dim]."""
+    assert q.is_cuda and q.dtype == torch.bfloat16 and q.dim() == 4 and q.stride(3) == 1
+    B, T, H, D = q.shape
+    assert (H == 1 or q.stride(2) == D) and workspace.buf.device == q.device
+    assert k.device == q.device and k.dtype == torch.bfloat16 and k.dim() == 4 and k.stride(3) == 1 and k.shape[0] == B and k.shape[3] == D
+    assert v.device == q.device and v.dtype == torch.bfloat16 and v.shape == k.shape and _strides(v) == _strides(k)
+    S, K = k.shape[1], k.shape[2]
+    if kv_len is not None:
+        assert kv_len.device == q.device and kv_len.dtype == torch.int32 and kv_len.is_contiguous() and kv_len.numel() == B
+    if mask is not None:
+        assert mask.device == q.device and mask.dtype in (torch.uint8, torch.bool) and mask.is_contiguous()
+        assert block_len >= 1 and mask.shape == (B, T, -(-S // block_len))
+    kv = _EncoderKv(k.data_ptr(), v.data_ptr(), B, S, K, D, *_strides(k)[:3])
+    with _On(q.device, stream) as st:
+        out = _attn_out((B, T, H, D), q.device, out, lse)
+        _check(_lib.tq_cross_attention(kv, q.data_ptr(), q.stride(0) if B > 1 else 0, q.stride(1) if T > 1 else 0, T, H, None if kv_len is None else kv_len.data_ptr(),
+                                       None if mask is None else mask.data_ptr(), block_len, D ** -0.5 if scale is None else scale,
+                                       out.data_ptr(), None if lse is None else lse.data_ptr(), workspace.ptr, workspace.bytes, st),
+               "tq_cross_attention")
+    return out

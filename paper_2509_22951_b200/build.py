@@ -10,8 +10,9 @@ PKG = Path(__file__).resolve().parent
 ROOT = PKG.parent
 CSRC = PKG / "csrc"
 LIB = PKG / "libtq.so"
-SOURCES = [CSRC / "tq_device.cu", CSRC / "tq_gemm.cu", CSRC / "tq_gemm_ws.cu", CSRC / "tq_tiles.cu", CSRC / "tq_wide.cu", CSRC / "tq_encode.cu", CSRC / "tq_dict_device.cu", CSRC / "tq_host.cpp"]
-HEADERS = [CSRC / "tq_internal.h", CSRC / "tq_sm100.cuh", CSRC / "tq_tiles_common.cuh", ROOT / "include" / "tq.h"]
+SOURCES = [CSRC / "tq_device.cu", CSRC / "tq_gemm.cu", CSRC / "tq_gemm_ws.cu", CSRC / "tq_tiles.cu", CSRC / "tq_wide.cu", CSRC / "tq_encode.cu", CSRC / "tq_dict_device.cu",
+           CSRC / "tq_norm.cu", CSRC / "tq_rope.cu", CSRC / "tq_attn.cu", CSRC / "tq_host.cpp"]
+HEADERS = [CSRC / "tq_internal.h", CSRC / "tq_sm100.cuh", CSRC / "tq_tiles_common.cuh", CSRC / "tq_ops_common.cuh", ROOT / "include" / "tq.h"]
 
 
 def _nvcc() -> str | None:
@@ -40,7 +41,7 @@ def build_library(force: bool = False, verbose: bool = False) -> Path:
         raise RuntimeError("libtq.so is missing or stale and nvcc was not found; cannot build the CUDA library")
     tmp = LIB.with_name(f"libtq.tmp{os.getpid()}.so")
     cmd = [nvcc, "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-           "-Xcompiler", "-fPIC,-O3,-pthread", "-shared", "-I", str(ROOT / "include"), "-I", str(CSRC),
+           "--threads", "8", "-Xcompiler", "-fPIC,-O3,-pthread", "-shared", "-I", str(ROOT / "include"), "-I", str(CSRC),
            "-o", str(tmp)] + [str(s) for s in SOURCES] + ["-lpthread"]
     if verbose:
         cmd.insert(1, "-Xptxas=-v")

@@ -231,3 +231,18 @@ int tq_tiles_build_device(const tq_ddict* dict, const uint8_t* d_levels, uint32_
 // A host table from windows that are already ranked (tq_host.cpp; used by the device-side builder).
 int tq_dict_from_ranked(const uint32_t* keys, const uint64_t* counts, uint32_t K, uint64_t n_windows,
                         uint64_t n_distinct, tq_dict** out);
+
+// Checks of a cache's description (tq_attn.cu).
+int tq_check_cache(const tq_kv_cache* cache);
+
+// Plan of the attention workspace: counters (one per CTA that can be the first of a split group; every
+// call leaves them zero), the status word, then the partial results of the CTAs.
+constexpr uint32_t kAttnMaxCtas = 512;
+struct tq_attn_ws {
+  uint32_t* counters;
+  uint32_t* status;
+  float* parts;
+};
+constexpr uint64_t kAttnWsHeader = kAttnMaxCtas * 4 + 256;
+// nullptr counters: d_ws is not usable as a workspace of ws_bytes bytes
+tq_attn_ws tq_attn_ws_plan(void* d_ws, uint64_t ws_bytes);

@@ -1,0 +1,185 @@
+// Rotary positions of new tokens and the write of their keys and values to the cache (tq_rope_append).
+//
+// Pair i of a head, (a, b) -> (a cos - b sin, a sin + b cos), with the cosine and sine of table row p,
+// p the position on the pair's axis.  The pairs of a head are independent of one another: a thread owns
+// four pairs (eight elements) of the heads it visits, loads their eight cosines and sines once per token
+// and reuses them over the token's query and key heads.  8 to 16 bytes move per two or three operations:
+// memory bound for prompts, latency for a decode step.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "tq_internal.h"
+#include "tq_ops_common.cuh"
+
+namespace {
+
+using namespace tq_ops;
+
+constexpr uint32_t kRopeThreads = 256;
+
+struct RopeParams {
+  const void* q;
+  const void* k;
+  const void* v;
+  int64_t q_stride, k_stride, v_stride;
+  const float* table;
+  const int32_t* positions;
+  const int32_t* slots;
+  __nv_bfloat16* q_out;
+  tq_kv_cache cache;
+  uint32_t n_tokens, n_q_heads, n_positions, rot_dim;
+  uint32_t axis_end[TQ_ROPE_MAX_AXES];  // first pair past each axis' section
+  uint32_t n_axes;
+};
+
+// Eight elements of a head as two runs of four: the first and second members of four pairs, or eight
+// consecutive elements (interleaved pairs, elements that pass unchanged).
+template <int TYPE>
+struct Raw4x2 {
+  uint4 a, b;
+  __device__ __forceinline__ void load(const void* base, size_t i, size_t j) {
+    if constexpr (TYPE == TQ_TYPE_F32) {
+      a = load_once((const float*)base + i);
+      b = load_once((const float*)base + j);
+    } else {
+      const uint2 x = *reinterpret_cast<const uint2*>((const __nv_bfloat16*)base + i);
+      const uint2 y = *reinterpret_cast<const uint2*>((const __nv_bfloat16*)base + j);
+      a = make_uint4(x.x, x.y, 0, 0);
+      b = make_uint4(y.x, y.y, 0, 0);
+    }
+  }
+  __device__ __forceinline__ void get(float (&f)[8]) const {
+    if constexpr (TYPE == TQ_TYPE_F32) {
+      f[0] = __uint_as_float(a.x), f[1] = __uint_as_float(a.y), f[2] = __uint_as_float(a.z), f[3] = __uint_as_float(a.w);
+      f[4] = __uint_as_float(b.x), f[5] = __uint_as_float(b.y), f[6] = __uint_as_float(b.z), f[7] = __uint_as_float(b.w);
+    } else {
+      f[0] = bf16_lo(a.x), f[1] = bf16_hi(a.x), f[2] = bf16_lo(a.y), f[3] = bf16_hi(a.y);
+      f[4] = bf16_lo(b.x), f[5] = bf16_hi(b.x), f[6] = bf16_lo(b.y), f[7] = bf16_hi(b.y);
+    }
+  }
+};
+
+// grid (tokens, parts of the heads); the 256 threads are 256 / (head_dim / 8) heads side by side.
+template <int TYPE, bool INTERLEAVED>
+__global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopeParams p) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const uint32_t D = p.cache.head_dim, per_head = D / 8u, side = kRopeThreads / per_head;
+  const uint32_t j = threadIdx.x % per_head, t = blockIdx.x;
+  const uint32_t pairs = p.rot_dim / 2u, pair0 = 4u * j;
+  const bool turns = pair0 < pairs;
+  // where this thread's eight elements of a head lie
+  const uint32_t e0 = INTERLEAVED ? 8u * j : (turns ? pair0 : p.rot_dim + 2u * (pair0 - pairs));
+  const uint32_t e1 = !INTERLEAVED && turns ? pairs + pair0 : e0 + 4u;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+
+  const int32_t slot = p.slots[t];
+  const uint32_t page = (uint32_t)slot / p.cache.page_size;  // a negative slot becomes a page past the pool
+  const bool in_pool = slot >= 0 && page < p.cache.n_pages;
+  bool known = true;
+  for (uint32_t a = 0; a < p.n_axes; ++a) known = known && (uint32_t)p.positions[(size_t)a * p.n_tokens + t] < p.n_positions;
+  if (threadIdx.x == 0 && blockIdx.y == 0 && p.cache.d_status != nullptr) {
+    const uint32_t bad = (known ? 0u : TQ_STATUS_BAD_POSITION) | (slot >= 0 && !in_pool ? TQ_STATUS_BAD_PAGE : 0u);
+    if (bad) atomicOr(p.cache.d_status, bad);
+  }
+  const bool keep = in_pool && known;
+  const size_t slot_at = keep ? (size_t)page * p.cache.page_stride + (size_t)((uint32_t)slot % p.cache.page_size) * p.cache.slot_stride : 0;
+
+  float cs[4] = {1.f, 1.f, 1.f, 1.f}, sn[4] = {0.f, 0.f, 0.f, 0.f};
+  if (turns && known) {
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) {
+      uint32_t a = 0;
+      while (pair0 + i >= p.axis_end[a]) ++a;  // the sections add up to all pairs
+      const float* row = p.table + (size_t)p.positions[(size_t)a * p.n_tokens + t] * p.rot_dim + pair0 + i;
+      cs[i] = __ldg(row);
+      sn[i] = __ldg(row + pairs);
+    }
+  }
+  if (!known) cs[0] = cs[1] = cs[2] = cs[3] = __int_as_float(0x7FC00000);
+
+  const uint32_t K = p.cache.n_kv_heads, heads = p.n_q_heads + 2u * K;
+  for (uint32_t n = blockIdx.y * side + threadIdx.x / per_head; n < heads; n += gridDim.y * side) {
+    // heads in order: queries, keys, values
+    const uint32_t kind = n < p.n_q_heads ? 0u : (n < p.n_q_heads + K ? 1u : 2u);
+    if (kind != 0u && !keep) continue;
+    const uint32_t h = kind == 0u ? n : (kind == 1u ? n - p.n_q_heads : n - p.n_q_heads - K);
+    const void* src = kind == 0u ? p.q : (kind == 1u ? p.k : p.v);
+    const size_t row = (size_t)t * (kind == 0u ? p.q_stride : (kind == 1u ? p.k_stride : p.v_stride)) + (size_t)h * D;
+    const bool plain = kind == 2u;
+    Raw4x2<TYPE> raw;
+    raw.load(src, row + e0, row + e1);
+    float f[8];
+    raw.get(f);
+    if (!plain && (turns || !known)) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float& x = INTERLEAVED ? f[2 * i] : f[i];
+        float& y = INTERLEAVED ? f[2 * i + 1] : f[4 + i];
+        const float a = x * cs[i] - y * sn[i], b = x * sn[i] + y * cs[i];
+        x = a;
+        y = b;
+      }
+    }
+    __nv_bfloat16* dst = kind == 0u ? p.q_out + ((size_t)t * p.n_q_heads + h) * D
+                                    : (__nv_bfloat16*)(kind == 1u ? p.cache.d_k : p.cache.d_v) + slot_at + (size_t)h * p.cache.head_stride;
+    const uint4 o = pack8(f);
+    *reinterpret_cast<uint2*>(dst + e0) = make_uint2(o.x, o.y);
+    *reinterpret_cast<uint2*>(dst + e1) = make_uint2(o.z, o.w);
+  }
+}
+
+}  // namespace
+
+extern "C" int tq_rope_append(const void* d_q, const void* d_k, const void* d_v, int x_type, int64_t q_stride, int64_t k_stride,
+                              int64_t v_stride, uint32_t n_tokens, uint32_t n_q_heads, const float* d_table, uint32_t n_positions,
+                              uint32_t rot_dim, const int32_t* d_positions, const uint32_t* sections, uint32_t n_axes,
+                              int interleaved, const int32_t* d_slots, const tq_kv_cache* cache, void* d_q_out,
+                              void* cuda_stream) {
+  if (int rc = tq_check_cache(cache)) return rc;
+  if (x_type != TQ_TYPE_BF16 && x_type != TQ_TYPE_F32) return TQ_ERR_INVALID_ARG;
+  if (!sections || n_axes == 0 || n_axes > TQ_ROPE_MAX_AXES || rot_dim == 0 || rot_dim % 8u || rot_dim > cache->head_dim) return TQ_ERR_INVALID_ARG;
+  RopeParams p{};
+  uint64_t end = 0;
+  for (uint32_t a = 0; a < n_axes; ++a) {
+    end += sections[a];
+    if (end > rot_dim / 2u) return TQ_ERR_INVALID_ARG;
+    p.axis_end[a] = (uint32_t)end;
+  }
+  if (end != rot_dim / 2u) return TQ_ERR_INVALID_ARG;
+  if (n_tokens > 0x7FFFFFFFu || n_q_heads > 65536u) return TQ_ERR_UNSUPPORTED_SHAPE;
+  if (n_tokens == 0) return TQ_OK;
+  auto bad = [](const void* ptr, uintptr_t align) { return ptr == nullptr || ((uintptr_t)ptr & (align - 1u)) != 0; };
+  if (bad(d_q, 16) || bad(d_k, 16) || bad(d_v, 16) || bad(d_table, 4) || bad(d_positions, 4) || bad(d_slots, 4) || bad(d_q_out, 16)) return TQ_ERR_INVALID_ARG;
+  if (n_q_heads == 0 || n_positions == 0 || q_stride % 8 || k_stride % 8 || v_stride % 8) return TQ_ERR_INVALID_ARG;
+  p.q = d_q;
+  p.k = d_k;
+  p.v = d_v;
+  p.q_stride = q_stride;
+  p.k_stride = k_stride;
+  p.v_stride = v_stride;
+  p.table = d_table;
+  p.positions = d_positions;
+  p.slots = d_slots;
+  p.q_out = (__nv_bfloat16*)d_q_out;
+  p.cache = *cache;
+  p.n_tokens = n_tokens;
+  p.n_q_heads = n_q_heads;
+  p.n_positions = n_positions;
+  p.rot_dim = rot_dim;
+  p.n_axes = n_axes;
+  const uint32_t side = kRopeThreads / (cache->head_dim / 8u), heads = n_q_heads + 2u * cache->n_kv_heads;
+  // few tokens: a block for every set of heads; many: one block walks all heads of its token and keeps
+  // the cosines and sines
+  const uint32_t parts = n_tokens < 2u * (uint32_t)sm_count() ? (heads + side - 1u) / side : 1u;
+  const dim3 grid(n_tokens, parts);
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  const char* what = "rope_append launch";
+  if (x_type == TQ_TYPE_F32) {
+    return interleaved ? launch_pdl(rope_append_kernel<TQ_TYPE_F32, true>, grid, kRopeThreads, 0, st, what, p)
+                       : launch_pdl(rope_append_kernel<TQ_TYPE_F32, false>, grid, kRopeThreads, 0, st, what, p);
+  }
+  return interleaved ? launch_pdl(rope_append_kernel<TQ_TYPE_BF16, true>, grid, kRopeThreads, 0, st, what, p)
+                     : launch_pdl(rope_append_kernel<TQ_TYPE_BF16, false>, grid, kRopeThreads, 0, st, what, p);
+}
