@@ -468,7 +468,7 @@ int tq_attn_workspace_init(void* d_ws, uint64_t ws_bytes, void* cuda_stream);
 /* Attention of one new token per sequence over a paged cache:
  *   out[b][h] = sum_s softmax_s(scale * q[b][h] . k_s) v_s,  s = 0 .. lens[b]-1,
  * k_s and v_s those of key-value head h / (n_q_heads / n_kv_heads) in slot s % page_size of page
- * page_table[b][s / page_size].  The length is split over the GPU and the parts are joined in a fixed
+ * page_table[b][s / page_size]; scale positive and finite.  The length is split over the GPU and the parts are joined in a fixed
  * order: the same call gives the same bits.
  * d_q: DEVICE bf16, n_seqs rows of [n_q_heads][head_dim], q_stride elements from row to row (multiple
  * of 8), 16-byte aligned.  d_page_table: DEVICE int32, n_seqs rows of max_pages entries, of which a row's first
@@ -496,7 +496,8 @@ typedef struct tq_encoder_kv {
  *   out[b][t][h] = sum_s softmax_s(scale * q[b][t][h] . k_s) v_s
  * over the states s < kv_len[b] whose block the token sees: mask[b][t][s / block_len] != 0 (image
  * tiles; block_len 1 is a mask of single states).  A token that sees nothing gives zeros and lse -inf.
- * States at or past kv_len and states that a token does not see may hold anything, Inf and NaN included.
+ * States at or past kv_len and states that a token does not see may hold anything, Inf and NaN included
+ * (a token is slow where some of its sequence's tokens see such a state and it does not).
  * d_q: DEVICE bf16, [n_q_heads][head_dim] for each sequence and token, q_batch_stride and q_token_stride
  * elements apart (multiples of 8), 16-byte aligned.  d_kv_len: DEVICE int32 [n_seqs] or NULL (all states); values are
  * clamped to 0..n_states.  d_mask: DEVICE uint8 [n_seqs][n_tokens][ceil(n_states / block_len)] or NULL.

@@ -11,7 +11,7 @@ ROOT = PKG.parent
 CSRC = PKG / "csrc"
 LIB = PKG / "libtq.so"
 SOURCES = [CSRC / "tq_device.cu", CSRC / "tq_gemm.cu", CSRC / "tq_gemm_ws.cu", CSRC / "tq_tiles.cu", CSRC / "tq_wide.cu", CSRC / "tq_encode.cu", CSRC / "tq_dict_device.cu",
-           CSRC / "tq_norm.cu", CSRC / "tq_rope.cu", CSRC / "tq_attn.cu", CSRC / "tq_host.cpp"]
+           CSRC / "tq_norm.cu", CSRC / "tq_rope.cu", CSRC / "tq_attn.cu", CSRC / "tq_cross.cu", CSRC / "tq_host.cpp"]
 HEADERS = [CSRC / "tq_internal.h", CSRC / "tq_sm100.cuh", CSRC / "tq_tiles_common.cuh", CSRC / "tq_ops_common.cuh", ROOT / "include" / "tq.h"]
 
 

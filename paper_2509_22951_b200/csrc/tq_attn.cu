@@ -463,6 +463,7 @@ int launch(AttnParams& p, cudaStream_t st) {
   return launch_pdl(kern, dim3(grid), kThreads, smem, st, what, p);
 }
 
+bool scale_ok(float scale) { return scale > 0.f && scale < INFINITY; }
 bool misaligned(const void* ptr, uintptr_t align) { return ptr == nullptr || ((uintptr_t)ptr & (align - 1u)) != 0; }
 
 }  // namespace
@@ -490,7 +491,8 @@ extern "C" {
 int tq_attn_workspace_size(uint64_t* device_bytes) {
   if (!device_bytes) return TQ_ERR_INVALID_ARG;
   const uint64_t ctas = min(2u * (uint32_t)sm_count(), kAttnMaxCtas);
-  *device_bytes = kAttnWsHeader + ctas * 2u * kPartFloats * sizeof(float);
+  const uint64_t split = ctas * 2u * kPartFloats * sizeof(float), cross = tq_cross_workspace_bytes();
+  *device_bytes = kAttnWsHeader + (split > cross ? split : cross);
   return TQ_OK;
 }
 
@@ -515,7 +517,7 @@ int tq_paged_attention(const tq_kv_cache* cache, const void* d_q, int64_t q_stri
                        const int32_t* d_page_table, uint32_t max_pages, const int32_t* d_lens, float scale, void* d_out,
                        float* d_lse, void* d_ws, uint64_t ws_bytes, void* cuda_stream) {
   if (int rc = tq_check_cache(cache)) return rc;
-  if (n_q_heads == 0 || n_q_heads % cache->n_kv_heads || q_stride % 8 || max_pages == 0) return TQ_ERR_INVALID_ARG;
+  if (n_q_heads == 0 || n_q_heads % cache->n_kv_heads || q_stride % 8 || max_pages == 0 || !scale_ok(scale)) return TQ_ERR_INVALID_ARG;
   if (n_q_heads > 65536u || n_seqs > 0x7FFFFFFFu) return TQ_ERR_UNSUPPORTED_SHAPE;
   if (n_seqs == 0) return TQ_OK;
   if (misaligned(d_q, 16) || misaligned(d_page_table, 4) || misaligned(d_lens, 4) || misaligned(d_out, 16) || ((uintptr_t)d_lse & 3u)) return TQ_ERR_INVALID_ARG;
@@ -555,7 +557,7 @@ int tq_cross_attention(const tq_encoder_kv* kv, const void* d_q, int64_t q_batch
                        void* cuda_stream) {
   if (!kv || kv->n_kv_heads == 0 || (kv->n_states && (misaligned(kv->d_k, 16) || misaligned(kv->d_v, 16)))) return TQ_ERR_INVALID_ARG;
   if (kv->batch_stride % 8 || kv->state_stride % 8 || kv->head_stride % 8 || kv->batch_stride < 0 || kv->state_stride < 0 || kv->head_stride < 0) return TQ_ERR_INVALID_ARG;
-  if (n_q_heads == 0 || n_q_heads % kv->n_kv_heads || q_batch_stride % 8 || q_token_stride % 8 || (d_mask && block_len == 0)) return TQ_ERR_INVALID_ARG;
+  if (n_q_heads == 0 || n_q_heads % kv->n_kv_heads || q_batch_stride % 8 || q_token_stride % 8 || (d_mask && block_len == 0) || !scale_ok(scale)) return TQ_ERR_INVALID_ARG;
   if ((kv->head_dim != 64 && kv->head_dim != 128) || n_q_heads > 65536u || kv->n_states > 0x7FFFFFFFu || n_tokens > 0x7FFFFFFFu ||
       kv->n_seqs > 0x7FFFFFFFu || (uint64_t)n_tokens * n_q_heads > 0x7FFFFFFFull)
     return TQ_ERR_UNSUPPORTED_SHAPE;
@@ -588,6 +590,12 @@ int tq_cross_attention(const tq_encoder_kv* kv, const void* d_q, int64_t q_batch
   p.head_parts = (p.group + kHeads - 1u) / kHeads;
   p.scale_log2 = scale * 1.4426950408889634f;
   cudaStream_t st = (cudaStream_t)cuda_stream;
+  if (n_tokens > 1) {
+    bool served = false;
+    const int rc = tq_cross_launch(kv, d_q, q_batch_stride, q_token_stride, n_tokens, n_q_heads, d_kv_len, d_mask, p.block_len, p.n_blocks,
+                                   p.scale_log2, d_out, d_lse, p.ws, cuda_stream, &served);
+    if (served) return rc;
+  }
   return kv->head_dim == 64 ? launch<64, false>(p, st) : launch<128, false>(p, st);
 }
 

@@ -1,0 +1,825 @@
+// Attention of many queries to an encoder's states (tq_cross_attention with more than one token) on the
+// 5th-generation tensor cores.
+//
+//   out = sum_s p_s v_s / sum_s p_s,   p_s = exp(scale q.k_s - m),   m a running maximum
+//
+// 4 D operations per query, state and head against a few bytes: bound by the tensor cores and, next to
+// them, by the exponentials (a 128 x 128 tile of scores costs 1024 cycles of an SM's tensor core at
+// head_dim 128 and 1024 cycles of its 16 exponentials a cycle).
+//
+// Work.  The G query heads that share a key-value head and the tokens are one list of rows (row r = token
+// r / G, head r % G); 256 of them are a group's tile.  The units are (sequence, key-value head, tile of
+// rows, 128 states), and, as in the one-token kernel, each CTA takes an equal share of consecutive units:
+// a group that lies in several shares leaves its parts in the workspace and the CTA that finishes last
+// joins them in order.  So short prompts use all SMs too, and long ones have no last wave.
+//
+// CTA, one to an SM.  Warp 8 loads: it decides which tiles of states some row of the group
+// sees, announces them one by one in a ring of entries that all roles follow, and brings their K and V
+// (128-byte swizzled, 2 x 64 columns) with TMA into a ring of stages.  One thread of warp 9 issues the
+// products.  Warps 0-3 and 4-7 each own 128 rows, a thread a row: scores from tensor memory, mask,
+// maximum, exponentials, p as bf16 back to tensor memory over the scores, where it is the A operand of the
+// product with V.  The two halves alternate: the tensor core multiplies for one while the other takes its
+// exponentials.  Tensor memory: 2 x 128 columns of scores, 2 x head_dim columns of output.
+//
+// The output is rescaled only when a row's maximum has grown by more than 2^8 since the last rescaling:
+// p then stays below 2^8, which costs no precision in bf16 or in the fp32 sum, and nearly all of the
+// passes over the output in tensor memory are saved.
+//
+// States that no row may see are not multiplied: whole tiles are skipped, the tail past kv_len is zeroed in
+// shared memory.  A state that only some rows see enters the others' sums with p = 0; if its value is Inf or
+// NaN that product is NaN, so a row whose sum of p is finite but whose output has a NaN is computed again
+// from the states it sees (slow, and only with a mask).
+//
+// Every wait is bounded; one that runs out raises TQ_STATUS_WAIT_EXPIRED, all roles leave their loops and
+// tensor memory is released on every path.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "tq_internal.h"
+#include "tq_ops_common.cuh"
+
+namespace {
+
+using namespace tq_ops;
+using namespace tq_sm100;
+
+constexpr uint32_t kRows = 256;        // rows of a group's tile
+constexpr uint32_t kHalf = 128;        // rows of a half: one thread each
+constexpr uint32_t kStates = 128;      // states of a unit
+constexpr int kSoftWarps = 8, kLoadWarp = 8, kMmaWarp = 9;
+constexpr int kCrossThreads = 384;  // 12 warps: the last two only make the third warpgroup whole for its register split
+// registers a thread: 168 at launch (12 warps of an SM's 65536); 200 for the softmax warps, whose row of scores is 128 of
+// them, 96 for the others.  The launch checks the kernel's own count: a split above it would wait for ever.
+constexpr int kSoftRegs = 200, kOtherRegs = 96;
+constexpr uint32_t kEntries = 4;       // announced tiles that may be under way
+constexpr uint32_t kTmemCols = 512;
+constexpr float kRescale = 8.0f;       // log2 of how far p may exceed 1
+
+enum : uint32_t { kTile = 0, kEnd = 1, kStop = 2 };
+
+// What the loader announces: a tile of states for the group's rows, the end of the group (or of this CTA's
+// part of it), the end of the work.
+struct Entry {
+  uint32_t kind, b, kvh, qt;  // sequence, key-value head, tile of rows
+  uint32_t tile, len;         // tile of states; states of the sequence
+  uint32_t first;             // first tile of this CTA's part
+  uint32_t t0, t1;            // kEnd: tiles of states of this CTA's part
+  uint32_t c0, parts;         // kEnd: first CTA with a part of the group, number of parts
+  uint32_t pad;
+};
+
+struct CrossParams {
+  const __nv_bfloat16* k;
+  const __nv_bfloat16* v;
+  int64_t batch_stride, state_stride, head_stride;
+  const __nv_bfloat16* q;
+  int64_t q_batch_stride, q_token_stride;
+  __nv_bfloat16* out;
+  float* lse;
+  const int32_t* kv_len;
+  const uint8_t* mask;
+  uint32_t n_states, block_len, n_blocks;
+  uint32_t n_seqs, n_tokens, n_q_heads, n_kv_heads, group;
+  uint32_t rows, row_tiles;  // n_tokens * group, and its tiles of 256
+  float scale_log2;
+  tq_attn_ws ws;
+};
+
+template <int D>
+struct CrossSmem {
+  static constexpr uint32_t kSlabs = D / 64;                       // 64 columns = 128 bytes of a swizzled row
+  static constexpr uint32_t kQHalf = kSlabs * kHalf * 128;         // queries of a half
+  static constexpr uint32_t kStageBytes = kSlabs * kStates * 128;  // K or V of a tile
+  static constexpr uint32_t kStages = D == 128 ? 5 : 8;
+  static constexpr uint32_t kOffKv = 2 * kQHalf;
+  static constexpr uint32_t kOffMisc = kOffKv + kStages * kStageBytes;
+  // misc: [0] dead flag, [4] tensor-memory base, [8] join flag, barriers from 16 on, entries behind them
+  static constexpr uint32_t kBarKvFull = 16, kBarKvEmpty = kBarKvFull + 8 * kStages, kBarQFull = kBarKvEmpty + 8 * kStages;
+  static constexpr uint32_t kBarSFull = kBarQFull + 16, kBarPFull = kBarSFull + 16, kBarODone = kBarPFull + 16;
+  static constexpr uint32_t kBarJoin = kBarODone + 16;
+  static constexpr uint32_t kBarEFull = kBarJoin + 8, kBarEEmpty = kBarEFull + 8 * kEntries;
+  static constexpr uint32_t kOffEntries = (kBarEEmpty + 8 * kEntries + 15) / 16 * 16;
+  static constexpr uint32_t kTotal = kOffMisc + kOffEntries + kEntries * sizeof(Entry);
+  static_assert(kTotal + 1024 <= 232448, "shared memory of one CTA");
+};
+// a part of a split group: [D / 4][256] float4 of output, then the rows' maxima and sums
+constexpr uint64_t kCrossPartFloats = kRows * (128 + 2);
+
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+               "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
+               : "memory");
+}
+// A operand in tensor memory, B described in shared memory.
+__device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// V as it lies, states x columns: the operand's N index (column) is contiguous.  128-byte swizzle: 64 columns x 8
+// states are 1024 bytes, the next 8 states follow, the next 64 columns are a slab of 128 states away.
+__device__ __forceinline__ uint64_t umma_desc_n_major(uint32_t smem_addr) {
+  uint64_t d = umma_desc(smem_addr);
+  d &= ~((uint64_t)0x3FFF << 16);
+  return d | ((uint64_t)((kStates * 128u) >> 4) << 16);
+}
+constexpr uint32_t kIdescNMajorB = 1u << 16;
+
+#define TMEM_LD32(r, addr)                                                                                                          \
+  asm volatile(                                                                                                                     \
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,"  \
+      "%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"                                                                                \
+      : "=r"((r)[0]), "=r"((r)[1]), "=r"((r)[2]), "=r"((r)[3]), "=r"((r)[4]), "=r"((r)[5]), "=r"((r)[6]), "=r"((r)[7]),             \
+        "=r"((r)[8]), "=r"((r)[9]), "=r"((r)[10]), "=r"((r)[11]), "=r"((r)[12]), "=r"((r)[13]), "=r"((r)[14]), "=r"((r)[15]),       \
+        "=r"((r)[16]), "=r"((r)[17]), "=r"((r)[18]), "=r"((r)[19]), "=r"((r)[20]), "=r"((r)[21]), "=r"((r)[22]), "=r"((r)[23]),     \
+        "=r"((r)[24]), "=r"((r)[25]), "=r"((r)[26]), "=r"((r)[27]), "=r"((r)[28]), "=r"((r)[29]), "=r"((r)[30]), "=r"((r)[31])      \
+      : "r"(addr))
+#define TMEM_ST32(addr, r)                                                                                                          \
+  asm volatile(                                                                                                                     \
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,"   \
+      "%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(addr),                                                                  \
+      "r"((r)[0]), "r"((r)[1]), "r"((r)[2]), "r"((r)[3]), "r"((r)[4]), "r"((r)[5]), "r"((r)[6]), "r"((r)[7]), "r"((r)[8]),          \
+      "r"((r)[9]), "r"((r)[10]), "r"((r)[11]), "r"((r)[12]), "r"((r)[13]), "r"((r)[14]), "r"((r)[15]), "r"((r)[16]), "r"((r)[17]),  \
+      "r"((r)[18]), "r"((r)[19]), "r"((r)[20]), "r"((r)[21]), "r"((r)[22]), "r"((r)[23]), "r"((r)[24]), "r"((r)[25]),               \
+      "r"((r)[26]), "r"((r)[27]), "r"((r)[28]), "r"((r)[29]), "r"((r)[30]), "r"((r)[31])                                            \
+      : "memory")
+#define TMEM_LD16(r, addr)                                                                                                          \
+  asm volatile(                                                                                                                     \
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"                      \
+      : "=r"((r)[0]), "=r"((r)[1]), "=r"((r)[2]), "=r"((r)[3]), "=r"((r)[4]), "=r"((r)[5]), "=r"((r)[6]), "=r"((r)[7]),             \
+        "=r"((r)[8]), "=r"((r)[9]), "=r"((r)[10]), "=r"((r)[11]), "=r"((r)[12]), "=r"((r)[13]), "=r"((r)[14]), "=r"((r)[15])        \
+      : "r"(addr))
+#define TMEM_ST16(addr, r)                                                                                                          \
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr), \
+               "r"((r)[0]), "r"((r)[1]), "r"((r)[2]), "r"((r)[3]), "r"((r)[4]), "r"((r)[5]), "r"((r)[6]), "r"((r)[7]), "r"((r)[8]), \
+               "r"((r)[9]), "r"((r)[10]), "r"((r)[11]), "r"((r)[12]), "r"((r)[13]), "r"((r)[14]), "r"((r)[15])                      \
+               : "memory")
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ float exp2_fast(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+__device__ __forceinline__ uint32_t states_of(const CrossParams& p, uint32_t b) {
+  if (p.kv_len == nullptr) return p.n_states;
+  const int32_t n = __ldg(p.kv_len + b);
+  return n <= 0 ? 0u : min((uint32_t)n, p.n_states);
+}
+__device__ __forceinline__ uint32_t units_of(uint32_t len) { return len == 0u ? 1u : (len + kStates - 1u) / kStates; }
+// The low n bits, n clamped to 0..32.
+__device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : (n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1u); }
+
+template <int D>
+__global__ void __launch_bounds__(kCrossThreads, 1)
+    cross_attention_kernel(const CrossParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+  using L = CrossSmem<D>;
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  uint8_t* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);  // swizzled tiles start on 1024 bytes
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const uint32_t smem0 = smem_u32(smem), misc = smem0 + L::kOffMisc;
+  volatile uint32_t* const dead = reinterpret_cast<uint32_t*>(smem + L::kOffMisc);
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(smem + L::kOffMisc + 4);
+  uint32_t* const join_flag = reinterpret_cast<uint32_t*>(smem + L::kOffMisc + 8);
+  volatile Entry* const entries = reinterpret_cast<Entry*>(smem + L::kOffMisc + L::kOffEntries);
+  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+  auto bar = [&](uint32_t off, uint32_t i) { return misc + off + 8u * i; };
+
+  if (threadIdx.x == 0) {
+    *dead = 0u;
+    for (uint32_t i = 0; i < L::kStages; ++i) {
+      mbar_init(bar(L::kBarKvFull, i), 1);
+      mbar_init(bar(L::kBarKvEmpty, i), 1);
+    }
+    for (uint32_t i = 0; i < 2; ++i) {
+      mbar_init(bar(L::kBarQFull, i), 4);
+      mbar_init(bar(L::kBarSFull, i), 1);
+      mbar_init(bar(L::kBarPFull, i), 4);
+      mbar_init(bar(L::kBarODone, i), 1);
+    }
+    for (uint32_t i = 0; i < kEntries; ++i) {
+      mbar_init(bar(L::kBarEFull, i), 1);
+      mbar_init(bar(L::kBarEEmpty, i), kSoftWarps + 1);
+    }
+    mbar_init(bar(L::kBarJoin, 0), kSoftWarps);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(kTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tmem_fence_before();
+  __syncthreads();
+  tmem_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+
+  bool ok = true;
+  auto wait = [&](uint32_t b, uint32_t parity) {
+    ok = ok && mbar_wait(b, parity, dead);
+    ok = __all_sync(kFull, ok);
+  };
+  uint32_t en = 0;  // entries this warp has taken (or announced)
+  auto take = [&](Entry& e) {  // the next entry, which stays in its slot until it is released
+    wait(bar(L::kBarEFull, en % kEntries), (en / kEntries) & 1u);
+    if (!ok) return;
+    const volatile Entry& s = entries[en % kEntries];
+    e.kind = s.kind, e.b = s.b, e.kvh = s.kvh, e.qt = s.qt, e.tile = s.tile, e.len = s.len, e.first = s.first;
+    e.t0 = s.t0, e.t1 = s.t1, e.c0 = s.c0, e.parts = s.parts;
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar(L::kBarEEmpty, en % kEntries));
+    ++en;
+  };
+
+  if (warp >= kLoadWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+  if (warp == kLoadWarp) {
+    // ---- which tiles, and their K and V ---------------------------------------------------------------
+    const uint32_t groups = p.n_kv_heads * p.row_tiles;  // of one sequence
+    uint64_t total = 0, before = 0;
+    for (uint32_t b = lane; b < p.n_seqs; b += 32u) total += units_of(states_of(p, b));
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) total += __shfl_xor_sync(kFull, total, d);
+    total *= groups;
+    const uint32_t ctas = (uint32_t)min((uint64_t)gridDim.x, total);
+    uint64_t u = 0, u1 = 0;
+    if (blockIdx.x < ctas) {
+      u = total * blockIdx.x / ctas;
+      u1 = total * (blockIdx.x + 1u) / ctas;
+    }
+    const uint64_t u0 = u;
+    uint32_t b = 0, n = 1, len = 0, st = 0, st_round = 0;
+    if (u < u1) {
+      for (;; ++b) {
+        len = states_of(p, b);
+        n = units_of(len);
+        if (u < before + (uint64_t)n * groups) break;
+        before += (uint64_t)n * groups;
+      }
+    }
+    auto announce = [&](const Entry& e) {
+      if (en >= kEntries) wait(bar(L::kBarEEmpty, en % kEntries), ((en / kEntries) - 1u) & 1u);
+      if (!ok) return;
+      if (lane == 0) {
+        volatile Entry& s = entries[en % kEntries];
+        s.kind = e.kind, s.b = e.b, s.kvh = e.kvh, s.qt = e.qt, s.tile = e.tile, s.len = e.len, s.first = e.first;
+        s.t0 = e.t0, s.t1 = e.t1, s.c0 = e.c0, s.parts = e.parts;
+        mbar_arrive(bar(L::kBarEFull, en % kEntries));
+      }
+      __syncwarp();
+      ++en;
+    };
+    auto load = [&](const CUtensorMap* map, const Entry& e) {
+      if (st_round) wait(bar(L::kBarKvEmpty, st), (st_round - 1u) & 1u);
+      if (!ok) return;
+      if (lane == 0) {
+        const uint32_t full = bar(L::kBarKvFull, st), dst = smem0 + L::kOffKv + st * L::kStageBytes;
+        mbar_expect_tx(full, L::kStageBytes);
+#pragma unroll
+        for (uint32_t s = 0; s < L::kSlabs; ++s)
+          tma_load_4d(dst + s * kStates * 128u, map, (int)(s * 64u), (int)(e.tile * kStates), p.head_stride ? (int)e.kvh : 0, p.batch_stride ? (int)e.b : 0, full);
+      }
+      __syncwarp();
+      if (++st == L::kStages) {
+        st = 0;
+        ++st_round;
+      }
+    };
+    while (u < u1 && ok) {
+      const uint64_t in = u - before;
+      Entry e{};
+      e.b = b;
+      e.len = len;
+      const uint32_t g = (uint32_t)(in / n);
+      e.kvh = g / p.row_tiles;
+      e.qt = g % p.row_tiles;
+      e.t0 = (uint32_t)(in % n);
+      e.t1 = (uint32_t)min((uint64_t)n, (uint64_t)e.t0 + (u1 - u));
+      const uint64_t first = u - e.t0, end = first + n;  // units of the whole group
+      e.first = 1u;
+      // tokens of the group's rows, whose mask bytes decide which tiles are needed
+      const uint32_t tok0 = e.qt * kRows / p.group, tok1 = (min(p.rows, (e.qt + 1u) * kRows) - 1u) / p.group + 1u;
+      uint32_t known = 0xFFFFFFFFu;  // block whose visibility is known (blocks of at least a tile), and it
+      bool known_seen = false;
+      auto seen = [&](uint32_t tile) {
+        const uint32_t s0 = tile * kStates, s1 = min(s0 + kStates, len);
+        if (s0 >= s1) return false;
+        if (p.mask == nullptr) return true;
+        const uint32_t b0 = s0 / p.block_len, b1 = (s1 - 1u) / p.block_len;
+        const uint8_t* m = p.mask + (size_t)b * p.n_tokens * p.n_blocks;
+        if (p.block_len >= kStates) {  // at most two blocks: lanes over the tokens
+          for (uint32_t blk = b0; blk <= b1; ++blk) {
+            if (blk != known) {
+              bool any = false;
+              for (uint32_t t = tok0 + lane; t < tok1; t += 32u) any = any || __ldg(m + (size_t)t * p.n_blocks + blk) != 0;
+              known_seen = __any_sync(kFull, any);
+              known = blk;
+            }
+            if (known_seen) return true;
+          }
+          return false;
+        }
+        for (uint32_t t = tok0; t < tok1; ++t) {  // many blocks: lanes over the blocks
+          bool any = false;
+          for (uint32_t blk = b0 + lane; blk <= b1; blk += 32u) any = any || __ldg(m + (size_t)t * p.n_blocks + blk) != 0;
+          if (__any_sync(kFull, any)) return true;
+        }
+        return false;
+      };
+      for (uint32_t t = e.t0; t < e.t1 && ok; ++t) {
+        if (!seen(t)) continue;
+        e.kind = kTile;
+        e.tile = t;
+        announce(e);
+        if (ok) load(&k_map, e);
+        if (ok) load(&v_map, e);
+        e.first = 0u;
+      }
+      if (!ok) break;
+      e.kind = kEnd;
+      const bool whole = first >= u0 && end <= u1;
+      e.c0 = (uint32_t)(((first + 1u) * ctas - 1u) / total);
+      e.parts = whole ? 1u : (uint32_t)((end * ctas - 1u) / total) - e.c0 + 1u;
+      announce(e);
+      u += e.t1 - e.t0;
+      if (u - before == (uint64_t)n * groups && u < u1) {
+        before = u;
+        len = states_of(p, ++b);
+        n = units_of(len);
+      }
+    }
+    if (ok) {
+      Entry e{};
+      e.kind = kStop;
+      announce(e);
+    }
+  } else if (warp == kMmaWarp) {
+    // ---- products -------------------------------------------------------------------------------------
+    uint32_t st = 0, st_round = 0;  // stage of the next K
+    bool have = false, accumulate = false;
+    uint32_t v_st = 0, v_round = 0, v_valid = kStates, halves = 2;
+    uint32_t p_phase[2] = {0, 0}, q_phase[2] = {0, 0};
+    const uint32_t idesc_qk = umma_idesc(128, 128), idesc_pv = umma_idesc(128, D) | kIdescNMajorB;
+    auto qk = [&](uint32_t w, uint32_t k_tile) {
+      if (lane == 0) {
+        const uint32_t q_tile = smem0 + w * L::kQHalf;
+#pragma unroll
+        for (uint32_t kk = 0; kk < D / 16; ++kk) {
+          const uint32_t off = (kk / 4u) * (128u * 128u) + (kk % 4u) * 32u;
+          umma_bf16(tmem + w * kStates, umma_desc(q_tile + off), umma_desc(k_tile + off), idesc_qk, kk != 0u);
+        }
+        umma_commit(bar(L::kBarSFull, w));
+      }
+      __syncwarp();
+    };
+    auto pv = [&](uint32_t w) {
+      wait(bar(L::kBarPFull, w), p_phase[w]);
+      p_phase[w] ^= 1u;
+      if (!ok) return;
+      tmem_fence_after();
+      if (lane == 0) {
+        const uint32_t v_tile = smem0 + L::kOffKv + v_st * L::kStageBytes;
+#pragma unroll
+        for (uint32_t kk = 0; kk < kStates / 16; ++kk)
+          umma_bf16_ts(tmem + 2 * kStates + w * D, tmem + w * kStates + kk * 8u, umma_desc_n_major(v_tile + kk * 2048u), idesc_pv,
+                       accumulate || kk != 0u);
+        if (w + 1u == halves) umma_commit(bar(L::kBarKvEmpty, v_st));
+      }
+      __syncwarp();
+    };
+    auto wait_v = [&]() {
+      wait(bar(L::kBarKvFull, v_st), v_round & 1u);
+      if (!ok || v_valid >= kStates) return;
+      // past the sequence's last state memory may hold anything, and 0 x NaN is NaN
+      constexpr uint32_t kChunks = D / 8;
+      uint8_t* tile = smem + L::kOffKv + v_st * L::kStageBytes;
+      for (uint32_t i = lane; i < (kStates - v_valid) * kChunks; i += 32u) {
+        const uint32_t r = v_valid + i / kChunks, c = i % kChunks;
+        *reinterpret_cast<uint4*>(tile + (c / 8u) * (kStates * 128u) + r * 128u + (c % 8u) * 16u) = make_uint4(0, 0, 0, 0);
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+    };
+    auto bump = [&]() {
+      if (++st == L::kStages) {
+        st = 0;
+        ++st_round;
+      }
+    };
+    Entry e;
+    while (ok) {
+      take(e);
+      if (!ok || e.kind == kStop) break;
+      if (have) wait_v();
+      if (!ok) break;
+      if (e.kind == kTile) {
+        if (e.first) halves = min(p.rows - e.qt * kRows, kRows) > kHalf ? 2u : 1u;
+        const uint32_t k_st = st;
+        wait(bar(L::kBarKvFull, k_st), st_round & 1u);
+        bump();
+        for (uint32_t w = 0; w < halves && ok; ++w) {
+          if (have) pv(w);
+          if (e.first) {
+            wait(bar(L::kBarQFull, w), q_phase[w]);
+            q_phase[w] ^= 1u;
+          }
+          if (ok) qk(w, smem0 + L::kOffKv + k_st * L::kStageBytes);
+        }
+        if (!ok) break;
+        if (lane == 0) umma_commit(bar(L::kBarKvEmpty, k_st));
+        __syncwarp();
+        accumulate = have;
+        have = true;
+        v_st = st;
+        v_round = st_round;
+        v_valid = min(kStates, e.len - e.tile * kStates);
+        bump();
+      } else if (have) {
+        for (uint32_t w = 0; w < halves && ok; ++w) {
+          pv(w);
+          if (ok && lane == 0) umma_commit(bar(L::kBarODone, w));
+          __syncwarp();
+        }
+        have = false;
+      }
+    }
+  }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
+    // ---- softmax: a thread a row ------------------------------------------------------------------------
+    const uint32_t w = warp >> 2, row_in = threadIdx.x & 127u;
+    const uint32_t lane_field = (warp & 3u) << 21;  // 32 lanes of tensor memory to a warp
+    const uint32_t s_addr = tmem + lane_field + w * kStates, o_addr = tmem + lane_field + 2 * kStates + w * D;
+    const float c = p.scale_log2;
+    uint32_t s_phase = 0, o_phase = 0;
+    float m = -INFINITY, l = 0.f;
+    bool any_tile = false, q_ready = false;
+    uint32_t row = 0, tok = 0;
+    bool live = false, half_live = false;
+
+    auto place = [&](const Entry& e) {  // this thread's row in the entry's group
+      row = e.qt * kRows + w * kHalf + row_in;
+      live = row < p.rows;
+      half_live = e.qt * kRows + w * kHalf < p.rows;
+      tok = live ? row / p.group : 0u;
+    };
+    auto q_row = [&](const Entry& e) {
+      return p.q + (int64_t)e.b * p.q_batch_stride + (int64_t)tok * p.q_token_stride + (size_t)(e.kvh * p.group + row % p.group) * D;
+    };
+    auto load_q = [&](const Entry& e) {
+      if (!half_live) return;
+      const uint4* src = reinterpret_cast<const uint4*>(q_row(e));
+      uint8_t* dst = smem + w * L::kQHalf + row_in * 128u;
+      uint4 v[D / 8];
+#pragma unroll
+      for (uint32_t i = 0; i < D / 8; ++i) v[i] = live ? __ldg(src + i) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (uint32_t i = 0; i < D / 8; ++i) *reinterpret_cast<uint4*>(dst + (i / 8u) * (kHalf * 128u) + (((i % 8u) ^ (row_in & 7u)) << 4)) = v[i];
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(L::kBarQFull, w));
+    };
+    uint32_t met = 0;
+    auto meet = [&]() {  // the eight softmax warps (a bounded wait, as every other)
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(L::kBarJoin, 0));
+      wait(bar(L::kBarJoin, 0), met & 1u);
+      ++met;
+    };
+    // bit i: this row sees state s0 + i
+    auto visible = [&](const Entry& e, uint32_t (&bits)[4]) {
+      const uint32_t s0 = e.tile * kStates, s1 = min(s0 + kStates, e.len);
+      if (p.mask == nullptr) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bits[i] = low_bits((int)(s1 - s0) - 32 * i);
+        return;
+      }
+      bits[0] = bits[1] = bits[2] = bits[3] = 0u;
+      const uint8_t* mr = p.mask + ((size_t)e.b * p.n_tokens + tok) * p.n_blocks;
+      for (uint32_t blk = s0 / p.block_len; blk <= (s1 - 1u) / p.block_len; ++blk) {
+        const uint64_t from = (uint64_t)blk * p.block_len;
+        const int lo = from > s0 ? (int)(from - s0) : 0, hi = (int)min((uint64_t)s1 - s0, from + p.block_len - s0);
+        if (__ldg(mr + blk) == 0) continue;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bits[i] |= low_bits(hi - 32 * i) & ~low_bits(lo - 32 * i);
+      }
+    };
+
+    Entry e;
+    bool pending = false;  // e holds an entry that was taken early
+    while (ok) {
+      if (!pending) take(e);
+      pending = false;
+      if (!ok || e.kind == kStop) break;
+      if (e.kind == kTile) {
+        if (e.first) {
+          place(e);
+          if (!q_ready) load_q(e);
+          q_ready = false;
+          m = -INFINITY;
+          l = 0.f;
+          any_tile = true;
+        }
+        if (!half_live) continue;
+        uint32_t bits[4];
+        visible(e, bits);
+        const bool partial = __any_sync(kFull, (bits[0] & bits[1] & bits[2] & bits[3]) != 0xFFFFFFFFu);
+        wait(bar(L::kBarSFull, w), s_phase);
+        s_phase ^= 1u;
+        if (!ok) break;
+        tmem_fence_after();
+        uint32_t s[128];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) TMEM_LD32(s + 32 * i, s_addr + 32u * i);
+        tmem_wait_ld();
+        if (partial) {
+#pragma unroll
+          for (int i = 0; i < 128; ++i) s[i] = (bits[i / 32] >> (i % 32)) & 1u ? s[i] : 0xFF800000u;
+        }
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int i = 0; i < 128; i += 4) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], __uint_as_float(s[i + k]));
+        }
+        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
+        const bool grow = top > m + kRescale;
+        if (__any_sync(kFull, grow)) {
+          const float mn = fmaxf(m, top);
+          const float f = mn == -INFINITY ? 1.f : exp2_fast(m - mn);
+          m = mn;
+          l *= f;
+          if (!e.first) {  // these scores were committed after the products with V before them: the output is complete
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+              uint32_t o[16];
+              TMEM_LD16(o, o_addr + 16u * i);
+              tmem_wait_ld();
+#pragma unroll
+              for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+              TMEM_ST16(o_addr + 16u * i, o);
+            }
+          }
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
+        float ls[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t pk[32];
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            const float a = exp2_fast(fmaf(__uint_as_float(s[64 * h + 2 * i]), c, -ref));
+            const float b = exp2_fast(fmaf(__uint_as_float(s[64 * h + 2 * i + 1]), c, -ref));
+            ls[(2 * i) & 3] += a;
+            ls[(2 * i + 1) & 3] += b;
+            pk[i] = pack_bf16(a, b);
+          }
+          TMEM_ST32(s_addr + 32u * h, pk);
+        }
+        l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
+        tmem_wait_st();
+        tmem_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(L::kBarPFull, w));
+        continue;
+      }
+      // ---- end of the group, or of this CTA's part: the next group's queries first, they are waited for ------
+      const Entry g = e;
+      const bool had = any_tile;
+      if (!had) {
+        place(g);
+        m = -INFINITY;
+        l = 0.f;
+      }
+      any_tile = false;
+      const uint32_t g_row = row, g_tok = tok;
+      const bool g_live = live, g_half = half_live;
+      take(e);
+      pending = true;
+      if (!ok) break;
+      if (e.kind == kTile) {
+        place(e);
+        load_q(e);
+        q_ready = true;
+        row = g_row, tok = g_tok, live = g_live, half_live = g_half;
+      }
+      const bool real = had && g_half;  // there is an output in tensor memory
+      if (real) {
+        wait(bar(L::kBarODone, w), o_phase);
+        o_phase ^= 1u;
+        if (!ok) break;
+        tmem_fence_after();
+      }
+      const size_t at = ((size_t)g.b * p.n_tokens + tok) * p.n_q_heads + g.kvh * p.group + row % p.group;
+      auto part = [&](uint32_t i) { return p.ws.parts + (size_t)(2u * (g.c0 + i) + (i == 0u ? 1u : 0u)) * kCrossPartFloats; };
+      const uint32_t slot = threadIdx.x;  // 0 .. 255
+      const bool whole = g.parts == 1u;
+      float* const mine = part(blockIdx.x - g.c0);
+      auto write = [&](int i, const uint32_t (&o)[32]) {  // columns 32 i .. 32 i + 31 of a finished row
+        if (!live) return;
+        const float inv = 1.0f / l;
+#pragma unroll
+        for (int k = 0; k < 32; k += 8) {
+          float f[8];
+#pragma unroll
+          for (int x = 0; x < 8; ++x) f[x] = l == 0.f ? 0.f : __uint_as_float(o[k + x]) * inv;
+          store8<TQ_TYPE_BF16>(p.out, at * D + 32 * i + k, f);
+        }
+        if (i == 0 && p.lse) p.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+      };
+      bool nan = false;
+#pragma unroll 1
+      for (int i = 0; i < D / 32; ++i) {
+        uint32_t o[32];
+        if (real) {
+          TMEM_LD32(o, o_addr + 32u * i);
+          tmem_wait_ld();
+        } else {
+#pragma unroll
+          for (int k = 0; k < 32; ++k) o[k] = 0u;
+        }
+#pragma unroll
+        for (int k = 0; k < 32; ++k) nan = nan || __uint_as_float(o[k]) != __uint_as_float(o[k]);
+        if (whole) {
+          write(i, o);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) reinterpret_cast<uint4*>(mine)[(8 * i + k) * kRows + slot] = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+        }
+      }
+      tmem_fence_before();
+      if (p.mask != nullptr) {  // rows that a state they do not see has spoiled: again, a warp a row, D / 32 columns a lane
+        uint32_t again = __ballot_sync(kFull, live && nan && l < INFINITY);
+#pragma unroll 1
+        while (again) {
+          const int src = __ffs(again) - 1;
+          again &= again - 1u;
+          constexpr int kPer = D / 32;
+          const uint32_t rr = __shfl_sync(kFull, row, src), rt = __shfl_sync(kFull, tok, src), rs = __shfl_sync(kFull, slot, src);
+          const float rm = __shfl_sync(kFull, m, src), rl = __shfl_sync(kFull, l, src);
+          const __nv_bfloat16* q = p.q + (int64_t)g.b * p.q_batch_stride + (int64_t)rt * p.q_token_stride + (size_t)(g.kvh * p.group + rr % p.group) * D + lane * kPer;
+          const uint8_t* mr = p.mask + ((size_t)g.b * p.n_tokens + rt) * p.n_blocks;
+          float acc[kPer], qv[kPer];
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) {
+            acc[i] = 0.f;
+            qv[i] = __bfloat162float(q[i]);
+          }
+          const int64_t base = (int64_t)g.b * p.batch_stride + (int64_t)g.kvh * p.head_stride + lane * kPer;
+          const uint32_t s1 = min(g.t1 * kStates, g.len);
+#pragma unroll 1
+          for (uint32_t s = g.t0 * kStates; s < s1; ++s) {
+            if (__ldg(mr + s / p.block_len) == 0) continue;
+            const int64_t from = base + (int64_t)s * p.state_stride;
+            float x = 0.f;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) x += qv[i] * __bfloat162float(p.k[from + i]);
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(kFull, x, d);
+            const float pr = exp2_fast(fmaf(x, c, -rm));
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) acc[i] += pr * __bfloat162float(p.v[from + i]);
+          }
+          const size_t ra = ((size_t)g.b * p.n_tokens + rt) * p.n_q_heads + g.kvh * p.group + rr % p.group;
+          __syncwarp();  // after the row's own thread has written it
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) {
+            const uint32_t col = lane * kPer + i;
+            if (whole)
+              p.out[ra * D + col] = __float2bfloat16_rn(rl == 0.f ? 0.f : acc[i] / rl);
+            else
+              mine[(col / 4u * kRows + rs) * 4u + col % 4u] = acc[i];
+          }
+        }
+      }
+      if (whole) continue;
+      mine[kRows * 128 + slot] = m;
+      mine[kRows * 129 + slot] = l;
+      __threadfence();
+      meet();
+      if (!ok) break;
+      // atomicInc wraps to 0 with the last part, which is the state the next call needs
+      if (threadIdx.x == 0) *join_flag = atomicInc(p.ws.counters + g.c0, g.parts - 1u) == g.parts - 1u;
+      meet();
+      if (!ok) break;
+      if (*join_flag) {
+        __threadfence();
+        float M = -INFINITY;
+        for (uint32_t i = 0; i < g.parts; ++i) M = fmaxf(M, __ldcg(part(i) + kRows * 128 + slot));
+        const float ref = M == -INFINITY ? 0.f : M;
+        l = 0.f;
+        for (uint32_t i = 0; i < g.parts; ++i) l += exp2_fast(__ldcg(part(i) + kRows * 128 + slot) - ref) * __ldcg(part(i) + kRows * 129 + slot);
+        m = M;
+#pragma unroll 1
+        for (int i = 0; i < D / 32; ++i) {
+          uint32_t o[32];
+#pragma unroll
+          for (int k = 0; k < 32; ++k) o[k] = 0u;
+#pragma unroll 1
+          for (uint32_t x = 0; x < g.parts; ++x) {
+            const float f = exp2_fast(__ldcg(part(x) + kRows * 128 + slot) - ref);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const float4 y = __ldcg(reinterpret_cast<const float4*>(part(x)) + (8 * i + k) * kRows + slot);
+              o[4 * k] = __float_as_uint(__uint_as_float(o[4 * k]) + f * y.x);
+              o[4 * k + 1] = __float_as_uint(__uint_as_float(o[4 * k + 1]) + f * y.y);
+              o[4 * k + 2] = __float_as_uint(__uint_as_float(o[4 * k + 2]) + f * y.z);
+              o[4 * k + 3] = __float_as_uint(__uint_as_float(o[4 * k + 3]) + f * y.w);
+            }
+          }
+          write(i, o);
+        }
+      }
+      meet();  // the flag has been read
+    }
+  }
+
+  if (!ok) {
+    *dead = 1u;
+    if (lane == 0) atomicOr(p.ws.status, TQ_STATUS_WAIT_EXPIRED);
+    // copies that are still in flight target this CTA's shared memory: give them time to land
+    for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+  }
+  tmem_fence_before();
+  __syncthreads();
+  if (warp == kMmaWarp) {
+    tmem_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+  }
+}
+
+// The tensor map of K or V: (column, state, head, sequence), boxes of 64 columns x 128 states, 128-byte swizzle.
+// A dimension of stride 0 is one that every index shares.
+bool encode(CUtensorMap* map, const void* base, const tq_encoder_kv* kv) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t row = kv->head_dim * 2u;
+  const cuuint64_t dims[4] = {kv->head_dim, kv->n_states, kv->head_stride ? kv->n_kv_heads : 1u, kv->batch_stride ? kv->n_seqs : 1u};
+  const cuuint64_t strides[3] = {kv->state_stride ? (cuuint64_t)kv->state_stride * 2u : row, kv->head_stride ? (cuuint64_t)kv->head_stride * 2u : row,
+                                 kv->batch_stride ? (cuuint64_t)kv->batch_stride * 2u : row};
+  const cuuint32_t box[4] = {64u, kStates, 1u, 1u}, step[4] = {1u, 1u, 1u, 1u};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D>
+int launch(const CrossParams& p, const CUtensorMap& k_map, const CUtensorMap& v_map, cudaStream_t st) {
+  auto kern = cross_attention_kernel<D>;
+  constexpr size_t smem = CrossSmem<D>::kTotal + 1024;
+  const char* what = "cross attention (tensor core) launch";
+  if (int rc = tq_ensure_dynamic_smem((const void*)kern, smem, what)) return rc;
+  static const int regs = [&] {
+    cudaFuncAttributes a{};
+    return cudaFuncGetAttributes(&a, (const void*)kern) == cudaSuccess ? a.numRegs : 0;
+  }();
+  if (256 * kSoftRegs + 128 * kOtherRegs > kCrossThreads * regs) return tq_cuda_status((int)cudaErrorInvalidConfiguration, what);
+  const uint32_t grid = min((uint32_t)sm_count(), kAttnMaxCtas);
+  return launch_pdl(kern, dim3(grid), kCrossThreads, smem, st, what, p, k_map, v_map);
+}
+
+}  // namespace
+
+uint64_t tq_cross_workspace_bytes() { return (uint64_t)min((uint32_t)sm_count(), kAttnMaxCtas) * 2u * kCrossPartFloats * sizeof(float); }
+
+int tq_cross_launch(const tq_encoder_kv* kv, const void* d_q, int64_t q_batch_stride, int64_t q_token_stride, uint32_t n_tokens,
+                    uint32_t n_q_heads, const int32_t* d_kv_len, const uint8_t* d_mask, uint32_t block_len, uint32_t n_blocks,
+                    float scale_log2, void* d_out, float* d_lse, const tq_attn_ws& ws, void* cuda_stream, bool* served) {
+  CUtensorMap k_map, v_map;
+  *served = kv->n_states != 0 && (kv->state_stride != 0 || kv->n_states == 1) && encode(&k_map, kv->d_k, kv) && encode(&v_map, kv->d_v, kv);
+  if (!*served) return TQ_OK;
+  CrossParams p{};
+  p.k = (const __nv_bfloat16*)kv->d_k;
+  p.v = (const __nv_bfloat16*)kv->d_v;
+  p.batch_stride = kv->batch_stride;
+  p.state_stride = kv->state_stride;
+  p.head_stride = kv->head_stride;
+  p.q = (const __nv_bfloat16*)d_q;
+  p.q_batch_stride = q_batch_stride;
+  p.q_token_stride = q_token_stride;
+  p.out = (__nv_bfloat16*)d_out;
+  p.lse = d_lse;
+  p.kv_len = d_kv_len;
+  p.mask = d_mask;
+  p.n_states = kv->n_states;
+  p.block_len = block_len;
+  p.n_blocks = n_blocks;
+  p.n_seqs = kv->n_seqs;
+  p.n_tokens = n_tokens;
+  p.n_q_heads = n_q_heads;
+  p.n_kv_heads = kv->n_kv_heads;
+  p.group = n_q_heads / kv->n_kv_heads;
+  p.rows = n_tokens * p.group;
+  p.row_tiles = (p.rows + kRows - 1u) / kRows;
+  p.scale_log2 = scale_log2;
+  p.ws = ws;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  return kv->head_dim == 64 ? launch<64>(p, k_map, v_map, st) : launch<128>(p, k_map, v_map, st);
+}

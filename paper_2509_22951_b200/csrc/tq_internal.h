@@ -246,3 +246,10 @@ struct tq_attn_ws {
 constexpr uint64_t kAttnWsHeader = kAttnMaxCtas * 4 + 256;
 // nullptr counters: d_ws is not usable as a workspace of ws_bytes bytes
 tq_attn_ws tq_attn_ws_plan(void* d_ws, uint64_t ws_bytes);
+
+// The tensor-core form of tq_cross_attention (tq_cross.cu): *served is false, and nothing was launched, if the states
+// cannot be described by a tensor map (strides of 2^40 bytes and more, no states).
+uint64_t tq_cross_workspace_bytes();
+int tq_cross_launch(const tq_encoder_kv* kv, const void* d_q, int64_t q_batch_stride, int64_t q_token_stride, uint32_t n_tokens,
+                    uint32_t n_q_heads, const int32_t* d_kv_len, const uint8_t* d_mask, uint32_t block_len, uint32_t n_blocks,
+                    float scale_log2, void* d_out, float* d_lse, const tq_attn_ws& ws, void* cuda_stream, bool* served);

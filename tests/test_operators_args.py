@@ -86,21 +86,22 @@ def test_no_cache():
     assert lib.tq_paged_attention(None, A, 256, 2, 4, A, 8, A, 1.0, A, None, A, _ws_bytes(), None) == -1
 
 
-PAGED = dict(q=A, qs=256, B=2, H=4, table=A, max_pages=8, lens=A, out=A, lse=None, ws=A, short=0)
+PAGED = dict(scale=0.125, q=A, qs=256, B=2, H=4, table=A, max_pages=8, lens=A, out=A, lse=None, ws=A, short=0)
 
 
 @pytest.mark.parametrize("change,status", [
     (dict(q=None), -1), (dict(q=A + 8), -1), (dict(qs=4), -1), (dict(H=0), -1), (dict(H=5), -1), (dict(table=None), -1), (dict(max_pages=0), -1),
     (dict(lens=None), -1), (dict(out=A + 2), -1), (dict(lse=A + 1), -1), (dict(ws=None), -1), (dict(ws=A + 16), -1), (dict(short=1), -3), (dict(B=0), 0),
+    (dict(scale=0.0), -1), (dict(scale=-1.0), -1), (dict(scale=float("nan")), -1), (dict(scale=float("inf")), -1),
 ])
 def test_paged_attention(change, status):
     a, c = dict(PAGED, **change), _cache()
-    assert lib.tq_paged_attention(C.byref(c), a["q"], a["qs"], a["B"], a["H"], a["table"], a["max_pages"], a["lens"], 0.125, a["out"], a["lse"], a["ws"],
+    assert lib.tq_paged_attention(C.byref(c), a["q"], a["qs"], a["B"], a["H"], a["table"], a["max_pages"], a["lens"], a["scale"], a["out"], a["lse"], a["ws"],
                                   _ws_bytes() - a["short"], None) == status
 
 
 KV = dict(d_k=A, d_v=A, n_seqs=2, n_states=100, n_kv_heads=2, head_dim=64, batch_stride=12800, state_stride=128, head_stride=64)
-CROSS = dict(q=A, qb=1024, qt=256, T=4, H=4, kv_len=None, mask=None, block=0, out=A, lse=None, ws=A, short=0)
+CROSS = dict(scale=0.125, q=A, qb=1024, qt=256, T=4, H=4, kv_len=None, mask=None, block=0, out=A, lse=None, ws=A, short=0)
 
 
 @pytest.mark.parametrize("kv,change,status", [
@@ -109,10 +110,11 @@ CROSS = dict(q=A, qb=1024, qt=256, T=4, H=4, kv_len=None, mask=None, block=0, ou
     ({}, dict(q=None), -1), ({}, dict(q=A + 8), -1), ({}, dict(qb=4), -1), ({}, dict(qt=4), -1), ({}, dict(H=3), -1), ({}, dict(H=0), -1),
     ({}, dict(kv_len=A + 1), -1), ({}, dict(mask=A), -1), ({}, dict(out=None), -1), ({}, dict(lse=A + 2), -1), ({}, dict(ws=None), -1),
     ({}, dict(short=1), -3), ({}, dict(T=0), 0), ({}, dict(T=1 << 30, H=4), -4),
+    ({}, dict(scale=0.0), -1), ({}, dict(scale=float("nan")), -1),
 ])
 def test_cross_attention(kv, change, status):
     a, e = dict(CROSS, **change), tq._EncoderKv(**dict(KV, **kv))
-    assert lib.tq_cross_attention(C.byref(e), a["q"], a["qb"], a["qt"], a["T"], a["H"], a["kv_len"], a["mask"], a["block"], 0.125, a["out"], a["lse"],
+    assert lib.tq_cross_attention(C.byref(e), a["q"], a["qb"], a["qt"], a["T"], a["H"], a["kv_len"], a["mask"], a["block"], a["scale"], a["out"], a["lse"],
                                   a["ws"], _ws_bytes() - a["short"], None) == status
 
 
