@@ -7,6 +7,7 @@ built with nvcc) importing this module raises.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 from dataclasses import dataclass
 
 import numpy as np
@@ -698,32 +699,19 @@ def tq_device_status(m: DeviceMatrix, stream=None) -> int:
 
 # ------------------------------------------------------------------------------ between the linear layers
 _TYPES = {torch.bfloat16: TQ_TYPE_BF16, torch.float32: TQ_TYPE_F32}
+_raw_stream = torch._C._cuda_getCurrentRawStream
+_current_device = torch._C._cuda_getDevice
 
 
-class _On:
-    """Device and stream of a call: a call on a stream that is not the current one gets its results from that stream's memory."""
-
-    __slots__ = ("ptr", "ctx")
-
-    def __init__(self, device: torch.device, stream):
-        index = device.index
-        if stream is None and torch.cuda.current_device() == index:  # the usual case, without a context manager
-            self.ptr, self.ctx = torch._C._cuda_getCurrentRawStream(index), None
-        elif stream is None:
-            self.ctx = torch.cuda.device(index)
-            self.ptr = torch.cuda.current_stream(index).cuda_stream
-        else:
-            self.ctx = torch.cuda.stream(stream)
-            self.ptr = stream.cuda_stream
-
-    def __enter__(self):
-        if self.ctx is not None:
-            self.ctx.__enter__()
-        return self.ptr
-
-    def __exit__(self, *exc):
-        if self.ctx is not None:
-            self.ctx.__exit__(*exc)
+# A decode step makes dozens of these calls of a few microseconds each, so their checks use the cheap tensor attributes
+# (get_device() is -1 for a CPU tensor) and build no objects in the usual case.
+def _elsewhere(device: int, stream):
+    """None if the call is for the current device and its current stream; else a context in which it is, so that the call's results
+    come from that stream's memory."""
+    if stream is None:
+        return None if _current_device() == device else torch.cuda.device(device)
+    assert stream.device.index == device
+    return torch.cuda.stream(stream)
 
 
 def _strides(x: torch.Tensor):
@@ -731,46 +719,58 @@ def _strides(x: torch.Tensor):
     return tuple(st if n > 1 else 0 for n, st in zip(x.shape, x.stride()))
 
 
-def _norm_args(h, weight, delta, h_out):
-    assert h.is_cuda and h.dtype in _TYPES and h.dim() == 2 and (h.stride(1) == 1 or h.shape[1] == 1)
-    rows, cols = h.shape
-    assert weight.is_cuda and weight.dtype == torch.float32 and weight.is_contiguous() and weight.numel() == cols
+def _norm_args(h, weight, delta, h_out, device):
+    rows, cols = shape = h.shape
+    stride = h.stride()
+    assert device >= 0 and h.dtype in _TYPES and (stride[1] == 1 or cols == 1)
+    assert weight.get_device() == device and weight.dtype == torch.float32 and weight.is_contiguous() and weight.numel() == cols
     dp, dt, ds = None, 0, 0
     if delta is not None:
-        assert delta.is_cuda and delta.dtype in _TYPES and delta.shape == h.shape and (delta.stride(1) == 1 or cols == 1)
-        dp, dt, ds = delta.data_ptr(), _TYPES[delta.dtype], delta.stride(0)
+        dst = delta.stride()
+        assert delta.get_device() == device and delta.shape == shape and (dst[1] == 1 or cols == 1)
+        dp, dt, ds = delta.data_ptr(), _TYPES[delta.dtype], dst[0]
         if h_out is None:
             h_out = h
-    if h_out is not None:
-        assert h_out.is_cuda and h_out.dtype == h.dtype and h_out.shape == h.shape and _strides(h_out) == _strides(h)
-    return rows, cols, (h.data_ptr(), _TYPES[h.dtype], h.stride(0), dp, dt, ds, weight.data_ptr()), None if h_out is None else h_out.data_ptr()
+    if h_out is not None and h_out is not h:
+        assert h_out.get_device() == device and h_out.dtype == h.dtype and h_out.shape == shape
+        assert h_out.stride() == stride or _strides(h_out) == _strides(h)
+    return rows, cols, (h.data_ptr(), _TYPES[h.dtype], stride[0], dp, dt, ds, weight.data_ptr()), None if h_out is None else h_out.data_ptr()
 
 
 def tq_rmsnorm(h: torch.Tensor, weight: torch.Tensor, delta: torch.Tensor | None = None, eps: float = 1e-5,
                out: torch.Tensor | None = None, h_out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """h: CUDA bf16 / fp32 [rows][cols] (rows may be strided); delta: bf16 / fp32 of the same shape; weight: fp32 [cols].
     With a delta the sum h + delta goes to h_out (a tensor like h), or to h itself when h_out is None.  -> bf16 [rows][cols]."""
-    rows, cols, args, h_out = _norm_args(h, weight, delta, h_out)
-    with _On(h.device, stream) as st:
-        if out is None:
-            out = torch.empty((rows, cols), dtype=torch.bfloat16, device=h.device)
-        assert out.is_cuda and out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() == rows * cols
-        _check(_lib.tq_rmsnorm(*args, eps, rows, cols, h_out, out.data_ptr(), st), "tq_rmsnorm")
+    device = h.get_device()
+    ctx = _elsewhere(device, stream)
+    if ctx is not None:
+        with ctx:
+            return tq_rmsnorm(h, weight, delta, eps, out, h_out)
+    rows, cols, args, h_out = _norm_args(h, weight, delta, h_out, device)
+    if out is None:
+        out = torch.empty((rows, cols), dtype=torch.bfloat16, device=h.device)
+    else:
+        assert out.get_device() == device and out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() == rows * cols
+    _check(_lib.tq_rmsnorm(*args, eps, rows, cols, h_out, out.data_ptr(), _raw_stream(device)), "tq_rmsnorm")
     return out
 
 
 def tq_rmsnorm_q8(h: torch.Tensor, weight: torch.Tensor, delta: torch.Tensor | None = None, eps: float = 1e-5,
                   q: torch.Tensor | None = None, scale: torch.Tensor | None = None, h_out: torch.Tensor | None = None, stream=None):
     """tq_rmsnorm with the result in 8 bits: -> (int8 [rows][cols], fp32 [rows] scales)."""
-    rows, cols, args, h_out = _norm_args(h, weight, delta, h_out)
-    with _On(h.device, stream) as st:
-        if q is None:
-            q = torch.empty((rows, cols), dtype=torch.int8, device=h.device)
-        if scale is None:
-            scale = torch.empty(rows, dtype=torch.float32, device=h.device)
-        assert q.is_cuda and q.dtype == torch.int8 and q.is_contiguous() and q.numel() == rows * cols
-        assert scale.is_cuda and scale.dtype == torch.float32 and scale.is_contiguous() and scale.numel() == rows
-        _check(_lib.tq_rmsnorm_q8(*args, eps, rows, cols, h_out, q.data_ptr(), scale.data_ptr(), st), "tq_rmsnorm_q8")
+    device = h.get_device()
+    ctx = _elsewhere(device, stream)
+    if ctx is not None:
+        with ctx:
+            return tq_rmsnorm_q8(h, weight, delta, eps, q, scale, h_out)
+    rows, cols, args, h_out = _norm_args(h, weight, delta, h_out, device)
+    if q is None:
+        q = torch.empty((rows, cols), dtype=torch.int8, device=h.device)
+    if scale is None:
+        scale = torch.empty(rows, dtype=torch.float32, device=h.device)
+    assert q.get_device() == device and q.dtype == torch.int8 and q.is_contiguous() and q.numel() == rows * cols
+    assert scale.get_device() == device and scale.dtype == torch.float32 and scale.is_contiguous() and scale.numel() == rows
+    _check(_lib.tq_rmsnorm_q8(*args, eps, rows, cols, h_out, q.data_ptr(), scale.data_ptr(), _raw_stream(device)), "tq_rmsnorm_q8")
     return q, scale
 
 
@@ -782,6 +782,7 @@ class KvCache:
         assert v.device == k.device and v.dtype == k.dtype and v.shape == k.shape and _strides(v) == _strides(k)
         self.k, self.v = k, v
         self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
+        self.device = k.get_device()
         self.status = torch.zeros(1, dtype=torch.int32, device=k.device)
         self._c = _KvCache(k.data_ptr(), v.data_ptr(), self.n_pages, self.page_size, self.n_kv_heads, self.head_dim,
                            *_strides(k)[:3], self.status.data_ptr())
@@ -801,11 +802,20 @@ def tq_kv_cache_status(cache: KvCache) -> int:
     return st
 
 
-def _heads(x: torch.Tensor, n: int, dim: int):
+def _heads(x: torch.Tensor, tokens: int, n: int, dim: int, device: int, dtype) -> int:
     """Token stride of x, [tokens][n * dim] or [tokens][n][dim]."""
-    assert x.dim() in (2, 3) and x.stride(-1) == 1
-    assert (x.shape[1] == n * dim) if x.dim() == 2 else (x.shape[1] == n and x.shape[2] == dim and (n == 1 or x.stride(1) == dim))
-    return x.stride(0)
+    shape, stride = x.shape, x.stride()
+    assert x.get_device() == device and x.dtype == dtype and shape[0] == tokens and stride[-1] == 1
+    if len(shape) == 2:
+        assert shape[1] == n * dim
+    else:
+        assert shape[1:] == (n, dim) and (n == 1 or stride[1] == dim)
+    return stride[0]
+
+
+@functools.lru_cache(maxsize=64)
+def _sections(sections):
+    return (C.c_uint32 * len(sections))(*sections)
 
 
 def tq_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, positions: torch.Tensor,
@@ -814,26 +824,29 @@ def tq_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, table: tor
     """q, k, v: CUDA bf16 or fp32 [tokens][heads * head dim] or [tokens][heads][head dim] (tokens may be strided); table: fp32
     [positions][rot dim], cosines then sines; positions: int32 [axes][tokens] or [tokens]; slots: int32 [tokens], -1 for none;
     sections: pairs of each axis (one axis: all).  -> rotated q, bf16 [tokens][q heads][head dim]; k and v are in the cache."""
-    D, K, T = cache.head_dim, cache.n_kv_heads, q.shape[0]
-    assert q.is_cuda and q.dtype in _TYPES and k.dtype == q.dtype and v.dtype == q.dtype and k.shape[0] == T and v.shape[0] == T
-    assert k.device == q.device and v.device == q.device and cache.k.device == q.device
-    H = q.shape[1] if q.dim() == 3 else q.shape[1] // D
-    qs, ks, vs = _heads(q, H, D), _heads(k, K, D), _heads(v, K, D)
-    assert table.is_cuda and table.dtype == torch.float32 and table.is_contiguous() and table.dim() == 2
-    assert positions.is_cuda and positions.dtype == torch.int32 and positions.is_contiguous() and slots.is_cuda
-    assert slots.dtype == torch.int32 and slots.is_contiguous() and slots.numel() == T
+    device = q.get_device()
+    ctx = _elsewhere(device, stream)
+    if ctx is not None:
+        with ctx:
+            return tq_rope_append(q, k, v, table, positions, slots, cache, sections, interleaved, out)
+    D, K, shape, dtype = cache.head_dim, cache.n_kv_heads, q.shape, q.dtype
+    T, H = shape[0], (shape[1] if len(shape) == 3 else shape[1] // D)
+    assert cache.device == device and dtype in _TYPES
+    qs, ks, vs = _heads(q, T, H, D, device, dtype), _heads(k, T, K, D, device, dtype), _heads(v, T, K, D, device, dtype)
+    n_positions, rot = table.shape
+    assert table.get_device() == device and table.dtype == torch.float32 and table.is_contiguous()
     axes = 1 if positions.dim() == 1 else positions.shape[0]
-    assert positions.numel() == axes * T
-    rot = table.shape[1]
-    sec = (rot // 2,) if sections is None else sections
+    assert positions.get_device() == device and positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == axes * T
+    assert slots.get_device() == device and slots.dtype == torch.int32 and slots.is_contiguous() and slots.numel() == T
+    sec = (rot // 2,) if sections is None else tuple(sections)
     assert len(sec) == axes
-    with _On(q.device, stream) as st:
-        if out is None:
-            out = torch.empty((T, H, D), dtype=torch.bfloat16, device=q.device)
-        assert out.is_cuda and out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() == T * H * D
-        _check(_lib.tq_rope_append(q.data_ptr(), k.data_ptr(), v.data_ptr(), _TYPES[q.dtype], qs, ks, vs, T, H, table.data_ptr(),
-                                   table.shape[0], rot, positions.data_ptr(), (C.c_uint32 * axes)(*sec), axes, int(interleaved),
-                                   slots.data_ptr(), cache._ref, out.data_ptr(), st), "tq_rope_append")
+    if out is None:
+        out = torch.empty((T, H, D), dtype=torch.bfloat16, device=q.device)
+    else:
+        assert out.get_device() == device and out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() == T * H * D
+    _check(_lib.tq_rope_append(q.data_ptr(), k.data_ptr(), v.data_ptr(), _TYPES[dtype], qs, ks, vs, T, H, table.data_ptr(), n_positions,
+                               rot, positions.data_ptr(), _sections(sec), axes, interleaved, slots.data_ptr(), cache._ref,
+                               out.data_ptr(), _raw_stream(device)), "tq_rope_append")
     return out
 
 
@@ -842,33 +855,35 @@ class AttnWorkspace:
 
     def __init__(self, buf: torch.Tensor):
         self.buf = buf
-        self.ptr, self.bytes = buf.data_ptr(), buf.numel()
+        self.device, self.ptr, self.bytes = buf.get_device(), buf.data_ptr(), buf.numel()
 
 
 def tq_attn_workspace(device="cuda", stream=None) -> AttnWorkspace:
-    dev = torch.empty(0, device=device).device
-    need = C.c_uint64()
-    with torch.cuda.device(dev), _On(dev, stream) as st:
+    with torch.cuda.device(device) if stream is None else torch.cuda.stream(stream):
+        need = C.c_uint64()
         _check(_lib.tq_attn_workspace_size(C.byref(need)), "tq_attn_workspace_size")
-        buf = torch.empty(need.value, dtype=torch.uint8, device=dev)
-        _check(_lib.tq_attn_workspace_init(buf.data_ptr(), buf.numel(), st), "tq_attn_workspace_init")
+        buf = torch.empty(need.value, dtype=torch.uint8, device="cuda")
+        _check(_lib.tq_attn_workspace_init(buf.data_ptr(), buf.numel(), _stream_ptr()), "tq_attn_workspace_init")
     return AttnWorkspace(buf)
 
 
 def tq_attn_status(workspace: AttnWorkspace, stream=None) -> int:
     st = C.c_uint32()
-    with _On(workspace.buf.device, stream) as sp:
-        _check(_lib.tq_attn_status(workspace.ptr, sp, C.byref(st)), "tq_attn_status")
+    with torch.cuda.device(workspace.device) if stream is None else torch.cuda.stream(stream):
+        _check(_lib.tq_attn_status(workspace.ptr, _stream_ptr(), C.byref(st)), "tq_attn_status")
     return st.value
 
 
-def _attn_out(shape, device, out, lse):
+def _attn_out(q, out, lse, device):
+    shape = q.shape
     if out is None:
-        out = torch.empty(shape, dtype=torch.bfloat16, device=device)
-    assert out.is_cuda and out.dtype == torch.bfloat16 and out.is_contiguous() and out.shape == shape
-    if lse is not None:
-        assert lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == shape[:-1]
-    return out
+        out = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
+    else:
+        assert out.get_device() == device and out.dtype == torch.bfloat16 and out.is_contiguous() and out.shape == shape
+    if lse is None:
+        return out, None
+    assert lse.get_device() == device and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == shape[:-1]
+    return out, lse.data_ptr()
 
 
 def tq_paged_attention(q: torch.Tensor, cache: KvCache, page_table: torch.Tensor, lens: torch.Tensor, workspace: AttnWorkspace,
@@ -876,18 +891,21 @@ def tq_paged_attention(q: torch.Tensor, cache: KvCache, page_table: torch.Tensor
                        stream=None) -> torch.Tensor:
     """q: CUDA bf16 [sequences][q heads][head dim] (sequences may be strided); page_table: int32 [sequences][max pages]; lens: int32
     [sequences]; scale: 1 / sqrt(head dim) when None; lse: fp32 [sequences][q heads], filled when given.  -> bf16 like q."""
-    D = cache.head_dim
-    assert q.is_cuda and q.dtype == torch.bfloat16 and q.dim() == 3 and q.shape[2] == D and q.stride(2) == 1
-    B, H = q.shape[0], q.shape[1]
-    assert (H == 1 or q.stride(1) == D) and cache.k.device == q.device and workspace.buf.device == q.device
-    assert page_table.is_cuda and page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.is_contiguous()
-    assert lens.is_cuda and lens.dtype == torch.int32 and lens.is_contiguous() and lens.numel() == B and page_table.shape[0] == B
-    with _On(q.device, stream) as st:
-        out = _attn_out((B, H, D), q.device, out, lse)
-        _check(_lib.tq_paged_attention(cache._ref, q.data_ptr(), q.stride(0) if B > 1 else 0, B, H, page_table.data_ptr(), page_table.shape[1],
-                                       lens.data_ptr(), D ** -0.5 if scale is None else scale, out.data_ptr(),
-                                       None if lse is None else lse.data_ptr(), workspace.ptr, workspace.bytes, st),
-               "tq_paged_attention")
+    device = q.get_device()
+    ctx = _elsewhere(device, stream)
+    if ctx is not None:
+        with ctx:
+            return tq_paged_attention(q, cache, page_table, lens, workspace, scale, out, lse)
+    (B, H, D), stride = q.shape, q.stride()
+    assert cache.device == device and workspace.device == device and q.dtype == torch.bfloat16
+    assert D == cache.head_dim and stride[2] == 1 and (H == 1 or stride[1] == D)
+    rows, max_pages = page_table.shape
+    assert page_table.get_device() == device and page_table.dtype == torch.int32 and page_table.is_contiguous() and rows == B
+    assert lens.get_device() == device and lens.dtype == torch.int32 and lens.is_contiguous() and lens.numel() == B
+    out, lse = _attn_out(q, out, lse, device)
+    _check(_lib.tq_paged_attention(cache._ref, q.data_ptr(), stride[0] if B > 1 else 0, B, H, page_table.data_ptr(), max_pages, lens.data_ptr(),
+                                   D ** -0.5 if scale is None else scale, out.data_ptr(), lse, workspace.ptr, workspace.bytes,
+                                   _raw_stream(device)), "tq_paged_attention")
     return out
 
 
@@ -898,22 +916,27 @@ def tq_cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, worksp
     expanded batch has the same states for every sequence); kv_len: int32 [sequences]; mask: uint8 / bool
     [sequences][tokens][ceil(states / block_len)], nonzero where a token sees the block; lse: fp32 [sequences][tokens][q heads],
     filled when given.  -> bf16 [sequences][tokens][q heads][head dim]."""
-    assert q.is_cuda and q.dtype == torch.bfloat16 and q.dim() == 4 and q.stride(3) == 1
-    B, T, H, D = q.shape
-    assert (H == 1 or q.stride(2) == D) and workspace.buf.device == q.device
-    assert k.device == q.device and k.dtype == torch.bfloat16 and k.dim() == 4 and k.stride(3) == 1 and k.shape[0] == B and k.shape[3] == D
-    assert v.device == q.device and v.dtype == torch.bfloat16 and v.shape == k.shape and _strides(v) == _strides(k)
-    S, K = k.shape[1], k.shape[2]
+    device = q.get_device()
+    ctx = _elsewhere(device, stream)
+    if ctx is not None:
+        with ctx:
+            return tq_cross_attention(q, k, v, workspace, kv_len, mask, block_len, scale, out, lse)
+    (B, T, H, D), stride = q.shape, q.stride()
+    assert workspace.device == device and q.dtype == torch.bfloat16 and stride[3] == 1 and (H == 1 or stride[2] == D)
+    n, S, K, dim = k.shape
+    ks = _strides(k)
+    assert k.get_device() == device and k.dtype == torch.bfloat16 and n == B and dim == D and ks[3] == 1
+    assert v.get_device() == device and v.dtype == torch.bfloat16 and v.shape == k.shape and _strides(v) == ks
     if kv_len is not None:
-        assert kv_len.device == q.device and kv_len.dtype == torch.int32 and kv_len.is_contiguous() and kv_len.numel() == B
+        assert kv_len.get_device() == device and kv_len.dtype == torch.int32 and kv_len.is_contiguous() and kv_len.numel() == B
+        kv_len = kv_len.data_ptr()
     if mask is not None:
-        assert mask.device == q.device and mask.dtype in (torch.uint8, torch.bool) and mask.is_contiguous()
+        assert mask.get_device() == device and mask.dtype in (torch.uint8, torch.bool) and mask.is_contiguous()
         assert block_len >= 1 and mask.shape == (B, T, -(-S // block_len))
-    kv = _EncoderKv(k.data_ptr(), v.data_ptr(), B, S, K, D, *_strides(k)[:3])
-    with _On(q.device, stream) as st:
-        out = _attn_out((B, T, H, D), q.device, out, lse)
-        _check(_lib.tq_cross_attention(kv, q.data_ptr(), q.stride(0) if B > 1 else 0, q.stride(1) if T > 1 else 0, T, H, None if kv_len is None else kv_len.data_ptr(),
-                                       None if mask is None else mask.data_ptr(), block_len, D ** -0.5 if scale is None else scale,
-                                       out.data_ptr(), None if lse is None else lse.data_ptr(), workspace.ptr, workspace.bytes, st),
-               "tq_cross_attention")
+        mask = mask.data_ptr()
+    out, lse = _attn_out(q, out, lse, device)
+    _check(_lib.tq_cross_attention(_EncoderKv(k.data_ptr(), v.data_ptr(), B, S, K, D, ks[0], ks[1], ks[2]), q.data_ptr(),
+                                   stride[0] if B > 1 else 0, stride[1] if T > 1 else 0, T, H, kv_len, mask, block_len,
+                                   D ** -0.5 if scale is None else scale, out.data_ptr(), lse, workspace.ptr, workspace.bytes,
+                                   _raw_stream(device)), "tq_cross_attention")
     return out
