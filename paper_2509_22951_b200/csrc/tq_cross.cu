@@ -57,17 +57,16 @@ constexpr uint32_t kEntries = 4;       // announced tiles that may be under way
 constexpr uint32_t kTmemCols = 512;
 constexpr float kRescale = 8.0f;       // log2 of how far p may exceed 1
 
-enum : uint32_t { kTile = 0, kEnd = 1, kStop = 2 };
+// What the loader announces, in the first word of an entry: a tile of states for the group's rows, the end of the
+// group (or of this CTA's part of it), the end of the work; with a tile, whether it is the first of the part, whether
+// the group has rows in the second half, and how many of the tile's states are there (1 .. 128).
+enum : uint32_t { kTile = 0, kEnd = 1, kStop = 2, kKind = 3, kFirst = 4, kTwoHalves = 8, kValidShift = 8 };
 
-// What the loader announces: a tile of states for the group's rows, the end of the group (or of this CTA's
-// part of it), the end of the work.
+// The first four words are all that a tile needs; the rest is read with the first tile and the end.
 struct Entry {
-  uint32_t kind, b, kvh, qt;  // sequence, key-value head, tile of rows
-  uint32_t tile, len;         // tile of states; states of the sequence
-  uint32_t first;             // first tile of this CTA's part
-  uint32_t t0, t1;            // kEnd: tiles of states of this CTA's part
-  uint32_t c0, parts;         // kEnd: first CTA with a part of the group, number of parts
-  uint32_t pad;
+  uint32_t ctl, tile, len, qt;      // tile of states; states of the sequence; tile of rows
+  uint32_t b, kvh, t0, t1;          // sequence, key-value head; kEnd: tiles of states of this CTA's part
+  uint32_t c0, parts, unused0, unused1;  // kEnd: first CTA with a part of the group, number of parts
 };
 
 struct CrossParams {
@@ -101,6 +100,7 @@ struct CrossSmem {
   static constexpr uint32_t kBarJoin = kBarODone + 16;
   static constexpr uint32_t kBarEFull = kBarJoin + 8, kBarEEmpty = kBarEFull + 8 * kEntries;
   static constexpr uint32_t kOffEntries = (kBarEEmpty + 8 * kEntries + 15) / 16 * 16;
+  static_assert(sizeof(Entry) % 16 == 0, "entries are read in 16-byte words");
   static constexpr uint32_t kTotal = kOffMisc + kOffEntries + kEntries * sizeof(Entry);
   static_assert(kTotal + 1024 <= 232448, "shared memory of one CTA");
 };
@@ -163,6 +163,18 @@ __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void lds128(uint32_t addr, uint32_t& a, uint32_t& b, uint32_t& c, uint32_t& d) {
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(a), "=r"(b), "=r"(c), "=r"(d) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+// One lane of a converged warp, chosen so that the compiler knows it is one.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t yes;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+  return yes != 0;
+}
 __device__ __forceinline__ float exp2_fast(float x) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -189,8 +201,9 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
   volatile uint32_t* const dead = reinterpret_cast<uint32_t*>(smem + L::kOffMisc);
   uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(smem + L::kOffMisc + 4);
   uint32_t* const join_flag = reinterpret_cast<uint32_t*>(smem + L::kOffMisc + 8);
-  volatile Entry* const entries = reinterpret_cast<Entry*>(smem + L::kOffMisc + L::kOffEntries);
-  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+  const uint32_t entries = misc + L::kOffEntries;
+  // the same in all lanes, and known to be: what depends on it alone stays on the uniform data path
+  const uint32_t warp = __shfl_sync(kFull, threadIdx.x >> 5, 0), lane = threadIdx.x & 31u;
   auto bar = [&](uint32_t off, uint32_t i) { return misc + off + 8u * i; };
 
   if (threadIdx.x == 0) {
@@ -227,16 +240,26 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
     ok = ok && mbar_wait(b, parity, dead);
     ok = __all_sync(kFull, ok);
   };
-  uint32_t en = 0;  // entries this warp has taken (or announced)
-  auto take = [&](Entry& e) {  // the next entry, which stays in its slot until it is released
-    wait(bar(L::kBarEFull, en % kEntries), (en / kEntries) & 1u);
+  uint32_t e_slot = 0, e_round = 0;  // slot of the next entry this warp takes (or announces), and how often the slots have wrapped
+  auto next_slot = [&]() {
+    if (++e_slot == kEntries) {
+      e_slot = 0;
+      ++e_round;
+    }
+  };
+  // the next entry: all of it, or its first words unless it opens or closes a group
+  auto take = [&](Entry& e) {
+    wait(bar(L::kBarEFull, e_slot), e_round & 1u);
     if (!ok) return;
-    const volatile Entry& s = entries[en % kEntries];
-    e.kind = s.kind, e.b = s.b, e.kvh = s.kvh, e.qt = s.qt, e.tile = s.tile, e.len = s.len, e.first = s.first;
-    e.t0 = s.t0, e.t1 = s.t1, e.c0 = s.c0, e.parts = s.parts;
+    const uint32_t at = entries + e_slot * (uint32_t)sizeof(Entry);
+    lds128(at, e.ctl, e.tile, e.len, e.qt);
+    if ((e.ctl & (kKind | kFirst)) != kTile) {
+      lds128(at + 16u, e.b, e.kvh, e.t0, e.t1);
+      lds128(at + 32u, e.c0, e.parts, e.unused0, e.unused1);
+    }
     __syncwarp();
-    if (lane == 0) mbar_arrive(bar(L::kBarEEmpty, en % kEntries));
-    ++en;
+    if (lane == 0) mbar_arrive(bar(L::kBarEEmpty, e_slot));
+    next_slot();
   };
 
   if (warp >= kLoadWarp) {
@@ -266,16 +289,17 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
       }
     }
     auto announce = [&](const Entry& e) {
-      if (en >= kEntries) wait(bar(L::kBarEEmpty, en % kEntries), ((en / kEntries) - 1u) & 1u);
+      if (e_round) wait(bar(L::kBarEEmpty, e_slot), (e_round - 1u) & 1u);
       if (!ok) return;
       if (lane == 0) {
-        volatile Entry& s = entries[en % kEntries];
-        s.kind = e.kind, s.b = e.b, s.kvh = e.kvh, s.qt = e.qt, s.tile = e.tile, s.len = e.len, s.first = e.first;
-        s.t0 = e.t0, s.t1 = e.t1, s.c0 = e.c0, s.parts = e.parts;
-        mbar_arrive(bar(L::kBarEFull, en % kEntries));
+        const uint32_t at = entries + e_slot * (uint32_t)sizeof(Entry);
+        sts128(at, e.ctl, e.tile, e.len, e.qt);
+        sts128(at + 16u, e.b, e.kvh, e.t0, e.t1);
+        sts128(at + 32u, e.c0, e.parts, 0u, 0u);
+        mbar_arrive(bar(L::kBarEFull, e_slot));
       }
       __syncwarp();
-      ++en;
+      next_slot();
     };
     auto load = [&](const CUtensorMap* map, const Entry& e) {
       if (st_round) wait(bar(L::kBarKvEmpty, st), (st_round - 1u) & 1u);
@@ -304,7 +328,8 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
       e.t0 = (uint32_t)(in % n);
       e.t1 = (uint32_t)min((uint64_t)n, (uint64_t)e.t0 + (u1 - u));
       const uint64_t first = u - e.t0, end = first + n;  // units of the whole group
-      e.first = 1u;
+      const uint32_t two = p.rows - e.qt * kRows > kHalf ? kTwoHalves : 0u;
+      uint32_t opens = kFirst;
       // tokens of the group's rows, whose mask bytes decide which tiles are needed
       const uint32_t tok0 = e.qt * kRows / p.group, tok1 = (min(p.rows, (e.qt + 1u) * kRows) - 1u) / p.group + 1u;
       uint32_t known = 0xFFFFFFFFu;  // block whose visibility is known (blocks of at least a tile), and it
@@ -336,15 +361,15 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
       };
       for (uint32_t t = e.t0; t < e.t1 && ok; ++t) {
         if (!seen(t)) continue;
-        e.kind = kTile;
+        e.ctl = kTile | opens | two | (min(kStates, len - t * kStates) << kValidShift);
         e.tile = t;
         announce(e);
         if (ok) load(&k_map, e);
         if (ok) load(&v_map, e);
-        e.first = 0u;
+        opens = 0u;
       }
       if (!ok) break;
-      e.kind = kEnd;
+      e.ctl = kEnd;
       const bool whole = first >= u0 && end <= u1;
       e.c0 = (uint32_t)(((first + 1u) * ctas - 1u) / total);
       e.parts = whole ? 1u : (uint32_t)((end * ctas - 1u) / total) - e.c0 + 1u;
@@ -358,39 +383,43 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
     }
     if (ok) {
       Entry e{};
-      e.kind = kStop;
+      e.ctl = kStop;
       announce(e);
     }
   } else if (warp == kMmaWarp) {
     // ---- products -------------------------------------------------------------------------------------
+    // This warp's path between two waits is on the critical path of both halves, and it shares its scheduler with the long
+    // softmax code: it is kept short, with operand descriptors that one addition moves on.
     uint32_t st = 0, st_round = 0;  // stage of the next K
-    bool have = false, accumulate = false;
-    uint32_t v_st = 0, v_round = 0, v_valid = kStates, halves = 2;
-    uint32_t p_phase[2] = {0, 0}, q_phase[2] = {0, 0};
+    bool have = false;
+    uint32_t accumulate = 0, v_st = 0, v_round = 0, v_valid = kStates, halves = 2;
+    uint32_t p_phase = 0, q_phase = 0;  // bit w: half w
     const uint32_t idesc_qk = umma_idesc(128, 128), idesc_pv = umma_idesc(128, D) | kIdescNMajorB;
-    auto qk = [&](uint32_t w, uint32_t k_tile) {
-      if (lane == 0) {
-        const uint32_t q_tile = smem0 + w * L::kQHalf;
+    const uint64_t q_desc = umma_desc(smem0), kv_desc = umma_desc(smem0 + L::kOffKv), v_desc = umma_desc_n_major(smem0 + L::kOffKv);
+    auto qk = [&](uint32_t w, uint32_t k_st) {
+      if (elect_one()) {
+        const uint64_t a = q_desc + w * (L::kQHalf >> 4), b = kv_desc + k_st * (L::kStageBytes >> 4);
 #pragma unroll
         for (uint32_t kk = 0; kk < D / 16; ++kk) {
-          const uint32_t off = (kk / 4u) * (128u * 128u) + (kk % 4u) * 32u;
-          umma_bf16(tmem + w * kStates, umma_desc(q_tile + off), umma_desc(k_tile + off), idesc_qk, kk != 0u);
+          constexpr uint32_t kSlab = (kHalf * 128u) >> 4;
+          const uint32_t off = (kk / 4u) * kSlab + (kk % 4u) * 2u;  // in 16 bytes
+          umma_bf16(tmem + w * kStates, a + off, b + off, idesc_qk, kk != 0u);
         }
         umma_commit(bar(L::kBarSFull, w));
       }
       __syncwarp();
     };
     auto pv = [&](uint32_t w) {
-      wait(bar(L::kBarPFull, w), p_phase[w]);
-      p_phase[w] ^= 1u;
+      wait(bar(L::kBarPFull, w), (p_phase >> w) & 1u);
+      p_phase ^= 1u << w;
       if (!ok) return;
       tmem_fence_after();
-      if (lane == 0) {
-        const uint32_t v_tile = smem0 + L::kOffKv + v_st * L::kStageBytes;
+      if (elect_one()) {
+        const uint64_t b = v_desc + v_st * (L::kStageBytes >> 4);
+        const uint32_t d = tmem + 2 * kStates + w * D, a = tmem + w * kStates;
+        umma_bf16_ts(d, a, b, idesc_pv, accumulate);
 #pragma unroll
-        for (uint32_t kk = 0; kk < kStates / 16; ++kk)
-          umma_bf16_ts(tmem + 2 * kStates + w * D, tmem + w * kStates + kk * 8u, umma_desc_n_major(v_tile + kk * 2048u), idesc_pv,
-                       accumulate || kk != 0u);
+        for (uint32_t kk = 1; kk < kStates / 16; ++kk) umma_bf16_ts(d, a + kk * 8u, b + kk * (2048u >> 4), idesc_pv, 1u);
         if (w + 1u == halves) umma_commit(bar(L::kBarKvEmpty, v_st));
       }
       __syncwarp();
@@ -417,35 +446,36 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
     Entry e;
     while (ok) {
       take(e);
-      if (!ok || e.kind == kStop) break;
+      const uint32_t kind = e.ctl & kKind;
+      if (!ok || kind == kStop) break;
       if (have) wait_v();
       if (!ok) break;
-      if (e.kind == kTile) {
-        if (e.first) halves = min(p.rows - e.qt * kRows, kRows) > kHalf ? 2u : 1u;
+      if (kind == kTile) {
+        if (e.ctl & kFirst) halves = e.ctl & kTwoHalves ? 2u : 1u;
         const uint32_t k_st = st;
         wait(bar(L::kBarKvFull, k_st), st_round & 1u);
         bump();
         for (uint32_t w = 0; w < halves && ok; ++w) {
           if (have) pv(w);
-          if (e.first) {
-            wait(bar(L::kBarQFull, w), q_phase[w]);
-            q_phase[w] ^= 1u;
+          if (e.ctl & kFirst) {
+            wait(bar(L::kBarQFull, w), (q_phase >> w) & 1u);
+            q_phase ^= 1u << w;
           }
-          if (ok) qk(w, smem0 + L::kOffKv + k_st * L::kStageBytes);
+          if (ok) qk(w, k_st);
         }
         if (!ok) break;
-        if (lane == 0) umma_commit(bar(L::kBarKvEmpty, k_st));
+        if (elect_one()) umma_commit(bar(L::kBarKvEmpty, k_st));
         __syncwarp();
-        accumulate = have;
+        accumulate = have ? 1u : 0u;
         have = true;
         v_st = st;
         v_round = st_round;
-        v_valid = min(kStates, e.len - e.tile * kStates);
+        v_valid = e.ctl >> kValidShift;
         bump();
       } else if (have) {
         for (uint32_t w = 0; w < halves && ok; ++w) {
           pv(w);
-          if (ok && lane == 0) umma_commit(bar(L::kBarODone, w));
+          if (ok && elect_one()) umma_commit(bar(L::kBarODone, w));
           __syncwarp();
         }
         have = false;
@@ -518,9 +548,9 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
     while (ok) {
       if (!pending) take(e);
       pending = false;
-      if (!ok || e.kind == kStop) break;
-      if (e.kind == kTile) {
-        if (e.first) {
+      if (!ok || (e.ctl & kKind) == kStop) break;
+      if ((e.ctl & kKind) == kTile) {
+        if (e.ctl & kFirst) {
           place(e);
           if (!q_ready) load_q(e);
           q_ready = false;
@@ -530,8 +560,11 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
         }
         if (!half_live) continue;
         uint32_t bits[4];
-        visible(e, bits);
-        const bool partial = __any_sync(kFull, (bits[0] & bits[1] & bits[2] & bits[3]) != 0xFFFFFFFFu);
+        bool partial = (e.ctl >> kValidShift) != kStates;  // some row does not see some state
+        if (p.mask != nullptr || partial) {
+          visible(e, bits);
+          partial = __any_sync(kFull, (bits[0] & bits[1] & bits[2] & bits[3]) != 0xFFFFFFFFu);
+        }
         wait(bar(L::kBarSFull, w), s_phase);
         s_phase ^= 1u;
         if (!ok) break;
@@ -557,7 +590,7 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
           const float f = mn == -INFINITY ? 1.f : exp2_fast(m - mn);
           m = mn;
           l *= f;
-          if (!e.first) {  // these scores were committed after the products with V before them: the output is complete
+          if (!(e.ctl & kFirst)) {  // these scores were committed after the products with V before them: the output is complete
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) {
               uint32_t o[16];
@@ -605,7 +638,7 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
       take(e);
       pending = true;
       if (!ok) break;
-      if (e.kind == kTile) {
+      if ((e.ctl & kKind) == kTile) {
         place(e);
         load_q(e);
         q_ready = true;
