@@ -55,6 +55,14 @@ constexpr int kCrossThreads = 384;  // 12 warps: the last two only make the thir
 constexpr int kSoftRegs = 200, kOtherRegs = 96;
 constexpr uint32_t kEntries = 4;       // announced tiles that may be under way
 constexpr uint32_t kTmemCols = 512;
+// With a mask of few large blocks (kCountBlocks at most, kCountBytes of mask in all, kCounts pairs of sequence and tile of
+// rows), every CTA first counts the tiles of states that each pair's rows see, and the shares are equal in those; otherwise
+// a unit is any tile below kv_len, and the shares of a CTA whose tiles are hidden are finished early.
+constexpr uint32_t kCounts = 512, kCountBlocks = 32, kCountBytes = 1u << 18;
+// Cutting groups costs about as much as this many tiles of states (their parts go through memory, the last CTA joins them;
+// 12 us of 1.9 us a tile); where whole groups spread evenly enough, none is cut.
+constexpr uint32_t kCutTiles = 6;
+constexpr int kChunks = 2;              // p of a tile is handed to the product with V in so many pieces
 constexpr float kRescale = 8.0f;       // log2 of how far p may exceed 1
 
 // What the loader announces, in the first word of an entry: a tile of states for the group's rows, the end of the
@@ -65,7 +73,7 @@ enum : uint32_t { kTile = 0, kEnd = 1, kStop = 2, kKind = 3, kFirst = 4, kTwoHal
 // The first four words are all that a tile needs; the rest is read with the first tile and the end.
 struct Entry {
   uint32_t ctl, tile, len, qt;      // tile of states; states of the sequence; tile of rows
-  uint32_t b, kvh, t0, t1;          // sequence, key-value head; kEnd: tiles of states of this CTA's part
+  uint32_t b, kvh, t0, t1;          // sequence, key-value head; kEnd: first and one past the last of the part's tiles of states
   uint32_t c0, parts, unused0, unused1;  // kEnd: first CTA with a part of the group, number of parts
 };
 
@@ -83,6 +91,7 @@ struct CrossParams {
   uint32_t n_seqs, n_tokens, n_q_heads, n_kv_heads, group;
   uint32_t rows, row_tiles;  // n_tokens * group, and its tiles of 256
   float scale_log2;
+  uint32_t counted;  // the units are the tiles of states that some row of the group sees (see kCounts)
   tq_attn_ws ws;
 };
 
@@ -96,12 +105,13 @@ struct CrossSmem {
   static constexpr uint32_t kOffMisc = kOffKv + kStages * kStageBytes;
   // misc: [0] dead flag, [4] tensor-memory base, [8] join flag, barriers from 16 on, entries behind them
   static constexpr uint32_t kBarKvFull = 16, kBarKvEmpty = kBarKvFull + 8 * kStages, kBarQFull = kBarKvEmpty + 8 * kStages;
-  static constexpr uint32_t kBarSFull = kBarQFull + 16, kBarPFull = kBarSFull + 16, kBarODone = kBarPFull + 16;
+  static constexpr uint32_t kBarSFull = kBarQFull + 16, kBarPFull = kBarSFull + 16, kBarODone = kBarPFull + 16 * kChunks;
   static constexpr uint32_t kBarJoin = kBarODone + 16;
   static constexpr uint32_t kBarEFull = kBarJoin + 8, kBarEEmpty = kBarEFull + 8 * kEntries;
   static constexpr uint32_t kOffEntries = (kBarEEmpty + 8 * kEntries + 15) / 16 * 16;
   static_assert(sizeof(Entry) % 16 == 0, "entries are read in 16-byte words");
-  static constexpr uint32_t kTotal = kOffMisc + kOffEntries + kEntries * sizeof(Entry);
+  static constexpr uint32_t kOffCounts = kOffEntries + kEntries * sizeof(Entry);
+  static constexpr uint32_t kTotal = kOffMisc + kOffCounts + kCounts * sizeof(uint16_t);
   static_assert(kTotal + 1024 <= 232448, "shared memory of one CTA");
 };
 // a part of a split group: [D / 4][256] float4 of output, then the rows' maxima and sums
@@ -175,6 +185,28 @@ __device__ __forceinline__ bool elect_one() {
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
   return yes != 0;
 }
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
 __device__ __forceinline__ float exp2_fast(float x) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -215,7 +247,7 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
     for (uint32_t i = 0; i < 2; ++i) {
       mbar_init(bar(L::kBarQFull, i), 4);
       mbar_init(bar(L::kBarSFull, i), 1);
-      mbar_init(bar(L::kBarPFull, i), 4);
+      for (uint32_t x = 0; x < kChunks; ++x) mbar_init(bar(L::kBarPFull, i * kChunks + x), 4);
       mbar_init(bar(L::kBarODone, i), 1);
     }
     for (uint32_t i = 0; i < kEntries; ++i) {
@@ -234,6 +266,48 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
   tmem_fence_after();
   const uint32_t tmem = *tmem_slot;
   asm volatile("griddepcontrol.wait;" ::: "memory");
+
+  uint16_t* const counts = reinterpret_cast<uint16_t*>(smem + L::kOffMisc + L::kOffCounts);
+  if (p.counted) {
+    uint32_t* const seen = reinterpret_cast<uint32_t*>(smem + L::kOffKv);  // the blocks that a pair's rows see, a bit each
+    const uint32_t pairs = p.n_seqs * p.row_tiles, bytes = p.n_seqs * p.n_tokens * p.n_blocks;
+    for (uint32_t i = threadIdx.x; i < pairs; i += kCrossThreads) seen[i] = 0u;
+    __syncthreads();
+    const bool words = ((uintptr_t)p.mask & 3u) == 0u;
+#pragma unroll 4
+    for (uint32_t i = threadIdx.x * 4u; i < bytes; i += kCrossThreads * 4u) {
+      uint32_t v = 0;
+      if (words && i + 4u <= bytes) {
+        v = __ldg(reinterpret_cast<const uint32_t*>(p.mask + i));
+      } else {
+        for (uint32_t k = i; k < min(i + 4u, bytes); ++k) v |= (uint32_t)__ldg(p.mask + k) << (8u * (k - i));
+      }
+      for (uint32_t k = 0; v != 0u; ++k, v >>= 8) {
+        if ((v & 255u) == 0u) continue;
+        const uint32_t bt = (i + k) / p.n_blocks, bit = 1u << ((i + k) - bt * p.n_blocks);
+        const uint32_t b = bt / p.n_tokens, r = (bt - b * p.n_tokens) * p.group;
+        for (uint32_t q = r / kRows; q <= (r + p.group - 1u) / kRows; ++q) {
+          uint32_t* at = seen + b * p.row_tiles + q;
+          if ((*(volatile uint32_t*)at & bit) == 0u) atomicOr(at, bit);
+        }
+      }
+    }
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < pairs; i += kCrossThreads) {
+      const uint32_t len = states_of(p, i / p.row_tiles);
+      uint32_t n = 0, next = 0;  // tiles; the first one that is not counted yet
+      for (uint32_t bits = seen[i]; bits != 0u; bits &= bits - 1u) {
+        const uint32_t blk = __ffs(bits) - 1u, from = blk * p.block_len;
+        if (from >= len) break;
+        const uint32_t t0 = max(from / kStates, next), t1 = (min(from + p.block_len, len) - 1u) / kStates + 1u;
+        if (t1 > t0) n += t1 - t0;
+        next = max(next, t1);
+      }
+      counts[i] = (uint16_t)max(n, 1u);
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the stages are TMA's from here on
+    __syncthreads();
+  }
 
   bool ok = true;
   auto wait = [&](uint32_t b, uint32_t parity) {
@@ -266,27 +340,57 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
   if (warp == kLoadWarp) {
     // ---- which tiles, and their K and V ---------------------------------------------------------------
-    const uint32_t groups = p.n_kv_heads * p.row_tiles;  // of one sequence
-    uint64_t total = 0, before = 0;
-    for (uint32_t b = lane; b < p.n_seqs; b += 32u) total += units_of(states_of(p, b));
+    // units of a group; of the row tiles of a sequence for one key-value head
+    auto units = [&](uint32_t b, uint32_t qt) { return p.counted ? (uint32_t)counts[b * p.row_tiles + qt] : units_of(states_of(p, b)); };
+    auto head_units = [&](uint32_t b) {
+      if (!p.counted) return (uint64_t)units_of(states_of(p, b)) * p.row_tiles;
+      uint64_t n = 0;
+      for (uint32_t q = 0; q < p.row_tiles; ++q) n += counts[b * p.row_tiles + q];
+      return n;
+    };
+    uint64_t total = 0;
+    for (uint32_t b = lane; b < p.n_seqs; b += 32u) total += head_units(b);
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) total += __shfl_xor_sync(kFull, total, d);
-    total *= groups;
+    total *= p.n_kv_heads;
     const uint32_t ctas = (uint32_t)min((uint64_t)gridDim.x, total);
-    uint64_t u = 0, u1 = 0;
+    const uint64_t n_groups = (uint64_t)p.n_seqs * p.n_kv_heads * p.row_tiles;
+    const bool cut = (n_groups + ctas - 1u) / ctas * (total / n_groups) > total / ctas + kCutTiles;
+    uint64_t u0 = 0, u1 = 0;  // this CTA's share; without cuts, the groups that start in it
     if (blockIdx.x < ctas) {
-      u = total * blockIdx.x / ctas;
+      u0 = total * blockIdx.x / ctas;
       u1 = total * (blockIdx.x + 1u) / ctas;
     }
-    const uint64_t u0 = u;
-    uint32_t b = 0, n = 1, len = 0, st = 0, st_round = 0;
-    if (u < u1) {
-      for (;; ++b) {
-        len = states_of(p, b);
-        n = units_of(len);
-        if (u < before + (uint64_t)n * groups) break;
-        before += (uint64_t)n * groups;
+    uint64_t first = 0;  // first unit of the group (b, kvh, qt)
+    uint32_t b = 0, kvh = 0, qt = 0, n = 1, st = 0, st_round = 0;
+    auto next_group = [&]() {
+      first += n;
+      if (++qt == p.row_tiles) {
+        qt = 0;
+        if (++kvh == p.n_kv_heads) {
+          kvh = 0;
+          ++b;
+        }
       }
+      if (b < p.n_seqs) n = units(b, qt);
+    };
+    if (u0 < u1) {
+      uint64_t h;
+      while (u0 >= first + (h = head_units(b)) * p.n_kv_heads) {
+        first += h * p.n_kv_heads;
+        ++b;
+      }
+      kvh = (uint32_t)((u0 - first) / h);
+      first += h * kvh;
+      if (!p.counted) {
+        n = units(b, 0);
+        qt = (uint32_t)((u0 - first) / n);
+        first += (uint64_t)n * qt;
+      } else {
+        n = units(b, 0);
+        while (u0 >= first + n) next_group();
+      }
+      if (!cut && first < u0) next_group();
     }
     auto announce = [&](const Entry& e) {
       if (e_round) wait(bar(L::kBarEEmpty, e_slot), (e_round - 1u) & 1u);
@@ -317,17 +421,15 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
         ++st_round;
       }
     };
-    while (u < u1 && ok) {
-      const uint64_t in = u - before;
+    for (; first < u1 && b < p.n_seqs && ok; next_group()) {
+      const uint32_t len = states_of(p, b);
+      // this CTA's units of the group
+      const uint32_t x0 = cut && u0 > first ? (uint32_t)(u0 - first) : 0u, x1 = cut && u1 < first + n ? (uint32_t)(u1 - first) : n;
       Entry e{};
       e.b = b;
       e.len = len;
-      const uint32_t g = (uint32_t)(in / n);
-      e.kvh = g / p.row_tiles;
-      e.qt = g % p.row_tiles;
-      e.t0 = (uint32_t)(in % n);
-      e.t1 = (uint32_t)min((uint64_t)n, (uint64_t)e.t0 + (u1 - u));
-      const uint64_t first = u - e.t0, end = first + n;  // units of the whole group
+      e.kvh = kvh;
+      e.qt = qt;
       const uint32_t two = p.rows - e.qt * kRows > kHalf ? kTwoHalves : 0u;
       uint32_t opens = kFirst;
       // tokens of the group's rows, whose mask bytes decide which tiles are needed
@@ -359,27 +461,30 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
         }
         return false;
       };
-      for (uint32_t t = e.t0; t < e.t1 && ok; ++t) {
-        if (!seen(t)) continue;
+      const uint32_t tiles = (len + kStates - 1u) / kStates;
+      uint32_t x = p.counted ? 0u : x0;  // the unit that the next tile is
+      for (uint32_t t = x; t < tiles && x < x1 && ok; ++t) {
+        const bool yes = seen(t);
+        if (!yes) {
+          if (!p.counted) ++x;
+          continue;
+        }
+        if (x++ < x0) continue;
         e.ctl = kTile | opens | two | (min(kStates, len - t * kStates) << kValidShift);
         e.tile = t;
         announce(e);
         if (ok) load(&k_map, e);
         if (ok) load(&v_map, e);
+        if (opens) e.t0 = t;
+        e.t1 = t + 1u;
         opens = 0u;
       }
       if (!ok) break;
       e.ctl = kEnd;
-      const bool whole = first >= u0 && end <= u1;
+      const uint64_t end = first + n;
       e.c0 = (uint32_t)(((first + 1u) * ctas - 1u) / total);
-      e.parts = whole ? 1u : (uint32_t)((end * ctas - 1u) / total) - e.c0 + 1u;
+      e.parts = !cut || (first >= u0 && end <= u1) ? 1u : (uint32_t)((end * ctas - 1u) / total) - e.c0 + 1u;
       announce(e);
-      u += e.t1 - e.t0;
-      if (u - before == (uint64_t)n * groups && u < u1) {
-        before = u;
-        len = states_of(p, ++b);
-        n = units_of(len);
-      }
     }
     if (ok) {
       Entry e{};
@@ -410,18 +515,23 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
       __syncwarp();
     };
     auto pv = [&](uint32_t w) {
-      wait(bar(L::kBarPFull, w), (p_phase >> w) & 1u);
-      p_phase ^= 1u << w;
-      if (!ok) return;
-      tmem_fence_after();
-      if (elect_one()) {
-        const uint64_t b = v_desc + v_st * (L::kStageBytes >> 4);
-        const uint32_t d = tmem + 2 * kStates + w * D, a = tmem + w * kStates;
-        umma_bf16_ts(d, a, b, idesc_pv, accumulate);
+      const uint64_t b = v_desc + v_st * (L::kStageBytes >> 4);
+      const uint32_t d = tmem + 2 * kStates + w * D, a = tmem + w * kStates;
+#pragma unroll 1
+      for (uint32_t x = 0; x < kChunks; ++x) {
+        wait(bar(L::kBarPFull, w * kChunks + x), (p_phase >> w) & 1u);
+        if (!ok) return;
+        tmem_fence_after();
+        if (elect_one()) {
+          constexpr uint32_t kSteps = kStates / 16 / kChunks;
 #pragma unroll
-        for (uint32_t kk = 1; kk < kStates / 16; ++kk) umma_bf16_ts(d, a + kk * 8u, b + kk * (2048u >> 4), idesc_pv, 1u);
-        if (w + 1u == halves) umma_commit(bar(L::kBarKvEmpty, v_st));
+          for (uint32_t kk = 0; kk < kSteps; ++kk)
+            umma_bf16_ts(d, a + (x * kSteps + kk) * 8u, b + (x * kSteps + kk) * (2048u >> 4), idesc_pv, accumulate | x | kk);
+        }
+        __syncwarp();
       }
+      p_phase ^= 1u << w;
+      if (w + 1u == halves && elect_one()) umma_commit(bar(L::kBarKvEmpty, v_st));
       __syncwarp();
     };
     auto wait_v = [&]() {
@@ -579,11 +689,11 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
         }
         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int i = 0; i < 128; i += 4) {
+        for (int i = 0; i < 128; i += 8) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], __uint_as_float(s[i + k]));
+          for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], __uint_as_float(s[i + 2 * k]), __uint_as_float(s[i + 2 * k + 1]));
         }
-        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
+        const float top = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]) * c;
         const bool grow = top > m + kRescale;
         if (__any_sync(kFull, grow)) {
           const float mn = fmaxf(m, top);
@@ -603,25 +713,38 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
           }
         }
         const float ref = m == -INFINITY ? 0.f : m;
-        float ls[4] = {0.f, 0.f, 0.f, 0.f};
+        const uint64_t c2 = pair(c, c), ref2 = pair(-ref, -ref);
+        uint64_t sum[2] = {0, 0};
+        auto hand_over = [&](int x) {  // piece x of p is in tensor memory
+          tmem_wait_st();
+          tmem_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(L::kBarPFull, w * kChunks + x));
+        };
+        constexpr int kPairs = 64 / kChunks;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t pk[32];
+        for (int x = 0; x < kChunks; ++x) {
+          uint32_t pk[kPairs];
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            const float a = exp2_fast(fmaf(__uint_as_float(s[64 * h + 2 * i]), c, -ref));
-            const float b = exp2_fast(fmaf(__uint_as_float(s[64 * h + 2 * i + 1]), c, -ref));
-            ls[(2 * i) & 3] += a;
-            ls[(2 * i + 1) & 3] += b;
+          for (int i = 0; i < kPairs; ++i) {
+            const int at = 2 * (x * kPairs + i);
+            float a, b;
+            unpair(fma2(pair(__uint_as_float(s[at]), __uint_as_float(s[at + 1])), c2, ref2), a, b);
+            a = exp2_fast(a);
+            b = exp2_fast(b);
+            sum[i & 1] = add2(sum[i & 1], pair(a, b));
             pk[i] = pack_bf16(a, b);
           }
-          TMEM_ST32(s_addr + 32u * h, pk);
+          if (x) hand_over(x - 1);
+          if constexpr (kPairs == 16)
+            TMEM_ST16(s_addr + kPairs * x, pk);
+          else
+            TMEM_ST32(s_addr + kPairs * x, pk);
         }
-        l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
-        tmem_wait_st();
-        tmem_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(L::kBarPFull, w));
+        hand_over(kChunks - 1);
+        float l0, l1;
+        unpair(add2(sum[0], sum[1]), l0, l1);
+        l += l0 + l1;
         continue;
       }
       // ---- end of the group, or of this CTA's part: the next group's queries first, they are waited for ------
@@ -736,39 +859,47 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
       if (whole) continue;
       mine[kRows * 128 + slot] = m;
       mine[kRows * 129 + slot] = l;
-      __threadfence();
       meet();
       if (!ok) break;
-      // atomicInc wraps to 0 with the last part, which is the state the next call needs
-      if (threadIdx.x == 0) *join_flag = atomicInc(p.ws.counters + g.c0, g.parts - 1u) == g.parts - 1u;
+      if (threadIdx.x == 0) {
+        // what the warps wrote before they met is published with this thread's fence; atomicInc wraps to 0 with the last
+        // part, which is the state the next call needs
+        __threadfence();
+        *join_flag = atomicInc(p.ws.counters + g.c0, g.parts - 1u) == g.parts - 1u;
+        __threadfence();
+      }
       meet();
       if (!ok) break;
       if (*join_flag) {
-        __threadfence();
+        const uint32_t own = blockIdx.x - g.c0;
         float M = -INFINITY;
-        for (uint32_t i = 0; i < g.parts; ++i) M = fmaxf(M, __ldcg(part(i) + kRows * 128 + slot));
+#pragma unroll 4
+        for (uint32_t x = 0; x < g.parts; ++x) M = fmaxf(M, __ldcg(part(x) + kRows * 128 + slot));
         const float ref = M == -INFINITY ? 0.f : M;
         l = 0.f;
-        for (uint32_t i = 0; i < g.parts; ++i) l += exp2_fast(__ldcg(part(i) + kRows * 128 + slot) - ref) * __ldcg(part(i) + kRows * 129 + slot);
+#pragma unroll 4
+        for (uint32_t x = 0; x < g.parts; ++x) l += exp2_fast(__ldcg(part(x) + kRows * 128 + slot) - ref) * __ldcg(part(x) + kRows * 129 + slot);
+        const float m_own = m;
         m = M;
+        constexpr int kCols = 64;  // 16 loads under way a thread
 #pragma unroll 1
-        for (int i = 0; i < D / 32; ++i) {
-          uint32_t o[32];
+        for (int i = 0; i < D / kCols; ++i) {
+          float o[kCols];
 #pragma unroll
-          for (int k = 0; k < 32; ++k) o[k] = 0u;
+          for (int k = 0; k < kCols; ++k) o[k] = 0.f;
 #pragma unroll 1
-          for (uint32_t x = 0; x < g.parts; ++x) {
-            const float f = exp2_fast(__ldcg(part(x) + kRows * 128 + slot) - ref);
+          for (uint32_t x = 0; x < g.parts; ++x) {  // in the order of the parts
+            float4 y[kCols / 4];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const float4 y = __ldcg(reinterpret_cast<const float4*>(part(x)) + (8 * i + k) * kRows + slot);
-              o[4 * k] = __float_as_uint(__uint_as_float(o[4 * k]) + f * y.x);
-              o[4 * k + 1] = __float_as_uint(__uint_as_float(o[4 * k + 1]) + f * y.y);
-              o[4 * k + 2] = __float_as_uint(__uint_as_float(o[4 * k + 2]) + f * y.z);
-              o[4 * k + 3] = __float_as_uint(__uint_as_float(o[4 * k + 3]) + f * y.w);
+            for (int k = 0; k < kCols / 4; ++k) y[k] = __ldcg(reinterpret_cast<const float4*>(part(x)) + (kCols / 4 * i + k) * kRows + slot);
+            const float f = exp2_fast((x == own ? m_own : __ldcg(part(x) + kRows * 128 + slot)) - ref);
+#pragma unroll
+            for (int k = 0; k < kCols / 4; ++k) {
+              o[4 * k] += f * y[k].x, o[4 * k + 1] += f * y[k].y, o[4 * k + 2] += f * y[k].z, o[4 * k + 3] += f * y[k].w;
             }
           }
-          write(i, o);
+          write(2 * i, reinterpret_cast<const uint32_t(&)[32]>(o[0]));
+          write(2 * i + 1, reinterpret_cast<const uint32_t(&)[32]>(o[32]));
         }
       }
       meet();  // the flag has been read
@@ -852,6 +983,8 @@ int tq_cross_launch(const tq_encoder_kv* kv, const void* d_q, int64_t q_batch_st
   p.rows = n_tokens * p.group;
   p.row_tiles = (p.rows + kRows - 1u) / kRows;
   p.scale_log2 = scale_log2;
+  p.counted = d_mask != nullptr && block_len >= kStates && n_blocks <= kCountBlocks && kv->n_states <= 65535u * kStates &&
+              (uint64_t)kv->n_seqs * p.row_tiles <= kCounts && (uint64_t)kv->n_seqs * n_tokens * n_blocks <= kCountBytes;
   p.ws = ws;
   cudaStream_t st = (cudaStream_t)cuda_stream;
   return kv->head_dim == 64 ? launch<64>(p, k_map, v_map, st) : launch<128>(p, k_map, v_map, st);
