@@ -703,11 +703,30 @@ _raw_stream = torch._C._cuda_getCurrentRawStream
 _current_device = torch._C._cuda_getDevice
 
 
-# A decode step makes dozens of these calls of a few microseconds each, so their checks use the cheap tensor attributes
-# (get_device() is -1 for a CPU tensor) and build no objects in the usual case.
+def _load_fast():
+    """The native form of the calls below for their usual case (csrc/tq_fast.cpp), or None (no headers to build it with, a torch
+    without the DLPack exchange interface).  It answers None for whatever it does not take, and the checks here speak."""
+    import importlib.util
+
+    path = _build.build_fast()
+    if path is None:
+        return None
+    spec = importlib.util.spec_from_file_location("_tqfast", str(path))
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    names = ("tq_rmsnorm", "tq_rmsnorm_q8", "tq_rope_append", "tq_paged_attention", "tq_cross_attention")
+    return module if module.setup(torch, *(C.cast(getattr(_lib, n), C.c_void_p).value for n in names)) else None
+
+
+_fast = _load_fast()
+
+
+# A decode step makes dozens of these calls of a few microseconds each: the usual case goes through _fast, and the checks
+# here use the cheap tensor attributes (get_device() is -1 for a CPU tensor) and build no objects.
 def _elsewhere(device: int, stream):
     """None if the call is for the current device and its current stream; else a context in which it is, so that the call's results
     come from that stream's memory."""
+    assert device >= 0, "a CUDA tensor is wanted"
     if stream is None:
         return None if _current_device() == device else torch.cuda.device(device)
     assert stream.device.index == device
@@ -741,6 +760,10 @@ def tq_rmsnorm(h: torch.Tensor, weight: torch.Tensor, delta: torch.Tensor | None
                out: torch.Tensor | None = None, h_out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """h: CUDA bf16 / fp32 [rows][cols] (rows may be strided); delta: bf16 / fp32 of the same shape; weight: fp32 [cols].
     With a delta the sum h + delta goes to h_out (a tensor like h), or to h itself when h_out is None.  -> bf16 [rows][cols]."""
+    if stream is None and _fast is not None:
+        r = _fast.rmsnorm(h, weight, delta, eps, out, h_out)
+        if r is not None:
+            return r
     device = h.get_device()
     ctx = _elsewhere(device, stream)
     if ctx is not None:
@@ -758,6 +781,10 @@ def tq_rmsnorm(h: torch.Tensor, weight: torch.Tensor, delta: torch.Tensor | None
 def tq_rmsnorm_q8(h: torch.Tensor, weight: torch.Tensor, delta: torch.Tensor | None = None, eps: float = 1e-5,
                   q: torch.Tensor | None = None, scale: torch.Tensor | None = None, h_out: torch.Tensor | None = None, stream=None):
     """tq_rmsnorm with the result in 8 bits: -> (int8 [rows][cols], fp32 [rows] scales)."""
+    if stream is None and q is None and scale is None and _fast is not None:
+        r = _fast.rmsnorm_q8(h, weight, delta, eps, h_out)
+        if r is not None:
+            return r
     device = h.get_device()
     ctx = _elsewhere(device, stream)
     if ctx is not None:
@@ -787,6 +814,8 @@ class KvCache:
         self._c = _KvCache(k.data_ptr(), v.data_ptr(), self.n_pages, self.page_size, self.n_kv_heads, self.head_dim,
                            *_strides(k)[:3], self.status.data_ptr())
         self._ref = C.byref(self._c)
+        self._addr = C.addressof(self._c)
+        self.scale = self.head_dim ** -0.5  # of the scores, unless a call says otherwise
 
 
 def tq_kv_cache(k: torch.Tensor, v: torch.Tensor) -> KvCache:
@@ -824,6 +853,10 @@ def tq_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, table: tor
     """q, k, v: CUDA bf16 or fp32 [tokens][heads * head dim] or [tokens][heads][head dim] (tokens may be strided); table: fp32
     [positions][rot dim], cosines then sines; positions: int32 [axes][tokens] or [tokens]; slots: int32 [tokens], -1 for none;
     sections: pairs of each axis (one axis: all).  -> rotated q, bf16 [tokens][q heads][head dim]; k and v are in the cache."""
+    if stream is None and _fast is not None:
+        r = _fast.rope_append(q, k, v, table, positions, slots, cache._addr, cache.device, sections, interleaved, out)
+        if r is not None:
+            return r
     device = q.get_device()
     ctx = _elsewhere(device, stream)
     if ctx is not None:
@@ -891,6 +924,11 @@ def tq_paged_attention(q: torch.Tensor, cache: KvCache, page_table: torch.Tensor
                        stream=None) -> torch.Tensor:
     """q: CUDA bf16 [sequences][q heads][head dim] (sequences may be strided); page_table: int32 [sequences][max pages]; lens: int32
     [sequences]; scale: 1 / sqrt(head dim) when None; lse: fp32 [sequences][q heads], filled when given.  -> bf16 like q."""
+    if stream is None and _fast is not None:
+        r = _fast.paged_attention(q, cache._addr, cache.device, page_table, lens, workspace.ptr, workspace.bytes, workspace.device,
+                                  cache.scale if scale is None else scale, out, lse)
+        if r is not None:
+            return r
     device = q.get_device()
     ctx = _elsewhere(device, stream)
     if ctx is not None:
@@ -904,7 +942,7 @@ def tq_paged_attention(q: torch.Tensor, cache: KvCache, page_table: torch.Tensor
     assert lens.get_device() == device and lens.dtype == torch.int32 and lens.is_contiguous() and lens.numel() == B
     out, lse = _attn_out(q, out, lse, device)
     _check(_lib.tq_paged_attention(cache._ref, q.data_ptr(), stride[0] if B > 1 else 0, B, H, page_table.data_ptr(), max_pages, lens.data_ptr(),
-                                   D ** -0.5 if scale is None else scale, out.data_ptr(), lse, workspace.ptr, workspace.bytes,
+                                   cache.scale if scale is None else scale, out.data_ptr(), lse, workspace.ptr, workspace.bytes,
                                    _raw_stream(device)), "tq_paged_attention")
     return out
 
@@ -916,6 +954,11 @@ def tq_cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, worksp
     expanded batch has the same states for every sequence); kv_len: int32 [sequences]; mask: uint8 / bool
     [sequences][tokens][ceil(states / block_len)], nonzero where a token sees the block; lse: fp32 [sequences][tokens][q heads],
     filled when given.  -> bf16 [sequences][tokens][q heads][head dim]."""
+    if stream is None and _fast is not None:
+        r = _fast.cross_attention(q, k, v, workspace.ptr, workspace.bytes, workspace.device, kv_len, mask, block_len,
+                                  q.shape[-1] ** -0.5 if scale is None else scale, out, lse)
+        if r is not None:
+            return r
     device = q.get_device()
     ctx = _elsewhere(device, stream)
     if ctx is not None:

@@ -10,6 +10,8 @@ PKG = Path(__file__).resolve().parent
 ROOT = PKG.parent
 CSRC = PKG / "csrc"
 LIB = PKG / "libtq.so"
+FAST = PKG / "_tqfast.so"  # CPython module: the usual case of the calls between the linear layers
+FAST_SOURCE = CSRC / "tq_fast.cpp"
 SOURCES = [CSRC / "tq_device.cu", CSRC / "tq_gemm.cu", CSRC / "tq_gemm_ws.cu", CSRC / "tq_tiles.cu", CSRC / "tq_wide.cu", CSRC / "tq_encode.cu", CSRC / "tq_dict_device.cu",
            CSRC / "tq_norm.cu", CSRC / "tq_rope.cu", CSRC / "tq_attn.cu", CSRC / "tq_cross.cu", CSRC / "tq_host.cpp"]
 HEADERS = [CSRC / "tq_internal.h", CSRC / "tq_sm100.cuh", CSRC / "tq_tiles_common.cuh", CSRC / "tq_ops_common.cuh", ROOT / "include" / "tq.h"]
@@ -50,6 +52,26 @@ def build_library(force: bool = False, verbose: bool = False) -> Path:
     return LIB
 
 
+def build_fast(force: bool = False) -> Path | None:
+    """Builds _tqfast.so; None where the headers of the running interpreter or of torch (dlpack.h) are missing."""
+    import sysconfig
+
+    import torch
+    sources = [FAST_SOURCE, ROOT / "include" / "tq.h"]
+    if not force and FAST.exists() and FAST.stat().st_mtime >= max(p.stat().st_mtime for p in sources):
+        return FAST
+    python, dlpack = Path(sysconfig.get_paths()["include"]), Path(torch.__file__).parent / "include"
+    gxx = shutil.which("g++")
+    if gxx is None or not (python / "Python.h").exists() or not (dlpack / "ATen" / "dlpack.h").exists():
+        return FAST if FAST.exists() else None
+    tmp = FAST.with_name(f"_tqfast.tmp{os.getpid()}.so")
+    subprocess.check_call([gxx, "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-I", str(ROOT / "include"), "-I", str(python), "-I", str(dlpack),
+                           str(FAST_SOURCE), "-o", str(tmp)])
+    os.replace(tmp, FAST)
+    return FAST
+
+
 if __name__ == "__main__":
     import sys
+    build_fast(force=True)
     print(build_library(force=True, verbose="-v" in sys.argv))

@@ -483,3 +483,70 @@ def test_streams_and_graphs(tq):
         torch.cuda.synchronize()
         assert torch.equal(o1, ref) and torch.equal(o2, cross)
     assert tq.tq_attn_status(w2) == 0
+
+
+def test_native_and_python_form_of_a_call_agree(tq, ws, monkeypatch):
+    """The calls' usual case runs in a CPython module; the checks in Python make the same call of the library."""
+    assert tq._fast is not None
+    g = gen(20)
+    h, w, d = randn(g, 5, 384, dtype=BF), randn(g, 384), randn(g, 5, 384)
+    q, k, v = randn(g, 5, 6, 64), randn(g, 5, 2, 64), randn(g, 5, 2, 64)
+    pos = torch.arange(10, dtype=torch.int32, device="cuda").view(2, 5)
+    slots = torch.tensor([3, 17, -1, 30, 8], dtype=torch.int32, device="cuda")
+    pages, lens = torch.tensor([[0, 1], [1, 0]], dtype=torch.int32, device="cuda"), torch.tensor([20, 9], dtype=torch.int32, device="cuda")
+    enc, mask = randn(g, 2, 50, 2, 64, dtype=BF), torch.rand(2, 3, 5, generator=g, device="cuda") < 0.5
+    table = rope_table(10, 64)
+    base = randn(g, 2, 2, 16, 64, dtype=BF)
+
+    def all_calls():
+        kp, vp = base.clone(), base.clone()
+        cache, ho = tq.tq_kv_cache(kp, vp), torch.empty_like(h)
+        res = [tq.tq_rmsnorm(h, w), tq.tq_rmsnorm(h, w, d, h_out=ho), ho, *tq.tq_rmsnorm_q8(h, w, d, h_out=torch.empty_like(h))]
+        res += [tq.tq_rope_append(q, k, v, table, pos, slots, cache, sections=[20, 12], interleaved=True), kp, vp]
+        res += [tq.tq_rope_append(q.flatten(1), k, v, table, pos[1], slots, cache)]
+        lse = torch.empty(2, 6, device="cuda")
+        res += [tq.tq_paged_attention(res[-1][:2], cache, pages, lens, ws, lse=lse), lse]
+        qq = randn(gen(21), 2, 3, 6, 64, dtype=BF)
+        res += [tq.tq_cross_attention(qq, enc, enc, ws, kv_len=lens, mask=mask, block_len=10), tq.tq_cross_attention(qq[:, :1], enc, enc, ws, scale=0.3)]
+        return res
+
+    native = all_calls()
+    monkeypatch.setattr(tq, "_fast", None)
+    for a, b in zip(native, all_calls(), strict=True):
+        assert a.shape == b.shape and a.dtype == b.dtype and torch.equal(a, b)
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_refusals_of_the_binding(tq, ws, monkeypatch, native):
+    if not native:
+        monkeypatch.setattr(tq, "_fast", None)
+    g = gen(22)
+    h, w = randn(g, 4, 64, dtype=BF), randn(g, 64)
+    bad = (AssertionError, tq.TqError, KeyError, ValueError)
+    for call in [lambda: tq.tq_rmsnorm(h.cpu(), w), lambda: tq.tq_rmsnorm(h.half(), w), lambda: tq.tq_rmsnorm(h, w[:63]), lambda: tq.tq_rmsnorm(h, w.to(BF)),
+                 lambda: tq.tq_rmsnorm(h[0], w), lambda: tq.tq_rmsnorm(h.t(), w[:4]), lambda: tq.tq_rmsnorm(h, w, h[:3]), lambda: tq.tq_rmsnorm(h, w, h.half()),
+                 lambda: tq.tq_rmsnorm(h, w, out=h.float()), lambda: tq.tq_rmsnorm(h, w, h, h_out=h.float()), lambda: tq.tq_rmsnorm(h, w, eps=-1.0)]:
+        with pytest.raises(bad):
+            call()
+    kp = randn(g, 3, 2, 16, 64, dtype=BF)
+    cache = tq.tq_kv_cache(kp, kp.clone())
+    q, k, t, i = randn(g, 4, 4, 64), randn(g, 4, 2, 64), rope_table(9, 64), torch.zeros(4, dtype=torch.int32, device="cuda")
+    for call in [lambda: tq.tq_rope_append(q, k, q, t, i, i, cache), lambda: tq.tq_rope_append(q, k, k.to(BF), t, i, i, cache),
+                 lambda: tq.tq_rope_append(q, k, k, t, i.long(), i, cache), lambda: tq.tq_rope_append(q, k, k, t, i, i[:3], cache),
+                 lambda: tq.tq_rope_append(q, k, k, t, i, i, cache, sections=[31]), lambda: tq.tq_rope_append(q, k, k, t, i, i, cache, sections=[16, 16]),
+                 lambda: tq.tq_rope_append(q, k, k, t[:, :60], i, i, cache), lambda: tq.tq_kv_cache(kp, kp[:2]), lambda: tq.tq_kv_cache(kp, kp.float())]:
+        with pytest.raises(bad):
+            call()
+    qb, pages, lens = q.to(BF), torch.zeros(4, 2, dtype=torch.int32, device="cuda"), i
+    for call in [lambda: tq.tq_paged_attention(q, cache, pages, lens, ws), lambda: tq.tq_paged_attention(qb[:, :3], cache, pages, lens, ws),
+                 lambda: tq.tq_paged_attention(qb, cache, pages[:3], lens, ws), lambda: tq.tq_paged_attention(qb, cache, pages, lens.long(), ws),
+                 lambda: tq.tq_paged_attention(qb, cache, pages, lens, ws, scale=0.0), lambda: tq.tq_paged_attention(qb, cache, pages, lens, ws, lse=lens)]:
+        with pytest.raises(bad):
+            call()
+    qc, e, m = randn(g, 2, 3, 4, 64, dtype=BF), randn(g, 2, 20, 2, 64, dtype=BF), torch.ones(2, 3, 4, dtype=torch.uint8, device="cuda")
+    for call in [lambda: tq.tq_cross_attention(qc, e, e[:, :19], ws), lambda: tq.tq_cross_attention(qc, e[:1], e[:1], ws),
+                 lambda: tq.tq_cross_attention(qc, e, e, ws, mask=m, block_len=4), lambda: tq.tq_cross_attention(qc, e, e, ws, mask=m.int(), block_len=5),
+                 lambda: tq.tq_cross_attention(qc[:, :, :3], e, e, ws), lambda: tq.tq_cross_attention(qc, e, e, ws, kv_len=m[0, 0]),
+                 lambda: tq.tq_cross_attention(qc, e, e, ws, out=qc[:1])]:
+        with pytest.raises(bad):
+            call()
