@@ -406,8 +406,8 @@ void tq_dmat_free(tq_dmat* m); /* host handle only */
  * h, h_out: DEVICE, rows x cols of h_type, h_stride elements from row to row; h_out may be h (in place)
  * and may be NULL (the sum is not kept).  delta: DEVICE, rows x cols of delta_type, delta_stride.
  * d_weight: DEVICE fp32 [cols].  d_out: DEVICE bf16 [rows][cols].  cols: 1..TQ_NORM_MAX_COLS.
- * Any alignment of the elements' own size is accepted; 16-byte aligned rows (cols a multiple of 8) are
- * read and written in 16-byte pieces.  rows == 0 is a call that does nothing. */
+ * Any alignment of the elements' own size is accepted; rows whose every eight elements are aligned to their
+ * 16 or 32 bytes (cols and strides multiples of 8) are read and written in such pieces.  rows == 0 is a call that does nothing. */
 #define TQ_NORM_MAX_COLS 16384u
 int tq_rmsnorm(const void* d_h, int h_type, int64_t h_stride, const void* d_delta, int delta_type,
                int64_t delta_stride, const float* d_weight, float eps, uint32_t rows, uint32_t cols,

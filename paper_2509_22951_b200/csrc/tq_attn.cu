@@ -6,16 +6,19 @@
 // Every key and value is used by the G = n_q_heads / n_kv_heads query heads that share it, at 2 G
 // operations a byte: memory bound by a factor of 20 and more, so the kernel is built around the loads.
 //
-// Split.  The work is a flat list of units of 64 states, all sequences' and heads' one after the other;
+// Split.  The work is a flat list of units of 128 states, all sequences' and heads' one after the other;
 // each CTA takes an equal share of consecutive units, whatever the lengths are (they are known on the
 // device only).  A group (sequence, key-value head) that lies in several shares leaves its parts
 // (maximum, sum, unnormalised output) in the workspace and the CTA that finishes last joins them in the
 // order of the CTAs, so the result does not depend on timing.
 //
-// CTA.  Four warps, two CTAs to an SM.  A warp works on its own 16 states of each unit with its own
-// ring of three stages filled by 16-byte cp.async: nothing in the loop waits for another warp, and 128 KB
-// are under way on every SM (6.5 TB/s x 1 us of latency / 148 SMs = 44 KB are the least).  The page ids of
-// a step are loaded one step before its copies are issued.
+// CTA.  Eight warps, one CTA to an SM.  A warp works on its own 16 states of each unit with its own ring of two
+// stages filled by 16-byte cp.async, so nothing in the loop waits for another warp, and 64 KB and more are under way
+// on every SM (6.5 TB/s x 1 us of latency / 148 SMs = 44 KB are the least).  The page ids of a step are loaded one
+// step before its copies are issued.  Measured for 8 sequences of up to 8191 tokens with 24 / 8 heads | one of
+// 131071, 32 / 8 | 64 of up to 16384, 64 / 8 | 4 over 6404 encoder states, 32 / 8 (us): 34.7 | 90.1 | 392 | 24.6;
+// three stages 35.6 | 93.0 | 414 | 25.4; two CTAs of four warps, which leave twice the parts to join,
+// 35.6 | 90.3 | 392 | 28.1; ten warps 34.4 | 93.7 | 402 | 25.5, six 37.8 | 95.4 | 418 | 26.4.
 //
 // Arithmetic.  mma.sync m16n8k16, bf16 in, fp32 out, with the states as the rows: S^T = K Q^T (16 states x
 // 8 heads), then O^T = V^T P^T (head_dim x 8 heads), so that a group of up to 8 heads wastes nothing but
@@ -35,8 +38,8 @@ namespace {
 
 using namespace tq_ops;
 
-constexpr int kWarps = 4, kThreads = kWarps * 32;
-constexpr int kStages = 3;
+constexpr int kWarps = 8, kThreads = kWarps * 32;
+constexpr int kStages = 2;
 constexpr uint32_t kStepStates = 16;                     // states of a warp's step
 constexpr uint32_t kUnitStates = kWarps * kStepStates;   // states of a CTA's unit
 constexpr uint32_t kHeads = 8;                           // query heads of a group: the columns of the products
@@ -54,6 +57,7 @@ struct AttnParams {
   const uint8_t* mask;        // cross: or nullptr
   uint32_t max_pages, page_size, n_pages;
   uint32_t n_states, block_len, n_blocks;
+  uint32_t compact;           // cross: the units are those of the visible blocks alone (one token, at most 32 blocks)
   uint32_t n_seqs, n_tokens, n_q_heads, n_kv_heads, group, head_parts;  // head_parts: groups of 8 heads that share a key-value head
   float scale_log2;
   uint32_t* status;
@@ -103,6 +107,11 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return r;
 }
 
+// Quotient of counts that nearly always fit 32 bits.
+__device__ __forceinline__ uint64_t quotient(uint64_t a, uint64_t b) {
+  return ((a | b) >> 32) == 0u ? (uint64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
 // States of sequence b that a call may look at.
 template <bool PAGED>
 __device__ __forceinline__ uint32_t length_of(const AttnParams& p, uint32_t b) {
@@ -111,9 +120,18 @@ __device__ __forceinline__ uint32_t length_of(const AttnParams& p, uint32_t b) {
     const uint64_t cap = (uint64_t)p.max_pages * p.page_size;
     return n <= 0 ? 0u : (uint32_t)((uint64_t)n > cap ? cap : (uint64_t)n);
   }
-  if (p.lens == nullptr) return p.n_states;
-  const int32_t n = __ldg(p.lens + b);
-  return n <= 0 ? 0u : min((uint32_t)n, p.n_states);
+  uint32_t len = p.n_states;
+  if (p.lens != nullptr) {
+    const int32_t n = __ldg(p.lens + b);
+    len = n <= 0 ? 0u : min((uint32_t)n, p.n_states);
+  }
+  if (!p.compact) return len;
+  // the visible blocks' states, one block after the other; only the last one of them can be cut by the length
+  const uint8_t* m = p.mask + (size_t)b * p.n_blocks;
+  uint32_t sum = 0;
+#pragma unroll 8
+  for (uint32_t k = 0; k < p.n_blocks; ++k) sum += __ldg(m + k) != 0 && k * p.block_len < len ? min(p.block_len, len - k * p.block_len) : 0u;
+  return sum;
 }
 // Units of a group of sequence b; a group without states keeps one, whose CTA writes its zeros.
 __device__ __forceinline__ uint32_t units_of(uint32_t len) { return len == 0u ? 1u : (len + kUnitStates - 1u) / kUnitStates; }
@@ -137,7 +155,7 @@ struct Walk {
 };
 
 template <int D, bool PAGED>
-__global__ void __launch_bounds__(kThreads, 2) split_attention_kernel(const AttnParams p) {
+__global__ void __launch_bounds__(kThreads, 1) split_attention_kernel(const AttnParams p) {
   using L = Smem<D>;
   extern __shared__ __align__(128) uint8_t smem[];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -166,8 +184,8 @@ __global__ void __launch_bounds__(kThreads, 2) split_attention_kernel(const Attn
     total = __shfl_sync(kFull, incl, 31) * groups;
     ctas = (uint32_t)min((uint64_t)gridDim.x, total);
     if (blockIdx.x >= ctas) return;  // nothing waits for this CTA
-    u0 = total * blockIdx.x / ctas;
-    u1 = total * (blockIdx.x + 1u) / ctas;
+    u0 = quotient(total * blockIdx.x, ctas);
+    u1 = quotient(total * (blockIdx.x + 1u), ctas);
     const uint32_t owner = __ffs(__ballot_sync(kFull, u0 < incl * groups)) - 1u;
     uint64_t before = incl - sum;  // units of one group of each earlier sequence
     uint32_t b = first;
@@ -182,8 +200,8 @@ __global__ void __launch_bounds__(kThreads, 2) split_attention_kernel(const Attn
     before = __shfl_sync(kFull, before, owner);
     at.enter<PAGED>(p);
     const uint64_t rest = u0 - before * groups;
-    at.m = (uint32_t)(rest / at.tiles);
-    at.tile = (uint32_t)(rest % at.tiles);
+    at.m = (uint32_t)quotient(rest, at.tiles);
+    at.tile = (uint32_t)(rest - (uint64_t)at.m * at.tiles);
   }
   const uint32_t n_units = (uint32_t)(u1 - u0);
 
@@ -196,6 +214,7 @@ __global__ void __launch_bounds__(kThreads, 2) split_attention_kernel(const Attn
   uint32_t f_head = 0, f_b = 0;
   bool f_live = false;
   bool bad_page = false;
+  uint32_t list = 0, list_b = 0xFFFFFFFFu;  // compact: lane k has the k-th visible block of sequence list_b
   auto fetch = [&]() {
     f_live = false;
     if (f_left == 0) return;
@@ -208,6 +227,15 @@ __global__ void __launch_bounds__(kThreads, 2) split_attention_kernel(const Attn
       f_inner = s - pg * p.page_size;
       if (f_live) f_id = __ldg(p.page_table + (size_t)fw.b * p.max_pages + pg);
       if (fw.tile == 0 && __ldg(p.lens + fw.b) > 0 && (uint32_t)__ldg(p.lens + fw.b) > fw.len) bad_page = true;
+    } else if (p.compact) {
+      if (fw.b != list_b) {
+        list_b = fw.b;
+        const bool seen = lane < p.n_blocks && __ldg(p.mask + (size_t)fw.b * p.n_blocks + lane) != 0;
+        list = __fns(__ballot_sync(kFull, seen), 0, (int)lane + 1);
+      }
+      const uint32_t k = f_live ? s / p.block_len : 0u;
+      f_inner = __shfl_sync(kFull, list, k) * p.block_len + (s - k * p.block_len);
+      f_id = 1;
     } else {
       f_inner = s;
       f_id = 1;
@@ -251,6 +279,13 @@ __global__ void __launch_bounds__(kThreads, 2) split_attention_kernel(const Attn
     asm volatile("cp.async.commit_group;" ::: "memory");
     return there;
   };
+
+  // groups of which this CTA has a part: [0] one that began in an earlier CTA's share, [1] one that goes on in the next
+  struct Part {
+    uint32_t parts, c0, n_heads;
+    size_t out0;
+  };
+  Part open_parts[2] = {};
 
   uint32_t there[kStages];
   fetch();
@@ -376,7 +411,7 @@ __global__ void __launch_bounds__(kThreads, 2) split_attention_kernel(const Attn
     __syncthreads();
     const uint64_t first = group_first, end = first + at.tiles;  // units of the whole group
     const bool whole = first >= u0 && end <= u1;
-    const uint32_t c0 = (uint32_t)(((first + 1u) * ctas - 1u) / total), c1 = (uint32_t)((end * ctas - 1u) / total);
+    const uint32_t c0 = (uint32_t)quotient((first + 1u) * ctas - 1u, total), c1 = (uint32_t)quotient(end * ctas - 1u, total);
     float* const mine = p.ws.parts + (size_t)(2u * blockIdx.x + (blockIdx.x == c0 ? 1u : 0u)) * kPartFloats;
     const size_t out0 = ((size_t)at.b * p.n_tokens + t) * p.n_q_heads + h0;
     for (uint32_t x = tid; x < n_heads * D; x += kThreads) {
@@ -403,47 +438,12 @@ __global__ void __launch_bounds__(kThreads, 2) split_attention_kernel(const Attn
         }
       }
     }
-    if (!whole) {
-      const uint32_t parts = c1 - c0 + 1u;
-      __threadfence();
-      __syncthreads();
-      // atomicInc wraps to 0 with the last part, which is the state the next call needs
-      if (tid == 0) *flag = atomicInc(p.ws.counters + c0, parts - 1u) == parts - 1u;
-      __syncthreads();
-      if (*flag) {
-        __threadfence();
-        auto part_of = [&](uint32_t i) { return p.ws.parts + (size_t)(2u * (c0 + i) + (i == 0 ? 1u : 0u)) * kPartFloats; };
-        // the parts' factors, a head to a warp; then the sum in the order of the parts
-        float* const factor = so;
-        for (uint32_t h = warp; h < n_heads; h += kWarps) {
-          float M = -INFINITY, Ls = 0.f;
-          for (uint32_t i = lane; i < parts; i += 32u) M = fmaxf(M, __ldcg(part_of(i) + kHeads * D + h));
-#pragma unroll
-          for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(kFull, M, d));
-          const float ref = M == -INFINITY ? 0.f : M;
-          for (uint32_t i = lane; i < parts; i += 32u) {
-            const float f = exp2_fast(__ldcg(part_of(i) + kHeads * D + h) - ref);
-            Ls += f * __ldcg(part_of(i) + kHeads * D + kHeads + h);
-            factor[i * kHeads + h] = f;
-          }
-#pragma unroll
-          for (int d = 16; d > 0; d >>= 1) Ls += __shfl_xor_sync(kFull, Ls, d);
-          if (lane == 0) {
-            sm[h] = M;
-            sl[h] = Ls;
-          }
-        }
-        __syncthreads();
-        for (uint32_t x = tid; x < n_heads * D; x += kThreads) {
-          const uint32_t h = x / D, d = x % D;
-          float Os = 0.f;
-#pragma unroll 4
-          for (uint32_t i = 0; i < parts; ++i) Os += factor[i * kHeads + h] * __ldcg(part_of(i) + x);
-          const float M = sm[h], Ls = sl[h];
-          p.out[(out0 + h) * D + d] = __float2bfloat16_rn(Ls == 0.f ? 0.f : Os / Ls);
-          if (d == 0 && p.lse) p.lse[out0 + h] = Ls == 0.f ? -INFINITY : (M + log2f(Ls)) * 0.6931471805599453f;
-        }
-      }
+    if (!whole) {  // published when the share is done: a fence and an atomic here would hold up the loads
+      const Part g{c1 - c0 + 1u, c0, n_heads, out0};
+      if (blockIdx.x == c0)
+        open_parts[1] = g;
+      else
+        open_parts[0] = g;
     }
     __syncthreads();  // the merge area is free again
     group_first = end;
@@ -451,6 +451,84 @@ __global__ void __launch_bounds__(kThreads, 2) split_attention_kernel(const Attn
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
   if (PAGED && bad_page && p.status != nullptr) atomicOr(p.status, TQ_STATUS_BAD_PAGE);
+
+  // ---- the at most two groups that other CTAs have parts of as well ---------------------------------------
+  if (open_parts[0].parts == 0u && open_parts[1].parts == 0u) return;
+  if (tid == 0) {
+    // what the CTA wrote before the last barrier is published with this thread's fence; atomicInc wraps to 0 with the
+    // last part, which is the state the next call needs
+    __threadfence();
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      flag[k] = open_parts[k].parts != 0u && atomicInc(p.ws.counters + open_parts[k].c0, open_parts[k].parts - 1u) == open_parts[k].parts - 1u;
+    __threadfence();
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int k = 0; k < 2; ++k) {
+    if (!flag[k]) continue;
+    const Part g = k ? open_parts[1] : open_parts[0];
+    auto part_of = [&](uint32_t i) { return p.ws.parts + (size_t)(2u * (g.c0 + i) + (i == 0 ? 1u : 0u)) * kPartFloats; };
+    constexpr int kMine = (kHeads * D + kThreads - 1) / kThreads;  // outputs of a thread
+    constexpr uint32_t kEarly = 8;                // parts whose outputs are asked for before their factors are known
+    float early[kEarly][kMine];
+#pragma unroll
+    for (uint32_t i = 0; i < kEarly; ++i)
+#pragma unroll
+      for (int c = 0; c < kMine; ++c) {
+        const uint32_t x = c * kThreads + tid;
+        early[i][c] = i < g.parts && x < g.n_heads * D ? __ldcg(part_of(i) + x) : 0.f;
+      }
+    // the parts' factors, a head to a warp; then the sum in the order of the parts
+    float* const factor = so;
+    for (uint32_t h = warp; h < g.n_heads; h += kWarps) {
+      float M = -INFINITY, Ls = 0.f;  // of this lane's parts
+      for (uint32_t i = lane; i < g.parts; i += 32u) {
+        const float mi = __ldcg(part_of(i) + kHeads * D + h), li = __ldcg(part_of(i) + kHeads * D + kHeads + h);
+        const float mn = fmaxf(M, mi), r = mn == -INFINITY ? 0.f : mn;
+        Ls = Ls * exp2_fast(M - r) + li * exp2_fast(mi - r);
+        M = mn;
+        factor[i * kHeads + h] = mi;
+      }
+      float top = M;
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, d));
+      const float ref = top == -INFINITY ? 0.f : top;
+      Ls *= exp2_fast(M - ref);
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) Ls += __shfl_xor_sync(kFull, Ls, d);
+      for (uint32_t i = lane; i < g.parts; i += 32u) factor[i * kHeads + h] = exp2_fast(factor[i * kHeads + h] - ref);
+      if (lane == 0) {
+        sm[h] = top;
+        sl[h] = Ls;
+      }
+    }
+    __syncthreads();
+    float acc[kMine] = {};
+#pragma unroll
+    for (uint32_t i = 0; i < kEarly; ++i)
+#pragma unroll
+      for (int c = 0; c < kMine; ++c)
+        if (i < g.parts) acc[c] += factor[i * kHeads + (c * kThreads + tid) / D] * early[i][c];
+#pragma unroll 4
+    for (uint32_t i = kEarly; i < g.parts; ++i) {
+      const float* src = part_of(i);
+#pragma unroll
+      for (int c = 0; c < kMine; ++c) {
+        const uint32_t x = c * kThreads + tid;
+        if (x < g.n_heads * D) acc[c] += factor[i * kHeads + x / D] * __ldcg(src + x);
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < kMine; ++c) {
+      const uint32_t x = c * kThreads + tid, h = x / D, d = x % D;
+      if (x >= g.n_heads * D) continue;
+      const float M = sm[h], Ls = sl[h];
+      p.out[(g.out0 + h) * D + d] = __float2bfloat16_rn(Ls == 0.f ? 0.f : acc[c] / Ls);
+      if (d == 0 && p.lse) p.lse[g.out0 + h] = Ls == 0.f ? -INFINITY : (M + log2f(Ls)) * 0.6931471805599453f;
+    }
+    __syncthreads();
+  }
 }
 
 template <int D, bool PAGED>
@@ -459,7 +537,7 @@ int launch(AttnParams& p, cudaStream_t st) {
   constexpr size_t smem = Smem<D>::kTotal;
   const char* what = PAGED ? "paged attention launch" : "cross attention launch";
   if (int rc = tq_ensure_dynamic_smem((const void*)kern, smem, what)) return rc;
-  const uint32_t grid = min(2u * (uint32_t)sm_count(), kAttnMaxCtas);
+  const uint32_t grid = min((uint32_t)sm_count(), kAttnMaxCtas);
   return launch_pdl(kern, dim3(grid), kThreads, smem, st, what, p);
 }
 
@@ -490,7 +568,7 @@ extern "C" {
 
 int tq_attn_workspace_size(uint64_t* device_bytes) {
   if (!device_bytes) return TQ_ERR_INVALID_ARG;
-  const uint64_t ctas = min(2u * (uint32_t)sm_count(), kAttnMaxCtas);
+  const uint64_t ctas = min((uint32_t)sm_count(), kAttnMaxCtas);
   const uint64_t split = ctas * 2u * kPartFloats * sizeof(float), cross = tq_cross_workspace_bytes();
   *device_bytes = kAttnWsHeader + (split > cross ? split : cross);
   return TQ_OK;
@@ -582,6 +660,7 @@ int tq_cross_attention(const tq_encoder_kv* kv, const void* d_q, int64_t q_batch
   p.n_states = kv->n_states;
   p.block_len = d_mask ? block_len : 1u;
   p.n_blocks = d_mask ? (uint32_t)(((uint64_t)kv->n_states + block_len - 1u) / block_len) : 0u;
+  p.compact = d_mask != nullptr && n_tokens == 1 && p.n_blocks <= 32u;
   p.n_seqs = kv->n_seqs;
   p.n_tokens = n_tokens;
   p.n_q_heads = n_q_heads;

@@ -3,7 +3,7 @@
 //
 //   s = h + delta,  r = 1 / sqrt(mean_c s_c^2 + eps),  n_c = (s_c * r) * w_c
 //
-// One pass: a row's sums s stay in the registers of the threads that read it (8, 16 or 32 a thread), so
+// One pass: a row's sums s stay in the registers of the threads that read it (8 or 16 a thread), so
 // h and delta are read once and the row is scaled from registers when its sum of squares is known.
 // Everything is fp32; h_out is rounded to h's type after s has gone into the norm, out once.
 // A call moves 2-12 bytes per element for about 6 operations: memory bound, and for few rows bound by
@@ -42,42 +42,68 @@ __device__ __forceinline__ uint32_t column(uint32_t u, int e, uint32_t tid, uint
   return VEC ? (u * threads + tid) * 8u + (uint32_t)e : (u * 8u + (uint32_t)e) * threads + tid;
 }
 
-// TPR: threads of a row: 16 or 32 (several rows to a block of 128, shuffles only) or 0 (the whole block).
-template <int HT, int DT, bool VEC, int TPR, int NU>
-__global__ void __launch_bounds__(TPR ? 128 : (NU == 4 ? 512 : 1024)) rmsnorm_kernel(const NormParams p) {
+// The sums of a unit.
+template <int HT, int DT, class H, class Dl>
+__device__ __forceinline__ void add(const H& h, const Dl& d, float (&s)[8]) {
+  h.get(s);
+  if constexpr (DT != kNone) {
+    float x[8];
+    d.get(x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[e] += x[e];
+  }
+}
+__device__ __forceinline__ float squares(const float (&s)[8]) {
+  float sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sum = fmaf(s[e], s[e], sum);
+  return sum;
+}
+__device__ __forceinline__ void load_weights(const float* w, float (&f)[8]) {
+  Raw8<TQ_TYPE_F32> raw;
+  raw.load_cached(w, 0);
+  raw.get(f);
+}
+// 8 bits by the rule of tq_quantize_rows: amax is the row's largest magnitude (NaN if it has one), then IEEE division and
+// rounding half to even.
+__device__ __forceinline__ float scale_of(float amax) { return amax == 0.f ? 1.0f : __fdiv_rn(amax, 127.0f); }
+__device__ __forceinline__ void levels(const float (&n)[8], float scale, int8_t (&b)[8]) {
+  const float inv = 1.0f / scale;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    // the product with 1 / scale is within 2^-16 of the quotient: only near a half can the two round differently, and there
+    // the quotient itself is taken
+    const float v = n[e] * inv;
+    float r = rintf(v);
+    if (fabsf(fabsf(v - r) - 0.5f) < 1e-3f) r = rintf(__fdiv_rn(n[e], scale));
+    b[e] = scale == scale ? (int8_t)fminf(fmaxf(r, -127.f), 127.f) : (int8_t)0;
+  }
+}
+
+// One row to a block.
+template <int HT, int DT, bool VEC, int NU>
+__global__ void __launch_bounds__(1024) rmsnorm_kernel(const NormParams p) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const uint32_t threads = TPR ? TPR : blockDim.x;
-  const uint32_t tid = TPR ? threadIdx.x % (TPR ? TPR : 1) : threadIdx.x;
-  const uint32_t row = TPR ? blockIdx.x * (128u / (TPR ? TPR : 1)) + threadIdx.x / (TPR ? TPR : 1) : blockIdx.x;
-  const bool live = row < p.rows;
+  const uint32_t threads = blockDim.x, tid = threadIdx.x, row = blockIdx.x;
   asm volatile("griddepcontrol.wait;" ::: "memory");
 
   float s[NU][8];
-  const size_t hb = (size_t)row * p.h_stride, db = (size_t)row * p.delta_stride;
+  const size_t hb = (size_t)row * p.h_stride, db = (size_t)row * p.delta_stride, ob = (size_t)row * p.cols;
   if constexpr (VEC) {
     Raw8<HT> hr[NU];
     Raw8<DT == kNone ? TQ_TYPE_BF16 : DT> dr[NU];
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
       const uint32_t c = column<true>(u, 0, tid, threads);
-      if (live && c < p.cols) {
+      hr[u].clear();
+      dr[u].clear();
+      if (c < p.cols) {
         hr[u].load(p.h, hb + c);
         if constexpr (DT != kNone) dr[u].load(p.delta, db + c);
-      } else {
-        hr[u].clear();
-        if constexpr (DT != kNone) dr[u].clear();
       }
     }
 #pragma unroll
-    for (int u = 0; u < NU; ++u) {
-      hr[u].get(s[u]);
-      if constexpr (DT != kNone) {
-        float d[8];
-        dr[u].get(d);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s[u][e] += d[e];
-      }
-    }
+    for (int u = 0; u < NU; ++u) add<HT, DT>(hr[u], dr[u], s[u]);
   } else {
 #pragma unroll
     for (int u = 0; u < NU; ++u)
@@ -85,7 +111,7 @@ __global__ void __launch_bounds__(TPR ? 128 : (NU == 4 ? 512 : 1024)) rmsnorm_ke
       for (int e = 0; e < 8; ++e) {
         const uint32_t c = column<false>(u, e, tid, threads);
         float v = 0.f;
-        if (live && c < p.cols) {
+        if (c < p.cols) {
           v = load1<HT>(p.h, hb + c);
           if constexpr (DT != kNone) v += load1<DT>(p.delta, db + c);
         }
@@ -95,48 +121,27 @@ __global__ void __launch_bounds__(TPR ? 128 : (NU == 4 ? 512 : 1024)) rmsnorm_ke
 
   float sum = 0.f;
 #pragma unroll
-  for (int u = 0; u < NU; ++u)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sum = fmaf(s[u][e], s[u][e], sum);
+  for (int u = 0; u < NU; ++u) sum += squares(s[u]);
   __shared__ float red[2][32];
   const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
 #pragma unroll
-  for (int d = (TPR ? TPR : 32) / 2; d > 0; d >>= 1) sum += __shfl_xor_sync(kFull, sum, d);
-  if (TPR == 0) {
-    if (lane == 0) red[0][warp] = sum;
-    __syncthreads();
-    sum = lane < (blockDim.x >> 5) ? red[0][lane] : 0.f;
+  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(kFull, sum, d);
+  if (lane == 0) red[0][warp] = sum;
+  __syncthreads();
+  sum = lane < (blockDim.x >> 5) ? red[0][lane] : 0.f;
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(kFull, sum, d);
-  }
+  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(kFull, sum, d);
   const float r = 1.0f / sqrtf(sum / (float)p.cols + p.eps);
 
-  const size_t ob = (size_t)row * p.cols;
-  if (p.h_out != nullptr) {
-#pragma unroll
-    for (int u = 0; u < NU; ++u) {
-      if constexpr (VEC) {
-        const uint32_t c = column<true>(u, 0, tid, threads);
-        if (live && c < p.cols) store8<HT>(p.h_out, hb + c, s[u]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const uint32_t c = column<false>(u, e, tid, threads);
-          if (live && c < p.cols) store1<HT>(p.h_out, hb + c, s[u][e]);
-        }
-      }
-    }
-  }
   float amax = 0.f;
 #pragma unroll
   for (int u = 0; u < NU; ++u) {
     if constexpr (VEC) {
       const uint32_t c = column<true>(u, 0, tid, threads);
-      if (!(live && c < p.cols)) continue;
+      if (c >= p.cols) continue;
+      if (p.h_out) store8<HT>(p.h_out, hb + c, s[u]);
       float w[8];
-      Raw8<TQ_TYPE_F32> wr;
-      wr.load_cached(p.w, c);
-      wr.get(w);
+      load_weights(p.w + c, w);
 #pragma unroll
       for (int e = 0; e < 8; ++e) s[u][e] = s[u][e] * r * w[e];
       if (p.out) store8<TQ_TYPE_BF16>(p.out, ob + c, s[u]);
@@ -144,7 +149,8 @@ __global__ void __launch_bounds__(TPR ? 128 : (NU == 4 ? 512 : 1024)) rmsnorm_ke
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const uint32_t c = column<false>(u, e, tid, threads);
-        if (!(live && c < p.cols)) continue;
+        if (c >= p.cols) continue;
+        if (p.h_out) store1<HT>(p.h_out, hb + c, s[u][e]);
         s[u][e] = s[u][e] * r * __ldg(p.w + c);
         if (p.out) store1<TQ_TYPE_BF16>(p.out, ob + c, s[u][e]);
       }
@@ -154,59 +160,115 @@ __global__ void __launch_bounds__(TPR ? 128 : (NU == 4 ? 512 : 1024)) rmsnorm_ke
   }
   if (p.q == nullptr) return;
 
-  // 8 bits: the row's largest magnitude (a NaN anywhere makes it NaN), then IEEE division and rounding
-  // half to even, as tq_quantize_rows does it
 #pragma unroll
-  for (int d = (TPR ? TPR : 32) / 2; d > 0; d >>= 1) amax = max_nan(amax, __shfl_xor_sync(kFull, amax, d));
-  if (TPR == 0) {
-    if (lane == 0) red[1][warp] = amax;
-    __syncthreads();
-    amax = lane < (blockDim.x >> 5) ? red[1][lane] : 0.f;
+  for (int d = 16; d > 0; d >>= 1) amax = max_nan(amax, __shfl_xor_sync(kFull, amax, d));
+  if (lane == 0) red[1][warp] = amax;
+  __syncthreads();
+  amax = lane < (blockDim.x >> 5) ? red[1][lane] : 0.f;
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) amax = max_nan(amax, __shfl_xor_sync(kFull, amax, d));
-  }
-  const float scale = amax == 0.f ? 1.0f : __fdiv_rn(amax, 127.0f);
-  if (live && tid == 0) p.q_scale[row] = scale;
+  for (int d = 16; d > 0; d >>= 1) amax = max_nan(amax, __shfl_xor_sync(kFull, amax, d));
+  const float scale = scale_of(amax);
+  if (tid == 0) p.q_scale[row] = scale;
 #pragma unroll
   for (int u = 0; u < NU; ++u) {
     int8_t b[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float v = rintf(__fdiv_rn(s[u][e], scale));
-      b[e] = amax == amax ? (int8_t)fminf(fmaxf(v, -127.f), 127.f) : (int8_t)0;
-    }
+    levels(s[u], scale, b);
     if constexpr (VEC) {
       const uint32_t c = column<true>(u, 0, tid, threads);
-      if (live && c < p.cols) *reinterpret_cast<uint2*>(p.q + ob + c) = *reinterpret_cast<const uint2*>(b);
+      if (c < p.cols) *reinterpret_cast<uint2*>(p.q + ob + c) = *reinterpret_cast<const uint2*>(b);
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const uint32_t c = column<false>(u, e, tid, threads);
-        if (live && c < p.cols) p.q[ob + c] = b[e];
+        if (c < p.cols) p.q[ob + c] = b[e];
       }
     }
   }
 }
 
+// Short rows (heads): TPR lanes to a row, one unit of eight columns a lane, shuffles only; a lane works on NR rows at once, so
+// that it has NR loads under way, with one load of its weights.  Rows that are not aligned for units go the long way above.
+constexpr uint32_t kShortThreads = 128;
+template <int HT, int DT, int TPR, int NR>
+__global__ void __launch_bounds__(kShortThreads) rmsnorm_short_kernel(const NormParams p) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  constexpr uint32_t kSide = kShortThreads / TPR;
+  const uint32_t c = threadIdx.x % TPR * 8u, row0 = blockIdx.x * (kSide * NR) + threadIdx.x / TPR;
+  const bool live = c < p.cols;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+
+  Raw8<HT> hr[NR];
+  Raw8<DT == kNone ? TQ_TYPE_BF16 : DT> dr[NR];
+#pragma unroll
+  for (int k = 0; k < NR; ++k) {
+    const uint32_t row = row0 + k * kSide;
+    hr[k].clear();
+    dr[k].clear();
+    if (live && row < p.rows) {
+      hr[k].load(p.h, (size_t)row * p.h_stride + c);
+      if constexpr (DT != kNone) dr[k].load(p.delta, (size_t)row * p.delta_stride + c);
+    }
+  }
+  float w[8] = {};
+  if (live) load_weights(p.w + c, w);
+#pragma unroll
+  for (int k = 0; k < NR; ++k) {
+    const uint32_t row = row0 + k * kSide;
+    const bool mine = live && row < p.rows;
+    float s[8];
+    add<HT, DT>(hr[k], dr[k], s);
+    float sum = squares(s);
+#pragma unroll
+    for (int d = TPR / 2; d > 0; d >>= 1) sum += __shfl_xor_sync(kFull, sum, d);
+    const float r = 1.0f / sqrtf(sum / (float)p.cols + p.eps);
+    if (mine && p.h_out) store8<HT>(p.h_out, (size_t)row * p.h_stride + c, s);
+    float amax = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      s[e] = s[e] * r * w[e];
+      if (live) amax = max_nan(amax, fabsf(s[e]));
+    }
+    if (mine && p.out) store8<TQ_TYPE_BF16>(p.out, (size_t)row * p.cols + c, s);
+    if (p.q == nullptr) continue;
+#pragma unroll
+    for (int d = TPR / 2; d > 0; d >>= 1) amax = max_nan(amax, __shfl_xor_sync(kFull, amax, d));
+    const float scale = scale_of(amax);
+    int8_t b[8];
+    levels(s, scale, b);
+    if (mine) *reinterpret_cast<uint2*>(p.q + (size_t)row * p.cols + c) = *reinterpret_cast<const uint2*>(b);
+    if (mine && c == 0u) p.q_scale[row] = scale;
+  }
+}
+
 template <int HT, int DT, bool VEC>
 int launch(const NormParams& p, cudaStream_t st) {
-  const uint32_t units = (p.cols + 7u) / 8u;
-  if (units <= 16u) return launch_pdl(rmsnorm_kernel<HT, DT, VEC, 16, 1>, dim3((p.rows + 7u) / 8u), 128, 0, st, "rmsnorm launch", p);
-  if (units <= 32u) return launch_pdl(rmsnorm_kernel<HT, DT, VEC, 32, 1>, dim3((p.rows + 3u) / 4u), 128, 0, st, "rmsnorm launch", p);
-  // few rows: as many threads as the row has units, for latency; many rows: four units a thread, for
-  // bytes in flight (512 threads of four units or 1024 of two are TQ_NORM_MAX_COLS columns)
-  const bool few = p.rows < 2u * (uint32_t)sm_count();
-  auto threads_for = [&](uint32_t nu) { return ((units + nu - 1u) / nu + 31u) / 32u * 32u; };
-  if (!few) return launch_pdl(rmsnorm_kernel<HT, DT, VEC, 0, 4>, dim3(p.rows), threads_for(4), 0, st, "rmsnorm launch", p);
-  if (units <= 1024u) return launch_pdl(rmsnorm_kernel<HT, DT, VEC, 0, 1>, dim3(p.rows), threads_for(1), 0, st, "rmsnorm launch", p);
-  return launch_pdl(rmsnorm_kernel<HT, DT, VEC, 0, 2>, dim3(p.rows), threads_for(2), 0, st, "rmsnorm launch", p);
+  const char* what = "rmsnorm launch";
+  const uint32_t units = (p.cols + 7u) / 8u, sms = (uint32_t)sm_count();
+  if constexpr (VEC) {
+    if (units <= 32u) {
+      // one row a lane until the device is full of blocks, four beyond (51232 rows of 128: 7.9 us with one, 5.7 with four)
+      auto grid = [&](uint32_t tpr, uint32_t nr) { return (p.rows + kShortThreads / tpr * nr - 1u) / (kShortThreads / tpr * nr); };
+      const uint32_t tpr = units <= 16u ? 16u : 32u;
+      const bool many = grid(tpr, 4u) >= 4u * sms;
+      if (tpr == 16u)
+        return many ? launch_pdl(rmsnorm_short_kernel<HT, DT, 16, 4>, dim3(grid(16, 4)), kShortThreads, 0, st, what, p)
+                    : launch_pdl(rmsnorm_short_kernel<HT, DT, 16, 1>, dim3(grid(16, 1)), kShortThreads, 0, st, what, p);
+      return many ? launch_pdl(rmsnorm_short_kernel<HT, DT, 32, 4>, dim3(grid(32, 4)), kShortThreads, 0, st, what, p)
+                  : launch_pdl(rmsnorm_short_kernel<HT, DT, 32, 1>, dim3(grid(32, 1)), kShortThreads, 0, st, what, p);
+    }
+  }
+  // One unit a thread where rows are few and the latency of a row counts, two where there are many (2049 rows of 8192 fp32
+  // with an fp32 delta: 38.2 us with two, 39.7 with four; alone 53.8 with one, 50.6 with two).  1024 threads of two units are
+  // TQ_NORM_MAX_COLS columns.
+  auto threads = [&](uint32_t nu) { return ((units + nu - 1u) / nu + 31u) / 32u * 32u; };
+  if (p.rows < 2u * sms && units <= 1024u) return launch_pdl(rmsnorm_kernel<HT, DT, VEC, 1>, dim3(p.rows), threads(1), 0, st, what, p);
+  return launch_pdl(rmsnorm_kernel<HT, DT, VEC, 2>, dim3(p.rows), threads(2), 0, st, what, p);
 }
 
 template <int HT, int DT>
 int launch_vec(const NormParams& p, cudaStream_t st) {
   auto fits = [](const void* ptr, int64_t stride, int type) {
-    const int64_t step = type == TQ_TYPE_F32 ? 4 : 8;  // elements in 16 bytes
-    return ((uintptr_t)ptr & 15u) == 0 && stride % step == 0;
+    return ((uintptr_t)ptr & (type == TQ_TYPE_F32 ? 31u : 15u)) == 0 && stride % 8 == 0;  // eight elements are one access
   };
   bool vec = p.cols % 8u == 0 && fits(p.h, p.h_stride, HT) && fits(p.w, 0, TQ_TYPE_F32);
   if (DT != kNone) vec = vec && fits(p.delta, p.delta_stride, DT);

@@ -18,6 +18,7 @@ namespace {
 using namespace tq_ops;
 
 constexpr uint32_t kRopeThreads = 256;
+constexpr uint32_t kAhead = 2;
 
 struct RopeParams {
   const void* q;
@@ -34,8 +35,8 @@ struct RopeParams {
   uint32_t n_axes;
 };
 
-// Eight elements of a head as two runs of four: the first and second members of four pairs, or eight
-// consecutive elements (interleaved pairs, elements that pass unchanged).
+// Eight elements of a head as two runs of four, so that neighbouring lanes read neighbouring runs whatever the type and the
+// order of the pairs (eight consecutive fp32 to a lane in two accesses would touch every sector twice).
 template <int TYPE>
 struct Raw4x2 {
   uint4 a, b;
@@ -67,11 +68,24 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopePar
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const uint32_t D = p.cache.head_dim, per_head = D / 8u, side = kRopeThreads / per_head;
   const uint32_t j = threadIdx.x % per_head, t = blockIdx.x;
-  const uint32_t pairs = p.rot_dim / 2u, pair0 = 4u * j;
-  const bool turns = pair0 < pairs;
-  // where this thread's eight elements of a head lie
-  const uint32_t e0 = INTERLEAVED ? 8u * j : (turns ? pair0 : p.rot_dim + 2u * (pair0 - pairs));
-  const uint32_t e1 = !INTERLEAVED && turns ? pairs + pair0 : e0 + 4u;
+  const uint32_t pairs = p.rot_dim / 2u;
+  // where this thread's two runs lie, the first pair of each two of its four, and whether the runs turn
+  uint32_t e0, e1, pair_a, pair_b;
+  bool turn_a, turn_b;
+  if (INTERLEAVED) {  // two pairs to a run
+    e0 = 4u * j;
+    e1 = D / 2u + 4u * j;
+    pair_a = e0 / 2u;
+    pair_b = e1 / 2u;
+    turn_a = e0 < p.rot_dim;
+    turn_b = e1 < p.rot_dim;
+  } else {  // first and second members of four pairs, or eight elements past the pairs
+    turn_a = turn_b = 4u * j < pairs;
+    e0 = turn_a ? 4u * j : 8u * j;
+    e1 = turn_a ? pairs + 4u * j : e0 + 4u;
+    pair_a = 4u * j;
+    pair_b = pair_a + 2u;
+  }
   asm volatile("griddepcontrol.wait;" ::: "memory");
 
   const int32_t slot = p.slots[t];
@@ -86,47 +100,65 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopePar
   const bool keep = in_pool && known;
   const size_t slot_at = keep ? (size_t)page * p.cache.page_stride + (size_t)((uint32_t)slot % p.cache.page_size) * p.cache.slot_stride : 0;
 
-  float cs[4] = {1.f, 1.f, 1.f, 1.f}, sn[4] = {0.f, 0.f, 0.f, 0.f};
-  if (turns && known) {
+  // Heads in order: queries, keys, values.  A thread asks for kAhead of its heads before it uses the first, and for the first of
+  // them before the cosines and sines, which wait for the positions.
+  const uint32_t K = p.cache.n_kv_heads, heads = p.n_q_heads + (keep ? 2u * K : 0u), step = gridDim.y * side;
+  Raw4x2<TYPE> raw[kAhead];
+  auto kind_of = [&](uint32_t n) { return n < p.n_q_heads ? 0u : (n < p.n_q_heads + K ? 1u : 2u); };
+  auto head_of = [&](uint32_t n) { return n < p.n_q_heads ? n : (n < p.n_q_heads + K ? n - p.n_q_heads : n - p.n_q_heads - K); };
+  auto load = [&](uint32_t n0) {
 #pragma unroll
-    for (uint32_t i = 0; i < 4; ++i) {
-      uint32_t a = 0;
-      while (pair0 + i >= p.axis_end[a]) ++a;  // the sections add up to all pairs
-      const float* row = p.table + (size_t)p.positions[(size_t)a * p.n_tokens + t] * p.rot_dim + pair0 + i;
-      cs[i] = __ldg(row);
-      sn[i] = __ldg(row + pairs);
+    for (uint32_t u = 0; u < kAhead; ++u) {
+      const uint32_t n = n0 + u * step;
+      if (n >= heads) continue;
+      const uint32_t kind = kind_of(n);
+      const void* src = kind == 0u ? p.q : (kind == 1u ? p.k : p.v);
+      const size_t row = (size_t)t * (kind == 0u ? p.q_stride : (kind == 1u ? p.k_stride : p.v_stride)) + (size_t)head_of(n) * D;
+      raw[u].load(src, row + e0, row + e1);
     }
+  };
+  uint32_t n0 = blockIdx.y * side + threadIdx.x / per_head;
+  load(n0);
+
+  float cs[4] = {1.f, 1.f, 1.f, 1.f}, sn[4] = {0.f, 0.f, 0.f, 0.f};  
+#pragma unroll
+  for (uint32_t i = 0; i < 4; ++i) {
+    if (!known || !(i < 2 ? turn_a : turn_b)) continue;
+    const uint32_t pair = i < 2 ? pair_a + i : pair_b + i - 2u;
+    uint32_t a = 0;
+    while (pair >= p.axis_end[a]) ++a;  // the sections add up to all pairs
+    const float* row = p.table + (size_t)p.positions[(size_t)a * p.n_tokens + t] * p.rot_dim + pair;
+    cs[i] = __ldg(row);
+    sn[i] = __ldg(row + pairs);
   }
   if (!known) cs[0] = cs[1] = cs[2] = cs[3] = __int_as_float(0x7FC00000);
 
-  const uint32_t K = p.cache.n_kv_heads, heads = p.n_q_heads + 2u * K;
-  for (uint32_t n = blockIdx.y * side + threadIdx.x / per_head; n < heads; n += gridDim.y * side) {
-    // heads in order: queries, keys, values
-    const uint32_t kind = n < p.n_q_heads ? 0u : (n < p.n_q_heads + K ? 1u : 2u);
-    if (kind != 0u && !keep) continue;
-    const uint32_t h = kind == 0u ? n : (kind == 1u ? n - p.n_q_heads : n - p.n_q_heads - K);
-    const void* src = kind == 0u ? p.q : (kind == 1u ? p.k : p.v);
-    const size_t row = (size_t)t * (kind == 0u ? p.q_stride : (kind == 1u ? p.k_stride : p.v_stride)) + (size_t)h * D;
-    const bool plain = kind == 2u;
-    Raw4x2<TYPE> raw;
-    raw.load(src, row + e0, row + e1);
-    float f[8];
-    raw.get(f);
-    if (!plain && (turns || !known)) {
+  for (; n0 < heads; n0 += kAhead * step) {
+    if (n0 != blockIdx.y * side + threadIdx.x / per_head) load(n0);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float& x = INTERLEAVED ? f[2 * i] : f[i];
-        float& y = INTERLEAVED ? f[2 * i + 1] : f[4 + i];
-        const float a = x * cs[i] - y * sn[i], b = x * sn[i] + y * cs[i];
-        x = a;
-        y = b;
+    for (uint32_t u = 0; u < kAhead; ++u) {
+      const uint32_t n = n0 + u * step;
+      if (n >= heads) continue;
+      const uint32_t kind = kind_of(n), h = head_of(n);
+      float f[8];
+      raw[u].get(f);
+      if (kind != 2u && (turn_a || turn_b || !known)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (!(i < 2 ? turn_a : turn_b) && known) continue;
+          float& x = INTERLEAVED ? f[2 * i] : f[i];
+          float& y = INTERLEAVED ? f[2 * i + 1] : f[4 + i];
+          const float a = x * cs[i] - y * sn[i], b = x * sn[i] + y * cs[i];
+          x = a;
+          y = b;
+        }
       }
+      __nv_bfloat16* dst = kind == 0u ? p.q_out + ((size_t)t * p.n_q_heads + h) * D
+                                      : (__nv_bfloat16*)(kind == 1u ? p.cache.d_k : p.cache.d_v) + slot_at + (size_t)h * p.cache.head_stride;
+      const uint4 o = pack8(f);
+      *reinterpret_cast<uint2*>(dst + e0) = make_uint2(o.x, o.y);
+      *reinterpret_cast<uint2*>(dst + e1) = make_uint2(o.z, o.w);
     }
-    __nv_bfloat16* dst = kind == 0u ? p.q_out + ((size_t)t * p.n_q_heads + h) * D
-                                    : (__nv_bfloat16*)(kind == 1u ? p.cache.d_k : p.cache.d_v) + slot_at + (size_t)h * p.cache.head_stride;
-    const uint4 o = pack8(f);
-    *reinterpret_cast<uint2*>(dst + e0) = make_uint2(o.x, o.y);
-    *reinterpret_cast<uint2*>(dst + e1) = make_uint2(o.z, o.w);
   }
 }
 
