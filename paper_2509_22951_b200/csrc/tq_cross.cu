@@ -349,13 +349,27 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
       return n;
     };
     uint64_t total = 0;
-    for (uint32_t b = lane; b < p.n_seqs; b += 32u) total += head_units(b);
+    uint32_t most = 0, least = 0xFFFFFFFFu;  // units of a group
+    for (uint32_t b = lane; b < p.n_seqs; b += 32u) {
+      total += head_units(b);
+      for (uint32_t q = 0; q < (p.counted ? p.row_tiles : 1u); ++q) {
+        const uint32_t n = units(b, q);
+        most = max(most, n);
+        least = min(least, n);
+      }
+    }
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) total += __shfl_xor_sync(kFull, total, d);
+    for (int d = 16; d > 0; d >>= 1) {
+      total += __shfl_xor_sync(kFull, total, d);
+      most = max(most, __shfl_xor_sync(kFull, most, d));
+      least = min(least, __shfl_xor_sync(kFull, least, d));
+    }
     total *= p.n_kv_heads;
     const uint32_t ctas = (uint32_t)min((uint64_t)gridDim.x, total);
+    // the longest share without cuts: whole groups of one size, or up to one group over the mean
     const uint64_t n_groups = (uint64_t)p.n_seqs * p.n_kv_heads * p.row_tiles;
-    const bool cut = (n_groups + ctas - 1u) / ctas * (total / n_groups) > total / ctas + kCutTiles;
+    const uint64_t longest = most == least ? (n_groups + ctas - 1u) / ctas * most : total / ctas + most;
+    const bool cut = longest > total / ctas + kCutTiles;
     uint64_t u0 = 0, u1 = 0;  // this CTA's share; without cuts, the groups that start in it
     if (blockIdx.x < ctas) {
       u0 = total * blockIdx.x / ctas;
