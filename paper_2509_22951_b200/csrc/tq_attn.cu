@@ -560,6 +560,7 @@ tq_attn_ws tq_attn_ws_plan(void* d_ws, uint64_t ws_bytes) {
   if (misaligned(d_ws, 256) || tq_attn_workspace_size(&need) != TQ_OK || ws_bytes < need) return w;
   w.counters = static_cast<uint32_t*>(d_ws);
   w.status = w.counters + kAttnMaxCtas;
+  w.open = reinterpret_cast<uint4*>(static_cast<uint8_t*>(d_ws) + kAttnWsOpen);
   w.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(d_ws) + kAttnWsHeader);
   return w;
 }

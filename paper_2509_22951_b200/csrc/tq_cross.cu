@@ -10,8 +10,9 @@
 // Work.  The G query heads that share a key-value head and the tokens are one list of rows (row r = token
 // r / G, head r % G); 256 of them are a group's tile.  The units are (sequence, key-value head, tile of
 // rows, 128 states), and, as in the one-token kernel, each CTA takes an equal share of consecutive units:
-// a group that lies in several shares leaves its parts in the workspace and the CTA that finishes last
-// joins them in order.  So short prompts use all SMs too, and long ones have no last wave.
+// a group that lies in several shares leaves its parts in the workspace, and a second, small kernel on all SMs joins
+// them in order.  (Joined by the CTA that finishes last: 1 x 17 tokens, 64 / 8 heads, 6404 states, 19 parts to a group: 77 us
+// instead of 38; 1 x 600 tokens, two or three parts: 132.8 instead of 135.3.)  So short prompts use all SMs too, and long ones have no last wave.
 //
 // CTA, one to an SM.  Warp 8 loads: it decides which tiles of states some row of the group
 // sees, announces them one by one in a ring of entries that all roles follow, and brings their K and V
@@ -103,11 +104,10 @@ struct CrossSmem {
   static constexpr uint32_t kStages = D == 128 ? 5 : 8;
   static constexpr uint32_t kOffKv = 2 * kQHalf;
   static constexpr uint32_t kOffMisc = kOffKv + kStages * kStageBytes;
-  // misc: [0] dead flag, [4] tensor-memory base, [8] join flag, barriers from 16 on, entries behind them
+  // misc: [0] dead flag, [4] tensor-memory base, barriers from 16 on, entries behind them
   static constexpr uint32_t kBarKvFull = 16, kBarKvEmpty = kBarKvFull + 8 * kStages, kBarQFull = kBarKvEmpty + 8 * kStages;
   static constexpr uint32_t kBarSFull = kBarQFull + 16, kBarPFull = kBarSFull + 16, kBarODone = kBarPFull + 16 * kChunks;
-  static constexpr uint32_t kBarJoin = kBarODone + 16;
-  static constexpr uint32_t kBarEFull = kBarJoin + 8, kBarEEmpty = kBarEFull + 8 * kEntries;
+  static constexpr uint32_t kBarEFull = kBarODone + 16, kBarEEmpty = kBarEFull + 8 * kEntries;
   static constexpr uint32_t kOffEntries = (kBarEEmpty + 8 * kEntries + 15) / 16 * 16;
   static_assert(sizeof(Entry) % 16 == 0, "entries are read in 16-byte words");
   static constexpr uint32_t kOffCounts = kOffEntries + kEntries * sizeof(Entry);
@@ -232,7 +232,6 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
   const uint32_t smem0 = smem_u32(smem), misc = smem0 + L::kOffMisc;
   volatile uint32_t* const dead = reinterpret_cast<uint32_t*>(smem + L::kOffMisc);
   uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(smem + L::kOffMisc + 4);
-  uint32_t* const join_flag = reinterpret_cast<uint32_t*>(smem + L::kOffMisc + 8);
   const uint32_t entries = misc + L::kOffEntries;
   // the same in all lanes, and known to be: what depends on it alone stays on the uniform data path
   const uint32_t warp = __shfl_sync(kFull, threadIdx.x >> 5, 0), lane = threadIdx.x & 31u;
@@ -254,7 +253,6 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
       mbar_init(bar(L::kBarEFull, i), 1);
       mbar_init(bar(L::kBarEEmpty, i), kSoftWarps + 1);
     }
-    mbar_init(bar(L::kBarJoin, 0), kSoftWarps);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kMmaWarp) {
@@ -435,6 +433,7 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
         ++st_round;
       }
     };
+    uint4 open = make_uint4(0u, 0u, 0u, 0u);  // the group that begins in this share and goes on in the next: its parts, b, kvh, qt
     for (; first < u1 && b < p.n_seqs && ok; next_group()) {
       const uint32_t len = states_of(p, b);
       // this CTA's units of the group
@@ -499,7 +498,9 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
       e.c0 = (uint32_t)(((first + 1u) * ctas - 1u) / total);
       e.parts = !cut || (first >= u0 && end <= u1) ? 1u : (uint32_t)((end * ctas - 1u) / total) - e.c0 + 1u;
       announce(e);
+      if (e.parts > 1u && first >= u0) open = make_uint4(e.parts, b, kvh, qt);
     }
+    if (lane == 0) p.ws.open[blockIdx.x] = open;
     if (ok) {
       Entry e{};
       e.ctl = kStop;
@@ -640,13 +641,6 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(L::kBarQFull, w));
-    };
-    uint32_t met = 0;
-    auto meet = [&]() {  // the eight softmax warps (a bounded wait, as every other)
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(L::kBarJoin, 0));
-      wait(bar(L::kBarJoin, 0), met & 1u);
-      ++met;
     };
     // bit i: this row sees state s0 + i
     auto visible = [&](const Entry& e, uint32_t (&bits)[4]) {
@@ -820,7 +814,7 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
         for (int k = 0; k < 32; ++k) nan = nan || __uint_as_float(o[k]) != __uint_as_float(o[k]);
         if (whole) {
           write(i, o);
-        } else {
+        } else if (live) {
 #pragma unroll
           for (int k = 0; k < 8; ++k) reinterpret_cast<uint4*>(mine)[(8 * i + k) * kRows + slot] = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
         }
@@ -870,53 +864,10 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
           }
         }
       }
-      if (whole) continue;
-      mine[kRows * 128 + slot] = m;
-      mine[kRows * 129 + slot] = l;
-      meet();
-      if (!ok) break;
-      if (threadIdx.x == 0) {
-        // what the warps wrote before they met is published with this thread's fence; atomicInc wraps to 0 with the last
-        // part, which is the state the next call needs
-        __threadfence();
-        *join_flag = atomicInc(p.ws.counters + g.c0, g.parts - 1u) == g.parts - 1u;
-        __threadfence();
+      if (!whole && live) {
+        mine[kRows * 128 + slot] = m;
+        mine[kRows * 129 + slot] = l;
       }
-      meet();
-      if (!ok) break;
-      if (*join_flag) {
-        const uint32_t own = blockIdx.x - g.c0;
-        float M = -INFINITY;
-#pragma unroll 4
-        for (uint32_t x = 0; x < g.parts; ++x) M = fmaxf(M, __ldcg(part(x) + kRows * 128 + slot));
-        const float ref = M == -INFINITY ? 0.f : M;
-        l = 0.f;
-#pragma unroll 4
-        for (uint32_t x = 0; x < g.parts; ++x) l += exp2_fast(__ldcg(part(x) + kRows * 128 + slot) - ref) * __ldcg(part(x) + kRows * 129 + slot);
-        const float m_own = m;
-        m = M;
-        constexpr int kCols = 64;  // 16 loads under way a thread
-#pragma unroll 1
-        for (int i = 0; i < D / kCols; ++i) {
-          float o[kCols];
-#pragma unroll
-          for (int k = 0; k < kCols; ++k) o[k] = 0.f;
-#pragma unroll 1
-          for (uint32_t x = 0; x < g.parts; ++x) {  // in the order of the parts
-            float4 y[kCols / 4];
-#pragma unroll
-            for (int k = 0; k < kCols / 4; ++k) y[k] = __ldcg(reinterpret_cast<const float4*>(part(x)) + (kCols / 4 * i + k) * kRows + slot);
-            const float f = exp2_fast((x == own ? m_own : __ldcg(part(x) + kRows * 128 + slot)) - ref);
-#pragma unroll
-            for (int k = 0; k < kCols / 4; ++k) {
-              o[4 * k] += f * y[k].x, o[4 * k + 1] += f * y[k].y, o[4 * k + 2] += f * y[k].z, o[4 * k + 3] += f * y[k].w;
-            }
-          }
-          write(2 * i, reinterpret_cast<const uint32_t(&)[32]>(o[0]));
-          write(2 * i + 1, reinterpret_cast<const uint32_t(&)[32]>(o[32]));
-        }
-      }
-      meet();  // the flag has been read
     }
   }
 
@@ -932,6 +883,63 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
     tmem_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
   }
+}
+
+// Joins the parts of the groups that were cut.  grid (CTAs of the kernel above, slices of 32 rows): block (c, y) has the group
+// that begins in CTA c's share and goes on, if there is one; a thread has a row and every eighth set of four columns, and adds
+// the parts up in their order.
+constexpr uint32_t kJoinRows = 32, kJoinThreads = 256;
+template <int D>
+__global__ void __launch_bounds__(kJoinThreads) cross_join_kernel(const CrossParams p) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const uint4 g = p.ws.open[blockIdx.x];  // parts, b, kvh, qt
+  if (g.x == 0u) return;
+  const uint32_t slot = blockIdx.y * kJoinRows + threadIdx.x % kJoinRows, row = g.w * kRows + slot;
+  if (row >= p.rows) return;
+  constexpr uint32_t kGroups = kJoinThreads / kJoinRows;
+  constexpr int kMine = D / 4 / kGroups, kAhead = 4;
+  const uint32_t first = threadIdx.x / kJoinRows;
+  auto part = [&](uint32_t i) { return p.ws.parts + (size_t)(2u * (blockIdx.x + i) + (i == 0u ? 1u : 0u)) * kCrossPartFloats; };
+  float M = -INFINITY, l = 0.f;
+  float4 o[kMine];
+#pragma unroll
+  for (int k = 0; k < kMine; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (uint32_t i0 = 0; i0 < g.x; i0 += kAhead) {
+    float4 y[kAhead][kMine];
+    float mi[kAhead], li[kAhead];
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+      const bool there = i0 + a < g.x;
+      const float* src = part(there ? i0 + a : i0);
+      mi[a] = there ? __ldcg(src + kRows * 128 + slot) : -INFINITY;
+      li[a] = there ? __ldcg(src + kRows * 129 + slot) : 0.f;
+#pragma unroll
+      for (int k = 0; k < kMine; ++k)
+        y[a][k] = there ? __ldcg(reinterpret_cast<const float4*>(src) + (first + k * kGroups) * kRows + slot) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+      const float mn = fmaxf(M, mi[a]), ref = mn == -INFINITY ? 0.f : mn, f = exp2_fast(M - ref), h = exp2_fast(mi[a] - ref);
+      M = mn;
+      l = l * f + li[a] * h;
+#pragma unroll
+      for (int k = 0; k < kMine; ++k) {
+        o[k].x = o[k].x * f + y[a][k].x * h;
+        o[k].y = o[k].y * f + y[a][k].y * h;
+        o[k].z = o[k].z * f + y[a][k].z * h;
+        o[k].w = o[k].w * f + y[a][k].w * h;
+      }
+    }
+  }
+  const size_t at = ((size_t)g.y * p.n_tokens + row / p.group) * p.n_q_heads + g.z * p.group + row % p.group;
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+#pragma unroll
+  for (int k = 0; k < kMine; ++k) {
+    const uint2 v = l == 0.f ? make_uint2(0u, 0u) : make_uint2(pack_bf16(o[k].x * inv, o[k].y * inv), pack_bf16(o[k].z * inv, o[k].w * inv));
+    *reinterpret_cast<uint2*>(p.out + at * D + 4u * (first + k * kGroups)) = v;
+  }
+  if (first == 0u && p.lse) p.lse[at] = l == 0.f ? -INFINITY : (M + log2f(l)) * 0.6931471805599453f;
 }
 
 // The tensor map of K or V: (column, state, head, sequence), boxes of 64 columns x 128 states, 128-byte swizzle.
@@ -960,7 +968,8 @@ int launch(const CrossParams& p, const CUtensorMap& k_map, const CUtensorMap& v_
   }();
   if (256 * kSoftRegs + 128 * kOtherRegs > kCrossThreads * regs) return tq_cuda_status((int)cudaErrorInvalidConfiguration, what);
   const uint32_t grid = min((uint32_t)sm_count(), kAttnMaxCtas);
-  return launch_pdl(kern, dim3(grid), kCrossThreads, smem, st, what, p, k_map, v_map);
+  if (int rc = launch_pdl(kern, dim3(grid), kCrossThreads, smem, st, what, p, k_map, v_map)) return rc;
+  return launch_pdl(cross_join_kernel<D>, dim3(grid, min(kRows, p.rows + kJoinRows - 1u) / kJoinRows), kJoinThreads, 0, st, "cross attention (join) launch", p);
 }
 
 }  // namespace

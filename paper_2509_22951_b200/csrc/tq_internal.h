@@ -236,14 +236,16 @@ int tq_dict_from_ranked(const uint32_t* keys, const uint64_t* counts, uint32_t K
 int tq_check_cache(const tq_kv_cache* cache);
 
 // Plan of the attention workspace: counters (one per CTA that can be the first of a split group; every
-// call leaves them zero), the status word, then the partial results of the CTAs.
+// call leaves them zero), the status word, the groups that go on past a CTA's share (parts, sequence, key-value head, tile of
+// rows; written and read by one call), then the partial results of the CTAs.
 constexpr uint32_t kAttnMaxCtas = 512;
 struct tq_attn_ws {
   uint32_t* counters;
   uint32_t* status;
+  uint4* open;
   float* parts;
 };
-constexpr uint64_t kAttnWsHeader = kAttnMaxCtas * 4 + 256;
+constexpr uint64_t kAttnWsOpen = kAttnMaxCtas * 4 + 256, kAttnWsHeader = kAttnWsOpen + kAttnMaxCtas * 16;
 // nullptr counters: d_ws is not usable as a workspace of ws_bytes bytes
 tq_attn_ws tq_attn_ws_plan(void* d_ws, uint64_t ws_bytes);
 
