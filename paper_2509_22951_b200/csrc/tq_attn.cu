@@ -1,5 +1,5 @@
 // Attention of few queries over a long run of keys: one new token of each sequence over its paged cache
-// (tq_paged_attention), one token over an encoder's states (tq_cross_attention with n_tokens 1).
+// (tq_paged_attention), one or a few tokens over an encoder's states (tq_cross_attention; each token is a query of its own).
 //
 //   out = sum_s p_s v_s / sum_s p_s,   p_s = exp(scale q.k_s - m),   m a running maximum
 //
@@ -670,7 +670,13 @@ int tq_cross_attention(const tq_encoder_kv* kv, const void* d_q, int64_t q_batch
   p.head_parts = (p.group + kHeads - 1u) / kHeads;
   p.scale_log2 = scale * 1.4426950408889634f;
   cudaStream_t st = (cudaStream_t)cuda_stream;
-  if (n_tokens > 1) {
+  // Few tokens over few bytes: this kernel, which reads the states again (from L2) for every token, against the tensor-core
+  // kernel, which reads them once but starts and joins more slowly.  Measured (us, this | the other): 1 x 6404 states of 8 x 128,
+  // 64 query heads: 2 tokens 19.6 | 30.8, 4: 23.2 | 32.3, 8: 34.7 | 34.3; 4 x 6404: 2 tokens 39.5 | 37.5, 4: 61 | 38; 4 x 1601:
+  // 4 tokens 23.7 | 23.6, 8: 35.7 | 25.0; 1 x 500 of 8 x 64: 4 tokens 7.2 | 13.0, 16: 12.0 | 13.4.
+  constexpr uint64_t kFewTokens = 16, kFewBytes = 110000000;
+  const uint64_t read = 4ull * kv->n_seqs * kv->n_states * kv->n_kv_heads * kv->head_dim;
+  if (n_tokens > 1 && (n_tokens > kFewTokens || n_tokens * read > kFewBytes)) {
     bool served = false;
     const int rc = tq_cross_launch(kv, d_q, q_batch_stride, q_token_stride, n_tokens, n_q_heads, d_kv_len, d_mask, p.block_len, p.n_blocks,
                                    p.scale_log2, d_out, d_lse, p.ws, cuda_stream, &served);

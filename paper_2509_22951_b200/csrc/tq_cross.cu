@@ -1,4 +1,4 @@
-// Attention of many queries to an encoder's states (tq_cross_attention with more than one token) on the
+// Attention of many queries to an encoder's states (tq_cross_attention but for a few tokens over few states) on the
 // 5th-generation tensor cores.
 //
 //   out = sum_s p_s v_s / sum_s p_s,   p_s = exp(scale q.k_s - m),   m a running maximum
