@@ -24,6 +24,7 @@ PyObject* g_bf16 = nullptr;          // torch.bfloat16
 PyObject* g_int8 = nullptr;
 PyObject* g_f32 = nullptr;
 PyObject* g_kwnames = nullptr;       // ("dtype", "device")
+PyObject* g_kwdtype = nullptr;       // ("dtype",)
 PyObject* g_device_attr = nullptr;   // "device"
 
 decltype(&tq_rmsnorm) f_rmsnorm = nullptr;
@@ -108,9 +109,11 @@ PyObject* result(PyObject* out, PyObject* like, const T& like_t, const int64_t* 
     Py_INCREF(out);
     return out;
   }
-  bool same = like_t.bf16() && like_t.contiguous() && like_t.d.ndim == ndim;
+  bool same = like_t.contiguous() && like_t.d.ndim == ndim;
   for (int i = 0; same && i < ndim; ++i) same = like_t.n(i) == shape[i];
-  PyObject* r = same ? PyObject_CallOneArg(g_empty_like, like) : empty(shape, ndim, g_bf16, like);
+  PyObject* args[2] = {like, g_bf16};
+  PyObject* r = !same ? empty(shape, ndim, g_bf16, like)
+                      : (like_t.bf16() ? PyObject_CallOneArg(g_empty_like, like) : PyObject_Vectorcall(g_empty_like, args, 1, g_kwdtype));
   if (r && !get(r, t, ndim, device)) {
     Py_DECREF(r);
     return nullptr;
@@ -352,8 +355,9 @@ PyObject* py_setup(PyObject*, PyObject* const* a, Py_ssize_t count) {
   g_int8 = PyObject_GetAttrString(torch, "int8");
   g_f32 = PyObject_GetAttrString(torch, "float32");
   g_kwnames = Py_BuildValue("(ss)", "dtype", "device");
+  g_kwdtype = Py_BuildValue("(s)", "dtype");
   g_device_attr = PyUnicode_InternFromString("device");
-  if (!g_device || !g_empty_like || !g_empty || !g_bf16 || !g_int8 || !g_f32 || !g_kwnames || !g_device_attr) {
+  if (!g_kwdtype || !g_device || !g_empty_like || !g_empty || !g_bf16 || !g_int8 || !g_f32 || !g_kwnames || !g_device_attr) {
     PyErr_Clear();
     Py_RETURN_FALSE;
   }
