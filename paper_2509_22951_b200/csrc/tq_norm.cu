@@ -119,6 +119,17 @@ __global__ void __launch_bounds__(1024) rmsnorm_kernel(const NormParams p) {
       }
   }
 
+  // the weights and the store of the sums do not wait for the reduction
+  Raw8<TQ_TYPE_F32> w[NU];
+  if constexpr (VEC) {
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+      const uint32_t c = column<true>(u, 0, tid, threads);
+      if (c >= p.cols) continue;
+      w[u].load_cached(p.w, c);
+      if (p.h_out) store8<HT>(p.h_out, hb + c, s[u]);
+    }
+  }
   float sum = 0.f;
 #pragma unroll
   for (int u = 0; u < NU; ++u) sum += squares(s[u]);
@@ -139,11 +150,10 @@ __global__ void __launch_bounds__(1024) rmsnorm_kernel(const NormParams p) {
     if constexpr (VEC) {
       const uint32_t c = column<true>(u, 0, tid, threads);
       if (c >= p.cols) continue;
-      if (p.h_out) store8<HT>(p.h_out, hb + c, s[u]);
-      float w[8];
-      load_weights(p.w + c, w);
+      float f[8];
+      w[u].get(f);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s[u][e] = s[u][e] * r * w[e];
+      for (int e = 0; e < 8; ++e) s[u][e] = s[u][e] * r * f[e];
       if (p.out) store8<TQ_TYPE_BF16>(p.out, ob + c, s[u]);
     } else {
 #pragma unroll
@@ -258,7 +268,7 @@ int launch(const NormParams& p, cudaStream_t st) {
     }
   }
   // One unit a thread where rows are few and the latency of a row counts, two where there are many (2049 rows of 8192 fp32
-  // with an fp32 delta: 38.2 us with two, 39.7 with four; alone 53.8 with one, 50.6 with two).  1024 threads of two units are
+  // with an fp32 delta: 36.9 us = 6.4 TB/s with two, 40.5 with one, 40.9 with four).  1024 threads of two units are
   // TQ_NORM_MAX_COLS columns.
   auto threads = [&](uint32_t nu) { return ((units + nu - 1u) / nu + 31u) / 32u * 32u; };
   if (p.rows < 2u * sms && units <= 1024u) return launch_pdl(rmsnorm_kernel<HT, DT, VEC, 1>, dim3(p.rows), threads(1), 0, st, what, p);
