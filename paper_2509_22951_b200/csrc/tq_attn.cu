@@ -107,11 +107,6 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return r;
 }
 
-// Quotient of counts that nearly always fit 32 bits.
-__device__ __forceinline__ uint64_t quotient(uint64_t a, uint64_t b) {
-  return ((a | b) >> 32) == 0u ? (uint64_t)((uint32_t)a / (uint32_t)b) : a / b;
-}
-
 // States of sequence b that a call may look at.
 template <bool PAGED>
 __device__ __forceinline__ uint32_t length_of(const AttnParams& p, uint32_t b) {

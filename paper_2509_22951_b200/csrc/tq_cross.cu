@@ -92,6 +92,7 @@ struct CrossParams {
   uint32_t n_seqs, n_tokens, n_q_heads, n_kv_heads, group;
   uint32_t rows, row_tiles;  // n_tokens * group, and its tiles of 256
   float scale_log2;
+  uint32_t by_group;  // the joining kernel finds the cut groups by their number (few groups), not by the CTA they begin in
   uint32_t counted;  // the units are the tiles of states that some row of the group sees (see kCounts)
   tq_attn_ws ws;
 };
@@ -341,13 +342,12 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
     // units of a group; of the row tiles of a sequence for one key-value head
     auto units = [&](uint32_t b, uint32_t qt) { return p.counted ? (uint32_t)counts[b * p.row_tiles + qt] : units_of(states_of(p, b)); };
     auto head_units = [&](uint32_t b) {
-      if (!p.counted) return (uint64_t)units_of(states_of(p, b)) * p.row_tiles;
-      uint64_t n = 0;
+      if (!p.counted) return units_of(states_of(p, b)) * p.row_tiles;
+      uint32_t n = 0;
       for (uint32_t q = 0; q < p.row_tiles; ++q) n += counts[b * p.row_tiles + q];
       return n;
     };
-    uint64_t total = 0;
-    uint32_t most = 0, least = 0xFFFFFFFFu;  // units of a group
+    uint32_t total = 0, most = 0, least = 0xFFFFFFFFu;  // units of all groups, of one group
     for (uint32_t b = lane; b < p.n_seqs; b += 32u) {
       total += head_units(b);
       for (uint32_t q = 0; q < (p.counted ? p.row_tiles : 1u); ++q) {
@@ -362,18 +362,20 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
       most = max(most, __shfl_xor_sync(kFull, most, d));
       least = min(least, __shfl_xor_sync(kFull, least, d));
     }
-    total *= p.n_kv_heads;
-    const uint32_t ctas = (uint32_t)min((uint64_t)gridDim.x, total);
+    total *= p.n_kv_heads;  // below 2^32: the launch has seen to it
+    // CTA i's share: units i * mean + min(i, over) and on
+    const uint32_t ctas = min(gridDim.x, total), mean = total / ctas, over = total - mean * ctas;
+    auto cta_of = [&](uint32_t u) { return u < over * (mean + 1u) ? u / (mean + 1u) : over + (u - over * (mean + 1u)) / mean; };
     // the longest share without cuts: whole groups of one size, or up to one group over the mean
-    const uint64_t n_groups = (uint64_t)p.n_seqs * p.n_kv_heads * p.row_tiles;
-    const uint64_t longest = most == least ? (n_groups + ctas - 1u) / ctas * most : total / ctas + most;
-    const bool cut = longest > total / ctas + kCutTiles;
-    uint64_t u0 = 0, u1 = 0;  // this CTA's share; without cuts, the groups that start in it
+    const uint32_t n_groups = p.n_seqs * p.n_kv_heads * p.row_tiles;
+    const uint32_t longest = most == least ? ((n_groups - 1u) / ctas + 1u) * most : mean + most;
+    const bool cut = longest > mean + kCutTiles;
+    uint32_t u0 = 0, u1 = 0;  // this CTA's share; without cuts, the groups that start in it
     if (blockIdx.x < ctas) {
-      u0 = total * blockIdx.x / ctas;
-      u1 = total * (blockIdx.x + 1u) / ctas;
+      u0 = mean * blockIdx.x + min(blockIdx.x, over);
+      u1 = u0 + mean + (blockIdx.x < over ? 1u : 0u);
     }
-    uint64_t first = 0;  // first unit of the group (b, kvh, qt)
+    uint32_t first = 0;  // first unit of the group (b, kvh, qt)
     uint32_t b = 0, kvh = 0, qt = 0, n = 1, st = 0, st_round = 0;
     auto next_group = [&]() {
       first += n;
@@ -387,22 +389,19 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
       if (b < p.n_seqs) n = units(b, qt);
     };
     if (u0 < u1) {
-      uint64_t h;
-      while (u0 >= first + (h = head_units(b)) * p.n_kv_heads) {
+      uint32_t h = head_units(0);
+      while (b + 1u < p.n_seqs && u0 - first >= h * p.n_kv_heads) {
         first += h * p.n_kv_heads;
-        ++b;
+        h = head_units(++b);
       }
-      kvh = (uint32_t)((u0 - first) / h);
+      kvh = (u0 - first) / h;
       first += h * kvh;
+      n = units(b, 0);
       if (!p.counted) {
-        n = units(b, 0);
-        qt = (uint32_t)((u0 - first) / n);
-        first += (uint64_t)n * qt;
-      } else {
-        n = units(b, 0);
-        while (u0 >= first + n) next_group();
+        qt = (u0 - first) / n;
+        first += n * qt;
       }
-      if (!cut && first < u0) next_group();
+      while (b < p.n_seqs && (u0 >= first + n || (!cut && first < u0))) next_group();
     }
     auto announce = [&](const Entry& e) {
       if (e_round) wait(bar(L::kBarEEmpty, e_slot), (e_round - 1u) & 1u);
@@ -433,11 +432,11 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
         ++st_round;
       }
     };
-    uint4 open = make_uint4(0u, 0u, 0u, 0u);  // the group that begins in this share and goes on in the next: its parts, b, kvh, qt
+    uint4 open = make_uint4(0u, 0u, 0u, 0u);  // the last group that begins in this share, the only one that can go on in the next
     for (; first < u1 && b < p.n_seqs && ok; next_group()) {
       const uint32_t len = states_of(p, b);
       // this CTA's units of the group
-      const uint32_t x0 = cut && u0 > first ? (uint32_t)(u0 - first) : 0u, x1 = cut && u1 < first + n ? (uint32_t)(u1 - first) : n;
+      const uint32_t x0 = cut && u0 > first ? u0 - first : 0u, x1 = cut && u1 - first < n ? u1 - first : n;
       Entry e{};
       e.b = b;
       e.len = len;
@@ -494,13 +493,23 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
       }
       if (!ok) break;
       e.ctl = kEnd;
-      const uint64_t end = first + n;
-      e.c0 = (uint32_t)(((first + 1u) * ctas - 1u) / total);
-      e.parts = !cut || (first >= u0 && end <= u1) ? 1u : (uint32_t)((end * ctas - 1u) / total) - e.c0 + 1u;
+      e.c0 = blockIdx.x;
+      e.parts = 1u;
+      if (cut && (first < u0 || u1 - first < n)) {
+        e.c0 = cta_of(first);
+        e.parts = cta_of(first + n - 1u) - e.c0 + 1u;
+      }
       announce(e);
-      if (e.parts > 1u && first >= u0) open = make_uint4(e.parts, b, kvh, qt);
+      if (first >= u0) {  // the CTA in which a group begins tells the joining kernel of it
+        const uint32_t id = (b * p.n_kv_heads + kvh) * p.row_tiles + qt;
+        const uint4 r = make_uint4(e.parts > 1u ? e.parts : 0u, blockIdx.x, id, 0u);
+        if (!p.by_group)
+          open = r;
+        else if (lane == 0)
+          p.ws.open[id] = r;
+      }
     }
-    if (lane == 0) p.ws.open[blockIdx.x] = open;
+    if (lane == 0 && !p.by_group) p.ws.open[blockIdx.x] = open;
     if (ok) {
       Entry e{};
       e.ctl = kStop;
@@ -885,61 +894,40 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
   }
 }
 
-// Joins the parts of the groups that were cut.  grid (CTAs of the kernel above, slices of 32 rows): block (c, y) has the group
-// that begins in CTA c's share and goes on, if there is one; a thread has a row and every eighth set of four columns, and adds
-// the parts up in their order.
-constexpr uint32_t kJoinRows = 32, kJoinThreads = 256;
+// Joins the parts of the groups that were cut.  grid (groups, or CTAs of the kernel above, slices of 8 rows): block (x, y) has
+// the cut group x, or the one that begins in CTA x's share and goes on, if there is one; a thread has four columns of a
+// row and adds the parts up in their order.
+constexpr uint32_t kJoinRows = 8;
 template <int D>
-__global__ void __launch_bounds__(kJoinThreads) cross_join_kernel(const CrossParams p) {
+__global__ void __launch_bounds__(kJoinRows * D / 4) cross_join_kernel(const CrossParams p) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const uint4 g = p.ws.open[blockIdx.x];  // parts, b, kvh, qt
+  const uint4 g = p.ws.open[blockIdx.x];  // parts, first CTA, number of the group
   if (g.x == 0u) return;
-  const uint32_t slot = blockIdx.y * kJoinRows + threadIdx.x % kJoinRows, row = g.w * kRows + slot;
+  const uint32_t bh = g.z / p.row_tiles, qt = g.z - bh * p.row_tiles, b = bh / p.n_kv_heads, kvh = bh - b * p.n_kv_heads;
+  const uint32_t slot = blockIdx.y * kJoinRows + threadIdx.x % kJoinRows, row = qt * kRows + slot, quad = threadIdx.x / kJoinRows;
   if (row >= p.rows) return;
-  constexpr uint32_t kGroups = kJoinThreads / kJoinRows;
-  constexpr int kMine = D / 4 / kGroups, kAhead = 4;
-  const uint32_t first = threadIdx.x / kJoinRows;
-  auto part = [&](uint32_t i) { return p.ws.parts + (size_t)(2u * (blockIdx.x + i) + (i == 0u ? 1u : 0u)) * kCrossPartFloats; };
+  auto part = [&](uint32_t i) { return p.ws.parts + (size_t)(2u * (g.y + i) + (i == 0u ? 1u : 0u)) * kCrossPartFloats; };
   float M = -INFINITY, l = 0.f;
-  float4 o[kMine];
-#pragma unroll
-  for (int k = 0; k < kMine; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (uint32_t i0 = 0; i0 < g.x; i0 += kAhead) {
-    float4 y[kAhead][kMine];
-    float mi[kAhead], li[kAhead];
-#pragma unroll
-    for (int a = 0; a < kAhead; ++a) {
-      const bool there = i0 + a < g.x;
-      const float* src = part(there ? i0 + a : i0);
-      mi[a] = there ? __ldcg(src + kRows * 128 + slot) : -INFINITY;
-      li[a] = there ? __ldcg(src + kRows * 129 + slot) : 0.f;
-#pragma unroll
-      for (int k = 0; k < kMine; ++k)
-        y[a][k] = there ? __ldcg(reinterpret_cast<const float4*>(src) + (first + k * kGroups) * kRows + slot) : make_float4(0.f, 0.f, 0.f, 0.f);
-    }
-#pragma unroll
-    for (int a = 0; a < kAhead; ++a) {
-      const float mn = fmaxf(M, mi[a]), ref = mn == -INFINITY ? 0.f : mn, f = exp2_fast(M - ref), h = exp2_fast(mi[a] - ref);
-      M = mn;
-      l = l * f + li[a] * h;
-#pragma unroll
-      for (int k = 0; k < kMine; ++k) {
-        o[k].x = o[k].x * f + y[a][k].x * h;
-        o[k].y = o[k].y * f + y[a][k].y * h;
-        o[k].z = o[k].z * f + y[a][k].z * h;
-        o[k].w = o[k].w * f + y[a][k].w * h;
-      }
-    }
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (uint32_t i = 0; i < g.x; ++i) {
+    const float* src = part(i);
+    const float mi = __ldcg(src + kRows * 128 + slot), li = __ldcg(src + kRows * 129 + slot);
+    const float4 y = __ldcg(reinterpret_cast<const float4*>(src) + quad * kRows + slot);
+    const float mn = fmaxf(M, mi), ref = mn == -INFINITY ? 0.f : mn, f = exp2_fast(M - ref), h = exp2_fast(mi - ref);
+    M = mn;
+    l = l * f + li * h;
+    o.x = o.x * f + y.x * h;
+    o.y = o.y * f + y.y * h;
+    o.z = o.z * f + y.z * h;
+    o.w = o.w * f + y.w * h;
   }
-  const size_t at = ((size_t)g.y * p.n_tokens + row / p.group) * p.n_q_heads + g.z * p.group + row % p.group;
+  const size_t at = ((size_t)b * p.n_tokens + row / p.group) * p.n_q_heads + kvh * p.group + row % p.group;
   const float inv = l == 0.f ? 0.f : 1.0f / l;
-#pragma unroll
-  for (int k = 0; k < kMine; ++k) {
-    const uint2 v = l == 0.f ? make_uint2(0u, 0u) : make_uint2(pack_bf16(o[k].x * inv, o[k].y * inv), pack_bf16(o[k].z * inv, o[k].w * inv));
-    *reinterpret_cast<uint2*>(p.out + at * D + 4u * (first + k * kGroups)) = v;
-  }
-  if (first == 0u && p.lse) p.lse[at] = l == 0.f ? -INFINITY : (M + log2f(l)) * 0.6931471805599453f;
+  *reinterpret_cast<uint2*>(p.out + at * D + 4u * quad) =
+      l == 0.f ? make_uint2(0u, 0u) : make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+  if (quad == 0u && p.lse) p.lse[at] = l == 0.f ? -INFINITY : (M + log2f(l)) * 0.6931471805599453f;
 }
 
 // The tensor map of K or V: (column, state, head, sequence), boxes of 64 columns x 128 states, 128-byte swizzle.
@@ -969,7 +957,8 @@ int launch(const CrossParams& p, const CUtensorMap& k_map, const CUtensorMap& v_
   if (256 * kSoftRegs + 128 * kOtherRegs > kCrossThreads * regs) return tq_cuda_status((int)cudaErrorInvalidConfiguration, what);
   const uint32_t grid = min((uint32_t)sm_count(), kAttnMaxCtas);
   if (int rc = launch_pdl(kern, dim3(grid), kCrossThreads, smem, st, what, p, k_map, v_map)) return rc;
-  return launch_pdl(cross_join_kernel<D>, dim3(grid, min(kRows, p.rows + kJoinRows - 1u) / kJoinRows), kJoinThreads, 0, st, "cross attention (join) launch", p);
+  const uint32_t x = p.by_group ? p.n_seqs * p.n_kv_heads * p.row_tiles : grid;
+  return launch_pdl(cross_join_kernel<D>, dim3(x, (min(kRows, p.rows) + kJoinRows - 1u) / kJoinRows), kJoinRows * D / 4, 0, st, "cross attention (join) launch", p);
 }
 
 }  // namespace
@@ -980,7 +969,9 @@ int tq_cross_launch(const tq_encoder_kv* kv, const void* d_q, int64_t q_batch_st
                     uint32_t n_q_heads, const int32_t* d_kv_len, const uint8_t* d_mask, uint32_t block_len, uint32_t n_blocks,
                     float scale_log2, void* d_out, float* d_lse, const tq_attn_ws& ws, void* cuda_stream, bool* served) {
   CUtensorMap k_map, v_map;
-  *served = kv->n_states != 0 && (kv->state_stride != 0 || kv->n_states == 1) && encode(&k_map, kv->d_k, kv) && encode(&v_map, kv->d_v, kv);
+  const uint64_t units = (uint64_t)kv->n_seqs * kv->n_kv_heads * (((uint64_t)n_tokens * (n_q_heads / kv->n_kv_heads) + kRows - 1u) / kRows) *
+                         (((uint64_t)kv->n_states + kStates - 1u) / kStates);
+  *served = units < 0xFFFFFFFFull && kv->n_states != 0 && (kv->state_stride != 0 || kv->n_states == 1) && encode(&k_map, kv->d_k, kv) && encode(&v_map, kv->d_v, kv);
   if (!*served) return TQ_OK;
   CrossParams p{};
   p.k = (const __nv_bfloat16*)kv->d_k;
@@ -1006,6 +997,7 @@ int tq_cross_launch(const tq_encoder_kv* kv, const void* d_q, int64_t q_batch_st
   p.rows = n_tokens * p.group;
   p.row_tiles = (p.rows + kRows - 1u) / kRows;
   p.scale_log2 = scale_log2;
+  p.by_group = (uint64_t)kv->n_seqs * kv->n_kv_heads * p.row_tiles <= kAttnMaxCtas;
   p.counted = d_mask != nullptr && block_len >= kStates && n_blocks <= kCountBlocks && kv->n_states <= 65535u * kStates &&
               (uint64_t)kv->n_seqs * p.row_tiles <= kCounts && (uint64_t)kv->n_seqs * n_tokens * n_blocks <= kCountBytes;
   p.ws = ws;

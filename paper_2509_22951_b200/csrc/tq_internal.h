@@ -236,8 +236,8 @@ int tq_dict_from_ranked(const uint32_t* keys, const uint64_t* counts, uint32_t K
 int tq_check_cache(const tq_kv_cache* cache);
 
 // Plan of the attention workspace: counters (one per CTA that can be the first of a split group; every
-// call leaves them zero), the status word, the groups that go on past a CTA's share (parts, sequence, key-value head, tile of
-// rows; written and read by one call), then the partial results of the CTAs.
+// call leaves them zero), the status word, the groups that go on past a CTA's share (number of parts, first CTA, number of the group;
+// written and read by one call), then the partial results of the CTAs.
 constexpr uint32_t kAttnMaxCtas = 512;
 struct tq_attn_ws {
   uint32_t* counters;
@@ -250,7 +250,7 @@ constexpr uint64_t kAttnWsOpen = kAttnMaxCtas * 4 + 256, kAttnWsHeader = kAttnWs
 tq_attn_ws tq_attn_ws_plan(void* d_ws, uint64_t ws_bytes);
 
 // The tensor-core form of tq_cross_attention (tq_cross.cu): *served is false, and nothing was launched, if the states
-// cannot be described by a tensor map (strides of 2^40 bytes and more, no states).
+// cannot be described by a tensor map (strides of 2^40 bytes and more, no states) or there are 2^32 and more pieces of work.
 uint64_t tq_cross_workspace_bytes();
 int tq_cross_launch(const tq_encoder_kv* kv, const void* d_q, int64_t q_batch_stride, int64_t q_token_stride, uint32_t n_tokens,
                     uint32_t n_q_heads, const int32_t* d_kv_len, const uint8_t* d_mask, uint32_t block_len, uint32_t n_blocks,
