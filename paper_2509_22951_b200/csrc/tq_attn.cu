@@ -71,9 +71,7 @@ struct Smem {
   static constexpr uint32_t kRing = kStages * 2 * kTile;         // of one warp
   static constexpr uint32_t kORow = D + 4;                       // floats: the four heads of a store land in different banks
   static constexpr uint32_t kOffO = kWarps * kRing;
-  // the warps' outputs, and in a join the factors of at most kAttnMaxCtas parts
-  static constexpr uint32_t kAreaO = kWarps * kHeads * kORow * 4 > kAttnMaxCtas * kHeads * 4 ? kWarps * kHeads * kORow * 4 : kAttnMaxCtas * kHeads * 4;
-  static constexpr uint32_t kOffM = kOffO + kAreaO;
+  static constexpr uint32_t kOffM = kOffO + kWarps * kHeads * kORow * 4;
   static constexpr uint32_t kOffL = kOffM + kWarps * kHeads * 4;
   static constexpr uint32_t kOffFlag = kOffL + kWarps * kHeads * 4;
   static constexpr uint32_t kTotal = kOffFlag + 16;
@@ -163,29 +161,29 @@ __global__ void __launch_bounds__(kThreads, 1) split_attention_kernel(const Attn
   asm volatile("griddepcontrol.wait;" ::: "memory");
 
   // ---- this CTA's share of the units: every warp finds it for itself -------------------------------
-  uint64_t total, u0, u1;
-  uint32_t ctas;  // CTAs with a share: all, or one for each unit where there are fewer
+  // (32-bit arithmetic, the launch has seen to it that the units fit: this code runs once and cold, so it is kept short)
+  uint32_t u0, n_units, mean, over;  // CTA i has the units i * mean + min(i, over) and on
   Walk at;
   {
-    const uint32_t per = (p.n_seqs + 31u) / 32u, first = min(lane * per, p.n_seqs), last = min(first + per, p.n_seqs);
-    uint64_t sum = 0;
-    for (uint32_t b = first; b < last; ++b) sum += units_of(length_of<PAGED>(p, b));
-    uint64_t incl = sum;
+    const uint32_t per = (p.n_seqs + 31u) / 32u, begin = min(lane * per, p.n_seqs), end = min(begin + per, p.n_seqs);
+    uint32_t sum = 0;
+    for (uint32_t b = begin; b < end; ++b) sum += units_of(length_of<PAGED>(p, b));
+    uint32_t incl = sum;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-      const uint64_t o = __shfl_up_sync(kFull, incl, d);
+      const uint32_t o = __shfl_up_sync(kFull, incl, d);
       if (lane >= (uint32_t)d) incl += o;
     }
-    total = __shfl_sync(kFull, incl, 31) * groups;
-    ctas = (uint32_t)min((uint64_t)gridDim.x, total);
+    const uint32_t total = __shfl_sync(kFull, incl, 31) * groups, ctas = min(gridDim.x, total);
     if (blockIdx.x >= ctas) return;  // nothing waits for this CTA
-    u0 = quotient(total * blockIdx.x, ctas);
-    u1 = quotient(total * (blockIdx.x + 1u), ctas);
+    mean = total / ctas;
+    over = total - mean * ctas;
+    u0 = blockIdx.x * mean + min(blockIdx.x, over);
+    n_units = mean + (blockIdx.x < over ? 1u : 0u);
     const uint32_t owner = __ffs(__ballot_sync(kFull, u0 < incl * groups)) - 1u;
-    uint64_t before = incl - sum;  // units of one group of each earlier sequence
-    uint32_t b = first;
+    uint32_t before = incl - sum, b = begin;  // before: units of one group of each earlier sequence
     if (lane == owner) {
-      for (;; ++b) {
+      for (; b + 1u < end; ++b) {
         const uint32_t n = units_of(length_of<PAGED>(p, b));
         if (u0 < (before + n) * groups) break;
         before += n;
@@ -194,11 +192,11 @@ __global__ void __launch_bounds__(kThreads, 1) split_attention_kernel(const Attn
     at.b = __shfl_sync(kFull, b, owner);
     before = __shfl_sync(kFull, before, owner);
     at.enter<PAGED>(p);
-    const uint64_t rest = u0 - before * groups;
-    at.m = (uint32_t)quotient(rest, at.tiles);
-    at.tile = (uint32_t)(rest - (uint64_t)at.m * at.tiles);
+    const uint32_t rest = u0 - before * groups;
+    at.m = rest / at.tiles;
+    at.tile = rest - at.m * at.tiles;
   }
-  const uint32_t n_units = (uint32_t)(u1 - u0);
+  auto cta_of = [&](uint32_t u) { return u < over * (mean + 1u) ? u / (mean + 1u) : over + (u - over * (mean + 1u)) / mean; };
 
   // ---- loads: page ids (or mask bytes) one step ahead of the copies ---------------------------------
   const uint32_t ring = tq_sm100::smem_u32(smem) + warp * L::kRing;
@@ -282,6 +280,17 @@ __global__ void __launch_bounds__(kThreads, 1) split_attention_kernel(const Attn
   };
   Part open_parts[2] = {};
 
+  // a thread's place where outputs are summed: four columns of a head
+  const uint32_t mine_h = tid / (D / 4), quad = tid % (D / 4);
+  static_assert(kThreads >= kHeads * D / 4, "four columns of each head to a thread");
+  auto finish = [&](size_t row, const float4& o, float M, float Ls) {
+    const float inv = 1.0f / Ls;
+    const bool none = Ls == 0.f;
+    *reinterpret_cast<uint2*>(p.out + row * D + 4u * quad) =
+        none ? make_uint2(0u, 0u) : make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+    if (quad == 0u && p.lse) p.lse[row] = none ? -INFINITY : (M + log2f(Ls)) * 0.6931471805599453f;
+  };
+
   uint32_t there[kStages];
   fetch();
 #pragma unroll
@@ -293,7 +302,7 @@ __global__ void __launch_bounds__(kThreads, 1) split_attention_kernel(const Attn
   uint32_t qb[D / 16][2];
   float o[D / 16][4], m[2], l[2];
   bool fresh = true;
-  uint64_t group_first = u0 - at.tile;  // first unit of the current group
+  uint32_t group_first = u0 - at.tile;  // first unit of the current group
   uint32_t stage = 0;
   for (uint32_t i = 0; i < n_units; ++i) {
     const uint32_t part = at.m % p.head_parts, kvh = (at.m / p.head_parts) % p.n_kv_heads;
@@ -404,37 +413,38 @@ __global__ void __launch_bounds__(kThreads, 1) split_attention_kernel(const Attn
       }
     }
     __syncthreads();
-    const uint64_t first = group_first, end = first + at.tiles;  // units of the whole group
-    const bool whole = first >= u0 && end <= u1;
-    const uint32_t c0 = (uint32_t)quotient((first + 1u) * ctas - 1u, total), c1 = (uint32_t)quotient(end * ctas - 1u, total);
-    float* const mine = p.ws.parts + (size_t)(2u * blockIdx.x + (blockIdx.x == c0 ? 1u : 0u)) * kPartFloats;
+    const uint32_t first = group_first, end = first + at.tiles;  // units of the whole group
+    const bool whole = first >= u0 && end - u0 <= n_units;
+    const uint32_t c0 = whole ? blockIdx.x : cta_of(first);
     const size_t out0 = ((size_t)at.b * p.n_tokens + t) * p.n_q_heads + h0;
-    for (uint32_t x = tid; x < n_heads * D; x += kThreads) {
-      const uint32_t h = x / D, d = x % D;
-      float M = sm[h];
+    if (mine_h < n_heads) {  // four columns of a head to a thread
+      const float* const ow = so + mine_h * L::kORow + 4u * quad;
+      float M = sm[mine_h];
 #pragma unroll
-      for (int w = 1; w < kWarps; ++w) M = fmaxf(M, sm[w * kHeads + h]);
+      for (int w = 1; w < kWarps; ++w) M = fmaxf(M, sm[w * kHeads + mine_h]);
       const float ref = M == -INFINITY ? 0.f : M;
-      float Ls = 0.f, Os = 0.f;
+      float Ls = 0.f;
+      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
-        const float f = exp2_fast(sm[w * kHeads + h] - ref);
-        Ls += f * sl[w * kHeads + h];
-        Os += f * so[(w * kHeads + h) * L::kORow + d];
+        const float f = exp2_fast(sm[w * kHeads + mine_h] - ref);
+        const float4 y = *reinterpret_cast<const float4*>(ow + w * kHeads * L::kORow);
+        Ls += f * sl[w * kHeads + mine_h];
+        sum.x += f * y.x, sum.y += f * y.y, sum.z += f * y.z, sum.w += f * y.w;
       }
       if (whole) {
-        p.out[(out0 + h) * D + d] = __float2bfloat16_rn(Ls == 0.f ? 0.f : Os / Ls);
-        if (d == 0 && p.lse) p.lse[out0 + h] = Ls == 0.f ? -INFINITY : (M + log2f(Ls)) * 0.6931471805599453f;
+        finish(out0 + mine_h, sum, M, Ls);
       } else {
-        mine[h * D + d] = Os;
-        if (d == 0) {
-          mine[kHeads * D + h] = M;
-          mine[kHeads * D + kHeads + h] = Ls;
+        float* const mine = p.ws.parts + (size_t)(2u * blockIdx.x + (blockIdx.x == c0 ? 1u : 0u)) * kPartFloats;
+        reinterpret_cast<float4*>(mine)[mine_h * (D / 4) + quad] = sum;
+        if (quad == 0u) {
+          mine[kHeads * D + mine_h] = M;
+          mine[kHeads * D + kHeads + mine_h] = Ls;
         }
       }
     }
     if (!whole) {  // published when the share is done: a fence and an atomic here would hold up the loads
-      const Part g{c1 - c0 + 1u, c0, n_heads, out0};
+      const Part g{cta_of(end - 1u) - c0 + 1u, c0, n_heads, out0};
       if (blockIdx.x == c0)
         open_parts[1] = g;
       else
@@ -463,71 +473,31 @@ __global__ void __launch_bounds__(kThreads, 1) split_attention_kernel(const Attn
   for (int k = 0; k < 2; ++k) {
     if (!flag[k]) continue;
     const Part g = k ? open_parts[1] : open_parts[0];
-    auto part_of = [&](uint32_t i) { return p.ws.parts + (size_t)(2u * (g.c0 + i) + (i == 0 ? 1u : 0u)) * kPartFloats; };
-    constexpr int kMine = (kHeads * D + kThreads - 1) / kThreads;  // outputs of a thread
-    constexpr uint32_t kEarly = 8;                // parts whose outputs are asked for before their factors are known
-    float early[kEarly][kMine];
-#pragma unroll
-    for (uint32_t i = 0; i < kEarly; ++i)
-#pragma unroll
-      for (int c = 0; c < kMine; ++c) {
-        const uint32_t x = c * kThreads + tid;
-        early[i][c] = i < g.parts && x < g.n_heads * D ? __ldcg(part_of(i) + x) : 0.f;
-      }
-    // the parts' factors, a head to a warp; then the sum in the order of the parts
-    float* const factor = so;
-    for (uint32_t h = warp; h < g.n_heads; h += kWarps) {
-      float M = -INFINITY, Ls = 0.f;  // of this lane's parts
-      for (uint32_t i = lane; i < g.parts; i += 32u) {
-        const float mi = __ldcg(part_of(i) + kHeads * D + h), li = __ldcg(part_of(i) + kHeads * D + kHeads + h);
-        const float mn = fmaxf(M, mi), r = mn == -INFINITY ? 0.f : mn;
-        Ls = Ls * exp2_fast(M - r) + li * exp2_fast(mi - r);
-        M = mn;
-        factor[i * kHeads + h] = mi;
-      }
-      float top = M;
-#pragma unroll
-      for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, d));
-      const float ref = top == -INFINITY ? 0.f : top;
-      Ls *= exp2_fast(M - ref);
-#pragma unroll
-      for (int d = 16; d > 0; d >>= 1) Ls += __shfl_xor_sync(kFull, Ls, d);
-      for (uint32_t i = lane; i < g.parts; i += 32u) factor[i * kHeads + h] = exp2_fast(factor[i * kHeads + h] - ref);
-      if (lane == 0) {
-        sm[h] = top;
-        sl[h] = Ls;
-      }
-    }
-    __syncthreads();
-    float acc[kMine] = {};
-#pragma unroll
-    for (uint32_t i = 0; i < kEarly; ++i)
-#pragma unroll
-      for (int c = 0; c < kMine; ++c)
-        if (i < g.parts) acc[c] += factor[i * kHeads + (c * kThreads + tid) / D] * early[i][c];
+    if (mine_h >= g.n_heads) continue;
+    float M = -INFINITY, Ls = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-    for (uint32_t i = kEarly; i < g.parts; ++i) {
-      const float* src = part_of(i);
-#pragma unroll
-      for (int c = 0; c < kMine; ++c) {
-        const uint32_t x = c * kThreads + tid;
-        if (x < g.n_heads * D) acc[c] += factor[i * kHeads + x / D] * __ldcg(src + x);
-      }
+    for (uint32_t i = 0; i < g.parts; ++i) {  // in the order of the parts
+      const float* src = p.ws.parts + (size_t)(2u * (g.c0 + i) + (i == 0 ? 1u : 0u)) * kPartFloats;
+      const float mi = __ldcg(src + kHeads * D + mine_h), li = __ldcg(src + kHeads * D + kHeads + mine_h);
+      const float4 y = __ldcg(reinterpret_cast<const float4*>(src) + mine_h * (D / 4) + quad);
+      const float mn = fmaxf(M, mi), ref = mn == -INFINITY ? 0.f : mn, f = exp2_fast(M - ref), h = exp2_fast(mi - ref);
+      M = mn;
+      Ls = Ls * f + li * h;
+      o.x = o.x * f + y.x * h;
+      o.y = o.y * f + y.y * h;
+      o.z = o.z * f + y.z * h;
+      o.w = o.w * f + y.w * h;
     }
-#pragma unroll
-    for (int c = 0; c < kMine; ++c) {
-      const uint32_t x = c * kThreads + tid, h = x / D, d = x % D;
-      if (x >= g.n_heads * D) continue;
-      const float M = sm[h], Ls = sl[h];
-      p.out[(g.out0 + h) * D + d] = __float2bfloat16_rn(Ls == 0.f ? 0.f : acc[c] / Ls);
-      if (d == 0 && p.lse) p.lse[g.out0 + h] = Ls == 0.f ? -INFINITY : (M + log2f(Ls)) * 0.6931471805599453f;
-    }
-    __syncthreads();
+    finish(g.out0 + mine_h, o, M, Ls);
   }
 }
 
 template <int D, bool PAGED>
 int launch(AttnParams& p, cudaStream_t st) {
+  const uint64_t states = PAGED ? (uint64_t)p.max_pages * p.page_size : p.n_states;
+  const uint64_t tiles = (states < 0x7FFFFFFFull ? states : 0x7FFFFFFFull) / kUnitStates + 1u, groups = (uint64_t)p.n_tokens * p.n_kv_heads * p.head_parts;
+  if (groups > 0xFFFFFFFFull / tiles || groups * tiles > 0xFFFFFFFFull / p.n_seqs) return TQ_ERR_UNSUPPORTED_SHAPE;
   auto kern = split_attention_kernel<D, PAGED>;
   constexpr size_t smem = Smem<D>::kTotal;
   const char* what = PAGED ? "paged attention launch" : "cross attention launch";

@@ -22,10 +22,6 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
-// Quotient of counts that nearly always fit 32 bits (a division of 64 bits takes a few hundred cycles).
-__device__ __forceinline__ uint64_t quotient(uint64_t a, uint64_t b) {
-  return ((a | b) >> 32) == 0u ? (uint64_t)((uint32_t)a / (uint32_t)b) : a / b;
-}
 // A NaN on either side is the result (fmaxf drops it).
 __device__ __forceinline__ float max_nan(float a, float b) {
   float r;
