@@ -502,7 +502,8 @@ typedef struct tq_encoder_kv {
  * elements apart (multiples of 8), 16-byte aligned.  d_kv_len: DEVICE int32 [n_seqs] or NULL (all states); values are
  * clamped to 0..n_states.  d_mask: DEVICE uint8 [n_seqs][n_tokens][ceil(n_states / block_len)] or NULL.
  * d_out: DEVICE bf16 [n_seqs][n_tokens][n_q_heads][head_dim]; d_lse: DEVICE fp32
- * [n_seqs][n_tokens][n_q_heads] or NULL. */
+ * [n_seqs][n_tokens][n_q_heads] or NULL.  TQ_ERR_UNSUPPORTED_SHAPE where sequences x tokens x key-value heads x
+ * (states / 128) reach 2^32 (likewise above, with the states that max_pages can hold). */
 int tq_cross_attention(const tq_encoder_kv* kv, const void* d_q, int64_t q_batch_stride,
                        int64_t q_token_stride, uint32_t n_tokens, uint32_t n_q_heads,
                        const int32_t* d_kv_len, const uint8_t* d_mask, uint32_t block_len, float scale,

@@ -738,12 +738,14 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(L::kBarPFull, w * kChunks + x));
         };
-        constexpr int kPairs = 64 / kChunks;
+        constexpr int kPairs = 64 / kChunks, kLate = 3;
+        static_assert(kPairs == 32, "one store of 32 columns a piece");
 #pragma unroll
         for (int x = 0; x < kChunks; ++x) {
           uint32_t pk[kPairs];
 #pragma unroll
           for (int i = 0; i < kPairs; ++i) {
+            if (x != 0 && i == kLate) hand_over(x - 1);  // its stores have had time to land
             const int at = 2 * (x * kPairs + i);
             float a, b;
             unpair(fma2(pair(__uint_as_float(s[at]), __uint_as_float(s[at + 1])), c2, ref2), a, b);
@@ -752,11 +754,7 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
             sum[i & 1] = add2(sum[i & 1], pair(a, b));
             pk[i] = pack_bf16(a, b);
           }
-          if (x) hand_over(x - 1);
-          if constexpr (kPairs == 16)
-            TMEM_ST16(s_addr + kPairs * x, pk);
-          else
-            TMEM_ST32(s_addr + kPairs * x, pk);
+          TMEM_ST32(s_addr + kPairs * x, pk);
         }
         hand_over(kChunks - 1);
         float l0, l1;

@@ -398,6 +398,20 @@ def test_cross_attention_split_over_the_states(tq, ws):
     cross_case(tq, ws, 1, 130, 9000, 2, 1, 64, seed=9, block=601)
 
 
+def test_cross_attention_many_groups_of_different_lengths(tq, ws):
+    """More groups than the workspace can number, of lengths that make cutting them worth while."""
+    cross_case(tq, ws, 9, 20, 1500, 64, 64, 64, kv_len=[1500, 3, 700, 1500, 1100, 0, 900, 1499, 128], seed=10)
+
+
+@pytest.mark.parametrize("T", [1, 40])
+def test_cross_attention_one_head_for_all(tq, ws, T):
+    """Keys and values whose heads are one head, expanded (stride 0)."""
+    g = gen(23)
+    q, k, v = randn(g, 2, T, 8, 64, dtype=BF), randn(g, 2, 300, 1, 64, dtype=BF), randn(g, 2, 300, 1, 64, dtype=BF)
+    wide = tq.tq_cross_attention(q, k.expand(-1, -1, 4, -1), v.expand(-1, -1, 4, -1), ws)
+    assert torch.equal(wide, tq.tq_cross_attention(q, k.repeat(1, 1, 4, 1), v.repeat(1, 1, 4, 1), ws))
+
+
 @pytest.mark.parametrize("T", [1, 50])
 def test_cross_attention_large_scores(tq, ws, T):
     """A maximum that keeps rising along the states: the running results are rescaled again and again."""
