@@ -459,7 +459,7 @@ int tq_rope_append(const void* d_q, const void* d_k, const void* d_v, int x_type
 
 /* Workspace of the two attention calls below: what the parts of a split hand to one another, the
  * counters that find the last part, a status word.  tq_attn_workspace_size: bytes for the current
- * device, whatever the sizes of the calls.  d_ws: DEVICE, 256-byte aligned; tq_attn_workspace_init
+ * device, whatever the sizes of the calls (about 40 MB).  d_ws: DEVICE, 256-byte aligned; tq_attn_workspace_init
  * clears it once, and every call leaves its counters cleared for the next.  Calls that share a
  * workspace must not overlap on the GPU (calls on one stream never do). */
 int tq_attn_workspace_size(uint64_t* device_bytes);

@@ -16,7 +16,8 @@
 // stages filled by 16-byte cp.async, so nothing in the loop waits for another warp, and 64 KB and more are under way
 // on every SM (6.5 TB/s x 1 us of latency / 148 SMs = 44 KB are the least).  The page ids of a step are loaded one
 // step before its copies are issued.  Measured for 8 sequences of up to 8191 tokens with 24 / 8 heads | one of
-// 131071, 32 / 8 | 64 of up to 16384, 64 / 8 | 4 over 6404 encoder states, 32 / 8 (us): 34.7 | 90.1 | 392 | 24.6;
+// 131071, 32 / 8 | 64 of up to 16384, 64 / 8 | 4 over 6404 encoder states, 32 / 8 (us), before the last two steps
+// (now 32.4 | 90.8 | 402 | 23.2 on another GPU): 34.7 | 90.1 | 392 | 24.6;
 // three stages 35.6 | 93.0 | 414 | 25.4; two CTAs of four warps, which leave twice the parts to join,
 // 35.6 | 90.3 | 392 | 28.1; ten warps 34.4 | 93.7 | 402 | 25.5, six 37.8 | 95.4 | 418 | 26.4.
 //
