@@ -414,8 +414,8 @@ int tq_rmsnorm(const void* d_h, int h_type, int64_t h_stride, const void* d_delt
                void* d_h_out, void* d_out_bf16, void* cuda_stream);
 
 /* The same with the result in 8 bits and a scale for each row, by the rule of tq_quantize_rows:
- * scale_r = max_c |n_c| / 127 (1 for a row of zeros), q = clamp(round(n / scale_r), -127, 127), n the
- * normalised row in 32 bits.  A row with a NaN in n has scale NaN and levels 0.
+ * scale_r = max_c |n_c| / 127 (1 where that rounds to 0: a row of zeros, or of less than 64 * 2^-149),
+ * q = clamp(round(n / scale_r), -127, 127), n the normalised row in 32 bits.  A row with a NaN in n has scale NaN and levels 0.
  * d_q: DEVICE int8 [rows][cols]; d_scale: DEVICE fp32 [rows]. */
 int tq_rmsnorm_q8(const void* d_h, int h_type, int64_t h_stride, const void* d_delta, int delta_type,
                   int64_t delta_stride, const float* d_weight, float eps, uint32_t rows, uint32_t cols,

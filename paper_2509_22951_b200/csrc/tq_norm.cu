@@ -65,17 +65,20 @@ __device__ __forceinline__ void load_weights(const float* w, float (&f)[8]) {
   raw.get(f);
 }
 // 8 bits by the rule of tq_quantize_rows: amax is the row's largest magnitude (NaN if it has one), then IEEE division and
-// rounding half to even.
-__device__ __forceinline__ float scale_of(float amax) { return amax == 0.f ? 1.0f : __fdiv_rn(amax, 127.0f); }
+// rounding half to even.  Where amax / 127 rounds to 0 (below 64 * 2^-149) the row counts as zeros.
+__device__ __forceinline__ float scale_of(float amax) {
+  const float s = __fdiv_rn(amax, 127.0f);
+  return s == 0.f ? 1.0f : s;
+}
 __device__ __forceinline__ void levels(const float (&n)[8], float scale, int8_t (&b)[8]) {
   const float inv = 1.0f / scale;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     // the product with 1 / scale is within 2^-16 of the quotient: only near a half can the two round differently, and there
-    // the quotient itself is taken
+    // the quotient itself is taken; so it is where 1 / scale overflows (scale below 2^-128)
     const float v = n[e] * inv;
     float r = rintf(v);
-    if (fabsf(fabsf(v - r) - 0.5f) < 1e-3f) r = rintf(__fdiv_rn(n[e], scale));
+    if (inv == INFINITY || fabsf(fabsf(v - r) - 0.5f) < 1e-3f) r = rintf(__fdiv_rn(n[e], scale));
     b[e] = scale == scale ? (int8_t)fminf(fmaxf(r, -127.f), 127.f) : (int8_t)0;
   }
 }
