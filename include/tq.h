@@ -513,6 +513,11 @@ int tq_cross_attention(const tq_encoder_kv* kv, const void* d_q, int64_t q_batch
  * valid); synchronises cuda_stream. */
 int tq_attn_status(void* d_ws, void* cuda_stream, uint32_t* status);
 
+/* Test hook like tq_test_withhold_table_chunk: while on, tq_cross_attention's tensor-core kernel is launched with a loader that
+ * gives up before its first tile, as it does when a wait of its own runs out.  The other roles leave at once, the call ends
+ * normally with undefined outputs and TQ_STATUS_WAIT_EXPIRED, and nothing beside the outputs is written. */
+void tq_test_withhold_cross_entry(int on);
+
 #ifdef __cplusplus
 }
 #endif

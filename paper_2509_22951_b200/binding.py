@@ -48,7 +48,7 @@ EXPORTS = [
     "tq_gemm_plan_status", "tq_gemm_plan_free", "tq_stack_size", "tq_stack_plan_host", "tq_stack_create",
     "tq_fused_gemv_stack", "tq_fused_gemv_stack_host", "tq_stack_launches", "tq_test_withhold_table_chunk", "tq_decompress_stack", "tq_stack_free", "tq_device_status", "tq_dmat_free",
     "tq_rmsnorm", "tq_rmsnorm_q8", "tq_rope_append", "tq_attn_workspace_size", "tq_attn_workspace_init", "tq_paged_attention",
-    "tq_cross_attention", "tq_attn_status",
+    "tq_cross_attention", "tq_attn_status", "tq_test_withhold_cross_entry",
 ]
 
 
@@ -136,6 +136,7 @@ def _load() -> C.CDLL:
         "tq_fused_gemv_stack_host": (C.c_int, [vp, vp, vp, C.c_uint64, vp, vp, C.c_uint64, vp]),
         "tq_stack_launches": (C.c_int, [vp]),
         "tq_test_withhold_table_chunk": (None, [C.c_int]),
+        "tq_test_withhold_cross_entry": (None, [C.c_int]),
         "tq_decompress_stack": (C.c_int, [vp, vp, vp]),
         "tq_stack_free": (None, [vp]),
         "tq_device_status": (C.c_int, [vp, vp, u32p]),
@@ -898,6 +899,11 @@ def tq_attn_workspace(device="cuda", stream=None) -> AttnWorkspace:
         buf = torch.empty(need.value, dtype=torch.uint8, device="cuda")
         _check(_lib.tq_attn_workspace_init(buf.data_ptr(), buf.numel(), _stream_ptr()), "tq_attn_workspace_init")
     return AttnWorkspace(buf)
+
+
+def tq_test_withhold_cross_entry(on: bool) -> None:
+    """Test hook: see tq.h."""
+    _lib.tq_test_withhold_cross_entry(int(bool(on)))
 
 
 def tq_attn_status(workspace: AttnWorkspace, stream=None) -> int:

@@ -36,6 +36,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 
 #include "tq_internal.h"
@@ -94,6 +95,7 @@ struct CrossParams {
   float scale_log2;
   uint32_t by_group;  // the joining kernel finds the cut groups by their number (few groups), not by the CTA they begin in
   uint32_t counted;  // the units are the tiles of states that some row of the group sees (see kCounts)
+  uint32_t test_withhold;  // test hook (tq_test_withhold_cross_entry): the loader gives up where it would announce
   tq_attn_ws ws;
 };
 
@@ -404,6 +406,7 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
       while (b < p.n_seqs && (u0 >= first + n || (!cut && first < u0))) next_group();
     }
     auto announce = [&](const Entry& e) {
+      if (p.test_withhold) ok = false;
       if (e_round) wait(bar(L::kBarEEmpty, e_slot), (e_round - 1u) & 1u);
       if (!ok) return;
       if (lane == 0) {
@@ -894,15 +897,18 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
 
 // Joins the parts of the groups that were cut.  grid (groups, or CTAs of the kernel above, slices of 8 rows): block (x, y) has
 // the cut group x, or the one that begins in CTA x's share and goes on, if there is one; a thread has four columns of a
-// row and adds the parts up in their order.
+// row and adds the parts up in their order.  After an expired wait the entries may be an earlier call's (then the outputs are
+// not valid, and nothing beside them is written): a block that goes by the group's number takes no other group, and a number past the
+// last group is not followed.
 constexpr uint32_t kJoinRows = 8;
 template <int D>
 __global__ void __launch_bounds__(kJoinRows * D / 4) cross_join_kernel(const CrossParams p) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const uint4 g = p.ws.open[blockIdx.x];  // parts, first CTA, number of the group
-  if (g.x == 0u) return;
-  const uint32_t bh = g.z / p.row_tiles, qt = g.z - bh * p.row_tiles, b = bh / p.n_kv_heads, kvh = bh - b * p.n_kv_heads;
+  const uint32_t id = p.by_group ? blockIdx.x : g.z;
+  if (g.x == 0u || id >= p.n_seqs * p.n_kv_heads * p.row_tiles) return;
+  const uint32_t bh = id / p.row_tiles, qt = id - bh * p.row_tiles, b = bh / p.n_kv_heads, kvh = bh - b * p.n_kv_heads;
   const uint32_t slot = blockIdx.y * kJoinRows + threadIdx.x % kJoinRows, row = qt * kRows + slot, quad = threadIdx.x / kJoinRows;
   if (row >= p.rows) return;
   auto part = [&](uint32_t i) { return p.ws.parts + (size_t)(2u * (g.y + i) + (i == 0u ? 1u : 0u)) * kCrossPartFloats; };
@@ -959,7 +965,11 @@ int launch(const CrossParams& p, const CUtensorMap& k_map, const CUtensorMap& v_
   return launch_pdl(cross_join_kernel<D>, dim3(x, (min(kRows, p.rows) + kJoinRows - 1u) / kJoinRows), kJoinRows * D / 4, 0, st, "cross attention (join) launch", p);
 }
 
+std::atomic<int> g_test_withhold{0};
+
 }  // namespace
+
+extern "C" void tq_test_withhold_cross_entry(int on) { g_test_withhold.store(on ? 1 : 0); }
 
 uint64_t tq_cross_workspace_bytes() { return (uint64_t)min((uint32_t)sm_count(), kAttnMaxCtas) * 2u * kCrossPartFloats * sizeof(float); }
 
@@ -998,6 +1008,7 @@ int tq_cross_launch(const tq_encoder_kv* kv, const void* d_q, int64_t q_batch_st
   p.by_group = (uint64_t)kv->n_seqs * kv->n_kv_heads * p.row_tiles <= kAttnMaxCtas;
   p.counted = d_mask != nullptr && block_len >= kStates && n_blocks <= kCountBlocks && kv->n_states <= 65535u * kStates &&
               (uint64_t)kv->n_seqs * p.row_tiles <= kCounts && (uint64_t)kv->n_seqs * n_tokens * n_blocks <= kCountBytes;
+  p.test_withhold = (uint32_t)g_test_withhold.load();
   p.ws = ws;
   cudaStream_t st = (cudaStream_t)cuda_stream;
   return kv->head_dim == 64 ? launch<64>(p, k_map, v_map, st) : launch<128>(p, k_map, v_map, st);

@@ -39,3 +39,50 @@ def test_rmsnorm_q8_of_tiny_rows(tq, cols, top):
     q, s = tq.tq_rmsnorm_q8(torch.from_numpy(h).cuda(), torch.from_numpy(w).cuda(), eps=0.0)
     assert np.array_equal(s.cpu().numpy(), scale)
     assert np.array_equal(q.cpu().numpy(), want)
+
+
+# ------------------------------------------------------------------------------------------------ cross attention
+@pytest.fixture(scope="module")
+def ws(tq):
+    w = tq.tq_attn_workspace()
+    yield w
+    assert tq.tq_attn_status(w) == 0
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def randn(g, *shape, dtype=F32, scale=1.0):
+    return (torch.randn(*shape, generator=g, device="cuda") * scale).to(dtype)
+
+
+def test_cross_attention_that_gave_up_writes_its_outputs_alone(tq, ws):
+    """A call with more groups than entries numbers them by CTA; the call after it has two groups, its entries' places still hold
+    the first call's, and its loaders give up before they write theirs."""
+    g = gen(1)
+    B, T, S, K, D = 9, 20, 1500, 64, 64
+    k, v = randn(g, B, S, K, D, dtype=BF), randn(g, B, S, K, D, dtype=BF)
+    lens = torch.tensor([1500, 3, 700, 1500, 1100, 0, 900, 1499, 128], dtype=torch.int32, device="cuda")
+    tq.tq_cross_attention(randn(g, B, T, K, D, dtype=BF), k, v, ws, kv_len=lens)
+    entries = ws.buf[512 * 4 + 256:][:512 * 16].view(torch.int32).view(512, 4)
+    assert bool(((entries[:2, 0] > 1) & (entries[:2, 2] >= 2)).any())  # an entry that a block of the next call would find
+
+    q, k, v = randn(g, 1, 17, 2, D, dtype=BF), randn(g, 1, 300, 2, D, dtype=BF), randn(g, 1, 300, 2, D, dtype=BF)
+    good = tq.tq_cross_attention(q, k, v, ws)
+    tq.tq_cross_attention(randn(g, B, T, K, D, dtype=BF), randn(g, B, S, K, D, dtype=BF), randn(g, B, S, K, D, dtype=BF), ws, kv_len=lens)
+    n, room = q.numel(), 1 << 20
+    out, lse = torch.full((n + room,), 7.0, dtype=BF, device="cuda"), torch.full((34 + room,), 7.0, device="cuda")
+    o, ls = out[:n].view(q.shape), lse[:34].view(1, 17, 2)
+    tq.tq_test_withhold_cross_entry(True)
+    try:
+        tq.tq_cross_attention(q, k, v, ws, out=o, lse=ls)
+        torch.cuda.synchronize()
+    finally:
+        tq.tq_test_withhold_cross_entry(False)
+    assert tq.tq_attn_status(ws) == tq.TQ_STATUS_WAIT_EXPIRED
+    assert bool((out[n:] == 7.0).all()) and bool((lse[34:] == 7.0).all())
+    assert torch.equal(tq.tq_cross_attention(q, k, v, ws, out=o, lse=ls), good)  # the workspace is as good as before
+    assert tq.tq_attn_status(ws) == 0
