@@ -705,16 +705,21 @@ _current_device = torch._C._cuda_getDevice
 
 
 def _load_fast():
-    """The native form of the calls below for their usual case (csrc/tq_fast.cpp), or None (no headers to build it with, a torch
-    without the DLPack exchange interface).  It answers None for whatever it does not take, and the checks here speak."""
+    """The native form of the calls below for their usual case (csrc/tq_fast.cpp), or None (it cannot be built or loaded here, or
+    torch is without the DLPack exchange interface).  It answers None for whatever it does not take, and the checks here speak."""
     import importlib.util
+    import warnings
 
     path = _build.build_fast()
     if path is None:
         return None
     spec = importlib.util.spec_from_file_location("_tqfast", str(path))
-    module = importlib.util.module_from_spec(spec)
-    spec.loader.exec_module(module)
+    try:
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+    except ImportError as e:
+        warnings.warn(f"the native form of the small calls was not loaded, they go through Python: {e}", RuntimeWarning)
+        return None
     names = ("tq_rmsnorm", "tq_rmsnorm_q8", "tq_rope_append", "tq_paged_attention", "tq_cross_attention")
     return module if module.setup(torch, *(C.cast(getattr(_lib, n), C.c_void_p).value for n in names)) else None
 

@@ -4,14 +4,15 @@ from __future__ import annotations
 import os
 import shutil
 import subprocess
+import sysconfig
+import warnings
 from pathlib import Path
 
 PKG = Path(__file__).resolve().parent
 ROOT = PKG.parent
 CSRC = PKG / "csrc"
 LIB = PKG / "libtq.so"
-FAST = PKG / "_tqfast.so"  # CPython module: the usual case of the calls between the linear layers
-FAST_SOURCE = CSRC / "tq_fast.cpp"
+FAST_SOURCE = CSRC / "tq_fast.cpp"  # CPython module: the usual case of the calls between the linear layers
 SOURCES = [CSRC / "tq_device.cu", CSRC / "tq_gemm.cu", CSRC / "tq_gemm_ws.cu", CSRC / "tq_tiles.cu", CSRC / "tq_wide.cu", CSRC / "tq_encode.cu", CSRC / "tq_dict_device.cu",
            CSRC / "tq_norm.cu", CSRC / "tq_rope.cu", CSRC / "tq_attn.cu", CSRC / "tq_cross.cu", CSRC / "tq_host.cpp"]
 HEADERS = [CSRC / "tq_internal.h", CSRC / "tq_sm100.cuh", CSRC / "tq_tiles_common.cuh", CSRC / "tq_ops_common.cuh", ROOT / "include" / "tq.h"]
@@ -52,23 +53,37 @@ def build_library(force: bool = False, verbose: bool = False) -> Path:
     return LIB
 
 
-def build_fast(force: bool = False) -> Path | None:
-    """Builds _tqfast.so; None where the headers of the running interpreter or of torch (dlpack.h) are missing."""
-    import sysconfig
-
+def fast_path() -> Path:
+    """Where the CPython module lies: it is built against one interpreter and one torch, and its name says which."""
     import torch
+    return PKG / f"_tqfast.{sysconfig.get_config_var('SOABI')}.torch-{torch.__version__}.so"
+
+
+def build_fast(force: bool = False) -> Path | None:
+    """Builds the CPython module; None where that is not possible (no compiler, no headers of the running interpreter or of torch, a
+    dlpack.h without the exchange interface, a folder that cannot be written): binding.py does without.  force: raises instead where
+    the compiler fails."""
+    import torch
+    fast = fast_path()
     sources = [FAST_SOURCE, ROOT / "include" / "tq.h"]
-    if not force and FAST.exists() and FAST.stat().st_mtime >= max(p.stat().st_mtime for p in sources):
-        return FAST
+    if not force and fast.exists() and fast.stat().st_mtime >= max(p.stat().st_mtime for p in sources):
+        return fast
     python, dlpack = Path(sysconfig.get_paths()["include"]), Path(torch.__file__).parent / "include"
     gxx = shutil.which("g++")
     if gxx is None or not (python / "Python.h").exists() or not (dlpack / "ATen" / "dlpack.h").exists():
-        return FAST if FAST.exists() else None
-    tmp = FAST.with_name(f"_tqfast.tmp{os.getpid()}.so")
-    subprocess.check_call([gxx, "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-I", str(ROOT / "include"), "-I", str(python), "-I", str(dlpack),
-                           str(FAST_SOURCE), "-o", str(tmp)])
-    os.replace(tmp, FAST)
-    return FAST
+        return None
+    tmp = PKG / f"_tqfast.tmp{os.getpid()}.so"
+    cmd = [gxx, "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-I", str(ROOT / "include"), "-I", str(python), "-I", str(dlpack), str(FAST_SOURCE), "-o", str(tmp)]
+    try:
+        subprocess.run(cmd, check=True, stderr=None if force else subprocess.PIPE)
+        os.replace(tmp, fast)
+    except (subprocess.CalledProcessError, OSError) as e:
+        tmp.unlink(missing_ok=True)
+        if force:
+            raise
+        warnings.warn(f"the native form of the small calls was not built, they go through Python: {e}", RuntimeWarning, stacklevel=2)
+        return None
+    return fast
 
 
 if __name__ == "__main__":
