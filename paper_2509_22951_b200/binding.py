@@ -700,8 +700,8 @@ def tq_device_status(m: DeviceMatrix, stream=None) -> int:
 
 # ------------------------------------------------------------------------------ between the linear layers
 _TYPES = {torch.bfloat16: TQ_TYPE_BF16, torch.float32: TQ_TYPE_F32}
-_raw_stream = torch._C._cuda_getCurrentRawStream
-_current_device = torch._C._cuda_getDevice
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # a torch without CUDA still has the host's half of this module
+_current_device = getattr(torch._C, "_cuda_getDevice", None)
 
 
 def _load_fast():

@@ -78,3 +78,11 @@ def test_force_says_what_is_wrong(monkeypatch, tmp_path):
         assert build.build_fast() is None
     with pytest.warns(RuntimeWarning):
         assert tq._load_fast() is None
+
+
+def test_a_torch_without_cuda_still_imports_the_binding():
+    code = "import torch\nfor n in ('_cuda_getCurrentRawStream', '_cuda_getDevice'): delattr(torch._C, n)\n" \
+           "import paper_2509_22951_b200.binding as b, numpy as np\nassert b._fast is None\n" \
+           "q, s = b.tq_quantize_rows(np.ones((2, 8), np.float32)); print(int(q[0, 0]))"
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True)
+    assert r.returncode == 0 and r.stdout.split() == ["127"], r.stderr
