@@ -112,10 +112,10 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopePar
   uint32_t n = blockIdx.y * kSide + threadIdx.x / kPerHead;
   load(n);
 
-  const uint32_t page = (uint32_t)slot / p.cache.page_size;  // a negative slot becomes a page past the pool
+  const uint32_t page = (uint32_t)slot / p.cache.page_size;  // -1: no slot; other negative ones are out of range like those past the pool
   const bool in_pool = slot >= 0 && page < p.cache.n_pages, keep = in_pool && known;
   if (threadIdx.x == 0 && blockIdx.y == 0 && p.cache.d_status != nullptr) {
-    const uint32_t bad = (known ? 0u : TQ_STATUS_BAD_POSITION) | (slot >= 0 && !in_pool ? TQ_STATUS_BAD_PAGE : 0u);
+    const uint32_t bad = (known ? 0u : TQ_STATUS_BAD_POSITION) | (slot != -1 && !in_pool ? TQ_STATUS_BAD_PAGE : 0u);
     if (bad) atomicOr(p.cache.d_status, bad);
   }
   const size_t slot_at = keep ? (size_t)page * p.cache.page_stride + (size_t)((uint32_t)slot - page * p.cache.page_size) * p.cache.slot_stride + e0 : 0;

@@ -86,3 +86,22 @@ def test_cross_attention_that_gave_up_writes_its_outputs_alone(tq, ws):
     assert bool((out[n:] == 7.0).all()) and bool((lse[34:] == 7.0).all())
     assert torch.equal(tq.tq_cross_attention(q, k, v, ws, out=o, lse=ls), good)  # the workspace is as good as before
     assert tq.tq_attn_status(ws) == 0
+
+
+# ------------------------------------------------------------------------------------------------ rotary positions, cache write
+@pytest.mark.parametrize("slot,bad", [(-1, False), (-2, True), (-2 ** 31, True), (31, False), (32, True), (2 ** 31 - 1, True)])
+def test_rope_append_says_which_slots_are_out_of_range(tq, slot, bad):
+    """-1 is padding; every other slot outside the pool sets the bit, alone among good ones."""
+    g = gen(2)
+    kp, vp = randn(g, 2, 1, 16, 64, dtype=BF), randn(g, 2, 1, 16, 64, dtype=BF)
+    k0, v0 = kp.clone(), vp.clone()
+    cache = tq.tq_kv_cache(kp, vp)
+    q, k, v, table = randn(g, 3, 2, 64), randn(g, 3, 1, 64), randn(g, 3, 1, 64), torch.cat([torch.ones(4, 32), torch.zeros(4, 32)], 1).cuda()
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    out = tq.tq_rope_append(q, k, v, table, i32(0, 1, 2), i32(5, slot, 20), cache)
+    assert tq.tq_kv_cache_status(cache) == (tq.TQ_STATUS_BAD_PAGE if bad else 0)
+    assert torch.equal(out, q.to(BF))  # angles of 0
+    k0[0, 0, 5], v0[0, 0, 5], k0[1, 0, 4], v0[1, 0, 4] = k[0, 0], v[0, 0], k[2, 0], v[2, 0]
+    if slot == 31:
+        k0[1, 0, 15], v0[1, 0, 15] = k[1, 0], v[1, 0]
+    assert torch.equal(kp, k0) and torch.equal(vp, v0)
