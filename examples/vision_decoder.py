@@ -87,6 +87,7 @@ class Decoder:
         self.workspace = tq.tq_attn_workspace()
         self.image = {}  # layer -> keys, values
         self.lens = torch.zeros(batch, dtype=torch.int32, device="cuda")
+        self.steps = 0  # tokens of every sequence, on the host
         self.tile_mask = None
 
         # operands of the products and the products that can run together
@@ -126,6 +127,9 @@ class Decoder:
     def step(self, tokens: torch.Tensor) -> torch.Tensor:
         """One new token per sequence -> logits, fp32 [batch][vocab] (the decoder's own buffer)."""
         c, B = self.cfg, self.batch
+        if self.steps >= c.max_tokens:
+            raise ValueError(f"the cache has room for {c.max_tokens} tokens of a sequence")
+        self.steps += 1
         h = self.embed[tokens]
         positions = self.lens.clone()
         page = self.pages.gather(1, (positions // c.page).long()[:, None])[:, 0]
@@ -198,6 +202,8 @@ class Decoder:
 def run(cfg: Config, batch: int, steps: int, seed: int = 0, check: bool = True):
     """Greedy decoding from one start token per sequence; -> (tokens [batch][steps], largest error of the last logits relative to
     their largest magnitude, us per step)."""
+    if not 1 <= steps <= cfg.max_tokens:
+        raise ValueError(f"1 to {cfg.max_tokens} steps, not {steps}")
     d = Decoder(cfg, batch, seed)
     g = torch.Generator(device="cuda").manual_seed(seed + 1)
     d.see(torch.randn(batch, cfg.tiles * cfg.patches, cfg.hidden, generator=g, device="cuda").to(torch.bfloat16),
