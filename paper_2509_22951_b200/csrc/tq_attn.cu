@@ -16,8 +16,8 @@
 // stages filled by 16-byte cp.async, so nothing in the loop waits for another warp, and 64 KB and more are under way
 // on every SM (6.5 TB/s x 1 us of latency / 148 SMs = 44 KB are the least).  The page ids of a step are loaded one
 // step before its copies are issued.  Measured for 8 sequences of up to 8191 tokens with 24 / 8 heads | one of
-// 131071, 32 / 8 | 64 of up to 16384, 64 / 8 | 4 over 6404 encoder states, 32 / 8 (us), before the last two steps
-// (now 32.4 | 90.8 | 402 | 23.2 on another GPU): 34.7 | 90.1 | 392 | 24.6;
+// 131071, 32 / 8 | 64 of up to 16384, 64 / 8 | 4 over 6404 encoder states, 32 / 8 (us), before the last steps
+// (now 33.4 | 91.1 | 391 | 24.8 on another GPU): 34.7 | 90.1 | 392 | 24.6;
 // three stages 35.6 | 93.0 | 414 | 25.4; two CTAs of four warps, which leave twice the parts to join,
 // 35.6 | 90.3 | 392 | 28.1; ten warps 34.4 | 93.7 | 402 | 25.5, six 37.8 | 95.4 | 418 | 26.4.
 //
@@ -25,7 +25,10 @@
 // 8 heads), then O^T = V^T P^T (head_dim x 8 heads), so that a group of up to 8 heads wastes nothing but
 // the columns it lacks; the accumulators of S^T become the operand P^T by one 8x8 transpose in registers
 // (movmatrix).  tcgen05 would have to run with 120 of 128 rows empty and gains nothing on a kernel that
-// waits for memory.  p is rounded to bf16 for the product with V; its sum is taken in fp32 before that.
+// waits for memory.  p goes into the product with V as two bf16 parts, which hold 16 of its bits between them: in one part, the
+// error against 64 bits is 1.9e-3 of the result's norm, in two 1.7e-3, which is the rounding of the result (8 sequences 32.8 us in one
+// part, 33.4 in two; 64: 388 and 391; encoder states 24.4 and 24.8).  The lower parts' products are summed apart: where a value of V
+// is infinite they are 0 x Inf, and the upper parts' sum is the answer.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -301,7 +304,7 @@ __global__ void __launch_bounds__(kThreads, 1) split_attention_kernel(const Attn
   }
 
   uint32_t qb[D / 16][2];
-  float o[D / 16][4], m[2], l[2];
+  float o[D / 16][4], o_low[D / 16][4], m[2], l[2];  // o: by p's upper parts; o_low: by its lower ones
   bool fresh = true;
   uint32_t group_first = u0 - at.tile;  // first unit of the current group
   uint32_t stage = 0;
@@ -319,7 +322,9 @@ __global__ void __launch_bounds__(kThreads, 1) split_attention_kernel(const Attn
         qb[kk][1] = n < n_heads ? __ldg(reinterpret_cast<const uint32_t*>(q + kk * 16 + 8)) : 0u;
       }
 #pragma unroll
-      for (int d = 0; d < D / 16; ++d) o[d][0] = o[d][1] = o[d][2] = o[d][3] = 0.f;
+      for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[d][c] = o_low[d][c] = 0.f;
       m[0] = m[1] = -INFINITY;
       l[0] = l[1] = 0.f;
     }
@@ -366,6 +371,8 @@ __global__ void __launch_bounds__(kThreads, 1) split_attention_kernel(const Attn
           for (int d = 0; d < D / 16; ++d) {
             o[d][c] *= f;
             o[d][c + 2] *= f;
+            o_low[d][c] *= f;
+            o_low[d][c + 2] *= f;
           }
         }
       }
@@ -373,13 +380,16 @@ __global__ void __launch_bounds__(kThreads, 1) split_attention_kernel(const Attn
       const float e0 = exp2_fast(x[0] - r0), e1 = exp2_fast(x[1] - r1), e2 = exp2_fast(x[2] - r0), e3 = exp2_fast(x[3] - r1);
       l[0] += e0 + e2;
       l[1] += e1 + e3;
-      const uint32_t b0 = transpose8x8(pack_bf16(e0, e1)), b1 = transpose8x8(pack_bf16(e2, e3));
+      const uint32_t h0 = pack_bf16(e0, e1), h1 = pack_bf16(e2, e3);
+      const uint32_t b0 = transpose8x8(h0), b1 = transpose8x8(h1);
+      const uint32_t c0 = transpose8x8(pack_bf16(e0 - bf16_lo(h0), e1 - bf16_hi(h0))), c1 = transpose8x8(pack_bf16(e2 - bf16_lo(h1), e3 - bf16_hi(h1)));
 #pragma unroll
       for (int d = 0; d < D / 16; ++d) {
         uint32_t a[4];
         const uint32_t r = (mi >> 1) * 8u + r8;
         ldsm4_t(a, vt + r * L::kRow + (((d * 2u + (mi & 1u)) ^ r8) << 4));
         mma_bf16(o[d], a, b0, b1);
+        mma_bf16(o_low[d], a, c0, c1);
       }
     }
 #pragma unroll
@@ -390,7 +400,7 @@ __global__ void __launch_bounds__(kThreads, 1) split_attention_kernel(const Attn
       ++at.tile;
       continue;
     }
-    // ---- end of the group, or of this CTA's part of it: the four warps' results become one ------------
+    // ---- end of the group, or of this CTA's part of it: the warps' results become one ------------
     fresh = true;
 #pragma unroll
     for (int d = 4; d < 32; d <<= 1) {
@@ -407,6 +417,8 @@ __global__ void __launch_bounds__(kThreads, 1) split_attention_kernel(const Attn
       float* w = so + (warp * kHeads + 2u * (lane & 3u)) * L::kORow + (lane >> 2);
 #pragma unroll
       for (int d = 0; d < D / 16; ++d) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[d][c] += fabsf(o_low[d][c]) < INFINITY ? o_low[d][c] : 0.f;
         w[d * 16] = o[d][0];
         w[d * 16 + L::kORow] = o[d][1];
         w[d * 16 + 8] = o[d][2];

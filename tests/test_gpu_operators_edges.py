@@ -105,3 +105,53 @@ def test_rope_append_says_which_slots_are_out_of_range(tq, slot, bad):
     if slot == 31:
         k0[1, 0, 15], v0[1, 0, 15] = k[1, 0], v[1, 0]
     assert torch.equal(kp, k0) and torch.equal(vp, v0)
+
+
+# ------------------------------------------------------------------------------------------------ attention of one token: p
+def _cancelling(g, n, K, D):
+    """Keys of small scores and values of both signs: weights are alike and the sums of p v nearly cancel, so that an error of p shows."""
+    return randn(g, n, K, D, dtype=BF, scale=0.5), torch.where(torch.rand(n, K, D, generator=g, device="cuda") < 0.5, -1.0, 1.0).to(BF)
+
+
+def _close(got, q, k, v, scale):
+    """The scores' sums of |q k| scale stay below 8: their fp32 errors (128 * 2^-24 * 8 at most) move p by 2^-14 of itself, p's two parts keep
+    it to 2^-16, and a weight is a quotient of two such sums: 2^-12.9 of sum p |v| in all, taken as 2^-12, and the result's rounding."""
+    q, k, v = q.to(F64), k.to(F64), v.to(F64)
+    assert float((q.abs() @ k.abs().t()).max()) * scale < 8
+    p = torch.softmax(q @ k.t() * scale, -1)
+    out = p @ v
+    bound = (p @ v.abs()) * 2.0 ** -12 + out.abs() * 2.0 ** -8
+    assert bool(((got.to(F64) - out).abs() <= bound).all()), float(((got.to(F64) - out).abs() - bound).max())
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n", [2, 3, 5, 16, 40])
+def test_one_token_holds_p_to_more_than_bf16(tq, ws, D, n):
+    g = gen(n + D)
+    H, K = 16, 2
+    k, v = _cancelling(g, n, K, D)
+    q = randn(g, 6, H, D, dtype=BF, scale=0.7)
+    cross = tq.tq_cross_attention(q[:, None], k.expand(6, -1, -1, -1), v.expand(6, -1, -1, -1), ws)[:, 0]
+    kp, vp = (torch.zeros(n, K, 1, D, dtype=BF, device="cuda") for _ in range(2))
+    kp[:, :, 0], vp[:, :, 0] = k, v
+    table = torch.arange(n, dtype=torch.int32, device="cuda").expand(6, -1).contiguous()
+    paged = tq.tq_paged_attention(q, tq.tq_kv_cache(kp, vp), table, torch.full((6,), n, dtype=torch.int32, device="cuda"), ws)
+    for out in (cross, paged):
+        for h in range(K):
+            hs = slice(h * (H // K), (h + 1) * (H // K))
+            _close(out[:, hs].reshape(-1, D), q[:, hs].reshape(-1, D), k[:, h], v[:, h], D ** -0.5)
+
+
+def test_one_token_and_infinite_values(tq, ws):
+    """A value of V that is infinite makes its column infinite (both signs: NaN), and no other; so also where p's lower part is 0 or negative."""
+    g = gen(3)
+    k, v = _cancelling(g, 40, 1, 64)
+    v[0, 0, 1], v[7, 0, 2], v[39, 0, 3] = math.inf, -math.inf, math.inf
+    v[3, 0, 4], v[5, 0, 4] = math.inf, -math.inf
+    q = randn(g, 4, 3, 64, dtype=BF, scale=0.7)
+    for n in (1, 40):  # one state: p is 1
+        out = tq.tq_cross_attention(q[:, None], k[:n].expand(4, -1, -1, -1), v[:n].expand(4, -1, -1, -1), ws)[:, 0]
+        assert bool((out[..., 1] == math.inf).all())
+        if n > 1:
+            assert bool((out[..., 2] == -math.inf).all()) and bool((out[..., 3] == math.inf).all()) and bool(out[..., 4].isnan().all())
+        assert bool(out[..., 5:].isfinite().all()) and bool(out[..., 0].isfinite().all())
