@@ -648,13 +648,27 @@ int tq_cross_attention(const tq_encoder_kv* kv, const void* d_q, int64_t q_batch
   p.head_parts = (p.group + kHeads - 1u) / kHeads;
   p.scale_log2 = scale * 1.4426950408889634f;
   cudaStream_t st = (cudaStream_t)cuda_stream;
-  // Few tokens over few bytes: this kernel, which reads the states again (from L2) for every token, against the tensor-core
-  // kernel, which reads them once but starts and joins more slowly.  Measured (us, this | the other): 1 x 6404 states of 8 x 128,
-  // 64 query heads: 2 tokens 19.6 | 30.8, 4: 23.2 | 32.3, 8: 34.7 | 34.3; 4 x 6404: 2 tokens 39.5 | 37.5, 4: 61 | 38; 4 x 1601:
-  // 4 tokens 23.7 | 23.6, 8: 35.7 | 25.0; 1 x 500 of 8 x 64: 4 tokens 7.2 | 13.0, 16: 12.0 | 13.4.
-  constexpr uint64_t kFewTokens = 16, kFewBytes = 110000000;
-  const uint64_t read = 4ull * kv->n_seqs * kv->n_states * kv->n_kv_heads * kv->head_dim;
-  if (n_tokens > 1 && (n_tokens > kFewTokens || n_tokens * read > kFewBytes)) {
+  // Few tokens over few states: this kernel, which reads the states again (from L2) for every token and every 8 heads of a group,
+  // against the tensor-core kernel, which reads them once but starts slowly and, where groups are few, leaves many parts of
+  // 256 rows to be joined.  One side's cost goes by its visits of (token, key-value head, 8 heads, state), the other's by the
+  // parts of a group and their size.  Measured (us, this | the other), at head_dim 128 but for the last two:
+  //   1 x 6404 states, 64 / 8 heads: 4 tokens 21.4 | 30.0, 6: 25.8 | 31.0, 8: 32.6 | 31.4, 16: 54.3 | 33.2
+  //   4 x 6404, 32 / 8: 2 tokens 37.0 | 37.1, 4: 57.0 | 37.8
+  //   4 x 1601, 64 / 8: 2 tokens 17.0 | 22.5, 4: 23.3 | 23.6, 8: 36.7 | 24.5
+  //   4 x 1601, 64 / 2: 2 tokens 15.8 | 20.4, 4: 21.7 | 21.6, 8: 34.5 | 25.2, 16: 59.7 | 31.1
+  //   1 x 6404, 64 / 2: 4 tokens 21.4 | 43.6, 8: 32.7 | 49.6, 12: 43.5 | 47.3, 16: 54.3 | 50.9
+  //   1 x 20000, 64 / 2: 4 tokens 44.9 | 68.1, 8: 78.0 | 74.3, 16: 143 | 55
+  //   2 x 3000, 32 / 2 x 64: 4 tokens 12.4 | 20.0, 12: 21.0 | 21.4, 16: 25.2 | 22.2
+  //   1 x 500, 32 / 8 x 64: 4 tokens 6.6 | 12.6, 16: 10.4 | 12.9
+  constexpr uint64_t kFewTokens = 16, kFewVisits = 120000, kPartVisits = 84;  // of a column of a part
+  auto few = [&] {
+    const uint64_t tokens = (uint64_t)kv->n_seqs * n_tokens, tiles = ((uint64_t)kv->n_states + 127u) / 128u;
+    const uint64_t groups = (uint64_t)kv->n_seqs * kv->n_kv_heads * (((uint64_t)n_tokens * p.group + 255u) / 256u);
+    const uint64_t ctas = (uint64_t)sm_count(), parts = min(tiles, groups < ctas ? ctas / groups : 1u);
+    const uint64_t visits = tokens * kv->n_kv_heads * p.head_parts;  // of a state
+    return kv->n_states == 0 || visits <= (kFewVisits + kPartVisits * kv->head_dim * parts) / kv->n_states;
+  };
+  if (n_tokens > 1 && (n_tokens > kFewTokens || !few())) {
     bool served = false;
     const int rc = tq_cross_launch(kv, d_q, q_batch_stride, q_token_stride, n_tokens, n_q_heads, d_kv_len, d_mask, p.block_len, p.n_blocks,
                                    p.scale_log2, d_out, d_lse, p.ws, cuda_stream, &served);

@@ -155,3 +155,23 @@ def test_one_token_and_infinite_values(tq, ws):
         if n > 1:
             assert bool((out[..., 2] == -math.inf).all()) and bool((out[..., 3] == math.inf).all()) and bool(out[..., 4].isnan().all())
         assert bool(out[..., 5:].isfinite().all()) and bool(out[..., 0].isfinite().all())
+
+
+# ------------------------------------------------------------------------------------------------ which kernel a call takes
+def tensor_core_kernel(ws, call):
+    """Whether the call ran on the tcgen05 kernel, which leaves an entry for every group (or CTA) in the workspace."""
+    entries = ws.buf[512 * 4 + 256:][:512 * 16]
+    entries.zero_()
+    call()
+    return bool(entries.any())
+
+
+@pytest.mark.parametrize("B,S,H,K,D,few,many", [(1, 6404, 64, 8, 128, 6, 8), (4, 1601, 64, 8, 128, 2, 6), (4, 1601, 64, 2, 128, 3, 8), (1, 6404, 64, 2, 128, 8, 17),
+                                                (1, 20000, 64, 2, 128, 4, 12), (2, 3000, 32, 2, 64, 8, 16), (1, 500, 32, 8, 64, 16, 17)])
+def test_the_faster_kernel_for_few_tokens(tq, ws, B, S, H, K, D, few, many):
+    """Sizes at which one kernel was measured to be the faster one by 10 % and more; groups of 4 to 32 heads."""
+    g = gen(4)
+    k, v = randn(g, B, S, K, D, dtype=BF), randn(g, B, S, K, D, dtype=BF)
+    for T, want in ((few, False), (many, True)):
+        q = randn(g, B, T, H, D, dtype=BF)
+        assert tensor_core_kernel(ws, lambda: tq.tq_cross_attention(q, k, v, ws)) == want, T
