@@ -497,8 +497,7 @@ typedef struct tq_encoder_kv {
  * over the states s < kv_len[b] whose block the token sees: mask[b][t][s / block_len] != 0 (image
  * tiles; block_len 1 is a mask of single states).  A token that sees nothing gives zeros and lse -inf.
  * States at or past kv_len and states that a token does not see may hold anything, Inf and NaN included
- * (a token is slow where some of its sequence's tokens see such a state and it does not: its output is computed again, which for
- * more than a million states may end in TQ_STATUS_WAIT_EXPIRED).
+ * (a token is slow where some of its sequence's tokens see such a state and it does not).
  * d_q: DEVICE bf16, [n_q_heads][head_dim] for each sequence and token, q_batch_stride and q_token_stride
  * elements apart (multiples of 8), 16-byte aligned.  d_kv_len: DEVICE int32 [n_seqs] or NULL (all states); values are
  * clamped to 0..n_states.  d_mask: DEVICE uint8 [n_seqs][n_tokens][ceil(n_states / block_len)] or NULL.

@@ -32,8 +32,7 @@
 // from the states it sees (slow, and only with a mask).
 //
 // Every wait is bounded; one that runs out raises TQ_STATUS_WAIT_EXPIRED, all roles leave their loops and
-// tensor memory is released on every path.  The limit leaves room for the slowest thing that a role may have to wait for: 32 rows
-// that a warp computes again one after the other, 18 ms for 1000 states (measured), seconds for 200000.
+// tensor memory is released on every path.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -66,7 +65,6 @@ constexpr uint32_t kCounts = 512, kCountBlocks = 32, kCountBytes = 1u << 18;
 // 12 us of 1.9 us a tile); where whole groups spread evenly enough, none is cut.
 constexpr uint32_t kCutTiles = 6;
 constexpr int kChunks = 2;              // p of a tile is handed to the product with V in so many pieces
-constexpr uint32_t kWaitLimit = 1u << 30;  // attempts: half a minute, 32 rows of 1.7 million states
 constexpr float kRescale = 8.0f;       // log2 of how far p may exceed 1
 
 // What the loader announces, in the first word of an entry: a tile of states for the group's rows, the end of the
@@ -314,7 +312,7 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
 
   bool ok = true;
   auto wait = [&](uint32_t b, uint32_t parity) {
-    ok = ok && mbar_wait<kWaitLimit>(b, parity, dead);
+    ok = ok && mbar_wait(b, parity, dead);
     ok = __all_sync(kFull, ok);
   };
   uint32_t e_slot = 0, e_round = 0;  // slot of the next entry this warp takes (or announces), and how often the slots have wrapped

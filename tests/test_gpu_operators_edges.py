@@ -175,25 +175,3 @@ def test_the_faster_kernel_for_few_tokens(tq, ws, B, S, H, K, D, few, many):
     for T, want in ((few, False), (many, True)):
         q = randn(g, B, T, H, D, dtype=BF)
         assert tensor_core_kernel(ws, lambda: tq.tq_cross_attention(q, k, v, ws)) == want, T
-
-
-def test_rows_computed_again_outlast_no_wait(tq, ws):
-    """An infinite value that one token sees and 39 do not: those rows are computed again from the states they see, 32 to a warp one
-    after the other, which takes longer (3.7 s) than the limit of the waits of the other warps (2 s).  A sequence to an SM, so that no
-    group is cut."""
-    g = gen(5)
-    B, T, S, D, n = torch.cuda.get_device_properties(0).multi_processor_count, 40, 200000, 64, 25
-    k, v = randn(g, 1, S, 1, D, dtype=BF), randn(g, 1, S, 1, D, dtype=BF)
-    v[0, 5] = math.inf
-    q = randn(g, B, T, 1, D, dtype=BF)
-    mask = torch.ones(B, T, n, dtype=torch.uint8, device="cuda")
-    mask[:, :T - 1, 0] = 0
-    out = tq.tq_cross_attention(q, k.expand(B, -1, -1, -1), v.expand(B, -1, -1, -1), ws, mask=mask, block_len=S // n)
-    assert tq.tq_attn_status(ws) == 0
-    assert not bool(out[:, T - 1].isfinite().any())
-    ks, vs = k[0, S // n:, 0].to(F64), v[0, S // n:, 0].to(F64)
-    for b in (0, B // 2, B - 1):
-        p = torch.softmax(q[b, :T - 1, 0].to(F64) @ ks.t() * D ** -0.5, -1)
-        want = p @ vs
-        bound = (p @ vs.abs()) * (2.0 ** -8 + 2.0 ** -10) + want.abs() * 2.0 ** -8
-        assert bool(((out[b, :T - 1, 0].to(F64) - want).abs() <= bound).all())
