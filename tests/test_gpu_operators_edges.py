@@ -175,3 +175,148 @@ def test_the_faster_kernel_for_few_tokens(tq, ws, B, S, H, K, D, few, many):
     for T, want in ((few, False), (many, True)):
         q = randn(g, B, T, H, D, dtype=BF)
         assert tensor_core_kernel(ws, lambda: tq.tq_cross_attention(q, k, v, ws)) == want, T
+
+
+# ------------------------------------------------------------------------------------------------ both kernels of cross attention
+def on(kernel, tq, ws, monkeypatch):
+    """Calls of tq_cross_attention from here on have to run on the tensor-core kernel, or on the other one."""
+    call = tq.tq_cross_attention
+
+    def checked(*a, **k):
+        got = []
+        assert tensor_core_kernel(ws, lambda: got.append(call(*a, **k))) == kernel
+        return got[0]
+
+    monkeypatch.setattr(tq, "tq_cross_attention", checked)
+
+
+@pytest.mark.parametrize("T,kernel", [(9, False), (40, True)])
+def test_a_broken_query_stays_by_itself(tq, ws, monkeypatch, T, kernel):
+    """A NaN in a query makes its own output NaN and leaves the others within their bound, with a mask (where spoiled rows are looked
+    for) and without.  (Not bit for bit: when a row's output is rescaled is decided for 32 rows together.)"""
+    from test_gpu_operators import attend_ref, within
+
+    on(kernel, tq, ws, monkeypatch)
+    g = gen(6)
+    S, H, K, D = 1500, 4, 2, 64
+    q, k, v = randn(g, 1, T, H, D, dtype=BF), randn(g, 1, S, K, D, dtype=BF), randn(g, 1, S, K, D, dtype=BF)
+    q[0, 4, 1, 3] = float("nan")
+    q[0, 5, 3] = float("inf")  # scores of both infinities
+    mask = torch.ones(1, T, 15, dtype=torch.uint8, device="cuda")
+    mask[0, 4:7, 3] = 0
+    for m in (None, mask):
+        seen = torch.ones(T, S, dtype=torch.bool, device="cuda") if m is None else m[0].bool().repeat_interleave(100, -1)
+        out = tq.tq_cross_attention(q, k, v, ws, mask=m, block_len=100)
+        assert bool(out[0, 4, 1].isnan().all()) and bool(out[0, 5, 3].isnan().all())
+        for h in range(H):
+            ok = torch.tensor([t for t in range(T) if (t, h) not in ((4, 1), (5, 3))], device="cuda")
+            want, _, bound = attend_ref(q[0, ok, h], k[0, :, h // 2], v[0, :, h // 2], seen[ok], D ** -0.5)
+            within(out[0, ok, h], want, bound)
+    assert tq.tq_attn_status(ws) == 0
+
+
+@pytest.mark.parametrize("T,kernel", [(2, False), (17, True)])
+@pytest.mark.parametrize("S,block", [(200, 1), (300, 7), (500, 100), (640, 128), (1000, 1000), (1300, 333), (90, 500)])
+def test_masks_on_both_kernels(tq, ws, monkeypatch, T, S, block, kernel):
+    from test_gpu_operators import cross_case
+
+    if S > 128 or not kernel:  # a single group of one tile leaves no entry to tell by
+        on(kernel, tq, ws, monkeypatch)
+    cross_case(tq, ws, 2, T, S, 8, 2, 128, kv_len=[S, max(1, S // 2 + 3)], block=block, seed=1)
+    cross_case(tq, ws, 2, T, S, 4, 4, 64, block=block, seed=2, mask_rate=0.1, layout=1)
+
+
+@pytest.mark.parametrize("T,kernel", [(3, False), (17, True)])
+def test_lengths_on_both_kernels(tq, ws, monkeypatch, T, kernel):
+    from test_gpu_operators import cross_case
+
+    on(kernel, tq, ws, monkeypatch)
+    cross_case(tq, ws, 4, T, 300, 8, 4, 64, kv_len=[0, 1, 300, 129], seed=3)
+    cross_case(tq, ws, 3, T, 257, 4, 1, 128, kv_len=[-4, 256, 1000], seed=4, spoil=False)
+
+
+@pytest.mark.parametrize("T,kernel", [(2, False), (20, True)])
+def test_a_long_split_on_both_kernels(tq, ws, monkeypatch, T, kernel):
+    from test_gpu_operators import cross_case
+
+    on(kernel, tq, ws, monkeypatch)
+    cross_case(tq, ws, 1, T, 20000, 8, 1, 128, seed=7)
+    cross_case(tq, ws, 1, T, 20000, 8, 1, 64, seed=8, block=2000)
+
+
+@pytest.mark.parametrize("B,T,S,H,K,D", [(4, 6, 1601, 64, 8, 128), (4, 16, 1601, 64, 2, 128), (3, 16, 4000, 40, 4, 64), (1, 16, 6404, 36, 2, 128)])
+def test_few_tokens_on_the_tensor_core_kernel(tq, ws, monkeypatch, B, T, S, H, K, D):
+    """2 to 16 tokens over so many states that the tensor-core kernel takes them."""
+    from test_gpu_operators import cross_case
+
+    on(True, tq, ws, monkeypatch)
+    cross_case(tq, ws, B, T, S, H, K, D, kv_len=[S - 7 * b for b in range(B)], seed=9)
+    cross_case(tq, ws, B, T, S, H, K, D, block=401, seed=10)
+
+
+# ------------------------------------------------------------------------------------------------ graphs and streams
+def _calls(tq, g, T):
+    """One call of each operator on tensors of its own: -> (run(workspace, cache) writing into `outs`, outs)."""
+    h, w, d = randn(g, 5, 512, dtype=BF), randn(g, 512), randn(g, 5, 512)
+    q, k, v = randn(g, 5, 4, 64), randn(g, 5, 2, 64), randn(g, 5, 2, 64)
+    pos, slots = torch.arange(5, dtype=torch.int32, device="cuda"), torch.tensor([3, 17, -1, 30, 8], dtype=torch.int32, device="cuda")
+    pages, lens = torch.tensor([[0, 1]] * 5, dtype=torch.int32, device="cuda"), torch.tensor([20, 9, 0, 32, 1], dtype=torch.int32, device="cuda")
+    table = torch.rand(8, 64, generator=g, device="cuda")
+    kp, vp = randn(g, 2, 2, 16, 64, dtype=BF), randn(g, 2, 2, 16, 64, dtype=BF)
+    cache = tq.tq_kv_cache(kp, vp)
+    qc, kc, vc = randn(g, 2, T, 8, 64, dtype=BF), randn(g, 2, 3000, 2, 64, dtype=BF), randn(g, 2, 3000, 2, 64, dtype=BF)
+    ho, o, rot = torch.empty_like(h), torch.empty(5, 512, dtype=BF, device="cuda"), torch.empty(5, 4, 64, dtype=BF, device="cuda")
+    paged, cross, lse = torch.empty_like(rot), torch.empty_like(qc), torch.empty(2, T, 8, device="cuda")
+    outs = [ho, o, rot, kp, vp, paged, cross, lse]
+
+    def run(ws):
+        tq.tq_rmsnorm(h, w, d, h_out=ho, out=o)
+        tq.tq_rope_append(q, k, v, table, pos, slots, cache, out=rot)
+        tq.tq_paged_attention(rot, cache, pages, lens, ws, out=paged)
+        tq.tq_cross_attention(qc, kc, vc, ws, out=cross, lse=lse)
+
+    return run, outs
+
+
+@pytest.mark.parametrize("T", [1, 40])
+def test_graphs(tq, ws, T):
+    run, outs = _calls(tq, gen(7), T)
+    run(ws)
+    want = [x.clone() for x in outs]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(ws)
+        run(ws)
+    for _ in range(3):
+        for x in (outs[0], outs[1], outs[2], *outs[5:]):
+            x.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
+    assert tq.tq_attn_status(ws) == 0
+
+
+@pytest.mark.parametrize("T", [1, 40])
+def test_two_streams_with_a_workspace_each(tq, T):
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    spaces = [tq.tq_attn_workspace(stream=s) for s in streams]
+    sets = [_calls(tq, gen(8 + n), T) for n in range(2)]
+    want = []
+    for (run, outs), space in zip(sets, spaces):
+        torch.cuda.synchronize()
+        run(space)
+        want.append([x.clone() for x in outs])
+    for _ in range(5):
+        for _, outs in sets:
+            for x in (outs[0], outs[1], outs[2], *outs[5:]):
+                x.zero_()
+        torch.cuda.synchronize()
+        for _ in range(20):
+            for (run, _), space, stream in zip(sets, spaces, streams):
+                with torch.cuda.stream(stream):
+                    run(space)
+        torch.cuda.synchronize()
+        for (_, outs), w in zip(sets, want):
+            assert all(torch.equal(a, b) for a, b in zip(outs, w))
+    assert [tq.tq_attn_status(s) for s in spaces] == [0, 0]
