@@ -61,8 +61,11 @@ constexpr uint32_t kTmemCols = 512;
 // rows), every CTA first counts the tiles of states that each pair's rows see, and the shares are equal in those; otherwise
 // a unit is any tile below kv_len, and the shares of a CTA whose tiles are hidden are finished early.
 constexpr uint32_t kCounts = 512, kCountBlocks = 32, kCountBytes = 1u << 18;
-// Cutting groups costs about as much as this many tiles of states (their parts go through memory, the last CTA joins them;
-// 12 us of 1.9 us a tile); where whole groups spread evenly enough, none is cut.
+// Where whole groups spread evenly enough none is cut: up to a quarter of a share, or kCutTiles tiles of states, over the shares
+// that cuts would give.  Parts go through memory to the joining kernel, and the long shares of CTAs that go through the same states
+// side by side fall apart.  Measured (us, cut | whole; tiles of a share | over it): 152 groups of 3 tiles (4 | 2) 32.3 | 35.5, of
+// 5 (6 | 4) 36.0 | 42.4; 64 / 8 heads of 64, 2 x 600 tokens, 1024 states (17 | 7) 57.0 | 68.5; 32 / 8 heads of
+// 128, 3 x 1000 tokens, 1601 states (34 | 5) 119 | 116; 64 / 8, 1 x 4096 tokens, 6404 states (353 | 4) 719 | 715.
 constexpr uint32_t kCutTiles = 6;
 constexpr int kChunks = 2;              // p of a tile is handed to the product with V in so many pieces
 constexpr float kRescale = 8.0f;       // log2 of how far p may exceed 1
@@ -371,7 +374,7 @@ __global__ void __launch_bounds__(kCrossThreads, 1)
     // the longest share without cuts: whole groups of one size, or up to one group over the mean
     const uint32_t n_groups = p.n_seqs * p.n_kv_heads * p.row_tiles;
     const uint32_t longest = most == least ? ((n_groups - 1u) / ctas + 1u) * most : mean + most;
-    const bool cut = longest > mean + kCutTiles;
+    const bool cut = longest > mean + (over != 0u ? 1u : 0u) + min(kCutTiles, mean / 4u);
     uint32_t u0 = 0, u1 = 0;  // this CTA's share; without cuts, the groups that start in it
     if (blockIdx.x < ctas) {
       u0 = mean * blockIdx.x + min(blockIdx.x, over);

@@ -320,3 +320,21 @@ def test_two_streams_with_a_workspace_each(tq, T):
         for (_, outs), w in zip(sets, want):
             assert all(torch.equal(a, b) for a, b in zip(outs, w))
     assert [tq.tq_attn_status(s) for s in spaces] == [0, 0]
+
+
+@pytest.mark.parametrize("B,T,S,H,K,D,cut", [(19, 256, 384, 8, 8, 128, True), (10, 256, 640, 16, 16, 128, True), (12, 700, 900, 8, 8, 128, False), (3, 1000, 1601, 32, 8, 128, False)])
+def test_groups_are_cut_where_that_is_faster(tq, ws, B, T, S, H, K, D, cut):
+    """Sizes at which one side was measured to be the faster one (on 148 SMs), and the first and last group's results."""
+    from test_gpu_operators import attend_ref, within
+
+    if torch.cuda.get_device_properties(0).multi_processor_count != 148:
+        pytest.skip("the shares are those of 148 SMs")
+    g = gen(11)
+    q, k, v = randn(g, B, T, H, D, dtype=BF), randn(g, B, S, K, D, dtype=BF), randn(g, B, S, K, D, dtype=BF)
+    entries = ws.buf[512 * 4 + 256:][:512 * 16].view(torch.int32).view(512, 4)
+    entries.zero_()
+    out = tq.tq_cross_attention(q, k, v, ws)
+    assert bool((entries[:, 0] > 1).any()) == cut
+    for b, h in ((0, 0), (B // 2, H // 2), (B - 1, H - 1)):
+        want, _, bound = attend_ref(q[b, :, h], k[b, :, h // (H // K)], v[b, :, h // (H // K)], torch.ones(T, S, dtype=torch.bool, device="cuda"), D ** -0.5)
+        within(out[b, :, h], want, bound)
