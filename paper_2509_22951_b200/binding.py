@@ -845,7 +845,7 @@ def _heads(x: torch.Tensor, tokens: int, n: int, dim: int, device: int, dtype) -
         assert shape[1] == n * dim
     else:
         assert shape[1:] == (n, dim) and (n == 1 or stride[1] == dim)
-    return stride[0]
+    return stride[0] if tokens > 1 else 0  # of one token it means nothing
 
 
 @functools.lru_cache(maxsize=64)

@@ -338,3 +338,20 @@ def test_groups_are_cut_where_that_is_faster(tq, ws, B, T, S, H, K, D, cut):
     for b, h in ((0, 0), (B // 2, H // 2), (B - 1, H - 1)):
         want, _, bound = attend_ref(q[b, :, h], k[b, :, h // (H // K)], v[b, :, h // (H // K)], torch.ones(T, S, dtype=torch.bool, device="cuda"), D ** -0.5)
         within(out[b, :, h], want, bound)
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_one_token_of_a_row_of_any_length(tq, monkeypatch, native):
+    """The stride of a single token means nothing, in either form of the call."""
+    if not native:
+        monkeypatch.setattr(tq, "_fast", None)
+    g = gen(12)
+    wide = randn(g, 3, 515)
+    q, k, v = wide[:1, :256], wide[:1, 256:384], wide[:1, 384:512]
+    kp, vp = (torch.zeros(2, 2, 16, 64, dtype=BF, device="cuda") for _ in range(2))
+    table = torch.cat([torch.ones(4, 32), torch.zeros(4, 32)], 1).cuda()
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    out = tq.tq_rope_append(q, k, v, table, i32(2), i32(17), tq.tq_kv_cache(kp, vp))
+    assert torch.equal(out.view(-1), q[0].to(BF)) and torch.equal(kp[1, :, 1].reshape(-1), k[0].to(BF)) and torch.equal(vp[1, :, 1].reshape(-1), v[0].to(BF))
+    with pytest.raises(tq.TqError):  # of two tokens it has to be a multiple of 8
+        tq.tq_rope_append(wide[:2, :256], wide[:2, 256:384], wide[:2, 384:512], table, i32(1, 2), i32(3, 4), tq.tq_kv_cache(kp, vp))
