@@ -355,3 +355,19 @@ def test_one_token_of_a_row_of_any_length(tq, monkeypatch, native):
     assert torch.equal(out.view(-1), q[0].to(BF)) and torch.equal(kp[1, :, 1].reshape(-1), k[0].to(BF)) and torch.equal(vp[1, :, 1].reshape(-1), v[0].to(BF))
     with pytest.raises(tq.TqError):  # of two tokens it has to be a multiple of 8
         tq.tq_rope_append(wide[:2, :256], wide[:2, 256:384], wide[:2, 384:512], table, i32(1, 2), i32(3, 4), tq.tq_kv_cache(kp, vp))
+
+
+@pytest.mark.parametrize("cols", [64, 256, 2048, 4096, 8192])
+@pytest.mark.parametrize("ht", [BF, F32])
+def test_rmsnorm_of_exact_sums_is_that_of_elementary_operations(tq, cols, ht):
+    """Small integers in rows of a power of two: the mean square is exact in any order of summation, so scale and levels are those of
+    the formula in fp32 operations, bit for bit (the scale by IEEE division, which torch's division by a number is not)."""
+    g = gen(13)
+    h, w = torch.randint(-8, 9, (300, cols), generator=g, device="cuda").to(ht), randn(g, cols, scale=0.2) + 1
+    x = h.float()
+    n = x * torch.rsqrt((x * x).mean(-1, keepdim=True) + 1e-5) * w
+    scale = torch.from_numpy(n.abs().amax(-1).cpu().numpy() / np.float32(127)).cuda()
+    q, s = tq.tq_rmsnorm_q8(h, w, eps=1e-5)
+    assert torch.equal(s, scale)
+    assert torch.equal(q.float(), (n / scale[:, None]).round().clamp(-127, 127))
+    assert torch.equal(tq.tq_rmsnorm(h, w, eps=1e-5), n.to(BF))
