@@ -73,15 +73,20 @@ __device__ __forceinline__ float scale_of(float amax) {
   const float s = __fdiv_rn(amax, 127.0f);
   return s == 0.f ? 1.0f : s;
 }
-__device__ __forceinline__ void levels(const float (&n)[8], float scale, int8_t (&b)[8]) {
+__device__ __forceinline__ void levels(float (&n)[8], float scale, int8_t (&b)[8]) {
+  if (scale < 0x1p-100f) {  // 1 / scale may overflow: both sides of the quotient 2^64 times as large, which is exact
+    scale *= 0x1p64f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) n[e] *= 0x1p64f;
+  }
   const float inv = 1.0f / scale;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     // the product with 1 / scale is within 2^-16 of the quotient: only near a half can the two round differently, and there
-    // the quotient itself is taken; so it is where 1 / scale overflows (scale below 2^-128)
+    // the quotient itself is taken
     const float v = n[e] * inv;
     float r = rintf(v);
-    if (inv == INFINITY || fabsf(fabsf(v - r) - 0.5f) < 1e-3f) r = rintf(__fdiv_rn(n[e], scale));
+    if (fabsf(fabsf(v - r) - 0.5f) < 1e-3f) r = rintf(__fdiv_rn(n[e], scale));
     b[e] = scale == scale ? (int8_t)fminf(fmaxf(r, -127.f), 127.f) : (int8_t)0;
   }
 }
