@@ -63,10 +63,11 @@ constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kCounts = 512, kCountBlocks = 32, kCountBytes = 1u << 18;
 // Where whole groups spread evenly enough none is cut: up to a quarter of a share, or kCutTiles tiles of states, over the shares
 // that cuts would give.  Parts go through memory to the joining kernel, and the long shares of CTAs that go through the same states
-// side by side fall apart.  Measured (us, cut | whole; tiles of a share | over it): 152 groups of 3 tiles (4 | 2) 32.3 | 35.5, of
-// 5 (6 | 4) 36.0 | 42.4; 64 / 8 heads of 64, 2 x 600 tokens, 1024 states (17 | 7) 57.0 | 68.5; 32 / 8 heads of
-// 128, 3 x 1000 tokens, 1601 states (34 | 5) 119 | 116; 64 / 8, 1 x 4096 tokens, 6404 states (353 | 4) 719 | 715.
-constexpr uint32_t kCutTiles = 6;
+// side by side fall apart.  Measured (us, cut | whole; tiles of a cut share | over it): 152 groups of 3 tiles (4 | 2) 32.3 | 35.5, of
+// 5 (6 | 4) 36.0 | 42.4; 64 / 8 heads of 64, 2 x 600 tokens, 1024 states (17 | 7) 57.0 | 68.5; 32 / 8 heads of 64, 1 x 1024 tokens,
+// 6404 states (45 | 6) 105 | 112; 32 / 8 heads of 128, 3 x 1000 tokens, 1601 states (34 | 5) 119 | 116; 64 / 8, 1 x 4096 tokens, 6404
+// states (353 | 4) 719 | 715.
+constexpr uint32_t kCutTiles = 5;
 constexpr int kChunks = 2;              // p of a tile is handed to the product with V in so many pieces
 constexpr float kRescale = 8.0f;       // log2 of how far p may exceed 1
 

@@ -322,7 +322,8 @@ def test_two_streams_with_a_workspace_each(tq, T):
     assert [tq.tq_attn_status(s) for s in spaces] == [0, 0]
 
 
-@pytest.mark.parametrize("B,T,S,H,K,D,cut", [(19, 256, 384, 8, 8, 128, True), (10, 256, 640, 16, 16, 128, True), (12, 700, 900, 8, 8, 128, False), (3, 1000, 1601, 32, 8, 128, False)])
+@pytest.mark.parametrize("B,T,S,H,K,D,cut", [(19, 256, 384, 8, 8, 128, True), (10, 256, 640, 16, 16, 128, True), (1, 1024, 6404, 32, 8, 64, True),
+                                             (12, 700, 900, 8, 8, 128, False), (3, 1000, 1601, 32, 8, 128, False)])
 def test_groups_are_cut_where_that_is_faster(tq, ws, B, T, S, H, K, D, cut):
     """Sizes at which one side was measured to be the faster one (on 148 SMs), and the first and last group's results."""
     from test_gpu_operators import attend_ref, within
