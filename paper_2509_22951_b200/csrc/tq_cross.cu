@@ -1,4 +1,4 @@
-// Attention of many queries to an encoder's states (tq_cross_attention but for a few tokens over few states) on the
+// Attention of many queries to an encoder's states (tq_cross_attention but for a few tokens, see there) on the
 // 5th-generation tensor cores.
 //
 //   out = sum_s p_s v_s / sum_s p_s,   p_s = exp(scale q.k_s - m),   m a running maximum
@@ -12,7 +12,7 @@
 // rows, 128 states), and, as in the one-token kernel, each CTA takes an equal share of consecutive units:
 // a group that lies in several shares leaves its parts in the workspace, and a second, small kernel on all SMs joins
 // them in order.  (Joined by the CTA that finishes last: 1 x 17 tokens, 64 / 8 heads, 6404 states, 19 parts to a group: 77 us
-// instead of 38; 1 x 600 tokens, two or three parts: 132.8 instead of 135.3.)  So short prompts use all SMs too, and long ones have no last wave.
+// instead of 38, now 34; 1 x 600 tokens, two or three parts: 132.8 instead of 135.3.)  So short prompts use all SMs too, and long ones have no last wave.
 //
 // CTA, one to an SM.  Warp 8 loads: it decides which tiles of states some row of the group
 // sees, announces them one by one in a ring of entries that all roles follow, and brings their K and V
@@ -22,9 +22,10 @@
 // product with V.  The two halves alternate: the tensor core multiplies for one while the other takes its
 // exponentials.  Tensor memory: 2 x 128 columns of scores, 2 x head_dim columns of output.
 //
-// The output is rescaled only when a row's maximum has grown by more than 2^8 since the last rescaling:
-// p then stays below 2^8, which costs no precision in bf16 or in the fp32 sum, and nearly all of the
-// passes over the output in tensor memory are saved.
+// The output is rescaled only when a row's maximum has grown by more than 2^8 since the last rescaling (the online softmax of
+// Milakov and Gimelshein, 2018, with the rescaling delayed up to a threshold, a published refinement of it): p then stays
+// below 2^8, which costs no precision in bf16 or in the fp32 sum, and nearly all of the passes over the output in tensor
+// memory are saved.
 //
 // States that no row may see are not multiplied: whole tiles are skipped, the tail past kv_len is zeroed in
 // shared memory.  A state that only some rows see enters the others' sums with p = 0; if its value is Inf or
