@@ -183,13 +183,13 @@ def prepare(case, seed):
         s["k_pool"], s["v_pool"] = (randn(pool, K, page, D, dtype=torch.bfloat16) for _ in range(2))
     elif case["op"] == "sample":
         R, V, kind = case["rows"], case["vocab"], case["set"]
-        # a broad floor and, in other tokens for every row, a head that falls off with the rank; some rows are sharper than others;
-        # a few tokens are never allowed
-        x = randn(R, V, scale=2.0)
+        # a broad floor and, in other tokens for every row, a head that falls off with the rank; a third of the rows have hardly more than
+        # the floor, the others are the sharper the higher their head; a few tokens are never allowed
+        x = randn(R, V, scale=1.5)
         n = min(V, 256)
         at = torch.randint(0, V, (R, n), generator=g, device="cuda")
         sharp = torch.rand(R, 1, generator=g, device="cuda")
-        x.scatter_add_(1, at, (3.0 + 11.0 * sharp) - (1.0 + sharp) * torch.arange(1, n + 1, device="cuda").log()[None])
+        x.scatter_add_(1, at, (9.0 + 11.0 * sharp) - (1.0 + sharp) * torch.arange(1, n + 1, device="cuda").log()[None])
         if V > 8:
             x[:, 3] = x[:, 5] = -math.inf
         s["logits"] = x.to(DTYPES[case["x"]])
