@@ -518,6 +518,82 @@ int tq_attn_status(void* d_ws, void* cuda_stream, uint32_t* status);
  * normally with undefined outputs and TQ_STATUS_WAIT_EXPIRED, and nothing beside the outputs is written. */
 void tq_test_withhold_cross_entry(int on);
 
+/* ------------------------------------------------------------------------------------------
+ * A decode step with drafted tokens: several new tokens of a sequence go through the layers at once (the fused products take
+ * up to 32 vectors in one pass), the samples of all of them are drawn, and the drafted tokens that the samples agree with stay.
+ * The tokens of a step are rows, sequence after sequence: sequence b has rows first[b] .. first[b+1] - 1 (d_first: DEVICE
+ * int32 [n_seqs + 1], rising; values are clamped to 0..n_tokens).  Rows before the first sequence or past the last belong to no
+ * sequence (padding): nothing is written for them.  Row first[b] is the last token that is certain, the others are drafts; each follows an
+ * earlier one (its parent), so they are a tree, or a chain where each follows the one before.
+ * ---------------------------------------------------------------------------------------- */
+
+/* tq_rope_append of normalised queries and keys: every head of q and of k is first replaced by
+ *   x / sqrt(mean_c x_c^2 + eps) * w,   c = 0 .. head_dim - 1,
+ * in 32 bits (w: d_q_weight or d_k_weight, DEVICE fp32 [head_dim]; eps >= 0), then turned, and rounded once.  v is not normalised.
+ * Everything else is as with tq_rope_append. */
+int tq_qk_norm_rope_append(const void* d_q, const void* d_k, const void* d_v, int x_type, int64_t q_stride,
+                           int64_t k_stride, int64_t v_stride, uint32_t n_tokens, uint32_t n_q_heads,
+                           const float* d_q_weight, const float* d_k_weight, float eps, const float* d_table,
+                           uint32_t n_positions, uint32_t rot_dim, const int32_t* d_positions,
+                           const uint32_t* sections, uint32_t n_axes, int interleaved, const int32_t* d_slots,
+                           const tq_kv_cache* cache, void* d_q_out, void* cuda_stream);
+
+/* Attention of the new tokens over a paged cache that holds them already: lens[b] counts the states of sequence b with its n =
+ * first[b+1] - first[b] new tokens, which are the last n of them.  Token i (row first[b] + i) sees the states before them all, and
+ * of the new tokens' own
+ *   those whose bit is set in its row of d_mask (bit j % 32 of word j / 32 for new token j; tokens past 32 * mask_words - 1 are not
+ *   seen), DEVICE uint32 [n_tokens][mask_words], or
+ *   0 .. i where d_mask is NULL (a chain; a piece of a prompt).
+ *   out[row][h] = sum_s softmax_s(scale * q[row][h] . k_s) v_s,  lse[row][h] the natural logarithm of the denominator;
+ * a token that sees nothing gives zeros and lse -inf.  States that a token does not see may hold anything, Inf and NaN included (a token
+ * is slow where another token of its sequence sees such a state).  The same call gives the same bits.
+ * d_q: DEVICE bf16, n_tokens rows of [n_q_heads][head_dim], q_stride elements from row to row (multiple of 8), 16-byte aligned.
+ * Page table, lengths, workspace and status are those of tq_paged_attention, d_out bf16 [n_tokens][n_q_heads][head_dim],
+ * d_lse fp32 [n_tokens][n_q_heads] or NULL.  Fewer states than new tokens (lens[b] < n): the first ones have none.
+ * TQ_ERR_UNSUPPORTED_SHAPE where n_tokens x n_q_heads reaches 2^31 or tiles of 128 rows x key-value heads x tiles of 128 states 2^32. */
+int tq_tree_attention(const tq_kv_cache* cache, const void* d_q, int64_t q_stride, uint32_t n_tokens, uint32_t n_seqs,
+                      uint32_t n_q_heads, const int32_t* d_first, const int32_t* d_page_table, uint32_t max_pages,
+                      const int32_t* d_lens, const uint32_t* d_mask, uint32_t mask_words, float scale, void* d_out,
+                      float* d_lse, void* d_ws, uint64_t ws_bytes, void* cuda_stream);
+
+/* One token for each row of logits, by the row's own settings and its own uniform number u in [0, 1):
+ *   w_i = exp((x_i - max x) / temperature); the tokens in the order of falling x, the lower one first among equals:
+ *   top_k:  the first k are kept (all where k <= 0),
+ *   top_p:  of those, the ones before which less than p of their sum lies (all where p >= 1),
+ *   min_p:  of those, the ones with w_i >= min_p;
+ * the first one is always kept.  The sample is the first token, in the order of the vocabulary, up to which more than u of the kept
+ * tokens' sum lies.  A temperature of 0 (or less, or NaN) takes the first token in falling order, with logprob 0.
+ * d_logits: DEVICE, rows x vocab of x_type, row_stride elements from row to row (any).  d_uniform: DEVICE fp32 [rows].
+ * d_temperature, d_top_p, d_min_p: DEVICE fp32 [rows], d_top_k: DEVICE int32 [rows], each may be NULL (1; all; all; all).
+ * d_token: DEVICE int32 [rows].  d_logprob: DEVICE fp32 [rows] or NULL: logarithm of the token's share of the kept tokens' sum.
+ * A NaN counts as -inf.  Where some x_i are +inf they alone are kept, as equals.  A row without anything above -inf gives token -1 and
+ * logprob -inf.  vocab: 1..TQ_SAMPLE_MAX_VOCAB.
+ * Weights are held as integers, 40 bits below the largest and each within 2^-30 of itself or half a unit, and their sums are exact: a row's
+ * token depends on nothing but the row. */
+#define TQ_SAMPLE_MAX_VOCAB 262144u
+int tq_sample(const void* d_logits, int x_type, int64_t row_stride, uint32_t rows, uint32_t vocab,
+              const float* d_uniform, const float* d_temperature, const int32_t* d_top_k, const float* d_top_p,
+              const float* d_min_p, int32_t* d_token, float* d_logprob, void* cuda_stream);
+
+/* Which drafted tokens the samples agree with, and their keys and values moved to where they belong.  From row first[b] on: the
+ * sample of the row is the next token; the first later row of the sequence whose parent is the row and whose token is the sample is the
+ * next row; the walk ends where there is none, or after max_path rows.
+ *   d_path[b][d]: the d-th row of the walk (counted from first[b]; d_path[b][0] = 0), d_out_tokens[b][d]: its sample, both -1 past the
+ *   end; d_count[b]: rows of the walk; d_lens_out[b] = lens[b] - n + d_count[b],
+ * with lens and n as for tq_tree_attention.  In every cache the state of row d_path[b][d] (position lens[b] - n + d_path[b][d]) is copied to position
+ * lens[b] - n + d.  A sequence without rows has count 0 and keeps its length.
+ * d_tokens (drafted), d_parents (row of the parent, counted from first[b]; of row first[b] it means nothing; not below the row itself: never
+ * followed), d_sampled: DEVICE int32 [n_tokens].  caches: HOST, n_caches (0..TQ_MAX_CACHES) descriptions of the layers' caches, alike but for d_k,
+ * d_v and d_status, which share the page table (d_page_table may be NULL where n_caches is 0).  max_path: 1..TQ_TREE_MAX_PATH.  d_path, d_out_tokens: DEVICE
+ * int32 [n_seqs][max_path]; d_count, d_lens_out: DEVICE int32 [n_seqs], not overlapping an input.  A position or a page
+ * outside the cache is not touched and sets TQ_STATUS_BAD_PAGE in the caches' status words. */
+#define TQ_MAX_CACHES 128u
+#define TQ_TREE_MAX_PATH 256u
+int tq_tree_accept(const tq_kv_cache* caches, uint32_t n_caches, const int32_t* d_page_table, uint32_t max_pages,
+                   uint32_t n_seqs, uint32_t n_tokens, const int32_t* d_first, const int32_t* d_lens,
+                   const int32_t* d_tokens, const int32_t* d_parents, const int32_t* d_sampled, uint32_t max_path,
+                   int32_t* d_out_tokens, int32_t* d_path, int32_t* d_count, int32_t* d_lens_out, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -37,6 +37,9 @@ TQ_TYPE_BF16 = 0
 TQ_TYPE_F32 = 1
 TQ_NORM_MAX_COLS = 16384
 TQ_ROPE_MAX_AXES = 3
+TQ_SAMPLE_MAX_VOCAB = 262144
+TQ_MAX_CACHES = 128
+TQ_TREE_MAX_PATH = 256
 
 EXPORTS = [
     "tq_strerror", "tq_last_cuda_error", "tq_set_num_threads", "tq_quantize_tensor", "tq_quantize_tensor_bits", "tq_quantize_rows",
@@ -49,6 +52,7 @@ EXPORTS = [
     "tq_fused_gemv_stack", "tq_fused_gemv_stack_host", "tq_stack_launches", "tq_test_withhold_table_chunk", "tq_decompress_stack", "tq_stack_free", "tq_device_status", "tq_dmat_free",
     "tq_rmsnorm", "tq_rmsnorm_q8", "tq_rope_append", "tq_attn_workspace_size", "tq_attn_workspace_init", "tq_paged_attention",
     "tq_cross_attention", "tq_attn_status", "tq_test_withhold_cross_entry",
+    "tq_qk_norm_rope_append", "tq_tree_attention", "tq_sample", "tq_tree_accept",
 ]
 
 
@@ -153,6 +157,13 @@ def _load() -> C.CDLL:
         "tq_cross_attention": (C.c_int, [C.POINTER(_EncoderKv), vp, C.c_int64, C.c_int64, C.c_uint32, C.c_uint32, vp, vp, C.c_uint32,
                                          C.c_float, vp, vp, vp, C.c_uint64, vp]),
         "tq_attn_status": (C.c_int, [vp, vp, u32p]),
+        "tq_qk_norm_rope_append": (C.c_int, [vp, vp, vp, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_uint32, C.c_uint32, vp, vp, C.c_float, vp,
+                                             C.c_uint32, C.c_uint32, vp, u32p, C.c_uint32, C.c_int, vp, C.POINTER(_KvCache), vp, vp]),
+        "tq_tree_attention": (C.c_int, [C.POINTER(_KvCache), vp, C.c_int64, C.c_uint32, C.c_uint32, C.c_uint32, vp, vp, C.c_uint32, vp, vp,
+                                        C.c_uint32, C.c_float, vp, vp, vp, C.c_uint64, vp]),
+        "tq_sample": (C.c_int, [vp, C.c_int, C.c_int64, C.c_uint32, C.c_uint32, vp, vp, vp, vp, vp, vp, vp, vp]),
+        "tq_tree_accept": (C.c_int, [C.POINTER(_KvCache), C.c_uint32, vp, C.c_uint32, C.c_uint32, C.c_uint32, vp, vp, vp, vp, vp, C.c_uint32,
+                                     vp, vp, vp, vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -853,21 +864,9 @@ def _sections(sections):
     return (C.c_uint32 * len(sections))(*sections)
 
 
-def tq_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, positions: torch.Tensor,
-                   slots: torch.Tensor, cache: KvCache, sections=None, interleaved: bool = False, out: torch.Tensor | None = None,
-                   stream=None) -> torch.Tensor:
-    """q, k, v: CUDA bf16 or fp32 [tokens][heads * head dim] or [tokens][heads][head dim] (tokens may be strided); table: fp32
-    [positions][rot dim], cosines then sines; positions: int32 [axes][tokens] or [tokens]; slots: int32 [tokens], -1 for none;
-    sections: pairs of each axis (one axis: all).  -> rotated q, bf16 [tokens][q heads][head dim]; k and v are in the cache."""
-    if stream is None and _fast is not None:
-        r = _fast.rope_append(q, k, v, table, positions, slots, cache._addr, cache.device, sections, interleaved, out)
-        if r is not None:
-            return r
-    device = q.get_device()
-    ctx = _elsewhere(device, stream)
-    if ctx is not None:
-        with ctx:
-            return tq_rope_append(q, k, v, table, positions, slots, cache, sections, interleaved, out)
+def _rope_args(q, k, v, table, positions, slots, cache, sections, out, device):
+    """Checks what the calls with rotary positions share; -> tokens, heads, the arguments of q, k, v, those of table and positions, slots,
+    the result and its address."""
     D, K, shape, dtype = cache.head_dim, cache.n_kv_heads, q.shape, q.dtype
     T, H = shape[0], (shape[1] if len(shape) == 3 else shape[1] // D)
     assert cache.device == device and dtype in _TYPES
@@ -883,9 +882,27 @@ def tq_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, table: tor
         out = torch.empty((T, H, D), dtype=torch.bfloat16, device=q.device)
     else:
         assert out.get_device() == device and out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() == T * H * D
-    _check(_lib.tq_rope_append(q.data_ptr(), k.data_ptr(), v.data_ptr(), _TYPES[dtype], qs, ks, vs, T, H, table.data_ptr(), n_positions,
-                               rot, positions.data_ptr(), _sections(sec), axes, interleaved, slots.data_ptr(), cache._ref,
-                               out.data_ptr(), _raw_stream(device)), "tq_rope_append")
+    return (T, H, (q.data_ptr(), k.data_ptr(), v.data_ptr(), _TYPES[dtype], qs, ks, vs),
+            (table.data_ptr(), n_positions, rot, positions.data_ptr(), _sections(sec), axes), slots.data_ptr(), out, out.data_ptr())
+
+
+def tq_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, positions: torch.Tensor,
+                   slots: torch.Tensor, cache: KvCache, sections=None, interleaved: bool = False, out: torch.Tensor | None = None,
+                   stream=None) -> torch.Tensor:
+    """q, k, v: CUDA bf16 or fp32 [tokens][heads * head dim] or [tokens][heads][head dim] (tokens may be strided); table: fp32
+    [positions][rot dim], cosines then sines; positions: int32 [axes][tokens] or [tokens]; slots: int32 [tokens], -1 for none;
+    sections: pairs of each axis (one axis: all).  -> rotated q, bf16 [tokens][q heads][head dim]; k and v are in the cache."""
+    if stream is None and _fast is not None:
+        r = _fast.rope_append(q, k, v, table, positions, slots, cache._addr, cache.device, sections, interleaved, out)
+        if r is not None:
+            return r
+    device = q.get_device()
+    ctx = _elsewhere(device, stream)
+    if ctx is not None:
+        with ctx:
+            return tq_rope_append(q, k, v, table, positions, slots, cache, sections, interleaved, out)
+    T, H, x, where, slots, out, o = _rope_args(q, k, v, table, positions, slots, cache, sections, out, device)
+    _check(_lib.tq_rope_append(*x, T, H, *where, interleaved, slots, cache._ref, o, _raw_stream(device)), "tq_rope_append")
     return out
 
 
@@ -994,3 +1011,124 @@ def tq_cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, worksp
                                    D ** -0.5 if scale is None else scale, out.data_ptr(), lse, workspace.ptr, workspace.bytes,
                                    _raw_stream(device)), "tq_cross_attention")
     return out
+
+
+# ------------------------------------------------------------------------------ a decode step with drafted tokens
+def _like(x: torch.Tensor, device: int, dtype, *shape) -> int:
+    """Address of a contiguous tensor of this type and shape on the call's device."""
+    assert x.get_device() == device and x.dtype == dtype and x.is_contiguous() and x.shape == shape, f"{dtype} {shape} on device {device} is wanted"
+    return x.data_ptr()
+
+
+def tq_qk_norm_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_weight: torch.Tensor, k_weight: torch.Tensor,
+                           table: torch.Tensor, positions: torch.Tensor, slots: torch.Tensor, cache: KvCache, eps: float = 1e-5,
+                           sections=None, interleaved: bool = False, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """tq_rope_append with every head of q and k normalised first; q_weight, k_weight: fp32 [head dim]."""
+    device = q.get_device()
+    ctx = _elsewhere(device, stream)
+    if ctx is not None:
+        with ctx:
+            return tq_qk_norm_rope_append(q, k, v, q_weight, k_weight, table, positions, slots, cache, eps, sections, interleaved, out)
+    D = cache.head_dim
+    weights = _like(q_weight, device, torch.float32, D), _like(k_weight, device, torch.float32, D)
+    T, H, x, where, slots, out, o = _rope_args(q, k, v, table, positions, slots, cache, sections, out, device)
+    _check(_lib.tq_qk_norm_rope_append(*x, T, H, *weights, eps, *where, interleaved, slots, cache._ref, o, _raw_stream(device)),
+           "tq_qk_norm_rope_append")
+    return out
+
+
+def tq_tree_attention(q: torch.Tensor, cache: KvCache, page_table: torch.Tensor, first: torch.Tensor, lens: torch.Tensor,
+                      workspace: AttnWorkspace, mask: torch.Tensor | None = None, scale: float | None = None,
+                      out: torch.Tensor | None = None, lse: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """q: CUDA bf16 [tokens][q heads][head dim] (tokens may be strided); first: int32 [sequences + 1], rows of each sequence; page_table:
+    int32 [sequences][max pages]; lens: int32 [sequences], new tokens included; mask: int32 [tokens][words], bit j of a row's words set
+    where it sees the sequence's new token j (None: a chain); lse: fp32 [tokens][q heads], filled when given.  -> bf16 like q; rows of no
+    sequence are not written."""
+    device = q.get_device()
+    ctx = _elsewhere(device, stream)
+    if ctx is not None:
+        with ctx:
+            return tq_tree_attention(q, cache, page_table, first, lens, workspace, mask, scale, out, lse)
+    (T, H, D), stride = q.shape, q.stride()
+    assert cache.device == device and workspace.device == device and q.dtype == torch.bfloat16
+    assert D == cache.head_dim and stride[2] == 1 and (H == 1 or stride[1] == D)
+    B, max_pages = page_table.shape
+    table, first, lens = _like(page_table, device, torch.int32, B, max_pages), _like(first, device, torch.int32, B + 1), _like(lens, device, torch.int32, B)
+    words = 0 if mask is None else mask.shape[1]
+    mask = None if mask is None else _like(mask, device, torch.int32, T, words)
+    out, lse = _attn_out(q, out, lse, device)
+    _check(_lib.tq_tree_attention(cache._ref, q.data_ptr(), stride[0] if T > 1 else 0, T, B, H, first, table, max_pages, lens, mask, words,
+                                  cache.scale if scale is None else scale, out.data_ptr(), lse, workspace.ptr, workspace.bytes,
+                                  _raw_stream(device)), "tq_tree_attention")
+    return out
+
+
+def tq_sample(logits: torch.Tensor, uniform: torch.Tensor, temperature: torch.Tensor | None = None, top_k: torch.Tensor | None = None,
+              top_p: torch.Tensor | None = None, min_p: torch.Tensor | None = None, out: torch.Tensor | None = None,
+              logprob: torch.Tensor | bool | None = None, stream=None):
+    """logits: CUDA bf16 or fp32 [rows][vocab] (rows may be strided); uniform: fp32 [rows] in [0, 1); temperature, top_p, min_p: fp32
+    [rows]; top_k: int32 [rows].  -> int32 [rows] tokens; with logprob (True, or the fp32 [rows] tensor to fill) also their logarithms."""
+    device = logits.get_device()
+    ctx = _elsewhere(device, stream)
+    if ctx is not None:
+        with ctx:
+            return tq_sample(logits, uniform, temperature, top_k, top_p, min_p, out, logprob)
+    (R, V), stride = logits.shape, logits.stride()
+    assert logits.dtype in _TYPES and (stride[1] == 1 or V == 1)
+    u = _like(uniform, device, torch.float32, R)
+    t, k, p, m = (None if x is None else _like(x, device, dt, R) for x, dt in
+                  ((temperature, torch.float32), (top_k, torch.int32), (top_p, torch.float32), (min_p, torch.float32)))
+    if out is None:
+        out = torch.empty(R, dtype=torch.int32, device=logits.device)
+    if logprob is True:
+        logprob = torch.empty(R, dtype=torch.float32, device=logits.device)
+    lp = None if logprob is None or logprob is False else _like(logprob, device, torch.float32, R)
+    _check(_lib.tq_sample(logits.data_ptr(), _TYPES[logits.dtype], stride[0] if R > 1 else 0, R, V, u, t, k, p, m, _like(out, device, torch.int32, R),
+                          lp, _raw_stream(device)), "tq_sample")
+    return out if lp is None else (out, logprob)
+
+
+class KvCaches:
+    """The caches of a model's layers, alike in shape and strides, that share a page table; keeps them alive."""
+
+    def __init__(self, caches):
+        self.caches = list(caches)
+        assert len(self.caches) <= TQ_MAX_CACHES and len({c.device for c in self.caches}) <= 1
+        self._c = (_KvCache * max(1, len(self.caches)))(*[c._c for c in self.caches])
+        self._addr = C.addressof(self._c)
+        self.device = self.caches[0].device if self.caches else None
+
+    def __len__(self):
+        return len(self.caches)
+
+
+def tq_kv_caches(caches) -> KvCaches:
+    """caches: KvCache objects, one for each layer."""
+    return KvCaches(caches)
+
+
+def tq_tree_accept(caches: KvCaches | None, page_table: torch.Tensor | None, first: torch.Tensor, lens: torch.Tensor, tokens: torch.Tensor,
+                   parents: torch.Tensor, sampled: torch.Tensor, max_path: int, stream=None):
+    """first: CUDA int32 [sequences + 1]; lens: int32 [sequences], new tokens included; tokens (drafted), parents (counted from the
+    sequence's first row), sampled: int32 [rows]; page_table: int32 [sequences][max pages].  -> (samples along the path, int32
+    [sequences][max_path]; the path's rows, likewise, both -1 past its end; its length, int32 [sequences]; new lens): the path's keys
+    and values lie behind the certain ones in every cache."""
+    device = first.get_device()
+    ctx = _elsewhere(device, stream)
+    if ctx is not None:
+        with ctx:
+            return tq_tree_accept(caches, page_table, first, lens, tokens, parents, sampled, max_path)
+    n = 0 if caches is None else len(caches)
+    assert not n or caches.device == device
+    B, T = first.numel() - 1, tokens.numel()
+    assert max_path >= 1
+    f, length = _like(first, device, torch.int32, B + 1), _like(lens, device, torch.int32, B)
+    rows = [_like(x, device, torch.int32, T) for x in (tokens, parents, sampled)]
+    max_pages = page_table.shape[1] if n else 0
+    table = _like(page_table, device, torch.int32, B, max_pages) if n else None
+    both = torch.empty((2, B, max_path), dtype=torch.int32, device=first.device)
+    ends = torch.empty((2, B), dtype=torch.int32, device=first.device)
+    (out_tokens, path), (count, lens_out) = both.unbind(), ends.unbind()
+    _check(_lib.tq_tree_accept(caches._c if n else None, n, table, max_pages, B, T, f, length, *rows, max_path, out_tokens.data_ptr(),
+                               path.data_ptr(), count.data_ptr(), lens_out.data_ptr(), _raw_stream(device)), "tq_tree_accept")
+    return out_tokens, path, count, lens_out

@@ -1,10 +1,14 @@
-// Rotary positions of new tokens and the write of their keys and values to the cache (tq_rope_append).
+// Rotary positions of new tokens and the write of their keys and values to the cache (tq_rope_append), with the norm of every
+// query and key head before it (tq_qk_norm_rope_append).
 //
 // Pair i of a head, (a, b) -> (a cos - b sin, a sin + b cos), with the cosine and sine of table row p,
 // p the position on the pair's axis.  The pairs of a head are independent of one another: a thread owns
 // four pairs (eight elements) of the heads it visits, loads their eight cosines and sines once per token
 // and reuses them over the token's query and key heads.  8 to 16 bytes move per two or three operations:
 // memory bound for prompts, latency for a decode step.
+//
+// Norm: the D / 8 lanes that have a head add its squares up by shuffles, and a thread keeps the eight weights of its elements
+// for queries and the eight for keys.  Eight multiplications and four shuffles an element group more on a path that waits for memory.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -32,6 +36,9 @@ struct RopeParams {
   uint32_t n_tokens, n_q_heads, n_positions, rot_dim;
   uint32_t axis_end[TQ_ROPE_MAX_AXES];  // first pair past each axis' section
   uint32_t n_axes;
+  const float* q_weight;  // norm of the heads
+  const float* k_weight;
+  float eps;
 };
 
 // Eight elements of a head as two runs of four, so that neighbouring lanes read neighbouring runs whatever the type and the
@@ -62,7 +69,7 @@ struct Raw4x2 {
 };
 
 // grid (tokens, parts of the heads); the 256 threads are 256 / (D / 8) heads side by side.
-template <int TYPE, bool INTERLEAVED, int D>
+template <int TYPE, bool INTERLEAVED, int D, bool NORM>
 __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopeParams p) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   constexpr uint32_t kPerHead = D / 8, kSide = kRopeThreads / kPerHead;
@@ -120,6 +127,16 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopePar
   }
   const size_t slot_at = keep ? (size_t)page * p.cache.page_stride + (size_t)((uint32_t)slot - page * p.cache.page_size) * p.cache.slot_stride + e0 : 0;
 
+  float wq[NORM ? 8 : 1], wk[NORM ? 8 : 1];
+  if constexpr (NORM) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t at = (i < 4 ? e0 : e1 - 4u) + i;
+      wq[i] = __ldg(p.q_weight + at);
+      wk[i] = __ldg(p.k_weight + at);
+    }
+  }
+
   float cs[4], sn[4];
 #pragma unroll
   for (uint32_t i = 0; i < 4; ++i) {
@@ -136,6 +153,20 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopePar
   for (; n < heads && (n < H || keep); n += step, load(n)) {
     float f[8];
     raw.get(f);
+    if constexpr (NORM) {
+      if (n < H + K) {
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += f[i] * f[i];
+        // the lanes of one head take the same way through this loop, those of the warp's other heads need not
+        const uint32_t mine = ((1u << kPerHead) - 1u) << (threadIdx.x % 32u / kPerHead * kPerHead);
+#pragma unroll
+        for (uint32_t d = kPerHead / 2u; d > 0; d >>= 1) sum += __shfl_xor_sync(mine, sum, d);
+        const float r = rsqrtf(sum * (1.f / D) + p.eps);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = f[i] * r * (n < H ? wq[i] : wk[i]);
+      }
+    }
     if (n < H + K && (turn_a || turn_b || !known)) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -156,25 +187,23 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopePar
   }
 }
 
-template <int TYPE, bool INTERLEAVED>
+template <int TYPE, bool INTERLEAVED, bool NORM>
 int launch(const RopeParams& p, cudaStream_t st) {
   const uint32_t side = kRopeThreads / (p.cache.head_dim / 8u), heads = p.n_q_heads + 2u * p.cache.n_kv_heads;
   // few tokens: a block for every set of heads; many: one block walks all heads of its token and keeps
   // the cosines and sines
   const uint32_t parts = p.n_tokens < 2u * (uint32_t)sm_count() ? (heads + side - 1u) / side : 1u;
   const dim3 grid(p.n_tokens, parts);
-  const char* what = "rope_append launch";
-  return p.cache.head_dim == 64 ? launch_pdl(rope_append_kernel<TYPE, INTERLEAVED, 64>, grid, kRopeThreads, 0, st, what, p)
-                                : launch_pdl(rope_append_kernel<TYPE, INTERLEAVED, 128>, grid, kRopeThreads, 0, st, what, p);
+  const char* what = NORM ? "qk_norm_rope_append launch" : "rope_append launch";
+  return p.cache.head_dim == 64 ? launch_pdl(rope_append_kernel<TYPE, INTERLEAVED, 64, NORM>, grid, kRopeThreads, 0, st, what, p)
+                                : launch_pdl(rope_append_kernel<TYPE, INTERLEAVED, 128, NORM>, grid, kRopeThreads, 0, st, what, p);
 }
 
-}  // namespace
-
-extern "C" int tq_rope_append(const void* d_q, const void* d_k, const void* d_v, int x_type, int64_t q_stride, int64_t k_stride,
-                              int64_t v_stride, uint32_t n_tokens, uint32_t n_q_heads, const float* d_table, uint32_t n_positions,
-                              uint32_t rot_dim, const int32_t* d_positions, const uint32_t* sections, uint32_t n_axes,
-                              int interleaved, const int32_t* d_slots, const tq_kv_cache* cache, void* d_q_out,
-                              void* cuda_stream) {
+template <bool NORM>
+int rope(const void* d_q, const void* d_k, const void* d_v, int x_type, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+         uint32_t n_tokens, uint32_t n_q_heads, const float* d_q_weight, const float* d_k_weight, float eps, const float* d_table,
+         uint32_t n_positions, uint32_t rot_dim, const int32_t* d_positions, const uint32_t* sections, uint32_t n_axes,
+         int interleaved, const int32_t* d_slots, const tq_kv_cache* cache, void* d_q_out, void* cuda_stream) {
   if (int rc = tq_check_cache(cache)) return rc;
   if (x_type != TQ_TYPE_BF16 && x_type != TQ_TYPE_F32) return TQ_ERR_INVALID_ARG;
   if (!sections || n_axes == 0 || n_axes > TQ_ROPE_MAX_AXES || rot_dim == 0 || rot_dim % 8u || rot_dim > cache->head_dim) return TQ_ERR_INVALID_ARG;
@@ -187,10 +216,12 @@ extern "C" int tq_rope_append(const void* d_q, const void* d_k, const void* d_v,
   }
   for (uint32_t a = n_axes; a < TQ_ROPE_MAX_AXES; ++a) p.axis_end[a] = p.axis_end[n_axes - 1];
   if (end != rot_dim / 2u) return TQ_ERR_INVALID_ARG;
+  if (NORM && !(eps >= 0.f)) return TQ_ERR_INVALID_ARG;
   if (n_tokens > 0x7FFFFFFFu || n_q_heads > 65536u) return TQ_ERR_UNSUPPORTED_SHAPE;
   if (n_tokens == 0) return TQ_OK;
   auto bad = [](const void* ptr, uintptr_t align) { return ptr == nullptr || ((uintptr_t)ptr & (align - 1u)) != 0; };
   if (bad(d_q, 16) || bad(d_k, 16) || bad(d_v, 16) || bad(d_table, 4) || bad(d_positions, 4) || bad(d_slots, 4) || bad(d_q_out, 16)) return TQ_ERR_INVALID_ARG;
+  if (NORM && (bad(d_q_weight, 4) || bad(d_k_weight, 4))) return TQ_ERR_INVALID_ARG;
   if (n_q_heads == 0 || n_positions == 0 || q_stride % 8 || k_stride % 8 || v_stride % 8) return TQ_ERR_INVALID_ARG;
   p.q = d_q;
   p.k = d_k;
@@ -208,7 +239,34 @@ extern "C" int tq_rope_append(const void* d_q, const void* d_k, const void* d_v,
   p.n_positions = n_positions;
   p.rot_dim = rot_dim;
   p.n_axes = n_axes;
+  p.q_weight = d_q_weight;
+  p.k_weight = d_k_weight;
+  p.eps = eps;
   cudaStream_t st = (cudaStream_t)cuda_stream;
-  if (x_type == TQ_TYPE_F32) return interleaved ? launch<TQ_TYPE_F32, true>(p, st) : launch<TQ_TYPE_F32, false>(p, st);
-  return interleaved ? launch<TQ_TYPE_BF16, true>(p, st) : launch<TQ_TYPE_BF16, false>(p, st);
+  if (x_type == TQ_TYPE_F32) return interleaved ? launch<TQ_TYPE_F32, true, NORM>(p, st) : launch<TQ_TYPE_F32, false, NORM>(p, st);
+  return interleaved ? launch<TQ_TYPE_BF16, true, NORM>(p, st) : launch<TQ_TYPE_BF16, false, NORM>(p, st);
 }
+
+}  // namespace
+
+extern "C" {
+
+int tq_rope_append(const void* d_q, const void* d_k, const void* d_v, int x_type, int64_t q_stride, int64_t k_stride,
+                   int64_t v_stride, uint32_t n_tokens, uint32_t n_q_heads, const float* d_table, uint32_t n_positions,
+                   uint32_t rot_dim, const int32_t* d_positions, const uint32_t* sections, uint32_t n_axes,
+                   int interleaved, const int32_t* d_slots, const tq_kv_cache* cache, void* d_q_out,
+                   void* cuda_stream) {
+  return rope<false>(d_q, d_k, d_v, x_type, q_stride, k_stride, v_stride, n_tokens, n_q_heads, nullptr, nullptr, 0.f, d_table,
+                     n_positions, rot_dim, d_positions, sections, n_axes, interleaved, d_slots, cache, d_q_out, cuda_stream);
+}
+
+int tq_qk_norm_rope_append(const void* d_q, const void* d_k, const void* d_v, int x_type, int64_t q_stride, int64_t k_stride,
+                           int64_t v_stride, uint32_t n_tokens, uint32_t n_q_heads, const float* d_q_weight,
+                           const float* d_k_weight, float eps, const float* d_table, uint32_t n_positions, uint32_t rot_dim,
+                           const int32_t* d_positions, const uint32_t* sections, uint32_t n_axes, int interleaved,
+                           const int32_t* d_slots, const tq_kv_cache* cache, void* d_q_out, void* cuda_stream) {
+  return rope<true>(d_q, d_k, d_v, x_type, q_stride, k_stride, v_stride, n_tokens, n_q_heads, d_q_weight, d_k_weight, eps, d_table,
+                    n_positions, rot_dim, d_positions, sections, n_axes, interleaved, d_slots, cache, d_q_out, cuda_stream);
+}
+
+}  // extern "C"
