@@ -901,8 +901,8 @@ def tq_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, table: tor
     if ctx is not None:
         with ctx:
             return tq_rope_append(q, k, v, table, positions, slots, cache, sections, interleaved, out)
-    T, H, x, where, slots, out, o = _rope_args(q, k, v, table, positions, slots, cache, sections, out, device)
-    _check(_lib.tq_rope_append(*x, T, H, *where, interleaved, slots, cache._ref, o, _raw_stream(device)), "tq_rope_append")
+    T, H, x, where, at, out, o = _rope_args(q, k, v, table, positions, slots, cache, sections, out, device)
+    _check(_lib.tq_rope_append(*x, T, H, *where, interleaved, at, cache._ref, o, _raw_stream(device)), "tq_rope_append")
     return out
 
 
@@ -1015,7 +1015,8 @@ def tq_cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, worksp
 
 # ------------------------------------------------------------------------------ a decode step with drafted tokens
 def _like(x: torch.Tensor, device: int, dtype, *shape) -> int:
-    """Address of a contiguous tensor of this type and shape on the call's device."""
+    """Address of a contiguous tensor of this type and shape on the call's device.  (The caller keeps the tensor in a name of its own: an
+    argument that nobody else holds would be freed, and its memory be the next result's.)"""
     assert x.get_device() == device and x.dtype == dtype and x.is_contiguous() and x.shape == shape, f"{dtype} {shape} on device {device} is wanted"
     return x.data_ptr()
 
@@ -1031,8 +1032,8 @@ def tq_qk_norm_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_
             return tq_qk_norm_rope_append(q, k, v, q_weight, k_weight, table, positions, slots, cache, eps, sections, interleaved, out)
     D = cache.head_dim
     weights = _like(q_weight, device, torch.float32, D), _like(k_weight, device, torch.float32, D)
-    T, H, x, where, slots, out, o = _rope_args(q, k, v, table, positions, slots, cache, sections, out, device)
-    _check(_lib.tq_qk_norm_rope_append(*x, T, H, *weights, eps, *where, interleaved, slots, cache._ref, o, _raw_stream(device)),
+    T, H, x, where, at, out, o = _rope_args(q, k, v, table, positions, slots, cache, sections, out, device)
+    _check(_lib.tq_qk_norm_rope_append(*x, T, H, *weights, eps, *where, interleaved, at, cache._ref, o, _raw_stream(device)),
            "tq_qk_norm_rope_append")
     return out
 
@@ -1053,12 +1054,12 @@ def tq_tree_attention(q: torch.Tensor, cache: KvCache, page_table: torch.Tensor,
     assert cache.device == device and workspace.device == device and q.dtype == torch.bfloat16
     assert D == cache.head_dim and stride[2] == 1 and (H == 1 or stride[1] == D)
     B, max_pages = page_table.shape
-    table, first, lens = _like(page_table, device, torch.int32, B, max_pages), _like(first, device, torch.int32, B + 1), _like(lens, device, torch.int32, B)
+    table, f, n = _like(page_table, device, torch.int32, B, max_pages), _like(first, device, torch.int32, B + 1), _like(lens, device, torch.int32, B)
     words = 0 if mask is None else mask.shape[1]
-    mask = None if mask is None else _like(mask, device, torch.int32, T, words)
-    out, lse = _attn_out(q, out, lse, device)
-    _check(_lib.tq_tree_attention(cache._ref, q.data_ptr(), stride[0] if T > 1 else 0, T, B, H, first, table, max_pages, lens, mask, words,
-                                  cache.scale if scale is None else scale, out.data_ptr(), lse, workspace.ptr, workspace.bytes,
+    m = None if mask is None else _like(mask, device, torch.int32, T, words)
+    out, e = _attn_out(q, out, lse, device)
+    _check(_lib.tq_tree_attention(cache._ref, q.data_ptr(), stride[0] if T > 1 else 0, T, B, H, f, table, max_pages, n, m, words,
+                                  cache.scale if scale is None else scale, out.data_ptr(), e, workspace.ptr, workspace.bytes,
                                   _raw_stream(device)), "tq_tree_attention")
     return out
 

@@ -15,7 +15,7 @@ LIB = PKG / "libtq.so"
 FAST_SOURCE = CSRC / "tq_fast.cpp"  # CPython module: the usual case of the calls between the linear layers
 SOURCES = [CSRC / "tq_device.cu", CSRC / "tq_gemm.cu", CSRC / "tq_gemm_ws.cu", CSRC / "tq_tiles.cu", CSRC / "tq_wide.cu", CSRC / "tq_encode.cu", CSRC / "tq_dict_device.cu",
            CSRC / "tq_norm.cu", CSRC / "tq_rope.cu", CSRC / "tq_attn.cu", CSRC / "tq_cross.cu", CSRC / "tq_tree.cu", CSRC / "tq_sample.cu", CSRC / "tq_accept.cu", CSRC / "tq_host.cpp"]
-HEADERS = [CSRC / "tq_internal.h", CSRC / "tq_sm100.cuh", CSRC / "tq_tiles_common.cuh", CSRC / "tq_ops_common.cuh", ROOT / "include" / "tq.h"]
+HEADERS = [CSRC / "tq_internal.h", CSRC / "tq_sm100.cuh", CSRC / "tq_tiles_common.cuh", CSRC / "tq_ops_common.cuh", CSRC / "tq_attn_sm100.cuh", ROOT / "include" / "tq.h"]
 
 
 def _nvcc() -> str | None:

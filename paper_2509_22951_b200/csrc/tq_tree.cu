@@ -1,17 +1,60 @@
-// Attention of several new tokens of each sequence over its paged cache (tq_tree_attention).
+// Attention of several new tokens of each sequence over its paged cache (tq_tree_attention): drafted tokens, or a piece of a prompt.
 //
 //   out = sum_s p_s v_s / sum_s p_s,   p_s = exp(scale q.k_s - m),   m a running maximum
+//
+// The G query heads that share a key-value head and the sequence's new tokens are R = G n rows over the same states: 4 R D operations
+// and 4 D bytes a state and key-value head.  For R up to about 200 the bytes bound it, above that the tensor cores and the exponentials; so
+// everything is built to keep the loads going while tiles of 128 rows x 128 states go through the 5th-generation tensor cores.
+//
+// Work.  The units are (sequence, key-value head, tile of 128 rows, tile of 128 states); of a chain, only the tiles that a tile's last row sees.  Each
+// CTA takes an equal share of consecutive units, whatever the lengths are (they are known on the device only).  A group (sequence, key-value
+// head, tile of rows) that lies in several shares leaves its parts in the workspace, and a second kernel joins them in the order of the
+// CTAs: the result does not depend on timing.
+//
+// CTA, one to an SM, 16 warps:
+//   8-11   copy K and V, row by row with cp.async (pages may have any size and a slot any place), into a ring of tiles in the layout that the
+//          tensor core reads (128-byte swizzle); each has its 32 states of a tile and says which of them are there.
+//   13-15  copy the queries of the next group (two buffers).
+//   12     issues the products: scores of tile t (128 x 128, into one of two buffers of tensor memory), then, while their softmax is
+//          taken, the product of tile t - 1 with V.
+//   0-3, 4-7  softmax, a thread a row: the first four take the states 0-63 of a tile, the others 64-127, each with a running maximum and sum
+//          and an output in tensor memory of its own, so that neither waits for the other but at a group's end, where the two become one.
+//          p goes back to tensor memory as bf16 over its scores, where it is the A operand of the product with V.
+// The output is rescaled only when a row's maximum has grown by more than 2^8 since the last rescaling (online softmax with the rescaling
+// delayed up to a threshold, as in the kernel of cross attention): p stays below 2^8, which costs no precision in bf16 or the fp32 sum.
+//
+// States that are not there (past the end, on a page outside the pool) are zeros in shared memory and hidden from all rows.  A state that only
+// some rows see enters the others' sums with p = 0; if its value is Inf or NaN that product is NaN, so a row whose sum of p is finite but whose
+// output has a NaN is computed again from the states it sees (slow).
+//
+// Every wait is bounded; one that runs out raises TQ_STATUS_WAIT_EXPIRED, all roles leave their loops and tensor memory is released on
+// every path.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
 #include <cstdint>
 
+#include "tq_attn_sm100.cuh"
 #include "tq_internal.h"
 #include "tq_ops_common.cuh"
 
 namespace {
 
 using namespace tq_ops;
+using namespace tq_sm100;
+using namespace tq_attn;
+
+constexpr uint32_t kRows = 128;    // rows of a tile: the lanes of tensor memory
+constexpr uint32_t kStates = 128;  // states of a tile
+constexpr uint32_t kSide = 64;     // states of a tile that one half of the softmax warps takes
+constexpr int kSoftWarps = 8, kLoadWarp = 8, kLoadWarps = 4, kMmaWarp = 12, kQueryWarp = 13, kQueryWarps = 3;
+constexpr int kTreeThreads = 512;
+// registers a thread: 128 at launch (16 warps of an SM's 65536); the softmax warps hold a row of 64 scores and two of output.  The launch
+// checks the kernel's own count: a split above it would wait for ever.
+constexpr int kSoftRegs = 192, kOtherRegs = 64;
+constexpr uint32_t kTmemCols = 512;
+constexpr uint32_t kThere = 8;     // tiles whose words of present states are kept: loads run at most six tiles ahead of the softmax
+constexpr float kRescale = 8.0f;   // log2 of how far p may exceed 1
 
 struct TreeParams {
   const __nv_bfloat16* k;
@@ -26,69 +69,694 @@ struct TreeParams {
   const int32_t* page_table;
   const uint32_t* mask;
   uint32_t mask_words, max_pages, page_size, n_pages;
-  uint32_t n_tokens, n_seqs, n_q_heads, group;
+  uint32_t n_tokens, n_seqs, n_q_heads, n_kv_heads, group;
   float scale_log2;
   uint32_t* status;
+  tq_attn_ws ws;
 };
 
-// A warp for a token and a query head.
 template <int D>
-__global__ void __launch_bounds__(128) tree_attention_kernel(const TreeParams p) {
+struct TreeSmem {
+  static constexpr uint32_t kSlabs = D / 64;                       // 64 columns = 128 bytes of a swizzled row
+  static constexpr uint32_t kTileBytes = kSlabs * kStates * 128;   // queries, keys or values of a tile
+  static constexpr uint32_t kStages = D == 128 ? 5 : 10;           // K, V, K, V, ...
+  static constexpr uint32_t kAhead = kStages - 2;                  // copies of a loading warp that may be under way behind the one it announces
+  static constexpr uint32_t kOffKv = 2 * kTileBytes;
+  static constexpr uint32_t kOffMisc = kOffKv + kStages * kTileBytes;
+  // misc: [0] dead flag, [4] tensor-memory base, barriers from 16 on
+  static constexpr uint32_t kBarKvFull = 16, kBarKvEmpty = kBarKvFull + 8 * kStages;
+  static constexpr uint32_t kBarQFull = kBarKvEmpty + 8 * kStages, kBarQEmpty = kBarQFull + 16;
+  static constexpr uint32_t kBarSFull = kBarQEmpty + 16, kBarPFull = kBarSFull + 16, kBarODone = kBarPFull + 16, kBarMl = kBarODone + 16;
+  static constexpr uint32_t kOffPlan = (kBarMl + 8 + 15) / 16 * 16;
+  static constexpr uint32_t kOffThere = kOffPlan + 48;
+  static constexpr uint32_t kOffMl = kOffThere + kThere * 16;
+  static constexpr uint32_t kTotal = kOffMisc + kOffMl + 2 * kRows * 8;
+  static_assert(kTotal <= 232448, "shared memory of one CTA");
+};
+// a part of a cut group: [D / 4][128] float4 of output, then the rows' maxima and sums
+constexpr uint64_t kTreePartFloats = kRows * (128 + 2);
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+
+// A group of the list of work: tile rt of the rows of sequence b over key-value head kvh.
+struct Walk {
+  uint32_t b, kvh, rt, row_tiles;
+  int32_t lo;       // first row of the sequence
+  uint32_t n, len;  // its new tokens and states
+  int64_t before;   // states before its new tokens (negative: the first ones have none)
+  uint32_t end;     // states that the tile's rows may look at
+  uint32_t tiles, unit;  // of states; first unit
+
+  __device__ __forceinline__ void enter(const TreeParams& p) {
+    const int32_t most = (int32_t)p.n_tokens;
+    lo = max(0, min(__ldg(p.first + b), most));
+    n = (uint32_t)(max(lo, min(__ldg(p.first + b + 1), most)) - lo);
+    const int32_t given = __ldg(p.lens + b);
+    const uint64_t cap = min((uint64_t)p.max_pages * p.page_size, (uint64_t)0x7FFFFFFF);
+    len = given <= 0 ? 0u : (uint32_t)min((uint64_t)given, cap);
+    before = (int64_t)given - n;
+    row_tiles = (uint32_t)(((uint64_t)n * p.group + kRows - 1u) / kRows);
+  }
+  __device__ __forceinline__ void tile(const TreeParams& p) {
+    end = len;
+    if (p.mask == nullptr) {
+      const uint32_t last = (uint32_t)min((uint64_t)n - 1u, (((uint64_t)rt + 1u) * kRows - 1u) / p.group);
+      end = (uint32_t)max((int64_t)0, min((int64_t)len, before + last + 1));
+    }
+    tiles = max(1u, (end + kStates - 1u) / kStates);
+  }
+  // the next sequence with rows, from b on
+  __device__ __forceinline__ void settle(const TreeParams& p) {
+    for (; b < p.n_seqs; ++b) {
+      enter(p);
+      if (n != 0u) {
+        tile(p);
+        return;
+      }
+    }
+  }
+  __device__ __forceinline__ void next(const TreeParams& p) {
+    unit += tiles;
+    if (++rt == row_tiles) {
+      rt = 0;
+      if (++kvh == p.n_kv_heads) {
+        kvh = 0;
+        ++b;
+        settle(p);
+        return;
+      }
+    }
+    if (p.mask == nullptr) tile(p);
+  }
+};
+
+// This CTA's share of the units, found by one warp.
+struct Plan {
+  uint32_t u0, u1, cut;             // units; whether groups are cut (else the groups that begin in the share are the share)
+  uint32_t mean, over;              // CTA i has the units i * mean + min(i, over) and on
+  uint32_t b, kvh, rt, unit;        // first group
+  __device__ __forceinline__ uint32_t cta_of(uint32_t u) const { return u < over * (mean + 1u) ? u / (mean + 1u) : over + (u - over * (mean + 1u)) / mean; }
+};
+static_assert(sizeof(Plan) <= 48, "room for the plan");
+
+// Groups are left whole where the longest share is then no more than kWholeTiles tiles above the mean of the shares.
+constexpr uint32_t kWholeTiles = 3;
+
+__device__ __forceinline__ Plan make_plan(const TreeParams& p, uint32_t lane) {
+  Plan r{};
+  Walk w{};
+  const uint32_t per = (p.n_seqs + 31u) / 32u, begin = min(lane * per, p.n_seqs), end = min(begin + per, p.n_seqs);
+  uint32_t sum = 0, most = 0, least = 0xFFFFFFFFu, groups = 0;  // units and groups of one key-value head
+  auto units = [&](uint32_t b) {
+    w.b = b;
+    w.enter(p);
+    uint32_t u = 0;
+    for (w.rt = 0; w.rt < w.row_tiles; ++w.rt) {
+      w.tile(p);
+      u += w.tiles;
+      most = max(most, w.tiles);
+      least = min(least, w.tiles);
+    }
+    return u;
+  };
+  for (uint32_t b = begin; b < end; ++b) {
+    sum += units(b);
+    groups += w.row_tiles;
+  }
+  uint32_t incl = sum;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const uint32_t o = __shfl_up_sync(kFull, incl, d);
+    if (lane >= (uint32_t)d) incl += o;
+  }
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) {
+    most = max(most, __shfl_xor_sync(kFull, most, d));
+    least = min(least, __shfl_xor_sync(kFull, least, d));
+    groups += __shfl_xor_sync(kFull, groups, d);
+  }
+  const uint32_t total = __shfl_sync(kFull, incl, 31) * p.n_kv_heads;
+  r.b = p.n_seqs;
+  if (total == 0u) return r;
+  const uint32_t ctas = min(gridDim.x, total);
+  r.mean = total / ctas;
+  r.over = total - r.mean * ctas;
+  // the longest share without cuts: whole groups of one size, or up to one group over the mean
+  const uint32_t longest = most == least ? ((groups * p.n_kv_heads - 1u) / ctas + 1u) * most : r.mean + most;
+  r.cut = longest > r.mean + (r.over != 0u ? 1u : 0u) + kWholeTiles;
+  if (blockIdx.x >= ctas) return r;
+  r.u0 = r.mean * blockIdx.x + min(blockIdx.x, r.over);
+  r.u1 = r.u0 + r.mean + (blockIdx.x < r.over ? 1u : 0u);
+  const uint32_t owner = __ffs(__ballot_sync(kFull, r.u0 < incl * p.n_kv_heads)) - 1u;
+  uint32_t at = (incl - sum) * p.n_kv_heads, b = begin, u = 0;
+  if (lane == owner) {
+    for (; b < end; ++b) {
+      u = units(b);
+      if (r.u0 < at + u * p.n_kv_heads) break;
+      at += u * p.n_kv_heads;
+    }
+  }
+  w.b = __shfl_sync(kFull, b, owner);
+  at = __shfl_sync(kFull, at, owner);
+  u = __shfl_sync(kFull, u, owner);
+  if (u == 0u || w.b >= p.n_seqs) return r;  // only rows that overlap (first not rising) get here
+  w.kvh = (r.u0 - at) / u;
+  w.unit = at + w.kvh * u;
+  w.rt = 0;
+  w.enter(p);
+  w.tile(p);
+  while (w.b < p.n_seqs && (r.u0 >= w.unit + w.tiles || (!r.cut && w.unit < r.u0))) w.next(p);
+  r.b = w.b;
+  r.kvh = w.kvh;
+  r.rt = w.rt;
+  r.unit = w.unit;
+  return r;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kTreeThreads, 1) tree_attention_kernel(const TreeParams p) {
+  using L = TreeSmem<D>;
+  extern __shared__ __align__(1024) uint8_t smem[];  // swizzled tiles start on 1024 bytes
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const uint32_t smem0 = smem_u32(smem), misc = smem0 + L::kOffMisc;
+  volatile uint32_t* const dead = reinterpret_cast<uint32_t*>(smem + L::kOffMisc);
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(smem + L::kOffMisc + 4);
+  Plan* const s_plan = reinterpret_cast<Plan*>(smem + L::kOffMisc + L::kOffPlan);
+  float2* const s_ml = reinterpret_cast<float2*>(smem + L::kOffMisc + L::kOffMl);
+  uint32_t* const s_there = reinterpret_cast<uint32_t*>(smem + L::kOffMisc + L::kOffThere);
+  // the same in all lanes, and known to be: what depends on it alone stays on the uniform data path
+  const uint32_t warp = __shfl_sync(kFull, threadIdx.x >> 5, 0), lane = threadIdx.x & 31u;
+  auto bar = [&](uint32_t off, uint32_t i) { return misc + off + 8u * i; };
+
+  if (smem0 & 1023u) {  // nothing is placed before it, so this does not happen
+    if (threadIdx.x == 0) atomicOr(p.ws.status, TQ_STATUS_WAIT_EXPIRED);
+    return;
+  }
+  if (threadIdx.x == 0) {
+    *dead = 0u;
+    for (uint32_t i = 0; i < L::kStages; ++i) {
+      mbar_init(bar(L::kBarKvFull, i), kLoadWarps);
+      mbar_init(bar(L::kBarKvEmpty, i), 1);
+    }
+    for (uint32_t i = 0; i < 2; ++i) {
+      mbar_init(bar(L::kBarQFull, i), kQueryWarps);
+      mbar_init(bar(L::kBarQEmpty, i), 1);
+      mbar_init(bar(L::kBarSFull, i), 2);  // the products' completion, and the issuing thread, which has seen the words of present states
+      mbar_init(bar(L::kBarPFull, i), kSoftWarps);
+      mbar_init(bar(L::kBarODone, i), 1);
+    }
+    mbar_init(bar(L::kBarMl, 0), kSoftWarps);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(kTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (warp == kQueryWarp) {
+    const Plan mine = make_plan(p, lane);
+    if (lane == 0) *s_plan = mine;
+  }
+  tmem_fence_before();
+  __syncthreads();
+  tmem_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const Plan& plan = *s_plan;
+
+  bool ok = true;
+  auto wait = [&](uint32_t b, uint32_t parity) {
+    ok = ok && mbar_wait(b, parity, dead);
+    ok = __all_sync(kFull, ok);
+  };
+  Walk g{};
+  g.b = plan.b;
+  g.kvh = plan.kvh;
+  g.rt = plan.rt;
+  g.unit = plan.unit;
+  if (g.b < p.n_seqs) {
+    g.enter(p);
+    g.tile(p);
+  }
+  // the tiles of states of group w that are this CTA's
+  auto more = [&](const Walk& w) { return w.b < p.n_seqs && w.unit < plan.u1; };
+  auto begin_of = [&](const Walk& w) { return plan.cut && plan.u0 > w.unit ? plan.u0 - w.unit : 0u; };
+  auto end_of = [&](const Walk& w) { return plan.cut && plan.u1 - w.unit < w.tiles ? plan.u1 - w.unit : w.tiles; };
+
+  if (warp >= kSoftWarps) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+  if (warp < kLoadWarp + kLoadWarps) {
+    // ---- K and V ----------------------------------------------------------------------------------------
+    const uint32_t mine = warp - kLoadWarp;
+    // the page of this lane's state of the next tile, asked for one tile ahead of its copies
+    bool f_any = more(g), f_live = false;
+    uint32_t f_slot = 0, f_kvh = 0, t = f_any ? begin_of(g) : 0u, t1 = f_any ? end_of(g) : 0u;
+    int32_t f_page = 0;
+    bool bad = false;
+    auto fetch = [&]() {
+      f_any = more(g);
+      if (!f_any) return;
+      const uint32_t s = t * kStates + mine * 32u + lane;
+      const uint32_t pg = s / p.page_size;
+      f_live = s < g.end;
+      f_slot = s - pg * p.page_size;
+      f_kvh = g.kvh;
+      if (f_live) f_page = __ldg(p.page_table + (size_t)g.b * p.max_pages + pg);
+      if (t == 0u && lane == 0u && __ldg(p.lens + g.b) > 0 && (uint32_t)__ldg(p.lens + g.b) > g.len) bad = true;
+      if (++t == t1) {
+        g.next(p);
+        if (more(g)) {
+          t = begin_of(g);
+          t1 = end_of(g);
+        }
+      }
+    };
+    uint32_t st = 0, round = 0, under_way = 0, told = 0, count = 0;  // stage to fill, stage to announce
+    auto announce = [&]() {
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(L::kBarKvFull, told));
+      if (++told == L::kStages) told = 0;
+      --under_way;
+    };
+    constexpr uint32_t kChunks = D / 8, kAtOnce = 32 / kChunks;  // 16 bytes of a row; rows of a warp-wide copy
+    const uint32_t c = lane % kChunks;
+    auto copy = [&](const __nv_bfloat16* src, int64_t off, uint32_t there) {
+      if (round) wait(bar(L::kBarKvEmpty, st), (round - 1u) & 1u);
+      if (!ok) return;
+      const uint32_t dst = smem0 + L::kOffKv + st * L::kTileBytes + (c / 8u) * (kStates * 128u) + mine * 32u * 128u;
+#pragma unroll
+      for (uint32_t r0 = 0; r0 < 32u; r0 += kAtOnce) {
+        const uint32_t r = r0 + lane / kChunks;
+        const int64_t o = __shfl_sync(kFull, off, r) + c * 8u;
+        cp_async16(dst + r * 128u + (((c % 8u) ^ (r & 7u)) << 4), src + o, (there >> r) & 1u ? 16u : 0u);  // 0: zeros, nothing is read
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      if (++st == L::kStages) {
+        st = 0;
+        ++round;
+      }
+      if (++under_way > L::kAhead) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(L::kAhead) : "memory");
+        announce();
+      }
+    };
+    fetch();
+    while (f_any && ok) {
+      bool live = f_live;
+      if (live && (uint32_t)f_page >= p.n_pages) {
+        live = false;
+        bad = true;
+      }
+      const int64_t off = live ? (int64_t)f_page * p.page_stride + (int64_t)f_kvh * p.head_stride + (int64_t)f_slot * p.slot_stride : 0;
+      fetch();
+      const uint32_t there = __ballot_sync(kFull, live);
+      if (lane == 0) s_there[(count % kThere) * 4u + mine] = there;
+      ++count;
+      copy(p.k, off, there);
+      if (ok) copy(p.v, off, there);
+    }
+    if (ok) {
+      while (under_way) {  // the last ones, one by one
+        if (under_way > 4u)
+          asm volatile("cp.async.wait_group 4;" ::: "memory");
+        else if (under_way > 2u)
+          asm volatile("cp.async.wait_group 2;" ::: "memory");
+        else if (under_way > 1u)
+          asm volatile("cp.async.wait_group 1;" ::: "memory");
+        else
+          asm volatile("cp.async.wait_group 0;" ::: "memory");
+        announce();
+      }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    if (bad && p.status != nullptr) atomicOr(p.status, TQ_STATUS_BAD_PAGE);
+  } else if (warp >= kQueryWarp) {
+    // ---- queries ----------------------------------------------------------------------------------------
+    constexpr uint32_t kChunks = D / 8, kAtOnce = 32 / kChunks;
+    const uint32_t c = lane % kChunks;
+    uint32_t count = 0;
+    uint4 open = make_uint4(0u, 0u, 0u, 0u);  // the last group that begins in this share, the only one that can go on in the next
+    for (; more(g) && ok; g.next(p)) {
+      const uint32_t qb = count & 1u;
+      if (count >= 2u) wait(bar(L::kBarQEmpty, qb), (count / 2u - 1u) & 1u);
+      if (!ok) break;
+      const uint32_t rows = (uint32_t)min((uint64_t)kRows, (uint64_t)g.n * p.group - (uint64_t)g.rt * kRows);
+      const uint32_t dst = smem0 + qb * L::kTileBytes + (c / 8u) * (kRows * 128u);
+      const __nv_bfloat16* const q = p.q + (int64_t)g.lo * p.q_stride + (size_t)g.kvh * p.group * D + c * 8u;
+      for (uint32_t r = (warp - kQueryWarp) * kAtOnce + lane / kChunks; r < rows; r += kQueryWarps * kAtOnce) {
+        const uint32_t row = g.rt * kRows + r, tok = row / p.group;
+        cp_async16(dst + r * 128u + (((c % 8u) ^ (r & 7u)) << 4), q + (int64_t)tok * p.q_stride + (row - tok * p.group) * D, 16u);
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(L::kBarQFull, qb));
+      ++count;
+      open = make_uint4(0u, g.b, g.kvh, g.rt);
+      if (plan.cut && g.unit >= plan.u0 && plan.u1 - g.unit < g.tiles) open.x = plan.cta_of(g.unit + g.tiles - 1u) - blockIdx.x + 1u;
+    }
+    if (warp == kQueryWarp && lane == 0) p.ws.open[blockIdx.x] = open;  // for the joining kernel
+  } else if (warp == kMmaWarp) {
+    // ---- products ---------------------------------------------------------------------------------------
+    uint32_t st = 0, round = 0, count = 0, q_count = 0;  // count: tiles
+    bool have = false;                                   // a tile whose product with V is to come
+    uint32_t v_st = 0, v_round = 0, accumulate = 0;
+    const uint32_t idesc_qk = umma_idesc(128, 128), idesc_pv = umma_idesc(128, D) | kIdescNMajorB;
+    const uint64_t q_desc = umma_desc(smem0), kv_desc = umma_desc(smem0 + L::kOffKv), v_desc = umma_desc_n_major(smem0 + L::kOffKv, kStates);
+    auto bump = [&]() {
+      if (++st == L::kStages) {
+        st = 0;
+        ++round;
+      }
+    };
+    // the pending tile's p times V, both halves of its states
+    auto pv = [&]() {
+      const uint32_t sb = (count - 1u) & 1u;
+      wait(bar(L::kBarKvFull, v_st), v_round & 1u);
+      if (ok) wait(bar(L::kBarPFull, sb), ((count - 1u) >> 1) & 1u);
+      if (!ok) return;
+      tmem_fence_after();
+      if (elect_one()) {
+        const uint64_t b = v_desc + v_st * (L::kTileBytes >> 4);
+#pragma unroll
+        for (uint32_t kk = 0; kk < kStates / 16u; ++kk) {
+          const uint32_t w = kk / 4u;
+          umma_bf16_ts(tmem + 2u * kStates + w * D, tmem + sb * kStates + w * kSide + (kk % 4u) * 8u, b + kk * (2048u >> 4), idesc_pv,
+                       accumulate | (kk % 4u));
+        }
+        umma_commit(bar(L::kBarODone, sb));
+        umma_commit(bar(L::kBarKvEmpty, v_st));
+      }
+      __syncwarp();
+      have = false;
+    };
+    for (; more(g) && ok; g.next(p), ++q_count) {
+      const uint32_t t0 = begin_of(g), t1 = end_of(g), qb = q_count & 1u;
+      for (uint32_t t = t0; t < t1 && ok; ++t) {
+        if (t == t0) {
+          if (have) pv();
+          if (ok) wait(bar(L::kBarQFull, qb), (q_count >> 1) & 1u);
+        }
+        if (ok) wait(bar(L::kBarKvFull, st), round & 1u);
+        if (!ok) break;
+        tmem_fence_after();
+        if (elect_one()) {
+          const uint64_t a = q_desc + qb * (L::kTileBytes >> 4), b = kv_desc + st * (L::kTileBytes >> 4);
+#pragma unroll
+          for (uint32_t kk = 0; kk < D / 16; ++kk) {
+            constexpr uint32_t kSlab = (kStates * 128u) >> 4;
+            const uint32_t off = (kk / 4u) * kSlab + (kk % 4u) * 2u;  // in 16 bytes
+            umma_bf16(tmem + (count & 1u) * kStates, a + off, b + off, idesc_qk, kk != 0u);
+          }
+          umma_commit(bar(L::kBarSFull, count & 1u));
+          umma_commit(bar(L::kBarKvEmpty, st));
+          if (t + 1u == t1) umma_commit(bar(L::kBarQEmpty, qb));
+          mbar_arrive(bar(L::kBarSFull, count & 1u));
+        }
+        __syncwarp();
+        bump();
+        if (have) pv();
+        have = true;
+        accumulate = t != t0 ? 1u : 0u;
+        v_st = st;
+        v_round = round;
+        bump();
+        ++count;
+      }
+    }
+    if (have && ok) pv();
+  }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
+    // ---- softmax: a thread a row, half the states ---------------------------------------------------------
+    const uint32_t w = warp >> 2, row_in = threadIdx.x & 127u;
+    const uint32_t lane_field = (warp & 3u) << 21;  // 32 lanes of tensor memory to a warp
+    const uint32_t o_addr = tmem + lane_field + 2u * kStates;
+    const float c = p.scale_log2;
+    uint32_t count = 0, groups = 0;
+    for (; more(g) && ok; g.next(p), ++groups) {
+      const uint32_t t0 = begin_of(g), t1 = end_of(g);
+      const uint64_t rows = (uint64_t)g.n * p.group;
+      const uint64_t row = (uint64_t)g.rt * kRows + row_in;
+      const bool live = row < rows, warp_live = row - lane < rows;
+      const uint32_t tok = live ? (uint32_t)row / p.group : 0u, head = g.kvh * p.group + ((uint32_t)row - tok * p.group);
+      const uint32_t* const bits_row = p.mask ? p.mask + (size_t)(g.lo + (int32_t)tok) * p.mask_words : nullptr;
+      float m = -INFINITY, l = 0.f;
+      // bit i: this row sees state s0 + i, as far as the order of the new tokens goes
+      auto visible = [&](int64_t s0) -> uint64_t {
+        const int64_t j0 = s0 - g.before;  // new token of the first of the 64 states
+        if (j0 <= -(int64_t)kSide) return ~0ull;
+        if (bits_row == nullptr) {
+          const int64_t n = (int64_t)tok + 1 - j0;
+          return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull;
+        }
+        const int64_t from = max((int64_t)0, j0);
+        const uint32_t word = (uint32_t)(from >> 5), off = (uint32_t)from & 31u;
+        auto at = [&](uint32_t i) { return (int64_t)(from >> 5) + i < p.mask_words ? __ldg(bits_row + word + i) : 0u; };
+        const uint32_t a = at(0), b = at(1), e = at(2);
+        const uint64_t v = ((uint64_t)__funnelshift_r(b, e, off) << 32) | __funnelshift_r(a, b, off);
+        return j0 >= 0 ? v : (v << -j0) | ((1ull << -j0) - 1ull);
+      };
+      for (uint32_t t = t0; t < t1; ++t, ++count) {
+        const uint32_t sb = count & 1u, s_addr = tmem + lane_field + sb * kStates + w * kSide;
+        const uint64_t order = warp_live ? visible((int64_t)t * kStates + w * kSide) : 0ull;
+        wait(bar(L::kBarSFull, sb), (count >> 1) & 1u);
+        if (!ok) break;
+        tmem_fence_after();
+        if (warp_live) {
+          const uint2 here = *reinterpret_cast<const uint2*>(s_there + (count % kThere) * 4u + w * 2u);
+          const uint64_t seen = order & (((uint64_t)here.y << 32) | here.x);
+          uint32_t s[kSide];
+          TMEM_LD32(s, s_addr);
+          TMEM_LD32(s + 32, s_addr + 32u);
+          tmem_wait_ld();
+          if (__any_sync(kFull, seen != ~0ull)) {
+            const uint32_t lo = (uint32_t)seen, hi = (uint32_t)(seen >> 32);
+#pragma unroll
+            for (int i = 0; i < 64; ++i) s[i] = ((i < 32 ? lo : hi) >> (i % 32)) & 1u ? s[i] : 0xFF800000u;
+          }
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int i = 0; i < 64; i += 8) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], __uint_as_float(s[i + 2 * k]), __uint_as_float(s[i + 2 * k + 1]));
+          }
+          const float top = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]) * c;
+          if (__any_sync(kFull, top > m + kRescale)) {
+            const float mn = fmaxf(m, top), f = mn == -INFINITY ? 1.f : exp2_fast(m - mn);
+            m = mn;
+            l *= f;
+            if (t != t0) {
+              wait(bar(L::kBarODone, sb ^ 1u), ((count - 1u) >> 1) & 1u);  // the products with V up to the tile before
+              if (!ok) break;
+              tmem_fence_after();
+#pragma unroll
+              for (int i = 0; i < D / 16; ++i) {
+                uint32_t o[16];
+                TMEM_LD16(o, o_addr + w * D + 16u * i);
+                tmem_wait_ld();
+#pragma unroll
+                for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                TMEM_ST16(o_addr + w * D + 16u * i, o);
+              }
+            }
+          }
+          const float ref = m == -INFINITY ? 0.f : m;
+          const uint64_t c2 = pair(c, c), ref2 = pair(-ref, -ref);
+          uint64_t sum[2] = {0, 0};
+          uint32_t pk[32];
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            float a, b;
+            unpair(fma2(pair(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), c2, ref2), a, b);
+            a = exp2_fast(a);
+            b = exp2_fast(b);
+            sum[i & 1] = add2(sum[i & 1], pair(a, b));
+            pk[i] = pack_bf16(a, b);
+          }
+          TMEM_ST32(s_addr, pk);
+          float l0, l1;
+          unpair(add2(sum[0], sum[1]), l0, l1);
+          l += l0 + l1;
+          tmem_wait_st();
+        }
+        tmem_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(L::kBarPFull, sb));
+      }
+      if (!ok) break;
+      // ---- end of the group, or of this CTA's part of it: the two halves of the states become one ---------------
+      s_ml[w * kRows + row_in] = make_float2(m, l);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(L::kBarMl, 0));
+      wait(bar(L::kBarODone, (count - 1u) & 1u), ((count - 1u) >> 1) & 1u);
+      if (ok) wait(bar(L::kBarMl, 0), groups & 1u);
+      if (!ok) break;
+      if (!warp_live) continue;
+      tmem_fence_after();
+      const float2 a = s_ml[row_in], b = s_ml[kRows + row_in];
+      const float M = fmaxf(a.x, b.x), ref = M == -INFINITY ? 0.f : M;
+      const float fa = exp2_fast(a.x - ref), fb = exp2_fast(b.x - ref), sum = a.y * fa + b.y * fb;
+      const bool whole = t0 == 0u && t1 == g.tiles;
+      float* const mine = p.ws.parts + (size_t)(2u * blockIdx.x + (t0 == 0u ? 1u : 0u)) * kTreePartFloats;
+      const size_t at = (size_t)(g.lo + (int32_t)tok) * p.n_q_heads + head;
+      const float inv = 1.0f / sum;
+      bool nan = false;
+      constexpr uint32_t kColumns = D / 2;  // of a row, for each of its two threads
+#pragma unroll 1
+      for (uint32_t i = 0; i < kColumns; i += 16u) {
+        const uint32_t col = w * kColumns + i;
+        uint32_t x[16], y[16];
+        TMEM_LD16(x, o_addr + col);
+        TMEM_LD16(y, o_addr + D + col);
+        tmem_wait_ld();
+        float o[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          o[k] = __uint_as_float(x[k]) * fa + __uint_as_float(y[k]) * fb;
+          nan = nan || o[k] != o[k];
+        }
+        if (!live) continue;
+        if (whole) {
+#pragma unroll
+          for (int k = 0; k < 16; k += 8) {
+            float f[8];
+#pragma unroll
+            for (int z = 0; z < 8; ++z) f[z] = sum == 0.f ? 0.f : o[k + z] * inv;
+            store8<TQ_TYPE_BF16>(p.out, at * D + col + k, f);
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            reinterpret_cast<float4*>(mine)[(col / 4u + k) * kRows + row_in] = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+        }
+      }
+      if (live && w == 0u) {
+        if (!whole) {
+          mine[kRows * 128 + row_in] = M;
+          mine[kRows * 129 + row_in] = sum;
+        } else if (p.lse) {
+          p.lse[at] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * 0.6931471805599453f;
+        }
+      }
+      // rows that a state they do not see has spoiled: again, a warp a row
+      uint32_t again = __ballot_sync(kFull, live && nan && sum < INFINITY);
+#pragma unroll 1
+      while (again) {
+        const int src = __ffs(again) - 1;
+        again &= again - 1u;
+        constexpr int kPer = D / 32, kOwn = D / 64;  // elements of a row a lane, and of this warp's half of it
+        const uint32_t rt = __shfl_sync(kFull, tok, src), rh = __shfl_sync(kFull, head, src), rs = __shfl_sync(kFull, row_in, src);
+        const float rm = __shfl_sync(kFull, ref, src), rl = __shfl_sync(kFull, sum, src);
+        const __nv_bfloat16* q = p.q + (int64_t)(g.lo + (int32_t)rt) * p.q_stride + (size_t)rh * D + lane * kPer;
+        float acc[kOwn], qv[kPer];
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) acc[i] = 0.f;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) qv[i] = __bfloat162float(q[i]);
+        const uint32_t s1 = min(t1 * kStates, g.end);
+#pragma unroll 1
+        for (uint32_t s = t0 * kStates; s < s1; ++s) {
+          const int64_t j = (int64_t)s - g.before;
+          if (j >= 0 && (p.mask ? (j >> 5) >= (int64_t)p.mask_words ||
+                                      !((__ldg(p.mask + (size_t)(g.lo + (int32_t)rt) * p.mask_words + (j >> 5)) >> (j & 31)) & 1u)
+                                : j > (int64_t)rt))
+            continue;
+          const uint32_t pg = s / p.page_size;
+          const int32_t page = __ldg(p.page_table + (size_t)g.b * p.max_pages + pg);
+          if ((uint32_t)page >= p.n_pages) continue;
+          const int64_t from = (int64_t)page * p.page_stride + (int64_t)g.kvh * p.head_stride + (int64_t)(s - pg * p.page_size) * p.slot_stride;
+          float x = 0.f;
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) x += qv[i] * __bfloat162float(p.k[from + lane * kPer + i]);
+#pragma unroll
+          for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(kFull, x, d);
+          const float pr = exp2_fast(fmaf(x, c, -rm));
+#pragma unroll
+          for (int i = 0; i < kOwn; ++i) acc[i] += pr * __bfloat162float(p.v[from + w * kColumns + lane * kOwn + i]);
+        }
+        __syncwarp();  // after the row's own thread has written it
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+          const uint32_t col = w * kColumns + lane * kOwn + i;
+          if (whole)
+            p.out[((size_t)(g.lo + (int32_t)rt) * p.n_q_heads + rh) * D + col] = __float2bfloat16_rn(rl == 0.f ? 0.f : acc[i] / rl);
+          else
+            mine[(col / 4u * kRows + rs) * 4u + col % 4u] = acc[i];
+        }
+      }
+    }
+  }
+
+  if (!ok) {
+    *dead = 1u;
+    if (lane == 0) atomicOr(p.ws.status, TQ_STATUS_WAIT_EXPIRED);
+    for (int i = 0; i < 2000; ++i) __nanosleep(1000);  // products in flight still read shared memory: give them time to end
+  }
+  tmem_fence_before();
+  __syncthreads();
+  if (warp == kMmaWarp) {
+    tmem_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+  }
+}
+
+// Joins the parts of the groups that were cut.  grid (CTAs of the kernel above, slices of 8 rows): the group that begins in CTA x's share and goes
+// on, if there is one; a thread has four columns of a row and adds the parts up in their order.
+constexpr uint32_t kJoinRows = 8;
+template <int D>
+__global__ void __launch_bounds__(kJoinRows * D / 4) tree_join_kernel(const TreeParams p) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const uint64_t job = (uint64_t)blockIdx.x * 4u + threadIdx.x / 32u;
-  const uint32_t lane = threadIdx.x % 32u;
-  if (job >= (uint64_t)p.n_tokens * p.n_q_heads) return;
-  const int32_t row = (int32_t)(job / p.n_q_heads), h = (int32_t)(job % p.n_q_heads);
-  uint32_t b = 0, end = p.n_seqs;  // the last sequence that begins at or before the row
-  while (end - b > 1u) {
-    const uint32_t mid = b + (end - b) / 2u;
-    if (p.first[mid] <= row)
-      b = mid;
-    else
-      end = mid;
+  const uint4 e = p.ws.open[blockIdx.x];  // parts, sequence, key-value head, tile of rows
+  if (e.x < 2u || e.x > gridDim.x - blockIdx.x || e.y >= p.n_seqs || e.z >= p.n_kv_heads) return;  // nothing, or not valid after an expired wait
+  Walk g{};
+  g.b = e.y;
+  g.enter(p);
+  const uint32_t slot = blockIdx.y * kJoinRows + threadIdx.x % kJoinRows, quad = threadIdx.x / kJoinRows;
+  const uint64_t row = (uint64_t)e.w * kRows + slot;
+  if (row >= (uint64_t)g.n * p.group) return;
+  auto part = [&](uint32_t i) { return p.ws.parts + (size_t)(2u * (blockIdx.x + i) + (i == 0u ? 1u : 0u)) * kTreePartFloats; };
+  float M = -INFINITY, l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (uint32_t i = 0; i < e.x; ++i) {
+    const float* src = part(i);
+    const float mi = __ldcg(src + kRows * 128 + slot), li = __ldcg(src + kRows * 129 + slot);
+    const float4 y = __ldcg(reinterpret_cast<const float4*>(src) + quad * kRows + slot);
+    const float mn = fmaxf(M, mi), ref = mn == -INFINITY ? 0.f : mn, f = exp2_fast(M - ref), h = exp2_fast(mi - ref);
+    M = mn;
+    l = l * f + li * h;
+    o.x = o.x * f + y.x * h;
+    o.y = o.y * f + y.y * h;
+    o.z = o.z * f + y.z * h;
+    o.w = o.w * f + y.w * h;
   }
-  const int32_t most = (int32_t)p.n_tokens, lo = max(0, min(p.first[b], most)), hi = max(lo, min(p.first[b + 1], most));
-  if (row < lo || row >= hi) return;
-  const int64_t cap = (int64_t)p.max_pages * p.page_size, given = p.lens[b], len = max((int64_t)0, min(given, cap));
-  bool bad = given > cap;
-  const int64_t before = given - (hi - lo);
-  const int32_t i = row - lo;
-  constexpr int kPer = D / 32;
-  float q[kPer], o[kPer], m = -INFINITY, l = 0.f;
-#pragma unroll
-  for (int x = 0; x < kPer; ++x) {
-    q[x] = __bfloat162float(p.q[(int64_t)row * p.q_stride + (int64_t)h * D + lane * kPer + x]);
-    o[x] = 0.f;
-  }
-  for (int64_t s = 0; s < len; ++s) {
-    if (s >= before) {
-      const int64_t j = s - before;
-      if (p.mask ? j >= (int64_t)p.mask_words * 32 || !((p.mask[(size_t)row * p.mask_words + j / 32] >> (j % 32)) & 1u) : j > i) continue;
-    }
-    const int32_t page = p.page_table[(size_t)b * p.max_pages + s / p.page_size];
-    if ((uint32_t)page >= p.n_pages) {
-      bad = true;
-      continue;
-    }
-    const int64_t at = (int64_t)page * p.page_stride + (int64_t)(h / p.group) * p.head_stride + (s % p.page_size) * p.slot_stride + lane * kPer;
-    float x = 0.f;
-#pragma unroll
-    for (int c = 0; c < kPer; ++c) x += q[c] * __bfloat162float(p.k[at + c]);
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(kFull, x, d);
-    x *= p.scale_log2;
-    const float mn = fmaxf(m, x), ref = mn == -INFINITY ? 0.f : mn, f = mn == -INFINITY ? 1.f : exp2f(m - mn), e = exp2f(x - ref);
-    m = mn;
-    l = l * f + e;
-#pragma unroll
-    for (int c = 0; c < kPer; ++c) o[c] = o[c] * f + e * __bfloat162float(p.v[at + c]);
-  }
-  const size_t at = ((size_t)row * p.n_q_heads + h);
-#pragma unroll
-  for (int c = 0; c < kPer; ++c) p.out[at * D + lane * kPer + c] = __float2bfloat16_rn(l == 0.f ? 0.f : o[c] / l);
-  if (lane == 0 && p.lse) p.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
-  if (bad && lane == 0 && p.status) atomicOr(p.status, TQ_STATUS_BAD_PAGE);
+  const uint32_t tok = (uint32_t)row / p.group;
+  const size_t at = (size_t)(g.lo + (int32_t)tok) * p.n_q_heads + e.z * p.group + ((uint32_t)row - tok * p.group);
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+  *reinterpret_cast<uint2*>(p.out + at * D + 4u * quad) =
+      l == 0.f ? make_uint2(0u, 0u) : make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+  if (quad == 0u && p.lse) p.lse[at] = l == 0.f ? -INFINITY : (M + log2f(l)) * 0.6931471805599453f;
+}
+
+template <int D>
+int launch(const TreeParams& p, cudaStream_t st) {
+  auto kern = tree_attention_kernel<D>;
+  constexpr size_t smem = TreeSmem<D>::kTotal;
+  const char* what = "tree attention launch";
+  if (int rc = tq_ensure_dynamic_smem((const void*)kern, smem, what)) return rc;
+  static const int regs = [&] {
+    cudaFuncAttributes a{};
+    return cudaFuncGetAttributes(&a, (const void*)kern) == cudaSuccess ? a.numRegs : 0;
+  }();
+  if (256 * kSoftRegs + 256 * kOtherRegs > kTreeThreads * regs) return tq_cuda_status((int)cudaErrorInvalidConfiguration, what);
+  const uint32_t grid = min((uint32_t)sm_count(), kAttnMaxCtas);
+  if (int rc = launch_pdl(kern, dim3(grid), kTreeThreads, smem, st, what, p)) return rc;
+  const uint32_t rows = (uint32_t)min((uint64_t)kRows, (uint64_t)p.n_tokens * p.group);
+  return launch_pdl(tree_join_kernel<D>, dim3(grid, (rows + kJoinRows - 1u) / kJoinRows), kJoinRows * D / 4, 0, st, "tree attention (join) launch", p);
 }
 
 bool misaligned(const void* ptr, uintptr_t align) { return ptr == nullptr || ((uintptr_t)ptr & (align - 1u)) != 0; }
@@ -109,9 +777,9 @@ extern "C" int tq_tree_attention(const tq_kv_cache* cache, const void* d_q, int6
   if (misaligned(d_q, 16) || misaligned(d_first, 4) || misaligned(d_page_table, 4) || misaligned(d_lens, 4) || ((uintptr_t)d_mask & 3u) || misaligned(d_out, 16) ||
       ((uintptr_t)d_lse & 3u) || misaligned(d_ws, 256))
     return TQ_ERR_INVALID_ARG;
-  const tq_attn_ws ws = tq_attn_ws_plan(d_ws, ws_bytes);
-  if (!ws.counters) return TQ_ERR_BUFFER_TOO_SMALL;
   TreeParams p{};
+  p.ws = tq_attn_ws_plan(d_ws, ws_bytes);
+  if (!p.ws.counters) return TQ_ERR_BUFFER_TOO_SMALL;
   p.k = (const __nv_bfloat16*)cache->d_k;
   p.v = (const __nv_bfloat16*)cache->d_v;
   p.page_stride = cache->page_stride;
@@ -132,12 +800,10 @@ extern "C" int tq_tree_attention(const tq_kv_cache* cache, const void* d_q, int6
   p.n_tokens = n_tokens;
   p.n_seqs = n_seqs;
   p.n_q_heads = n_q_heads;
+  p.n_kv_heads = cache->n_kv_heads;
   p.group = n_q_heads / cache->n_kv_heads;
   p.scale_log2 = scale * 1.4426950408889634f;
   p.status = cache->d_status;
   cudaStream_t st = (cudaStream_t)cuda_stream;
-  const uint32_t blocks = (uint32_t)(((uint64_t)n_tokens * n_q_heads + 3u) / 4u);
-  const char* what = "tree attention launch";
-  return cache->head_dim == 64 ? launch_pdl(tree_attention_kernel<64>, dim3(blocks), 128, 0, st, what, p)
-                               : launch_pdl(tree_attention_kernel<128>, dim3(blocks), 128, 0, st, what, p);
+  return cache->head_dim == 64 ? launch<64>(p, st) : launch<128>(p, st);
 }
