@@ -786,12 +786,12 @@ def tq_rmsnorm(h: torch.Tensor, weight: torch.Tensor, delta: torch.Tensor | None
     if ctx is not None:
         with ctx:
             return tq_rmsnorm(h, weight, delta, eps, out, h_out)
-    rows, cols, args, h_out = _norm_args(h, weight, delta, h_out, device)
+    rows, cols, args, ho = _norm_args(h, weight, delta, h_out, device)
     if out is None:
         out = torch.empty((rows, cols), dtype=torch.bfloat16, device=h.device)
     else:
         assert out.get_device() == device and out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() == rows * cols
-    _check(_lib.tq_rmsnorm(*args, eps, rows, cols, h_out, out.data_ptr(), _raw_stream(device)), "tq_rmsnorm")
+    _check(_lib.tq_rmsnorm(*args, eps, rows, cols, ho, out.data_ptr(), _raw_stream(device)), "tq_rmsnorm")
     return out
 
 
@@ -807,14 +807,14 @@ def tq_rmsnorm_q8(h: torch.Tensor, weight: torch.Tensor, delta: torch.Tensor | N
     if ctx is not None:
         with ctx:
             return tq_rmsnorm_q8(h, weight, delta, eps, q, scale, h_out)
-    rows, cols, args, h_out = _norm_args(h, weight, delta, h_out, device)
+    rows, cols, args, ho = _norm_args(h, weight, delta, h_out, device)
     if q is None:
         q = torch.empty((rows, cols), dtype=torch.int8, device=h.device)
     if scale is None:
         scale = torch.empty(rows, dtype=torch.float32, device=h.device)
     assert q.get_device() == device and q.dtype == torch.int8 and q.is_contiguous() and q.numel() == rows * cols
     assert scale.get_device() == device and scale.dtype == torch.float32 and scale.is_contiguous() and scale.numel() == rows
-    _check(_lib.tq_rmsnorm_q8(*args, eps, rows, cols, h_out, q.data_ptr(), scale.data_ptr(), _raw_stream(device)), "tq_rmsnorm_q8")
+    _check(_lib.tq_rmsnorm_q8(*args, eps, rows, cols, ho, q.data_ptr(), scale.data_ptr(), _raw_stream(device)), "tq_rmsnorm_q8")
     return q, scale
 
 
@@ -998,16 +998,17 @@ def tq_cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, worksp
     ks = _strides(k)
     assert k.get_device() == device and k.dtype == torch.bfloat16 and n == B and dim == D and ks[3] == 1
     assert v.get_device() == device and v.dtype == torch.bfloat16 and v.shape == k.shape and _strides(v) == ks
+    n_valid = seen = None  # names of their own: an argument that nobody else holds would be freed, and its memory be the result's
     if kv_len is not None:
         assert kv_len.get_device() == device and kv_len.dtype == torch.int32 and kv_len.is_contiguous() and kv_len.numel() == B
-        kv_len = kv_len.data_ptr()
+        n_valid = kv_len.data_ptr()
     if mask is not None:
         assert mask.get_device() == device and mask.dtype in (torch.uint8, torch.bool) and mask.is_contiguous()
         assert block_len >= 1 and mask.shape == (B, T, -(-S // block_len))
-        mask = mask.data_ptr()
+        seen = mask.data_ptr()
     out, lse = _attn_out(q, out, lse, device)
     _check(_lib.tq_cross_attention(_EncoderKv(k.data_ptr(), v.data_ptr(), B, S, K, D, ks[0], ks[1], ks[2]), q.data_ptr(),
-                                   stride[0] if B > 1 else 0, stride[1] if T > 1 else 0, T, H, kv_len, mask, block_len,
+                                   stride[0] if B > 1 else 0, stride[1] if T > 1 else 0, T, H, n_valid, seen, block_len,
                                    D ** -0.5 if scale is None else scale, out.data_ptr(), lse, workspace.ptr, workspace.bytes,
                                    _raw_stream(device)), "tq_cross_attention")
     return out
