@@ -80,7 +80,6 @@ struct TreeSmem {
   static constexpr uint32_t kSlabs = D / 64;                       // 64 columns = 128 bytes of a swizzled row
   static constexpr uint32_t kTileBytes = kSlabs * kStates * 128;   // queries, keys or values of a tile
   static constexpr uint32_t kStages = D == 128 ? 5 : 10;           // K, V, K, V, ...
-  static constexpr uint32_t kAhead = kStages - 2;                  // copies of a loading warp that may be under way behind the one it announces
   static constexpr uint32_t kOffKv = 2 * kTileBytes;
   static constexpr uint32_t kOffMisc = kOffKv + kStages * kTileBytes;
   // misc: [0] dead flag, [4] tensor-memory base, barriers from 16 on
@@ -99,6 +98,14 @@ constexpr uint64_t kTreePartFloats = kRows * (128 + 2);
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
+
+// The barrier is arrived at when the thread's copies so far have landed.
+__device__ __forceinline__ void arrive_after_copies(uint32_t bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+// Between a wait for copies by cp.async and an instruction that reads what they have written through the asynchronous proxy.
+__device__ __forceinline__ void copies_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 // A group of the list of work: tile rt of the rows of sequence b over key-value head kvh.
 struct Walk {
@@ -257,7 +264,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_attention_kernel(const T
   if (threadIdx.x == 0) {
     *dead = 0u;
     for (uint32_t i = 0; i < L::kStages; ++i) {
-      mbar_init(bar(L::kBarKvFull, i), kLoadWarps);
+      mbar_init(bar(L::kBarKvFull, i), kLoadWarps * 33);  // every lane's copies, and a lane that publishes the words of present states
       mbar_init(bar(L::kBarKvEmpty, i), 1);
     }
     for (uint32_t i = 0; i < 2; ++i) {
@@ -332,34 +339,21 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_attention_kernel(const T
         }
       }
     };
-    uint32_t st = 0, round = 0, under_way = 0, told = 0, count = 0;  // stage to fill, stage to announce
-    auto announce = [&]() {
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(L::kBarKvFull, told));
-      if (++told == L::kStages) told = 0;
-      --under_way;
-    };
     constexpr uint32_t kChunks = D / 8, kAtOnce = 32 / kChunks;  // 16 bytes of a row; rows of a warp-wide copy
-    const uint32_t c = lane % kChunks;
-    auto copy = [&](const __nv_bfloat16* src, int64_t off, uint32_t there) {
+    // A lane copies the same 16 bytes of rows lane / kChunks, + kAtOnce, ...: the swizzle turns the place in a row with the row's last three
+    // bits, of which kAtOnce's own are the lane's and the others the loop's.
+    const uint32_t c = lane % kChunks, r_mine = lane / kChunks;
+    const uint32_t place = (c / 8u) * (kStates * 128u) + (mine * 32u + r_mine) * 128u + (((c % 8u) ^ r_mine) << 4);
+    const char* const k_mine = reinterpret_cast<const char*>(p.k + c * 8u);
+    const int64_t k_to_v = reinterpret_cast<const char*>(p.v) - reinterpret_cast<const char*>(p.k);
+    uint32_t st = 0, round = 0, count = 0;  // stage to fill
+    auto claim = [&](uint32_t& dst, uint32_t& full) {
       if (round) wait(bar(L::kBarKvEmpty, st), (round - 1u) & 1u);
-      if (!ok) return;
-      const uint32_t dst = smem0 + L::kOffKv + st * L::kTileBytes + (c / 8u) * (kStates * 128u) + mine * 32u * 128u;
-#pragma unroll
-      for (uint32_t r0 = 0; r0 < 32u; r0 += kAtOnce) {
-        const uint32_t r = r0 + lane / kChunks;
-        const int64_t o = __shfl_sync(kFull, off, r) + c * 8u;
-        cp_async16(dst + r * 128u + (((c % 8u) ^ (r & 7u)) << 4), src + o, (there >> r) & 1u ? 16u : 0u);  // 0: zeros, nothing is read
-      }
-      asm volatile("cp.async.commit_group;" ::: "memory");
+      dst = smem0 + L::kOffKv + st * L::kTileBytes + place;
+      full = bar(L::kBarKvFull, st);
       if (++st == L::kStages) {
         st = 0;
         ++round;
-      }
-      if (++under_way > L::kAhead) {
-        asm volatile("cp.async.wait_group %0;" ::"n"(L::kAhead) : "memory");
-        announce();
       }
     };
     fetch();
@@ -369,25 +363,33 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_attention_kernel(const T
         live = false;
         bad = true;
       }
-      const int64_t off = live ? (int64_t)f_page * p.page_stride + (int64_t)f_kvh * p.head_stride + (int64_t)f_slot * p.slot_stride : 0;
+      const int64_t off = live ? 2 * ((int64_t)f_page * p.page_stride + (int64_t)f_kvh * p.head_stride + (int64_t)f_slot * p.slot_stride) : 0;  // bytes
       fetch();
       const uint32_t there = __ballot_sync(kFull, live);
+      uint32_t k_dst, v_dst, k_full, v_full;
+      claim(k_dst, k_full);
+      claim(v_dst, v_full);
+      if (!ok) break;
       if (lane == 0) s_there[(count % kThere) * 4u + mine] = there;
       ++count;
-      copy(p.k, off, there);
-      if (ok) copy(p.v, off, there);
-    }
-    if (ok) {
-      while (under_way) {  // the last ones, one by one
-        if (under_way > 4u)
-          asm volatile("cp.async.wait_group 4;" ::: "memory");
-        else if (under_way > 2u)
-          asm volatile("cp.async.wait_group 2;" ::: "memory");
-        else if (under_way > 1u)
-          asm volatile("cp.async.wait_group 1;" ::: "memory");
-        else
-          asm volatile("cp.async.wait_group 0;" ::: "memory");
-        announce();
+      auto copy = [&](bool all) {
+#pragma unroll
+        for (uint32_t r0 = 0; r0 < 32u; r0 += kAtOnce) {
+          const char* const from = k_mine + __shfl_sync(kFull, off, r0 + r_mine);
+          const uint32_t turn = (r0 & 7u) << 4, bytes = all || ((there >> (r0 + r_mine)) & 1u) ? 16u : 0u;  // 0: zeros, nothing is read
+          cp_async16((k_dst ^ turn) + r0 * 128u, from, bytes);
+          cp_async16((v_dst ^ turn) + r0 * 128u, from + k_to_v, bytes);
+        }
+      };
+      if (there == 0xFFFFFFFFu)
+        copy(true);
+      else
+        copy(false);
+      arrive_after_copies(k_full);
+      arrive_after_copies(v_full);
+      if (lane == 0) {  // publishes the word of present states
+        mbar_arrive(k_full);
+        mbar_arrive(v_full);
       }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
@@ -437,6 +439,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_attention_kernel(const T
       wait(bar(L::kBarKvFull, v_st), v_round & 1u);
       if (ok) wait(bar(L::kBarPFull, sb), ((count - 1u) >> 1) & 1u);
       if (!ok) return;
+      copies_fence();
       tmem_fence_after();
       if (elect_one()) {
         const uint64_t b = v_desc + v_st * (L::kTileBytes >> 4);
@@ -461,6 +464,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_attention_kernel(const T
         }
         if (ok) wait(bar(L::kBarKvFull, st), round & 1u);
         if (!ok) break;
+        copies_fence();
         tmem_fence_after();
         if (elect_one()) {
           const uint64_t a = q_desc + qb * (L::kTileBytes >> 4), b = kv_desc + st * (L::kTileBytes >> 4);
