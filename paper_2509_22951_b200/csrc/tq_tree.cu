@@ -53,7 +53,7 @@ constexpr int kTreeThreads = 512;
 // checks the kernel's own count: a split above it would wait for ever.
 constexpr int kSoftRegs = 192, kOtherRegs = 64;
 constexpr uint32_t kTmemCols = 512;
-constexpr uint32_t kThere = 8;     // tiles whose words of present states are kept: loads run at most six tiles ahead of the softmax
+constexpr uint32_t kThere = 16;    // tiles whose words of present states are kept: more than loads run ahead of the softmax
 constexpr float kRescale = 8.0f;   // log2 of how far p may exceed 1
 
 struct TreeParams {
@@ -71,6 +71,7 @@ struct TreeParams {
   uint32_t mask_words, max_pages, page_size, n_pages;
   uint32_t n_tokens, n_seqs, n_q_heads, n_kv_heads, group;
   float scale_log2;
+  uint32_t box, boxes;  // slots of a page that one tensor copy brings, copies to a tile of 128 states
   uint32_t* status;
   tq_attn_ws ws;
 };
@@ -80,6 +81,8 @@ struct TreeSmem {
   static constexpr uint32_t kSlabs = D / 64;                       // 64 columns = 128 bytes of a swizzled row
   static constexpr uint32_t kTileBytes = kSlabs * kStates * 128;   // queries, keys or values of a tile
   static constexpr uint32_t kStages = D == 128 ? 5 : 10;           // K, V, K, V, ...
+  // The loading warps work in teams, a tile to a team in turn: a team waits for its copies and announces them, the others' are under way.
+  static constexpr uint32_t kTeams = D == 128 ? 2 : 4;
   static constexpr uint32_t kOffKv = 2 * kTileBytes;
   static constexpr uint32_t kOffMisc = kOffKv + kStages * kTileBytes;
   // misc: [0] dead flag, [4] tensor-memory base, barriers from 16 on
@@ -99,11 +102,11 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 
-// The barrier is arrived at when the thread's copies so far have landed.
-__device__ __forceinline__ void arrive_after_copies(uint32_t bar) {
-  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+               "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
+               : "memory");
 }
-
 // Between a wait for copies by cp.async and an instruction that reads what they have written through the asynchronous proxy.
 __device__ __forceinline__ void copies_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
@@ -242,8 +245,10 @@ __device__ __forceinline__ Plan make_plan(const TreeParams& p, uint32_t lane) {
   return r;
 }
 
-template <int D>
-__global__ void __launch_bounds__(kTreeThreads, 1) tree_attention_kernel(const TreeParams p) {
+// TMA: K and V come by tensor copies of p.box slots of a page, else by cp.async, row by row.
+template <int D, bool TMA>
+__global__ void __launch_bounds__(kTreeThreads, 1)
+    tree_attention_kernel(const TreeParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
   using L = TreeSmem<D>;
   extern __shared__ __align__(1024) uint8_t smem[];  // swizzled tiles start on 1024 bytes
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -264,7 +269,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_attention_kernel(const T
   if (threadIdx.x == 0) {
     *dead = 0u;
     for (uint32_t i = 0; i < L::kStages; ++i) {
-      mbar_init(bar(L::kBarKvFull, i), kLoadWarps * 33);  // every lane's copies, and a lane that publishes the words of present states
+      mbar_init(bar(L::kBarKvFull, i), TMA ? 1 : kLoadWarps / L::kTeams);
       mbar_init(bar(L::kBarKvEmpty, i), 1);
     }
     for (uint32_t i = 0; i < 2; ++i) {
@@ -313,84 +318,173 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_attention_kernel(const T
 
   if (warp >= kSoftWarps) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-  if (warp < kLoadWarp + kLoadWarps) {
+  if (TMA && warp < kLoadWarp + kLoadWarps) {
+    // ---- K and V by tensor copies: one warp, a lane for each box of a tile -----------------------------------
+    if (warp == kLoadWarp) {
+      uint32_t t = more(g) ? begin_of(g) : 0u, t1 = more(g) ? end_of(g) : 0u;
+      // the page of this lane's box of the next tile, asked for one tile ahead of its copies
+      bool f_any = false, f_live = false, bad = false;
+      uint32_t f_slot = 0, f_kvh = 0, f_valid = 0;
+      int32_t f_page = 0;
+      auto fetch = [&]() {
+        f_any = more(g);
+        if (!f_any) return;
+        const uint32_t s0 = t * kStates, s = s0 + lane * p.box, pg = s / p.page_size;
+        f_live = lane < p.boxes && s < g.end;
+        f_slot = s - pg * p.page_size;
+        f_kvh = g.kvh;
+        f_valid = g.end > s0 ? min(kStates, g.end - s0) : 0u;
+        if (f_live) f_page = __ldg(p.page_table + (size_t)g.b * p.max_pages + pg);
+        if (t == 0u && lane == 0u && __ldg(p.lens + g.b) > 0 && (uint32_t)__ldg(p.lens + g.b) > g.len) bad = true;
+        if (++t == t1) {
+          g.next(p);
+          if (more(g)) {
+            t = begin_of(g);
+            t1 = end_of(g);
+          }
+        }
+      };
+      uint32_t st = 0, round = 0, count = 0;
+      auto load = [&](const CUtensorMap* map, bool live, uint32_t kvh, uint32_t slot, int32_t page, uint32_t bytes) {
+        if (round) wait(bar(L::kBarKvEmpty, st), (round - 1u) & 1u);
+        if (!ok) return;
+        const uint32_t full = bar(L::kBarKvFull, st), dst = smem0 + L::kOffKv + st * L::kTileBytes + lane * p.box * 128u;
+        if (lane == 0) mbar_expect_tx(full, bytes);
+        __syncwarp();
+        if (live) {
+#pragma unroll
+          for (uint32_t x = 0; x < L::kSlabs; ++x) tma_load_4d(dst + x * kStates * 128u, map, (int)(x * 64u), (int)slot, (int)kvh, page, full);
+        }
+        __syncwarp();
+        if (++st == L::kStages) {
+          st = 0;
+          ++round;
+        }
+      };
+      fetch();
+      while (f_any && ok) {
+        const uint32_t kvh = f_kvh, slot = f_slot, valid = f_valid;
+        const int32_t page = f_page;
+        bool live = f_live;
+        if (live && (uint32_t)page >= p.n_pages) {
+          live = false;
+          bad = true;
+        }
+        fetch();
+        const uint32_t there = __ballot_sync(kFull, live), bytes = (uint32_t)__popc(there) * p.box * 128u * L::kSlabs;
+        if (lane < 4u) {  // states that are there, 32 to a word
+          uint32_t word = low_bits((int)valid - 32 * (int)lane);
+          if ((uint32_t)__popc(there) * p.box < valid) {  // a page outside the pool
+            for (uint32_t i = 0; i < 32u; ++i)
+              if (!((there >> ((lane * 32u + i) / p.box)) & 1u)) word &= ~(1u << i);
+          }
+          s_there[(count % kThere) * 4u + lane] = word;
+        }
+        __syncwarp();
+        ++count;
+        load(&k_map, live, kvh, slot, page, bytes);
+        if (ok) load(&v_map, live, kvh, slot, page, bytes);
+      }
+      if (__any_sync(kFull, bad) && lane == 0u && p.status != nullptr) atomicOr(p.status, TQ_STATUS_BAD_PAGE);
+    }
+  } else if (warp < kLoadWarp + kLoadWarps) {
     // ---- K and V ----------------------------------------------------------------------------------------
-    const uint32_t mine = warp - kLoadWarp;
-    // the page of this lane's state of the next tile, asked for one tile ahead of its copies
-    bool f_any = more(g), f_live = false;
-    uint32_t f_slot = 0, f_kvh = 0, t = f_any ? begin_of(g) : 0u, t1 = f_any ? end_of(g) : 0u;
-    int32_t f_page = 0;
-    bool bad = false;
+    constexpr uint32_t kTeams = L::kTeams, kTeamWarps = kLoadWarps / kTeams, kMine = kStates / kTeamWarps, kLanes = kMine / 32u;  // states of a warp, of a lane
+    const uint32_t team = (warp - kLoadWarp) / kTeamWarps, s_mine = (warp - kLoadWarp) % kTeamWarps * kMine;
+    uint32_t t = more(g) ? begin_of(g) : 0u, t1 = more(g) ? end_of(g) : 0u;
+    auto step = [&]() {  // to the next tile
+      if (!more(g) || ++t < t1) return;
+      g.next(p);
+      if (more(g)) {
+        t = begin_of(g);
+        t1 = end_of(g);
+      }
+    };
+    for (uint32_t i = 0; i < team; ++i) step();
+    // the pages of this lane's states of the team's next tile, asked for one tile ahead of its copies
+    bool f_any = false, bad = false;
+    uint32_t f_slot[kLanes], f_kvh = 0, f_live = 0;
+    int32_t f_page[kLanes];
     auto fetch = [&]() {
       f_any = more(g);
       if (!f_any) return;
-      const uint32_t s = t * kStates + mine * 32u + lane;
-      const uint32_t pg = s / p.page_size;
-      f_live = s < g.end;
-      f_slot = s - pg * p.page_size;
       f_kvh = g.kvh;
-      if (f_live) f_page = __ldg(p.page_table + (size_t)g.b * p.max_pages + pg);
-      if (t == 0u && lane == 0u && __ldg(p.lens + g.b) > 0 && (uint32_t)__ldg(p.lens + g.b) > g.len) bad = true;
-      if (++t == t1) {
-        g.next(p);
-        if (more(g)) {
-          t = begin_of(g);
-          t1 = end_of(g);
+      f_live = 0u;
+#pragma unroll
+      for (uint32_t i = 0; i < kLanes; ++i) {
+        const uint32_t s = t * kStates + s_mine + i * 32u + lane, pg = s / p.page_size;
+        f_slot[i] = s - pg * p.page_size;
+        f_page[i] = 0;
+        if (s < g.end) {
+          f_live |= 1u << i;
+          f_page[i] = __ldg(p.page_table + (size_t)g.b * p.max_pages + pg);
         }
       }
+      if (t == 0u && lane == 0u && __ldg(p.lens + g.b) > 0 && (uint32_t)__ldg(p.lens + g.b) > g.len) bad = true;
+      for (uint32_t i = 0; i < kTeams; ++i) step();
     };
     constexpr uint32_t kChunks = D / 8, kAtOnce = 32 / kChunks;  // 16 bytes of a row; rows of a warp-wide copy
     // A lane copies the same 16 bytes of rows lane / kChunks, + kAtOnce, ...: the swizzle turns the place in a row with the row's last three
     // bits, of which kAtOnce's own are the lane's and the others the loop's.
     const uint32_t c = lane % kChunks, r_mine = lane / kChunks;
-    const uint32_t place = (c / 8u) * (kStates * 128u) + (mine * 32u + r_mine) * 128u + (((c % 8u) ^ r_mine) << 4);
+    const uint32_t place = smem0 + L::kOffKv + (c / 8u) * (kStates * 128u) + (s_mine + r_mine) * 128u + (((c % 8u) ^ r_mine) << 4);
     const char* const k_mine = reinterpret_cast<const char*>(p.k + c * 8u);
     const int64_t k_to_v = reinterpret_cast<const char*>(p.v) - reinterpret_cast<const char*>(p.k);
-    uint32_t st = 0, round = 0, count = 0;  // stage to fill
-    auto claim = [&](uint32_t& dst, uint32_t& full) {
-      if (round) wait(bar(L::kBarKvEmpty, st), (round - 1u) & 1u);
-      dst = smem0 + L::kOffKv + st * L::kTileBytes + place;
-      full = bar(L::kBarKvFull, st);
-      if (++st == L::kStages) {
-        st = 0;
-        ++round;
+    uint32_t st = 2u * team % L::kStages, round = 0, count = team;  // stage of the keys; tile
+    auto bump = [&](uint32_t& at, uint32_t& turn, uint32_t by) {
+      at += by;
+      if (at >= L::kStages) {
+        at -= L::kStages;
+        ++turn;
       }
     };
     fetch();
     while (f_any && ok) {
-      bool live = f_live;
-      if (live && (uint32_t)f_page >= p.n_pages) {
-        live = false;
-        bad = true;
-      }
-      const int64_t off = live ? 2 * ((int64_t)f_page * p.page_stride + (int64_t)f_kvh * p.head_stride + (int64_t)f_slot * p.slot_stride) : 0;  // bytes
-      fetch();
-      const uint32_t there = __ballot_sync(kFull, live);
-      uint32_t k_dst, v_dst, k_full, v_full;
-      claim(k_dst, k_full);
-      claim(v_dst, v_full);
-      if (!ok) break;
-      if (lane == 0) s_there[(count % kThere) * 4u + mine] = there;
-      ++count;
-      auto copy = [&](bool all) {
+      int64_t off[kLanes];  // bytes
+      uint32_t there[kLanes];
 #pragma unroll
-        for (uint32_t r0 = 0; r0 < 32u; r0 += kAtOnce) {
-          const char* const from = k_mine + __shfl_sync(kFull, off, r0 + r_mine);
-          const uint32_t turn = (r0 & 7u) << 4, bytes = all || ((there >> (r0 + r_mine)) & 1u) ? 16u : 0u;  // 0: zeros, nothing is read
-          cp_async16((k_dst ^ turn) + r0 * 128u, from, bytes);
-          cp_async16((v_dst ^ turn) + r0 * 128u, from + k_to_v, bytes);
+      for (uint32_t i = 0; i < kLanes; ++i) {
+        bool live = (f_live >> i) & 1u;
+        if (live && (uint32_t)f_page[i] >= p.n_pages) {
+          live = false;
+          bad = true;
         }
-      };
-      if (there == 0xFFFFFFFFu)
-        copy(true);
-      else
-        copy(false);
-      arrive_after_copies(k_full);
-      arrive_after_copies(v_full);
-      if (lane == 0) {  // publishes the word of present states
-        mbar_arrive(k_full);
-        mbar_arrive(v_full);
+        off[i] = live ? 2 * ((int64_t)f_page[i] * p.page_stride + (int64_t)f_kvh * p.head_stride + (int64_t)f_slot[i] * p.slot_stride) : 0;
+        there[i] = __ballot_sync(kFull, live);
       }
+      fetch();
+      uint32_t v_st = st, v_round = round;
+      bump(v_st, v_round, 1u);
+      if (round) wait(bar(L::kBarKvEmpty, st), (round - 1u) & 1u);
+      if (v_round && ok) wait(bar(L::kBarKvEmpty, v_st), (v_round - 1u) & 1u);
+      if (!ok) break;
+#pragma unroll
+      for (uint32_t i = 0; i < kLanes; ++i) {
+        if (lane == 0) s_there[(count % kThere) * 4u + s_mine / 32u + i] = there[i];
+        const uint32_t k_dst = place + st * L::kTileBytes + i * 4096u, v_dst = place + v_st * L::kTileBytes + i * 4096u;
+        auto copy = [&](bool all) {
+#pragma unroll
+          for (uint32_t r0 = 0; r0 < 32u; r0 += kAtOnce) {
+            const char* const from = k_mine + __shfl_sync(kFull, off[i], r0 + r_mine);
+            const uint32_t turn = (r0 & 7u) << 4, bytes = all || ((there[i] >> (r0 + r_mine)) & 1u) ? 16u : 0u;  // 0: zeros, nothing is read
+            cp_async16((k_dst ^ turn) + r0 * 128u, from, bytes);
+            cp_async16((v_dst ^ turn) + r0 * 128u, from + k_to_v, bytes);
+          }
+        };
+        if (there[i] == 0xFFFFFFFFu)
+          copy(true);
+        else
+          copy(false);
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(bar(L::kBarKvFull, st));
+        mbar_arrive(bar(L::kBarKvFull, v_st));
+      }
+      bump(st, round, 2u * kTeams % L::kStages);
+      round += 2u * kTeams / L::kStages;
+      count += kTeams;
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     if (bad && p.status != nullptr) atomicOr(p.status, TQ_STATUS_BAD_PAGE);
@@ -422,9 +516,9 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_attention_kernel(const T
     if (warp == kQueryWarp && lane == 0) p.ws.open[blockIdx.x] = open;  // for the joining kernel
   } else if (warp == kMmaWarp) {
     // ---- products ---------------------------------------------------------------------------------------
-    uint32_t st = 0, round = 0, count = 0, q_count = 0;  // count: tiles
-    bool have = false;                                   // a tile whose product with V is to come
-    uint32_t v_st = 0, v_round = 0, accumulate = 0;
+    // Scores of the next tile or the product of an earlier one with V, whichever is ready: up to two tiles' scores may wait for their p.
+    uint32_t st = 0, round = 0, done = 0, asked = 0, q_count = 0;  // stage of the next keys; tiles multiplied with V, tiles with scores
+    uint32_t v_st[2] = {0, 0}, v_round[2] = {0, 0}, v_flags[2] = {0, 0};  // of the tiles in between, by buffer: stage of their values; 1: not the group's first tile; states that are there << 8
     const uint32_t idesc_qk = umma_idesc(128, 128), idesc_pv = umma_idesc(128, D) | kIdescNMajorB;
     const uint64_t q_desc = umma_desc(smem0), kv_desc = umma_desc(smem0 + L::kOffKv), v_desc = umma_desc_n_major(smem0 + L::kOffKv, kStates);
     auto bump = [&]() {
@@ -433,37 +527,48 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_attention_kernel(const T
         ++round;
       }
     };
-    // the pending tile's p times V, both halves of its states
-    auto pv = [&]() {
-      const uint32_t sb = (count - 1u) & 1u;
-      wait(bar(L::kBarKvFull, v_st), v_round & 1u);
-      if (ok) wait(bar(L::kBarPFull, sb), ((count - 1u) >> 1) & 1u);
-      if (!ok) return;
-      copies_fence();
-      tmem_fence_after();
-      if (elect_one()) {
-        const uint64_t b = v_desc + v_st * (L::kTileBytes >> 4);
+    bool any = more(g);
+    uint32_t t = any ? begin_of(g) : 0u, t0 = t, t1 = any ? end_of(g) : 0u;
+    uint32_t idle = 0;
+    while (ok && (any || done != asked)) {
+      const uint32_t sb = done & 1u;
+      // the tile's p times V, both halves of its states
+      if (done != asked && mbar_test(bar(L::kBarPFull, sb), (done >> 1) & 1u) && mbar_test(bar(L::kBarKvFull, v_st[sb]), v_round[sb] & 1u)) {
+        idle = 0;
+        if (TMA) {
+          const uint32_t valid = v_flags[sb] >> 8;
+          if (valid < kStates) {  // past the last state memory may hold anything, and 0 x NaN is NaN
+            constexpr uint32_t kChunks = D / 8;
+            uint8_t* const tile = smem + L::kOffKv + v_st[sb] * L::kTileBytes;
+            for (uint32_t i = lane; i < (kStates - valid) * kChunks; i += 32u) {
+              const uint32_t r = valid + i / kChunks, c = i % kChunks;
+              *reinterpret_cast<uint4*>(tile + (c / 8u) * (kStates * 128u) + r * 128u + (c % 8u) * 16u) = make_uint4(0, 0, 0, 0);
+            }
+          }
+        }
+        copies_fence();
+        tmem_fence_after();
+        __syncwarp();
+        if (elect_one()) {
+          const uint64_t b = v_desc + v_st[sb] * (L::kTileBytes >> 4);
 #pragma unroll
-        for (uint32_t kk = 0; kk < kStates / 16u; ++kk) {
-          const uint32_t w = kk / 4u;
-          umma_bf16_ts(tmem + 2u * kStates + w * D, tmem + sb * kStates + w * kSide + (kk % 4u) * 8u, b + kk * (2048u >> 4), idesc_pv,
-                       accumulate | (kk % 4u));
+          for (uint32_t kk = 0; kk < kStates / 16u; ++kk) {
+            const uint32_t w = kk / 4u;
+            umma_bf16_ts(tmem + 2u * kStates + w * D, tmem + sb * kStates + w * kSide + (kk % 4u) * 8u, b + kk * (2048u >> 4), idesc_pv,
+                         (v_flags[sb] & 1u) | (kk % 4u));
+          }
+          umma_commit(bar(L::kBarODone, sb));
+          umma_commit(bar(L::kBarKvEmpty, v_st[sb]));
         }
-        umma_commit(bar(L::kBarODone, sb));
-        umma_commit(bar(L::kBarKvEmpty, v_st));
+        __syncwarp();
+        ++done;
+        continue;
       }
-      __syncwarp();
-      have = false;
-    };
-    for (; more(g) && ok; g.next(p), ++q_count) {
-      const uint32_t t0 = begin_of(g), t1 = end_of(g), qb = q_count & 1u;
-      for (uint32_t t = t0; t < t1 && ok; ++t) {
-        if (t == t0) {
-          if (have) pv();
-          if (ok) wait(bar(L::kBarQFull, qb), (q_count >> 1) & 1u);
-        }
-        if (ok) wait(bar(L::kBarKvFull, st), round & 1u);
-        if (!ok) break;
+      // the next tile's scores, when the buffer's last p is spent
+      if (any && asked - done < 2u && mbar_test(bar(L::kBarKvFull, st), round & 1u) &&
+          (t != t0 || mbar_test(bar(L::kBarQFull, q_count & 1u), (q_count >> 1) & 1u))) {
+        idle = 0;
+        const uint32_t qb = q_count & 1u, to = asked & 1u;
         copies_fence();
         tmem_fence_after();
         if (elect_one()) {
@@ -472,25 +577,41 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_attention_kernel(const T
           for (uint32_t kk = 0; kk < D / 16; ++kk) {
             constexpr uint32_t kSlab = (kStates * 128u) >> 4;
             const uint32_t off = (kk / 4u) * kSlab + (kk % 4u) * 2u;  // in 16 bytes
-            umma_bf16(tmem + (count & 1u) * kStates, a + off, b + off, idesc_qk, kk != 0u);
+            umma_bf16(tmem + to * kStates, a + off, b + off, idesc_qk, kk != 0u);
           }
-          umma_commit(bar(L::kBarSFull, count & 1u));
+          umma_commit(bar(L::kBarSFull, to));
           umma_commit(bar(L::kBarKvEmpty, st));
           if (t + 1u == t1) umma_commit(bar(L::kBarQEmpty, qb));
-          mbar_arrive(bar(L::kBarSFull, count & 1u));
+          mbar_arrive(bar(L::kBarSFull, to));
         }
         __syncwarp();
         bump();
-        if (have) pv();
-        have = true;
-        accumulate = t != t0 ? 1u : 0u;
-        v_st = st;
-        v_round = round;
+        const uint32_t flags = (t != t0 ? 1u : 0u) | (g.end > t * kStates ? min(kStates, g.end - t * kStates) << 8 : 0u);
+        if (to) {
+          v_st[1] = st;
+          v_round[1] = round;
+          v_flags[1] = flags;
+        } else {
+          v_st[0] = st;
+          v_round[0] = round;
+          v_flags[0] = flags;
+        }
         bump();
-        ++count;
+        ++asked;
+        if (++t == t1) {
+          g.next(p);
+          ++q_count;
+          any = more(g);
+          if (any) {
+            t = t0 = begin_of(g);
+            t1 = end_of(g);
+          }
+        }
+        continue;
       }
+      if (++idle == kSpinLimit || ((idle & 1023u) == 1023u && *dead)) ok = false;
+      ok = __all_sync(kFull, ok);
     }
-    if (have && ok) pv();
   }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
@@ -746,9 +867,25 @@ __global__ void __launch_bounds__(kJoinRows * D / 4) tree_join_kernel(const Tree
   if (quad == 0u && p.lse) p.lse[at] = l == 0.f ? -INFINITY : (M + log2f(l)) * 0.6931471805599453f;
 }
 
-template <int D>
-int launch(const TreeParams& p, cudaStream_t st) {
-  auto kern = tree_attention_kernel<D>;
+// The tensor map of a pool: (column, slot, head, page), boxes of 64 columns x `box` slots, 128-byte swizzle.
+bool encode(CUtensorMap* map, const void* base, const tq_kv_cache* c, uint32_t box) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t row = c->head_dim * 2u;
+  const cuuint64_t dims[4] = {c->head_dim, c->page_size, c->n_kv_heads, c->n_pages};
+  cuuint64_t strides[3] = {(cuuint64_t)c->slot_stride * 2u, (cuuint64_t)c->head_stride * 2u, (cuuint64_t)c->page_stride * 2u};
+  for (int i = 0; i < 3; ++i) {
+    if (dims[i + 1] == 1u) strides[i] = row;  // means nothing
+    if (strides[i] == 0u) return false;
+  }
+  const cuuint32_t boxes[4] = {64u, box, 1u, 1u}, step[4] = {1u, 1u, 1u, 1u};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, boxes, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, bool TMA>
+int launch(const TreeParams& p, const CUtensorMap& k_map, const CUtensorMap& v_map, cudaStream_t st) {
+  auto kern = tree_attention_kernel<D, TMA>;
   constexpr size_t smem = TreeSmem<D>::kTotal;
   const char* what = "tree attention launch";
   if (int rc = tq_ensure_dynamic_smem((const void*)kern, smem, what)) return rc;
@@ -758,7 +895,7 @@ int launch(const TreeParams& p, cudaStream_t st) {
   }();
   if (256 * kSoftRegs + 256 * kOtherRegs > kTreeThreads * regs) return tq_cuda_status((int)cudaErrorInvalidConfiguration, what);
   const uint32_t grid = min((uint32_t)sm_count(), kAttnMaxCtas);
-  if (int rc = launch_pdl(kern, dim3(grid), kTreeThreads, smem, st, what, p)) return rc;
+  if (int rc = launch_pdl(kern, dim3(grid), kTreeThreads, smem, st, what, p, k_map, v_map)) return rc;
   const uint32_t rows = (uint32_t)min((uint64_t)kRows, (uint64_t)p.n_tokens * p.group);
   return launch_pdl(tree_join_kernel<D>, dim3(grid, (rows + kJoinRows - 1u) / kJoinRows), kJoinRows * D / 4, 0, st, "tree attention (join) launch", p);
 }
@@ -809,5 +946,12 @@ extern "C" int tq_tree_attention(const tq_kv_cache* cache, const void* d_q, int6
   p.scale_log2 = scale * 1.4426950408889634f;
   p.status = cache->d_status;
   cudaStream_t st = (cudaStream_t)cuda_stream;
-  return cache->head_dim == 64 ? launch<64>(p, st) : launch<128>(p, st);
+  // Boxes that fit pages and tiles alike; the swizzle repeats every 8 rows, so pages of other sizes are copied row by row.
+  p.box = 128u;
+  while (cache->page_size % p.box) p.box /= 2u;
+  p.boxes = kStates / p.box;
+  CUtensorMap k_map{}, v_map{};
+  if (p.box >= 8u && encode(&k_map, cache->d_k, cache, p.box) && encode(&v_map, cache->d_v, cache, p.box))
+    return cache->head_dim == 64 ? launch<64, true>(p, k_map, v_map, st) : launch<128, true>(p, k_map, v_map, st);
+  return cache->head_dim == 64 ? launch<64, false>(p, k_map, v_map, st) : launch<128, false>(p, k_map, v_map, st);
 }
