@@ -90,7 +90,7 @@ struct TreeSmem {
   static constexpr uint32_t kBarQFull = kBarKvEmpty + 8 * kStages, kBarQEmpty = kBarQFull + 16;
   static constexpr uint32_t kBarSFull = kBarQEmpty + 16, kBarPFull = kBarSFull + 16, kBarODone = kBarPFull + 16, kBarMl = kBarODone + 16;
   static constexpr uint32_t kOffPlan = (kBarMl + 8 + 15) / 16 * 16;
-  static constexpr uint32_t kOffThere = kOffPlan + 48;
+  static constexpr uint32_t kOffThere = kOffPlan + 96;
   static constexpr uint32_t kOffMl = kOffThere + kThere * 16;
   static constexpr uint32_t kTotal = kOffMisc + kOffMl + 2 * kRows * 8;
   static_assert(kTotal <= 232448, "shared memory of one CTA");
@@ -110,6 +110,9 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
 // Between a wait for copies by cp.async and an instruction that reads what they have written through the asynchronous proxy.
 __device__ __forceinline__ void copies_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
+// Units that a group counts beside its tiles of states: what its end and the next one's beginning cost the softmax warps.
+constexpr uint32_t kGroupUnits = 1;
+
 // A group of the list of work: tile rt of the rows of sequence b over key-value head kvh.
 struct Walk {
   uint32_t b, kvh, rt, row_tiles;
@@ -117,7 +120,7 @@ struct Walk {
   uint32_t n, len;  // its new tokens and states
   int64_t before;   // states before its new tokens (negative: the first ones have none)
   uint32_t end;     // states that the tile's rows may look at
-  uint32_t tiles, unit;  // of states; first unit
+  uint32_t tiles, unit;  // of states; first unit (kGroupUnits of them, then a unit for each tile)
 
   __device__ __forceinline__ void enter(const TreeParams& p) {
     const int32_t most = (int32_t)p.n_tokens;
@@ -148,7 +151,7 @@ struct Walk {
     }
   }
   __device__ __forceinline__ void next(const TreeParams& p) {
-    unit += tiles;
+    unit += tiles + kGroupUnits;
     if (++rt == row_tiles) {
       rt = 0;
       if (++kvh == p.n_kv_heads) {
@@ -166,10 +169,10 @@ struct Walk {
 struct Plan {
   uint32_t u0, u1, cut;             // units; whether groups are cut (else the groups that begin in the share are the share)
   uint32_t mean, over;              // CTA i has the units i * mean + min(i, over) and on
-  uint32_t b, kvh, rt, unit;        // first group
+  Walk at;                          // first group; at.b = n_seqs: none
   __device__ __forceinline__ uint32_t cta_of(uint32_t u) const { return u < over * (mean + 1u) ? u / (mean + 1u) : over + (u - over * (mean + 1u)) / mean; }
 };
-static_assert(sizeof(Plan) <= 48, "room for the plan");
+static_assert(sizeof(Plan) <= 96 && alignof(Plan) <= 16, "room for the plan");
 
 // Groups are left whole where the longest share is then no more than kWholeTiles tiles above the mean of the shares.
 constexpr uint32_t kWholeTiles = 3;
@@ -185,9 +188,9 @@ __device__ __forceinline__ Plan make_plan(const TreeParams& p, uint32_t lane) {
     uint32_t u = 0;
     for (w.rt = 0; w.rt < w.row_tiles; ++w.rt) {
       w.tile(p);
-      u += w.tiles;
-      most = max(most, w.tiles);
-      least = min(least, w.tiles);
+      u += w.tiles + kGroupUnits;
+      most = max(most, w.tiles + kGroupUnits);
+      least = min(least, w.tiles + kGroupUnits);
     }
     return u;
   };
@@ -208,7 +211,7 @@ __device__ __forceinline__ Plan make_plan(const TreeParams& p, uint32_t lane) {
     groups += __shfl_xor_sync(kFull, groups, d);
   }
   const uint32_t total = __shfl_sync(kFull, incl, 31) * p.n_kv_heads;
-  r.b = p.n_seqs;
+  r.at.b = p.n_seqs;
   if (total == 0u) return r;
   const uint32_t ctas = min(gridDim.x, total);
   r.mean = total / ctas;
@@ -237,11 +240,8 @@ __device__ __forceinline__ Plan make_plan(const TreeParams& p, uint32_t lane) {
   w.rt = 0;
   w.enter(p);
   w.tile(p);
-  while (w.b < p.n_seqs && (r.u0 >= w.unit + w.tiles || (!r.cut && w.unit < r.u0))) w.next(p);
-  r.b = w.b;
-  r.kvh = w.kvh;
-  r.rt = w.rt;
-  r.unit = w.unit;
+  while (w.b < p.n_seqs && (r.u0 >= w.unit + kGroupUnits + w.tiles || (!r.cut && w.unit < r.u0))) w.next(p);
+  r.at = w;
   return r;
 }
 
@@ -269,7 +269,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
   if (threadIdx.x == 0) {
     *dead = 0u;
     for (uint32_t i = 0; i < L::kStages; ++i) {
-      mbar_init(bar(L::kBarKvFull, i), TMA ? 1 : kLoadWarps / L::kTeams);
+      mbar_init(bar(L::kBarKvFull, i), TMA ? 2 : kLoadWarps / L::kTeams);
       mbar_init(bar(L::kBarKvEmpty, i), 1);
     }
     for (uint32_t i = 0; i < 2; ++i) {
@@ -302,91 +302,84 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
     ok = ok && mbar_wait(b, parity, dead);
     ok = __all_sync(kFull, ok);
   };
-  Walk g{};
-  g.b = plan.b;
-  g.kvh = plan.kvh;
-  g.rt = plan.rt;
-  g.unit = plan.unit;
-  if (g.b < p.n_seqs) {
-    g.enter(p);
-    g.tile(p);
-  }
+  Walk g = plan.at;
   // the tiles of states of group w that are this CTA's
-  auto more = [&](const Walk& w) { return w.b < p.n_seqs && w.unit < plan.u1; };
-  auto begin_of = [&](const Walk& w) { return plan.cut && plan.u0 > w.unit ? plan.u0 - w.unit : 0u; };
-  auto end_of = [&](const Walk& w) { return plan.cut && plan.u1 - w.unit < w.tiles ? plan.u1 - w.unit : w.tiles; };
+  auto in_share = [&](const Walk& w) { return w.b < p.n_seqs && w.unit < plan.u1; };
+  auto clip = [&](const Walk& w, uint32_t u) { return u > w.unit + kGroupUnits ? min(u - w.unit - kGroupUnits, w.tiles) : 0u; };
+  auto begin_of = [&](const Walk& w) { return plan.cut ? clip(w, plan.u0) : 0u; };
+  auto end_of = [&](const Walk& w) { return plan.cut ? clip(w, plan.u1) : w.tiles; };
+  // (the share's last group may have none of its tiles in it: then the share has ended)
+  auto more = [&](const Walk& w) { return in_share(w) && begin_of(w) < end_of(w); };
 
   if (warp >= kSoftWarps) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
   if (TMA && warp < kLoadWarp + kLoadWarps) {
-    // ---- K and V by tensor copies: one warp, a lane for each box of a tile -----------------------------------
-    if (warp == kLoadWarp) {
-      uint32_t t = more(g) ? begin_of(g) : 0u, t1 = more(g) ? end_of(g) : 0u;
-      // the page of this lane's box of the next tile, asked for one tile ahead of its copies
-      bool f_any = false, f_live = false, bad = false;
-      uint32_t f_slot = 0, f_kvh = 0, f_valid = 0;
-      int32_t f_page = 0;
-      auto fetch = [&]() {
-        f_any = more(g);
-        if (!f_any) return;
-        const uint32_t s0 = t * kStates, s = s0 + lane * p.box, pg = s / p.page_size;
-        f_live = lane < p.boxes && s < g.end;
-        f_slot = s - pg * p.page_size;
-        f_kvh = g.kvh;
-        f_valid = g.end > s0 ? min(kStates, g.end - s0) : 0u;
-        if (f_live) f_page = __ldg(p.page_table + (size_t)g.b * p.max_pages + pg);
-        if (t == 0u && lane == 0u && __ldg(p.lens + g.b) > 0 && (uint32_t)__ldg(p.lens + g.b) > g.len) bad = true;
-        if (++t == t1) {
-          g.next(p);
-          if (more(g)) {
-            t = begin_of(g);
-            t1 = end_of(g);
-          }
+    // ---- K and V by tensor copies: two warps for each, which share a tile's boxes, a lane to a box ------------------
+    const uint32_t values = (warp - kLoadWarp) >> 1, part = (warp - kLoadWarp) & 1u;
+    const CUtensorMap* const map = values ? &v_map : &k_map;
+    uint32_t t = more(g) ? begin_of(g) : 0u, t1 = more(g) ? end_of(g) : 0u;
+    // the page of this lane's box of the next tile, asked for one tile ahead of its copies
+    bool f_any = false, f_live = false, bad = false;
+    uint32_t f_slot = 0, f_kvh = 0, f_valid = 0;
+    int32_t f_page = 0;
+    auto fetch = [&]() {
+      f_any = more(g);
+      if (!f_any) return;
+      const uint32_t s0 = t * kStates, s = s0 + lane * p.box, pg = s / p.page_size;
+      f_live = lane < p.boxes && s < g.end;
+      f_slot = s - pg * p.page_size;
+      f_kvh = g.kvh;
+      f_valid = g.end > s0 ? min(kStates, g.end - s0) : 0u;
+      if (f_live) f_page = __ldg(p.page_table + (size_t)g.b * p.max_pages + pg);
+      if (t == 0u && lane == 0u && __ldg(p.lens + g.b) > 0 && (uint32_t)__ldg(p.lens + g.b) > g.len) bad = true;
+      if (++t == t1) {
+        g.next(p);
+        if (more(g)) {
+          t = begin_of(g);
+          t1 = end_of(g);
         }
-      };
-      uint32_t st = 0, round = 0, count = 0;
-      auto load = [&](const CUtensorMap* map, bool live, uint32_t kvh, uint32_t slot, int32_t page, uint32_t bytes) {
-        if (round) wait(bar(L::kBarKvEmpty, st), (round - 1u) & 1u);
-        if (!ok) return;
-        const uint32_t full = bar(L::kBarKvFull, st), dst = smem0 + L::kOffKv + st * L::kTileBytes + lane * p.box * 128u;
-        if (lane == 0) mbar_expect_tx(full, bytes);
-        __syncwarp();
-        if (live) {
-#pragma unroll
-          for (uint32_t x = 0; x < L::kSlabs; ++x) tma_load_4d(dst + x * kStates * 128u, map, (int)(x * 64u), (int)slot, (int)kvh, page, full);
-        }
-        __syncwarp();
-        if (++st == L::kStages) {
-          st = 0;
-          ++round;
-        }
-      };
-      fetch();
-      while (f_any && ok) {
-        const uint32_t kvh = f_kvh, slot = f_slot, valid = f_valid;
-        const int32_t page = f_page;
-        bool live = f_live;
-        if (live && (uint32_t)page >= p.n_pages) {
-          live = false;
-          bad = true;
-        }
-        fetch();
-        const uint32_t there = __ballot_sync(kFull, live), bytes = (uint32_t)__popc(there) * p.box * 128u * L::kSlabs;
-        if (lane < 4u) {  // states that are there, 32 to a word
-          uint32_t word = low_bits((int)valid - 32 * (int)lane);
-          if ((uint32_t)__popc(there) * p.box < valid) {  // a page outside the pool
-            for (uint32_t i = 0; i < 32u; ++i)
-              if (!((there >> ((lane * 32u + i) / p.box)) & 1u)) word &= ~(1u << i);
-          }
-          s_there[(count % kThere) * 4u + lane] = word;
-        }
-        __syncwarp();
-        ++count;
-        load(&k_map, live, kvh, slot, page, bytes);
-        if (ok) load(&v_map, live, kvh, slot, page, bytes);
       }
-      if (__any_sync(kFull, bad) && lane == 0u && p.status != nullptr) atomicOr(p.status, TQ_STATUS_BAD_PAGE);
+    };
+    uint32_t st = values, round = 0, count = 0;
+    fetch();
+    while (f_any && ok) {
+      const uint32_t kvh = f_kvh, slot = f_slot, valid = f_valid;
+      const int32_t page = f_page;
+      bool live = f_live;
+      if (live && (uint32_t)page >= p.n_pages) {
+        live = false;
+        bad = true;
+      }
+      fetch();
+      const uint32_t there = __ballot_sync(kFull, live);
+      if (warp == kLoadWarp && lane < 4u) {  // states that are there, 32 to a word
+        uint32_t word = low_bits((int)valid - 32 * (int)lane);
+        if ((uint32_t)__popc(there) * p.box < valid) {  // a page outside the pool
+          for (uint32_t i = 0; i < 32u; ++i)
+            if (!((there >> ((lane * 32u + i) / p.box)) & 1u)) word &= ~(1u << i);
+        }
+        s_there[(count % kThere) * 4u + lane] = word;
+      }
+      ++count;
+      if (round) wait(bar(L::kBarKvEmpty, st), (round - 1u) & 1u);
+      if (!ok) break;
+      // columns of 64 to a warp, or, where there are no more, boxes in turn
+      const bool mine = L::kSlabs == 2u ? live : live && (lane & 1u) == part;
+      const uint32_t slab = L::kSlabs == 2u ? part : 0u;
+      const uint32_t full = bar(L::kBarKvFull, st), dst = smem0 + L::kOffKv + st * L::kTileBytes + slab * kStates * 128u + lane * p.box * 128u;
+      const uint32_t bytes = (uint32_t)__popc(__ballot_sync(kFull, mine)) * p.box * 128u;
+      __syncwarp();  // the words of present states are written
+      if (lane == 0) mbar_expect_tx(full, bytes);
+      __syncwarp();
+      if (mine) tma_load_4d(dst, map, (int)(slab * 64u), (int)slot, (int)kvh, page, full);
+      __syncwarp();
+      st += 2u;
+      if (st >= L::kStages) {
+        st -= L::kStages;
+        ++round;
+      }
     }
+    if (warp == kLoadWarp && __any_sync(kFull, bad) && lane == 0u && p.status != nullptr) atomicOr(p.status, TQ_STATUS_BAD_PAGE);
   } else if (warp < kLoadWarp + kLoadWarps) {
     // ---- K and V ----------------------------------------------------------------------------------------
     constexpr uint32_t kTeams = L::kTeams, kTeamWarps = kLoadWarps / kTeams, kMine = kStates / kTeamWarps, kLanes = kMine / 32u;  // states of a warp, of a lane
@@ -510,8 +503,8 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(L::kBarQFull, qb));
       ++count;
-      open = make_uint4(0u, g.b, g.kvh, g.rt);
-      if (plan.cut && g.unit >= plan.u0 && plan.u1 - g.unit < g.tiles) open.x = plan.cta_of(g.unit + g.tiles - 1u) - blockIdx.x + 1u;
+      open = make_uint4(0u, (uint32_t)g.lo, g.kvh, g.rt);
+      if (begin_of(g) == 0u && end_of(g) < g.tiles) open.x = plan.cta_of(g.unit + kGroupUnits + g.tiles - 1u) - blockIdx.x + 1u | rows << 16;
     }
     if (warp == kQueryWarp && lane == 0) p.ws.open[blockIdx.x] = open;  // for the joining kernel
   } else if (warp == kMmaWarp) {
@@ -730,32 +723,32 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
       const float inv = 1.0f / sum;
       bool nan = false;
       constexpr uint32_t kColumns = D / 2;  // of a row, for each of its two threads
-#pragma unroll 1
-      for (uint32_t i = 0; i < kColumns; i += 16u) {
-        const uint32_t col = w * kColumns + i;
-        uint32_t x[16], y[16];
-        TMEM_LD16(x, o_addr + col);
-        TMEM_LD16(y, o_addr + D + col);
-        tmem_wait_ld();
-        float o[16];
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          o[k] = __uint_as_float(x[k]) * fa + __uint_as_float(y[k]) * fb;
-          nan = nan || o[k] != o[k];
+      for (uint32_t i = 0; i < kColumns; i += 32u) {
+        const uint32_t col = w * kColumns + i;
+        uint32_t x[32], y[32];
+        TMEM_LD32(x, o_addr + col);
+        TMEM_LD32(y, o_addr + D + col);
+        tmem_wait_ld();
+#pragma unroll
+        for (int k = 0; k < 32; ++k) {
+          const float o = __uint_as_float(x[k]) * fa + __uint_as_float(y[k]) * fb;
+          nan = nan || o != o;
+          x[k] = __float_as_uint(o);
         }
         if (!live) continue;
         if (whole) {
 #pragma unroll
-          for (int k = 0; k < 16; k += 8) {
+          for (int k = 0; k < 32; k += 8) {
             float f[8];
 #pragma unroll
-            for (int z = 0; z < 8; ++z) f[z] = sum == 0.f ? 0.f : o[k + z] * inv;
+            for (int z = 0; z < 8; ++z) f[z] = sum == 0.f ? 0.f : __uint_as_float(x[k + z]) * inv;
             store8<TQ_TYPE_BF16>(p.out, at * D + col + k, f);
           }
         } else {
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            reinterpret_cast<float4*>(mine)[(col / 4u + k) * kRows + row_in] = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+          for (int k = 0; k < 8; ++k)
+            reinterpret_cast<uint4*>(mine)[(col / 4u + k) * kRows + row_in] = make_uint4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
         }
       }
       if (live && w == 0u) {
@@ -828,39 +821,45 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
   }
 }
 
-// Joins the parts of the groups that were cut.  grid (CTAs of the kernel above, slices of 8 rows): the group that begins in CTA x's share and goes
-// on, if there is one; a thread has four columns of a row and adds the parts up in their order.
-constexpr uint32_t kJoinRows = 8;
+// Joins the parts of the groups that were cut.  grid (CTAs of the kernel above, slices of 8 rows): the group whose first tile is in CTA x's share and
+// whose last is not, if there is one; a thread has four columns of a row and adds the parts up in their order, kJoinAtOnce of them asked for together.
+constexpr uint32_t kJoinRows = 8, kJoinAtOnce = 8;
 template <int D>
 __global__ void __launch_bounds__(kJoinRows * D / 4) tree_join_kernel(const TreeParams p) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const uint4 e = p.ws.open[blockIdx.x];  // parts, sequence, key-value head, tile of rows
-  if (e.x < 2u || e.x > gridDim.x - blockIdx.x || e.y >= p.n_seqs || e.z >= p.n_kv_heads) return;  // nothing, or not valid after an expired wait
-  Walk g{};
-  g.b = e.y;
-  g.enter(p);
-  const uint32_t slot = blockIdx.y * kJoinRows + threadIdx.x % kJoinRows, quad = threadIdx.x / kJoinRows;
-  const uint64_t row = (uint64_t)e.w * kRows + slot;
-  if (row >= (uint64_t)g.n * p.group) return;
-  auto part = [&](uint32_t i) { return p.ws.parts + (size_t)(2u * (blockIdx.x + i) + (i == 0u ? 1u : 0u)) * kTreePartFloats; };
+  const uint4 e = p.ws.open[blockIdx.x];  // parts and rows << 16, first row of the sequence, key-value head, tile of rows
+  const uint32_t parts = e.x & 0xFFFFu, slot = blockIdx.y * kJoinRows + threadIdx.x % kJoinRows, quad = threadIdx.x / kJoinRows;
+  if (parts < 2u || parts > gridDim.x - blockIdx.x || slot >= e.x >> 16) return;  // none, or not valid after an expired wait
+  const uint32_t row = e.w * kRows + slot, tok = row / p.group;
+  const uint64_t out_row = (uint64_t)e.y + tok;
+  if (e.z >= p.n_kv_heads || out_row >= p.n_tokens) return;
   float M = -INFINITY, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (uint32_t i = 0; i < e.x; ++i) {
-    const float* src = part(i);
-    const float mi = __ldcg(src + kRows * 128 + slot), li = __ldcg(src + kRows * 129 + slot);
-    const float4 y = __ldcg(reinterpret_cast<const float4*>(src) + quad * kRows + slot);
-    const float mn = fmaxf(M, mi), ref = mn == -INFINITY ? 0.f : mn, f = exp2_fast(M - ref), h = exp2_fast(mi - ref);
-    M = mn;
-    l = l * f + li * h;
-    o.x = o.x * f + y.x * h;
-    o.y = o.y * f + y.y * h;
-    o.z = o.z * f + y.z * h;
-    o.w = o.w * f + y.w * h;
+  for (uint32_t i0 = 0; i0 < parts; i0 += kJoinAtOnce) {
+    float mi[kJoinAtOnce], li[kJoinAtOnce];
+    float4 y[kJoinAtOnce];
+#pragma unroll
+    for (uint32_t i = 0; i < kJoinAtOnce; ++i) {
+      const uint32_t at = min(i0 + i, parts - 1u);
+      const float* const src = p.ws.parts + (size_t)(2u * (blockIdx.x + at) + (at == 0u ? 1u : 0u)) * kTreePartFloats;
+      mi[i] = __ldcg(src + kRows * 128 + slot);
+      li[i] = __ldcg(src + kRows * 129 + slot);
+      y[i] = __ldcg(reinterpret_cast<const float4*>(src) + quad * kRows + slot);
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kJoinAtOnce; ++i) {
+      if (i0 + i >= parts) break;
+      const float mn = fmaxf(M, mi[i]), ref = mn == -INFINITY ? 0.f : mn, f = exp2_fast(M - ref), h = exp2_fast(mi[i] - ref);
+      M = mn;
+      l = l * f + li[i] * h;
+      o.x = o.x * f + y[i].x * h;
+      o.y = o.y * f + y[i].y * h;
+      o.z = o.z * f + y[i].z * h;
+      o.w = o.w * f + y[i].w * h;
+    }
   }
-  const uint32_t tok = (uint32_t)row / p.group;
-  const size_t at = (size_t)(g.lo + (int32_t)tok) * p.n_q_heads + e.z * p.group + ((uint32_t)row - tok * p.group);
+  const size_t at = (size_t)out_row * p.n_q_heads + e.z * p.group + (row - tok * p.group);
   const float inv = l == 0.f ? 0.f : 1.0f / l;
   *reinterpret_cast<uint2*>(p.out + at * D + 4u * quad) =
       l == 0.f ? make_uint2(0u, 0u) : make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
