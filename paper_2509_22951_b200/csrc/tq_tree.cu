@@ -80,15 +80,18 @@ template <int D>
 struct TreeSmem {
   static constexpr uint32_t kSlabs = D / 64;                       // 64 columns = 128 bytes of a swizzled row
   static constexpr uint32_t kTileBytes = kSlabs * kStates * 128;   // queries, keys or values of a tile
-  static constexpr uint32_t kStages = D == 128 ? 5 : 10;           // K, V, K, V, ...
-  // The loading warps work in teams, a tile to a team in turn: a team waits for its copies and announces them, the others' are under way.
+  // Buffers of queries, keys and values.  Keys and values have a ring each: values are wanted a softmax later than keys, and in one ring they
+  // would wait in slots that keys could use.
+  static constexpr uint32_t kQueries = D == 128 ? 1 : 2, kKeys = D == 128 ? 3 : 6, kValues = D == 128 ? 3 : 5;
+  // The loading warps of the other path work in teams, a tile to a team in turn: a team waits for its copies and announces them, the others' are
+  // under way.
   static constexpr uint32_t kTeams = D == 128 ? 2 : 4;
-  static constexpr uint32_t kOffKv = 2 * kTileBytes;
-  static constexpr uint32_t kOffMisc = kOffKv + kStages * kTileBytes;
+  static constexpr uint32_t kOffK = kQueries * kTileBytes, kOffV = kOffK + kKeys * kTileBytes;
+  static constexpr uint32_t kOffMisc = kOffV + kValues * kTileBytes;
   // misc: [0] dead flag, [4] tensor-memory base, barriers from 16 on
-  static constexpr uint32_t kBarKvFull = 16, kBarKvEmpty = kBarKvFull + 8 * kStages;
-  static constexpr uint32_t kBarQFull = kBarKvEmpty + 8 * kStages, kBarQEmpty = kBarQFull + 16;
-  static constexpr uint32_t kBarSFull = kBarQEmpty + 16, kBarPFull = kBarSFull + 16, kBarODone = kBarPFull + 16, kBarMl = kBarODone + 16;
+  static constexpr uint32_t kBarKFull = 16, kBarKEmpty = kBarKFull + 8 * kKeys, kBarVFull = kBarKEmpty + 8 * kKeys, kBarVEmpty = kBarVFull + 8 * kValues;
+  static constexpr uint32_t kBarQFull = kBarVEmpty + 8 * kValues, kBarQEmpty = kBarQFull + 8 * kQueries;
+  static constexpr uint32_t kBarSFull = kBarQEmpty + 8 * kQueries, kBarPFull = kBarSFull + 16, kBarODone = kBarPFull + 16, kBarMl = kBarODone + 16;
   static constexpr uint32_t kOffPlan = (kBarMl + 8 + 15) / 16 * 16;
   static constexpr uint32_t kOffThere = kOffPlan + 96;
   static constexpr uint32_t kOffMl = kOffThere + kThere * 16;
@@ -268,13 +271,19 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
   }
   if (threadIdx.x == 0) {
     *dead = 0u;
-    for (uint32_t i = 0; i < L::kStages; ++i) {
-      mbar_init(bar(L::kBarKvFull, i), TMA ? 2 : kLoadWarps / L::kTeams);
-      mbar_init(bar(L::kBarKvEmpty, i), 1);
+    for (uint32_t i = 0; i < L::kKeys; ++i) {
+      mbar_init(bar(L::kBarKFull, i), TMA ? 2 : kLoadWarps / L::kTeams);
+      mbar_init(bar(L::kBarKEmpty, i), 1);
     }
-    for (uint32_t i = 0; i < 2; ++i) {
+    for (uint32_t i = 0; i < L::kValues; ++i) {
+      mbar_init(bar(L::kBarVFull, i), TMA ? 2 : kLoadWarps / L::kTeams);
+      mbar_init(bar(L::kBarVEmpty, i), 1);
+    }
+    for (uint32_t i = 0; i < L::kQueries; ++i) {
       mbar_init(bar(L::kBarQFull, i), kQueryWarps);
       mbar_init(bar(L::kBarQEmpty, i), 1);
+    }
+    for (uint32_t i = 0; i < 2; ++i) {
       mbar_init(bar(L::kBarSFull, i), 2);  // the products' completion, and the issuing thread, which has seen the words of present states
       mbar_init(bar(L::kBarPFull, i), kSoftWarps);
       mbar_init(bar(L::kBarODone, i), 1);
@@ -340,7 +349,9 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         }
       }
     };
-    uint32_t st = values, round = 0, count = 0;
+    const uint32_t ring = values ? L::kValues : L::kKeys, offset = values ? L::kOffV : L::kOffK;
+    const uint32_t bar_full = values ? L::kBarVFull : L::kBarKFull, bar_empty = values ? L::kBarVEmpty : L::kBarKEmpty;
+    uint32_t st = 0, round = 0, count = 0;
     fetch();
     while (f_any && ok) {
       const uint32_t kvh = f_kvh, slot = f_slot, valid = f_valid;
@@ -361,21 +372,20 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         s_there[(count % kThere) * 4u + lane] = word;
       }
       ++count;
-      if (round) wait(bar(L::kBarKvEmpty, st), (round - 1u) & 1u);
+      if (round) wait(bar(bar_empty, st), (round - 1u) & 1u);
       if (!ok) break;
       // columns of 64 to a warp, or, where there are no more, boxes in turn
       const bool mine = L::kSlabs == 2u ? live : live && (lane & 1u) == part;
       const uint32_t slab = L::kSlabs == 2u ? part : 0u;
-      const uint32_t full = bar(L::kBarKvFull, st), dst = smem0 + L::kOffKv + st * L::kTileBytes + slab * kStates * 128u + lane * p.box * 128u;
+      const uint32_t full = bar(bar_full, st), dst = smem0 + offset + st * L::kTileBytes + slab * kStates * 128u + lane * p.box * 128u;
       const uint32_t bytes = (uint32_t)__popc(__ballot_sync(kFull, mine)) * p.box * 128u;
       __syncwarp();  // the words of present states are written
       if (lane == 0) mbar_expect_tx(full, bytes);
       __syncwarp();
       if (mine) tma_load_4d(dst, map, (int)(slab * 64u), (int)slot, (int)kvh, page, full);
       __syncwarp();
-      st += 2u;
-      if (st >= L::kStages) {
-        st -= L::kStages;
+      if (++st == ring) {
+        st = 0;
         ++round;
       }
     }
@@ -420,17 +430,10 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
     // A lane copies the same 16 bytes of rows lane / kChunks, + kAtOnce, ...: the swizzle turns the place in a row with the row's last three
     // bits, of which kAtOnce's own are the lane's and the others the loop's.
     const uint32_t c = lane % kChunks, r_mine = lane / kChunks;
-    const uint32_t place = smem0 + L::kOffKv + (c / 8u) * (kStates * 128u) + (s_mine + r_mine) * 128u + (((c % 8u) ^ r_mine) << 4);
+    const uint32_t place = smem0 + (c / 8u) * (kStates * 128u) + (s_mine + r_mine) * 128u + (((c % 8u) ^ r_mine) << 4);
     const char* const k_mine = reinterpret_cast<const char*>(p.k + c * 8u);
     const int64_t k_to_v = reinterpret_cast<const char*>(p.v) - reinterpret_cast<const char*>(p.k);
-    uint32_t st = 2u * team % L::kStages, round = 0, count = team;  // stage of the keys; tile
-    auto bump = [&](uint32_t& at, uint32_t& turn, uint32_t by) {
-      at += by;
-      if (at >= L::kStages) {
-        at -= L::kStages;
-        ++turn;
-      }
-    };
+    uint32_t count = team;  // tile
     fetch();
     while (f_any && ok) {
       int64_t off[kLanes];  // bytes
@@ -446,15 +449,14 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         there[i] = __ballot_sync(kFull, live);
       }
       fetch();
-      uint32_t v_st = st, v_round = round;
-      bump(v_st, v_round, 1u);
-      if (round) wait(bar(L::kBarKvEmpty, st), (round - 1u) & 1u);
-      if (v_round && ok) wait(bar(L::kBarKvEmpty, v_st), (v_round - 1u) & 1u);
+      const uint32_t k_round = count / L::kKeys, k_st = count - k_round * L::kKeys, v_round = count / L::kValues, v_st = count - v_round * L::kValues;
+      if (k_round) wait(bar(L::kBarKEmpty, k_st), (k_round - 1u) & 1u);
+      if (v_round && ok) wait(bar(L::kBarVEmpty, v_st), (v_round - 1u) & 1u);
       if (!ok) break;
 #pragma unroll
       for (uint32_t i = 0; i < kLanes; ++i) {
         if (lane == 0) s_there[(count % kThere) * 4u + s_mine / 32u + i] = there[i];
-        const uint32_t k_dst = place + st * L::kTileBytes + i * 4096u, v_dst = place + v_st * L::kTileBytes + i * 4096u;
+        const uint32_t k_dst = place + L::kOffK + k_st * L::kTileBytes + i * 4096u, v_dst = place + L::kOffV + v_st * L::kTileBytes + i * 4096u;
         auto copy = [&](bool all) {
 #pragma unroll
           for (uint32_t r0 = 0; r0 < 32u; r0 += kAtOnce) {
@@ -472,11 +474,9 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
       asm volatile("cp.async.wait_all;" ::: "memory");
       __syncwarp();
       if (lane == 0) {
-        mbar_arrive(bar(L::kBarKvFull, st));
-        mbar_arrive(bar(L::kBarKvFull, v_st));
+        mbar_arrive(bar(L::kBarKFull, k_st));
+        mbar_arrive(bar(L::kBarVFull, v_st));
       }
-      bump(st, round, 2u * kTeams % L::kStages);
-      round += 2u * kTeams / L::kStages;
       count += kTeams;
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
@@ -488,8 +488,8 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
     uint32_t count = 0;
     uint4 open = make_uint4(0u, 0u, 0u, 0u);  // the last group that begins in this share, the only one that can go on in the next
     for (; more(g) && ok; g.next(p)) {
-      const uint32_t qb = count & 1u;
-      if (count >= 2u) wait(bar(L::kBarQEmpty, qb), (count / 2u - 1u) & 1u);
+      const uint32_t qb = count % L::kQueries;
+      if (count >= L::kQueries) wait(bar(L::kBarQEmpty, qb), (count / L::kQueries - 1u) & 1u);
       if (!ok) break;
       const uint32_t rows = (uint32_t)min((uint64_t)kRows, (uint64_t)g.n * p.group - (uint64_t)g.rt * kRows);
       const uint32_t dst = smem0 + qb * L::kTileBytes + (c / 8u) * (kRows * 128u);
@@ -510,29 +510,24 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
   } else if (warp == kMmaWarp) {
     // ---- products ---------------------------------------------------------------------------------------
     // Scores of the next tile or the product of an earlier one with V, whichever is ready: up to two tiles' scores may wait for their p.
-    uint32_t st = 0, round = 0, done = 0, asked = 0, q_count = 0;  // stage of the next keys; tiles multiplied with V, tiles with scores
-    uint32_t v_st[2] = {0, 0}, v_round[2] = {0, 0}, v_flags[2] = {0, 0};  // of the tiles in between, by buffer: stage of their values; 1: not the group's first tile; states that are there << 8
+    uint32_t done = 0, asked = 0, q_count = 0;  // tiles multiplied with V, tiles with scores, groups
+    uint32_t k_st = 0, k_round = 0, v_st = 0, v_round = 0;
+    uint32_t flags[2] = {0, 0};  // of the tiles in between, by buffer: 1: not the group's first tile; states that are there << 8
     const uint32_t idesc_qk = umma_idesc(128, 128), idesc_pv = umma_idesc(128, D) | kIdescNMajorB;
-    const uint64_t q_desc = umma_desc(smem0), kv_desc = umma_desc(smem0 + L::kOffKv), v_desc = umma_desc_n_major(smem0 + L::kOffKv, kStates);
-    auto bump = [&]() {
-      if (++st == L::kStages) {
-        st = 0;
-        ++round;
-      }
-    };
+    const uint64_t q_desc = umma_desc(smem0), k_desc = umma_desc(smem0 + L::kOffK), v_desc = umma_desc_n_major(smem0 + L::kOffV, kStates);
     bool any = more(g);
     uint32_t t = any ? begin_of(g) : 0u, t0 = t, t1 = any ? end_of(g) : 0u;
     uint32_t idle = 0;
     while (ok && (any || done != asked)) {
       const uint32_t sb = done & 1u;
       // the tile's p times V, both halves of its states
-      if (done != asked && mbar_test(bar(L::kBarPFull, sb), (done >> 1) & 1u) && mbar_test(bar(L::kBarKvFull, v_st[sb]), v_round[sb] & 1u)) {
+      if (done != asked && mbar_test(bar(L::kBarPFull, sb), (done >> 1) & 1u) && mbar_test(bar(L::kBarVFull, v_st), v_round & 1u)) {
         idle = 0;
         if (TMA) {
-          const uint32_t valid = v_flags[sb] >> 8;
+          const uint32_t valid = flags[sb] >> 8;
           if (valid < kStates) {  // past the last state memory may hold anything, and 0 x NaN is NaN
             constexpr uint32_t kChunks = D / 8;
-            uint8_t* const tile = smem + L::kOffKv + v_st[sb] * L::kTileBytes;
+            uint8_t* const tile = smem + L::kOffV + v_st * L::kTileBytes;
             for (uint32_t i = lane; i < (kStates - valid) * kChunks; i += 32u) {
               const uint32_t r = valid + i / kChunks, c = i % kChunks;
               *reinterpret_cast<uint4*>(tile + (c / 8u) * (kStates * 128u) + r * 128u + (c % 8u) * 16u) = make_uint4(0, 0, 0, 0);
@@ -543,29 +538,33 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         tmem_fence_after();
         __syncwarp();
         if (elect_one()) {
-          const uint64_t b = v_desc + v_st[sb] * (L::kTileBytes >> 4);
+          const uint64_t b = v_desc + v_st * (L::kTileBytes >> 4);
 #pragma unroll
           for (uint32_t kk = 0; kk < kStates / 16u; ++kk) {
             const uint32_t w = kk / 4u;
             umma_bf16_ts(tmem + 2u * kStates + w * D, tmem + sb * kStates + w * kSide + (kk % 4u) * 8u, b + kk * (2048u >> 4), idesc_pv,
-                         (v_flags[sb] & 1u) | (kk % 4u));
+                         (flags[sb] & 1u) | (kk % 4u));
           }
           umma_commit(bar(L::kBarODone, sb));
-          umma_commit(bar(L::kBarKvEmpty, v_st[sb]));
+          umma_commit(bar(L::kBarVEmpty, v_st));
         }
         __syncwarp();
         ++done;
+        if (++v_st == L::kValues) {
+          v_st = 0;
+          ++v_round;
+        }
         continue;
       }
       // the next tile's scores, when the buffer's last p is spent
-      if (any && asked - done < 2u && mbar_test(bar(L::kBarKvFull, st), round & 1u) &&
-          (t != t0 || mbar_test(bar(L::kBarQFull, q_count & 1u), (q_count >> 1) & 1u))) {
+      if (any && asked - done < 2u && mbar_test(bar(L::kBarKFull, k_st), k_round & 1u) &&
+          (t != t0 || mbar_test(bar(L::kBarQFull, q_count % L::kQueries), (q_count / L::kQueries) & 1u))) {
         idle = 0;
-        const uint32_t qb = q_count & 1u, to = asked & 1u;
+        const uint32_t qb = q_count % L::kQueries, to = asked & 1u;
         copies_fence();
         tmem_fence_after();
         if (elect_one()) {
-          const uint64_t a = q_desc + qb * (L::kTileBytes >> 4), b = kv_desc + st * (L::kTileBytes >> 4);
+          const uint64_t a = q_desc + qb * (L::kTileBytes >> 4), b = k_desc + k_st * (L::kTileBytes >> 4);
 #pragma unroll
           for (uint32_t kk = 0; kk < D / 16; ++kk) {
             constexpr uint32_t kSlab = (kStates * 128u) >> 4;
@@ -573,23 +572,20 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
             umma_bf16(tmem + to * kStates, a + off, b + off, idesc_qk, kk != 0u);
           }
           umma_commit(bar(L::kBarSFull, to));
-          umma_commit(bar(L::kBarKvEmpty, st));
+          umma_commit(bar(L::kBarKEmpty, k_st));
           if (t + 1u == t1) umma_commit(bar(L::kBarQEmpty, qb));
           mbar_arrive(bar(L::kBarSFull, to));
         }
         __syncwarp();
-        bump();
-        const uint32_t flags = (t != t0 ? 1u : 0u) | (g.end > t * kStates ? min(kStates, g.end - t * kStates) << 8 : 0u);
-        if (to) {
-          v_st[1] = st;
-          v_round[1] = round;
-          v_flags[1] = flags;
-        } else {
-          v_st[0] = st;
-          v_round[0] = round;
-          v_flags[0] = flags;
+        if (++k_st == L::kKeys) {
+          k_st = 0;
+          ++k_round;
         }
-        bump();
+        const uint32_t f = (t != t0 ? 1u : 0u) | (g.end > t * kStates ? min(kStates, g.end - t * kStates) << 8 : 0u);
+        if (to)
+          flags[1] = f;
+        else
+          flags[0] = f;
         ++asked;
         if (++t == t1) {
           g.next(p);
@@ -662,7 +658,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
             for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], __uint_as_float(s[i + 2 * k]), __uint_as_float(s[i + 2 * k + 1]));
           }
           const float top = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]) * c;
-          if (__any_sync(kFull, top > m + kRescale)) {
+          if (__any_sync(kFull, live && top > m + kRescale)) {  // (what lies in a dead row must not decide for the others)
             const float mn = fmaxf(m, top), f = mn == -INFINITY ? 1.f : exp2_fast(m - mn);
             m = mn;
             l *= f;
