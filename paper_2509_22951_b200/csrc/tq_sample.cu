@@ -2,14 +2,21 @@
 // function at a given uniform number.
 //
 // Exact sums.  Every decision is a comparison of sums of weights w = 2^t, t = (x - max) log2(e) / temperature, with a bound: a
-// weight is therefore an integer W = round(2^40 w), and sums of up to 2^18 of them are exact in 64 bits whatever their
-// order.  t comes from one fp64 fused multiply-add onto 1.5 * 2^20, whose last bit is 2^-32: the low word of the result
-// is the fraction of t and the high word its integer part.  2^fraction = table[upper 8 bits] * (1 + q), q a cubic in the lower 24.
+// weight is therefore an integer W = round(2^45 w), and sums of up to 2^18 of them are exact in 64 bits whatever their
+// order, so that neither the split of a row nor the order of atomics can change a token.  t comes from one fp64 fused multiply-add onto
+// 1.5 * 2^20, whose last bit is 2^-32: the low word of the result is the fraction of t and the high word its integer part.  2^fraction =
+// table[upper 8 bits] * (1 + q), q a cubic in the lower 24, to 29 bits; W below 2^21 (t < -24) is taken from the fp32 exponential, to a unit or two.
 //
 // Order.  Tokens fall by (x, lower index first): as one integer, the logit's bits made to rise with it above the index turned
 // round.  What is kept is all that is not below a border in that order, so every filter is a search for its border.
 //
-// A row is read once: a cluster of up to eight CTAs holds it in shared memory.
+// A row is read once: a cluster of up to eight CTAs holds it in shared memory and speaks through distributed shared memory.  Then
+//   top-k (up to 1024): the k-th largest of the threads' own maxima is a bound of the k-th logit that few others pass: those go to one CTA in
+//          the order of the vocabulary, which sorts them and does the rest;
+//   top-p alone: a histogram of the weights over 64 bins an octave (exact: two integers a bin) finds the bin of the border, whose
+//          tokens one CTA sorts; then every CTA adds up what it keeps;
+//   neither, or min-p alone: the border is known; every CTA adds up what it keeps.
+// Where so many logits are alike that a list does not hold them (2048), and for larger k, the border is found by bisection of the order.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -27,9 +34,14 @@ constexpr uint32_t kMaxCluster = 8;
 constexpr uint32_t kIndexBits = 18;
 static_assert((1u << kIndexBits) == TQ_SAMPLE_MAX_VOCAB, "a token's index fits its place in the order");
 constexpr uint32_t kIndexMask = (1u << kIndexBits) - 1u;
-constexpr int kOne = 40;  // W of the largest logit is 2^40
+constexpr int kOne = 45;     // W of the largest logit is 2^45
+constexpr int kOctaves = 24; // of the histogram, and of the weights that are computed to 29 bits
+constexpr uint32_t kBins = kOctaves * 64u;
+constexpr uint32_t kList = 2048;   // tokens that one CTA sorts
+constexpr uint32_t kListK = 1024;  // largest k of the list: the threads' maxima bound it well up to a quarter of their number
+constexpr uint32_t kKBins = 256;   // of the threads' maxima
 
-// 2^(i / 256) with 30 bits behind the point
+// 2^(i / 256) with 29 bits behind the point
 struct Powers {
   uint32_t v[256];
 };
@@ -42,7 +54,7 @@ constexpr Powers powers() {
       term *= y / k;
       sum += term;
     }
-    p.v[i] = (uint32_t)(sum * 1073741824.0 + 0.5);
+    p.v[i] = (uint32_t)(sum * 536870912.0 + 0.5);
   }
   return p;
 }
@@ -59,12 +71,22 @@ struct SampleParams {
   int32_t* token;
   float* logprob;
   uint32_t vocab, slice;  // slice: logits of a CTA
+  uint32_t vectors;       // rows may be read 16 bytes at a time
 };
 
 struct Shared {
-  uint64_t slots[2][kMaxCluster];  // what the cluster's CTAs tell one another; two sets, used in turn
-  uint64_t warps[2][kWarps];
+  uint64_t slots[2][kMaxCluster][2];  // what the cluster's CTAs tell one another; two sets, used in turn
+  uint64_t warps[2][kWarps][2];
+  uint64_t told[2];                   // by one CTA to all
   uint32_t powers[256];
+  uint32_t listed;                    // tokens in the list (of the first CTA)
+  union {
+    struct {
+      uint32_t hi[kBins], lo[kBins];  // sums of the upper and lower 15 bits of the weights of a bin
+    } bins;
+    uint64_t list[kList];
+    uint32_t k_bins[kKBins];
+  };
 };
 
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -80,10 +102,23 @@ __device__ __forceinline__ uint32_t cluster_size() {
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ void store_remote(uint64_t* at, uint32_t rank, uint64_t v) {
+__device__ __forceinline__ uint32_t at_rank(const void* ptr, uint32_t rank) {
   uint32_t a;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(tq_sm100::smem_u32(at)), "r"(rank));
-  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(v) : "memory");
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(tq_sm100::smem_u32(ptr)), "r"(rank));
+  return a;
+}
+__device__ __forceinline__ void store_remote(const uint64_t* ptr, uint32_t rank, uint64_t v) {
+  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(at_rank(ptr, rank)), "l"(v) : "memory");
+}
+__device__ __forceinline__ uint32_t load_remote(const uint32_t* ptr, uint32_t rank) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at_rank(ptr, rank)) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t add_remote(uint32_t* ptr, uint32_t rank, uint32_t v) {
+  uint32_t old;
+  asm volatile("atom.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(old) : "r"(at_rank(ptr, rank)), "r"(v) : "memory");
+  return old;
 }
 
 // Bits that rise with the number (no NaN, no -0).
@@ -91,109 +126,249 @@ __device__ __forceinline__ uint32_t rising(float x) {
   const uint32_t b = __float_as_uint(x);
   return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
+__device__ __forceinline__ float from_rising(uint32_t r) { return __uint_as_float(r ^ (r >> 31 ? 0x80000000u : 0xFFFFFFFFu)); }
 __device__ __forceinline__ uint64_t order_of(float x, uint32_t index) { return ((uint64_t)rising(x) << kIndexBits) | (kIndexMask - index); }
 
 struct Weights {
-  float top, c32;  // largest logit; log2(e) / temperature
+  float top, c32, c32_low;  // largest logit; log2(e) / temperature in two parts
   double c;
   const uint32_t* powers;
 
-  __device__ __forceinline__ uint64_t operator()(float x) const {
-    if (x == top) return 1ull << kOne;
-    if (x == -INFINITY || top == INFINITY || (x - top) * c32 < -42.f) return 0ull;  // below half a unit
+  // t in fp32; NaN for the largest logit where log2(e) / temperature overflows, and where it is 0 and the distance overflows (fine() knows both)
+  __device__ __forceinline__ float coarse(float x) const {
+    const float d = x - top, t = d * c32;
+    return t > -64.f ? fmaf(d, c32, d * c32_low) : t;
+  }
+  __device__ __forceinline__ bool none(float x) const { return x == -INFINITY || (top == INFINITY && x != top); }
+  // Octave n <= -1 (t = n + fraction) and the value of W = value << max(0, 16 + n): 29 bits of 2^fraction, or W itself below octave -16.
+  __device__ __forceinline__ uint32_t fine(float x, int& n, uint32_t& f) const {
     const double z = fma((double)x - (double)top, c, 1572864.0);  // 1.5 * 2^20
-    const int n = min(0, __double2hiint(z) - 0x41380000);         // t = n + fraction
-    const uint32_t f = (uint32_t)__double2loint(z);
+    n = __double2hiint(z) - 0x41380000;
+    f = (uint32_t)__double2loint(z);
+    if (x == top || n >= 0) {  // 2^30 in octave -1
+      n = -1;
+      f = 0xFFFFFFFFu;
+      return 1u << 30;
+    }
     const uint32_t base = powers[f >> 24];
     const float r = __uint_as_float(0x3F800000u | ((f & 0xFFFFFFu) >> 1)) - 1.0f;  // the lower 24 bits, 0 .. 1
     constexpr float a1 = 2.7076061740622863e-3f, a2 = 3.6655656e-6f, a3 = 3.3082868e-9f;  // (ln 2 / 256)^k / k!
     const float q = r * fmaf(r, fmaf(r, a3, a2), a1);
-    const uint32_t add = __float_as_uint(fmaf((float)base, q, 8388608.0f)) - 0x4B000000u;  // rounded to whole units of 2^-30
-    const uint64_t v = (uint64_t)(base + add);
-    const int up = kOne - 30 + n;
-    const uint64_t w = up >= 0 ? v << up : (v + (1ull << (-up - 1))) >> -up;
-    return n == 0 ? 1ull << kOne : w;  // t rounded to 0
+    const uint32_t v = base + (__float_as_uint(fmaf((float)base, q, 8388608.0f)) - 0x4B000000u);  // rounded to whole units of 2^-29
+    const int down = -16 - n;
+    return down > 0 ? (v + (1u << (down - 1))) >> down : v;
+  }
+  __device__ __forceinline__ static int shift(int n) { return max(0, 16 + n); }
+  // Octaves below the histogram's.
+  __device__ __forceinline__ uint32_t small(float t) const {
+    float w;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(w) : "f"(t + (float)kOne));
+    return t < -46.f ? 0u : __float2uint_rn(w);
+  }
+  __device__ __forceinline__ uint64_t operator()(float x) const {
+    if (none(x)) return 0ull;
+    const float t = coarse(x);
+    if (t < -(float)kOctaves) return small(t);
+    int n;
+    uint32_t f;
+    const uint32_t v = fine(x, n, f);
+    return (uint64_t)v << shift(n);
   }
 };
+__device__ __forceinline__ uint32_t bin_of(int n, uint32_t f) { return min((uint32_t)(-n - 1) * 64u + (63u - (f >> 26)), kBins - 1u); }
+
+// Sorts list[0 .. n), n <= kList, from the largest down: by every entry's rank where there are few, else bitonic.
+__device__ void sort_list(uint64_t* list, uint32_t n, uint32_t tid) {
+  if (n <= 128u) {
+    const uint64_t mine = tid < n ? list[tid] : 0ull;
+    uint32_t rank = 0;
+    if (tid < n)
+      for (uint32_t i = 0; i < n; ++i) rank += list[i] > mine ? 1u : 0u;
+    __syncthreads();
+    if (tid < n) list[rank] = mine;
+    __syncthreads();
+    return;
+  }
+  uint32_t size = 256;
+  while (size < n) size *= 2u;
+  for (uint32_t i = n + tid; i < size; i += kThreads) list[i] = 0ull;
+  __syncthreads();
+  for (uint32_t k = 2; k <= size; k *= 2u) {
+    for (uint32_t j = k / 2u; j > 0; j /= 2u) {
+      for (uint32_t i = tid; i < size / 2u; i += kThreads) {
+        const uint32_t a = 2u * i - (i & (j - 1u)), b = a + j;
+        const uint64_t x = list[a], y = list[b];
+        if ((x < y) == ((a & k) == 0u)) {
+          list[a] = y;
+          list[b] = x;
+        }
+      }
+      __syncthreads();
+    }
+  }
+}
 
 template <int TYPE>
-__global__ void __launch_bounds__(kThreads) sample_kernel(const SampleParams p) {
+__global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams p) {
   extern __shared__ __align__(16) uint8_t smem[];
   Shared& sh = *reinterpret_cast<Shared*>(smem);
-  float* const xs = reinterpret_cast<float*>(smem + sizeof(Shared));
+  float* const xs = reinterpret_cast<float*>(smem + (sizeof(Shared) + 15u) / 16u * 16u);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u, rank = cluster_rank(), ctas = cluster_size();
   const uint32_t row = blockIdx.x / ctas, from = min(rank * p.slice, p.vocab), n = min(p.slice, p.vocab - from);
   if (tid < 256) sh.powers[tid] = kPowers.v[tid];
+  if (tid == 0) sh.listed = 0u;
   asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
 
   uint32_t turn = 0;
-  // Adds (or takes the largest of) every thread's value over the cluster; of[r]: what CTA r had.
-  auto all = [&](uint64_t v, bool largest, uint64_t (&of)[kMaxCluster]) -> uint64_t {
+  // Two numbers of every thread added up (or the largest taken) over the CTA, then told to the whole cluster: of[r] is what CTA r had.
+  // warps[turn] keeps what the warps had.
+  auto all2 = [&](uint64_t& v0, uint64_t& v1, bool largest, uint64_t (&of0)[kMaxCluster]) {
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) {
-      const uint64_t o = __shfl_xor_sync(kFull, v, d);
-      v = largest ? (o > v ? o : v) : v + o;
+      const uint64_t a = __shfl_xor_sync(kFull, v0, d), b = __shfl_xor_sync(kFull, v1, d);
+      v0 = largest ? (a > v0 ? a : v0) : v0 + a;
+      v1 = largest ? (b > v1 ? b : v1) : v1 + b;
     }
-    if (lane == 0) sh.warps[turn][warp] = v;
+    if (lane == 0) {
+      sh.warps[turn][warp][0] = v0;
+      sh.warps[turn][warp][1] = v1;
+    }
     __syncthreads();
     if (warp == 0) {
-      v = lane < kWarps ? sh.warps[turn][lane] : 0ull;
+      v0 = lane < kWarps ? sh.warps[turn][lane][0] : 0ull;
+      v1 = lane < kWarps ? sh.warps[turn][lane][1] : 0ull;
 #pragma unroll
-      for (int d = 16; d > 0; d >>= 1) {
-        const uint64_t o = __shfl_xor_sync(kFull, v, d);
-        v = largest ? (o > v ? o : v) : v + o;
+      for (int d = 8; d > 0; d >>= 1) {
+        const uint64_t a = __shfl_xor_sync(kFull, v0, d), b = __shfl_xor_sync(kFull, v1, d);
+        v0 = largest ? (a > v0 ? a : v0) : v0 + a;
+        v1 = largest ? (b > v1 ? b : v1) : v1 + b;
       }
-      if (lane < ctas) store_remote(&sh.slots[turn][rank], lane, v);
+      v0 = __shfl_sync(kFull, v0, 0);
+      v1 = __shfl_sync(kFull, v1, 0);
+      if (lane < ctas) {
+        store_remote(&sh.slots[turn][rank][0], lane, v0);
+        store_remote(&sh.slots[turn][rank][1], lane, v1);
+      }
     }
     cluster_sync();
-    uint64_t r = 0;
+    v0 = v1 = 0;
+#pragma unroll
     for (uint32_t i = 0; i < kMaxCluster; ++i) {
-      of[i] = i < ctas ? sh.slots[turn][i] : 0ull;
-      r = largest ? (of[i] > r ? of[i] : r) : r + of[i];
+      of0[i] = i < ctas ? sh.slots[turn][i][0] : 0ull;
+      const uint64_t b = i < ctas ? sh.slots[turn][i][1] : 0ull;
+      v0 = largest ? (of0[i] > v0 ? of0[i] : v0) : v0 + of0[i];
+      v1 = largest ? (b > v1 ? b : v1) : v1 + b;
     }
     turn ^= 1u;
-    return r;
   };
   uint64_t of[kMaxCluster];
 
-  // ---- the row, and its first token in falling order -----------------------------------------------
-  uint64_t best = 0;
-  for (uint32_t i = tid; i < n; i += kThreads) {
-    float x = load1<TYPE>(p.logits, (size_t)((int64_t)row * p.row_stride) + from + i);
+  // ---- the row; its first token in falling order; the largest logit of every thread ------------------------
+  float mine = -INFINITY;
+  uint32_t mine_at = 0;
+  auto take = [&](float x, uint32_t i) {
     x = x != x ? -INFINITY : x + 0.f;  // -0 is 0
-    xs[i] = x;
-    const uint64_t o = order_of(x, from + i);
-    best = o > best ? o : best;
+    if (x > mine) {
+      mine = x;
+      mine_at = i;
+    }
+    return x;
+  };
+  const size_t row_at = (size_t)((int64_t)row * p.row_stride) + from;
+  if (p.vectors) {
+    constexpr uint32_t kPer = TYPE == TQ_TYPE_F32 ? 4 : 8;
+    const uint32_t whole = n / kPer;
+    const uint8_t* const src = (const uint8_t*)p.logits + row_at * (TYPE == TQ_TYPE_F32 ? 4 : 2);
+#pragma unroll 1
+    for (uint32_t i0 = tid; i0 < whole; i0 += 8u * kThreads) {
+      uint4 v[8];
+#pragma unroll
+      for (uint32_t k = 0; k < 8u; ++k)
+        if (i0 + k * kThreads < whole) v[k] = load_once(src + (size_t)(i0 + k * kThreads) * 16u);
+#pragma unroll
+      for (uint32_t k = 0; k < 8u; ++k) {
+        const uint32_t i = i0 + k * kThreads;
+        if (i >= whole) break;
+        const uint32_t at = i * kPer;
+        if constexpr (TYPE == TQ_TYPE_F32) {
+          float4 y;
+          y.x = take(__uint_as_float(v[k].x), at);
+          y.y = take(__uint_as_float(v[k].y), at + 1u);
+          y.z = take(__uint_as_float(v[k].z), at + 2u);
+          y.w = take(__uint_as_float(v[k].w), at + 3u);
+          *reinterpret_cast<float4*>(xs + at) = y;
+        } else {
+          float4 y, z;
+          y.x = take(bf16_lo(v[k].x), at);
+          y.y = take(bf16_hi(v[k].x), at + 1u);
+          y.z = take(bf16_lo(v[k].y), at + 2u);
+          y.w = take(bf16_hi(v[k].y), at + 3u);
+          z.x = take(bf16_lo(v[k].z), at + 4u);
+          z.y = take(bf16_hi(v[k].z), at + 5u);
+          z.z = take(bf16_lo(v[k].w), at + 6u);
+          z.w = take(bf16_hi(v[k].w), at + 7u);
+          *reinterpret_cast<float4*>(xs + at) = y;
+          *reinterpret_cast<float4*>(xs + at + 4u) = z;
+        }
+      }
+    }
+    for (uint32_t i = whole * kPer + tid; i < n; i += kThreads) xs[i] = take(load1<TYPE>(p.logits, row_at + i), i);
+  } else {
+    for (uint32_t i = tid; i < n; i += kThreads) xs[i] = take(load1<TYPE>(p.logits, row_at + i), i);
   }
   asm volatile("barrier.cluster.wait.aligned;" ::: "memory");  // every CTA of the cluster runs: its shared memory can be written
-  best = all(best, true, of);
-  const uint32_t first = kIndexMask - (uint32_t)(best & kIndexMask);
-  const uint32_t bits = (uint32_t)(best >> kIndexBits);
-  const float top = __uint_as_float(bits ^ (bits >> 31 ? 0x80000000u : 0xFFFFFFFFu));
+  uint64_t best = mine > -INFINITY ? order_of(mine, from + mine_at) : 0ull;
+  uint64_t lowest = mine > -INFINITY ? (uint64_t)~rising(mine) : 0ull;  // the least of the threads' maxima, turned round
+  all2(best, lowest, true, of);
   const float temperature = p.temperature ? p.temperature[row] : 1.f;
-  if (top == -INFINITY || !(temperature > 0.f)) {
+  if (best == 0ull || !(temperature > 0.f)) {
     if (rank == 0 && tid == 0) {
-      p.token[row] = top == -INFINITY ? -1 : (int32_t)first;
-      if (p.logprob) p.logprob[row] = top == -INFINITY ? -INFINITY : 0.f;
+      p.token[row] = best == 0ull ? -1 : (int32_t)(kIndexMask - (uint32_t)(best & kIndexMask));
+      if (p.logprob) p.logprob[row] = best == 0ull ? -INFINITY : 0.f;
     }
     return;
   }
+  const float top = from_rising((uint32_t)(best >> kIndexBits));
   Weights weight;
   weight.top = top;
   weight.c = 1.4426950408889634074 / (double)temperature;
   weight.c32 = (float)weight.c;
+  weight.c32_low = (float)(weight.c - (double)weight.c32);
+  if (!(fabsf(weight.c32) < INFINITY)) weight.c32_low = 0.f;
   weight.powers = sh.powers;
 
-  // Weight (or number) of the tokens that stand before `order`.
+  const int32_t k_given = p.top_k ? p.top_k[row] : 0;
+  const uint32_t k = k_given > 0 && (uint32_t)k_given < p.vocab ? (uint32_t)k_given : 0u;
+  const float top_p = p.top_p ? p.top_p[row] : 1.f, min_p = p.min_p ? p.min_p[row] : 0.f;
+  const float u = p.uniform[row];
+  uint64_t keep = 0;  // tokens at or after this are kept
+  if (min_p > 0.f) {
+    const double edge = (double)top + (double)temperature * log((double)min_p);
+    const float x = min_p >= 1.f || top == INFINITY ? top : fminf(__double2float_ru(edge), top);
+    keep = (uint64_t)rising(x + 0.f) << kIndexBits;
+  }
+  auto target_of = [&](uint64_t total) {
+    const uint64_t y = (uint64_t)((u > 0.f ? (double)u : 0.0) * (double)total);
+    return y < total ? y : total - 1u;
+  };
+  auto answer = [&](uint32_t index, float x, uint64_t total) {
+    p.token[row] = (int32_t)index;
+    if (p.logprob) {
+      const double t = x == top ? 0.0 : ((double)x - (double)top) / (double)temperature;
+      p.logprob[row] = (float)(t - (log((double)total) - kOne * 0.69314718055994530942));
+    }
+  };
+
+  // Bisection of the order: the last place before which less than `bound` (a weight, or a number) lies.
   auto before = [&](uint64_t order, bool count) {
-    uint64_t v = 0;
+    uint64_t v = 0, zero = 0;
     for (uint32_t i = tid; i < n; i += kThreads)
       if (order_of(xs[i], from + i) > order) v += count ? 1ull : weight(xs[i]);
-    return all(v, false, of);
+    all2(v, zero, false, of);
+    return v;
   };
-  // The last place in the order before which less than `bound` lies.
   auto border = [&](double bound, bool count, uint64_t lo) {
     uint64_t hi = best;  // nothing is before it
     while (lo < hi) {
@@ -205,39 +380,276 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleParams p) 
     }
     return hi;
   };
-
-  uint64_t keep = 0;  // tokens at or after this are kept
-  const int32_t k = p.top_k ? p.top_k[row] : 0;
-  if (k > 0 && (uint32_t)k < p.vocab) keep = border((double)k, true, keep);
-  const float top_p = p.top_p ? p.top_p[row] : 1.f;
-  if (top_p < 1.f) {
-    const uint64_t sum = before(keep ? keep - 1u : 0u, false);  // 0 is no token's place
-    keep = border((double)top_p * (double)sum, false, keep);
-  }
-  const float min_p = p.min_p ? p.min_p[row] : 0.f;
-  if (min_p > 0.f) {
-    const double edge = (double)top + (double)temperature * log((double)min_p);
-    const float x = min_p >= 1.f || top == INFINITY ? top : fminf(__double2float_ru(edge), top);
-    const uint64_t o = (uint64_t)rising(x + 0.f) << kIndexBits;
-    keep = o > keep ? o : keep;
-    keep = keep > best ? best : keep;
-  }
-
-  // ---- the token up to which more than u of the kept sum lies ---------------------------------------
   // warps own consecutive pieces of the slice
   const uint32_t piece = (n + kThreads - 1u) / kThreads * 32u, w0 = min(warp * piece, n), w1 = min(w0 + piece, n);
-  auto kept = [&](uint32_t i) { return order_of(xs[i], from + i) >= keep ? weight(xs[i]) : 0ull; };
-  uint64_t mine = 0;
-  for (uint32_t i = w0 + lane; i < w1; i += 32u) mine += kept(i);
+  const bool p_on = top_p < 1.f;
+  bool searched = !p_on && k == 0u;  // the border is known
+
+  if (!searched && k != 0u && k <= kListK) {
+    // ---- top-k: a bound from the threads' maxima, and a list -----------------------------------------------
+    for (uint32_t i = tid; i < kKBins; i += kThreads) sh.k_bins[i] = 0u;
+    __syncthreads();
+    const float low = from_rising(~(uint32_t)lowest), span = top - low;
+    // bins fall with x; equal logits, and infinite ones, are all in the first
+    const float scale = span > 0.f && span < INFINITY ? (float)(kKBins - 1u) / span : 0.f;
+    auto k_bin = [&](float x) { return scale == 0.f ? (x == top || span < INFINITY ? 0u : kKBins - 1u) : min((uint32_t)((top - x) * scale), kKBins - 1u); };
+    if (mine > -INFINITY) atomicAdd(&sh.k_bins[k_bin(mine)], 1u);
+    cluster_sync();
+    uint32_t in_bin = 0;
+    if (tid < kKBins)
+      for (uint32_t r = 0; r < ctas; ++r) in_bin += load_remote(&sh.k_bins[tid], r);
+    uint32_t upto = in_bin;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const uint32_t o = __shfl_up_sync(kFull, upto, d);
+      if (lane >= (uint32_t)d) upto += o;
+    }
+    if (lane == 31) sh.warps[turn][warp][0] = upto;
+    __syncthreads();
+    uint32_t earlier = 0;
+    for (uint32_t i = 0; i < min(warp, kKBins / 32u); ++i) earlier += (uint32_t)sh.warps[turn][i][0];
+    upto += earlier;
+    if (tid == 0) sh.told[0] = kKBins - 1u;  // fewer maxima than k: nothing is left out
+    __syncthreads();
+    if (tid < kKBins && upto >= k && upto - in_bin < k) sh.told[0] = tid;
+    __syncthreads();
+    const uint32_t cut = (uint32_t)sh.told[0];
+    auto listed = [&](float x) { return x > -INFINITY && k_bin(x) <= cut; };
+    uint32_t count = 0;
+    for (uint32_t i = w0 + lane; i < w1; i += 32u) count += listed(xs[i]) ? 1u : 0u;
+    uint64_t v = count, zero = 0;
+    const uint32_t last = turn;
+    all2(v, zero, false, of);  // (also: every CTA has read the bins, the list may lie over them)
+    if (v <= kList) {
+      // the list in the order of the vocabulary, in the first CTA
+      uint32_t at = 0;
+      for (uint32_t i = 0; i < rank; ++i) at += (uint32_t)of[i];
+      for (uint32_t i = 0; i < warp; ++i) at += (uint32_t)sh.warps[last][i][0];
+      for (uint32_t i0 = w0; i0 < w1; i0 += 32u) {
+        const uint32_t i = i0 + lane;
+        const bool yes = i < w1 && listed(xs[i]);
+        const uint32_t votes = __ballot_sync(kFull, yes);
+        if (yes) store_remote(&sh.list[at + __popc(votes & ((1u << lane) - 1u))], 0u, order_of(xs[i], from + i));
+        at += __popc(votes);
+      }
+      cluster_sync();
+      if (rank != 0) return;
+      const uint32_t m = (uint32_t)v;
+      constexpr uint32_t kEach = kList / kThreads;  // consecutive entries of a thread
+      uint64_t own[kEach];                          // in the order of the vocabulary
+#pragma unroll
+      for (uint32_t i = 0; i < kEach; ++i) own[i] = tid * kEach + i < m ? sh.list[tid * kEach + i] : 0ull;
+      __syncthreads();
+      sort_list(sh.list, m, tid);
+      // sums of weights over the threads' entries, and what is before them
+      auto scan = [&](uint64_t sum, uint64_t& total) {
+        uint64_t incl = sum;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const uint64_t o = __shfl_up_sync(kFull, incl, d);
+          if (lane >= (uint32_t)d) incl += o;
+        }
+        __syncthreads();
+        if (lane == 31) sh.warps[0][warp][0] = incl;
+        __syncthreads();
+        total = 0;
+        uint64_t prev = 0;
+        for (uint32_t i = 0; i < kWarps; ++i) {
+          const uint64_t o = sh.warps[0][i][0];
+          prev += i < warp ? o : 0ull;
+          total += o;
+        }
+        return prev + incl - sum;
+      };
+      uint32_t kept = min(k, m);
+      if (p_on) {
+        uint64_t w[kEach], sum = 0, total;
+#pragma unroll
+        for (uint32_t i = 0; i < kEach; ++i) {
+          const uint32_t j = tid * kEach + i;
+          w[i] = j < kept ? weight(from_rising((uint32_t)(sh.list[j] >> kIndexBits))) : 0ull;
+          sum += w[i];
+        }
+        uint64_t prev = scan(sum, total);
+        const double bound = (double)top_p * (double)total;
+        uint32_t in = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < kEach; ++i) {
+          in += tid * kEach + i < kept && (double)prev < bound ? 1u : 0u;
+          prev += w[i];
+        }
+        uint64_t sum_in;
+        scan(in, sum_in);
+        kept = max(1u, (uint32_t)sum_in);
+      }
+      const uint64_t edge = sh.list[kept - 1u];
+      keep = min(max(keep, edge), best);
+      uint64_t w[kEach], sum = 0, total;
+#pragma unroll
+      for (uint32_t i = 0; i < kEach; ++i) {
+        w[i] = own[i] != 0ull && own[i] >= keep ? weight(from_rising((uint32_t)(own[i] >> kIndexBits))) : 0ull;
+        sum += w[i];
+      }
+      uint64_t prev = scan(sum, total);
+      const uint64_t target = target_of(total);
+      if (target >= prev && target < prev + sum) {
+#pragma unroll
+        for (uint32_t i = 0; i < kEach; ++i) {
+          if (target >= prev && target < prev + w[i])
+            answer(kIndexMask - (uint32_t)(own[i] & kIndexMask), from_rising((uint32_t)(own[i] >> kIndexBits)), total);
+          prev += w[i];
+        }
+      }
+      return;
+    }
+  }
+  if (!searched && k == 0u) {
+    // ---- top-p: a histogram of the weights, and a list of the bin with the border -----------------------------
+    for (uint32_t i = tid; i < kBins; i += kThreads) sh.bins.hi[i] = sh.bins.lo[i] = 0u;
+    __syncthreads();
+    uint64_t rest = 0;  // of the octaves below
+    for (uint32_t i = tid; i < n; i += kThreads) {
+      const float x = xs[i];
+      if (weight.none(x)) continue;
+      const float t = weight.coarse(x);
+      if (t < -(float)kOctaves) {
+        rest += weight.small(t);
+        continue;
+      }
+      int o;
+      uint32_t f;
+      const uint32_t v = weight.fine(x, o, f), b = bin_of(o, f);
+      atomicAdd(&sh.bins.hi[b], v >> 15);
+      atomicAdd(&sh.bins.lo[b], v & 0x7FFFu);
+    }
+    cluster_sync();
+    // this CTA's bins of all CTAs: kBins / ctas consecutive ones, up to three to a thread
+    const uint32_t share = kBins / ctas, each = (share + kThreads - 1u) / kThreads, first = rank * share + tid * each;
+    uint64_t mass[3] = {0, 0, 0}, sum = 0;
+    for (uint32_t j = 0; j < each; ++j) {
+      if (tid * each + j >= share) break;
+      uint64_t hi = 0, lo = 0;
+      for (uint32_t r = 0; r < ctas; ++r) {
+        hi += load_remote(&sh.bins.hi[first + j], r);
+        lo += load_remote(&sh.bins.lo[first + j], r);
+      }
+      const uint64_t m = ((hi << 15) + lo) << Weights::shift(-1 - (int)((first + j) / 64u));
+      if (j == 0) mass[0] = m;
+      if (j == 1) mass[1] = m;
+      if (j == 2) mass[2] = m;
+      sum += m;
+    }
+    uint64_t total = sum, all_rest = rest;
+    const uint32_t last = turn;
+    uint64_t incl = sum;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const uint64_t o = __shfl_up_sync(kFull, incl, d);
+      if (lane >= (uint32_t)d) incl += o;
+    }
+    if (tid == 0) sh.told[0] = ~0ull;
+    all2(total, all_rest, false, of);
+    const double bound = (double)top_p * (double)(total + all_rest);
+    uint64_t prev = incl - sum;
+    for (uint32_t i = 0; i < rank; ++i) prev += of[i];
+    for (uint32_t i = 0; i < warp; ++i) prev += sh.warps[last][i][0];
+    if (0.0 < bound) {
+#pragma unroll
+      for (uint32_t j = 0; j < 3u; ++j) {
+        if (j < each && mass[j] != 0ull && (double)prev < bound && (double)(prev + mass[j]) >= bound) {
+          for (uint32_t r = 0; r < ctas; ++r) {
+            store_remote(&sh.told[0], r, first + j);
+            store_remote(&sh.told[1], r, prev);
+          }
+        }
+        prev += mass[j];
+      }
+    }
+    cluster_sync();  // (also: every CTA has read the bins, the list may lie over them)
+    const uint64_t bin = sh.told[0], ahead = sh.told[1];
+    if (!(0.0 < bound)) {
+      keep = best;
+      searched = true;
+    } else if (bin != ~0ull) {
+      for (uint32_t i0 = 0; i0 < n; i0 += kThreads) {
+        const uint32_t i = i0 + tid;
+        bool yes = false;
+        if (i < n && !weight.none(xs[i]) && !(weight.coarse(xs[i]) < -(float)kOctaves)) {
+          int o;
+          uint32_t f;
+          weight.fine(xs[i], o, f);
+          yes = bin_of(o, f) == (uint32_t)bin;
+        }
+        const uint32_t votes = __ballot_sync(kFull, yes);
+        if (votes == 0u) continue;
+        uint32_t at = 0;
+        if (lane == 0) at = add_remote(&sh.listed, 0u, __popc(votes));
+        at = __shfl_sync(kFull, at, 0) + __popc(votes & ((1u << lane) - 1u));
+        if (yes && at < kList) store_remote(&sh.list[at], 0u, order_of(xs[i], from + i));
+      }
+      cluster_sync();
+      const uint32_t m = load_remote(&sh.listed, 0u);
+      if (m <= kList) {
+        if (rank == 0) {
+          sort_list(sh.list, m, tid);
+          // the last entry before which less than the bound lies
+          constexpr uint32_t kEach = kList / kThreads;
+          uint64_t w[kEach], sum = 0, incl;
+#pragma unroll
+          for (uint32_t i = 0; i < kEach; ++i) {
+            const uint32_t j = tid * kEach + i;
+            w[i] = j < m ? weight(from_rising((uint32_t)(sh.list[j] >> kIndexBits))) : 0ull;
+            sum += w[i];
+          }
+          incl = sum;
+#pragma unroll
+          for (int d = 1; d < 32; d <<= 1) {
+            const uint64_t o = __shfl_up_sync(kFull, incl, d);
+            if (lane >= (uint32_t)d) incl += o;
+          }
+          if (lane == 31) sh.warps[turn][warp][0] = incl;
+          __syncthreads();
+          uint64_t prev = ahead + incl - sum;
+          for (uint32_t i = 0; i < warp; ++i) prev += sh.warps[turn][i][0];
+#pragma unroll
+          for (uint32_t i = 0; i < kEach; ++i) {
+            const uint32_t j = tid * kEach + i;
+            if (j < m && (double)prev < bound && (j + 1u == m || (double)(prev + w[i]) >= bound)) {
+              for (uint32_t r = 0; r < ctas; ++r) store_remote(&sh.told[0], r, sh.list[j]);
+            }
+            prev += w[i];
+          }
+          __syncthreads();
+        }
+        cluster_sync();
+        keep = min(max(keep, sh.told[0]), best);
+        searched = true;
+      }
+    }
+  }
+  if (!searched) {
+    uint64_t edge = 0;
+    if (k != 0u) edge = border((double)k, true, 0ull);
+    if (p_on) {
+      const uint64_t sum = before(edge ? edge - 1u : 0u, false);  // 0 is no token's place
+      edge = border((double)top_p * (double)sum, false, edge);
+    }
+    keep = max(keep, edge);
+  }
+  keep = min(keep, best);
+
+  // ---- the token up to which more than u of the kept sum lies ---------------------------------------
+  const float keep_x = from_rising((uint32_t)(keep >> kIndexBits));  // below it nothing is kept
+  auto kept = [&](uint32_t i) { return !(xs[i] < keep_x) && order_of(xs[i], from + i) >= keep ? weight(xs[i]) : 0ull; };
+  uint64_t sum_mine = 0, zero = 0;
+  for (uint32_t i = w0 + lane; i < w1; i += 32u) sum_mine += kept(i);
   const uint32_t last = turn;
-  const uint64_t total = all(mine, false, of);
-  const float u = p.uniform[row];
-  uint64_t target = (uint64_t)((u > 0.f ? (double)u : 0.0) * (double)total);
-  target = target < total ? target : total - 1u;
+  all2(sum_mine, zero, false, of);
+  const uint64_t total = sum_mine, target = target_of(total);
   uint64_t sum = 0;
   for (uint32_t i = 0; i < rank; ++i) sum += of[i];
-  for (uint32_t i = 0; i < warp; ++i) sum += sh.warps[last][i];
-  if (target < sum || target >= sum + sh.warps[last][warp]) return;  // another warp has it
+  for (uint32_t i = 0; i < warp; ++i) sum += sh.warps[last][i][0];
+  if (target < sum || target >= sum + sh.warps[last][warp][0]) return;  // another warp has it
   for (uint32_t i0 = w0; i0 < w1; i0 += 32u) {
     const uint32_t i = i0 + lane;
     const uint64_t w = i < w1 ? kept(i) : 0ull;
@@ -249,13 +661,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleParams p) 
     }
     const uint32_t past = __ballot_sync(kFull, sum + upto > target);
     if (past) {
-      if (lane == __ffs(past) - 1u) {
-        p.token[row] = (int32_t)(from + i);
-        if (p.logprob) {
-          const double t = top == INFINITY ? 0.0 : ((double)xs[i] - (double)top) / (double)temperature;
-          p.logprob[row] = (float)(t - (log((double)total) - kOne * 0.69314718055994530942));
-        }
-      }
+      if (lane == __ffs(past) - 1u) answer(from + i, xs[i], total);
       return;
     }
     sum += __shfl_sync(kFull, upto, 31);
@@ -269,13 +675,15 @@ int launch(SampleParams& p, uint32_t rows, cudaStream_t st) {
   uint32_t ctas = kMaxCluster;
   while (ctas > 1 && p.vocab < 2048u * ctas) ctas /= 2;
   if (rows > 0x7FFFFFFFu / ctas) return TQ_ERR_UNSUPPORTED_SHAPE;
-  p.slice = ((p.vocab + ctas - 1u) / ctas + 3u) / 4u * 4u;
+  p.slice = ((p.vocab + ctas - 1u) / ctas + 7u) / 8u * 8u;
+  p.vectors = ((uintptr_t)p.logits & 15u) == 0 && (rows == 1 || (p.row_stride * (TYPE == TQ_TYPE_F32 ? 4 : 2)) % 16 == 0);
   const char* what = "sample launch";
-  if (int rc = tq_ensure_dynamic_smem((const void*)kern, sizeof(Shared) + TQ_SAMPLE_MAX_VOCAB / kMaxCluster * sizeof(float), what)) return rc;
+  constexpr size_t kHead = (sizeof(Shared) + 15u) / 16u * 16u;
+  if (int rc = tq_ensure_dynamic_smem((const void*)kern, kHead + TQ_SAMPLE_MAX_VOCAB / kMaxCluster * sizeof(float), what)) return rc;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(rows * ctas);
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = sizeof(Shared) + p.slice * sizeof(float);
+  cfg.dynamicSmemBytes = kHead + p.slice * sizeof(float);
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
