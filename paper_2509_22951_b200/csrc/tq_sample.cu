@@ -3,9 +3,10 @@
 //
 // Exact sums.  Every decision is a comparison of sums of weights w = 2^t, t = (x - max) log2(e) / temperature, with a bound: a
 // weight is therefore an integer W = round(2^45 w), and sums of up to 2^18 of them are exact in 64 bits whatever their
-// order, so that neither the split of a row nor the order of atomics can change a token.  t comes from one fp64 fused multiply-add onto
-// 1.5 * 2^20, whose last bit is 2^-32: the low word of the result is the fraction of t and the high word its integer part.  2^fraction =
-// table[upper 8 bits] * (1 + q), q a cubic in the lower 24, to 29 bits; W below 2^21 (t < -24) is taken from the fp32 exponential, to a unit or two.
+// order, so that neither the split of a row nor the order of atomics can change a token.  t is held in two fp32 numbers (difference and
+// product with their errors, by the usual sums without loss of Dekker and Knuth); rounded to 1/256 it gives a place in a table of 2^(i/256) and an
+// octave, and what is left a cubic, to 29 bits.  (fp64 would say it in fewer words, but its instructions take some 40 cycles of an SM's
+// quarter each: a row of 128256 tokens 18.6 us that way, %%% this way.)  W below 2^21 (t < -24) is taken from the fp32 exponential, to a unit or two.
 //
 // Order.  Tokens fall by (x, lower index first): as one integer, the logit's bits made to rise with it above the index turned
 // round.  What is kept is all that is not below a border in that order, so every filter is a search for its border.
@@ -78,7 +79,7 @@ struct Shared {
   uint64_t slots[2][kMaxCluster][2];  // what the cluster's CTAs tell one another; two sets, used in turn
   uint64_t warps[2][kWarps][2];
   uint64_t told[2];                   // by one CTA to all
-  uint32_t powers[256];
+  uint2 powers[256];                  // 2^(i / 256) with 29 bits behind the point, and as fp32
   uint32_t listed;                    // tokens in the list (of the first CTA)
   union {
     struct {
@@ -129,36 +130,72 @@ __device__ __forceinline__ uint32_t rising(float x) {
 __device__ __forceinline__ float from_rising(uint32_t r) { return __uint_as_float(r ^ (r >> 31 ? 0x80000000u : 0xFFFFFFFFu)); }
 __device__ __forceinline__ uint64_t order_of(float x, uint32_t index) { return ((uint64_t)rising(x) << kIndexBits) | (kIndexMask - index); }
 
-struct Weights {
-  float top, c32, c32_low;  // largest logit; log2(e) / temperature in two parts
-  double c;
-  const uint32_t* powers;
+// Two fp32 numbers whose sum is meant, the second small against the first.
+struct Pair {
+  float hi, lo;
+};
+__device__ __forceinline__ Pair exact_sum(float a, float b) {
+  const float s = a + b, t = s - a;
+  return Pair{s, (a - (s - t)) + (b - t)};
+}
+constexpr float kLn2 = 0.693147182464599609375f, kLn2Low = -1.904654323148236e-09f;       // ln 2
+constexpr float kLog2e = 1.44269502162933349609375f, kLog2eLow = 1.92596303178237e-08f;   // 1 / ln 2
 
-  // t in fp32; NaN for the largest logit where log2(e) / temperature overflows, and where it is 0 and the distance overflows (fine() knows both)
-  __device__ __forceinline__ float coarse(float x) const {
-    const float d = x - top, t = d * c32;
-    return t > -64.f ? fmaf(d, c32, d * c32_low) : t;
+// log2(m 2^(k - 29)), 2^29 <= m < 2^30, to 2^-30.
+__device__ __forceinline__ Pair log2_of(uint32_t m, int k, const uint2* powers) {
+  int i = min(max((int)(__log2f((float)m) * 256.f) - 29 * 256, 0), 255);
+  if (powers[i].x > m && i > 0) --i;
+  const float z = (float)(int32_t)(m - powers[i].x) / __uint_as_float(powers[i].y);  // 0 .. 0.0028
+  return Pair{(float)k + (float)i * 0.00390625f, z * (1.f + z * (-0.5f + z * (0.33333334f - z * 0.25f))) * kLog2e};
+}
+__device__ __forceinline__ Pair log2_of(uint64_t v, int one, const uint2* powers) {  // log2(v 2^-one)
+  const int top = 63 - __clzll((long long)v);
+  return log2_of(top >= 29 ? (uint32_t)(v >> (top - 29)) : (uint32_t)v << (29 - top), top - one, powers);
+}
+
+struct Weights {
+  float top, c, c_low;  // largest logit; log2(e) / temperature
+  const uint2* powers;
+
+  __device__ __forceinline__ void set(float top_, float temperature, const uint2* powers_) {
+    top = top_;
+    powers = powers_;
+    c = c_low = 0.f;
+    if (temperature < INFINITY) {
+      const float T = fmaxf(temperature, 7.52316385e-37f);  // 2^-120: where the quotient stays finite
+      c = kLog2e / T;
+      c_low = (fmaf(-c, T, kLog2e) + kLog2eLow) / T;
+    }
+  }
+  // t in fp32 (NaN where the distance overflows and the temperature is infinite: fine() takes that for 0)
+  __device__ __forceinline__ float coarse(float x) const { return (x - top) * c; }
+  __device__ __forceinline__ Pair both(float x) const {
+    const Pair d = exact_sum(x, -top);
+    const float t = d.hi * c;
+    return Pair{t, fmaf(d.lo, c, fmaf(d.hi, c_low, fmaf(d.hi, c, -t)))};
   }
   __device__ __forceinline__ bool none(float x) const { return x == -INFINITY || (top == INFINITY && x != top); }
-  // Octave n <= -1 (t = n + fraction) and the value of W = value << max(0, 16 + n): 29 bits of 2^fraction, or W itself below octave -16.
-  __device__ __forceinline__ uint32_t fine(float x, int& n, uint32_t& f) const {
-    const double z = fma((double)x - (double)top, c, 1572864.0);  // 1.5 * 2^20
-    n = __double2hiint(z) - 0x41380000;
-    f = (uint32_t)__double2loint(z);
-    if (x == top || n >= 0) {  // 2^30 in octave -1
-      n = -1;
-      f = 0xFFFFFFFFu;
-      return 1u << 30;
-    }
-    const uint32_t base = powers[f >> 24];
-    const float r = __uint_as_float(0x3F800000u | ((f & 0xFFFFFFu) >> 1)) - 1.0f;  // the lower 24 bits, 0 .. 1
-    constexpr float a1 = 2.7076061740622863e-3f, a2 = 3.6655656e-6f, a3 = 3.3082868e-9f;  // (ln 2 / 256)^k / k!
+  // Place of t in 1/256 (octave n = place >> 8, at most -1) and the value of W = value << max(0, 16 + n): 29 bits of 2^fraction, or W itself below
+  // octave -16.  For t down to some octaves below the histogram's.
+  __device__ __forceinline__ uint32_t fine(float x, int& place) const {
+    const Pair t = both(x);
+    const float s = t.hi + 49152.0f;  // 1.5 * 2^15: rounded to 1/256
+    place = __float_as_int(s) - 0x47400000;
+    const float r = (t.hi - (s - 49152.0f)) + t.lo;  // -1/512 .. 1/512
+    const bool whole = x == top || place > 0;  // (not a number: above every place)
+    const uint2 base = powers[place & 255];
+    constexpr float a1 = kLn2, a2 = 0.24022651f, a3 = 0.055504109f;  // (ln 2)^k / k!
     const float q = r * fmaf(r, fmaf(r, a3, a2), a1);
-    const uint32_t v = base + (__float_as_uint(fmaf((float)base, q, 8388608.0f)) - 0x4B000000u);  // rounded to whole units of 2^-29
-    const int down = -16 - n;
+    // rounded to whole units of 2^-29
+    uint32_t v = whole ? 1u << 29 : base.x + (__float_as_uint(fmaf(__uint_as_float(base.y), q, 12582912.0f)) - 0x4B400000u);
+    if (whole || place == 0) {  // twice as much in octave -1, which then is the first
+      place = -1;
+      v *= 2u;
+    }
+    const int down = -16 - (place >> 8);
     return down > 0 ? (v + (1u << (down - 1))) >> down : v;
   }
-  __device__ __forceinline__ static int shift(int n) { return max(0, 16 + n); }
+  __device__ __forceinline__ static int shift(int place) { return max(0, 16 + (place >> 8)); }
   // Octaves below the histogram's.
   __device__ __forceinline__ uint32_t small(float t) const {
     float w;
@@ -169,13 +206,59 @@ struct Weights {
     if (none(x)) return 0ull;
     const float t = coarse(x);
     if (t < -(float)kOctaves) return small(t);
-    int n;
-    uint32_t f;
-    const uint32_t v = fine(x, n, f);
-    return (uint64_t)v << shift(n);
+    int place;
+    const uint32_t v = fine(x, place);
+    return (uint64_t)v << shift(place);
+  }
+  // Four at once, for a whole warp: the chains of fine() side by side, or none of them where all weights are small.  use(j, is fine, place,
+  // value) for each; value is 0 where there is no weight.
+  template <class Use>
+  __device__ __forceinline__ void four(const float (&x)[4], Use use) const {
+    float t[4];
+    bool any = false;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      t[j] = none(x[j]) ? -INFINITY : coarse(x[j]);
+      any = any || !(t[j] < -(float)kOctaves);
+    }
+    if (!__any_sync(kFull, any)) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) use(j, false, -1, small(t[j]));
+      return;
+    }
+    int place[4];
+    uint32_t v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = fine(t[j] < -(float)kOctaves ? top : x[j], place[j]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const bool is_small = t[j] < -(float)kOctaves;
+      use(j, !is_small, place[j], is_small ? small(t[j]) : v[j]);
+    }
   }
 };
-__device__ __forceinline__ uint32_t bin_of(int n, uint32_t f) { return min((uint32_t)(-n - 1) * 64u + (63u - (f >> 26)), kBins - 1u); }
+// Four places to a bin; what lies below the histogram by a rounding is in its last.
+__device__ __forceinline__ uint32_t bin_of(int place) { return min((uint32_t)(-1 - place) >> 2, kBins - 1u); }
+// floor(f * v), f >= 0 an fp32 number below 1, and whether there is a remainder
+__device__ __forceinline__ uint64_t times(float f, uint64_t v, bool& more) {
+  const uint32_t b = __float_as_uint(f), e = b >> 23, m = e ? (b & 0x7FFFFFu) | 0x800000u : b & 0x7FFFFFu;
+  const int s = 150 - (int)(e ? e : 1u);  // f = m 2^-s, s >= 24
+  const uint64_t hi = __umul64hi(v, (uint64_t)m), lo = v * (uint64_t)m;
+  if (s >= 64) {
+    const int d = s - 64;
+    more = lo != 0ull || (d < 64 ? (hi & ((1ull << d) - 1ull)) != 0ull : hi != 0ull);
+    return d < 64 ? hi >> d : 0ull;
+  }
+  more = (lo & ((1ull << s) - 1ull)) != 0ull;
+  return (hi << (64 - s)) | (lo >> s);
+}
+// The least integer not below f * v: as many units and more are not less than f * v.
+__device__ __forceinline__ uint64_t bound_of(float f, uint64_t v) {
+  if (!(f > 0.f)) return 0ull;
+  bool more;
+  const uint64_t r = times(f, v, more);
+  return r + (more ? 1ull : 0ull);
+}
 
 // Sorts list[0 .. n), n <= kList, from the largest down: by every entry's rank where there are few, else bitonic.
 __device__ void sort_list(uint64_t* list, uint32_t n, uint32_t tid) {
@@ -216,7 +299,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u, rank = cluster_rank(), ctas = cluster_size();
   const uint32_t row = blockIdx.x / ctas, from = min(rank * p.slice, p.vocab), n = min(p.slice, p.vocab - from);
-  if (tid < 256) sh.powers[tid] = kPowers.v[tid];
+  if (tid < 256) sh.powers[tid] = make_uint2(kPowers.v[tid], __float_as_uint((float)kPowers.v[tid]));
   if (tid == 0) sh.listed = 0u;
   asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -318,6 +401,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   } else {
     for (uint32_t i = tid; i < n; i += kThreads) xs[i] = take(load1<TYPE>(p.logits, row_at + i), i);
   }
+  if (tid < 4u && n + tid < (n + 3u) / 4u * 4u) xs[n + tid] = -INFINITY;
   asm volatile("barrier.cluster.wait.aligned;" ::: "memory");  // every CTA of the cluster runs: its shared memory can be written
   uint64_t best = mine > -INFINITY ? order_of(mine, from + mine_at) : 0ull;
   uint64_t lowest = mine > -INFINITY ? (uint64_t)~rising(mine) : 0ull;  // the least of the threads' maxima, turned round
@@ -332,32 +416,53 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   }
   const float top = from_rising((uint32_t)(best >> kIndexBits));
   Weights weight;
-  weight.top = top;
-  weight.c = 1.4426950408889634074 / (double)temperature;
-  weight.c32 = (float)weight.c;
-  weight.c32_low = (float)(weight.c - (double)weight.c32);
-  if (!(fabsf(weight.c32) < INFINITY)) weight.c32_low = 0.f;
-  weight.powers = sh.powers;
+  weight.set(top, temperature, sh.powers);
 
   const int32_t k_given = p.top_k ? p.top_k[row] : 0;
   const uint32_t k = k_given > 0 && (uint32_t)k_given < p.vocab ? (uint32_t)k_given : 0u;
   const float top_p = p.top_p ? p.top_p[row] : 1.f, min_p = p.min_p ? p.min_p[row] : 0.f;
   const float u = p.uniform[row];
   uint64_t keep = 0;  // tokens at or after this are kept
-  if (min_p > 0.f) {
-    const double edge = (double)top + (double)temperature * log((double)min_p);
-    const float x = min_p >= 1.f || top == INFINITY ? top : fminf(__double2float_ru(edge), top);
-    keep = (uint64_t)rising(x + 0.f) << kIndexBits;
+  if (min_p > 0.f) {  // the least logit with t >= log2(min_p), by a search of one warp over the numbers' order
+    if (warp == 0) {
+      uint32_t lo = rising(-INFINITY), hi = rising(top);  // hi is kept
+      if (min_p < 1.f && top < INFINITY) {
+        const uint32_t b = __float_as_uint(min_p), e = b >> 23;
+        const Pair edge = e ? log2_of((b & 0x7FFFFFu | 0x800000u) << 6, (int)e - 127, sh.powers) : log2_of((uint64_t)b, 149, sh.powers);
+        while (lo < hi) {
+          const uint32_t step = (hi - lo) / 33u + 1u;
+          const uint32_t at = min(lo + (lane + 1u) * step - 1u, hi);  // rising over the lanes
+          const float x = from_rising(at);
+          const Pair t = weight.both(x);
+          const bool in = at == hi || x == top || (!weight.none(x) && (t.hi - edge.hi) + (t.lo - edge.lo) >= 0.f);
+          const uint32_t votes = __ballot_sync(kFull, in);
+          const uint32_t first = votes ? __ffs(votes) - 1u : 32u;  // the first lane whose number is kept
+          const uint32_t new_lo = first ? min(lo + first * step, hi) : lo;
+          hi = first < 32u ? min(lo + (first + 1u) * step - 1u, hi) : hi;
+          lo = new_lo;
+        }
+      } else {
+        lo = hi;
+      }
+      if (lane == 0) sh.told[1] = hi;
+    }
+    __syncthreads();
+    keep = sh.told[1] << kIndexBits;
+    __syncthreads();
   }
   auto target_of = [&](uint64_t total) {
-    const uint64_t y = (uint64_t)((u > 0.f ? (double)u : 0.0) * (double)total);
-    return y < total ? y : total - 1u;
+    if (!(u < 1.f)) return u >= 1.f ? total - 1u : 0ull;
+    bool more;
+    return u > 0.f ? times(u, total, more) : 0ull;  // below the total
   };
   auto answer = [&](uint32_t index, float x, uint64_t total) {
     p.token[row] = (int32_t)index;
-    if (p.logprob) {
-      const double t = x == top ? 0.0 : ((double)x - (double)top) / (double)temperature;
-      p.logprob[row] = (float)(t - (log((double)total) - kOne * 0.69314718055994530942));
+    if (p.logprob) {  // ln 2 (t - log2(total / 2^45))
+      const Pair sum = log2_of(total, kOne, sh.powers);
+      const Pair t = x == top ? Pair{0.f, 0.f} : weight.both(x);
+      const Pair d = exact_sum(t.hi, -sum.hi);
+      const float low = d.lo + (t.lo - sum.lo), h = d.hi * kLn2;
+      p.logprob[row] = h + fmaf(low, kLn2, fmaf(d.hi, kLn2Low, fmaf(d.hi, kLn2, -h)));
     }
   };
 
@@ -369,19 +474,23 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     all2(v, zero, false, of);
     return v;
   };
-  auto border = [&](double bound, bool count, uint64_t lo) {
+  auto border = [&](uint64_t bound, bool count, uint64_t lo) {
     uint64_t hi = best;  // nothing is before it
     while (lo < hi) {
       const uint64_t mid = lo + (hi - lo) / 2u;
-      if ((double)before(mid, count) < bound)
+      if (before(mid, count) < bound)
         hi = mid;
       else
         lo = mid + 1u;
     }
     return hi;
   };
-  // warps own consecutive pieces of the slice
-  const uint32_t piece = (n + kThreads - 1u) / kThreads * 32u, w0 = min(warp * piece, n), w1 = min(w0 + piece, n);
+  // warps own consecutive pieces of the slice, a lane four consecutive logits of 128
+  const uint32_t piece = (n + 4u * kThreads - 1u) / (4u * kThreads) * 128u, w0 = min(warp * piece, n), w1 = min(w0 + piece, n);
+  auto read4 = [&](uint32_t i, uint32_t end, float (&x)[4]) {
+    const float4 y = i < end ? *reinterpret_cast<const float4*>(xs + i) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+    x[0] = y.x, x[1] = y.y, x[2] = y.z, x[3] = y.w;  // past the slice's end lies -inf
+  };
   const bool p_on = top_p < 1.f;
   bool searched = !p_on && k == 0u;  // the border is known
 
@@ -414,9 +523,17 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     if (tid < kKBins && upto >= k && upto - in_bin < k) sh.told[0] = tid;
     __syncthreads();
     const uint32_t cut = (uint32_t)sh.told[0];
-    auto listed = [&](float x) { return x > -INFINITY && k_bin(x) <= cut; };
+    // the same products as in k_bin, compared with the bin's end
+    const float last_bin = scale == 0.f ? 0.f : (float)(cut + 1u);
+    const bool all_bins = cut == kKBins - 1u;
+    auto listed = [&](float x) { return x > -INFINITY && (all_bins || (scale == 0.f ? k_bin(x) <= cut : (top - x) * scale < last_bin)); };
     uint32_t count = 0;
-    for (uint32_t i = w0 + lane; i < w1; i += 32u) count += listed(xs[i]) ? 1u : 0u;
+    for (uint32_t i = w0 + 4u * lane; i < w1; i += 128u) {
+      float x[4];
+      read4(i, w1, x);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) count += listed(x[j]) ? 1u : 0u;
+    }
     uint64_t v = count, zero = 0;
     const uint32_t last = turn;
     all2(v, zero, false, of);  // (also: every CTA has read the bins, the list may lie over them)
@@ -425,12 +542,26 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
       uint32_t at = 0;
       for (uint32_t i = 0; i < rank; ++i) at += (uint32_t)of[i];
       for (uint32_t i = 0; i < warp; ++i) at += (uint32_t)sh.warps[last][i][0];
-      for (uint32_t i0 = w0; i0 < w1; i0 += 32u) {
-        const uint32_t i = i0 + lane;
-        const bool yes = i < w1 && listed(xs[i]);
-        const uint32_t votes = __ballot_sync(kFull, yes);
-        if (yes) store_remote(&sh.list[at + __popc(votes & ((1u << lane) - 1u))], 0u, order_of(xs[i], from + i));
-        at += __popc(votes);
+      for (uint32_t i0 = w0; i0 < w1; i0 += 128u) {
+        const uint32_t i = i0 + 4u * lane;
+        float x[4];
+        read4(i, w1, x);
+        uint32_t mask = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) mask |= listed(x[j]) ? 1u << j : 0u;
+        if (!__any_sync(kFull, mask != 0u)) continue;
+        const uint32_t own = __popc(mask);
+        uint32_t upto = own;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const uint32_t o = __shfl_up_sync(kFull, upto, d);
+          if (lane >= (uint32_t)d) upto += o;
+        }
+        uint32_t to = at + upto - own;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if ((mask >> j) & 1u) store_remote(&sh.list[to++], 0u, order_of(x[j], from + i + j));
+        at += __shfl_sync(kFull, upto, 31);
       }
       cluster_sync();
       if (rank != 0) return;
@@ -471,11 +602,11 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
           sum += w[i];
         }
         uint64_t prev = scan(sum, total);
-        const double bound = (double)top_p * (double)total;
+        const uint64_t bound = bound_of(top_p, total);
         uint32_t in = 0;
 #pragma unroll
         for (uint32_t i = 0; i < kEach; ++i) {
-          in += tid * kEach + i < kept && (double)prev < bound ? 1u : 0u;
+          in += tid * kEach + i < kept && prev < bound ? 1u : 0u;
           prev += w[i];
         }
         uint64_t sum_in;
@@ -508,19 +639,18 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     for (uint32_t i = tid; i < kBins; i += kThreads) sh.bins.hi[i] = sh.bins.lo[i] = 0u;
     __syncthreads();
     uint64_t rest = 0;  // of the octaves below
-    for (uint32_t i = tid; i < n; i += kThreads) {
-      const float x = xs[i];
-      if (weight.none(x)) continue;
-      const float t = weight.coarse(x);
-      if (t < -(float)kOctaves) {
-        rest += weight.small(t);
-        continue;
-      }
-      int o;
-      uint32_t f;
-      const uint32_t v = weight.fine(x, o, f), b = bin_of(o, f);
-      atomicAdd(&sh.bins.hi[b], v >> 15);
-      atomicAdd(&sh.bins.lo[b], v & 0x7FFFu);
+    for (uint32_t i0 = w0; i0 < w1; i0 += 128u) {
+      float x[4];
+      read4(i0 + 4u * lane, w1, x);
+      weight.four(x, [&](int, bool fine, int place, uint32_t v) {
+        if (fine) {
+          const uint32_t b = bin_of(place);
+          atomicAdd(&sh.bins.hi[b], v >> 15);
+          atomicAdd(&sh.bins.lo[b], v & 0x7FFFu);
+        } else {
+          rest += v;
+        }
+      });
     }
     cluster_sync();
     // this CTA's bins of all CTAs: kBins / ctas consecutive ones, up to three to a thread
@@ -533,7 +663,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
         hi += load_remote(&sh.bins.hi[first + j], r);
         lo += load_remote(&sh.bins.lo[first + j], r);
       }
-      const uint64_t m = ((hi << 15) + lo) << Weights::shift(-1 - (int)((first + j) / 64u));
+      const uint64_t m = ((hi << 15) + lo) << Weights::shift(-1 - 4 * (int)(first + j));
       if (j == 0) mass[0] = m;
       if (j == 1) mass[1] = m;
       if (j == 2) mass[2] = m;
@@ -549,14 +679,14 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     }
     if (tid == 0) sh.told[0] = ~0ull;
     all2(total, all_rest, false, of);
-    const double bound = (double)top_p * (double)(total + all_rest);
+    const uint64_t bound = bound_of(top_p, total + all_rest);
     uint64_t prev = incl - sum;
     for (uint32_t i = 0; i < rank; ++i) prev += of[i];
     for (uint32_t i = 0; i < warp; ++i) prev += sh.warps[last][i][0];
-    if (0.0 < bound) {
+    if (bound != 0ull) {
 #pragma unroll
       for (uint32_t j = 0; j < 3u; ++j) {
-        if (j < each && mass[j] != 0ull && (double)prev < bound && (double)(prev + mass[j]) >= bound) {
+        if (j < each && mass[j] != 0ull && prev < bound && prev + mass[j] >= bound) {
           for (uint32_t r = 0; r < ctas; ++r) {
             store_remote(&sh.told[0], r, first + j);
             store_remote(&sh.told[1], r, prev);
@@ -567,25 +697,43 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     }
     cluster_sync();  // (also: every CTA has read the bins, the list may lie over them)
     const uint64_t bin = sh.told[0], ahead = sh.told[1];
-    if (!(0.0 < bound)) {
+    if (bound == 0ull) {
       keep = best;
       searched = true;
     } else if (bin != ~0ull) {
-      for (uint32_t i0 = 0; i0 < n; i0 += kThreads) {
-        const uint32_t i = i0 + tid;
-        bool yes = false;
-        if (i < n && !weight.none(xs[i]) && !(weight.coarse(xs[i]) < -(float)kOctaves)) {
-          int o;
-          uint32_t f;
-          weight.fine(xs[i], o, f);
-          yes = bin_of(o, f) == (uint32_t)bin;
+      // the bin's logits lie between these, give or take the roundings of fp32: only there is the bin looked at
+      const float t_hi = (float)bin * -0.015625f, t_lo = t_hi - 0.015625f;
+      for (uint32_t i0 = w0; i0 < w1; i0 += 128u) {
+        const uint32_t i = i0 + 4u * lane;
+        float x[4];
+        read4(i, w1, x);
+        uint32_t mask = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (weight.none(x[j])) continue;
+          const float t = weight.coarse(x[j]);
+          if (t < t_lo - 0.01f || t > t_hi + 0.01f || t < -(float)kOctaves) continue;  // (a place is rounded to 1/256)
+          int place;
+          weight.fine(x[j], place);
+          if (bin_of(place) == (uint32_t)bin) mask |= 1u << j;
         }
-        const uint32_t votes = __ballot_sync(kFull, yes);
-        if (votes == 0u) continue;
+        if (!__any_sync(kFull, mask != 0u)) continue;
+        const uint32_t own = __popc(mask);
+        uint32_t upto = own;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const uint32_t o = __shfl_up_sync(kFull, upto, d);
+          if (lane >= (uint32_t)d) upto += o;
+        }
         uint32_t at = 0;
-        if (lane == 0) at = add_remote(&sh.listed, 0u, __popc(votes));
-        at = __shfl_sync(kFull, at, 0) + __popc(votes & ((1u << lane) - 1u));
-        if (yes && at < kList) store_remote(&sh.list[at], 0u, order_of(xs[i], from + i));
+        if (lane == 31) at = add_remote(&sh.listed, 0u, upto);
+        at = __shfl_sync(kFull, at, 31) + upto - own;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (!((mask >> j) & 1u)) continue;
+          if (at < kList) store_remote(&sh.list[at], 0u, order_of(x[j], from + i + j));
+          ++at;
+        }
       }
       cluster_sync();
       const uint32_t m = load_remote(&sh.listed, 0u);
@@ -614,7 +762,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
 #pragma unroll
           for (uint32_t i = 0; i < kEach; ++i) {
             const uint32_t j = tid * kEach + i;
-            if (j < m && (double)prev < bound && (j + 1u == m || (double)(prev + w[i]) >= bound)) {
+            if (j < m && prev < bound && (j + 1u == m || prev + w[i] >= bound)) {
               for (uint32_t r = 0; r < ctas; ++r) store_remote(&sh.told[0], r, sh.list[j]);
             }
             prev += w[i];
@@ -629,10 +777,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   }
   if (!searched) {
     uint64_t edge = 0;
-    if (k != 0u) edge = border((double)k, true, 0ull);
+    if (k != 0u) edge = border(k, true, 0ull);
     if (p_on) {
       const uint64_t sum = before(edge ? edge - 1u : 0u, false);  // 0 is no token's place
-      edge = border((double)top_p * (double)sum, false, edge);
+      edge = border(bound_of(top_p, sum), false, edge);
     }
     keep = max(keep, edge);
   }
@@ -640,9 +788,26 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
 
   // ---- the token up to which more than u of the kept sum lies ---------------------------------------
   const float keep_x = from_rising((uint32_t)(keep >> kIndexBits));  // below it nothing is kept
-  auto kept = [&](uint32_t i) { return !(xs[i] < keep_x) && order_of(xs[i], from + i) >= keep ? weight(xs[i]) : 0ull; };
+  // weights of four logits, 0 where they are not kept
+  auto kept = [&](uint32_t i, uint64_t (&w)[4]) {
+    float x[4];
+    read4(i, w1, x);
+    bool any = false;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (x[j] < keep_x || order_of(x[j], from + i + j) < keep) x[j] = -INFINITY;
+      any = any || x[j] > -INFINITY;
+      w[j] = 0ull;
+    }
+    if (!__any_sync(kFull, any)) return;
+    weight.four(x, [&](int j, bool fine, int place, uint32_t v) { w[j] = fine ? (uint64_t)v << Weights::shift(place) : v; });
+  };
   uint64_t sum_mine = 0, zero = 0;
-  for (uint32_t i = w0 + lane; i < w1; i += 32u) sum_mine += kept(i);
+  for (uint32_t i0 = w0; i0 < w1; i0 += 128u) {
+    uint64_t w[4];
+    kept(i0 + 4u * lane, w);
+    sum_mine += w[0] + w[1] + w[2] + w[3];
+  }
   const uint32_t last = turn;
   all2(sum_mine, zero, false, of);
   const uint64_t total = sum_mine, target = target_of(total);
@@ -650,10 +815,12 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   for (uint32_t i = 0; i < rank; ++i) sum += of[i];
   for (uint32_t i = 0; i < warp; ++i) sum += sh.warps[last][i][0];
   if (target < sum || target >= sum + sh.warps[last][warp][0]) return;  // another warp has it
-  for (uint32_t i0 = w0; i0 < w1; i0 += 32u) {
-    const uint32_t i = i0 + lane;
-    const uint64_t w = i < w1 ? kept(i) : 0ull;
-    uint64_t upto = w;
+  for (uint32_t i0 = w0; i0 < w1; i0 += 128u) {
+    const uint32_t i = i0 + 4u * lane;
+    uint64_t w[4];
+    kept(i, w);
+    const uint64_t own = w[0] + w[1] + w[2] + w[3];
+    uint64_t upto = own;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
       const uint64_t o = __shfl_up_sync(kFull, upto, d);
@@ -661,7 +828,12 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     }
     const uint32_t past = __ballot_sync(kFull, sum + upto > target);
     if (past) {
-      if (lane == __ffs(past) - 1u) answer(from + i, xs[i], total);
+      if (lane == __ffs(past) - 1u) {
+        sum += upto - own;
+        uint32_t j = 0;
+        while (j < 3u && sum + w[j] <= target) sum += w[j++];
+        answer(from + i + j, xs[i + j], total);
+      }
       return;
     }
     sum += __shfl_sync(kFull, upto, 31);
