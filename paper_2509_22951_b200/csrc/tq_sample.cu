@@ -3,18 +3,18 @@
 //
 // Exact sums.  Every decision is a comparison of sums of weights w = 2^t, t = (x - max) log2(e) / temperature, with a bound: a
 // weight is therefore an integer W = round(2^45 w), and sums of up to 2^18 of them are exact in 64 bits whatever their
-// order, so that neither the split of a row nor the order of atomics can change a token.  t is held in two fp32 numbers (difference and
-// product with their errors, by the usual sums without loss of Dekker and Knuth); rounded to 1/256 it gives a place in a table of 2^(i/256) and an
-// octave, and what is left a cubic, to 29 bits.  (fp64 would say it in fewer words, but its instructions take some 40 cycles of an SM's
-// quarter each: a row of 128256 tokens 18.6 us that way, %%% this way.)  W below 2^21 (t < -24) is taken from the fp32 exponential, to a unit or two.
+// order, so that neither the split of a row nor the order of atomics can change a token.  With A a multiple of 1/32 next to max log2(e) / temperature,
+// one fused multiply-add rounds t to 1/32 and another, which takes that from the exact product again, leaves the rest to 2^-31: the first is a
+// place in a table of 2^(i/32) (a bank of shared memory for each entry) and an octave, the second goes into a polynomial: 27 bits and more in some
+// 25 instructions.  W below 2^21 (t < -24) is the fp32 exponential, to some units.
 //
 // Order.  Tokens fall by (x, lower index first): as one integer, the logit's bits made to rise with it above the index turned
 // round.  What is kept is all that is not below a border in that order, so every filter is a search for its border.
 //
 // A row is read once: a cluster of up to eight CTAs holds it in shared memory and speaks through distributed shared memory.  Then
-//   top-k (up to 1024): the k-th largest of the threads' own maxima is a bound of the k-th logit that few others pass: those go to one CTA in
-//          the order of the vocabulary, which sorts them and does the rest;
-//   top-p alone: a histogram of the weights over 64 bins an octave (exact: two integers a bin) finds the bin of the border, whose
+//   top-k (up to 1024): the k-th largest of the threads' own maxima is a bound of the k-th logit that few others pass: those go to one CTA,
+//          which sorts them and does the rest;
+//   top-p alone: a histogram of the weights over 32 bins an octave (exact: two integers a bin) finds the bin of the border, whose
 //          tokens one CTA sorts; then every CTA adds up what it keeps;
 //   neither, or min-p alone: the border is known; every CTA adds up what it keeps.
 // Where so many logits are alike that a list does not hold them (2048), and for larger k, the border is found by bisection of the order.
@@ -35,23 +35,23 @@ constexpr uint32_t kMaxCluster = 8;
 constexpr uint32_t kIndexBits = 18;
 static_assert((1u << kIndexBits) == TQ_SAMPLE_MAX_VOCAB, "a token's index fits its place in the order");
 constexpr uint32_t kIndexMask = (1u << kIndexBits) - 1u;
-constexpr int kOne = 45;     // W of the largest logit is 2^45
-constexpr int kOctaves = 24; // of the histogram, and of the weights that are computed to 29 bits
-constexpr uint32_t kBins = kOctaves * 64u;
+constexpr int kOne = 45;      // W of the largest logit is 2^45
+constexpr int kOctaves = 24;  // of the histogram, and of the weights that are computed to 29 bits
+constexpr uint32_t kBins = kOctaves * 32u + 2u;  // a place each; the last has what a rounding puts below
 constexpr uint32_t kList = 2048;   // tokens that one CTA sorts
 constexpr uint32_t kListK = 1024;  // largest k of the list: the threads' maxima bound it well up to a quarter of their number
 constexpr uint32_t kKBins = 256;   // of the threads' maxima
 
-// 2^(i / 256) with 29 bits behind the point
+// 2^(i / 32) with 29 bits behind the point
 struct Powers {
-  uint32_t v[256];
+  uint32_t v[32];
 };
 constexpr Powers powers() {
   Powers p{};
-  for (int i = 0; i < 256; ++i) {
-    const double y = i * (0.69314718055994530942 / 256.0);
+  for (int i = 0; i < 32; ++i) {
+    const double y = i * (0.69314718055994530942 / 32.0);
     double term = 1.0, sum = 1.0;
-    for (int k = 1; k < 24; ++k) {
+    for (int k = 1; k < 32; ++k) {
       term *= y / k;
       sum += term;
     }
@@ -76,19 +76,20 @@ struct SampleParams {
 };
 
 struct Shared {
-  uint64_t slots[2][kMaxCluster][2];  // what the cluster's CTAs tell one another; two sets, used in turn
-  uint64_t warps[2][kWarps][2];
-  uint64_t told[2];                   // by one CTA to all
-  uint2 powers[256];                  // 2^(i / 256) with 29 bits behind the point, and as fp32
-  uint32_t listed;                    // tokens in the list (of the first CTA)
+  uint64_t slots[3][kMaxCluster * kWarps];  // what the cluster's warps tell one another; two sets, used in turn, and one for the start
+  uint64_t told[2];                         // by one CTA to all
+  uint64_t warps[kWarps];                   // within a CTA
+  uint2 powers[32];                         // 2^(i / 32) with 29 bits behind the point, and as fp32
+  uint32_t listed;                          // tokens in the list (of the first CTA)
   union {
     struct {
-      uint32_t hi[kBins], lo[kBins];  // sums of the upper and lower 15 bits of the weights of a bin
+      uint32_t hi[kBins], lo[kBins];  // sums of the upper and lower 15 bits of the values of a bin
     } bins;
     uint64_t list[kList];
     uint32_t k_bins[kKBins];
   };
 };
+constexpr uint32_t kHead = (sizeof(Shared) + 15u) / 16u * 16u;  // the row's slice lies behind it
 
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
@@ -111,9 +112,10 @@ __device__ __forceinline__ uint32_t at_rank(const void* ptr, uint32_t rank) {
 __device__ __forceinline__ void store_remote(const uint64_t* ptr, uint32_t rank, uint64_t v) {
   asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(at_rank(ptr, rank)), "l"(v) : "memory");
 }
+// (not volatile: several are asked for together; the cluster's barriers order them)
 __device__ __forceinline__ uint32_t load_remote(const uint32_t* ptr, uint32_t rank) {
   uint32_t v;
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at_rank(ptr, rank)) : "memory");
+  asm("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at_rank(ptr, rank)) : "memory");
   return v;
 }
 __device__ __forceinline__ uint32_t add_remote(uint32_t* ptr, uint32_t rank, uint32_t v) {
@@ -129,32 +131,62 @@ __device__ __forceinline__ uint32_t rising(float x) {
 }
 __device__ __forceinline__ float from_rising(uint32_t r) { return __uint_as_float(r ^ (r >> 31 ? 0x80000000u : 0xFFFFFFFFu)); }
 __device__ __forceinline__ uint64_t order_of(float x, uint32_t index) { return ((uint64_t)rising(x) << kIndexBits) | (kIndexMask - index); }
+__device__ __forceinline__ uint32_t index_of(uint64_t order) { return kIndexMask - (uint32_t)(order & kIndexMask); }
+__device__ __forceinline__ float logit_of(uint64_t order) { return from_rising((uint32_t)(order >> kIndexBits)); }
+
+// Sums over a warp, in every lane, below 2^64: three pieces that 32 lanes cannot carry out of 32 bits.
+__device__ __forceinline__ uint64_t warp_sum(uint64_t v) {
+  const uint32_t a = __reduce_add_sync(kFull, (uint32_t)v & 0x3FFFFFu), b = __reduce_add_sync(kFull, (uint32_t)(v >> 22) & 0x3FFFFFu),
+                 c = __reduce_add_sync(kFull, (uint32_t)(v >> 44));
+  return (uint64_t)a + ((uint64_t)b << 22) + ((uint64_t)c << 44);
+}
+__device__ __forceinline__ uint64_t warp_upto(uint64_t v, uint32_t lane) {  // of this lane and those before it
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const uint64_t o = __shfl_up_sync(kFull, v, d);
+    if (lane >= (uint32_t)d) v += o;
+  }
+  return v;
+}
+__device__ __forceinline__ uint32_t warp_upto(uint32_t v, uint32_t lane) {
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const uint32_t o = __shfl_up_sync(kFull, v, d);
+    if (lane >= (uint32_t)d) v += o;
+  }
+  return v;
+}
 
 // Two fp32 numbers whose sum is meant, the second small against the first.
 struct Pair {
   float hi, lo;
 };
-__device__ __forceinline__ Pair exact_sum(float a, float b) {
+__device__ __forceinline__ Pair exact_sum(float a, float b) {  // Knuth's sum without loss
   const float s = a + b, t = s - a;
   return Pair{s, (a - (s - t)) + (b - t)};
 }
-constexpr float kLn2 = 0.693147182464599609375f, kLn2Low = -1.904654323148236e-09f;       // ln 2
-constexpr float kLog2e = 1.44269502162933349609375f, kLog2eLow = 1.92596303178237e-08f;   // 1 / ln 2
+constexpr float kLn2 = 0.693147182464599609375f, kLn2Low = -1.904654323148236e-09f;      // ln 2
+constexpr float kLog2e = 1.44269502162933349609375f, kLog2eLow = 1.92596303178237e-08f;  // 1 / ln 2
 
-// log2(m 2^(k - 29)), 2^29 <= m < 2^30, to 2^-30.
+// log2(m 2^(k - 29)), 2^29 <= m < 2^30, to 2^-29: the table's entry below m, and a series for the rest.
 __device__ __forceinline__ Pair log2_of(uint32_t m, int k, const uint2* powers) {
-  int i = min(max((int)(__log2f((float)m) * 256.f) - 29 * 256, 0), 255);
+  int i = min(max((int)((__log2f((float)m) - 29.f) * 32.f), 0), 31);
   if (powers[i].x > m && i > 0) --i;
-  const float z = (float)(int32_t)(m - powers[i].x) / __uint_as_float(powers[i].y);  // 0 .. 0.0028
-  return Pair{(float)k + (float)i * 0.00390625f, z * (1.f + z * (-0.5f + z * (0.33333334f - z * 0.25f))) * kLog2e};
+  const float z = (float)(int32_t)(m - powers[i].x) / __uint_as_float(powers[i].y);  // 0 .. 0.022
+  const float y = z * (1.f + z * (-0.5f + z * (0.33333334f + z * (-0.25f + z * (0.2f - z * 0.16666667f)))));
+  return Pair{(float)k + (float)i * 0.03125f, fmaf(y, kLog2e, y * kLog2eLow)};
 }
 __device__ __forceinline__ Pair log2_of(uint64_t v, int one, const uint2* powers) {  // log2(v 2^-one)
   const int top = 63 - __clzll((long long)v);
   return log2_of(top >= 29 ? (uint32_t)(v >> (top - 29)) : (uint32_t)v << (29 - top), top - one, powers);
 }
 
+// W = value << max(0, 16 + octave) with a place = 32 t, rounded, in octave place >> 5.
 struct Weights {
-  float top, c, c_low;  // largest logit; log2(e) / temperature
+  float top;          // largest logit, finite
+  float c, c_low;     // log2(e) / temperature
+  float a, a_low;     // top * log2(e) / temperature: a multiple of 1/32, and the rest
+  bool plain;         // a is small enough for the short form
   const uint2* powers;
 
   __device__ __forceinline__ void set(float top_, float temperature, const uint2* powers_) {
@@ -166,46 +198,54 @@ struct Weights {
       c = kLog2e / T;
       c_low = (fmaf(-c, T, kLog2e) + kLog2eLow) / T;
     }
+    const float full = top * c;
+    plain = fabsf(full) < 65536.f;
+    a = plain ? rintf(full * 32.f) * 0.03125f : 0.f;
+    a_low = fmaf(top, c, -a) + top * c_low;
   }
-  // t in fp32 (NaN where the distance overflows and the temperature is infinite: fine() takes that for 0)
+  // t in fp32 (NaN where the distance overflows and the temperature is infinite)
   __device__ __forceinline__ float coarse(float x) const { return (x - top) * c; }
   __device__ __forceinline__ Pair both(float x) const {
     const Pair d = exact_sum(x, -top);
     const float t = d.hi * c;
     return Pair{t, fmaf(d.lo, c, fmaf(d.hi, c_low, fmaf(d.hi, c, -t)))};
   }
-  __device__ __forceinline__ bool none(float x) const { return x == -INFINITY || (top == INFINITY && x != top); }
-  // Place of t in 1/256 (octave n = place >> 8, at most -1) and the value of W = value << max(0, 16 + n): 29 bits of 2^fraction, or W itself below
-  // octave -16.  For t down to some octaves below the histogram's.
+  // For t from 0 down to some octaves below the histogram's, and NaN, which is taken for 0.
   __device__ __forceinline__ uint32_t fine(float x, int& place) const {
-    const Pair t = both(x);
-    const float s = t.hi + 49152.0f;  // 1.5 * 2^15: rounded to 1/256
-    place = __float_as_int(s) - 0x47400000;
-    const float r = (t.hi - (s - 49152.0f)) + t.lo;  // -1/512 .. 1/512
-    const bool whole = x == top || place > 0;  // (not a number: above every place)
-    const uint2 base = powers[place & 255];
-    constexpr float a1 = kLn2, a2 = 0.24022651f, a3 = 0.055504109f;  // (ln 2)^k / k!
-    const float q = r * fmaf(r, fmaf(r, a3, a2), a1);
-    // rounded to whole units of 2^-29
-    uint32_t v = whole ? 1u << 29 : base.x + (__float_as_uint(fmaf(__uint_as_float(base.y), q, 12582912.0f)) - 0x4B400000u);
-    if (whole || place == 0) {  // twice as much in octave -1, which then is the first
-      place = -1;
-      v *= 2u;
+    constexpr float kRound = 393216.0f;  // 1.5 * 2^18: sums with it are rounded to 1/32
+    float r;
+    if (plain) {
+      const float k = kRound - a, s = fmaf(x, c, k);
+      place = __float_as_int(s) - 0x48C00000;
+      r = fmaf(x, c, k - s) + fmaf(x, c_low, -a_low);
+    } else {
+      const Pair t = both(x);
+      const float s = t.hi + kRound;
+      place = __float_as_int(s) - 0x48C00000;
+      r = (t.hi - (s - kRound)) + t.lo;
     }
-    const int down = -16 - (place >> 8);
+    if (place > 0) {  // the largest logit, where a is that far from the exact product
+      r += (float)place * 0.03125f;
+      place = 0;
+    }
+    const uint2 base = powers[place & 31];
+    constexpr float a2 = 0.24022651f, a3 = 0.055504109f, a4 = 0.0096181291f;  // (ln 2)^k / k!
+    const float q = r * fmaf(r, fmaf(r, fmaf(r, a4, a3), a2), kLn2);
+    // rounded to whole units of 2^-29
+    const uint32_t v = base.x + (uint32_t)__float2int_rn(__uint_as_float(base.y) * q);
+    const int down = -16 - (place >> 5);
     return down > 0 ? (v + (1u << (down - 1))) >> down : v;
   }
-  __device__ __forceinline__ static int shift(int place) { return max(0, 16 + (place >> 8)); }
-  // Octaves below the histogram's.
+  __device__ __forceinline__ static int shift(int place) { return max(0, 16 + (place >> 5)); }
+  // Octaves below the histogram's; 0 for -inf.
   __device__ __forceinline__ uint32_t small(float t) const {
     float w;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(w) : "f"(t + (float)kOne));
-    return t < -46.f ? 0u : __float2uint_rn(w);
+    return __float2uint_rn(w);
   }
   __device__ __forceinline__ uint64_t operator()(float x) const {
-    if (none(x)) return 0ull;
     const float t = coarse(x);
-    if (t < -(float)kOctaves) return small(t);
+    if (x == -INFINITY || t < -(float)kOctaves) return x == -INFINITY ? 0u : small(t);
     int place;
     const uint32_t v = fine(x, place);
     return (uint64_t)v << shift(place);
@@ -215,15 +255,12 @@ struct Weights {
   template <class Use>
   __device__ __forceinline__ void four(const float (&x)[4], Use use) const {
     float t[4];
-    bool any = false;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      t[j] = none(x[j]) ? -INFINITY : coarse(x[j]);
-      any = any || !(t[j] < -(float)kOctaves);
-    }
-    if (!__any_sync(kFull, any)) {
+    for (int j = 0; j < 4; ++j) t[j] = x[j] == -INFINITY ? -INFINITY : coarse(x[j]);
+    const float most = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));  // (a NaN beside numbers is dropped here: all of a row are, or none)
+    if (!__any_sync(kFull, !(most < -(float)kOctaves))) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) use(j, false, -1, small(t[j]));
+      for (int j = 0; j < 4; ++j) use(j, false, 0, small(t[j]));
       return;
     }
     int place[4];
@@ -237,9 +274,9 @@ struct Weights {
     }
   }
 };
-// Four places to a bin; what lies below the histogram by a rounding is in its last.
-__device__ __forceinline__ uint32_t bin_of(int place) { return min((uint32_t)(-1 - place) >> 2, kBins - 1u); }
-// floor(f * v), f >= 0 an fp32 number below 1, and whether there is a remainder
+__device__ __forceinline__ uint32_t bin_of(int place) { return min((uint32_t)-place, kBins - 1u); }
+
+// floor(f * v) for 0 <= f < 1, v < 2^64, and whether there is a remainder.
 __device__ __forceinline__ uint64_t times(float f, uint64_t v, bool& more) {
   const uint32_t b = __float_as_uint(f), e = b >> 23, m = e ? (b & 0x7FFFFFu) | 0x800000u : b & 0x7FFFFFu;
   const int s = 150 - (int)(e ? e : 1u);  // f = m 2^-s, s >= 24
@@ -252,7 +289,7 @@ __device__ __forceinline__ uint64_t times(float f, uint64_t v, bool& more) {
   more = (lo & ((1ull << s) - 1ull)) != 0ull;
   return (hi << (64 - s)) | (lo >> s);
 }
-// The least integer not below f * v: as many units and more are not less than f * v.
+// The least integer not below f * v: a sum of weights is less than f * v exactly if it is less than this.
 __device__ __forceinline__ uint64_t bound_of(float f, uint64_t v) {
   if (!(f > 0.f)) return 0ull;
   bool more;
@@ -263,10 +300,13 @@ __device__ __forceinline__ uint64_t bound_of(float f, uint64_t v) {
 // Sorts list[0 .. n), n <= kList, from the largest down: by every entry's rank where there are few, else bitonic.
 __device__ void sort_list(uint64_t* list, uint32_t n, uint32_t tid) {
   if (n <= 128u) {
-    const uint64_t mine = tid < n ? list[tid] : 0ull;
+    uint64_t mine = 0ull;
     uint32_t rank = 0;
-    if (tid < n)
+    if (tid < n) {
+      mine = list[tid];
+#pragma unroll 8
       for (uint32_t i = 0; i < n; ++i) rank += list[i] > mine ? 1u : 0u;
+    }
     __syncthreads();
     if (tid < n) list[rank] = mine;
     __syncthreads();
@@ -295,58 +335,38 @@ template <int TYPE>
 __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams p) {
   extern __shared__ __align__(16) uint8_t smem[];
   Shared& sh = *reinterpret_cast<Shared*>(smem);
-  float* const xs = reinterpret_cast<float*>(smem + (sizeof(Shared) + 15u) / 16u * 16u);
+  float* const xs = reinterpret_cast<float*>(smem + kHead);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u, rank = cluster_rank(), ctas = cluster_size();
   const uint32_t row = blockIdx.x / ctas, from = min(rank * p.slice, p.vocab), n = min(p.slice, p.vocab - from);
-  if (tid < 256) sh.powers[tid] = make_uint2(kPowers.v[tid], __float_as_uint((float)kPowers.v[tid]));
+  if (tid < 32) sh.powers[tid] = make_uint2(kPowers.v[tid], __float_as_uint((float)kPowers.v[tid]));
   if (tid == 0) sh.listed = 0u;
   asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  const float temperature = p.temperature ? p.temperature[row] : 1.f;
+  const int32_t k_given = p.top_k ? p.top_k[row] : 0;
+  const float top_p = p.top_p ? p.top_p[row] : 1.f, min_p = p.min_p ? p.min_p[row] : 0.f;
+  const float u = p.uniform[row];
 
   uint32_t turn = 0;
-  // Two numbers of every thread added up (or the largest taken) over the CTA, then told to the whole cluster: of[r] is what CTA r had.
-  // warps[turn] keeps what the warps had.
-  auto all2 = [&](uint64_t& v0, uint64_t& v1, bool largest, uint64_t (&of0)[kMaxCluster]) {
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) {
-      const uint64_t a = __shfl_xor_sync(kFull, v0, d), b = __shfl_xor_sync(kFull, v1, d);
-      v0 = largest ? (a > v0 ? a : v0) : v0 + a;
-      v1 = largest ? (b > v1 ? b : v1) : v1 + b;
-    }
-    if (lane == 0) {
-      sh.warps[turn][warp][0] = v0;
-      sh.warps[turn][warp][1] = v1;
-    }
-    __syncthreads();
-    if (warp == 0) {
-      v0 = lane < kWarps ? sh.warps[turn][lane][0] : 0ull;
-      v1 = lane < kWarps ? sh.warps[turn][lane][1] : 0ull;
-#pragma unroll
-      for (int d = 8; d > 0; d >>= 1) {
-        const uint64_t a = __shfl_xor_sync(kFull, v0, d), b = __shfl_xor_sync(kFull, v1, d);
-        v0 = largest ? (a > v0 ? a : v0) : v0 + a;
-        v1 = largest ? (b > v1 ? b : v1) : v1 + b;
-      }
-      v0 = __shfl_sync(kFull, v0, 0);
-      v1 = __shfl_sync(kFull, v1, 0);
-      if (lane < ctas) {
-        store_remote(&sh.slots[turn][rank][0], lane, v0);
-        store_remote(&sh.slots[turn][rank][1], lane, v1);
-      }
-    }
+  // Tells what every warp has (the same in its lanes) to the whole cluster; a lane then has the entries of four warps, in the order of the vocabulary.
+  auto tell = [&](uint64_t v, uint64_t (&e)[4]) {
+    if (lane < ctas) store_remote(&sh.slots[turn][rank * kWarps + warp], lane, v);
     cluster_sync();
-    v0 = v1 = 0;
 #pragma unroll
-    for (uint32_t i = 0; i < kMaxCluster; ++i) {
-      of0[i] = i < ctas ? sh.slots[turn][i][0] : 0ull;
-      const uint64_t b = i < ctas ? sh.slots[turn][i][1] : 0ull;
-      v0 = largest ? (of0[i] > v0 ? of0[i] : v0) : v0 + of0[i];
-      v1 = largest ? (b > v1 ? b : v1) : v1 + b;
-    }
+    for (uint32_t i = 0; i < 4u; ++i) e[i] = lane * 4u + i < ctas * kWarps ? sh.slots[turn][lane * 4u + i] : 0ull;
     turn ^= 1u;
   };
-  uint64_t of[kMaxCluster];
+  // The sum over the cluster, and what is of the warps before this one.
+  auto all = [&](uint64_t mine, uint64_t& prev) {
+    uint64_t e[4], b = 0;
+    tell(warp_sum(mine), e);
+    const uint32_t at = rank * kWarps + warp;
+#pragma unroll
+    for (uint32_t i = 0; i < 4u; ++i) b += lane * 4u + i < at ? e[i] : 0ull;
+    prev = warp_sum(b);
+    return warp_sum(e[0] + e[1] + e[2] + e[3]);
+  };
 
   // ---- the row; its first token in falling order; the largest logit of every thread ------------------------
   float mine = -INFINITY;
@@ -401,48 +421,64 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   } else {
     for (uint32_t i = tid; i < n; i += kThreads) xs[i] = take(load1<TYPE>(p.logits, row_at + i), i);
   }
-  if (tid < 4u && n + tid < (n + 3u) / 4u * 4u) xs[n + tid] = -INFINITY;
+  if (tid < 4u && n + tid < (n + 3u) / 4u * 4u) xs[n + tid] = -INFINITY;  // four are read together
   asm volatile("barrier.cluster.wait.aligned;" ::: "memory");  // every CTA of the cluster runs: its shared memory can be written
-  uint64_t best = mine > -INFINITY ? order_of(mine, from + mine_at) : 0ull;
-  uint64_t lowest = mine > -INFINITY ? (uint64_t)~rising(mine) : 0ull;  // the least of the threads' maxima, turned round
-  all2(best, lowest, true, of);
-  const float temperature = p.temperature ? p.temperature[row] : 1.f;
+  uint64_t best;  // 0: nothing is above -inf
+  uint32_t least;  // of the threads' maxima
+  {
+    const uint32_t bits = mine > -INFINITY ? rising(mine) : 0u, top_bits = __reduce_max_sync(kFull, bits);
+    const uint32_t at = __reduce_min_sync(kFull, bits == top_bits ? from + mine_at : kIndexMask);
+    const uint32_t low = ~__reduce_min_sync(kFull, bits ? bits : 0xFFFFFFFFu);  // turned round: 0 where there is none
+    if (lane < ctas) store_remote(&sh.slots[2][rank * kWarps + warp], lane, low);
+    uint64_t e[4];
+    tell(top_bits ? ((uint64_t)top_bits << kIndexBits) | (kIndexMask - at) : 0ull, e);
+    best = max(max(e[0], e[1]), max(e[2], e[3]));
+    const uint32_t hi = __reduce_max_sync(kFull, (uint32_t)(best >> kIndexBits));
+    const uint32_t lo = __reduce_max_sync(kFull, (uint32_t)(best >> kIndexBits) == hi ? (uint32_t)best & kIndexMask : 0u);
+    best = hi ? ((uint64_t)hi << kIndexBits) | lo : 0ull;
+    uint32_t l = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < 4u; ++i)
+      if (lane * 4u + i < ctas * kWarps) l = max(l, (uint32_t)sh.slots[2][lane * 4u + i]);
+    least = ~__reduce_max_sync(kFull, l);
+  }
   if (best == 0ull || !(temperature > 0.f)) {
     if (rank == 0 && tid == 0) {
-      p.token[row] = best == 0ull ? -1 : (int32_t)(kIndexMask - (uint32_t)(best & kIndexMask));
+      p.token[row] = best == 0ull ? -1 : (int32_t)index_of(best);
       if (p.logprob) p.logprob[row] = best == 0ull ? -INFINITY : 0.f;
     }
     return;
   }
-  const float top = from_rising((uint32_t)(best >> kIndexBits));
+  if (logit_of(best) == INFINITY) {  // the infinite ones alone are kept, as equals: 0 takes their place, and -inf the others'
+    for (uint32_t i = tid; i < (n + 3u) / 4u * 4u; i += kThreads) xs[i] = xs[i] == INFINITY ? 0.f : -INFINITY;
+    mine = mine == INFINITY ? 0.f : -INFINITY;
+    least = rising(0.f);
+    best = order_of(0.f, index_of(best));
+    __syncthreads();
+  }
+  const float top = logit_of(best);
   Weights weight;
   weight.set(top, temperature, sh.powers);
-
-  const int32_t k_given = p.top_k ? p.top_k[row] : 0;
   const uint32_t k = k_given > 0 && (uint32_t)k_given < p.vocab ? (uint32_t)k_given : 0u;
-  const float top_p = p.top_p ? p.top_p[row] : 1.f, min_p = p.min_p ? p.min_p[row] : 0.f;
-  const float u = p.uniform[row];
+
   uint64_t keep = 0;  // tokens at or after this are kept
   if (min_p > 0.f) {  // the least logit with t >= log2(min_p), by a search of one warp over the numbers' order
     if (warp == 0) {
       uint32_t lo = rising(-INFINITY), hi = rising(top);  // hi is kept
-      if (min_p < 1.f && top < INFINITY) {
+      if (min_p < 1.f) {
         const uint32_t b = __float_as_uint(min_p), e = b >> 23;
-        const Pair edge = e ? log2_of((b & 0x7FFFFFu | 0x800000u) << 6, (int)e - 127, sh.powers) : log2_of((uint64_t)b, 149, sh.powers);
+        const Pair edge = e ? log2_of(((b & 0x7FFFFFu) | 0x800000u) << 6, (int)e - 127, sh.powers) : log2_of((uint64_t)b, 149, sh.powers);
         while (lo < hi) {
-          const uint32_t step = (hi - lo) / 33u + 1u;
-          const uint32_t at = min(lo + (lane + 1u) * step - 1u, hi);  // rising over the lanes
+          const uint32_t step = (hi - lo) / 33u + 1u, at = min(lo + (lane + 1u) * step - 1u, hi);  // rising over the lanes
           const float x = from_rising(at);
           const Pair t = weight.both(x);
-          const bool in = at == hi || x == top || (!weight.none(x) && (t.hi - edge.hi) + (t.lo - edge.lo) >= 0.f);
+          const bool in = at == hi || (x > -INFINITY && (t.hi - edge.hi) + (t.lo - edge.lo) >= 0.f);
           const uint32_t votes = __ballot_sync(kFull, in);
           const uint32_t first = votes ? __ffs(votes) - 1u : 32u;  // the first lane whose number is kept
-          const uint32_t new_lo = first ? min(lo + first * step, hi) : lo;
+          const uint32_t new_lo = min(lo + first * step, hi);
           hi = first < 32u ? min(lo + (first + 1u) * step - 1u, hi) : hi;
           lo = new_lo;
         }
-      } else {
-        lo = hi;
       }
       if (lane == 0) sh.told[1] = hi;
     }
@@ -455,9 +491,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     bool more;
     return u > 0.f ? times(u, total, more) : 0ull;  // below the total
   };
-  auto answer = [&](uint32_t index, float x, uint64_t total) {
-    p.token[row] = (int32_t)index;
+  auto answer = [&](uint64_t order, uint64_t total) {
+    p.token[row] = (int32_t)index_of(order);
     if (p.logprob) {  // ln 2 (t - log2(total / 2^45))
+      const float x = logit_of(order);
       const Pair sum = log2_of(total, kOne, sh.powers);
       const Pair t = x == top ? Pair{0.f, 0.f} : weight.both(x);
       const Pair d = exact_sum(t.hi, -sum.hi);
@@ -465,14 +502,43 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
       p.logprob[row] = h + fmaf(low, kLn2, fmaf(d.hi, kLn2Low, fmaf(d.hi, kLn2, -h)));
     }
   };
+  // warps own consecutive pieces of the slice, a lane four consecutive logits of 128
+  const uint32_t piece = (n + 4u * kThreads - 1u) / (4u * kThreads) * 128u, w0 = min(warp * piece, n), w1 = min(w0 + piece, n);
+  auto read4 = [&](uint32_t i, float (&x)[4]) {
+    const float4 y = i < w1 ? *reinterpret_cast<const float4*>(xs + i) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+    x[0] = y.x, x[1] = y.y, x[2] = y.z, x[3] = y.w;  // past the slice's end lies -inf
+  };
+  // Entries of a warp's lanes into the first CTA's list, in no order.
+  auto list4 = [&](const float (&x)[4], uint32_t i, uint32_t mask) {
+    const uint32_t own = __popc(mask), upto = warp_upto(own, lane);
+    uint32_t at = 0;
+    if (lane == 31) at = add_remote(&sh.listed, 0u, upto);
+    at = __shfl_sync(kFull, at, 31) + upto - own;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (!((mask >> j) & 1u)) continue;
+      if (at < kList) store_remote(&sh.list[at], 0u, order_of(x[j], from + i + j));
+      ++at;
+    }
+  };
+  constexpr uint32_t kEach = kList / kThreads;  // consecutive entries of the list to a thread
+  // Sums over the threads of a CTA, and what is of the threads before.
+  auto scan = [&](uint64_t sum, uint64_t& total) {
+    const uint64_t upto = warp_upto(sum, lane);
+    __syncthreads();
+    if (lane == 31) sh.warps[warp] = upto;
+    __syncthreads();
+    const uint64_t w = lane < kWarps ? sh.warps[lane] : 0ull;
+    total = warp_sum(w);
+    return warp_sum(lane < warp ? w : 0ull) + upto - sum;
+  };
 
   // Bisection of the order: the last place before which less than `bound` (a weight, or a number) lies.
   auto before = [&](uint64_t order, bool count) {
-    uint64_t v = 0, zero = 0;
+    uint64_t v = 0, prev;
     for (uint32_t i = tid; i < n; i += kThreads)
       if (order_of(xs[i], from + i) > order) v += count ? 1ull : weight(xs[i]);
-    all2(v, zero, false, of);
-    return v;
+    return all(v, prev);
   };
   auto border = [&](uint64_t bound, bool count, uint64_t lo) {
     uint64_t hi = best;  // nothing is before it
@@ -485,123 +551,59 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     }
     return hi;
   };
-  // warps own consecutive pieces of the slice, a lane four consecutive logits of 128
-  const uint32_t piece = (n + 4u * kThreads - 1u) / (4u * kThreads) * 128u, w0 = min(warp * piece, n), w1 = min(w0 + piece, n);
-  auto read4 = [&](uint32_t i, uint32_t end, float (&x)[4]) {
-    const float4 y = i < end ? *reinterpret_cast<const float4*>(xs + i) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-    x[0] = y.x, x[1] = y.y, x[2] = y.z, x[3] = y.w;  // past the slice's end lies -inf
-  };
   const bool p_on = top_p < 1.f;
   bool searched = !p_on && k == 0u;  // the border is known
 
-  if (!searched && k != 0u && k <= kListK) {
+  if (k != 0u && k <= kListK) {
     // ---- top-k: a bound from the threads' maxima, and a list -----------------------------------------------
     for (uint32_t i = tid; i < kKBins; i += kThreads) sh.k_bins[i] = 0u;
     __syncthreads();
-    const float low = from_rising(~(uint32_t)lowest), span = top - low;
-    // bins fall with x; equal logits, and infinite ones, are all in the first
-    const float scale = span > 0.f && span < INFINITY ? (float)(kKBins - 1u) / span : 0.f;
-    auto k_bin = [&](float x) { return scale == 0.f ? (x == top || span < INFINITY ? 0u : kKBins - 1u) : min((uint32_t)((top - x) * scale), kKBins - 1u); };
-    if (mine > -INFINITY) atomicAdd(&sh.k_bins[k_bin(mine)], 1u);
+    // bins that fall with x from the largest logit to the least of the maxima; what is below is in the last
+    const float span = top - from_rising(least), scale = span > 0.f && span < INFINITY ? (float)(kKBins - 1u) / span : 0.f;
+    auto bin_at = [&](float x) { return min((uint32_t)((top - x) * scale), kKBins - 1u); };
+    if (mine > -INFINITY) atomicAdd(&sh.k_bins[bin_at(mine)], 1u);
     cluster_sync();
     uint32_t in_bin = 0;
-    if (tid < kKBins)
-      for (uint32_t r = 0; r < ctas; ++r) in_bin += load_remote(&sh.k_bins[tid], r);
-    uint32_t upto = in_bin;
+    if (tid < kKBins) {
+      uint32_t c[kMaxCluster];
 #pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const uint32_t o = __shfl_up_sync(kFull, upto, d);
-      if (lane >= (uint32_t)d) upto += o;
+      for (uint32_t r = 0; r < kMaxCluster; ++r) c[r] = r < ctas ? load_remote(&sh.k_bins[tid], r) : 0u;
+#pragma unroll
+      for (uint32_t r = 0; r < kMaxCluster; ++r) in_bin += c[r];
     }
-    if (lane == 31) sh.warps[turn][warp][0] = upto;
-    __syncthreads();
-    uint32_t earlier = 0;
-    for (uint32_t i = 0; i < min(warp, kKBins / 32u); ++i) earlier += (uint32_t)sh.warps[turn][i][0];
-    upto += earlier;
+    uint64_t maxima;
+    const uint32_t ahead = (uint32_t)scan(in_bin, maxima);
     if (tid == 0) sh.told[0] = kKBins - 1u;  // fewer maxima than k: nothing is left out
     __syncthreads();
-    if (tid < kKBins && upto >= k && upto - in_bin < k) sh.told[0] = tid;
-    __syncthreads();
+    if (ahead < k && ahead + in_bin >= k) sh.told[0] = tid;
+    cluster_sync();  // every CTA has read the bins: the list may lie over them
     const uint32_t cut = (uint32_t)sh.told[0];
-    // the same products as in k_bin, compared with the bin's end
-    const float last_bin = scale == 0.f ? 0.f : (float)(cut + 1u);
-    const bool all_bins = cut == kKBins - 1u;
-    auto listed = [&](float x) { return x > -INFINITY && (all_bins || (scale == 0.f ? k_bin(x) <= cut : (top - x) * scale < last_bin)); };
-    uint32_t count = 0;
-    for (uint32_t i = w0 + 4u * lane; i < w1; i += 128u) {
+    // the products of bin_at, compared with the bin's end; where all are alike, or in the last bin, everything is listed
+    const float end = cut == kKBins - 1u || scale == 0.f ? INFINITY : (float)(cut + 1u);
+    for (uint32_t i0 = w0; i0 < w1; i0 += 128u) {
       float x[4];
-      read4(i, w1, x);
+      read4(i0 + 4u * lane, x);
+      uint32_t mask = 0;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) count += listed(x[j]) ? 1u : 0u;
+      for (int j = 0; j < 4; ++j) mask |= x[j] > -INFINITY && (top - x[j]) * scale < end ? 1u << j : 0u;
+      if (__any_sync(kFull, mask != 0u)) list4(x, i0 + 4u * lane, mask);
     }
-    uint64_t v = count, zero = 0;
-    const uint32_t last = turn;
-    all2(v, zero, false, of);  // (also: every CTA has read the bins, the list may lie over them)
-    if (v <= kList) {
-      // the list in the order of the vocabulary, in the first CTA
-      uint32_t at = 0;
-      for (uint32_t i = 0; i < rank; ++i) at += (uint32_t)of[i];
-      for (uint32_t i = 0; i < warp; ++i) at += (uint32_t)sh.warps[last][i][0];
-      for (uint32_t i0 = w0; i0 < w1; i0 += 128u) {
-        const uint32_t i = i0 + 4u * lane;
-        float x[4];
-        read4(i, w1, x);
-        uint32_t mask = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) mask |= listed(x[j]) ? 1u << j : 0u;
-        if (!__any_sync(kFull, mask != 0u)) continue;
-        const uint32_t own = __popc(mask);
-        uint32_t upto = own;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-          const uint32_t o = __shfl_up_sync(kFull, upto, d);
-          if (lane >= (uint32_t)d) upto += o;
-        }
-        uint32_t to = at + upto - own;
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if ((mask >> j) & 1u) store_remote(&sh.list[to++], 0u, order_of(x[j], from + i + j));
-        at += __shfl_sync(kFull, upto, 31);
-      }
-      cluster_sync();
+    cluster_sync();
+    const uint32_t m = load_remote(&sh.listed, 0u);
+    if (m <= kList) {
+      asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // the first CTA stays until all have read that
       if (rank != 0) return;
-      const uint32_t m = (uint32_t)v;
-      constexpr uint32_t kEach = kList / kThreads;  // consecutive entries of a thread
-      uint64_t own[kEach];                          // in the order of the vocabulary
-#pragma unroll
-      for (uint32_t i = 0; i < kEach; ++i) own[i] = tid * kEach + i < m ? sh.list[tid * kEach + i] : 0ull;
-      __syncthreads();
       sort_list(sh.list, m, tid);
-      // sums of weights over the threads' entries, and what is before them
-      auto scan = [&](uint64_t sum, uint64_t& total) {
-        uint64_t incl = sum;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-          const uint64_t o = __shfl_up_sync(kFull, incl, d);
-          if (lane >= (uint32_t)d) incl += o;
-        }
-        __syncthreads();
-        if (lane == 31) sh.warps[0][warp][0] = incl;
-        __syncthreads();
-        total = 0;
-        uint64_t prev = 0;
-        for (uint32_t i = 0; i < kWarps; ++i) {
-          const uint64_t o = sh.warps[0][i][0];
-          prev += i < warp ? o : 0ull;
-          total += o;
-        }
-        return prev + incl - sum;
-      };
       uint32_t kept = min(k, m);
+      uint64_t w[kEach], sum = 0, total, prev;
       if (p_on) {
-        uint64_t w[kEach], sum = 0, total;
 #pragma unroll
         for (uint32_t i = 0; i < kEach; ++i) {
           const uint32_t j = tid * kEach + i;
-          w[i] = j < kept ? weight(from_rising((uint32_t)(sh.list[j] >> kIndexBits))) : 0ull;
+          w[i] = j < kept ? weight(logit_of(sh.list[j])) : 0ull;
           sum += w[i];
         }
-        uint64_t prev = scan(sum, total);
+        prev = scan(sum, total);
         const uint64_t bound = bound_of(top_p, total);
         uint32_t in = 0;
 #pragma unroll
@@ -609,39 +611,56 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
           in += tid * kEach + i < kept && prev < bound ? 1u : 0u;
           prev += w[i];
         }
-        uint64_t sum_in;
-        scan(in, sum_in);
-        kept = max(1u, (uint32_t)sum_in);
+        scan(in, total);
+        kept = max(1u, (uint32_t)total);
       }
-      const uint64_t edge = sh.list[kept - 1u];
-      keep = min(max(keep, edge), best);
-      uint64_t w[kEach], sum = 0, total;
+      if (keep != 0ull) {  // min-p
+        uint32_t in = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < kEach; ++i) in += tid * kEach + i < kept && sh.list[tid * kEach + i] >= min(keep, best) ? 1u : 0u;
+        scan(in, total);
+        kept = (uint32_t)total;
+      }
+      // those in the order of the vocabulary
+      uint64_t own[kEach];
+      __syncthreads();
 #pragma unroll
       for (uint32_t i = 0; i < kEach; ++i) {
-        w[i] = own[i] != 0ull && own[i] >= keep ? weight(from_rising((uint32_t)(own[i] >> kIndexBits))) : 0ull;
+        const uint32_t j = tid * kEach + i;
+        if (j < kept) sh.list[j] = (sh.list[j] & kIndexMask) << 32 | sh.list[j] >> kIndexBits;
+      }
+      __syncthreads();
+      sort_list(sh.list, kept, tid);
+      sum = 0;
+#pragma unroll
+      for (uint32_t i = 0; i < kEach; ++i) {
+        const uint32_t j = tid * kEach + i;
+        own[i] = j < kept ? sh.list[j] << kIndexBits & (0xFFFFFFFFull << kIndexBits) | sh.list[j] >> 32 : 0ull;
+        w[i] = j < kept ? weight(logit_of(own[i])) : 0ull;
         sum += w[i];
       }
-      uint64_t prev = scan(sum, total);
+      prev = scan(sum, total);
       const uint64_t target = target_of(total);
       if (target >= prev && target < prev + sum) {
 #pragma unroll
         for (uint32_t i = 0; i < kEach; ++i) {
-          if (target >= prev && target < prev + w[i])
-            answer(kIndexMask - (uint32_t)(own[i] & kIndexMask), from_rising((uint32_t)(own[i] >> kIndexBits)), total);
+          if (target >= prev && target < prev + w[i]) answer(own[i], total);
           prev += w[i];
         }
       }
+      asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
       return;
     }
   }
   if (!searched && k == 0u) {
     // ---- top-p: a histogram of the weights, and a list of the bin with the border -----------------------------
     for (uint32_t i = tid; i < kBins; i += kThreads) sh.bins.hi[i] = sh.bins.lo[i] = 0u;
+    if (tid == 0) sh.told[0] = ~0ull;
     __syncthreads();
     uint64_t rest = 0;  // of the octaves below
     for (uint32_t i0 = w0; i0 < w1; i0 += 128u) {
       float x[4];
-      read4(i0 + 4u * lane, w1, x);
+      read4(i0 + 4u * lane, x);
       weight.four(x, [&](int, bool fine, int place, uint32_t v) {
         if (fine) {
           const uint32_t b = bin_of(place);
@@ -653,87 +672,59 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
       });
     }
     cluster_sync();
-    // this CTA's bins of all CTAs: kBins / ctas consecutive ones, up to three to a thread
-    const uint32_t share = kBins / ctas, each = (share + kThreads - 1u) / kThreads, first = rank * share + tid * each;
-    uint64_t mass[3] = {0, 0, 0}, sum = 0;
-    for (uint32_t j = 0; j < each; ++j) {
-      if (tid * each + j >= share) break;
-      uint64_t hi = 0, lo = 0;
-      for (uint32_t r = 0; r < ctas; ++r) {
-        hi += load_remote(&sh.bins.hi[first + j], r);
-        lo += load_remote(&sh.bins.lo[first + j], r);
+    // this CTA's bins of all CTAs: consecutive ones, up to two to a thread
+    const uint32_t share = (kBins + ctas - 1u) / ctas, each = (share + kThreads - 1u) / kThreads;
+    uint64_t mass[2] = {0, 0};
+#pragma unroll
+    for (uint32_t j = 0; j < 2u; ++j) {
+      const uint32_t mine_of = tid * each + j, b = rank * share + mine_of;
+      if (j >= each || mine_of >= share || b >= kBins) continue;
+      uint32_t hi[kMaxCluster], lo[kMaxCluster];
+#pragma unroll
+      for (uint32_t r = 0; r < kMaxCluster; ++r) {
+        hi[r] = r < ctas ? load_remote(&sh.bins.hi[b], r) : 0u;
+        lo[r] = r < ctas ? load_remote(&sh.bins.lo[b], r) : 0u;
       }
-      const uint64_t m = ((hi << 15) + lo) << Weights::shift(-1 - 4 * (int)(first + j));
-      if (j == 0) mass[0] = m;
-      if (j == 1) mass[1] = m;
-      if (j == 2) mass[2] = m;
-      sum += m;
-    }
-    uint64_t total = sum, all_rest = rest;
-    const uint32_t last = turn;
-    uint64_t incl = sum;
+      uint64_t sum_hi = 0, sum_lo = 0;
 #pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const uint64_t o = __shfl_up_sync(kFull, incl, d);
-      if (lane >= (uint32_t)d) incl += o;
+      for (uint32_t r = 0; r < kMaxCluster; ++r) sum_hi += hi[r], sum_lo += lo[r];
+      mass[j] = ((sum_hi << 15) + sum_lo) << Weights::shift(-(int)b);
     }
-    if (tid == 0) sh.told[0] = ~0ull;
-    all2(total, all_rest, false, of);
-    const uint64_t bound = bound_of(top_p, total + all_rest);
-    uint64_t prev = incl - sum;
-    for (uint32_t i = 0; i < rank; ++i) prev += of[i];
-    for (uint32_t i = 0; i < warp; ++i) prev += sh.warps[last][i][0];
-    if (bound != 0ull) {
+    uint64_t ahead, before_rest;
+    const uint64_t sum = mass[0] + mass[1], upto = warp_upto(sum, lane), binned = all(sum, ahead), total = binned + all(rest, before_rest);
+    const uint64_t bound = bound_of(top_p, total);
+    uint64_t prev = ahead + upto - sum;
 #pragma unroll
-      for (uint32_t j = 0; j < 3u; ++j) {
-        if (j < each && mass[j] != 0ull && prev < bound && prev + mass[j] >= bound) {
-          for (uint32_t r = 0; r < ctas; ++r) {
-            store_remote(&sh.told[0], r, first + j);
-            store_remote(&sh.told[1], r, prev);
-          }
+    for (uint32_t j = 0; j < 2u; ++j) {
+      if (mass[j] != 0ull && prev < bound && prev + mass[j] >= bound) {
+        for (uint32_t r = 0; r < ctas; ++r) {
+          store_remote(&sh.told[0], r, rank * share + tid * each + j);
+          store_remote(&sh.told[1], r, prev);
         }
-        prev += mass[j];
       }
+      prev += mass[j];
     }
-    cluster_sync();  // (also: every CTA has read the bins, the list may lie over them)
-    const uint64_t bin = sh.told[0], ahead = sh.told[1];
+    cluster_sync();  // (every CTA has read the bins, the list may lie over them)
+    const uint64_t bin = sh.told[0], up_to_bin = sh.told[1];
     if (bound == 0ull) {
       keep = best;
       searched = true;
     } else if (bin != ~0ull) {
-      // the bin's logits lie between these, give or take the roundings of fp32: only there is the bin looked at
-      const float t_hi = (float)bin * -0.015625f, t_lo = t_hi - 0.015625f;
+      // the bin's logits lie about here (a place is rounded to 1/32 after a, which is off by up to 1/64 and a little): only there is the bin looked at
+      const float t_hi = (float)bin * -0.03125f + 0.04f, t_lo = t_hi - 0.08f;
       for (uint32_t i0 = w0; i0 < w1; i0 += 128u) {
-        const uint32_t i = i0 + 4u * lane;
         float x[4];
-        read4(i, w1, x);
+        read4(i0 + 4u * lane, x);
         uint32_t mask = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          if (weight.none(x[j])) continue;
           const float t = weight.coarse(x[j]);
-          if (t < t_lo - 0.01f || t > t_hi + 0.01f || t < -(float)kOctaves) continue;  // (a place is rounded to 1/256)
+          if (x[j] == -INFINITY || t < t_lo || t > t_hi || t < -(float)kOctaves) continue;
           int place;
           weight.fine(x[j], place);
           if (bin_of(place) == (uint32_t)bin) mask |= 1u << j;
         }
-        if (!__any_sync(kFull, mask != 0u)) continue;
-        const uint32_t own = __popc(mask);
-        uint32_t upto = own;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-          const uint32_t o = __shfl_up_sync(kFull, upto, d);
-          if (lane >= (uint32_t)d) upto += o;
-        }
-        uint32_t at = 0;
-        if (lane == 31) at = add_remote(&sh.listed, 0u, upto);
-        at = __shfl_sync(kFull, at, 31) + upto - own;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (!((mask >> j) & 1u)) continue;
-          if (at < kList) store_remote(&sh.list[at], 0u, order_of(x[j], from + i + j));
-          ++at;
-        }
+        if (__any_sync(kFull, mask != 0u)) list4(x, i0 + 4u * lane, mask);
       }
       cluster_sync();
       const uint32_t m = load_remote(&sh.listed, 0u);
@@ -741,36 +732,25 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
         if (rank == 0) {
           sort_list(sh.list, m, tid);
           // the last entry before which less than the bound lies
-          constexpr uint32_t kEach = kList / kThreads;
-          uint64_t w[kEach], sum = 0, incl;
+          uint64_t w[kEach], own = 0, in_bin;
 #pragma unroll
           for (uint32_t i = 0; i < kEach; ++i) {
             const uint32_t j = tid * kEach + i;
-            w[i] = j < m ? weight(from_rising((uint32_t)(sh.list[j] >> kIndexBits))) : 0ull;
-            sum += w[i];
+            w[i] = j < m ? weight(logit_of(sh.list[j])) : 0ull;
+            own += w[i];
           }
-          incl = sum;
-#pragma unroll
-          for (int d = 1; d < 32; d <<= 1) {
-            const uint64_t o = __shfl_up_sync(kFull, incl, d);
-            if (lane >= (uint32_t)d) incl += o;
-          }
-          if (lane == 31) sh.warps[turn][warp][0] = incl;
-          __syncthreads();
-          uint64_t prev = ahead + incl - sum;
-          for (uint32_t i = 0; i < warp; ++i) prev += sh.warps[turn][i][0];
+          uint64_t at = up_to_bin + scan(own, in_bin);
 #pragma unroll
           for (uint32_t i = 0; i < kEach; ++i) {
             const uint32_t j = tid * kEach + i;
-            if (j < m && prev < bound && (j + 1u == m || prev + w[i] >= bound)) {
+            if (j < m && at < bound && (j + 1u == m || at + w[i] >= bound)) {
               for (uint32_t r = 0; r < ctas; ++r) store_remote(&sh.told[0], r, sh.list[j]);
             }
-            prev += w[i];
+            at += w[i];
           }
-          __syncthreads();
         }
         cluster_sync();
-        keep = min(max(keep, sh.told[0]), best);
+        keep = max(keep, sh.told[0]);
         searched = true;
       }
     }
@@ -787,52 +767,41 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   keep = min(keep, best);
 
   // ---- the token up to which more than u of the kept sum lies ---------------------------------------
-  const float keep_x = from_rising((uint32_t)(keep >> kIndexBits));  // below it nothing is kept
+  const float keep_x = logit_of(keep);  // below it nothing is kept
+  const uint32_t keep_at = index_of(keep);  // and of its equals the first ones
   // weights of four logits, 0 where they are not kept
   auto kept = [&](uint32_t i, uint64_t (&w)[4]) {
     float x[4];
-    read4(i, w1, x);
-    bool any = false;
+    read4(i, x);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if (x[j] < keep_x || order_of(x[j], from + i + j) < keep) x[j] = -INFINITY;
-      any = any || x[j] > -INFINITY;
+      if (x[j] < keep_x || (x[j] == keep_x && from + i + j > keep_at)) x[j] = -INFINITY;
       w[j] = 0ull;
     }
-    if (!__any_sync(kFull, any)) return;
+    if (!__any_sync(kFull, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) > -INFINITY)) return false;
     weight.four(x, [&](int j, bool fine, int place, uint32_t v) { w[j] = fine ? (uint64_t)v << Weights::shift(place) : v; });
+    return true;
   };
-  uint64_t sum_mine = 0, zero = 0;
+  uint64_t sum_mine = 0, sum;
   for (uint32_t i0 = w0; i0 < w1; i0 += 128u) {
     uint64_t w[4];
     kept(i0 + 4u * lane, w);
-    sum_mine += w[0] + w[1] + w[2] + w[3];
+    sum_mine += (w[0] + w[1]) + (w[2] + w[3]);
   }
-  const uint32_t last = turn;
-  all2(sum_mine, zero, false, of);
-  const uint64_t total = sum_mine, target = target_of(total);
-  uint64_t sum = 0;
-  for (uint32_t i = 0; i < rank; ++i) sum += of[i];
-  for (uint32_t i = 0; i < warp; ++i) sum += sh.warps[last][i][0];
-  if (target < sum || target >= sum + sh.warps[last][warp][0]) return;  // another warp has it
+  const uint64_t of_warp = warp_sum(sum_mine), total = all(sum_mine, sum), target = target_of(total);
+  if (target < sum || target >= sum + of_warp) return;  // another warp has it
   for (uint32_t i0 = w0; i0 < w1; i0 += 128u) {
     const uint32_t i = i0 + 4u * lane;
     uint64_t w[4];
-    kept(i, w);
-    const uint64_t own = w[0] + w[1] + w[2] + w[3];
-    uint64_t upto = own;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const uint64_t o = __shfl_up_sync(kFull, upto, d);
-      if (lane >= (uint32_t)d) upto += o;
-    }
+    if (!kept(i, w)) continue;
+    const uint64_t own = (w[0] + w[1]) + (w[2] + w[3]), upto = warp_upto(own, lane);
     const uint32_t past = __ballot_sync(kFull, sum + upto > target);
     if (past) {
       if (lane == __ffs(past) - 1u) {
         sum += upto - own;
         uint32_t j = 0;
         while (j < 3u && sum + w[j] <= target) sum += w[j++];
-        answer(from + i + j, xs[i + j], total);
+        answer(order_of(xs[i + j], from + i + j), total);
       }
       return;
     }
@@ -850,7 +819,6 @@ int launch(SampleParams& p, uint32_t rows, cudaStream_t st) {
   p.slice = ((p.vocab + ctas - 1u) / ctas + 7u) / 8u * 8u;
   p.vectors = ((uintptr_t)p.logits & 15u) == 0 && (rows == 1 || (p.row_stride * (TYPE == TQ_TYPE_F32 ? 4 : 2)) % 16 == 0);
   const char* what = "sample launch";
-  constexpr size_t kHead = (sizeof(Shared) + 15u) / 16u * 16u;
   if (int rc = tq_ensure_dynamic_smem((const void*)kern, kHead + TQ_SAMPLE_MAX_VOCAB / kMaxCluster * sizeof(float), what)) return rc;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(rows * ctas);
