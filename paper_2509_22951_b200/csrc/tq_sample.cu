@@ -5,8 +5,8 @@
 // weight is therefore an integer W = round(2^45 w), and sums of up to 2^18 of them are exact in 64 bits whatever their
 // order, so that neither the split of a row nor the order of atomics can change a token.  With A a multiple of 1/32 next to max log2(e) / temperature,
 // one fused multiply-add rounds t to 1/32 and another, which takes that from the exact product again, leaves the rest to 2^-31: the first is a
-// place in a table of 2^(i/32) (a bank of shared memory for each entry) and an octave, the second goes into a polynomial: 27 bits and more in some
-// 25 instructions.  W below 2^21 (t < -24) is the fp32 exponential, to some units.
+// place in a table of 2^(i/32) (a bank of shared memory for each entry) and an octave, the second goes into a polynomial: 26 bits and more in some
+// 25 instructions, none of them a conversion.  W below 2^21 (t < -24) is the fp32 exponential, to some units.
 //
 // Order.  Tokens fall by (x, lower index first): as one integer, the logit's bits made to rise with it above the index turned
 // round.  What is kept is all that is not below a border in that order, so every filter is a search for its border.
@@ -79,7 +79,7 @@ struct Shared {
   uint64_t slots[3][kMaxCluster * kWarps];  // what the cluster's warps tell one another; two sets, used in turn, and one for the start
   uint64_t told[2];                         // by one CTA to all
   uint64_t warps[kWarps];                   // within a CTA
-  uint2 powers[32];                         // 2^(i / 32) with 29 bits behind the point, and as fp32
+  uint32_t powers[32];                      // 2^(i / 32) with 29 bits behind the point
   uint32_t listed;                          // tokens in the list (of the first CTA)
   union {
     struct {
@@ -169,14 +169,14 @@ constexpr float kLn2 = 0.693147182464599609375f, kLn2Low = -1.904654323148236e-0
 constexpr float kLog2e = 1.44269502162933349609375f, kLog2eLow = 1.92596303178237e-08f;  // 1 / ln 2
 
 // log2(m 2^(k - 29)), 2^29 <= m < 2^30, to 2^-29: the table's entry below m, and a series for the rest.
-__device__ __forceinline__ Pair log2_of(uint32_t m, int k, const uint2* powers) {
+__device__ __forceinline__ Pair log2_of(uint32_t m, int k, const uint32_t* powers) {
   int i = min(max((int)((__log2f((float)m) - 29.f) * 32.f), 0), 31);
-  if (powers[i].x > m && i > 0) --i;
-  const float z = (float)(int32_t)(m - powers[i].x) / __uint_as_float(powers[i].y);  // 0 .. 0.022
+  if (powers[i] > m && i > 0) --i;
+  const float z = (float)(int32_t)(m - powers[i]) / (float)powers[i];  // 0 .. 0.022
   const float y = z * (1.f + z * (-0.5f + z * (0.33333334f + z * (-0.25f + z * (0.2f - z * 0.16666667f)))));
   return Pair{(float)k + (float)i * 0.03125f, fmaf(y, kLog2e, y * kLog2eLow)};
 }
-__device__ __forceinline__ Pair log2_of(uint64_t v, int one, const uint2* powers) {  // log2(v 2^-one)
+__device__ __forceinline__ Pair log2_of(uint64_t v, int one, const uint32_t* powers) {  // log2(v 2^-one)
   const int top = 63 - __clzll((long long)v);
   return log2_of(top >= 29 ? (uint32_t)(v >> (top - 29)) : (uint32_t)v << (29 - top), top - one, powers);
 }
@@ -187,9 +187,9 @@ struct Weights {
   float c, c_low;     // log2(e) / temperature
   float a, a_low;     // top * log2(e) / temperature: a multiple of 1/32, and the rest
   bool plain;         // a is small enough for the short form
-  const uint2* powers;
+  const uint32_t* powers;
 
-  __device__ __forceinline__ void set(float top_, float temperature, const uint2* powers_) {
+  __device__ __forceinline__ void set(float top_, float temperature, const uint32_t* powers_) {
     top = top_;
     powers = powers_;
     c = c_low = 0.f;
@@ -210,48 +210,51 @@ struct Weights {
     const float t = d.hi * c;
     return Pair{t, fmaf(d.lo, c, fmaf(d.hi, c_low, fmaf(d.hi, c, -t)))};
   }
-  // For t from 0 down to some octaves below the histogram's, and NaN, which is taken for 0.
-  __device__ __forceinline__ uint32_t fine(float x, int& place) const {
-    constexpr float kRound = 393216.0f;  // 1.5 * 2^18: sums with it are rounded to 1/32
-    float r;
+  // 2^t = 2^(place / 32) (1 + q 2^-26), for t from 0 down to some octaves below the histogram's, and NaN, which is taken for 0.
+  __device__ __forceinline__ int fine(float x, int& place) const {
+    constexpr float kRound = 393216.0f, kQUnit = 67108864.0f;  // 1.5 * 2^18: sums with it are rounded to 1/32
+    float r, s;
     if (plain) {
-      const float k = kRound - a, s = fmaf(x, c, k);
+      const float k = kRound - a;
+      s = fmaf(x, c, k);
       place = __float_as_int(s) - 0x48C00000;
       r = fmaf(x, c, k - s) + fmaf(x, c_low, -a_low);
     } else {
       const Pair t = both(x);
-      const float s = t.hi + kRound;
+      s = t.hi + kRound;
       place = __float_as_int(s) - 0x48C00000;
       r = (t.hi - (s - kRound)) + t.lo;
     }
     if (place > 0) {  // the largest logit, where a is that far from the exact product
-      r += (float)place * 0.03125f;
+      r += s - kRound;
       place = 0;
     }
-    const uint2 base = powers[place & 31];
     constexpr float a2 = 0.24022651f, a3 = 0.055504109f, a4 = 0.0096181291f;  // (ln 2)^k / k!
     const float q = r * fmaf(r, fmaf(r, fmaf(r, a4, a3), a2), kLn2);
-    // rounded to whole units of 2^-29
-    const uint32_t v = base.x + (uint32_t)__float2int_rn(__uint_as_float(base.y) * q);
-    const int down = -16 - (place >> 5);
-    return down > 0 ? (v + (1u << (down - 1))) >> down : v;
+    return __float_as_int(fmaf(q, kQUnit, 12582912.0f)) - 0x4B400000;  // q to whole units of 2^-26, |q| < 0.031
+  }
+  // The value of a place and its q.
+  __device__ __forceinline__ uint32_t value(int place, int q) const {
+    const uint32_t base = powers[place & 31];
+    const uint32_t v = base + (uint32_t)(((int64_t)base * q) >> 26), down = (uint32_t)max(-16 - (place >> 5), 0);
+    return (v + ((1u << down) >> 1)) >> down;
   }
   __device__ __forceinline__ static int shift(int place) { return max(0, 16 + (place >> 5)); }
   // Octaves below the histogram's; 0 for -inf.
   __device__ __forceinline__ uint32_t small(float t) const {
     float w;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(w) : "f"(t + (float)kOne));
-    return __float2uint_rn(w);
+    return __float_as_uint(w + 8388608.0f) - 0x4B000000u;  // rounded
   }
   __device__ __forceinline__ uint64_t operator()(float x) const {
     const float t = coarse(x);
     if (x == -INFINITY || t < -(float)kOctaves) return x == -INFINITY ? 0u : small(t);
     int place;
-    const uint32_t v = fine(x, place);
-    return (uint64_t)v << shift(place);
+    const int q = fine(x, place);
+    return (uint64_t)value(place, q) << shift(place);
   }
-  // Four at once, for a whole warp: the chains of fine() side by side, or none of them where all weights are small.  use(j, is fine, place,
-  // value) for each; value is 0 where there is no weight.
+  // Four at once, for a whole warp: the chains of fine() side by side, or none of them where all weights are small.  use(j, is fine, place, q)
+  // for each, or with its weight in q's place where that is small.
   template <class Use>
   __device__ __forceinline__ void four(const float (&x)[4], Use use) const {
     float t[4];
@@ -260,21 +263,22 @@ struct Weights {
     const float most = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));  // (a NaN beside numbers is dropped here: all of a row are, or none)
     if (!__any_sync(kFull, !(most < -(float)kOctaves))) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) use(j, false, 0, small(t[j]));
+      for (int j = 0; j < 4; ++j) use(j, false, 0, (int)small(t[j]));
       return;
     }
-    int place[4];
-    uint32_t v[4];
+    int place[4], q[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = fine(t[j] < -(float)kOctaves ? top : x[j], place[j]);
+    for (int j = 0; j < 4; ++j) q[j] = fine(t[j] < -(float)kOctaves ? top : x[j], place[j]);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const bool is_small = t[j] < -(float)kOctaves;
-      use(j, !is_small, place[j], is_small ? small(t[j]) : v[j]);
+      use(j, !is_small, place[j], is_small ? (int)small(t[j]) : q[j]);
     }
   }
 };
-__device__ __forceinline__ uint32_t bin_of(int place) { return min((uint32_t)-place, kBins - 1u); }
+// A weight in 32 bits, in the place of its logit: the place turned round, and q; or, with the last place, the weight itself where it is small.
+constexpr uint32_t kSmallPlace = 1023u;
+__device__ __forceinline__ uint32_t code_of(bool fine, int place, int q) { return (fine ? (uint32_t)-place : kSmallPlace) << 22 | ((uint32_t)q & 0x3FFFFFu); }
 
 // floor(f * v) for 0 <= f < 1, v < 2^64, and whether there is a remainder.
 __device__ __forceinline__ uint64_t times(float f, uint64_t v, bool& more) {
@@ -339,7 +343,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u, rank = cluster_rank(), ctas = cluster_size();
   const uint32_t row = blockIdx.x / ctas, from = min(rank * p.slice, p.vocab), n = min(p.slice, p.vocab - from);
-  if (tid < 32) sh.powers[tid] = make_uint2(kPowers.v[tid], __float_as_uint((float)kPowers.v[tid]));
+  if (tid < 32) sh.powers[tid] = kPowers.v[tid];
   if (tid == 0) sh.listed = 0u;
   asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -449,7 +453,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     }
     return;
   }
-  if (logit_of(best) == INFINITY) {  // the infinite ones alone are kept, as equals: 0 takes their place, and -inf the others'
+  const bool infinite = logit_of(best) == INFINITY;
+  if (infinite) {  // the infinite ones alone are kept, as equals: 0 takes their place, and -inf the others'
     for (uint32_t i = tid; i < (n + 3u) / 4u * 4u; i += kThreads) xs[i] = xs[i] == INFINITY ? 0.f : -INFINITY;
     mine = mine == INFINITY ? 0.f : -INFINITY;
     least = rising(0.f);
@@ -551,6 +556,12 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     }
     return hi;
   };
+  // A logit of the slice from memory, as it was taken.
+  auto logit_at = [&](uint32_t i) {
+    const float x = load1<TYPE>(p.logits, row_at + i);
+    return infinite ? (x == INFINITY ? 0.f : -INFINITY) : x != x ? -INFINITY : x + 0.f;
+  };
+  bool coded = false;  // weights lie where the logits were
   const bool p_on = top_p < 1.f;
   bool searched = !p_on && k == 0u;  // the border is known
 
@@ -654,6 +665,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   }
   if (!searched && k == 0u) {
     // ---- top-p: a histogram of the weights, and a list of the bin with the border -----------------------------
+    // (the logits of a bin's tokens are read again from memory, for their order)
     for (uint32_t i = tid; i < kBins; i += kThreads) sh.bins.hi[i] = sh.bins.lo[i] = 0u;
     if (tid == 0) sh.told[0] = ~0ull;
     __syncthreads();
@@ -661,16 +673,22 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     for (uint32_t i0 = w0; i0 < w1; i0 += 128u) {
       float x[4];
       read4(i0 + 4u * lane, x);
-      weight.four(x, [&](int, bool fine, int place, uint32_t v) {
+      uint32_t code[4];
+      weight.four(x, [&](int j, bool fine, int place, int q) {
+        place = max(place, 1 - (int)kBins);
+        code[j] = code_of(fine, place, q);
         if (fine) {
-          const uint32_t b = bin_of(place);
-          atomicAdd(&sh.bins.hi[b], v >> 15);
-          atomicAdd(&sh.bins.lo[b], v & 0x7FFFu);
+          const uint32_t v = weight.value(place, q);
+          atomicAdd(&sh.bins.hi[-place], v >> 15);
+          atomicAdd(&sh.bins.lo[-place], v & 0x7FFFu);
         } else {
-          rest += v;
+          rest += (uint32_t)q;
         }
       });
+      // from here on the weights lie where the logits were
+      if (i0 + 4u * lane < w1) *reinterpret_cast<uint4*>(xs + i0 + 4u * lane) = make_uint4(code[0], code[1], code[2], code[3]);
     }
+    coded = true;
     cluster_sync();
     // this CTA's bins of all CTAs: consecutive ones, up to two to a thread
     const uint32_t share = (kBins + ctas - 1u) / ctas, each = (share + kThreads - 1u) / kThreads;
@@ -710,21 +728,19 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
       keep = best;
       searched = true;
     } else if (bin != ~0ull) {
-      // the bin's logits lie about here (a place is rounded to 1/32 after a, which is off by up to 1/64 and a little): only there is the bin looked at
-      const float t_hi = (float)bin * -0.03125f + 0.04f, t_lo = t_hi - 0.08f;
       for (uint32_t i0 = w0; i0 < w1; i0 += 128u) {
+        const uint32_t i = i0 + 4u * lane;
         float x[4];
-        read4(i0 + 4u * lane, x);
+        read4(i, x);
         uint32_t mask = 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float t = weight.coarse(x[j]);
-          if (x[j] == -INFINITY || t < t_lo || t > t_hi || t < -(float)kOctaves) continue;
-          int place;
-          weight.fine(x[j], place);
-          if (bin_of(place) == (uint32_t)bin) mask |= 1u << j;
-        }
-        if (__any_sync(kFull, mask != 0u)) list4(x, i0 + 4u * lane, mask);
+        for (int j = 0; j < 4; ++j) mask |= __float_as_uint(x[j]) >> 22 == (uint32_t)bin ? 1u << j : 0u;
+        if (i >= w1) mask = 0;
+        if (!__any_sync(kFull, mask != 0u)) continue;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if ((mask >> j) & 1u) x[j] = logit_at(i + j);
+        list4(x, i, mask);
       }
       cluster_sync();
       const uint32_t m = load_remote(&sh.listed, 0u);
@@ -756,6 +772,12 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     }
   }
   if (!searched) {
+    if (coded) {  // too many in one bin: the logits again
+      for (uint32_t i = tid; i < n; i += kThreads) xs[i] = logit_at(i);
+      if (tid < 4u && n + tid < (n + 3u) / 4u * 4u) xs[n + tid] = -INFINITY;
+      __syncthreads();
+      coded = false;
+    }
     uint64_t edge = 0;
     if (k != 0u) edge = border(k, true, 0ull);
     if (p_on) {
@@ -769,17 +791,50 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   // ---- the token up to which more than u of the kept sum lies ---------------------------------------
   const float keep_x = logit_of(keep);  // below it nothing is kept
   const uint32_t keep_at = index_of(keep);  // and of its equals the first ones
+  int keep_place = 1;  // coded: places above (weights below) are not kept, of this one's tokens it goes by the logit
+  if (coded) {
+    const float t = weight.coarse(keep_x);
+    keep_place = keep_x == -INFINITY || !(keep_x == keep_x) || t < -(float)kOctaves ? (int)kSmallPlace : 0;
+    if (keep_place == 0) {
+      int place;
+      weight.fine(keep_x, place);
+      keep_place = min(-place, (int)kBins - 1);
+    }
+  }
   // weights of four logits, 0 where they are not kept
   auto kept = [&](uint32_t i, uint64_t (&w)[4]) {
     float x[4];
     read4(i, x);
+    if (coded) {
+      int place[4];
+      bool any = false;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        place[j] = i < w1 ? (int)(__float_as_uint(x[j]) >> 22) : (int)kSmallPlace + 1;
+        any = any || place[j] <= keep_place;
+        w[j] = 0ull;
+      }
+      if (!__any_sync(kFull, any)) return false;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (place[j] > keep_place) continue;
+        const uint32_t code = __float_as_uint(x[j]);
+        if (place[j] == keep_place) {
+          const float y = i + j < n ? logit_at(i + j) : -INFINITY;
+          if (y < keep_x || (y == keep_x && from + i + j > keep_at)) continue;
+        }
+        w[j] = place[j] == (int)kSmallPlace ? code & 0x3FFFFFu
+                                            : (uint64_t)weight.value(-place[j], (int)(code << 10) >> 10) << Weights::shift(-place[j]);
+      }
+      return true;
+    }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       if (x[j] < keep_x || (x[j] == keep_x && from + i + j > keep_at)) x[j] = -INFINITY;
       w[j] = 0ull;
     }
     if (!__any_sync(kFull, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) > -INFINITY)) return false;
-    weight.four(x, [&](int j, bool fine, int place, uint32_t v) { w[j] = fine ? (uint64_t)v << Weights::shift(place) : v; });
+    weight.four(x, [&](int j, bool fine, int place, int q) { w[j] = fine ? (uint64_t)weight.value(place, q) << Weights::shift(place) : (uint64_t)(uint32_t)q; });
     return true;
   };
   uint64_t sum_mine = 0, sum;
@@ -801,7 +856,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
         sum += upto - own;
         uint32_t j = 0;
         while (j < 3u && sum + w[j] <= target) sum += w[j++];
-        answer(order_of(xs[i + j], from + i + j), total);
+        answer(order_of(coded ? logit_at(i + j) : xs[i + j], from + i + j), total);
       }
       return;
     }
