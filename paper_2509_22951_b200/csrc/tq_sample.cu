@@ -101,8 +101,18 @@ __device__ __forceinline__ uint32_t cluster_size() {
   asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
   return r;
 }
+// The cluster's barriers in the form that whole warps execute together; lanes that have gone separate ways before come together first.
+__device__ __forceinline__ void cluster_arrive() {
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+  __syncwarp();
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 __device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  cluster_arrive();
+  cluster_wait();
 }
 __device__ __forceinline__ uint32_t at_rank(const void* ptr, uint32_t rank) {
   uint32_t a;
@@ -345,7 +355,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   const uint32_t row = blockIdx.x / ctas, from = min(rank * p.slice, p.vocab), n = min(p.slice, p.vocab - from);
   if (tid < 32) sh.powers[tid] = kPowers.v[tid];
   if (tid == 0) sh.listed = 0u;
-  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+  cluster_arrive();
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const float temperature = p.temperature ? p.temperature[row] : 1.f;
   const int32_t k_given = p.top_k ? p.top_k[row] : 0;
@@ -426,7 +436,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     for (uint32_t i = tid; i < n; i += kThreads) xs[i] = take(load1<TYPE>(p.logits, row_at + i), i);
   }
   if (tid < 4u && n + tid < (n + 3u) / 4u * 4u) xs[n + tid] = -INFINITY;  // four are read together
-  asm volatile("barrier.cluster.wait.aligned;" ::: "memory");  // every CTA of the cluster runs: its shared memory can be written
+  cluster_wait();  // every CTA of the cluster runs: its shared memory can be written
   uint64_t best;  // 0: nothing is above -inf
   uint32_t least;  // of the threads' maxima
   {
@@ -602,7 +612,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     cluster_sync();
     const uint32_t m = load_remote(&sh.listed, 0u);
     if (m <= kList) {
-      asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // the first CTA stays until all have read that
+      cluster_arrive();  // the first CTA stays until all have read that
       if (rank != 0) return;
       sort_list(sh.list, m, tid);
       uint32_t kept = min(k, m);
@@ -659,7 +669,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
           prev += w[i];
         }
       }
-      asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+      cluster_wait();
       return;
     }
   }
