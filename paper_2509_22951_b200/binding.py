@@ -731,7 +731,8 @@ def _load_fast():
     except ImportError as e:
         warnings.warn(f"the native form of the small calls was not loaded, they go through Python: {e}", RuntimeWarning)
         return None
-    names = ("tq_rmsnorm", "tq_rmsnorm_q8", "tq_rope_append", "tq_paged_attention", "tq_cross_attention")
+    names = ("tq_rmsnorm", "tq_rmsnorm_q8", "tq_rope_append", "tq_paged_attention", "tq_cross_attention", "tq_qk_norm_rope_append",
+             "tq_tree_attention", "tq_sample", "tq_tree_accept")
     return module if module.setup(torch, *(C.cast(getattr(_lib, n), C.c_void_p).value for n in names)) else None
 
 
@@ -1026,6 +1027,10 @@ def tq_qk_norm_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_
                            table: torch.Tensor, positions: torch.Tensor, slots: torch.Tensor, cache: KvCache, eps: float = 1e-5,
                            sections=None, interleaved: bool = False, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """tq_rope_append with every head of q and k normalised first; q_weight, k_weight: fp32 [head dim]."""
+    if stream is None and _fast is not None:
+        r = _fast.qk_norm_rope_append(q, k, v, table, positions, slots, cache._addr, cache.device, sections, interleaved, out, q_weight, k_weight, eps)
+        if r is not None:
+            return r
     device = q.get_device()
     ctx = _elsewhere(device, stream)
     if ctx is not None:
@@ -1046,6 +1051,11 @@ def tq_tree_attention(q: torch.Tensor, cache: KvCache, page_table: torch.Tensor,
     int32 [sequences][max pages]; lens: int32 [sequences], new tokens included; mask: int32 [tokens][words], bit j of a row's words set
     where it sees the sequence's new token j (None: a chain); lse: fp32 [tokens][q heads], filled when given.  -> bf16 like q; rows of no
     sequence are not written."""
+    if stream is None and _fast is not None:
+        r = _fast.tree_attention(q, cache._addr, cache.device, page_table, first, lens, workspace.ptr, workspace.bytes, workspace.device, mask,
+                                 cache.scale if scale is None else scale, out, lse)
+        if r is not None:
+            return r
     device = q.get_device()
     ctx = _elsewhere(device, stream)
     if ctx is not None:
@@ -1070,6 +1080,10 @@ def tq_sample(logits: torch.Tensor, uniform: torch.Tensor, temperature: torch.Te
               logprob: torch.Tensor | bool | None = None, stream=None):
     """logits: CUDA bf16 or fp32 [rows][vocab] (rows may be strided); uniform: fp32 [rows] in [0, 1); temperature, top_p, min_p: fp32
     [rows]; top_k: int32 [rows].  -> int32 [rows] tokens; with logprob (True, or the fp32 [rows] tensor to fill) also their logarithms."""
+    if stream is None and out is None and (logprob is None or isinstance(logprob, bool)) and _fast is not None:
+        r = _fast.sample(logits, uniform, temperature, top_k, top_p, min_p, logprob is True)
+        if r is not None:
+            return r
     device = logits.get_device()
     ctx = _elsewhere(device, stream)
     if ctx is not None:
@@ -1115,6 +1129,11 @@ def tq_tree_accept(caches: KvCaches | None, page_table: torch.Tensor | None, fir
     sequence's first row), sampled: int32 [rows]; page_table: int32 [sequences][max pages].  -> (samples along the path, int32
     [sequences][max_path]; the path's rows, likewise, both -1 past its end; its length, int32 [sequences]; new lens): the path's keys
     and values lie behind the certain ones in every cache."""
+    if stream is None and _fast is not None:
+        n = 0 if caches is None else len(caches)
+        r = _fast.tree_accept(caches._addr if n else 0, n, caches.device if n else 0, page_table, first, lens, tokens, parents, sampled, max_path)
+        if r is not None:
+            return r
     device = first.get_device()
     ctx = _elsewhere(device, stream)
     if ctx is not None:

@@ -23,6 +23,7 @@ PyObject* g_empty = nullptr;         // torch.empty
 PyObject* g_bf16 = nullptr;          // torch.bfloat16
 PyObject* g_int8 = nullptr;
 PyObject* g_f32 = nullptr;
+PyObject* g_i32 = nullptr;
 PyObject* g_kwnames = nullptr;       // ("dtype", "device")
 PyObject* g_kwdtype = nullptr;       // ("dtype",)
 PyObject* g_device_attr = nullptr;   // "device"
@@ -32,6 +33,10 @@ decltype(&tq_rmsnorm_q8) f_rmsnorm_q8 = nullptr;
 decltype(&tq_rope_append) f_rope = nullptr;
 decltype(&tq_paged_attention) f_paged = nullptr;
 decltype(&tq_cross_attention) f_cross = nullptr;
+decltype(&tq_qk_norm_rope_append) f_heads = nullptr;
+decltype(&tq_tree_attention) f_tree = nullptr;
+decltype(&tq_sample) f_sample = nullptr;
+decltype(&tq_tree_accept) f_accept = nullptr;
 
 struct T {
   DLTensor d;
@@ -205,42 +210,79 @@ int64_t heads(PyObject* o, T& t, int64_t tokens, int64_t n, int64_t dim, int typ
   return t.stride(0) < 0 ? -1 : t.stride(0);
 }
 
-// (q, k, v, table, positions, slots, cache address, cache device, sections or None, interleaved, out)
-PyObject* py_rope_append(PyObject*, PyObject* const* a, Py_ssize_t count) {
+// What the calls with rotary positions share: q, k, v, table, positions, slots, cache address, cache device, sections or None, interleaved, out
+struct Rope {
   T q, k, v, table, pos, slots, o;
-  if (count != 11 || !get(a[0], q, -1, -1) || (q.d.ndim != 2 && q.d.ndim != 3)) return none();
-  const tq_kv_cache* c = cache_of(a[6]);
-  const int device = q.d.device.device_id, type = q.type();
-  if (!c || PyLong_AsLong(a[7]) != device || type < 0 || q.n(0) > 0x7FFFFFFF) return none();
-  const int64_t D = c->head_dim, K = c->n_kv_heads, tokens = q.n(0), H = q.d.ndim == 3 ? q.n(1) : q.n(1) / D;
-  const int64_t qs = heads(a[0], q, tokens, H, D, type, device), ks = heads(a[1], k, tokens, K, D, type, device),
-                vs = heads(a[2], v, tokens, K, D, type, device);
-  if (qs < 0 || ks < 0 || vs < 0 || H <= 0 || H > 65536) return none();
-  if (!get(a[3], table, 2, device) || !table.f32() || !table.contiguous() || table.n(0) > 0x7FFFFFFF || table.n(1) > 0x7FFFFFFF) return none();
-  if (!get(a[4], pos, -1, device) || !pos.i32() || !pos.contiguous() || pos.d.ndim < 1 || pos.d.ndim > 2) return none();
-  const int64_t axes = pos.d.ndim == 1 ? 1 : pos.n(0);
-  if (axes < 1 || axes > (int64_t)TQ_ROPE_MAX_AXES || pos.numel() != axes * tokens) return none();
-  if (!get(a[5], slots, -1, device) || !slots.i32() || !slots.contiguous() || slots.numel() != tokens) return none();
-  uint32_t sections[TQ_ROPE_MAX_AXES] = {(uint32_t)(table.n(1) / 2)};
+  const tq_kv_cache* c;
+  int device, type, inter;
+  int64_t D, K, tokens, H, qs, ks, vs, axes;
+  uint32_t sections[TQ_ROPE_MAX_AXES];
+  void* stream;
+};
+bool rope_args(PyObject* const* a, Rope& r) {
+  if (!get(a[0], r.q, -1, -1) || (r.q.d.ndim != 2 && r.q.d.ndim != 3)) return false;
+  r.c = cache_of(a[6]);
+  r.device = r.q.d.device.device_id;
+  r.type = r.q.type();
+  if (!r.c || PyLong_AsLong(a[7]) != r.device || r.type < 0 || r.q.n(0) > 0x7FFFFFFF) return false;
+  r.D = r.c->head_dim;
+  r.K = r.c->n_kv_heads;
+  r.tokens = r.q.n(0);
+  r.H = r.q.d.ndim == 3 ? r.q.n(1) : r.q.n(1) / r.D;
+  r.qs = heads(a[0], r.q, r.tokens, r.H, r.D, r.type, r.device);
+  r.ks = heads(a[1], r.k, r.tokens, r.K, r.D, r.type, r.device);
+  r.vs = heads(a[2], r.v, r.tokens, r.K, r.D, r.type, r.device);
+  if (r.qs < 0 || r.ks < 0 || r.vs < 0 || r.H <= 0 || r.H > 65536) return false;
+  if (!get(a[3], r.table, 2, r.device) || !r.table.f32() || !r.table.contiguous() || r.table.n(0) > 0x7FFFFFFF || r.table.n(1) > 0x7FFFFFFF) return false;
+  if (!get(a[4], r.pos, -1, r.device) || !r.pos.i32() || !r.pos.contiguous() || r.pos.d.ndim < 1 || r.pos.d.ndim > 2) return false;
+  r.axes = r.pos.d.ndim == 1 ? 1 : r.pos.n(0);
+  if (r.axes < 1 || r.axes > (int64_t)TQ_ROPE_MAX_AXES || r.pos.numel() != r.axes * r.tokens) return false;
+  if (!get(a[5], r.slots, -1, r.device) || !r.slots.i32() || !r.slots.contiguous() || r.slots.numel() != r.tokens) return false;
+  r.sections[0] = (uint32_t)(r.table.n(1) / 2);
   if (a[8] != Py_None) {
     const bool list = PyList_Check(a[8]);
-    if ((!list && !PyTuple_Check(a[8])) || PySequence_Fast_GET_SIZE(a[8]) != axes) return none();
-    for (int64_t i = 0; i < axes; ++i) {
+    if ((!list && !PyTuple_Check(a[8])) || PySequence_Fast_GET_SIZE(a[8]) != r.axes) return false;
+    for (int64_t i = 0; i < r.axes; ++i) {
       const long x = PyLong_AsLong(PySequence_Fast_GET_ITEM(a[8], i));
-      if (x < 0 || x > 0x7FFFFFFF) return none();
-      sections[i] = (uint32_t)x;
+      if (x < 0 || x > 0x7FFFFFFF) return false;
+      r.sections[i] = (uint32_t)x;
     }
-  } else if (axes != 1) {
-    return none();
+  } else if (r.axes != 1) {
+    return false;
   }
-  const int inter = PyObject_IsTrue(a[9]);
-  void* stream;
-  if (inter < 0 || !current(device, &stream)) return none();
-  const int64_t shape[3] = {tokens, H, D};
-  PyObject* out = result(a[10], a[0], q, shape, 3, device, o);
+  r.inter = PyObject_IsTrue(a[9]);
+  return r.inter >= 0 && current(r.device, &r.stream);
+}
+
+PyObject* py_rope_append(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  Rope r;
+  if (count != 11 || !rope_args(a, r)) return none();
+  const int64_t shape[3] = {r.tokens, r.H, r.D};
+  PyObject* out = result(a[10], a[0], r.q, shape, 3, r.device, r.o);
   if (!out) return none();
-  if (f_rope(q.ptr(), k.ptr(), v.ptr(), type, qs, ks, vs, (uint32_t)tokens, (uint32_t)H, (const float*)table.ptr(), (uint32_t)table.n(0),
-             (uint32_t)table.n(1), (const int32_t*)pos.ptr(), sections, (uint32_t)axes, inter, (const int32_t*)slots.ptr(), c, o.ptr(), stream) == TQ_OK)
+  if (f_rope(r.q.ptr(), r.k.ptr(), r.v.ptr(), r.type, r.qs, r.ks, r.vs, (uint32_t)r.tokens, (uint32_t)r.H, (const float*)r.table.ptr(),
+             (uint32_t)r.table.n(0), (uint32_t)r.table.n(1), (const int32_t*)r.pos.ptr(), r.sections, (uint32_t)r.axes, r.inter,
+             (const int32_t*)r.slots.ptr(), r.c, r.o.ptr(), r.stream) == TQ_OK)
+    return out;
+  Py_DECREF(out);
+  return none();
+}
+
+// (as above, q_weight, k_weight, eps)
+PyObject* py_qk_norm_rope_append(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  Rope r;
+  T qw, kw;
+  if (count != 14 || !rope_args(a, r)) return none();
+  if (!get(a[11], qw, 1, r.device) || !qw.f32() || !qw.contiguous() || qw.n(0) != r.D) return none();
+  if (!get(a[12], kw, 1, r.device) || !kw.f32() || !kw.contiguous() || kw.n(0) != r.D) return none();
+  const double eps = PyFloat_AsDouble(a[13]);
+  if (eps == -1.0 && PyErr_Occurred()) return none();
+  const int64_t shape[3] = {r.tokens, r.H, r.D};
+  PyObject* out = result(a[10], a[0], r.q, shape, 3, r.device, r.o);
+  if (!out) return none();
+  if (f_heads(r.q.ptr(), r.k.ptr(), r.v.ptr(), r.type, r.qs, r.ks, r.vs, (uint32_t)r.tokens, (uint32_t)r.H, (const float*)qw.ptr(),
+              (const float*)kw.ptr(), (float)eps, (const float*)r.table.ptr(), (uint32_t)r.table.n(0), (uint32_t)r.table.n(1),
+              (const int32_t*)r.pos.ptr(), r.sections, (uint32_t)r.axes, r.inter, (const int32_t*)r.slots.ptr(), r.c, r.o.ptr(), r.stream) == TQ_OK)
     return out;
   Py_DECREF(out);
   return none();
@@ -330,10 +372,108 @@ PyObject* py_cross_attention(PyObject*, PyObject* const* a, Py_ssize_t count) {
   return none();
 }
 
-// setup(torch, addresses of the five library functions): True if this torch has the exchange interface
+// A contiguous tensor of this type (32-bit integers, or fp32) with n elements in all.
+bool vec(PyObject* o, T& t, int64_t n, int device, bool ints) {
+  return get(o, t, -1, device) && (ints ? t.i32() : t.f32()) && t.contiguous() && t.numel() == n;
+}
+
+// (q, cache address, cache device, page_table, first, lens, workspace address, bytes, workspace device, mask, scale, out, lse)
+PyObject* py_tree_attention(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  T q, table, first, lens, mask, o;
+  if (count != 13 || !get(a[0], q, 3, -1) || !q.bf16()) return none();
+  const tq_kv_cache* c = cache_of(a[1]);
+  const int device = q.d.device.device_id;
+  if (!c || PyLong_AsLong(a[2]) != device || PyLong_AsLong(a[8]) != device) return none();
+  const int64_t tokens = q.n(0), H = q.n(1), D = q.n(2);
+  if (D != c->head_dim || q.d.strides[2] != 1 || (H > 1 && q.d.strides[1] != D) || tokens > 0x7FFFFFFF || H > 65536) return none();
+  if (!get(a[3], table, 2, device) || !table.i32() || !table.contiguous() || table.n(0) > 0x7FFFFFFE || table.n(1) > 0x7FFFFFFF) return none();
+  const int64_t B = table.n(0);
+  if (!vec(a[4], first, B + 1, device, true) || first.d.ndim != 1 || !vec(a[5], lens, B, device, true) || lens.d.ndim != 1) return none();
+  const uint32_t* bits = nullptr;
+  uint32_t words = 0;
+  if (a[9] != Py_None) {
+    if (!get(a[9], mask, 2, device) || !mask.i32() || !mask.contiguous() || mask.n(0) != tokens || mask.n(1) > 0x7FFFFFFF) return none();
+    bits = (const uint32_t*)mask.ptr();
+    words = (uint32_t)mask.n(1);
+  }
+  const double scale = PyFloat_AsDouble(a[10]);
+  void* ws = PyLong_AsVoidPtr(a[6]);
+  const uint64_t bytes = PyLong_AsUnsignedLongLong(a[7]);
+  void* stream;
+  if (PyErr_Occurred() || !current(device, &stream)) return none();
+  float* lse;
+  PyObject* out = attn_result(a[11], a[12], a[0], q, device, o, &lse);
+  if (!out) return none();
+  if (f_tree(c, q.ptr(), q.stride(0), (uint32_t)tokens, (uint32_t)B, (uint32_t)H, (const int32_t*)first.ptr(), (const int32_t*)table.ptr(),
+             (uint32_t)table.n(1), (const int32_t*)lens.ptr(), bits, words, (float)scale, o.ptr(), lse, ws, bytes, stream) == TQ_OK)
+    return out;
+  Py_DECREF(out);
+  return none();
+}
+
+// (logits, uniform, temperature, top_k, top_p, min_p, whether logprobs are wanted) -> tokens, or (tokens, logprobs)
+PyObject* py_sample(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  T x, u, s, out, lp;
+  if (count != 7 || !get(a[0], x, 2, -1) || x.type() < 0 || x.n(0) > 0x7FFFFFFF || x.n(1) > 0x7FFFFFFF || (x.n(1) > 1 && x.d.strides[1] != 1)) return none();
+  const int device = x.d.device.device_id;
+  const int64_t rows = x.n(0);
+  if (!vec(a[1], u, rows, device, false)) return none();
+  const void* given[4] = {};
+  for (int i = 0; i < 4; ++i) {
+    if (a[2 + i] == Py_None) continue;
+    if (!vec(a[2 + i], s, rows, device, i == 1)) return none();
+    given[i] = s.ptr();
+  }
+  const int wanted = PyObject_IsTrue(a[6]);
+  void* stream;
+  if (wanted < 0 || !current(device, &stream)) return none();
+  PyObject* token = empty(&rows, 1, g_i32, a[0]);
+  PyObject* logprob = token && wanted ? empty(&rows, 1, g_f32, a[0]) : nullptr;
+  PyObject* r = nullptr;
+  if (token && get(token, out, 1, device) && (!wanted || (logprob && get(logprob, lp, 1, device))) &&
+      f_sample(x.ptr(), x.type(), x.stride(0), (uint32_t)rows, (uint32_t)x.n(1), (const float*)u.ptr(), (const float*)given[0], (const int32_t*)given[1],
+               (const float*)given[2], (const float*)given[3], (int32_t*)out.ptr(), wanted ? (float*)lp.ptr() : nullptr, stream) == TQ_OK)
+    r = wanted ? PyTuple_Pack(2, token, logprob) : Py_NewRef(token);
+  Py_XDECREF(token);
+  Py_XDECREF(logprob);
+  return r ? r : none();
+}
+
+// (caches address, their number, their device, page_table or None, first, lens, tokens, parents, sampled, max_path) -> what the Python form returns
+PyObject* py_tree_accept(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  T table, first, lens, rows[3], o[4];
+  if (count != 10 || !get(a[4], first, 1, -1) || !first.i32() || !first.contiguous() || first.n(0) < 1 || first.n(0) > 0x7FFFFFFF) return none();
+  const int device = first.d.device.device_id;
+  const int64_t B = first.n(0) - 1;
+  const long n = PyLong_AsLong(a[1]);
+  if (n < 0 || (n > 0 && PyLong_AsLong(a[2]) != device)) return none();
+  if (!vec(a[5], lens, B, device, true) || !get(a[6], rows[0], 1, device) || rows[0].n(0) > 0x7FFFFFFF) return none();
+  for (int i = 0; i < 3; ++i)
+    if (!vec(a[6 + i], rows[i], rows[0].n(0), device, true)) return none();
+  if (n > 0 && (!get(a[3], table, 2, device) || !table.i32() || !table.contiguous() || table.n(0) != B || table.n(1) > 0x7FFFFFFF)) return none();
+  const int64_t path = PyLong_AsLongLong(a[9]);
+  const tq_kv_cache* caches = n > 0 ? static_cast<const tq_kv_cache*>(PyLong_AsVoidPtr(a[0])) : nullptr;
+  void* stream;
+  if (path < 1 || path > 0x7FFFFFFF || PyErr_Occurred() || !current(device, &stream)) return none();
+  const int64_t shape[2] = {B, path};
+  PyObject* r[4] = {empty(shape, 2, g_i32, a[4]), empty(shape, 2, g_i32, a[4]), empty(shape, 1, g_i32, a[4]), empty(shape, 1, g_i32, a[4])};
+  bool ok = true;
+  for (int i = 0; i < 4; ++i) ok = ok && r[i] && get(r[i], o[i], -1, device);
+  PyObject* all = nullptr;
+  if (ok && f_accept(caches, (uint32_t)n, n > 0 ? (const int32_t*)table.ptr() : nullptr, n > 0 ? (uint32_t)table.n(1) : 0u, (uint32_t)B, (uint32_t)rows[0].n(0),
+                     (const int32_t*)first.ptr(), (const int32_t*)lens.ptr(), (const int32_t*)rows[0].ptr(), (const int32_t*)rows[1].ptr(),
+                     (const int32_t*)rows[2].ptr(), (uint32_t)path, (int32_t*)o[0].ptr(), (int32_t*)o[1].ptr(), (int32_t*)o[2].ptr(),
+                     (int32_t*)o[3].ptr(), stream) == TQ_OK)
+    all = PyTuple_Pack(4, r[0], r[1], r[2], r[3]);
+  for (PyObject* x : r) Py_XDECREF(x);
+  return all ? all : none();
+}
+
+// setup(torch, addresses of the library's functions): True if this torch has the exchange interface
 PyObject* py_setup(PyObject*, PyObject* const* a, Py_ssize_t count) {
-  if (count != 6) {
-    PyErr_SetString(PyExc_TypeError, "setup(torch, rmsnorm, rmsnorm_q8, rope_append, paged_attention, cross_attention)");
+  if (count != 10) {
+    PyErr_SetString(PyExc_TypeError, "setup(torch, rmsnorm, rmsnorm_q8, rope_append, paged_attention, cross_attention, qk_norm_rope_append, "
+                                     "tree_attention, sample, tree_accept)");
     return nullptr;
   }
   PyObject* torch = a[0];
@@ -354,10 +494,11 @@ PyObject* py_setup(PyObject*, PyObject* const* a, Py_ssize_t count) {
   g_bf16 = PyObject_GetAttrString(torch, "bfloat16");
   g_int8 = PyObject_GetAttrString(torch, "int8");
   g_f32 = PyObject_GetAttrString(torch, "float32");
+  g_i32 = PyObject_GetAttrString(torch, "int32");
   g_kwnames = Py_BuildValue("(ss)", "dtype", "device");
   g_kwdtype = Py_BuildValue("(s)", "dtype");
   g_device_attr = PyUnicode_InternFromString("device");
-  if (!g_kwdtype || !g_device || !g_empty_like || !g_empty || !g_bf16 || !g_int8 || !g_f32 || !g_kwnames || !g_device_attr) {
+  if (!g_kwdtype || !g_device || !g_empty_like || !g_empty || !g_bf16 || !g_int8 || !g_f32 || !g_i32 || !g_kwnames || !g_device_attr) {
     PyErr_Clear();
     Py_RETURN_FALSE;
   }
@@ -366,14 +507,27 @@ PyObject* py_setup(PyObject*, PyObject* const* a, Py_ssize_t count) {
   f_rope = (decltype(f_rope))PyLong_AsVoidPtr(a[3]);
   f_paged = (decltype(f_paged))PyLong_AsVoidPtr(a[4]);
   f_cross = (decltype(f_cross))PyLong_AsVoidPtr(a[5]);
+  f_heads = (decltype(f_heads))PyLong_AsVoidPtr(a[6]);
+  f_tree = (decltype(f_tree))PyLong_AsVoidPtr(a[7]);
+  f_sample = (decltype(f_sample))PyLong_AsVoidPtr(a[8]);
+  f_accept = (decltype(f_accept))PyLong_AsVoidPtr(a[9]);
   if (PyErr_Occurred()) return nullptr;
   g_api = api;
   Py_RETURN_TRUE;
 }
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {FAST(setup),           FAST(rmsnorm),         FAST(rmsnorm_q8), FAST(rope_append),
-                         FAST(paged_attention), FAST(cross_attention), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {FAST(setup),
+                         FAST(rmsnorm),
+                         FAST(rmsnorm_q8),
+                         FAST(rope_append),
+                         FAST(paged_attention),
+                         FAST(cross_attention),
+                         FAST(qk_norm_rope_append),
+                         FAST(tree_attention),
+                         FAST(sample),
+                         FAST(tree_accept),
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tqfast", "The usual case of the calls between the linear layers.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

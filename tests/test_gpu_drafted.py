@@ -816,3 +816,40 @@ def test_refusals_of_the_binding(tq, ws):
         tq.tq_tree_attention(q, c, table, first, lens, ws, scale=0.0)
     with pytest.raises(tq.TqError):
         tq.tq_tree_accept(None, None, first, lens, i32([1] * 3), i32([0] * 3), i32([1] * 3), tq.TQ_TREE_MAX_PATH + 1)
+
+
+def test_native_and_python_form_of_a_call_agree(tq, ws, monkeypatch):
+    """The usual calls are served by the native module (none of them falls through it), and the Python form gives the same bits."""
+    g = gen(61)
+    c = tq.tq_kv_cache(randn(g, 9, 2, 16, 64, dtype=BF), randn(g, 9, 2, 16, 64, dtype=BF))
+    q, k, v = randn(g, 6, 4 * 64), randn(g, 6, 2, 64), randn(g, 6, 2 * 64 + 8)[:, :128]
+    w, rope, pos, slots = torch.rand(64, generator=g, device="cuda"), rope_table(20, 64), i32([[3, 4, 5, 6, 7, 8]] * 2), i32([0, 1, 2, 40, 41, -1])
+    table, first, lens, mask = i32([[0, 1, 2], [5, 6, 7]]), i32([0, 4, 6]), i32([40, 20]), i32([[1], [3], [1], [7], [1], [3]])
+    x, u, t, p = randn(g, 6, 3000, scale=3), torch.rand(6, generator=g, device="cuda"), f32([0.7] * 6), f32([0.9] * 6)
+    tokens, parents, sampled = i32([1, 2, 3, 4, 5, 6]), i32([-1, 0, 1, 0, -1, 0]), i32([2, 3, 4, 4, 6, 6])
+    caches = tq.tq_kv_caches([c])
+
+    def calls():
+        qb = torch.randn(6, 4, 64, generator=gen(62), device="cuda").to(BF)
+        lse = torch.empty(6, 4, device="cuda")
+        yield tq.tq_qk_norm_rope_append(q, k, v, w, w, rope, pos, slots, c, sections=(20, 12), interleaved=True)
+        yield tq.tq_qk_norm_rope_append(q, k, v, w, w, rope, pos[0], slots, c, eps=1e-6, out=torch.empty(6, 4, 64, dtype=BF, device="cuda"))
+        yield tq.tq_tree_attention(qb, c, table, first, lens, ws, mask=mask, lse=lse)
+        yield lse
+        yield tq.tq_tree_attention(qb, c, table, first, lens, ws, scale=0.3, out=torch.empty_like(qb))
+        yield tq.tq_sample(x, u)
+        yield from tq.tq_sample(x.to(BF), u, temperature=t, top_p=p, min_p=t * 0.01, logprob=True)
+        yield from tq.tq_tree_accept(caches, table, first, lens, tokens, parents, sampled, 3)
+        yield from tq.tq_tree_accept(None, None, first, lens, tokens, parents, sampled, 5)
+
+    if tq._fast is None:
+        pytest.skip("the native module is not here")
+    k0, v0 = c.k.clone(), c.v.clone()
+    with monkeypatch.context() as m:
+        m.setattr(tq, "_check", lambda rc, name: pytest.fail(f"{name} was not served by the native module"))
+        native = [y.clone() for y in calls()]
+    k1, v1 = c.k.clone(), c.v.clone()
+    c.k.copy_(k0), c.v.copy_(v0)
+    monkeypatch.setattr(tq, "_fast", None)
+    python = list(calls())
+    assert all(torch.equal(a, b) for a, b in zip(native, python)) and torch.equal(c.k, k1) and torch.equal(c.v, v1)
