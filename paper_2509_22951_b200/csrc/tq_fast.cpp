@@ -100,6 +100,12 @@ PyObject* empty(const int64_t* shape, int ndim, PyObject* dtype, PyObject* like)
   return r;
 }
 
+// A new contiguous tensor of like's shape and, where dtype is given, another type: cheaper than empty().
+PyObject* empty_as(PyObject* like, PyObject* dtype) {
+  PyObject* args[2] = {like, dtype};
+  return dtype ? PyObject_Vectorcall(g_empty_like, args, 1, g_kwdtype) : PyObject_CallOneArg(g_empty_like, like);
+}
+
 PyObject* none() {
   PyErr_Clear();
   Py_RETURN_NONE;
@@ -427,8 +433,8 @@ PyObject* py_sample(PyObject*, PyObject* const* a, Py_ssize_t count) {
   const int wanted = PyObject_IsTrue(a[6]);
   void* stream;
   if (wanted < 0 || !current(device, &stream)) return none();
-  PyObject* token = empty(&rows, 1, g_i32, a[0]);
-  PyObject* logprob = token && wanted ? empty(&rows, 1, g_f32, a[0]) : nullptr;
+  PyObject* token = u.d.ndim == 1 ? empty_as(a[1], g_i32) : nullptr;
+  PyObject* logprob = token && wanted ? empty_as(a[1], nullptr) : nullptr;
   PyObject* r = nullptr;
   if (token && get(token, out, 1, device) && (!wanted || (logprob && get(logprob, lp, 1, device))) &&
       f_sample(x.ptr(), x.type(), x.stride(0), (uint32_t)rows, (uint32_t)x.n(1), (const float*)u.ptr(), (const float*)given[0], (const int32_t*)given[1],
@@ -447,7 +453,7 @@ PyObject* py_tree_accept(PyObject*, PyObject* const* a, Py_ssize_t count) {
   const int64_t B = first.n(0) - 1;
   const long n = PyLong_AsLong(a[1]);
   if (n < 0 || (n > 0 && PyLong_AsLong(a[2]) != device)) return none();
-  if (!vec(a[5], lens, B, device, true) || !get(a[6], rows[0], 1, device) || rows[0].n(0) > 0x7FFFFFFF) return none();
+  if (!vec(a[5], lens, B, device, true) || lens.d.ndim != 1 || !get(a[6], rows[0], 1, device) || rows[0].n(0) > 0x7FFFFFFF) return none();
   for (int i = 0; i < 3; ++i)
     if (!vec(a[6 + i], rows[i], rows[0].n(0), device, true)) return none();
   if (n > 0 && (!get(a[3], table, 2, device) || !table.i32() || !table.contiguous() || table.n(0) != B || table.n(1) > 0x7FFFFFFF)) return none();
@@ -456,7 +462,8 @@ PyObject* py_tree_accept(PyObject*, PyObject* const* a, Py_ssize_t count) {
   void* stream;
   if (path < 1 || path > 0x7FFFFFFF || PyErr_Occurred() || !current(device, &stream)) return none();
   const int64_t shape[2] = {B, path};
-  PyObject* r[4] = {empty(shape, 2, g_i32, a[4]), empty(shape, 2, g_i32, a[4]), empty(shape, 1, g_i32, a[4]), empty(shape, 1, g_i32, a[4])};
+  PyObject* r[4] = {empty(shape, 2, g_i32, a[4]), nullptr, empty_as(a[5], nullptr), empty_as(a[5], nullptr)};
+  r[1] = r[0] ? empty_as(r[0], nullptr) : nullptr;
   bool ok = true;
   for (int i = 0; i < 4; ++i) ok = ok && r[i] && get(r[i], o[i], -1, device);
   PyObject* all = nullptr;

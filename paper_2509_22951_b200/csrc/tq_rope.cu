@@ -39,6 +39,7 @@ struct RopeParams {
   const float* q_weight;  // norm of the heads
   const float* k_weight;
   float eps;
+  bool weights_16;  // they may be read 16 bytes at a time
 };
 
 // Eight elements of a head as two runs of four, so that neighbouring lanes read neighbouring runs whatever the type and the
@@ -109,15 +110,16 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopePar
   const uint32_t H = p.n_q_heads, K = p.cache.n_kv_heads, heads = H + 2u * K, step = gridDim.y * kSide;
   const size_t tq = (size_t)t * p.q_stride + e0, tk = (size_t)t * p.k_stride + e0, tv = (size_t)t * p.v_stride + e0;
   const uint32_t gap = e1 - e0;
-  Raw4x2<TYPE> raw;
-  auto load = [&](uint32_t n) {
+  Raw4x2<TYPE> raw, next;  // next: with the norm, whose reduction takes its time, the head after this one is asked for before
+  auto load = [&](uint32_t n, Raw4x2<TYPE>& to) {
     if (n >= heads) return;
     const void* src = n < H ? p.q : (n < H + K ? p.k : p.v);
     const size_t at = (n < H ? tq : (n < H + K ? tk : tv)) + (n < H ? n : (n < H + K ? n - H : n - H - K)) * D;
-    raw.load(src, at, at + gap);
+    to.load(src, at, at + gap);
   };
   uint32_t n = blockIdx.y * kSide + threadIdx.x / kPerHead;
-  load(n);
+  load(n, raw);
+  if (NORM) load(n + step, next);
 
   const uint32_t page = (uint32_t)slot / p.cache.page_size;  // -1: no slot; other negative ones are out of range like those past the pool
   const bool in_pool = slot >= 0 && page < p.cache.n_pages, keep = in_pool && known;
@@ -129,11 +131,18 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopePar
 
   float wq[NORM ? 8 : 1], wk[NORM ? 8 : 1];
   if constexpr (NORM) {
+    if (p.weights_16) {
+      const float4 a = __ldg(reinterpret_cast<const float4*>(p.q_weight + e0)), b = __ldg(reinterpret_cast<const float4*>(p.q_weight + e1));
+      const float4 c = __ldg(reinterpret_cast<const float4*>(p.k_weight + e0)), d = __ldg(reinterpret_cast<const float4*>(p.k_weight + e1));
+      wq[0] = a.x, wq[1] = a.y, wq[2] = a.z, wq[3] = a.w, wq[4] = b.x, wq[5] = b.y, wq[6] = b.z, wq[7] = b.w;
+      wk[0] = c.x, wk[1] = c.y, wk[2] = c.z, wk[3] = c.w, wk[4] = d.x, wk[5] = d.y, wk[6] = d.z, wk[7] = d.w;
+    } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t at = (i < 4 ? e0 : e1 - 4u) + i;
-      wq[i] = __ldg(p.q_weight + at);
-      wk[i] = __ldg(p.k_weight + at);
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t at = (i < 4 ? e0 : e1 - 4u) + i;
+        wq[i] = __ldg(p.q_weight + at);
+        wk[i] = __ldg(p.k_weight + at);
+      }
     }
   }
 
@@ -150,9 +159,13 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopePar
     sn[i] = __ldg(row + pairs);
   }
 
-  for (; n < heads && (n < H || keep); n += step, load(n)) {
+  for (; n < heads && (n < H || keep); n += step) {
     float f[8];
     raw.get(f);
+    if (NORM) {
+      raw = next;
+      load(n + 2u * step, next);
+    }
     if constexpr (NORM) {
       if (n < H + K) {
         float sum = 0.f;
@@ -184,6 +197,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopePar
     const uint4 o = pack8(f);
     *reinterpret_cast<uint2*>(dst) = make_uint2(o.x, o.y);
     *reinterpret_cast<uint2*>(dst + gap) = make_uint2(o.z, o.w);
+    if (!NORM) load(n + step, raw);
   }
 }
 
@@ -242,6 +256,7 @@ int rope(const void* d_q, const void* d_k, const void* d_v, int x_type, int64_t 
   p.q_weight = d_q_weight;
   p.k_weight = d_k_weight;
   p.eps = eps;
+  p.weights_16 = (((uintptr_t)d_q_weight | (uintptr_t)d_k_weight) & 15u) == 0;
   cudaStream_t st = (cudaStream_t)cuda_stream;
   if (x_type == TQ_TYPE_F32) return interleaved ? launch<TQ_TYPE_F32, true, NORM>(p, st) : launch<TQ_TYPE_F32, false, NORM>(p, st);
   return interleaved ? launch<TQ_TYPE_BF16, true, NORM>(p, st) : launch<TQ_TYPE_BF16, false, NORM>(p, st);

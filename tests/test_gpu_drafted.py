@@ -853,3 +853,15 @@ def test_native_and_python_form_of_a_call_agree(tq, ws, monkeypatch):
     monkeypatch.setattr(tq, "_fast", None)
     python = list(calls())
     assert all(torch.equal(a, b) for a, b in zip(native, python)) and torch.equal(c.k, k1) and torch.equal(c.v, v1)
+
+
+def test_weights_of_any_alignment(tq):
+    g = gen(63)
+    kp = randn(g, 2, 2, 16, 128, dtype=BF)
+    c = tq.tq_kv_cache(kp, kp.clone())
+    q, k, w = randn(g, 3, 4, 128), randn(g, 3, 2, 128), randn(g, 260)
+    args = (rope_table(9, 128), i32([1, 2, 3]), i32([3, 4, 5]), c)
+    for at in (0, 1, 3, 4):
+        want = tq.tq_qk_norm_rope_append(q, k, k, w[at:at + 128].clone(), w[at + 128:at + 256].clone(), *args)
+        kw = kp.clone()
+        assert torch.equal(tq.tq_qk_norm_rope_append(q, k, k, w[at:at + 128], w[at + 128:at + 256], *args), want) and torch.equal(kp, kw)
