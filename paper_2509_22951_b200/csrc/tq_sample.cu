@@ -37,7 +37,8 @@ static_assert((1u << kIndexBits) == TQ_SAMPLE_MAX_VOCAB, "a token's index fits i
 constexpr uint32_t kIndexMask = (1u << kIndexBits) - 1u;
 constexpr int kOne = 45;      // W of the largest logit is 2^45
 constexpr int kOctaves = 24;  // of the histogram, and of the weights that are computed to 29 bits
-constexpr uint32_t kBins = kOctaves * 32u + 2u;  // a place each; the last has what a rounding puts below
+constexpr int kTopPlace = 1;  // place of the largest logit at most (a is off by up to 1/64 and a little)
+constexpr uint32_t kBins = kOctaves * 32u + 3u;  // a place each; the last has what a rounding puts below
 constexpr uint32_t kList = 2048;   // tokens that one CTA sorts
 constexpr uint32_t kListK = 1024;  // largest k of the list: the threads' maxima bound it well up to a quarter of their number
 constexpr uint32_t kKBins = 256;   // of the threads' maxima
@@ -76,7 +77,7 @@ struct SampleParams {
 };
 
 struct Shared {
-  uint64_t slots[3][kMaxCluster * kWarps];  // what the cluster's warps tell one another; two sets, used in turn, and one for the start
+  uint64_t slots[2][kMaxCluster * kWarps];  // what the cluster's warps tell one another; two sets, used in turn
   uint64_t told[2];                         // by one CTA to all
   uint64_t warps[kWarps];                   // within a CTA
   uint32_t powers[32];                      // 2^(i / 32) with 29 bits behind the point
@@ -202,25 +203,22 @@ struct Weights {
   __device__ __forceinline__ void set(float top_, float temperature, const uint32_t* powers_) {
     top = top_;
     powers = powers_;
-    c = c_low = 0.f;
-    if (temperature < INFINITY) {
-      const float T = fmaxf(temperature, 7.52316385e-37f);  // 2^-120: where the quotient stays finite
-      c = kLog2e / T;
-      c_low = (fmaf(-c, T, kLog2e) + kLog2eLow) / T;
-    }
+    const float T = fminf(fmaxf(temperature, 7.52316385e-37f), 1.26765060e30f);  // 2^-120 .. 2^100: the quotient stays finite, and is not 0
+    c = kLog2e / T;
+    c_low = (fmaf(-c, T, kLog2e) + kLog2eLow) / T;
     const float full = top * c;
     plain = fabsf(full) < 65536.f;
     a = plain ? rintf(full * 32.f) * 0.03125f : 0.f;
     a_low = fmaf(top, c, -a) + top * c_low;
   }
-  // t in fp32 (NaN where the distance overflows and the temperature is infinite)
-  __device__ __forceinline__ float coarse(float x) const { return (x - top) * c; }
+  // t in fp32; -inf where x is
+  __device__ __forceinline__ float coarse(float x) const { return plain ? fmaf(x, c, -a) - a_low : (x - top) * c; }
   __device__ __forceinline__ Pair both(float x) const {
     const Pair d = exact_sum(x, -top);
     const float t = d.hi * c;
     return Pair{t, fmaf(d.lo, c, fmaf(d.hi, c_low, fmaf(d.hi, c, -t)))};
   }
-  // 2^t = 2^(place / 32) (1 + q 2^-26), for t from 0 down to some octaves below the histogram's, and NaN, which is taken for 0.
+  // 2^t = 2^(place / 32) (1 + q 2^-26), for t from 0 down to some octaves below the histogram's.
   __device__ __forceinline__ int fine(float x, int& place) const {
     constexpr float kRound = 393216.0f, kQUnit = 67108864.0f;  // 1.5 * 2^18: sums with it are rounded to 1/32
     float r, s;
@@ -234,10 +232,6 @@ struct Weights {
       s = t.hi + kRound;
       place = __float_as_int(s) - 0x48C00000;
       r = (t.hi - (s - kRound)) + t.lo;
-    }
-    if (place > 0) {  // the largest logit, where a is that far from the exact product
-      r += s - kRound;
-      place = 0;
     }
     constexpr float a2 = 0.24022651f, a3 = 0.055504109f, a4 = 0.0096181291f;  // (ln 2)^k / k!
     const float q = r * fmaf(r, fmaf(r, fmaf(r, a4, a3), a2), kLn2);
@@ -258,7 +252,7 @@ struct Weights {
   }
   __device__ __forceinline__ uint64_t operator()(float x) const {
     const float t = coarse(x);
-    if (x == -INFINITY || t < -(float)kOctaves) return x == -INFINITY ? 0u : small(t);
+    if (t < -(float)kOctaves) return small(t);
     int place;
     const int q = fine(x, place);
     return (uint64_t)value(place, q) << shift(place);
@@ -269,16 +263,15 @@ struct Weights {
   __device__ __forceinline__ void four(const float (&x)[4], Use use) const {
     float t[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) t[j] = x[j] == -INFINITY ? -INFINITY : coarse(x[j]);
-    const float most = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));  // (a NaN beside numbers is dropped here: all of a row are, or none)
-    if (!__any_sync(kFull, !(most < -(float)kOctaves))) {
+    for (int j = 0; j < 4; ++j) t[j] = coarse(x[j]);
+    if (!__any_sync(kFull, fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) >= -(float)kOctaves)) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) use(j, false, 0, (int)small(t[j]));
       return;
     }
     int place[4], q[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) q[j] = fine(t[j] < -(float)kOctaves ? top : x[j], place[j]);
+    for (int j = 0; j < 4; ++j) q[j] = fine(x[j], place[j]);  // (of a small one it is not used)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const bool is_small = t[j] < -(float)kOctaves;
@@ -288,7 +281,7 @@ struct Weights {
 };
 // A weight in 32 bits, in the place of its logit: the place turned round, and q; or, with the last place, the weight itself where it is small.
 constexpr uint32_t kSmallPlace = 1023u;
-__device__ __forceinline__ uint32_t code_of(bool fine, int place, int q) { return (fine ? (uint32_t)-place : kSmallPlace) << 22 | ((uint32_t)q & 0x3FFFFFu); }
+__device__ __forceinline__ uint32_t code_of(bool fine, int place, int q) { return (fine ? (uint32_t)(kTopPlace - place) : kSmallPlace) << 22 | ((uint32_t)q & 0x3FFFFFu); }
 
 // floor(f * v) for 0 <= f < 1, v < 2^64, and whether there is a remainder.
 __device__ __forceinline__ uint64_t times(float f, uint64_t v, bool& more) {
@@ -384,13 +377,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
 
   // ---- the row; its first token in falling order; the largest logit of every thread ------------------------
   float mine = -INFINITY;
-  uint32_t mine_at = 0;
-  auto take = [&](float x, uint32_t i) {
-    x = x != x ? -INFINITY : x + 0.f;  // -0 is 0
-    if (x > mine) {
-      mine = x;
-      mine_at = i;
-    }
+  auto take = [&](float x) {
+    x = fmaxf(x + 0.f, -INFINITY);  // -0 is 0, and what is not a number -inf
+    mine = fmaxf(mine, x);
     return x;
   };
   const size_t row_at = (size_t)((int64_t)row * p.row_stride) + from;
@@ -411,69 +400,84 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
         const uint32_t at = i * kPer;
         if constexpr (TYPE == TQ_TYPE_F32) {
           float4 y;
-          y.x = take(__uint_as_float(v[k].x), at);
-          y.y = take(__uint_as_float(v[k].y), at + 1u);
-          y.z = take(__uint_as_float(v[k].z), at + 2u);
-          y.w = take(__uint_as_float(v[k].w), at + 3u);
+          y.x = take(__uint_as_float(v[k].x));
+          y.y = take(__uint_as_float(v[k].y));
+          y.z = take(__uint_as_float(v[k].z));
+          y.w = take(__uint_as_float(v[k].w));
           *reinterpret_cast<float4*>(xs + at) = y;
         } else {
           float4 y, z;
-          y.x = take(bf16_lo(v[k].x), at);
-          y.y = take(bf16_hi(v[k].x), at + 1u);
-          y.z = take(bf16_lo(v[k].y), at + 2u);
-          y.w = take(bf16_hi(v[k].y), at + 3u);
-          z.x = take(bf16_lo(v[k].z), at + 4u);
-          z.y = take(bf16_hi(v[k].z), at + 5u);
-          z.z = take(bf16_lo(v[k].w), at + 6u);
-          z.w = take(bf16_hi(v[k].w), at + 7u);
+          y.x = take(bf16_lo(v[k].x));
+          y.y = take(bf16_hi(v[k].x));
+          y.z = take(bf16_lo(v[k].y));
+          y.w = take(bf16_hi(v[k].y));
+          z.x = take(bf16_lo(v[k].z));
+          z.y = take(bf16_hi(v[k].z));
+          z.z = take(bf16_lo(v[k].w));
+          z.w = take(bf16_hi(v[k].w));
           *reinterpret_cast<float4*>(xs + at) = y;
           *reinterpret_cast<float4*>(xs + at + 4u) = z;
         }
       }
     }
-    for (uint32_t i = whole * kPer + tid; i < n; i += kThreads) xs[i] = take(load1<TYPE>(p.logits, row_at + i), i);
+    for (uint32_t i = whole * kPer + tid; i < n; i += kThreads) xs[i] = take(load1<TYPE>(p.logits, row_at + i));
   } else {
-    for (uint32_t i = tid; i < n; i += kThreads) xs[i] = take(load1<TYPE>(p.logits, row_at + i), i);
+    for (uint32_t i = tid; i < n; i += kThreads) xs[i] = take(load1<TYPE>(p.logits, row_at + i));
   }
   if (tid < 4u && n + tid < (n + 3u) / 4u * 4u) xs[n + tid] = -INFINITY;  // four are read together
   cluster_wait();  // every CTA of the cluster runs: its shared memory can be written
-  uint64_t best;  // 0: nothing is above -inf
-  uint32_t least;  // of the threads' maxima
+  float top, least;  // the largest logit, and the least of the threads' own largest
   {
-    const uint32_t bits = mine > -INFINITY ? rising(mine) : 0u, top_bits = __reduce_max_sync(kFull, bits);
-    const uint32_t at = __reduce_min_sync(kFull, bits == top_bits ? from + mine_at : kIndexMask);
+    const uint32_t bits = mine > -INFINITY ? rising(mine) : 0u, high = __reduce_max_sync(kFull, bits);
     const uint32_t low = ~__reduce_min_sync(kFull, bits ? bits : 0xFFFFFFFFu);  // turned round: 0 where there is none
-    if (lane < ctas) store_remote(&sh.slots[2][rank * kWarps + warp], lane, low);
     uint64_t e[4];
-    tell(top_bits ? ((uint64_t)top_bits << kIndexBits) | (kIndexMask - at) : 0ull, e);
-    best = max(max(e[0], e[1]), max(e[2], e[3]));
-    const uint32_t hi = __reduce_max_sync(kFull, (uint32_t)(best >> kIndexBits));
-    const uint32_t lo = __reduce_max_sync(kFull, (uint32_t)(best >> kIndexBits) == hi ? (uint32_t)best & kIndexMask : 0u);
-    best = hi ? ((uint64_t)hi << kIndexBits) | lo : 0ull;
-    uint32_t l = 0;
+    tell((uint64_t)high << 32 | low, e);
+    uint32_t h = 0, l = 0;
 #pragma unroll
-    for (uint32_t i = 0; i < 4u; ++i)
-      if (lane * 4u + i < ctas * kWarps) l = max(l, (uint32_t)sh.slots[2][lane * 4u + i]);
-    least = ~__reduce_max_sync(kFull, l);
+    for (uint32_t i = 0; i < 4u; ++i) {
+      h = max(h, (uint32_t)(e[i] >> 32));
+      l = max(l, (uint32_t)e[i]);
+    }
+    h = __reduce_max_sync(kFull, h);
+    top = h ? from_rising(h) : -INFINITY;
+    least = from_rising(~__reduce_max_sync(kFull, l));
   }
-  if (best == 0ull || !(temperature > 0.f)) {
+  // warps own consecutive pieces of the slice, a lane four consecutive logits of 128
+  const uint32_t piece = (n + 4u * kThreads - 1u) / (4u * kThreads) * 128u, w0 = min(warp * piece, n), w1 = min(w0 + piece, n);
+  auto read4 = [&](uint32_t i, uint32_t end, float (&x)[4]) {
+    const float4 y = i < end ? *reinterpret_cast<const float4*>(xs + i) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+    x[0] = y.x, x[1] = y.y, x[2] = y.z, x[3] = y.w;  // past the slice's end lies -inf
+  };
+  const bool p_on = top_p < 1.f;
+  // the first token of the largest alone, or none
+  if (top == -INFINITY || !(temperature > 0.f) || !(top_p > 0.f || top_p != top_p) || min_p > 1.f) {
+    uint32_t at = kIndexMask + 1u;
+    for (uint32_t i = w0 + 4u * lane; i < w1 && at > kIndexMask; i += 128u) {
+      float x[4];
+      read4(i, w1, x);
+#pragma unroll
+      for (int j = 3; j >= 0; --j)
+        if (x[j] == top) at = from + i + j;
+    }
+    uint64_t e[4];
+    tell(kIndexMask + 1u - __reduce_min_sync(kFull, at), e);
+    const uint32_t first = __reduce_max_sync(kFull, (uint32_t)max(max(e[0], e[1]), max(e[2], e[3])));
     if (rank == 0 && tid == 0) {
-      p.token[row] = best == 0ull ? -1 : (int32_t)index_of(best);
-      if (p.logprob) p.logprob[row] = best == 0ull ? -INFINITY : 0.f;
+      p.token[row] = top == -INFINITY ? -1 : (int32_t)(kIndexMask + 1u - first);
+      if (p.logprob) p.logprob[row] = top == -INFINITY ? -INFINITY : 0.f;
     }
     return;
   }
-  const bool infinite = logit_of(best) == INFINITY;
+  const bool infinite = top == INFINITY;
   if (infinite) {  // the infinite ones alone are kept, as equals: 0 takes their place, and -inf the others'
     for (uint32_t i = tid; i < (n + 3u) / 4u * 4u; i += kThreads) xs[i] = xs[i] == INFINITY ? 0.f : -INFINITY;
     mine = mine == INFINITY ? 0.f : -INFINITY;
-    least = rising(0.f);
-    best = order_of(0.f, index_of(best));
+    top = least = 0.f;
     __syncthreads();
   }
-  const float top = logit_of(best);
   Weights weight;
   weight.set(top, temperature, sh.powers);
+  const uint64_t best = order_of(top, 0u);  // nothing is before this
   const uint32_t k = k_given > 0 && (uint32_t)k_given < p.vocab ? (uint32_t)k_given : 0u;
 
   uint64_t keep = 0;  // tokens at or after this are kept
@@ -516,12 +520,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
       const float low = d.lo + (t.lo - sum.lo), h = d.hi * kLn2;
       p.logprob[row] = h + fmaf(low, kLn2, fmaf(d.hi, kLn2Low, fmaf(d.hi, kLn2, -h)));
     }
-  };
-  // warps own consecutive pieces of the slice, a lane four consecutive logits of 128
-  const uint32_t piece = (n + 4u * kThreads - 1u) / (4u * kThreads) * 128u, w0 = min(warp * piece, n), w1 = min(w0 + piece, n);
-  auto read4 = [&](uint32_t i, float (&x)[4]) {
-    const float4 y = i < w1 ? *reinterpret_cast<const float4*>(xs + i) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-    x[0] = y.x, x[1] = y.y, x[2] = y.z, x[3] = y.w;  // past the slice's end lies -inf
   };
   // Entries of a warp's lanes into the first CTA's list, in no order.
   auto list4 = [&](const float (&x)[4], uint32_t i, uint32_t mask) {
@@ -572,7 +570,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     return infinite ? (x == INFINITY ? 0.f : -INFINITY) : x != x ? -INFINITY : x + 0.f;
   };
   bool coded = false;  // weights lie where the logits were
-  const bool p_on = top_p < 1.f;
   bool searched = !p_on && k == 0u;  // the border is known
 
   if (k != 0u && k <= kListK) {
@@ -580,7 +577,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     for (uint32_t i = tid; i < kKBins; i += kThreads) sh.k_bins[i] = 0u;
     __syncthreads();
     // bins that fall with x from the largest logit to the least of the maxima; what is below is in the last
-    const float span = top - from_rising(least), scale = span > 0.f && span < INFINITY ? (float)(kKBins - 1u) / span : 0.f;
+    const float span = top - least, scale = span > 0.f && span < INFINITY ? (float)(kKBins - 1u) / span : 0.f;
     auto bin_at = [&](float x) { return min((uint32_t)((top - x) * scale), kKBins - 1u); };
     if (mine > -INFINITY) atomicAdd(&sh.k_bins[bin_at(mine)], 1u);
     cluster_sync();
@@ -603,7 +600,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     const float end = cut == kKBins - 1u || scale == 0.f ? INFINITY : (float)(cut + 1u);
     for (uint32_t i0 = w0; i0 < w1; i0 += 128u) {
       float x[4];
-      read4(i0 + 4u * lane, x);
+      read4(i0 + 4u * lane, w1, x);
       uint32_t mask = 0;
 #pragma unroll
       for (int j = 0; j < 4; ++j) mask |= x[j] > -INFINITY && (top - x[j]) * scale < end ? 1u << j : 0u;
@@ -638,7 +635,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
       if (keep != 0ull) {  // min-p
         uint32_t in = 0;
 #pragma unroll
-        for (uint32_t i = 0; i < kEach; ++i) in += tid * kEach + i < kept && sh.list[tid * kEach + i] >= min(keep, best) ? 1u : 0u;
+        for (uint32_t i = 0; i < kEach; ++i) in += tid * kEach + i < kept && sh.list[tid * kEach + i] >= keep ? 1u : 0u;
         scan(in, total);
         kept = (uint32_t)total;
       }
@@ -682,15 +679,15 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     uint64_t rest = 0;  // of the octaves below
     for (uint32_t i0 = w0; i0 < w1; i0 += 128u) {
       float x[4];
-      read4(i0 + 4u * lane, x);
+      read4(i0 + 4u * lane, w1, x);
       uint32_t code[4];
       weight.four(x, [&](int j, bool fine, int place, int q) {
-        place = max(place, 1 - (int)kBins);
+        place = max(place, kTopPlace + 1 - (int)kBins);
         code[j] = code_of(fine, place, q);
         if (fine) {
           const uint32_t v = weight.value(place, q);
-          atomicAdd(&sh.bins.hi[-place], v >> 15);
-          atomicAdd(&sh.bins.lo[-place], v & 0x7FFFu);
+          atomicAdd(&sh.bins.hi[kTopPlace - place], v >> 15);
+          atomicAdd(&sh.bins.lo[kTopPlace - place], v & 0x7FFFu);
         } else {
           rest += (uint32_t)q;
         }
@@ -716,7 +713,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
       uint64_t sum_hi = 0, sum_lo = 0;
 #pragma unroll
       for (uint32_t r = 0; r < kMaxCluster; ++r) sum_hi += hi[r], sum_lo += lo[r];
-      mass[j] = ((sum_hi << 15) + sum_lo) << Weights::shift(-(int)b);
+      mass[j] = ((sum_hi << 15) + sum_lo) << Weights::shift(kTopPlace - (int)b);
     }
     uint64_t ahead, before_rest;
     const uint64_t sum = mass[0] + mass[1], upto = warp_upto(sum, lane), binned = all(sum, ahead), total = binned + all(rest, before_rest);
@@ -734,14 +731,11 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     }
     cluster_sync();  // (every CTA has read the bins, the list may lie over them)
     const uint64_t bin = sh.told[0], up_to_bin = sh.told[1];
-    if (bound == 0ull) {
-      keep = best;
-      searched = true;
-    } else if (bin != ~0ull) {
+    if (bin != ~0ull) {
       for (uint32_t i0 = w0; i0 < w1; i0 += 128u) {
         const uint32_t i = i0 + 4u * lane;
         float x[4];
-        read4(i, x);
+        read4(i, w1, x);
         uint32_t mask = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) mask |= __float_as_uint(x[j]) >> 22 == (uint32_t)bin ? 1u << j : 0u;
@@ -796,7 +790,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     }
     keep = max(keep, edge);
   }
-  keep = min(keep, best);
 
   // ---- the token up to which more than u of the kept sum lies ---------------------------------------
   const float keep_x = logit_of(keep);  // below it nothing is kept
@@ -808,19 +801,20 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     if (keep_place == 0) {
       int place;
       weight.fine(keep_x, place);
-      keep_place = min(-place, (int)kBins - 1);
+      keep_place = min(kTopPlace - place, (int)kBins - 1);
     }
   }
   // weights of four logits, 0 where they are not kept
-  auto kept = [&](uint32_t i, uint64_t (&w)[4]) {
+  const bool every = keep == 0ull, ties = keep_at != kIndexMask;
+  auto kept = [&](uint32_t i, uint32_t end, uint64_t (&w)[4]) {
     float x[4];
-    read4(i, x);
+    read4(i, end, x);
     if (coded) {
       int place[4];
       bool any = false;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        place[j] = i < w1 ? (int)(__float_as_uint(x[j]) >> 22) : (int)kSmallPlace + 1;
+        place[j] = i < end ? (int)(__float_as_uint(x[j]) >> 22) : (int)kSmallPlace + 1;
         any = any || place[j] <= keep_place;
         w[j] = 0ull;
       }
@@ -834,44 +828,52 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
           if (y < keep_x || (y == keep_x && from + i + j > keep_at)) continue;
         }
         w[j] = place[j] == (int)kSmallPlace ? code & 0x3FFFFFu
-                                            : (uint64_t)weight.value(-place[j], (int)(code << 10) >> 10) << Weights::shift(-place[j]);
+                                            : (uint64_t)weight.value(kTopPlace - place[j], (int)(code << 10) >> 10) << Weights::shift(kTopPlace - place[j]);
       }
       return true;
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (x[j] < keep_x || (x[j] == keep_x && from + i + j > keep_at)) x[j] = -INFINITY;
-      w[j] = 0ull;
+    for (int j = 0; j < 4; ++j) w[j] = 0ull;
+    if (!every) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (x[j] < keep_x || (ties && x[j] == keep_x && from + i + j > keep_at)) x[j] = -INFINITY;
+      if (!__any_sync(kFull, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) > -INFINITY)) return false;
     }
-    if (!__any_sync(kFull, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) > -INFINITY)) return false;
     weight.four(x, [&](int j, bool fine, int place, int q) { w[j] = fine ? (uint64_t)weight.value(place, q) << Weights::shift(place) : (uint64_t)(uint32_t)q; });
     return true;
   };
   uint64_t sum_mine = 0, sum;
   for (uint32_t i0 = w0; i0 < w1; i0 += 128u) {
     uint64_t w[4];
-    kept(i0 + 4u * lane, w);
+    kept(i0 + 4u * lane, w1, w);
     sum_mine += (w[0] + w[1]) + (w[2] + w[3]);
   }
+  if (tid == 0) sh.told[0] = ~0ull;
   const uint64_t of_warp = warp_sum(sum_mine), total = all(sum_mine, sum), target = target_of(total);
-  if (target < sum || target >= sum + of_warp) return;  // another warp has it
-  for (uint32_t i0 = w0; i0 < w1; i0 += 128u) {
-    const uint32_t i = i0 + 4u * lane;
-    uint64_t w[4];
-    if (!kept(i, w)) continue;
-    const uint64_t own = (w[0] + w[1]) + (w[2] + w[3]), upto = warp_upto(own, lane);
-    const uint32_t past = __ballot_sync(kFull, sum + upto > target);
-    if (past) {
-      if (lane == __ffs(past) - 1u) {
-        sum += upto - own;
-        uint32_t j = 0;
-        while (j < 3u && sum + w[j] <= target) sum += w[j++];
-        answer(order_of(coded ? logit_at(i + j) : xs[i + j], from + i + j), total);
-      }
-      return;
-    }
-    sum += __shfl_sync(kFull, upto, 31);
+  if (lane == 0 && target >= sum && target < sum + of_warp) {
+    sh.told[0] = warp;
+    sh.told[1] = sum;
   }
+  __syncthreads();
+  if (sh.told[0] == ~0ull) return;  // another CTA has it
+  // a warp of the CTA to each 128 logits of the piece that has it (there are no more of them than warps)
+  static_assert(TQ_SAMPLE_MAX_VOCAB / kMaxCluster / kWarps <= 128u * kWarps, "a piece has a part for every warp at most");
+  const uint32_t p0 = min((uint32_t)sh.told[0] * piece, n), p1 = min(p0 + piece, n), i = p0 + warp * 128u + 4u * lane;
+  uint64_t w[4] = {0, 0, 0, 0};
+  kept(i, p1, w);
+  const uint64_t own = (w[0] + w[1]) + (w[2] + w[3]);
+  uint64_t in_piece, at = sh.told[1] + scan(own, in_piece);
+  if (target < at || target >= at + own) return;
+  uint32_t j = 0;
+#pragma unroll
+  for (uint32_t x = 0; x < 3u; ++x) {
+    if (j == x && at + w[x] <= target) {
+      at += w[x];
+      ++j;
+    }
+  }
+  answer(order_of(coded ? logit_at(i + j) : xs[i + j], from + i + j), total);
 }
 
 template <int TYPE>

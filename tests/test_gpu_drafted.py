@@ -537,6 +537,7 @@ def test_sample_of_equals(tq):
         sample_case(tq, x, u)
         sample_case(tq, x, u, top_k=i32([1, 2, 3, 10, 100, 500, 501, 1023, 1024, 1025, 1500, 2047, 2048, 2049, 2999, 3000]))
         sample_case(tq, x, u, top_p=f32([0.1 + 0.05 * r for r in range(R)]))
+        sample_case(tq, x, u, min_p=f32([0.0, 0.1, 0.5, 0.9999, 1.0, 1.0000001, 2.0, INF] * 2), temperature=f32([0.7] * R))
         sample_case(tq, x, u, top_k=i32([700] * R), top_p=f32([0.1 + 0.05 * r for r in range(R)]), temperature=f32([0.5] * R))
         assert sample_case(tq, x, u, temperature=f32([0.0] * R)).tolist() == [int((r == r.max()).nonzero()[0]) for r in x]
 
