@@ -114,7 +114,7 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
 __device__ __forceinline__ void copies_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 // Units that a group counts beside its tiles of states: what its end and the next one's beginning cost the softmax warps.
-constexpr uint32_t kGroupUnits = 1;
+constexpr uint32_t kGroupUnits = 5;
 
 // A group of the list of work: tile rt of the rows of sequence b over key-value head kvh.
 struct Walk {
@@ -290,6 +290,10 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
     }
     mbar_init(bar(L::kBarMl, 0), kSoftWarps);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (TMA && threadIdx.x == 32u * kLoadWarp) {  // the maps are on their way before the first copy wants them
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
   }
   if (warp == kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(kTmemCols) : "memory");
