@@ -81,8 +81,10 @@ struct TreeSmem {
   static constexpr uint32_t kSlabs = D / 64;                       // 64 columns = 128 bytes of a swizzled row
   static constexpr uint32_t kTileBytes = kSlabs * kStates * 128;   // queries, keys or values of a tile
   // Buffers of queries, keys and values.  Keys and values have a ring each: values are wanted a softmax later than keys, and in one ring they
-  // would wait in slots that keys could use.
-  static constexpr uint32_t kQueries = D == 128 ? 1 : 2, kKeys = D == 128 ? 3 : 6, kValues = D == 128 ? 3 : 5;
+  // would wait in slots that keys could use.  More is not better: 128 KB under way on every SM are three times what the memory's latency asks for,
+  // and what is beyond that waits in the memory system and lets other accesses (parts, page tables) wait with it.  Measured at head_dim 128 (us, two
+  // keys and values | three of each): 64 chains 387 | 423, 131071 states 103.5 | 117.6, 8 ragged 35.0 | 39.2.
+  static constexpr uint32_t kQueries = D == 128 ? 1 : 2, kKeys = D == 128 ? 2 : 4, kValues = D == 128 ? 2 : 4;
   // The loading warps of the other path work in teams, a tile to a team in turn: a team waits for its copies and announces them, the others' are
   // under way.
   static constexpr uint32_t kTeams = D == 128 ? 2 : 4;
@@ -114,7 +116,7 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
 __device__ __forceinline__ void copies_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 // Units that a group counts beside its tiles of states: what its end and the next one's beginning cost the softmax warps.
-constexpr uint32_t kGroupUnits = 5;
+constexpr uint32_t kGroupUnits = 3;
 
 // A group of the list of work: tile rt of the rows of sequence b over key-value head kvh.
 struct Walk {
