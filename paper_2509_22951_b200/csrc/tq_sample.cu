@@ -42,6 +42,8 @@ constexpr uint32_t kBins = kOctaves * 32u + 3u;  // a place each; the last has w
 constexpr uint32_t kList = 2048;   // tokens that one CTA sorts
 constexpr uint32_t kListK = 1024;  // largest k of the list: the threads' maxima bound it well up to a quarter of their number
 constexpr uint32_t kKBins = 256;   // of the threads' maxima
+constexpr uint32_t kSub = 256;     // parts of the bin with the border
+constexpr uint32_t kNear = 128;    // tokens that are compared each with each
 
 // 2^(i / 32) with 29 bits behind the point
 struct Powers {
@@ -79,9 +81,15 @@ struct SampleParams {
 struct Shared {
   uint64_t slots[2][kMaxCluster * kWarps];  // what the cluster's warps tell one another; two sets, used in turn
   uint64_t told[2];                         // by one CTA to all
+  uint64_t found[2];                        // the warp whose piece has the token, and what is before it
   uint64_t warps[kWarps];                   // within a CTA
   uint32_t powers[32];                      // 2^(i / 32) with 29 bits behind the point
   uint32_t listed;                          // tokens in the list (of the first CTA)
+  uint32_t near;                            // entries of `close`
+  struct {
+    uint32_t hi[kSub], lo[kSub];
+  } sub;                                    // as bins, of parts of one bin
+  uint64_t close[kNear], close_w[kNear];    // tokens next to the border, and their weights
   union {
     struct {
       uint32_t hi[kBins], lo[kBins];  // sums of the upper and lower 15 bits of the values of a bin
@@ -306,20 +314,20 @@ __device__ __forceinline__ uint64_t bound_of(float f, uint64_t v) {
 
 // Sorts list[0 .. n), n <= kList, from the largest down: by every entry's rank where there are few, else bitonic.
 __device__ void sort_list(uint64_t* list, uint32_t n, uint32_t tid) {
-  if (n <= 128u) {
-    uint64_t mine = 0ull;
+  if (n <= kThreads / 2u) {
+    const uint32_t each = n <= kThreads / 4u ? 4u : 2u, j = tid / each;  // threads to an entry
+    const uint64_t mine = j < n ? list[j] : ~0ull;
     uint32_t rank = 0;
-    if (tid < n) {
-      mine = list[tid];
-#pragma unroll 8
-      for (uint32_t i = 0; i < n; ++i) rank += list[i] > mine ? 1u : 0u;
-    }
+#pragma unroll 4
+    for (uint32_t i = tid % each; i < n; i += each) rank += list[i] > mine ? 1u : 0u;
+    rank += __shfl_xor_sync(kFull, rank, 1);
+    if (each == 4u) rank += __shfl_xor_sync(kFull, rank, 2);
     __syncthreads();
-    if (tid < n) list[rank] = mine;
+    if (j < n && tid % each == 0u) list[rank] = mine;
     __syncthreads();
     return;
   }
-  uint32_t size = 256;
+  uint32_t size = 512;
   while (size < n) size *= 2u;
   for (uint32_t i = n + tid; i < size; i += kThreads) list[i] = 0ull;
   __syncthreads();
@@ -347,7 +355,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u, rank = cluster_rank(), ctas = cluster_size();
   const uint32_t row = blockIdx.x / ctas, from = min(rank * p.slice, p.vocab), n = min(p.slice, p.vocab - from);
   if (tid < 32) sh.powers[tid] = kPowers.v[tid];
-  if (tid == 0) sh.listed = 0u;
+  if (tid == 0) {
+    sh.listed = sh.near = 0u;
+    sh.told[0] = sh.found[0] = ~0ull;
+  }
   cluster_arrive();
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const float temperature = p.temperature ? p.temperature[row] : 1.f;
@@ -373,6 +384,29 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     for (uint32_t i = 0; i < 4u; ++i) b += lane * 4u + i < at ? e[i] : 0ull;
     prev = warp_sum(b);
     return warp_sum(e[0] + e[1] + e[2] + e[3]);
+  };
+
+  // The same of two numbers.  Both sets of slots at once: the cluster comes together before and after it.
+  auto all_of_two = [&](uint64_t mine, uint64_t other, uint64_t& prev, uint64_t& sum_of_other) {
+    const uint64_t a = warp_sum(mine), b = warp_sum(other);
+    if (lane < ctas) {
+      store_remote(&sh.slots[0][rank * kWarps + warp], lane, a);
+      store_remote(&sh.slots[1][rank * kWarps + warp], lane, b);
+    }
+    cluster_sync();
+    const uint32_t at = rank * kWarps + warp;
+    uint64_t sum = 0, others = 0, ahead = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < 4u; ++i) {
+      const uint32_t j = lane * 4u + i;
+      const uint64_t e = j < ctas * kWarps ? sh.slots[0][j] : 0ull;
+      others += j < ctas * kWarps ? sh.slots[1][j] : 0ull;
+      sum += e;
+      ahead += j < at ? e : 0ull;
+    }
+    prev = warp_sum(ahead);
+    sum_of_other = warp_sum(others);
+    return warp_sum(sum);
   };
 
   // ---- the row; its first token in falling order; the largest logit of every thread ------------------------
@@ -425,6 +459,13 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     for (uint32_t i = tid; i < n; i += kThreads) xs[i] = take(load1<TYPE>(p.logits, row_at + i));
   }
   if (tid < 4u && n + tid < (n + 3u) / 4u * 4u) xs[n + tid] = -INFINITY;  // four are read together
+  if (k_given > 0) {
+    for (uint32_t i = tid; i < kKBins; i += kThreads) sh.k_bins[i] = 0u;
+  }
+  if (top_p < 1.f) {
+    for (uint32_t i = tid; i < kBins; i += kThreads) sh.bins.hi[i] = sh.bins.lo[i] = 0u;
+    if (tid < kSub) sh.sub.hi[tid] = sh.sub.lo[tid] = 0u;
+  }
   cluster_wait();  // every CTA of the cluster runs: its shared memory can be written
   float top, least;  // the largest logit, and the least of the threads' own largest
   {
@@ -521,18 +562,26 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
       p.logprob[row] = h + fmaf(low, kLn2, fmaf(d.hi, kLn2Low, fmaf(d.hi, kLn2, -h)));
     }
   };
-  // Entries of a warp's lanes into the first CTA's list, in no order.
-  auto list4 = [&](const float (&x)[4], uint32_t i, uint32_t mask) {
-    const uint32_t own = __popc(mask), upto = warp_upto(own, lane);
+  // Tokens of a warp's piece into the first CTA's list, in no order: 4 bits of hits[] for each 128 logits of the piece.
+  constexpr uint32_t kBlocks = TQ_SAMPLE_MAX_VOCAB / kMaxCluster / kWarps / 1024u;  // of 1024 logits of a piece
+  auto place_of = [&](uint32_t block, uint32_t bit) { return w0 + block * 1024u + (bit >> 2) * 128u + 4u * lane + (bit & 3u); };
+  auto list_hits = [&](const uint32_t (&hits)[kBlocks], auto logit) {
+    uint32_t own = 0;
+#pragma unroll
+    for (uint32_t b = 0; b < kBlocks; ++b) own += __popc(hits[b]);
+    if (!__any_sync(kFull, own != 0u)) return;
+    const uint32_t upto = warp_upto(own, lane);
     uint32_t at = 0;
     if (lane == 31) at = add_remote(&sh.listed, 0u, upto);
     at = __shfl_sync(kFull, at, 31) + upto - own;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (!((mask >> j) & 1u)) continue;
-      if (at < kList) store_remote(&sh.list[at], 0u, order_of(x[j], from + i + j));
-      ++at;
+    for (uint32_t b = 0; b < kBlocks; ++b) {
+      for (uint32_t left = hits[b]; left != 0u; left &= left - 1u, ++at) {
+        const uint32_t i = place_of(b, __ffs(left) - 1u);
+        if (at < kList) store_remote(&sh.list[at], 0u, order_of(logit(i), from + i));
+      }
     }
+    __syncwarp();
   };
   constexpr uint32_t kEach = kList / kThreads;  // consecutive entries of the list to a thread
   // Sums over the threads of a CTA, and what is of the threads before.
@@ -569,13 +618,93 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     const float x = load1<TYPE>(p.logits, row_at + i);
     return infinite ? (x == INFINITY ? 0.f : -INFINITY) : x != x ? -INFINITY : x + 0.f;
   };
+  // A weight out of 32 bits.
+  auto weight_of = [&](uint32_t code) {
+    const uint32_t turned = code >> 22;
+    if (turned == kSmallPlace) return (uint64_t)(code & 0x3FFFFFu);
+    const int place = kTopPlace - (int)turned;
+    return (uint64_t)weight.value(place, (int)(code << 10) >> 10) << Weights::shift(place);
+  };
+  // Of the m tokens of a bin in the list the one with which their sum, from the largest down, reaches `bound`: told to the cluster, by its first CTA.
+  auto border_in_list = [&](uint32_t m, uint64_t bound, uint32_t bin) {
+    const int place = kTopPlace - (int)bin, shift = Weights::shift(place);
+    // Parts of the bin that fall with x; which token is in which decides nothing but the work.
+    const float middle = weight.plain ? (weight.a + (float)place * 0.03125f) / weight.c : weight.top + (float)place * 0.03125f / weight.c;
+    const float per = weight.c * 32.f * (float)kSub;
+    auto part = [&](float x) { return (uint32_t)fminf(fmaxf((middle - x) * per + 0.5f * (float)kSub, 0.f), (float)(kSub - 1u)); };
+    const bool parts = m > kNear;
+    uint64_t ahead = 0;
+    uint32_t chosen = 0;
+    if (parts) {
+      for (uint32_t i = tid; i < m; i += kThreads) {
+        const float x = logit_of(sh.list[i]);
+        const uint32_t v = (uint32_t)(weight(x) >> shift), b = part(x);
+        atomicAdd(&sh.sub.hi[b], v >> 15);
+        atomicAdd(&sh.sub.lo[b], v & 0x7FFFu);
+      }
+      __syncthreads();
+      const uint64_t mass = tid < kSub ? (((uint64_t)sh.sub.hi[tid] << 15) + sh.sub.lo[tid]) << shift : 0ull;
+      uint64_t sum;
+      const uint64_t prev = scan(mass, sum);
+      if (prev < bound && prev + mass >= bound) {
+        sh.told[0] = tid;
+        sh.told[1] = prev;
+      }
+      __syncthreads();
+      chosen = (uint32_t)sh.told[0];
+      ahead = sh.told[1];
+    }
+    for (uint32_t i = tid; i < m; i += kThreads) {
+      const uint64_t order = sh.list[i];
+      const float x = logit_of(order);
+      if (parts && part(x) != chosen) continue;
+      const uint32_t at = atomicAdd(&sh.near, 1u);
+      if (at >= kNear) continue;
+      sh.close[at] = order;
+      sh.close_w[at] = weight(x);
+    }
+    __syncthreads();
+    const uint32_t near = sh.near;
+    if (near <= kNear) {  // each with each, four threads to a token
+      const uint32_t j = tid / 4u;
+      const uint64_t order = j < near ? sh.close[j] : ~0ull;
+      uint64_t at = 0;
+      for (uint32_t i = tid % 4u; i < near; i += 4u) at += sh.close[i] > order ? sh.close_w[i] : 0ull;
+      at += __shfl_xor_sync(kFull, at, 1);
+      at += __shfl_xor_sync(kFull, at, 2);
+      at += ahead;
+      if (j < near && at < bound && at + sh.close_w[j] >= bound) {
+        for (uint32_t r = tid % 4u; r < ctas; r += 4u) store_remote(&sh.told[0], r, order);
+      }
+      return;
+    }
+    sort_list(sh.list, m, tid);
+    uint64_t w[kEach], own = 0, sum;
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i) {
+      const uint32_t j = tid * kEach + i;
+      w[i] = j < m ? weight(logit_of(sh.list[j])) : 0ull;
+      own += w[i];
+    }
+    uint64_t at = scan(own, sum);
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i) {
+      const uint32_t j = tid * kEach + i;
+      if (j < m && at < bound && at + w[i] >= bound) {
+        for (uint32_t r = 0; r < ctas; ++r) store_remote(&sh.told[0], r, sh.list[j]);
+      }
+      at += w[i];
+    }
+  };
   bool coded = false;  // weights lie where the logits were
+  bool summed = false;  // sum_mine has what is before the bin of the border, hits[] the tokens in it
+  bool whole_bin = false;  // and all of them are kept
+  uint64_t sum_mine = 0;
+  uint32_t hits[kBlocks] = {}, border_bin = 0;
   bool searched = !p_on && k == 0u;  // the border is known
 
   if (k != 0u && k <= kListK) {
     // ---- top-k: a bound from the threads' maxima, and a list -----------------------------------------------
-    for (uint32_t i = tid; i < kKBins; i += kThreads) sh.k_bins[i] = 0u;
-    __syncthreads();
     // bins that fall with x from the largest logit to the least of the maxima; what is below is in the last
     const float span = top - least, scale = span > 0.f && span < INFINITY ? (float)(kKBins - 1u) / span : 0.f;
     auto bin_at = [&](float x) { return min((uint32_t)((top - x) * scale), kKBins - 1u); };
@@ -598,14 +727,18 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     const uint32_t cut = (uint32_t)sh.told[0];
     // the products of bin_at, compared with the bin's end; where all are alike, or in the last bin, everything is listed
     const float end = cut == kKBins - 1u || scale == 0.f ? INFINITY : (float)(cut + 1u);
-    for (uint32_t i0 = w0; i0 < w1; i0 += 128u) {
-      float x[4];
-      read4(i0 + 4u * lane, w1, x);
-      uint32_t mask = 0;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) mask |= x[j] > -INFINITY && (top - x[j]) * scale < end ? 1u << j : 0u;
-      if (__any_sync(kFull, mask != 0u)) list4(x, i0 + 4u * lane, mask);
+    for (uint32_t b = 0; b < kBlocks; ++b) {
+      for (uint32_t s = 0; s < 8u && w0 + b * 1024u + s * 128u < w1; ++s) {
+        float x[4];
+        read4(w0 + b * 1024u + s * 128u + 4u * lane, w1, x);
+        uint32_t mask = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) mask |= x[j] > -INFINITY && (top - x[j]) * scale < end ? 1u << j : 0u;
+        hits[b] |= mask << (4u * s);
+      }
     }
+    list_hits(hits, [&](uint32_t i) { return xs[i]; });
     cluster_sync();
     const uint32_t m = load_remote(&sh.listed, 0u);
     if (m <= kList) {
@@ -673,9 +806,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   if (!searched && k == 0u) {
     // ---- top-p: a histogram of the weights, and a list of the bin with the border -----------------------------
     // (the logits of a bin's tokens are read again from memory, for their order)
-    for (uint32_t i = tid; i < kBins; i += kThreads) sh.bins.hi[i] = sh.bins.lo[i] = 0u;
-    if (tid == 0) sh.told[0] = ~0ull;
-    __syncthreads();
     uint64_t rest = 0;  // of the octaves below
     for (uint32_t i0 = w0; i0 < w1; i0 += 128u) {
       float x[4];
@@ -715,15 +845,19 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
       for (uint32_t r = 0; r < kMaxCluster; ++r) sum_hi += hi[r], sum_lo += lo[r];
       mass[j] = ((sum_hi << 15) + sum_lo) << Weights::shift(kTopPlace - (int)b);
     }
-    uint64_t ahead, before_rest;
-    const uint64_t sum = mass[0] + mass[1], upto = warp_upto(sum, lane), binned = all(sum, ahead), total = binned + all(rest, before_rest);
+    uint64_t ahead, below;
+    const uint64_t sum = mass[0] + mass[1], upto = warp_upto(sum, lane), total = all_of_two(sum, rest, ahead, below) + below;
     const uint64_t bound = bound_of(top_p, total);
     uint64_t prev = ahead + upto - sum;
 #pragma unroll
     for (uint32_t j = 0; j < 2u; ++j) {
       if (mass[j] != 0ull && prev < bound && prev + mass[j] >= bound) {
+        // less than two of the bin's least weights (2^(-1/64) of the one in its middle) are one token
+        const uint32_t b = rank * share + tid * each + j;
+        const int place = kTopPlace - (int)b;
+        const uint64_t one = (uint64_t)weight.value(place, 0) << Weights::shift(place), single = mass[j] < 2u * one - one / 16u ? 1ull << 32 : 0ull;
         for (uint32_t r = 0; r < ctas; ++r) {
-          store_remote(&sh.told[0], r, rank * share + tid * each + j);
+          store_remote(&sh.told[0], r, single | b);
           store_remote(&sh.told[1], r, prev);
         }
       }
@@ -732,46 +866,43 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     cluster_sync();  // (every CTA has read the bins, the list may lie over them)
     const uint64_t bin = sh.told[0], up_to_bin = sh.told[1];
     if (bin != ~0ull) {
-      for (uint32_t i0 = w0; i0 < w1; i0 += 128u) {
-        const uint32_t i = i0 + 4u * lane;
-        float x[4];
-        read4(i, w1, x);
-        uint32_t mask = 0;
+      border_bin = (uint32_t)bin;
+      whole_bin = bin >> 32 != 0ull && keep == 0ull;
+      const uint32_t whole = border_bin + (whole_bin ? 1u : 0u);  // places below this are kept
 #pragma unroll
-        for (int j = 0; j < 4; ++j) mask |= __float_as_uint(x[j]) >> 22 == (uint32_t)bin ? 1u << j : 0u;
-        if (i >= w1) mask = 0;
-        if (!__any_sync(kFull, mask != 0u)) continue;
+      for (uint32_t b = 0; b < kBlocks; ++b) {
+        for (uint32_t s = 0; s < 8u && w0 + b * 1024u + s * 128u < w1; ++s) {
+          float x[4];
+          read4(w0 + b * 1024u + s * 128u + 4u * lane, w1, x);  // (past the end: a place that no bin has)
+          uint32_t code[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if ((mask >> j) & 1u) x[j] = logit_at(i + j);
-        list4(x, i, mask);
+          for (int j = 0; j < 4; ++j) code[j] = __float_as_uint(x[j]);
+          if (!__any_sync(kFull, min(min(code[0], code[1]), min(code[2], code[3])) >> 22 <= border_bin)) continue;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t place = code[j] >> 22;
+            if (place < whole)
+              sum_mine += weight_of(code[j]);
+            else if (place == border_bin)
+              hits[b] |= 1u << (4u * s + j);
+          }
+        }
       }
+      summed = keep == 0ull;
+    }
+    if (whole_bin) {
+      searched = true;
+    } else if (bin != ~0ull) {
+      list_hits(hits, logit_at);
       cluster_sync();
       const uint32_t m = load_remote(&sh.listed, 0u);
       if (m <= kList) {
-        if (rank == 0) {
-          sort_list(sh.list, m, tid);
-          // the last entry before which less than the bound lies
-          uint64_t w[kEach], own = 0, in_bin;
-#pragma unroll
-          for (uint32_t i = 0; i < kEach; ++i) {
-            const uint32_t j = tid * kEach + i;
-            w[i] = j < m ? weight(logit_of(sh.list[j])) : 0ull;
-            own += w[i];
-          }
-          uint64_t at = up_to_bin + scan(own, in_bin);
-#pragma unroll
-          for (uint32_t i = 0; i < kEach; ++i) {
-            const uint32_t j = tid * kEach + i;
-            if (j < m && at < bound && (j + 1u == m || at + w[i] >= bound)) {
-              for (uint32_t r = 0; r < ctas; ++r) store_remote(&sh.told[0], r, sh.list[j]);
-            }
-            at += w[i];
-          }
-        }
+        if (rank == 0) border_in_list(m, bound - up_to_bin, border_bin);
         cluster_sync();
         keep = max(keep, sh.told[0]);
         searched = true;
+      } else {
+        summed = false;
       }
     }
   }
@@ -794,16 +925,28 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   // ---- the token up to which more than u of the kept sum lies ---------------------------------------
   const float keep_x = logit_of(keep);  // below it nothing is kept
   const uint32_t keep_at = index_of(keep);  // and of its equals the first ones
-  int keep_place = 1;  // coded: places above (weights below) are not kept, of this one's tokens it goes by the logit
-  if (coded) {
+  // coded: places above this (weights below) are not kept; of the tokens of edge_place it goes by the logit, where their q is next to the border's:
+  // q rises with x but for its roundings, together less than 2 units.
+  int keep_place = 1, edge_place = -1, edge_q = 0, edge_near = 2;
+  if (coded && whole_bin) {
+    keep_place = (int)border_bin;
+  } else if (coded) {
     const float t = weight.coarse(keep_x);
     keep_place = keep_x == -INFINITY || !(keep_x == keep_x) || t < -(float)kOctaves ? (int)kSmallPlace : 0;
     if (keep_place == 0) {
       int place;
-      weight.fine(keep_x, place);
+      edge_q = weight.fine(keep_x, place);
       keep_place = min(kTopPlace - place, (int)kBins - 1);
     }
+    edge_place = keep_place;
+    if (keep_place >= (int)kBins - 1) edge_near = 1 << 24;  // of several places: always by the logit
   }
+  auto in_edge = [&](uint32_t i, uint32_t code) {
+    const int d = ((int)(code << 10) >> 10) - edge_q;
+    if (d > edge_near || d < -edge_near) return d > 0;
+    const float y = i < n ? logit_at(i) : -INFINITY;
+    return y > keep_x || (y == keep_x && from + i <= keep_at);
+  };
   // weights of four logits, 0 where they are not kept
   const bool every = keep == 0ull, ties = keep_at != kIndexMask;
   auto kept = [&](uint32_t i, uint32_t end, uint64_t (&w)[4]) {
@@ -823,12 +966,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
       for (int j = 0; j < 4; ++j) {
         if (place[j] > keep_place) continue;
         const uint32_t code = __float_as_uint(x[j]);
-        if (place[j] == keep_place) {
-          const float y = i + j < n ? logit_at(i + j) : -INFINITY;
-          if (y < keep_x || (y == keep_x && from + i + j > keep_at)) continue;
-        }
-        w[j] = place[j] == (int)kSmallPlace ? code & 0x3FFFFFu
-                                            : (uint64_t)weight.value(kTopPlace - place[j], (int)(code << 10) >> 10) << Weights::shift(kTopPlace - place[j]);
+        if (place[j] == edge_place && !in_edge(i + j, code)) continue;
+        w[j] = weight_of(code);
       }
       return true;
     }
@@ -843,27 +982,40 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     weight.four(x, [&](int j, bool fine, int place, int q) { w[j] = fine ? (uint64_t)weight.value(place, q) << Weights::shift(place) : (uint64_t)(uint32_t)q; });
     return true;
   };
-  uint64_t sum_mine = 0, sum;
-  for (uint32_t i0 = w0; i0 < w1; i0 += 128u) {
-    uint64_t w[4];
-    kept(i0 + 4u * lane, w1, w);
-    sum_mine += (w[0] + w[1]) + (w[2] + w[3]);
+  uint64_t sum;
+  if (summed) {
+    if (!whole_bin) {
+#pragma unroll
+      for (uint32_t b = 0; b < kBlocks; ++b) {
+        for (uint32_t left = hits[b]; left != 0u; left &= left - 1u) {
+          const uint32_t i = place_of(b, __ffs(left) - 1u), code = __float_as_uint(xs[i]);
+          if (in_edge(i, code)) sum_mine += weight_of(code);
+        }
+      }
+      __syncwarp();
+    }
+  } else {
+    sum_mine = 0;
+    for (uint32_t i0 = w0; i0 < w1; i0 += 128u) {
+      uint64_t w[4];
+      kept(i0 + 4u * lane, w1, w);
+      sum_mine += (w[0] + w[1]) + (w[2] + w[3]);
+    }
   }
-  if (tid == 0) sh.told[0] = ~0ull;
   const uint64_t of_warp = warp_sum(sum_mine), total = all(sum_mine, sum), target = target_of(total);
   if (lane == 0 && target >= sum && target < sum + of_warp) {
-    sh.told[0] = warp;
-    sh.told[1] = sum;
+    sh.found[0] = warp;
+    sh.found[1] = sum;
   }
   __syncthreads();
-  if (sh.told[0] == ~0ull) return;  // another CTA has it
+  if (sh.found[0] == ~0ull) return;  // another CTA has it
   // a warp of the CTA to each 128 logits of the piece that has it (there are no more of them than warps)
   static_assert(TQ_SAMPLE_MAX_VOCAB / kMaxCluster / kWarps <= 128u * kWarps, "a piece has a part for every warp at most");
-  const uint32_t p0 = min((uint32_t)sh.told[0] * piece, n), p1 = min(p0 + piece, n), i = p0 + warp * 128u + 4u * lane;
+  const uint32_t p0 = min((uint32_t)sh.found[0] * piece, n), p1 = min(p0 + piece, n), i = p0 + warp * 128u + 4u * lane;
   uint64_t w[4] = {0, 0, 0, 0};
   kept(i, p1, w);
   const uint64_t own = (w[0] + w[1]) + (w[2] + w[3]);
-  uint64_t in_piece, at = sh.told[1] + scan(own, in_piece);
+  uint64_t in_piece, at = sh.found[1] + scan(own, in_piece);
   if (target < at || target >= at + own) return;
   uint32_t j = 0;
 #pragma unroll

@@ -542,6 +542,22 @@ def test_sample_of_equals(tq):
         assert sample_case(tq, x, u, temperature=f32([0.0] * R)).tolist() == [int((r == r.max()).nonzero()[0]) for r in x]
 
 
+@pytest.mark.parametrize("vocab,scale", [(2500, 0.02), (30000, 1.0), (128256, 0.3), (128256, 1.5), (262144, 1.0), (262144, 2.5)])
+def test_sample_where_the_border_is_crowded(tq, vocab, scale):
+    """Top-p among few, hundreds and thousands of weights next to one another, distinct and (16 bits) in groups of equals, with and without min-p."""
+    g, R = gen(vocab + 1), 12
+    u, p = torch.rand(R, generator=g, device="cuda"), f32([0.02, 0.1, 0.3, 0.5, 0.7, 0.8, 0.9, 0.95, 0.97, 0.99, 0.999, 0.9999])
+    for dtype in (F32, BF):
+        x = randn(g, R, vocab, dtype=dtype, scale=scale)
+        for t in (0.4, 1.0):
+            sample_case(tq, x, u, temperature=f32([t] * R), top_p=p)
+        sample_case(tq, x, u, top_p=p, min_p=f32([0.0, 1e-3, 0.2] * (R // 3)))
+        # the draw at the far end is the last kept token: a border one place off shows
+        sample_case(tq, x, torch.full((R,), 1.0 - 2.0 ** -24, device="cuda"), top_p=p)
+    x[:, ::7] = x[:, :1]  # a seventh of the row is one logit
+    sample_case(tq, x, u, top_p=p)
+
+
 def test_sample_of_what_is_not_finite(tq):
     g, V = gen(31), 20000
     x = logits(g, 12, V)
