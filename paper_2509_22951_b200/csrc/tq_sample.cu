@@ -38,7 +38,7 @@ constexpr uint32_t kIndexMask = (1u << kIndexBits) - 1u;
 constexpr int kOne = 45;      // W of the largest logit is 2^45
 constexpr int kOctaves = 24;  // of the histogram, and of the weights that are computed to 29 bits
 constexpr int kTopPlace = 1;  // place of the largest logit at most (a is off by up to 1/64 and a little)
-constexpr uint32_t kBins = kOctaves * 32u + 3u;  // a place each; the last has what a rounding puts below
+constexpr uint32_t kBins = kOctaves * 32u + kTopPlace + 1u;  // a place each
 constexpr uint32_t kList = 2048;   // tokens that one CTA sorts
 constexpr uint32_t kListK = 1024;  // largest k of the list: the threads' maxima bound it well up to a quarter of their number
 constexpr uint32_t kKBins = 256;   // of the threads' maxima
@@ -94,9 +94,9 @@ struct Shared {
     struct {
       uint32_t hi[kBins], lo[kBins];  // sums of the upper and lower 15 bits of the values of a bin
     } bins;
-    uint64_t list[kList];
     uint32_t k_bins[kKBins];
   };
+  uint64_t list[kList];
 };
 constexpr uint32_t kHead = (sizeof(Shared) + 15u) / 16u * 16u;  // the row's slice lies behind it
 
@@ -205,6 +205,7 @@ struct Weights {
   float top;          // largest logit, finite
   float c, c_low;     // log2(e) / temperature
   float a, a_low;     // top * log2(e) / temperature: a multiple of 1/32, and the rest
+  float to_small;     // what base() lacks to 45 + t
   bool plain;         // a is small enough for the short form
   const uint32_t* powers;
 
@@ -218,27 +219,27 @@ struct Weights {
     plain = fabsf(full) < 65536.f;
     a = plain ? rintf(full * 32.f) * 0.03125f : 0.f;
     a_low = fmaf(top, c, -a) + top * c_low;
+    to_small = (float)kOne - (plain ? a_low : 0.f);
   }
-  // t in fp32; -inf where x is
-  __device__ __forceinline__ float coarse(float x) const { return plain ? fmaf(x, c, -a) - a_low : (x - top) * c; }
+  // t in fp32, to a constant below 1/32; -inf where x is
+  __device__ __forceinline__ float base(float x) const { return plain ? fmaf(x, c, -a) : (x - top) * c; }
   __device__ __forceinline__ Pair both(float x) const {
     const Pair d = exact_sum(x, -top);
     const float t = d.hi * c;
     return Pair{t, fmaf(d.lo, c, fmaf(d.hi, c_low, fmaf(d.hi, c, -t)))};
   }
-  // 2^t = 2^(place / 32) (1 + q 2^-26), for t from 0 down to some octaves below the histogram's.
-  __device__ __forceinline__ int fine(float x, int& place) const {
-    constexpr float kRound = 393216.0f, kQUnit = 67108864.0f;  // 1.5 * 2^18: sums with it are rounded to 1/32
-    float r, s;
+  // 32 t rounded, of a sum s of t with 1.5 * 2^18, which is rounded to 1/32; from some octaves below the histogram's on, something as low.
+  static constexpr float kRound = 393216.0f;
+  __device__ __forceinline__ static int place_in(float s) { return __float_as_int(s) - 0x48C00000; }
+  // 2^t = 2^(place / 32) (1 + q 2^-26), of s = base(x) + kRound.
+  __device__ __forceinline__ int fine(float x, float s) const {
+    constexpr float kQUnit = 67108864.0f;
+    float r;
     if (plain) {
       const float k = kRound - a;
-      s = fmaf(x, c, k);
-      place = __float_as_int(s) - 0x48C00000;
       r = fmaf(x, c, k - s) + fmaf(x, c_low, -a_low);
     } else {
       const Pair t = both(x);
-      s = t.hi + kRound;
-      place = __float_as_int(s) - 0x48C00000;
       r = (t.hi - (s - kRound)) + t.lo;
     }
     constexpr float a2 = 0.24022651f, a3 = 0.055504109f, a4 = 0.0096181291f;  // (ln 2)^k / k!
@@ -248,22 +249,23 @@ struct Weights {
   // The value of a place and its q.
   __device__ __forceinline__ uint32_t value(int place, int q) const {
     const uint32_t base = powers[place & 31];
-    const uint32_t v = base + (uint32_t)(((int64_t)base * q) >> 26), down = (uint32_t)max(-16 - (place >> 5), 0);
+    const uint32_t v = base + (uint32_t)__mulhi((int)base, q * 64), down = (uint32_t)max(-16 - (place >> 5), 0);
     return (v + ((1u << down) >> 1)) >> down;
   }
   __device__ __forceinline__ static int shift(int place) { return max(0, 16 + (place >> 5)); }
   // Octaves below the histogram's; 0 for -inf.
-  __device__ __forceinline__ uint32_t small(float t) const {
+  __device__ __forceinline__ uint32_t small(float base) const {
     float w;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(w) : "f"(t + (float)kOne));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(w) : "f"(base + to_small));
     return __float_as_uint(w + 8388608.0f) - 0x4B000000u;  // rounded
   }
+  // Below the octaves of the histogram a weight is small.
+  static constexpr int kLeastPlace = -32 * kOctaves;
   __device__ __forceinline__ uint64_t operator()(float x) const {
-    const float t = coarse(x);
-    if (t < -(float)kOctaves) return small(t);
-    int place;
-    const int q = fine(x, place);
-    return (uint64_t)value(place, q) << shift(place);
+    const float t = base(x), s = t + kRound;
+    const int place = place_in(s);
+    if (place < kLeastPlace) return small(t);
+    return (uint64_t)value(place, fine(x, s)) << shift(place);
   }
   // Four at once, for a whole warp: the chains of fine() side by side, or none of them where all weights are small.  use(j, is fine, place, q)
   // for each, or with its weight in q's place where that is small.
@@ -271,18 +273,22 @@ struct Weights {
   __device__ __forceinline__ void four(const float (&x)[4], Use use) const {
     float t[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) t[j] = coarse(x[j]);
-    if (!__any_sync(kFull, fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) >= -(float)kOctaves)) {
+    for (int j = 0; j < 4; ++j) t[j] = base(x[j]);
+    if (!__any_sync(kFull, place_in(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) + kRound) >= kLeastPlace)) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) use(j, false, 0, (int)small(t[j]));
       return;
     }
-    int place[4], q[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) q[j] = fine(x[j], place[j]);  // (of a small one it is not used)
+    int q[4], place[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const bool is_small = t[j] < -(float)kOctaves;
+      const float s = t[j] + kRound;
+      q[j] = fine(x[j], s);  // (of a small one it is not used)
+      place[j] = place_in(s);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const bool is_small = place[j] < kLeastPlace;
       use(j, !is_small, place[j], is_small ? (int)small(t[j]) : q[j]);
     }
   }
@@ -386,7 +392,21 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     return warp_sum(e[0] + e[1] + e[2] + e[3]);
   };
 
-  // The same of two numbers.  Both sets of slots at once: the cluster comes together before and after it.
+  // The sum over the cluster, and what is of the CTAs before this one and of this.
+  auto all_of_ctas = [&](uint64_t mine, uint64_t& prev, uint64_t& own) {
+    uint64_t e[4], b = 0, o = 0;
+    tell(warp_sum(mine), e);
+#pragma unroll
+    for (uint32_t i = 0; i < 4u; ++i) {
+      const uint32_t of = (lane * 4u + i) / kWarps;
+      b += of < rank ? e[i] : 0ull;
+      o += of == rank ? e[i] : 0ull;
+    }
+    prev = warp_sum(b);
+    own = warp_sum(o);
+    return warp_sum(e[0] + e[1] + e[2] + e[3]);
+  };
+  // The sums over the cluster of two numbers, and what is of the warps before this one.  Both sets of slots at once: the cluster comes together before and after it.
   auto all_of_two = [&](uint64_t mine, uint64_t other, uint64_t& prev, uint64_t& sum_of_other) {
     const uint64_t a = warp_sum(mine), b = warp_sum(other);
     if (lane < ctas) {
@@ -697,9 +717,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     }
   };
   bool coded = false;  // weights lie where the logits were
-  bool summed = false;  // sum_mine has what is before the bin of the border, hits[] the tokens in it
+  bool summed = false;  // the bins have the sums of what is kept, hits[] the tokens in the border's
   bool whole_bin = false;  // and all of them are kept
-  uint64_t sum_mine = 0;
   uint32_t hits[kBlocks] = {}, border_bin = 0;
   bool searched = !p_on && k == 0u;  // the border is known
 
@@ -723,7 +742,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     if (tid == 0) sh.told[0] = kKBins - 1u;  // fewer maxima than k: nothing is left out
     __syncthreads();
     if (ahead < k && ahead + in_bin >= k) sh.told[0] = tid;
-    cluster_sync();  // every CTA has read the bins: the list may lie over them
+    cluster_sync();
     const uint32_t cut = (uint32_t)sh.told[0];
     // the products of bin_at, compared with the bin's end; where all are alike, or in the last bin, everything is listed
     const float end = cut == kKBins - 1u || scale == 0.f ? INFINITY : (float)(cut + 1u);
@@ -812,7 +831,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
       read4(i0 + 4u * lane, w1, x);
       uint32_t code[4];
       weight.four(x, [&](int j, bool fine, int place, int q) {
-        place = max(place, kTopPlace + 1 - (int)kBins);
         code[j] = code_of(fine, place, q);
         if (fine) {
           const uint32_t v = weight.value(place, q);
@@ -863,32 +881,25 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
       }
       prev += mass[j];
     }
-    cluster_sync();  // (every CTA has read the bins, the list may lie over them)
+    cluster_sync();
     const uint64_t bin = sh.told[0], up_to_bin = sh.told[1];
     if (bin != ~0ull) {
       border_bin = (uint32_t)bin;
       whole_bin = bin >> 32 != 0ull && keep == 0ull;
-      const uint32_t whole = border_bin + (whole_bin ? 1u : 0u);  // places below this are kept
+      if (!whole_bin) {
 #pragma unroll
-      for (uint32_t b = 0; b < kBlocks; ++b) {
-        for (uint32_t s = 0; s < 8u && w0 + b * 1024u + s * 128u < w1; ++s) {
-          float x[4];
-          read4(w0 + b * 1024u + s * 128u + 4u * lane, w1, x);  // (past the end: a place that no bin has)
-          uint32_t code[4];
+        for (uint32_t b = 0; b < kBlocks; ++b) {
+          for (uint32_t s = 0; s < 8u && w0 + b * 1024u + s * 128u < w1; ++s) {
+            float x[4];
+            read4(w0 + b * 1024u + s * 128u + 4u * lane, w1, x);  // (past the end: a place that no bin has)
+            uint32_t mask = 0;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) code[j] = __float_as_uint(x[j]);
-          if (!__any_sync(kFull, min(min(code[0], code[1]), min(code[2], code[3])) >> 22 <= border_bin)) continue;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t place = code[j] >> 22;
-            if (place < whole)
-              sum_mine += weight_of(code[j]);
-            else if (place == border_bin)
-              hits[b] |= 1u << (4u * s + j);
+            for (int j = 0; j < 4; ++j) mask |= __float_as_uint(x[j]) >> 22 == border_bin ? 1u << j : 0u;
+            hits[b] |= mask << (4u * s);
           }
         }
       }
-      summed = keep == 0ull;
+      summed = keep == 0ull && !whole_bin;
     }
     if (whole_bin) {
       searched = true;
@@ -927,19 +938,20 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   const uint32_t keep_at = index_of(keep);  // and of its equals the first ones
   // coded: places above this (weights below) are not kept; of the tokens of edge_place it goes by the logit, where their q is next to the border's:
   // q rises with x but for its roundings, together less than 2 units.
-  int keep_place = 1, edge_place = -1, edge_q = 0, edge_near = 2;
+  int keep_place = 1, edge_place = -1, edge_q = 0, edge_near = 0;
   if (coded && whole_bin) {
     keep_place = (int)border_bin;
   } else if (coded) {
-    const float t = weight.coarse(keep_x);
-    keep_place = keep_x == -INFINITY || !(keep_x == keep_x) || t < -(float)kOctaves ? (int)kSmallPlace : 0;
-    if (keep_place == 0) {
-      int place;
-      edge_q = weight.fine(keep_x, place);
-      keep_place = min(kTopPlace - place, (int)kBins - 1);
+    const float s = weight.base(keep_x) + Weights::kRound;
+    const int place = Weights::place_in(s);
+    keep_place = (int)kSmallPlace;
+    edge_near = 1 << 24;  // small ones: always by the logit
+    if (keep_x > -INFINITY && place >= Weights::kLeastPlace) {
+      keep_place = kTopPlace - place;
+      edge_q = weight.fine(keep_x, s);
+      edge_near = 2;
     }
     edge_place = keep_place;
-    if (keep_place >= (int)kBins - 1) edge_near = 1 << 24;  // of several places: always by the logit
   }
   auto in_edge = [&](uint32_t i, uint32_t code) {
     const int d = ((int)(code << 10) >> 10) - edge_q;
@@ -982,27 +994,41 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     weight.four(x, [&](int j, bool fine, int place, int q) { w[j] = fine ? (uint64_t)weight.value(place, q) << Weights::shift(place) : (uint64_t)(uint32_t)q; });
     return true;
   };
-  uint64_t sum;
-  if (summed) {
-    if (!whole_bin) {
-#pragma unroll
-      for (uint32_t b = 0; b < kBlocks; ++b) {
-        for (uint32_t left = hits[b]; left != 0u; left &= left - 1u) {
-          const uint32_t i = place_of(b, __ffs(left) - 1u), code = __float_as_uint(xs[i]);
-          if (in_edge(i, code)) sum_mine += weight_of(code);
-        }
-      }
-      __syncwarp();
-    }
-  } else {
-    sum_mine = 0;
+  uint64_t sum_mine = 0, sum, total, target;
+  auto add_kept = [&] {
     for (uint32_t i0 = w0; i0 < w1; i0 += 128u) {
       uint64_t w[4];
       kept(i0 + 4u * lane, w1, w);
       sum_mine += (w[0] + w[1]) + (w[2] + w[3]);
     }
+  };
+  uint64_t of_warp;
+  if (summed) {  // the CTAs' sums are in their bins: only the one that has the token adds up its tokens
+    for (uint32_t b = tid; b < border_bin; b += kThreads) sum_mine += (((uint64_t)sh.bins.hi[b] << 15) + sh.bins.lo[b]) << Weights::shift(kTopPlace - (int)b);
+#pragma unroll
+    for (uint32_t b = 0; b < kBlocks; ++b) {
+      for (uint32_t left = hits[b]; left != 0u; left &= left - 1u) {
+        const uint32_t i = place_of(b, __ffs(left) - 1u), code = __float_as_uint(xs[i]);
+        if (in_edge(i, code)) sum_mine += weight_of(code);
+      }
+    }
+    __syncwarp();
+    uint64_t ahead, own;
+    total = all_of_ctas(sum_mine, ahead, own);
+    target = target_of(total);
+    if (target < ahead || target - ahead >= own) return;
+    sum_mine = 0;
+    add_kept();
+    of_warp = warp_sum(sum_mine);
+    if (lane == 0) sh.warps[warp] = of_warp;
+    __syncthreads();
+    sum = ahead + warp_sum(lane < warp ? sh.warps[lane] : 0ull);
+  } else {
+    add_kept();
+    of_warp = warp_sum(sum_mine);
+    total = all(sum_mine, sum);
+    target = target_of(total);
   }
-  const uint64_t of_warp = warp_sum(sum_mine), total = all(sum_mine, sum), target = target_of(total);
   if (lane == 0 && target >= sum && target < sum + of_warp) {
     sh.found[0] = warp;
     sh.found[1] = sum;
