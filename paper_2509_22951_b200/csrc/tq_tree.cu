@@ -6,22 +6,35 @@
 // and 4 D bytes a state and key-value head.  For R up to about 200 the bytes bound it, above that the tensor cores and the exponentials; so
 // everything is built to keep the loads going while tiles of 128 rows x 128 states go through the 5th-generation tensor cores.
 //
-// Work.  The units are (sequence, key-value head, tile of 128 rows, tile of 128 states); of a chain, only the tiles that a tile's last row sees.  Each
+// Work.  The units are (sequence, key-value head, tile of rows, tile of 128 states); of a chain, only the tiles that a tile's last row sees.  Each
 // CTA takes an equal share of consecutive units, whatever the lengths are (they are known on the device only).  A group (sequence, key-value
 // head, tile of rows) that lies in several shares leaves its parts in the workspace, and a second kernel joins them in the order of the
-// CTAs: the result does not depend on timing.
+// CTAs: the result does not depend on timing.  (Joined by the last CTA of a group instead, without a second kernel: 31 tokens over 131071 states
+// 148 us instead of 104, 8 ragged sequences 39.1 instead of 34.6; one SM reads the parts more slowly than all of them.)
 //
 // CTA, one to an SM, 16 warps:
-//   8-11   copy K and V, row by row with cp.async (pages may have any size and a slot any place), into a ring of tiles in the layout that the
-//          tensor core reads (128-byte swizzle); each has its 32 states of a tile and says which of them are there.
-//   13-15  copy the queries of the next group (two buffers).
-//   12     issues the products: scores of tile t (128 x 128, into one of two buffers of tensor memory), then, while their softmax is
-//          taken, the product of tile t - 1 with V.
-//   0-3, 4-7  softmax, a thread a row: the first four take the states 0-63 of a tile, the others 64-127, each with a running maximum and sum
-//          and an output in tensor memory of its own, so that neither waits for the other but at a group's end, where the two become one.
-//          p goes back to tensor memory as bf16 over its scores, where it is the A operand of the product with V.
+//   8-11   bring K and V, two warps each, a ring of tiles for each: tensor copies of boxes of a page's slots, the largest power of two that divides
+//          pages and tiles, in the layout that the tensor core reads (128-byte swizzle).  Pages that no box of 8 slots fits, or that a tensor
+//          map cannot describe, are copied row by row with cp.async, by the four warps in teams, a tile to a team.
+//   13-15  copy the queries of the next group.
+//   12     issues the products, of scores and with V, whichever has its operands.
+//   0-7    softmax, a thread a row, in fp32; p goes back to tensor memory as bf16 over its scores, where it is the A operand of the product
+//          with V.  The two forms of the kernel differ in what the two sets of four warps take:
+//     128 rows a tile: the first four take the states 0-63 of a tile, the others 64-127, each with a running maximum and sum and an output in
+//          tensor memory of its own, so that neither waits for the other but at a group's end, where the two become one.  Scores have two buffers.
+//     256 rows a tile: the first four take the rows 0-127, the others 128-255.  K and V are read once for twice the rows, and one half's products
+//          run during the other's softmax; the product with V begins when the first 64 states have their p.
+//   256 rows are taken where the sequences have more than 128 on average.  us, 256 rows | 128 rows, 32 heads on 8 of 128: 4096 tokens of a prompt
+//   194 | 246, 40 tokens over 131071 states 139 | 173, 64 sequences of up to 64 tokens and 4096 states 180 | 204; where it does not matter:
+//   512 tokens 28.0 | 27.5, 33 tokens over 1000 states 18.2 | 16.9.
+//   Of 256 rows x 128 states some 3200 cycles are left beside the 2048 of the tensor core at its full rate: a half's softmax takes 2100 (exponentials
+//   1450, 1024 at the special function unit's rate; maxima 450), its next scores come some 1300 after its p.
 // The output is rescaled only when a row's maximum has grown by more than 2^8 since the last rescaling (online softmax with the rescaling
 // delayed up to a threshold, as in the kernel of cross attention): p stays below 2^8, which costs no precision in bf16 or the fp32 sum.
+//
+// Measured (one B200, 6545 GB/s copied, us): 197 states x 8 tokens, 32 heads of 64 10; 8 sequences of up to 16 tokens and 8191 states, 24 heads 35 (its
+// bytes: 19); 31 tokens over 131071 states, 32 heads 104 (82); 64 chains of 5 tokens over up to 16384 states, 64 heads 390 (386); pieces of 1024
+// tokens of two prompts up to 9001 long, 32 heads 184 (operations at the rate of a library product: 106).
 //
 // States that are not there (past the end, on a page outside the pool) are zeros in shared memory and hidden from all rows.  A state that only
 // some rows see enters the others' sums with p = 0; if its value is Inf or NaN that product is NaN, so a row whose sum of p is finite but whose
@@ -44,7 +57,7 @@ using namespace tq_ops;
 using namespace tq_sm100;
 using namespace tq_attn;
 
-constexpr uint32_t kRows = 128;    // rows of a tile: the lanes of tensor memory
+constexpr uint32_t kRows = 128;    // rows of a product: the lanes of tensor memory
 constexpr uint32_t kStates = 128;  // states of a tile
 constexpr uint32_t kSide = 64;     // states of a tile that one half of the softmax warps takes
 constexpr int kSoftWarps = 8, kLoadWarp = 8, kLoadWarps = 4, kMmaWarp = 12, kQueryWarp = 13, kQueryWarps = 3;
@@ -54,6 +67,7 @@ constexpr int kTreeThreads = 512;
 constexpr int kSoftRegs = 192, kOtherRegs = 64;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kThere = 16;    // tiles whose words of present states are kept: more than loads run ahead of the softmax
+constexpr uint32_t kWideRows = 129;  // rows of a sequence, on average, from which on tiles have 256
 constexpr float kRescale = 8.0f;   // log2 of how far p may exceed 1
 
 struct TreeParams {
@@ -70,13 +84,14 @@ struct TreeParams {
   const uint32_t* mask;
   uint32_t mask_words, max_pages, page_size, n_pages;
   uint32_t n_tokens, n_seqs, n_q_heads, n_kv_heads, group;
+  uint32_t row_bits;  // log2 of a tile's rows: 7 or 8
   float scale_log2;
   uint32_t box, boxes;  // slots of a page that one tensor copy brings, copies to a tile of 128 states
   uint32_t* status;
   tq_attn_ws ws;
 };
 
-template <int D>
+template <int D, bool WIDE>
 struct TreeSmem {
   static constexpr uint32_t kSlabs = D / 64;                       // 64 columns = 128 bytes of a swizzled row
   static constexpr uint32_t kTileBytes = kSlabs * kStates * 128;   // queries, keys or values of a tile
@@ -88,19 +103,20 @@ struct TreeSmem {
   // The loading warps of the other path work in teams, a tile to a team in turn: a team waits for its copies and announces them, the others' are
   // under way.
   static constexpr uint32_t kTeams = D == 128 ? 2 : 4;
-  static constexpr uint32_t kOffK = kQueries * kTileBytes, kOffV = kOffK + kKeys * kTileBytes;
+  static constexpr uint32_t kQueryBytes = (WIDE ? 2 : 1) * kTileBytes;
+  static constexpr uint32_t kOffK = kQueries * kQueryBytes, kOffV = kOffK + kKeys * kTileBytes;
   static constexpr uint32_t kOffMisc = kOffV + kValues * kTileBytes;
   // misc: [0] dead flag, [4] tensor-memory base, barriers from 16 on
   static constexpr uint32_t kBarKFull = 16, kBarKEmpty = kBarKFull + 8 * kKeys, kBarVFull = kBarKEmpty + 8 * kKeys, kBarVEmpty = kBarVFull + 8 * kValues;
   static constexpr uint32_t kBarQFull = kBarVEmpty + 8 * kValues, kBarQEmpty = kBarQFull + 8 * kQueries;
-  static constexpr uint32_t kBarSFull = kBarQEmpty + 8 * kQueries, kBarPFull = kBarSFull + 16, kBarODone = kBarPFull + 16, kBarMl = kBarODone + 16;
+  static constexpr uint32_t kBarSFull = kBarQEmpty + 8 * kQueries, kBarPFull = kBarSFull + 16, kBarODone = kBarPFull + 32, kBarMl = kBarODone + 16;
   static constexpr uint32_t kOffPlan = (kBarMl + 8 + 15) / 16 * 16;
   static constexpr uint32_t kOffThere = kOffPlan + 96;
   static constexpr uint32_t kOffMl = kOffThere + kThere * 16;
   static constexpr uint32_t kTotal = kOffMisc + kOffMl + 2 * kRows * 8;
   static_assert(kTotal <= 232448, "shared memory of one CTA");
 };
-// a part of a cut group: [D / 4][128] float4 of output, then the rows' maxima and sums
+// a part of a cut group: [D / 4][128] float4 of output, then the rows' maxima and sums; two of them in a row where tiles have 256 rows
 constexpr uint64_t kTreePartFloats = kRows * (128 + 2);
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t bytes) {
@@ -116,6 +132,7 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
 __device__ __forceinline__ void copies_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 // Units that a group counts beside its tiles of states: what its end and the next one's beginning cost the softmax warps.
+// (us, 1 | 3 | 5 units: pieces of prompts 193 | 185 | 185, 64 sequences of up to 20 tokens and 4000 states 185 | 155 | 153, 8 chains of 333 tokens 84 | 76 | 77)
 constexpr uint32_t kGroupUnits = 3;
 
 // A group of the list of work: tile rt of the rows of sequence b over key-value head kvh.
@@ -135,12 +152,12 @@ struct Walk {
     const uint64_t cap = min((uint64_t)p.max_pages * p.page_size, (uint64_t)0x7FFFFFFF);
     len = given <= 0 ? 0u : (uint32_t)min((uint64_t)given, cap);
     before = (int64_t)given - n;
-    row_tiles = (uint32_t)(((uint64_t)n * p.group + kRows - 1u) / kRows);
+    row_tiles = (uint32_t)(((uint64_t)n * p.group + (1u << p.row_bits) - 1u) >> p.row_bits);
   }
   __device__ __forceinline__ void tile(const TreeParams& p) {
     end = len;
     if (p.mask == nullptr) {
-      const uint32_t last = (uint32_t)min((uint64_t)n - 1u, (((uint64_t)rt + 1u) * kRows - 1u) / p.group);
+      const uint32_t last = (uint32_t)min((uint64_t)n - 1u, ((((uint64_t)rt + 1u) << p.row_bits) - 1u) / p.group);
       end = (uint32_t)max((int64_t)0, min((int64_t)len, before + last + 1));
     }
     tiles = max(1u, (end + kStates - 1u) / kStates);
@@ -251,10 +268,10 @@ __device__ __forceinline__ Plan make_plan(const TreeParams& p, uint32_t lane) {
 }
 
 // TMA: K and V come by tensor copies of p.box slots of a page, else by cp.async, row by row.
-template <int D, bool TMA>
+template <int D, bool TMA, bool WIDE>
 __global__ void __launch_bounds__(kTreeThreads, 1)
     tree_attention_kernel(const TreeParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
-  using L = TreeSmem<D>;
+  using L = TreeSmem<D, WIDE>;
   extern __shared__ __align__(1024) uint8_t smem[];  // swizzled tiles start on 1024 bytes
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const uint32_t smem0 = smem_u32(smem), misc = smem0 + L::kOffMisc;
@@ -287,7 +304,8 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
     }
     for (uint32_t i = 0; i < 2; ++i) {
       mbar_init(bar(L::kBarSFull, i), 2);  // the products' completion, and the issuing thread, which has seen the words of present states
-      mbar_init(bar(L::kBarPFull, i), kSoftWarps);
+      mbar_init(bar(L::kBarPFull, i), WIDE ? kSoftWarps / 2 : kSoftWarps);
+      if (WIDE) mbar_init(bar(L::kBarPFull, i + 2u), kSoftWarps / 2);
       mbar_init(bar(L::kBarODone, i), 1);
     }
     mbar_init(bar(L::kBarMl, 0), kSoftWarps);
@@ -497,13 +515,13 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
       const uint32_t qb = count % L::kQueries;
       if (count >= L::kQueries) wait(bar(L::kBarQEmpty, qb), (count / L::kQueries - 1u) & 1u);
       if (!ok) break;
-      const uint32_t rows = (uint32_t)min((uint64_t)kRows, (uint64_t)g.n * p.group - (uint64_t)g.rt * kRows);
-      const uint32_t dst = smem0 + qb * L::kTileBytes + (c / 8u) * (kRows * 128u);
+      const uint32_t first = g.rt << p.row_bits, rows = (uint32_t)min((uint64_t)1 << p.row_bits, (uint64_t)g.n * p.group - first);
+      const uint32_t dst = smem0 + qb * L::kQueryBytes + (c / 8u) * (kRows * 128u);
       const __nv_bfloat16* const q = p.q + (int64_t)g.lo * p.q_stride + (size_t)g.kvh * p.group * D + c * 8u;
       // rows that are not there are zeros: products with them draw less power (64 chains of 40 rows: 1500 MHz under the power limit without that)
-      for (uint32_t r = (warp - kQueryWarp) * kAtOnce + lane / kChunks; r < kRows; r += kQueryWarps * kAtOnce) {
-        const uint32_t row = g.rt * kRows + min(r, rows - 1u), tok = row / p.group;
-        cp_async16(dst + r * 128u + (((c % 8u) ^ (r & 7u)) << 4), q + (int64_t)tok * p.q_stride + (row - tok * p.group) * D, r < rows ? 16u : 0u);
+      for (uint32_t r = (warp - kQueryWarp) * kAtOnce + lane / kChunks; r < (WIDE ? 2u : 1u) * kRows; r += kQueryWarps * kAtOnce) {
+        const uint32_t row = first + min(r, rows - 1u), tok = row / p.group;
+        cp_async16(dst + (r / kRows) * L::kTileBytes + (r % kRows) * 128u + (((c % 8u) ^ (r & 7u)) << 4), q + (int64_t)tok * p.q_stride + (row - tok * p.group) * D, r < rows ? 16u : 0u);
       }
       asm volatile("cp.async.wait_all;" ::: "memory");
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -516,6 +534,16 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
     if (warp == kQueryWarp && lane == 0) p.ws.open[blockIdx.x] = open;  // for the joining kernel
   } else if (warp == kMmaWarp) {
     // ---- products ---------------------------------------------------------------------------------------
+    // past the last state memory may hold anything, and 0 x NaN is NaN
+    auto zero_behind = [&](uint32_t st, uint32_t valid) {
+      if (valid == kStates) return;
+      constexpr uint32_t kChunks = D / 8, kStep = 32 / kChunks;  // of 16 bytes of a row; rows at once
+      const uint32_t c = lane % kChunks;
+      uint8_t* const tile = smem + L::kOffV + st * L::kTileBytes + (c / 8u) * (kStates * 128u) + (c % 8u) * 16u;
+#pragma unroll 4
+      for (uint32_t r = valid + lane / kChunks; r < kStates; r += kStep) *reinterpret_cast<uint4*>(tile + r * 128u) = make_uint4(0, 0, 0, 0);
+      copies_fence();
+    };
     // Scores of the next tile or the product of an earlier one with V, whichever is ready: up to two tiles' scores may wait for their p.
     uint32_t done = 0, asked = 0, q_count = 0;  // tiles multiplied with V, tiles with scores, groups
     uint32_t k_st = 0, k_round = 0, v_st = 0, v_round = 0;
@@ -524,76 +552,85 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
     const uint64_t q_desc = umma_desc(smem0), k_desc = umma_desc(smem0 + L::kOffK), v_desc = umma_desc_n_major(smem0 + L::kOffV, kStates);
     bool any = more(g);
     uint32_t t = any ? begin_of(g) : 0u, t0 = t, t1 = any ? end_of(g) : 0u;
-    uint32_t idle = 0;
-    while (ok && (any || done != asked)) {
-      const uint32_t sb = done & 1u;
-      // the tile's p times V, both halves of its states
-      if (done != asked && mbar_test(bar(L::kBarPFull, sb), (done >> 1) & 1u) && mbar_test(bar(L::kBarVFull, v_st), v_round & 1u)) {
-        idle = 0;
-        if (TMA) {
-          const uint32_t valid = flags[sb] >> 8;
-          if (valid < kStates) {  // past the last state memory may hold anything, and 0 x NaN is NaN
-            constexpr uint32_t kChunks = D / 8;
-            uint8_t* const tile = smem + L::kOffV + v_st * L::kTileBytes;
-            for (uint32_t i = lane; i < (kStates - valid) * kChunks; i += 32u) {
-              const uint32_t r = valid + i / kChunks, c = i % kChunks;
-              *reinterpret_cast<uint4*>(tile + (c / 8u) * (kStates * 128u) + r * 128u + (c % 8u) * 16u) = make_uint4(0, 0, 0, 0);
+    if constexpr (WIDE) {
+      // Two products a tile, in turn: while one half's softmax is taken the other's scores and its product with V are formed.
+      bool pending = false;  // a tile with scores waits for its p
+      uint32_t states = 0, adds = 0;  // of it: states that are there, whether it is not the group's first
+      auto product = [&](uint32_t r) {
+        if (r == 0u) {
+          wait(bar(L::kBarVFull, v_st), v_round & 1u);
+          if (!ok) return;
+          if (TMA)
+            zero_behind(v_st, states);
+          else
+            copies_fence();
+        }
+#pragma unroll 1
+        for (uint32_t h = 0; h < 2u; ++h) {  // the first half of the states while p of the second is being taken
+          wait(bar(L::kBarPFull, 2u * r + h), done & 1u);
+          if (!ok) return;
+          tmem_fence_after();
+          __syncwarp();
+          if (elect_one()) {
+            const uint64_t b = v_desc + v_st * (L::kTileBytes >> 4) + h * (4u * 2048u >> 4);
+#pragma unroll
+            for (uint32_t kk = 0; kk < kStates / 32u; ++kk)
+              umma_bf16_ts(tmem + 2u * kStates + r * D, tmem + r * kStates + (4u * h + kk) * 8u, b + kk * (2048u >> 4), idesc_pv, adds | h | kk);
+            if (h == 1u) {
+              umma_commit(bar(L::kBarODone, r));
+              if (r == 1u) umma_commit(bar(L::kBarVEmpty, v_st));
             }
           }
+          __syncwarp();
         }
-        copies_fence();
-        tmem_fence_after();
-        __syncwarp();
-        if (elect_one()) {
-          const uint64_t b = v_desc + v_st * (L::kTileBytes >> 4);
-#pragma unroll
-          for (uint32_t kk = 0; kk < kStates / 16u; ++kk) {
-            const uint32_t w = kk / 4u;
-            umma_bf16_ts(tmem + 2u * kStates + w * D, tmem + sb * kStates + w * kSide + (kk % 4u) * 8u, b + kk * (2048u >> 4), idesc_pv,
-                         (flags[sb] & 1u) | (kk % 4u));
-          }
-          umma_commit(bar(L::kBarODone, sb));
-          umma_commit(bar(L::kBarVEmpty, v_st));
-        }
-        __syncwarp();
+        if (r == 0u) return;
         ++done;
         if (++v_st == L::kValues) {
           v_st = 0;
           ++v_round;
         }
-        continue;
-      }
-      // the next tile's scores, when the buffer's last p is spent
-      if (any && asked - done < 2u && mbar_test(bar(L::kBarKFull, k_st), k_round & 1u) &&
-          (t != t0 || mbar_test(bar(L::kBarQFull, q_count % L::kQueries), (q_count / L::kQueries) & 1u))) {
-        idle = 0;
-        const uint32_t qb = q_count % L::kQueries, to = asked & 1u;
-        copies_fence();
+      };
+      auto scores = [&](uint32_t r) {
+        const uint32_t qb = q_count % L::kQueries;
+        if (r == 0u) {
+          wait(bar(L::kBarKFull, k_st), k_round & 1u);
+          if (t == t0 && ok) wait(bar(L::kBarQFull, qb), (q_count / L::kQueries) & 1u);
+        }
+        if (!ok) return;
+        if (!TMA || t == t0) copies_fence();
         tmem_fence_after();
         if (elect_one()) {
-          const uint64_t a = q_desc + qb * (L::kTileBytes >> 4), b = k_desc + k_st * (L::kTileBytes >> 4);
+          const uint64_t a = q_desc + (qb * L::kQueryBytes + r * L::kTileBytes >> 4), b = k_desc + k_st * (L::kTileBytes >> 4);
 #pragma unroll
           for (uint32_t kk = 0; kk < D / 16; ++kk) {
             constexpr uint32_t kSlab = (kStates * 128u) >> 4;
             const uint32_t off = (kk / 4u) * kSlab + (kk % 4u) * 2u;  // in 16 bytes
-            umma_bf16(tmem + to * kStates, a + off, b + off, idesc_qk, kk != 0u);
+            umma_bf16(tmem + r * kStates, a + off, b + off, idesc_qk, kk != 0u);
           }
-          umma_commit(bar(L::kBarSFull, to));
-          umma_commit(bar(L::kBarKEmpty, k_st));
-          if (t + 1u == t1) umma_commit(bar(L::kBarQEmpty, qb));
-          mbar_arrive(bar(L::kBarSFull, to));
+          umma_commit(bar(L::kBarSFull, r));
+          if (r == 1u) umma_commit(bar(L::kBarKEmpty, k_st));
+          if (r == 1u && t + 1u == t1) umma_commit(bar(L::kBarQEmpty, qb));
+          mbar_arrive(bar(L::kBarSFull, r));
         }
         __syncwarp();
+      };
+      while (ok && (any || pending)) {
+        const bool same = any && t != t0;  // the next tile is of the pending one's group: its queries are there
+#pragma unroll 1
+        for (uint32_t r = 0; r < 2u && ok; ++r) {
+          if (pending) product(r);
+          if (same && ok) scores(r);
+        }
+#pragma unroll 1
+        for (uint32_t r = 0; r < 2u && ok && any && !same; ++r) scores(r);
+        pending = any;
+        if (!any) break;
+        states = g.end > t * kStates ? min(kStates, g.end - t * kStates) : 0u;
+        adds = same ? 1u : 0u;
         if (++k_st == L::kKeys) {
           k_st = 0;
           ++k_round;
         }
-        const uint32_t f = (t != t0 ? 1u : 0u) | (g.end > t * kStates ? min(kStates, g.end - t * kStates) << 8 : 0u);
-        if (to)
-          flags[1] = f;
-        else
-          flags[0] = f;
-        ++asked;
         if (++t == t1) {
           g.next(p);
           ++q_count;
@@ -603,10 +640,84 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
             t1 = end_of(g);
           }
         }
-        continue;
       }
-      if (++idle == kSpinLimit || ((idle & 1023u) == 1023u && *dead)) ok = false;
-      ok = __all_sync(kFull, ok);
+    } else {
+      uint32_t idle = 0;
+      while (ok && (any || done != asked)) {
+        const uint32_t sb = done & 1u;
+        // the tile's p times V, both halves of its states
+        if (done != asked && mbar_test(bar(L::kBarPFull, sb), (done >> 1) & 1u) && mbar_test(bar(L::kBarVFull, v_st), v_round & 1u)) {
+          idle = 0;
+          if (TMA) {
+            zero_behind(v_st, flags[sb] >> 8);
+          }
+          copies_fence();
+          tmem_fence_after();
+          __syncwarp();
+          if (elect_one()) {
+            const uint64_t b = v_desc + v_st * (L::kTileBytes >> 4);
+#pragma unroll
+            for (uint32_t kk = 0; kk < kStates / 16u; ++kk) {
+              const uint32_t w = kk / 4u;
+              umma_bf16_ts(tmem + 2u * kStates + w * D, tmem + sb * kStates + w * kSide + (kk % 4u) * 8u, b + kk * (2048u >> 4), idesc_pv,
+                           (flags[sb] & 1u) | (kk % 4u));
+            }
+            umma_commit(bar(L::kBarODone, sb));
+            umma_commit(bar(L::kBarVEmpty, v_st));
+          }
+          __syncwarp();
+          ++done;
+          if (++v_st == L::kValues) {
+            v_st = 0;
+            ++v_round;
+          }
+          continue;
+        }
+        // the next tile's scores, when the buffer's last p is spent
+        if (any && asked - done < 2u && mbar_test(bar(L::kBarKFull, k_st), k_round & 1u) &&
+            (t != t0 || mbar_test(bar(L::kBarQFull, q_count % L::kQueries), (q_count / L::kQueries) & 1u))) {
+          idle = 0;
+          const uint32_t qb = q_count % L::kQueries, to = asked & 1u;
+          copies_fence();
+          tmem_fence_after();
+          if (elect_one()) {
+            const uint64_t a = q_desc + qb * (L::kTileBytes >> 4), b = k_desc + k_st * (L::kTileBytes >> 4);
+#pragma unroll
+            for (uint32_t kk = 0; kk < D / 16; ++kk) {
+              constexpr uint32_t kSlab = (kStates * 128u) >> 4;
+              const uint32_t off = (kk / 4u) * kSlab + (kk % 4u) * 2u;  // in 16 bytes
+              umma_bf16(tmem + to * kStates, a + off, b + off, idesc_qk, kk != 0u);
+            }
+            umma_commit(bar(L::kBarSFull, to));
+            umma_commit(bar(L::kBarKEmpty, k_st));
+            if (t + 1u == t1) umma_commit(bar(L::kBarQEmpty, qb));
+            mbar_arrive(bar(L::kBarSFull, to));
+          }
+          __syncwarp();
+          if (++k_st == L::kKeys) {
+            k_st = 0;
+            ++k_round;
+          }
+          const uint32_t f = (t != t0 ? 1u : 0u) | (g.end > t * kStates ? min(kStates, g.end - t * kStates) << 8 : 0u);
+          if (to)
+            flags[1] = f;
+          else
+            flags[0] = f;
+          ++asked;
+          if (++t == t1) {
+            g.next(p);
+            ++q_count;
+            any = more(g);
+            if (any) {
+              t = t0 = begin_of(g);
+              t1 = end_of(g);
+            }
+          }
+          continue;
+        }
+        if (++idle == kSpinLimit || ((idle & 1023u) == 1023u && *dead)) ok = false;
+        ok = __all_sync(kFull, ok);
+      }
     }
   }
   } else {
@@ -615,12 +726,13 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
     const uint32_t w = warp >> 2, row_in = threadIdx.x & 127u;
     const uint32_t lane_field = (warp & 3u) << 21;  // 32 lanes of tensor memory to a warp
     const uint32_t o_addr = tmem + lane_field + 2u * kStates;
+    constexpr uint32_t kParts = WIDE ? 1 : 2;  // threads of a row at the group's end, each with its part of the columns
     const float c = p.scale_log2;
     uint32_t count = 0, groups = 0;
     for (; more(g) && ok; g.next(p), ++groups) {
       const uint32_t t0 = begin_of(g), t1 = end_of(g);
       const uint64_t rows = (uint64_t)g.n * p.group;
-      const uint64_t row = (uint64_t)g.rt * kRows + row_in;
+      const uint64_t row = ((uint64_t)g.rt << p.row_bits) + (WIDE ? threadIdx.x : row_in);
       const bool live = row < rows, warp_live = row - lane < rows;
       const uint32_t tok = live ? (uint32_t)row / p.group : 0u, head = g.kvh * p.group + ((uint32_t)row - tok * p.group);
       const uint32_t* const bits_row = p.mask ? p.mask + (size_t)(g.lo + (int32_t)tok) * p.mask_words : nullptr;
@@ -640,102 +752,191 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         const uint64_t v = ((uint64_t)__funnelshift_r(b, e, off) << 32) | __funnelshift_r(a, b, off);
         return j0 >= 0 ? v : (v << -j0) | ((1ull << -j0) - 1ull);
       };
-      for (uint32_t t = t0; t < t1; ++t, ++count) {
-        const uint32_t sb = count & 1u, s_addr = tmem + lane_field + sb * kStates + w * kSide;
-        const uint64_t order = warp_live ? visible((int64_t)t * kStates + w * kSide) : 0ull;
-        wait(bar(L::kBarSFull, sb), (count >> 1) & 1u);
-        if (!ok) break;
-        tmem_fence_after();
-        if (warp_live) {
-          const uint2 here = *reinterpret_cast<const uint2*>(s_there + (count % kThere) * 4u + w * 2u);
-          const uint64_t seen = order & (((uint64_t)here.y << 32) | here.x);
-          uint32_t s[kSide];
-          TMEM_LD32(s, s_addr);
-          TMEM_LD32(s + 32, s_addr + 32u);
-          tmem_wait_ld();
-          if (__any_sync(kFull, seen != ~0ull)) {
-            const uint32_t lo = (uint32_t)seen, hi = (uint32_t)(seen >> 32);
+      if constexpr (WIDE) {
+        const uint32_t s_addr = tmem + lane_field + w * kStates;
+        for (uint32_t t = t0; t < t1; ++t, ++count) {
+          const uint64_t order[2] = {warp_live ? visible((int64_t)t * kStates) : 0ull, warp_live ? visible((int64_t)t * kStates + kSide) : 0ull};
+          wait(bar(L::kBarSFull, w), count & 1u);
+          if (!ok) break;
+          tmem_fence_after();
+          if (warp_live) {
+            const uint4 here = *reinterpret_cast<const uint4*>(s_there + (count % kThere) * 4u);
+            const uint32_t seen[4] = {(uint32_t)order[0] & here.x, (uint32_t)(order[0] >> 32) & here.y, (uint32_t)order[1] & here.z, (uint32_t)(order[1] >> 32) & here.w};
+            uint32_t s[kStates];
 #pragma unroll
-            for (int i = 0; i < 64; ++i) s[i] = ((i < 32 ? lo : hi) >> (i % 32)) & 1u ? s[i] : 0xFF800000u;
-          }
-          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            for (int i = 0; i < 4; ++i) TMEM_LD32(s + 32 * i, s_addr + 32u * i);
+            tmem_wait_ld();
+            if (__any_sync(kFull, (seen[0] & seen[1] & seen[2] & seen[3]) != ~0u)) {
 #pragma unroll
-          for (int i = 0; i < 64; i += 8) {
+              for (int i = 0; i < 128; ++i) s[i] = (seen[i / 32] >> (i % 32)) & 1u ? s[i] : 0xFF800000u;
+            }
+            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-            for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], __uint_as_float(s[i + 2 * k]), __uint_as_float(s[i + 2 * k + 1]));
-          }
-          const float top = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]) * c;
-          if (__any_sync(kFull, live && top > m + kRescale)) {  // (what lies in a dead row must not decide for the others)
-            const float mn = fmaxf(m, top), f = mn == -INFINITY ? 1.f : exp2_fast(m - mn);
-            m = mn;
-            l *= f;
-            if (t != t0) {
-              wait(bar(L::kBarODone, sb ^ 1u), ((count - 1u) >> 1) & 1u);  // the products with V up to the tile before
-              if (!ok) break;
-              tmem_fence_after();
+            for (int i = 0; i < 128; i += 8) {
 #pragma unroll
-              for (int i = 0; i < D / 16; ++i) {
-                uint32_t o[16];
-                TMEM_LD16(o, o_addr + w * D + 16u * i);
-                tmem_wait_ld();
+              for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], __uint_as_float(s[i + 2 * k]), __uint_as_float(s[i + 2 * k + 1]));
+            }
+            const float top = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]) * c;
+            if (__any_sync(kFull, live && top > m + kRescale)) {
+              const float mn = fmaxf(m, top), f = mn == -INFINITY ? 1.f : exp2_fast(m - mn);
+              m = mn;
+              l *= f;
+              if (t != t0) {
+                wait(bar(L::kBarODone, w), (count - 1u) & 1u);
+                if (!ok) break;
+                tmem_fence_after();
 #pragma unroll
-                for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-                TMEM_ST16(o_addr + w * D + 16u * i, o);
+                for (int i = 0; i < D / 16; ++i) {
+                  uint32_t o[16];
+                  TMEM_LD16(o, o_addr + w * D + 16u * i);
+                  tmem_wait_ld();
+#pragma unroll
+                  for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                  TMEM_ST16(o_addr + w * D + 16u * i, o);
+                }
               }
             }
-          }
-          const float ref = !live ? INFINITY : m == -INFINITY ? 0.f : m;  // p of a dead row is 0
-          const uint64_t c2 = pair(c, c), ref2 = pair(-ref, -ref);
-          uint64_t sum[2] = {0, 0};
-          uint32_t pk[32];
+            const float ref = !live ? INFINITY : m == -INFINITY ? 0.f : m;
+            const uint64_t c2 = pair(c, c), ref2 = pair(-ref, -ref);
+            uint64_t sum[2] = {0, 0};
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            float a, b;
-            unpair(fma2(pair(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), c2, ref2), a, b);
-            a = exp2_fast(a);
-            b = exp2_fast(b);
-            sum[i & 1] = add2(sum[i & 1], pair(a, b));
-            pk[i] = pack_bf16(a, b);
+            for (int h = 0; h < 4; ++h) {
+              uint32_t pk[16];
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                float a, b;
+                unpair(fma2(pair(__uint_as_float(s[32 * h + 2 * i]), __uint_as_float(s[32 * h + 2 * i + 1])), c2, ref2), a, b);
+                a = exp2_fast(a);
+                b = exp2_fast(b);
+                sum[i & 1] = add2(sum[i & 1], pair(a, b));
+                pk[i] = pack_bf16(a, b);
+              }
+              TMEM_ST16(s_addr + 16u * h, pk);
+              if (h == 1) {
+                tmem_wait_st();
+                tmem_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(L::kBarPFull, 2u * w));
+              }
+            }
+            float l0, l1;
+            unpair(add2(sum[0], sum[1]), l0, l1);
+            l += l0 + l1;
+            tmem_wait_st();
           }
-          TMEM_ST32(s_addr, pk);
-          float l0, l1;
-          unpair(add2(sum[0], sum[1]), l0, l1);
-          l += l0 + l1;
-          tmem_wait_st();
+          tmem_fence_before();
+          __syncwarp();
+          if (lane == 0) {
+            if (!warp_live) mbar_arrive(bar(L::kBarPFull, 2u * w));
+            mbar_arrive(bar(L::kBarPFull, 2u * w + 1u));
+          }
         }
-        tmem_fence_before();
+        if (ok) wait(bar(L::kBarODone, w), (count - 1u) & 1u);
+        if (!ok) break;
+      } else {
+        for (uint32_t t = t0; t < t1; ++t, ++count) {
+          const uint32_t sb = count & 1u, s_addr = tmem + lane_field + sb * kStates + w * kSide;
+          const uint64_t order = warp_live ? visible((int64_t)t * kStates + w * kSide) : 0ull;
+          wait(bar(L::kBarSFull, sb), (count >> 1) & 1u);
+          if (!ok) break;
+          tmem_fence_after();
+          if (warp_live) {
+            const uint2 here = *reinterpret_cast<const uint2*>(s_there + (count % kThere) * 4u + w * 2u);
+            const uint64_t seen = order & (((uint64_t)here.y << 32) | here.x);
+            uint32_t s[kSide];
+            TMEM_LD32(s, s_addr);
+            TMEM_LD32(s + 32, s_addr + 32u);
+            tmem_wait_ld();
+            if (__any_sync(kFull, seen != ~0ull)) {
+              const uint32_t lo = (uint32_t)seen, hi = (uint32_t)(seen >> 32);
+#pragma unroll
+              for (int i = 0; i < 64; ++i) s[i] = ((i < 32 ? lo : hi) >> (i % 32)) & 1u ? s[i] : 0xFF800000u;
+            }
+            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int i = 0; i < 64; i += 8) {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], __uint_as_float(s[i + 2 * k]), __uint_as_float(s[i + 2 * k + 1]));
+            }
+            const float top = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]) * c;
+            if (__any_sync(kFull, live && top > m + kRescale)) {  // (what lies in a dead row must not decide for the others)
+              const float mn = fmaxf(m, top), f = mn == -INFINITY ? 1.f : exp2_fast(m - mn);
+              m = mn;
+              l *= f;
+              if (t != t0) {
+                wait(bar(L::kBarODone, sb ^ 1u), ((count - 1u) >> 1) & 1u);  // the products with V up to the tile before
+                if (!ok) break;
+                tmem_fence_after();
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                  uint32_t o[16];
+                  TMEM_LD16(o, o_addr + w * D + 16u * i);
+                  tmem_wait_ld();
+#pragma unroll
+                  for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                  TMEM_ST16(o_addr + w * D + 16u * i, o);
+                }
+              }
+            }
+            const float ref = !live ? INFINITY : m == -INFINITY ? 0.f : m;  // p of a dead row is 0
+            const uint64_t c2 = pair(c, c), ref2 = pair(-ref, -ref);
+            uint64_t sum[2] = {0, 0};
+            uint32_t pk[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+              float a, b;
+              unpair(fma2(pair(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), c2, ref2), a, b);
+              a = exp2_fast(a);
+              b = exp2_fast(b);
+              sum[i & 1] = add2(sum[i & 1], pair(a, b));
+              pk[i] = pack_bf16(a, b);
+            }
+            TMEM_ST32(s_addr, pk);
+            float l0, l1;
+            unpair(add2(sum[0], sum[1]), l0, l1);
+            l += l0 + l1;
+            tmem_wait_st();
+          }
+          tmem_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(L::kBarPFull, sb));
+        }
+        if (!ok) break;
+        // ---- end of the group, or of this CTA's part of it: the two halves of the states become one ---------------
+        s_ml[w * kRows + row_in] = make_float2(m, l);
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(L::kBarPFull, sb));
+        if (lane == 0) mbar_arrive(bar(L::kBarMl, 0));
+        wait(bar(L::kBarODone, (count - 1u) & 1u), ((count - 1u) >> 1) & 1u);
+        if (ok) wait(bar(L::kBarMl, 0), groups & 1u);
+        if (!ok) break;
       }
-      if (!ok) break;
-      // ---- end of the group, or of this CTA's part of it: the two halves of the states become one ---------------
-      s_ml[w * kRows + row_in] = make_float2(m, l);
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(L::kBarMl, 0));
-      wait(bar(L::kBarODone, (count - 1u) & 1u), ((count - 1u) >> 1) & 1u);
-      if (ok) wait(bar(L::kBarMl, 0), groups & 1u);
-      if (!ok) break;
       if (!warp_live) continue;
       tmem_fence_after();
-      const float2 a = s_ml[row_in], b = s_ml[kRows + row_in];
-      const float M = fmaxf(a.x, b.x), ref = M == -INFINITY ? 0.f : M;
-      const float fa = exp2_fast(a.x - ref), fb = exp2_fast(b.x - ref), sum = a.y * fa + b.y * fb;
+      float M = m, fa = 1.f, fb = 0.f, sum = l;
+      if constexpr (!WIDE) {
+        const float2 a = s_ml[row_in], b = s_ml[kRows + row_in];
+        M = fmaxf(a.x, b.x);
+        const float ref = M == -INFINITY ? 0.f : M;
+        fa = exp2_fast(a.x - ref), fb = exp2_fast(b.x - ref), sum = a.y * fa + b.y * fb;
+      }
+      const float ref = M == -INFINITY ? 0.f : M;
       const bool whole = t0 == 0u && t1 == g.tiles;
-      float* const mine = p.ws.parts + (size_t)(2u * blockIdx.x + (t0 == 0u ? 1u : 0u)) * kTreePartFloats;
+      float* const mine = p.ws.parts + (size_t)((2u * blockIdx.x + (t0 == 0u ? 1u : 0u)) * (WIDE ? 2u : 1u) + (WIDE ? w : 0u)) * kTreePartFloats;
       const size_t at = (size_t)(g.lo + (int32_t)tok) * p.n_q_heads + head;
       const float inv = 1.0f / sum;
       bool nan = false;
-      constexpr uint32_t kColumns = D / 2;  // of a row, for each of its two threads
+      constexpr uint32_t kColumns = D / kParts;  // of a row, for each of its threads
+      const uint32_t col0 = WIDE ? 0u : w * kColumns;
 #pragma unroll
       for (uint32_t i = 0; i < kColumns; i += 32u) {
-        const uint32_t col = w * kColumns + i;
+        const uint32_t col = col0 + i;
         uint32_t x[32], y[32];
-        TMEM_LD32(x, o_addr + col);
-        TMEM_LD32(y, o_addr + D + col);
+        TMEM_LD32(x, o_addr + (WIDE ? w * D : 0u) + col);
+        if constexpr (!WIDE) TMEM_LD32(y, o_addr + D + col);
         tmem_wait_ld();
 #pragma unroll
         for (int k = 0; k < 32; ++k) {
-          const float o = __uint_as_float(x[k]) * fa + __uint_as_float(y[k]) * fb;
+          const float o = WIDE ? __uint_as_float(x[k]) : __uint_as_float(x[k]) * fa + __uint_as_float(y[k]) * fb;
           nan = nan || o != o;
           x[k] = __float_as_uint(o);
         }
@@ -754,7 +955,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
             reinterpret_cast<uint4*>(mine)[(col / 4u + k) * kRows + row_in] = make_uint4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
         }
       }
-      if (live && w == 0u) {
+      if (live && (WIDE || w == 0u)) {
         if (!whole) {
           mine[kRows * 128 + row_in] = M;
           mine[kRows * 129 + row_in] = sum;
@@ -768,7 +969,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
       while (again) {
         const int src = __ffs(again) - 1;
         again &= again - 1u;
-        constexpr int kPer = D / 32, kOwn = D / 64;  // elements of a row a lane, and of this warp's half of it
+        constexpr int kPer = D / 32, kOwn = kPer / kParts;  // elements of a row a lane, and of this warp's part of it
         const uint32_t rt = __shfl_sync(kFull, tok, src), rh = __shfl_sync(kFull, head, src), rs = __shfl_sync(kFull, row_in, src);
         const float rm = __shfl_sync(kFull, ref, src), rl = __shfl_sync(kFull, sum, src);
         const __nv_bfloat16* q = p.q + (int64_t)(g.lo + (int32_t)rt) * p.q_stride + (size_t)rh * D + lane * kPer;
@@ -796,12 +997,12 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
           for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(kFull, x, d);
           const float pr = exp2_fast(fmaf(x, c, -rm));
 #pragma unroll
-          for (int i = 0; i < kOwn; ++i) acc[i] += pr * __bfloat162float(p.v[from + w * kColumns + lane * kOwn + i]);
+          for (int i = 0; i < kOwn; ++i) acc[i] += pr * __bfloat162float(p.v[from + col0 + lane * kOwn + i]);
         }
         __syncwarp();  // after the row's own thread has written it
 #pragma unroll
         for (int i = 0; i < kOwn; ++i) {
-          const uint32_t col = w * kColumns + lane * kOwn + i;
+          const uint32_t col = col0 + lane * kOwn + i;
           if (whole)
             p.out[((size_t)(g.lo + (int32_t)rt) * p.n_q_heads + rh) * D + col] = __float2bfloat16_rn(rl == 0.f ? 0.f : acc[i] / rl);
           else
@@ -827,14 +1028,15 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
 // Joins the parts of the groups that were cut.  grid (CTAs of the kernel above, slices of 8 rows): the group whose first tile is in CTA x's share and
 // whose last is not, if there is one; a thread has four columns of a row and adds the parts up in their order, kJoinAtOnce of them asked for together.
 constexpr uint32_t kJoinRows = 8, kJoinAtOnce = 8;
-template <int D>
+template <int D, bool WIDE>
 __global__ void __launch_bounds__(kJoinRows * D / 4) tree_join_kernel(const TreeParams p) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const uint4 e = p.ws.open[blockIdx.x];  // parts and rows << 16, first row of the sequence, key-value head, tile of rows
   const uint32_t parts = e.x & 0xFFFFu, slot = blockIdx.y * kJoinRows + threadIdx.x % kJoinRows, quad = threadIdx.x / kJoinRows;
   if (parts < 2u || parts > gridDim.x - blockIdx.x || slot >= e.x >> 16) return;  // none, or not valid after an expired wait
-  const uint32_t row = e.w * kRows + slot, tok = row / p.group;
+  const uint32_t row = (e.w << p.row_bits) + slot, tok = row / p.group;
+  const uint32_t half = WIDE ? slot / kRows : 0u, lane_row = slot % kRows;
   const uint64_t out_row = (uint64_t)e.y + tok;
   if (e.z >= p.n_kv_heads || out_row >= p.n_tokens) return;
   float M = -INFINITY, l = 0.f;
@@ -845,10 +1047,10 @@ __global__ void __launch_bounds__(kJoinRows * D / 4) tree_join_kernel(const Tree
 #pragma unroll
     for (uint32_t i = 0; i < kJoinAtOnce; ++i) {
       const uint32_t at = min(i0 + i, parts - 1u);
-      const float* const src = p.ws.parts + (size_t)(2u * (blockIdx.x + at) + (at == 0u ? 1u : 0u)) * kTreePartFloats;
-      mi[i] = __ldcg(src + kRows * 128 + slot);
-      li[i] = __ldcg(src + kRows * 129 + slot);
-      y[i] = __ldcg(reinterpret_cast<const float4*>(src) + quad * kRows + slot);
+      const float* const src = p.ws.parts + (size_t)((2u * (blockIdx.x + at) + (at == 0u ? 1u : 0u)) * (WIDE ? 2u : 1u) + half) * kTreePartFloats;
+      mi[i] = __ldcg(src + kRows * 128 + lane_row);
+      li[i] = __ldcg(src + kRows * 129 + lane_row);
+      y[i] = __ldcg(reinterpret_cast<const float4*>(src) + quad * kRows + lane_row);
     }
 #pragma unroll
     for (uint32_t i = 0; i < kJoinAtOnce; ++i) {
@@ -885,10 +1087,10 @@ bool encode(CUtensorMap* map, const void* base, const tq_kv_cache* c, uint32_t b
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, bool TMA>
+template <int D, bool TMA, bool WIDE>
 int launch(const TreeParams& p, const CUtensorMap& k_map, const CUtensorMap& v_map, cudaStream_t st) {
-  auto kern = tree_attention_kernel<D, TMA>;
-  constexpr size_t smem = TreeSmem<D>::kTotal;
+  auto kern = tree_attention_kernel<D, TMA, WIDE>;
+  constexpr size_t smem = TreeSmem<D, WIDE>::kTotal;
   const char* what = "tree attention launch";
   if (int rc = tq_ensure_dynamic_smem((const void*)kern, smem, what)) return rc;
   static const int regs = [&] {
@@ -898,8 +1100,15 @@ int launch(const TreeParams& p, const CUtensorMap& k_map, const CUtensorMap& v_m
   if (256 * kSoftRegs + 256 * kOtherRegs > kTreeThreads * regs) return tq_cuda_status((int)cudaErrorInvalidConfiguration, what);
   const uint32_t grid = min((uint32_t)sm_count(), kAttnMaxCtas);
   if (int rc = launch_pdl(kern, dim3(grid), kTreeThreads, smem, st, what, p, k_map, v_map)) return rc;
-  const uint32_t rows = (uint32_t)min((uint64_t)kRows, (uint64_t)p.n_tokens * p.group);
-  return launch_pdl(tree_join_kernel<D>, dim3(grid, (rows + kJoinRows - 1u) / kJoinRows), kJoinRows * D / 4, 0, st, "tree attention (join) launch", p);
+  const uint32_t rows = (uint32_t)min((uint64_t)1 << p.row_bits, (uint64_t)p.n_tokens * p.group);
+  return launch_pdl(tree_join_kernel<D, WIDE>, dim3(grid, (rows + kJoinRows - 1u) / kJoinRows), kJoinRows * D / 4, 0, st, "tree attention (join) launch", p);
+}
+
+template <int D, bool TMA>
+int launch_rows(TreeParams& p, const CUtensorMap& k_map, const CUtensorMap& v_map, cudaStream_t st) {
+  const bool wide = (uint64_t)p.n_tokens * p.group >= (uint64_t)kWideRows * p.n_seqs;
+  p.row_bits = wide ? 8u : 7u;
+  return wide ? launch<D, TMA, true>(p, k_map, v_map, st) : launch<D, TMA, false>(p, k_map, v_map, st);
 }
 
 bool misaligned(const void* ptr, uintptr_t align) { return ptr == nullptr || ((uintptr_t)ptr & (align - 1u)) != 0; }
@@ -954,6 +1163,6 @@ extern "C" int tq_tree_attention(const tq_kv_cache* cache, const void* d_q, int6
   p.boxes = kStates / p.box;
   CUtensorMap k_map{}, v_map{};
   if (p.box >= 8u && encode(&k_map, cache->d_k, cache, p.box) && encode(&v_map, cache->d_v, cache, p.box))
-    return cache->head_dim == 64 ? launch<64, true>(p, k_map, v_map, st) : launch<128, true>(p, k_map, v_map, st);
-  return cache->head_dim == 64 ? launch<64, false>(p, k_map, v_map, st) : launch<128, false>(p, k_map, v_map, st);
+    return cache->head_dim == 64 ? launch_rows<64, true>(p, k_map, v_map, st) : launch_rows<128, true>(p, k_map, v_map, st);
+  return cache->head_dim == 64 ? launch_rows<64, false>(p, k_map, v_map, st) : launch_rows<128, false>(p, k_map, v_map, st);
 }

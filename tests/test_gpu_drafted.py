@@ -268,6 +268,14 @@ def test_wide_trees(tq, ws):
     tree_case(tq, ws, [100, 40], [900, 64], 8, 2, 128, 16, "random", seed=10, words=2)  # tokens past the words are not seen
 
 
+@pytest.mark.parametrize("kind", ["chain", "tree", "random"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("H,K", [(8, 2), (6, 1), (5, 5)])
+@pytest.mark.parametrize("new,lens,page", [([65], [65], 16), ([129], [5000], 24), ([300, 0, 131, 170], [700, 9, 131, 2900], 64), ([140, 1, 150], [140, 5000, 12000], 1)])
+def test_tiles_of_256_rows(tq, ws, kind, D, H, K, new, lens, page):
+    tree_case(tq, ws, new, lens, H, K, D, page, kind, seed=sum(lens) + H, layout=page % 2)
+
+
 def test_fewer_states_than_new_tokens(tq, ws):
     tree_case(tq, ws, [9, 5, 4], [4, 0, -3], 4, 2, 64, 16, "chain", seed=11)
     tree_case(tq, ws, [9, 5, 40], [4, 0, 33], 4, 2, 64, 16, "random", seed=12)
@@ -316,7 +324,7 @@ def test_large_scores(tq, ws):
 
 def test_states_that_a_token_does_not_see_may_hold_anything(tq, ws):
     g = gen(18)
-    for D, H, K, n, length in ((64, 4, 2, 6, 131), (128, 16, 2, 20, 700)):
+    for D, H, K, n, length in ((64, 4, 2, 6, 131), (128, 16, 2, 20, 700), (128, 8, 1, 30, 700), (64, 16, 2, 31, 900)):
         kp, vp = randn(g, 60, K, 16, D, dtype=BF), randn(g, 60, K, 16, D, dtype=BF)
         q = randn(g, n, H, D, dtype=BF)
         table = torch.randperm(60, generator=g, device="cuda").int()[None].contiguous()
