@@ -14,10 +14,17 @@
 // A row is read once: a cluster of up to eight CTAs holds it in shared memory and speaks through distributed shared memory.  Then
 //   top-k (up to 1024): the k-th largest of the threads' own maxima is a bound of the k-th logit that few others pass: those go to one CTA,
 //          which sorts them and does the rest;
-//   top-p alone: a histogram of the weights over 32 bins an octave (exact: two integers a bin) finds the bin of the border, whose
-//          tokens one CTA sorts; then every CTA adds up what it keeps;
-//   neither, or min-p alone: the border is known; every CTA adds up what it keeps.
+//   top-p alone: a histogram of the weights over 32 bins an octave (exact: two integers a bin, as many atomics; one that returns, with a carry
+//          now and then, takes as long, a 64-bit one longer) finds the bin of the border.  Where its sum is that of one token that is all;
+//          else one CTA gets the bin's tokens and finds the one with which the sum is reached: over 128 of them by a finer histogram of
+//          theirs, then each with each.  What is kept is in the CTAs' bins up to there: only the one that has the drawn token adds it up again;
+//   neither, or min-p: the border is known; every CTA adds up what it keeps.
 // Where so many logits are alike that a list does not hold them (2048), and for larger k, the border is found by bisection of the order.
+//
+// Bound: the bytes (a logit is read once) only for one row in 512; instructions otherwise, 25 to 60 of them a logit, issued in 55 % of the cycles
+// (shared memory's data path 37 % busy), and for few rows the eight barriers of the cluster, 1500 to 2500 cycles each with what they wait for.
+// One B200, 128256 logits in fp32, us: one row top-k 10.1, top-p 18.7, none 10.5; 64 rows with settings of all kinds 49; 512 rows greedy 96 (their
+// bytes: 40), top-k 162, none 154 - 228, top-p 0.9 259 (peaked) - 446 (flat).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
