@@ -546,7 +546,8 @@ int tq_qk_norm_rope_append(const void* d_q, const void* d_k, const void* d_v, in
  *   0 .. i where d_mask is NULL (a chain; a piece of a prompt).
  *   out[row][h] = sum_s softmax_s(scale * q[row][h] . k_s) v_s,  lse[row][h] the natural logarithm of the denominator;
  * a token that sees nothing gives zeros and lse -inf.  States that a token does not see may hold anything, Inf and NaN included (a token
- * is slow where another token of its sequence sees such a state).  The same call gives the same bits.
+ * is slow where another token of its sequence sees such a state: its output is computed again, which over more than 300000 states may
+ * end in TQ_STATUS_WAIT_EXPIRED).  The same call gives the same bits.
  * d_q: DEVICE bf16, n_tokens rows of [n_q_heads][head_dim], q_stride elements from row to row (multiple of 8), 16-byte aligned.
  * Page table, lengths, workspace and status are those of tq_paged_attention, d_out bf16 [n_tokens][n_q_heads][head_dim],
  * d_lse fp32 [n_tokens][n_q_heads] or NULL.  Fewer states than new tokens (lens[b] < n): the first ones have none.
@@ -569,8 +570,8 @@ int tq_tree_attention(const tq_kv_cache* cache, const void* d_q, int64_t q_strid
  * A NaN counts as -inf.  Where some x_i are +inf they alone are kept, as equals.  A row without anything above -inf gives token -1 and
  * logprob -inf.  vocab: 1..TQ_SAMPLE_MAX_VOCAB.
  * Weights are held as integers, the largest as 2^45 and each within 2^-26 of itself (or, below 2^21, some units), and their sums are exact: a
- * row's token depends on nothing but the row.  Temperatures below 2^-120 and above 2^100 are
- * taken as those, settings that are NaN as not given. */
+ * row's token depends on nothing but the row.  Temperatures below 2^-120 and above 2^100 are taken as
+ * those, settings that are NaN as not given. */
 #define TQ_SAMPLE_MAX_VOCAB 262144u
 int tq_sample(const void* d_logits, int x_type, int64_t row_stride, uint32_t rows, uint32_t vocab,
               const float* d_uniform, const float* d_temperature, const int32_t* d_top_k, const float* d_top_p,
@@ -585,7 +586,8 @@ int tq_sample(const void* d_logits, int x_type, int64_t row_stride, uint32_t row
  * lens[b] - n + d.  A sequence without rows has count 0 and keeps its length.
  * d_tokens (drafted), d_parents (row of the parent, counted from first[b]; of row first[b] it means nothing; not below the row itself: never
  * followed), d_sampled: DEVICE int32 [n_tokens].  caches: HOST, n_caches (0..TQ_MAX_CACHES) descriptions of the layers' caches, alike but for d_k,
- * d_v and d_status, which share the page table (d_page_table may be NULL where n_caches is 0).  max_path: 1..TQ_TREE_MAX_PATH.  d_path, d_out_tokens: DEVICE
+ * d_v and d_status, which share the page table (d_page_table may be NULL where n_caches is 0); a pool that is there twice is
+ * moved once.  max_path: 1..TQ_TREE_MAX_PATH.  d_path, d_out_tokens: DEVICE
  * int32 [n_seqs][max_path]; d_count, d_lens_out: DEVICE int32 [n_seqs], not overlapping an input.  A position or a page
  * outside the cache is not touched and sets TQ_STATUS_BAD_PAGE in the caches' status words. */
 #define TQ_MAX_CACHES 128u

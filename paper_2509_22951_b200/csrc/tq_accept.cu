@@ -37,7 +37,8 @@ struct AcceptParams {
   uint32_t n_tokens, max_path, max_pages, n_caches;
   uint32_t n_pages, page_size, n_kv_heads, chunks;  // chunks: 16 bytes of a head
   int64_t page_stride, head_stride, slot_stride;
-  uint4* kv[TQ_MAX_CACHES][2];
+  uint32_t n_pools;
+  uint4* pools[2 * TQ_MAX_CACHES];  // keys and values of the caches, each once
   uint32_t* status[TQ_MAX_CACHES];
 };
 
@@ -126,10 +127,10 @@ __global__ void __launch_bounds__(kAcceptThreads) tree_accept_kernel(const __gri
       if (p.status[c]) atomicOr(p.status[c], TQ_STATUS_BAD_PAGE);
   __syncthreads();
   if (s_moves == 0u) return;
-  const uint32_t per_head = p.chunks, per_side = p.n_kv_heads * per_head, columns = p.n_caches * 2u * per_side;
+  const uint32_t per_head = p.chunks, per_side = p.n_kv_heads * per_head, columns = p.n_pools * per_side;
   for (uint32_t col = blockIdx.y * kAcceptThreads + tid; col < columns; col += gridDim.y * kAcceptThreads) {
-    const uint32_t side = col / per_side, rest = col - side * per_side, head = rest / per_head, x = rest - head * per_head;
-    uint4* const base = p.kv[side >> 1][side & 1u] + ((int64_t)head * p.head_stride) / 8 + x;
+    const uint32_t pool = col / per_side, rest = col - pool * per_side, head = rest / per_head, x = rest - head * per_head;
+    uint4* const base = p.pools[pool] + ((int64_t)head * p.head_stride) / 8 + x;
     for (uint32_t d0 = 1; d0 < count; d0 += 4u) {
       uint4 v[4];
 #pragma unroll
@@ -154,14 +155,20 @@ extern "C" int tq_tree_accept(const tq_kv_cache* caches, uint32_t n_caches, cons
   if ((n_caches && !caches) || max_path == 0 || (n_caches && max_pages == 0)) return TQ_ERR_INVALID_ARG;
   if (n_caches > TQ_MAX_CACHES || max_path > TQ_TREE_MAX_PATH || n_seqs > 0x7FFFFFFFu || n_tokens > 0x7FFFFFFFu) return TQ_ERR_UNSUPPORTED_SHAPE;
   AcceptParams p{};
+  constexpr uint32_t kKnown = 512;  // places of a table of the pools, twice as many as there can be
+  static_assert(kKnown >= 4 * TQ_MAX_CACHES && kKnown == 1u << (32 - 23), "the table does not fill up");
+  const void* known[kKnown] = {};
   for (uint32_t i = 0; i < n_caches; ++i) {
     const tq_kv_cache &c = caches[i], &c0 = caches[0];
     if (int rc = tq_check_cache(&c)) return rc;
     if (c.n_pages != c0.n_pages || c.page_size != c0.page_size || c.n_kv_heads != c0.n_kv_heads || c.head_dim != c0.head_dim ||
         c.page_stride != c0.page_stride || c.head_stride != c0.head_stride || c.slot_stride != c0.slot_stride)
       return TQ_ERR_INVALID_ARG;
-    p.kv[i][0] = static_cast<uint4*>(c.d_k);
-    p.kv[i][1] = static_cast<uint4*>(c.d_v);
+    for (void* pool : {c.d_k, c.d_v}) {  // moved twice at once, a pool's states would be read after they have been written over
+      uint32_t at = (uint32_t)((uintptr_t)pool >> 4) * 2654435769u >> 23;
+      while (known[at] != nullptr && known[at] != pool) at = (at + 1u) % kKnown;
+      if (known[at] == nullptr) known[at] = p.pools[p.n_pools++] = static_cast<uint4*>(pool);
+    }
     p.status[i] = c.d_status;
   }
   if (n_seqs == 0) return TQ_OK;
@@ -192,7 +199,7 @@ extern "C" int tq_tree_accept(const tq_kv_cache* caches, uint32_t n_caches, cons
     p.slot_stride = caches[0].slot_stride;
   }
   // a block for every 256 pieces of 16 bytes of a state, but no more than eight blocks an SM in all: each walks the tree again
-  const uint64_t columns = (uint64_t)n_caches * 2u * p.n_kv_heads * p.chunks, room = 8ull * (uint64_t)sm_count() / n_seqs;
+  const uint64_t columns = (uint64_t)p.n_pools * p.n_kv_heads * p.chunks, room = 8ull * (uint64_t)sm_count() / n_seqs;
   const uint64_t shares = (columns + kAcceptThreads - 1u) / kAcceptThreads;
   const uint32_t y = (uint32_t)(shares < room ? shares : room);
   return launch_pdl(tree_accept_kernel, dim3(n_seqs, y ? y : 1u), kAcceptThreads, 0, (cudaStream_t)cuda_stream, "tree_accept launch", p);

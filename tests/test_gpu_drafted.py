@@ -890,3 +890,46 @@ def test_weights_of_any_alignment(tq):
         want = tq.tq_qk_norm_rope_append(q, k, k, w[at:at + 128].clone(), w[at + 128:at + 256].clone(), *args)
         kw = kp.clone()
         assert torch.equal(tq.tq_qk_norm_rope_append(q, k, k, w[at:at + 128], w[at + 128:at + 256], *args), want) and torch.equal(kp, kw)
+
+
+def test_a_pool_that_is_given_twice_is_moved_once(tq):
+    """A path on which every state comes from where an earlier one's neighbour lay: moved twice at once, states would be lost."""
+    g, n, K, D, page = gen(78), 40, 8, 128, 16
+    kp, vp = randn(g, 8, K, page, D, dtype=BF), randn(g, 8, K, page, D, dtype=BF)
+    table, length = torch.randperm(8, generator=g, device="cuda").int()[None].contiguous(), 100
+    path = [0] + list(range(2, n))  # row 1 is not taken
+    parents, tokens = [-1, 0, 0] + list(range(2, n - 1)), [5, 1] + [2 + i % 3 for i in range(n - 2)]
+    sampled = [tokens[2], 0] + [tokens[i + 1] for i in range(2, n - 1)] + [9]
+    place = table[0].long()
+    want = [x[place].transpose(1, 2).reshape(-1, K, D).clone() for x in (kp, vp)]
+    for w in want:
+        w[length - n:length - n + len(path)] = w[[length - n + i for i in path]]
+    c = tq.tq_kv_cache(kp, vp)
+    caches = tq.tq_kv_caches([c, tq.tq_kv_cache(vp, kp), c, tq.tq_kv_cache(kp, kp)] * 8)
+    got = tq.tq_tree_accept(caches, table, i32([0, n]), i32([length]), i32(tokens), i32(parents), i32(sampled), n)
+    assert got[1].tolist() == [path + [-1]] and got[2].tolist() == [n - 1] and got[3].tolist() == [length - 1]
+    for x, w in zip((kp, vp), want):
+        assert torch.equal(x[place].transpose(1, 2).reshape(-1, K, D)[:length - 1], w[:length - 1])
+
+
+def test_a_spoiled_row_of_a_long_cache(tq, ws):
+    """An infinite value that the others do not see, behind a cache of many tiles in several CTAs: they are computed again from what they see."""
+    g, n, H, K, D, page, length = gen(77), 20, 8, 1, 128, 16, 9001
+    P = -(-length // page)
+    kp, vp = randn(g, P, K, page, D, dtype=BF), randn(g, P, K, page, D, dtype=BF)
+    q, table = randn(g, n, H, D, dtype=BF, scale=1.5), torch.randperm(P, generator=g, device="cuda").int()[None].contiguous()
+    bits = torch.eye(n, dtype=torch.bool)
+    bits[:, 0] = True
+    k, v = (x[table[0].long(), 0].reshape(-1, D)[:length].clone() for x in (kp, vp))
+    s = length - n + 7
+    vp[int(table[0, s // page]), 0, s % page] = -INF
+    out, lse = torch.empty(n, H, D, dtype=BF, device="cuda"), torch.empty(n, H, device="cuda")
+    tq.tq_tree_attention(q, tq.tq_kv_cache(kp, vp), table, i32([0, n]), i32([length]), ws, mask=pack(bits, 1), out=out, lse=lse)
+    seen = torch.ones(n, length, dtype=torch.bool, device="cuda")
+    seen[:, length - n:] = bits.cuda()
+    others = [i for i in range(n) if i != 7]
+    for h in range(H):
+        want, wl, bound = attend_ref(q[others, h], k, v, seen[others], D ** -0.5)
+        within(out[others, h], want, bound)
+        check_lse(lse[others, h], wl)
+    assert bool((out[7] == -INF).all())
