@@ -980,24 +980,49 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         for (int i = 0; i < kPer; ++i) qv[i] = __bfloat162float(q[i]);
         const uint32_t s1 = min(t1 * kStates, g.end);
 #pragma unroll 1
-        for (uint32_t s = t0 * kStates; s < s1; ++s) {
+        for (uint32_t s0 = t0 * kStates; s0 < s1; s0 += 32u) {  // a lane looks a state up; four of those that are seen are loaded together
+          const uint32_t s = s0 + lane, pg = s / p.page_size;
           const int64_t j = (int64_t)s - g.before;
-          if (j >= 0 && (p.mask ? (j >> 5) >= (int64_t)p.mask_words ||
-                                      !((__ldg(p.mask + (size_t)(g.lo + (int32_t)rt) * p.mask_words + (j >> 5)) >> (j & 31)) & 1u)
-                                : j > (int64_t)rt))
-            continue;
-          const uint32_t pg = s / p.page_size;
-          const int32_t page = __ldg(p.page_table + (size_t)g.b * p.max_pages + pg);
-          if ((uint32_t)page >= p.n_pages) continue;
-          const int64_t from = (int64_t)page * p.page_stride + (int64_t)g.kvh * p.head_stride + (int64_t)(s - pg * p.page_size) * p.slot_stride;
-          float x = 0.f;
+          bool seen = s < s1;
+          if (seen && j >= 0)
+            seen = p.mask ? (j >> 5) < (int64_t)p.mask_words && ((__ldg(p.mask + (size_t)(g.lo + (int32_t)rt) * p.mask_words + (j >> 5)) >> (j & 31)) & 1u) != 0u
+                          : j <= (int64_t)rt;
+          int64_t place = 0;
+          if (seen) {
+            const int32_t page = __ldg(p.page_table + (size_t)g.b * p.max_pages + pg);
+            seen = (uint32_t)page < p.n_pages;
+            place = (int64_t)page * p.page_stride + (int64_t)g.kvh * p.head_stride + (int64_t)(s - pg * p.page_size) * p.slot_stride;
+          }
+          uint32_t left = __ballot_sync(kFull, seen);
+#pragma unroll 1
+          while (left) {
+            constexpr int kAtOnce = 4;
+            int64_t from[kAtOnce];
+            float x[kAtOnce], v[kAtOnce][kOwn];
+            bool on[kAtOnce];
 #pragma unroll
-          for (int i = 0; i < kPer; ++i) x += qv[i] * __bfloat162float(p.k[from + lane * kPer + i]);
+            for (int z = 0; z < kAtOnce; ++z) {
+              on[z] = left != 0u;
+              from[z] = __shfl_sync(kFull, (long long)place, on[z] ? __ffs(left) - 1 : 0);
+              left &= left - 1u;
+            }
 #pragma unroll
-          for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(kFull, x, d);
-          const float pr = exp2_fast(fmaf(x, c, -rm));
+            for (int z = 0; z < kAtOnce; ++z) {
+              x[z] = 0.f;
 #pragma unroll
-          for (int i = 0; i < kOwn; ++i) acc[i] += pr * __bfloat162float(p.v[from + col0 + lane * kOwn + i]);
+              for (int i = 0; i < kPer; ++i) x[z] += on[z] ? qv[i] * __bfloat162float(p.k[from[z] + lane * kPer + i]) : 0.f;
+#pragma unroll
+              for (int i = 0; i < kOwn; ++i) v[z][i] = on[z] ? __bfloat162float(p.v[from[z] + col0 + lane * kOwn + i]) : 0.f;
+            }
+#pragma unroll
+            for (int z = 0; z < kAtOnce; ++z) {
+#pragma unroll
+              for (int d = 16; d > 0; d >>= 1) x[z] += __shfl_xor_sync(kFull, x[z], d);
+              const float pr = on[z] ? exp2_fast(fmaf(x[z], c, -rm)) : 0.f;
+#pragma unroll
+              for (int i = 0; i < kOwn; ++i) acc[i] += pr * v[z][i];
+            }
+          }
         }
         __syncwarp();  // after the row's own thread has written it
 #pragma unroll
