@@ -271,7 +271,7 @@ def test_wide_trees(tq, ws):
 @pytest.mark.parametrize("kind", ["chain", "tree", "random"])
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("H,K", [(8, 2), (6, 1), (5, 5)])
-@pytest.mark.parametrize("new,lens,page", [([65], [65], 16), ([129], [5000], 24), ([300, 0, 131, 170], [700, 9, 131, 2900], 64), ([140, 1, 150], [140, 5000, 12000], 1)])
+@pytest.mark.parametrize("new,lens,page", [([65], [65], 16), ([129], [5000], 24), ([300, 0, 131, 170], [700, 9, 131, 2900], 64), ([140, 1, 150], [140, 5000, 12000], 1), ([150, 140, 133], [64, 0, -3], 16)])
 def test_tiles_of_256_rows(tq, ws, kind, D, H, K, new, lens, page):
     tree_case(tq, ws, new, lens, H, K, D, page, kind, seed=sum(lens) + H, layout=page % 2)
 
