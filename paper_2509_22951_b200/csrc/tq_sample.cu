@@ -723,6 +723,52 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
       at += w[i];
     }
   };
+  // The filters and the token of at most kNear listed ones by comparing each with each, four threads to a token: three steps of the CTA,
+  // where sorting by order and by place takes some thirty (one row 10.1 us with that).
+  auto few_in_list = [&](uint32_t m, uint32_t k, uint64_t keep) {
+    const uint32_t j = tid / 4u, part = tid % 4u;
+    const uint64_t order = j < m ? sh.list[j] : 0ull, own = j < m ? weight(logit_of(order)) : 0ull;
+    if (part == 0u && j < m) sh.close_w[j] = own;
+    __syncthreads();
+    uint32_t ahead = 0;
+    uint64_t before = 0;
+    for (uint32_t i = part; i < m; i += 4u) {
+      const bool larger = sh.list[i] > order;
+      ahead += larger ? 1u : 0u;
+      before += larger ? sh.close_w[i] : 0ull;
+    }
+#pragma unroll
+    for (int d = 1; d < 4; d *= 2) {
+      ahead += __shfl_xor_sync(kFull, ahead, d);
+      before += __shfl_xor_sync(kFull, before, d);
+    }
+    bool in = j < m && ahead < k;
+    if (p_on) {
+      const uint64_t of_warp = warp_sum(in && part == 0u ? own : 0ull);
+      if (lane == 0) sh.warps[warp] = of_warp;
+      __syncthreads();
+      const uint64_t bound = bound_of(top_p, warp_sum(lane < kWarps ? sh.warps[lane] : 0ull));  // (all lanes take part in the sum)
+      in = in && before < bound;
+    }
+    in = in && order >= keep;
+    __syncthreads();
+    if (part == 0u && j < m) sh.close_w[j] = in ? own : 0ull;
+    __syncthreads();
+    const uint32_t at = index_of(order);
+    uint64_t prev = 0, total = 0;
+    for (uint32_t i = part; i < m; i += 4u) {
+      const uint64_t w = sh.close_w[i];
+      total += w;
+      prev += index_of(sh.list[i]) < at ? w : 0ull;
+    }
+#pragma unroll
+    for (int d = 1; d < 4; d *= 2) {
+      total += __shfl_xor_sync(kFull, total, d);
+      prev += __shfl_xor_sync(kFull, prev, d);
+    }
+    const uint64_t target = target_of(total);
+    if (in && part == 0u && target >= prev && target < prev + own) answer(order, total);
+  };
   bool coded = false;  // weights lie where the logits were
   bool summed = false;  // the bins have the sums of what is kept, hits[] the tokens in the border's
   bool whole_bin = false;  // and all of them are kept
@@ -770,6 +816,11 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     if (m <= kList) {
       cluster_arrive();  // the first CTA stays until all have read that
       if (rank != 0) return;
+      if (m <= kNear) {
+        few_in_list(m, k, keep);
+        cluster_wait();
+        return;
+      }
       sort_list(sh.list, m, tid);
       uint32_t kept = min(k, m);
       uint64_t w[kEach], sum = 0, total, prev;
