@@ -85,6 +85,7 @@ struct TreeParams {
   uint32_t mask_words, max_pages, page_size, n_pages;
   uint32_t n_tokens, n_seqs, n_q_heads, n_kv_heads, group;
   uint32_t row_bits;  // log2 of a tile's rows: 7 or 8
+  bool whole;         // no group is cut
   float scale_log2;
   uint32_t box, boxes;  // slots of a page that one tensor copy brings, copies to a tile of 128 states
   uint32_t* status;
@@ -198,6 +199,10 @@ static_assert(sizeof(Plan) <= 96 && alignof(Plan) <= 16, "room for the plan");
 
 // Groups are left whole where the longest share is then no more than kWholeTiles tiles above the mean of the shares.
 constexpr uint32_t kWholeTiles = 3;
+// Where the page table has no room for longer sequences than this, none is cut and the joining kernel is not launched.  us, never cut | cut as the
+// lengths have it, 32 / 8 heads of 128, 8 new tokens: 1 sequence of 100 states 9.2 | 10.8, 16 of 500 15.5 | 18.7, 64 of 250 31.6 | 34.5; 512 tokens
+// of a prompt 24 | 28; but 1 sequence of 1000 states 17.2 | 14.7, of 760 14.9 | 13.8.
+constexpr uint32_t kNeverCutTiles = 4;
 
 __device__ __forceinline__ Plan make_plan(const TreeParams& p, uint32_t lane) {
   Plan r{};
@@ -240,7 +245,7 @@ __device__ __forceinline__ Plan make_plan(const TreeParams& p, uint32_t lane) {
   r.over = total - r.mean * ctas;
   // the longest share without cuts: whole groups of one size, or up to one group over the mean
   const uint32_t longest = most == least ? ((groups * p.n_kv_heads - 1u) / ctas + 1u) * most : r.mean + most;
-  r.cut = longest > r.mean + (r.over != 0u ? 1u : 0u) + kWholeTiles;
+  r.cut = !p.whole && longest > r.mean + (r.over != 0u ? 1u : 0u) + kWholeTiles;
   if (blockIdx.x >= ctas) return r;
   r.u0 = r.mean * blockIdx.x + min(blockIdx.x, r.over);
   r.u1 = r.u0 + r.mean + (blockIdx.x < r.over ? 1u : 0u);
@@ -1125,6 +1130,7 @@ int launch(const TreeParams& p, const CUtensorMap& k_map, const CUtensorMap& v_m
   if (256 * kSoftRegs + 256 * kOtherRegs > kTreeThreads * regs) return tq_cuda_status((int)cudaErrorInvalidConfiguration, what);
   const uint32_t grid = min((uint32_t)sm_count(), kAttnMaxCtas);
   if (int rc = launch_pdl(kern, dim3(grid), kTreeThreads, smem, st, what, p, k_map, v_map)) return rc;
+  if (p.whole) return TQ_OK;
   const uint32_t rows = (uint32_t)min((uint64_t)1 << p.row_bits, (uint64_t)p.n_tokens * p.group);
   return launch_pdl(tree_join_kernel<D, WIDE>, dim3(grid, (rows + kJoinRows - 1u) / kJoinRows), kJoinRows * D / 4, 0, st, "tree attention (join) launch", p);
 }
@@ -1181,6 +1187,7 @@ extern "C" int tq_tree_attention(const tq_kv_cache* cache, const void* d_q, int6
   p.group = n_q_heads / cache->n_kv_heads;
   p.scale_log2 = scale * 1.4426950408889634f;
   p.status = cache->d_status;
+  p.whole = states <= kStates * kNeverCutTiles;
   cudaStream_t st = (cudaStream_t)cuda_stream;
   // Boxes that fit pages and tiles alike; the swizzle repeats every 8 rows, so pages of other sizes are copied row by row.
   p.box = 128u;
