@@ -13,7 +13,7 @@
 //
 // A row is read once: a cluster of up to eight CTAs holds it in shared memory and speaks through distributed shared memory.  Then
 //   top-k (up to 1024): the k-th largest of the threads' own maxima is a bound of the k-th logit that few others pass: those go to one CTA,
-//          which sorts them and does the rest;
+//          which does the rest: up to 128 tokens by comparing each with each, more by sorting;
 //   top-p alone: a histogram of the weights over 32 bins an octave (exact: two integers a bin, as many atomics; one that returns, with a carry
 //          now and then, takes as long, a 64-bit one longer) finds the bin of the border.  Where its sum is that of one token that is all;
 //          else one CTA gets the bin's tokens and finds the one with which the sum is reached: over 128 of them by a finer histogram of
@@ -23,8 +23,8 @@
 //
 // Bound: the bytes (a logit is read once) only for one row in 512; instructions otherwise, 25 to 60 of them a logit, issued in 55 % of the cycles
 // (shared memory's data path 37 % busy), and for few rows the eight barriers of the cluster, 1500 to 2500 cycles each with what they wait for.
-// One B200, 128256 logits in fp32, us: one row top-k 10.1, top-p 18.7, none 10.5; 64 rows with settings of all kinds 49; 512 rows greedy 96 (their
-// bytes: 40), top-k 162, none 154 - 228, top-p 0.9 259 (peaked) - 446 (flat).
+// One B200, 128256 logits in fp32, us: one row top-k 8.5, top-p 18.8, none 10.5; 64 rows with settings of all kinds 48; 512 rows greedy 96 (their
+// bytes: 40), top-k 157, none 154 - 228, top-p 0.9 259 (peaked) - 446 (flat).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -724,7 +724,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     }
   };
   // The filters and the token of at most kNear listed ones by comparing each with each, four threads to a token: three steps of the CTA,
-  // where sorting by order and by place takes some thirty (one row 10.1 us with that).
+  // where sorting by order and by place takes some thirty (one row 10.1 us with that, 8.5 with this).
   auto few_in_list = [&](uint32_t m, uint32_t k, uint64_t keep) {
     const uint32_t j = tid / 4u, part = tid % 4u;
     const uint64_t order = j < m ? sh.list[j] : 0ull, own = j < m ? weight(logit_of(order)) : 0ull;

@@ -32,9 +32,9 @@
 // The output is rescaled only when a row's maximum has grown by more than 2^8 since the last rescaling (online softmax with the rescaling
 // delayed up to a threshold, as in the kernel of cross attention): p stays below 2^8, which costs no precision in bf16 or the fp32 sum.
 //
-// Measured (one B200, 6545 GB/s copied, us): 197 states x 8 tokens, 32 heads of 64 10; 8 sequences of up to 16 tokens and 8191 states, 24 heads 35 (its
-// bytes: 19); 31 tokens over 131071 states, 32 heads 104 (82); 64 chains of 5 tokens over up to 16384 states, 64 heads 390 (386); pieces of 1024
-// tokens of two prompts up to 9001 long, 32 heads 184 (operations at the rate of a library product: 106).
+// Measured (one B200, 6545 GB/s copied, us): 197 states x 8 tokens, 32 heads of 64 9.7; 8 sequences of up to 16 tokens and 8191 states, 24 heads 35 (its
+// bytes: 19); 31 tokens over 131071 states, 32 heads 104 (82); 64 chains of 5 tokens over up to 16384 states, 64 heads 392 (386), 453 under the
+// power limit; pieces of 1024 tokens of two prompts up to 9001 long, 32 heads 184, 207 under the limit (operations at the rate of a library product: 106).
 //
 // States that are not there (past the end, on a page outside the pool) are zeros in shared memory and hidden from all rows.  A state that only
 // some rows see enters the others' sums with p = 0; if its value is Inf or NaN that product is NaN, so a row whose sum of p is finite but whose
