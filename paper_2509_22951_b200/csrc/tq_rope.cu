@@ -7,9 +7,9 @@
 // and reuses them over the token's query and key heads.  8 to 16 bytes move per two or three operations:
 // memory bound for prompts, latency for a decode step.
 //
-// Norm: the D / 8 lanes that have a head add its squares up by shuffles, and a thread keeps the eight weights of its elements
-// for queries and the eight for keys.  Eight multiplications and four shuffles an element group more on a path that waits for memory:
-// 2047 tokens of 64 + 8 heads of 128 in bf16 take 23.2 us (their bytes: 12.8; issue slots 65 % busy), 32 tokens of 24 + 8 in fp32 2.2 us.
+// Norm: the D / 8 lanes that have a head add its squares up by shuffles, and a thread keeps the eight weights of its elements,
+// from its first key on those of keys (both sets at once, and a choice for every element: 23.2 us).  Eight multiplications and four shuffles
+// an element group more on a path that waits for memory: 2047 tokens of 64 + 8 heads of 128 in bf16 take 20.8 us (their bytes: 12.8), 32 tokens of 24 + 8 in fp32 2.2 us.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -105,13 +105,16 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopePar
     known = known && pos[a] < p.n_positions;
   }
 
+  // With the norm, whose reduction takes its time, the next head is under way during it, and of bf16 the one after that too (2047 tokens of 64 / 8
+  // heads of 128, us, one | two under way: bf16 21.6 | 20.8, 32 / 8 heads 16.3 | 15.2; fp32, whose second one costs a block an SM, 22.2 | 26.9).
+  constexpr bool kAhead = NORM && TYPE == TQ_TYPE_BF16;
   // Heads in order: queries, keys, values.  The first head is asked for before the cosines and sines, which wait for the
   // positions, and whether the token has a slot is not waited for either.  (Two or three heads of a thread under way: 15.5 and 14.1 us for 2047 tokens of 32 / 8 fp32 heads of 128, one:
   // 13.9.)
   const uint32_t H = p.n_q_heads, K = p.cache.n_kv_heads, heads = H + 2u * K, step = gridDim.y * kSide;
   const size_t tq = (size_t)t * p.q_stride + e0, tk = (size_t)t * p.k_stride + e0, tv = (size_t)t * p.v_stride + e0;
   const uint32_t gap = e1 - e0;
-  Raw4x2<TYPE> raw, next;  // next: with the norm, whose reduction takes its time, the head after this one is asked for before
+  Raw4x2<TYPE> raw, next;
   auto load = [&](uint32_t n, Raw4x2<TYPE>& to) {
     if (n >= heads) return;
     const void* src = n < H ? p.q : (n < H + K ? p.k : p.v);
@@ -120,7 +123,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopePar
   };
   uint32_t n = blockIdx.y * kSide + threadIdx.x / kPerHead;
   load(n, raw);
-  if (NORM) load(n + step, next);
+  if (kAhead) load(n + step, next);
 
   const uint32_t page = (uint32_t)slot / p.cache.page_size;  // -1: no slot; other negative ones are out of range like those past the pool
   const bool in_pool = slot >= 0 && page < p.cache.n_pages, keep = in_pool && known;
@@ -130,22 +133,18 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopePar
   }
   const size_t slot_at = keep ? (size_t)page * p.cache.page_stride + (size_t)((uint32_t)slot - page * p.cache.page_size) * p.cache.slot_stride + e0 : 0;
 
-  float wq[NORM ? 8 : 1], wk[NORM ? 8 : 1];
-  if constexpr (NORM) {
+  float w[NORM ? 8 : 1];  // of the queries, from the first key on of the keys
+  bool keys = n >= H;
+  auto weights = [&](const float* from) {
     if (p.weights_16) {
-      const float4 a = __ldg(reinterpret_cast<const float4*>(p.q_weight + e0)), b = __ldg(reinterpret_cast<const float4*>(p.q_weight + e1));
-      const float4 c = __ldg(reinterpret_cast<const float4*>(p.k_weight + e0)), d = __ldg(reinterpret_cast<const float4*>(p.k_weight + e1));
-      wq[0] = a.x, wq[1] = a.y, wq[2] = a.z, wq[3] = a.w, wq[4] = b.x, wq[5] = b.y, wq[6] = b.z, wq[7] = b.w;
-      wk[0] = c.x, wk[1] = c.y, wk[2] = c.z, wk[3] = c.w, wk[4] = d.x, wk[5] = d.y, wk[6] = d.z, wk[7] = d.w;
+      const float4 a = __ldg(reinterpret_cast<const float4*>(from + e0)), b = __ldg(reinterpret_cast<const float4*>(from + e1));
+      w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint32_t at = (i < 4 ? e0 : e1 - 4u) + i;
-        wq[i] = __ldg(p.q_weight + at);
-        wk[i] = __ldg(p.k_weight + at);
-      }
+      for (int i = 0; i < 8; ++i) w[i] = __ldg(from + (i < 4 ? e0 : e1 - 4u) + i);
     }
-  }
+  };
+  if constexpr (NORM) weights(keys ? p.k_weight : p.q_weight);
 
   float cs[4], sn[4];
 #pragma unroll
@@ -163,11 +162,17 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopePar
   for (; n < heads && (n < H || keep); n += step) {
     float f[8];
     raw.get(f);
-    if (NORM) {
+    if (kAhead) {
       raw = next;
       load(n + 2u * step, next);
+    } else if (NORM) {
+      load(n + step, raw);
     }
     if constexpr (NORM) {
+      if (n >= H && !keys) {
+        weights(p.k_weight);
+        keys = true;
+      }
       if (n < H + K) {
         float sum = 0.f;
 #pragma unroll
@@ -178,7 +183,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopePar
         for (uint32_t d = kPerHead / 2u; d > 0; d >>= 1) sum += __shfl_xor_sync(mine, sum, d);
         const float r = rsqrtf(sum * (1.f / D) + p.eps);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = f[i] * r * (n < H ? wq[i] : wk[i]);
+        for (int i = 0; i < 8; ++i) f[i] = f[i] * r * w[i];
       }
     }
     if (n < H + K && (turn_a || turn_b || !known)) {
