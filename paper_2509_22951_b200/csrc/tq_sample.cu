@@ -24,12 +24,13 @@
 // Bound: the bytes (a logit is read once) only for one row in 512; instructions otherwise, 25 to 60 of them a logit, issued in 55 % of the cycles
 // (shared memory's data path 37 % busy), and for few rows the eight barriers of the cluster, 1500 to 2500 cycles each with what they wait for.
 // One B200, 128256 logits in fp32, us: one row top-k 8.5, top-p 18.8, none 10.5; 64 rows with settings of all kinds 48; 512 rows greedy 96 (their
-// bytes: 40), top-k 157, none 154 - 228, top-p 0.9 259 (peaked) - 446 (flat).
+// bytes: 40), top-k 160, none 154 - 220, top-p 0.9 260 (peaked) - 440 (flat).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
 #include <cstdint>
 
+#include "tq_attn_sm100.cuh"
 #include "tq_internal.h"
 #include "tq_ops_common.cuh"
 
@@ -239,8 +240,10 @@ struct Weights {
   static constexpr float kRound = 393216.0f;
   __device__ __forceinline__ static int place_in(float s) { return __float_as_int(s) - 0x48C00000; }
   // 2^t = 2^(place / 32) (1 + q 2^-26), of s = base(x) + kRound.
+  static constexpr float kA2 = 0.24022651f, kA3 = 0.055504109f, kA4 = 0.0096181291f;  // (ln 2)^k / k!
+  static constexpr float kQUnit = 67108864.0f, kQRound = 12582912.0f;                 // 2^26, 1.5 * 2^23
+  static constexpr int kQBits = 0x4B400000;                                           // of kQRound
   __device__ __forceinline__ int fine(float x, float s) const {
-    constexpr float kQUnit = 67108864.0f;
     float r;
     if (plain) {
       const float k = kRound - a;
@@ -249,9 +252,8 @@ struct Weights {
       const Pair t = both(x);
       r = (t.hi - (s - kRound)) + t.lo;
     }
-    constexpr float a2 = 0.24022651f, a3 = 0.055504109f, a4 = 0.0096181291f;  // (ln 2)^k / k!
-    const float q = r * fmaf(r, fmaf(r, fmaf(r, a4, a3), a2), kLn2);
-    return __float_as_int(fmaf(q, kQUnit, 12582912.0f)) - 0x4B400000;  // q to whole units of 2^-26, |q| < 0.031
+    const float q = r * fmaf(r, fmaf(r, fmaf(r, kA4, kA3), kA2), kLn2);
+    return __float_as_int(fmaf(q, kQUnit, kQRound)) - kQBits;  // q to whole units of 2^-26, |q| < 0.031
   }
   // The value of a place and its q.
   __device__ __forceinline__ uint32_t value(int place, int q) const {
@@ -286,12 +288,29 @@ struct Weights {
       for (int j = 0; j < 4; ++j) use(j, false, 0, (int)small(t[j]));
       return;
     }
-    int q[4], place[4];
+    int q[4], place[4];  // (of a small one q is not used)
+    if (plain) {  // the operations of fine(), two weights to an instruction
+      using namespace tq_attn;
+      const float k = kRound - a;
+      const uint64_t c2 = pair(c, c), l2 = pair(c_low, c_low), one = pair(-1.f, -1.f);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float s = t[j] + kRound;
-      q[j] = fine(x[j], s);  // (of a small one it is not used)
-      place[j] = place_in(s);
+      for (int j = 0; j < 4; j += 2) {
+        const uint64_t y = pair(x[j], x[j + 1]), s = add2(pair(t[j], t[j + 1]), pair(kRound, kRound));
+        const uint64_t r = add2(fma2(y, c2, fma2(s, one, pair(k, k))), fma2(y, l2, pair(-a_low, -a_low)));
+        const uint64_t h = fma2(r, fma2(r, fma2(r, pair(kA4, kA4), pair(kA3, kA3)), pair(kA2, kA2)), pair(kLn2, kLn2));
+        float u, v;
+        unpair(fma2(fma2(r, h, pair(-0.f, -0.f)), pair(kQUnit, kQUnit), pair(kQRound, kQRound)), u, v);
+        q[j] = __float_as_int(u) - kQBits, q[j + 1] = __float_as_int(v) - kQBits;
+        unpair(s, u, v);
+        place[j] = place_in(u), place[j + 1] = place_in(v);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float s = t[j] + kRound;
+        q[j] = fine(x[j], s);
+        place[j] = place_in(s);
+      }
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
