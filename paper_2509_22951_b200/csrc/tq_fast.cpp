@@ -24,6 +24,7 @@ PyObject* g_bf16 = nullptr;          // torch.bfloat16
 PyObject* g_int8 = nullptr;
 PyObject* g_f32 = nullptr;
 PyObject* g_i32 = nullptr;
+PyObject* g_new_empty = nullptr;
 PyObject* g_kwnames = nullptr;       // ("dtype", "device")
 PyObject* g_kwdtype = nullptr;       // ("dtype",)
 PyObject* g_device_attr = nullptr;   // "device"
@@ -97,6 +98,15 @@ PyObject* empty(const int64_t* shape, int ndim, PyObject* dtype, PyObject* like)
   }
   Py_XDECREF(dev);
   Py_XDECREF(size);
+  return r;
+}
+
+// A new contiguous matrix of like's type: cheaper than empty() too.
+PyObject* matrix_as(PyObject* like, int64_t rows, int64_t cols) {
+  PyObject* args[3] = {like, PyLong_FromLongLong(rows), PyLong_FromLongLong(cols)};
+  PyObject* r = args[1] && args[2] ? PyObject_VectorcallMethod(g_new_empty, args, 3 | PY_VECTORCALL_ARGUMENTS_OFFSET, nullptr) : nullptr;
+  Py_XDECREF(args[1]);
+  Py_XDECREF(args[2]);
   return r;
 }
 
@@ -461,8 +471,7 @@ PyObject* py_tree_accept(PyObject*, PyObject* const* a, Py_ssize_t count) {
   const tq_kv_cache* caches = n > 0 ? static_cast<const tq_kv_cache*>(PyLong_AsVoidPtr(a[0])) : nullptr;
   void* stream;
   if (path < 1 || path > 0x7FFFFFFF || PyErr_Occurred() || !current(device, &stream)) return none();
-  const int64_t shape[2] = {B, path};
-  PyObject* r[4] = {empty(shape, 2, g_i32, a[4]), nullptr, empty_as(a[5], nullptr), empty_as(a[5], nullptr)};
+  PyObject* r[4] = {matrix_as(a[5], B, path), nullptr, empty_as(a[5], nullptr), empty_as(a[5], nullptr)};
   r[1] = r[0] ? empty_as(r[0], nullptr) : nullptr;
   bool ok = true;
   for (int i = 0; i < 4; ++i) ok = ok && r[i] && get(r[i], o[i], -1, device);
@@ -502,10 +511,11 @@ PyObject* py_setup(PyObject*, PyObject* const* a, Py_ssize_t count) {
   g_int8 = PyObject_GetAttrString(torch, "int8");
   g_f32 = PyObject_GetAttrString(torch, "float32");
   g_i32 = PyObject_GetAttrString(torch, "int32");
+  g_new_empty = PyUnicode_InternFromString("new_empty");
   g_kwnames = Py_BuildValue("(ss)", "dtype", "device");
   g_kwdtype = Py_BuildValue("(s)", "dtype");
   g_device_attr = PyUnicode_InternFromString("device");
-  if (!g_kwdtype || !g_device || !g_empty_like || !g_empty || !g_bf16 || !g_int8 || !g_f32 || !g_i32 || !g_kwnames || !g_device_attr) {
+  if (!g_kwdtype || !g_device || !g_empty_like || !g_empty || !g_bf16 || !g_int8 || !g_f32 || !g_i32 || !g_new_empty || !g_kwnames || !g_device_attr) {
     PyErr_Clear();
     Py_RETURN_FALSE;
   }
