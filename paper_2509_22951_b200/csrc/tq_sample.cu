@@ -13,7 +13,7 @@
 //
 // A row is read once: a cluster of up to eight CTAs holds it in shared memory and speaks through distributed shared memory.  Then
 //   top-k (up to 1024): the k-th largest of the threads' own maxima is a bound of the k-th logit that few others pass: those go to one CTA,
-//          which does the rest: up to 128 tokens by comparing each with each, more by sorting;
+//          which does the rest: up to 128 tokens by comparing each with each, more by sums over parts of them;
 //   top-p alone: a histogram of the weights over 32 bins an octave (exact: two integers a bin, as many atomics; one that returns, with a carry
 //          now and then, takes as long, a 64-bit one longer) finds the bin of the border.  Where its sum is that of one token that is all;
 //          else one CTA gets the bin's tokens and finds the one with which the sum is reached: over 128 of them by a finer histogram of
@@ -23,8 +23,8 @@
 //
 // Bound: the bytes (a logit is read once) only for one row in 512; instructions otherwise, 25 to 60 of them a logit, issued in 55 % of the cycles
 // (shared memory's data path 37 % busy), and for few rows the eight barriers of the cluster, 1500 to 2500 cycles each with what they wait for.
-// One B200, 128256 logits in fp32, us: one row top-k 8.5, top-p 18.8, none 10.5; 64 rows with settings of all kinds 48; 512 rows greedy 96 (their
-// bytes: 40), top-k 160, none 154 - 220, top-p 0.9 260 (peaked) - 440 (flat).
+// One B200, 128256 logits in fp32, us: one row top-k 8.7, top-p 18.9, none 10.4; 64 rows with settings of all kinds 41; 512 rows greedy 99 (their
+// bytes: 40), top-k 165, none 159 - 225, top-p 0.9 269 (peaked) - 450 (flat).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -51,6 +51,7 @@ constexpr uint32_t kList = 2048;   // tokens that one CTA sorts
 constexpr uint32_t kListK = 1024;  // largest k of the list: the threads' maxima bound it well up to a quarter of their number
 constexpr uint32_t kKBins = 256;   // of the threads' maxima
 constexpr uint32_t kSub = 256;     // parts of the bin with the border
+constexpr uint32_t kParts = 768;   // of the list
 constexpr uint32_t kNear = 128;    // tokens that are compared each with each
 
 // 2^(i / 32) with 29 bits behind the point
@@ -103,6 +104,7 @@ struct Shared {
       uint32_t hi[kBins], lo[kBins];  // sums of the upper and lower 15 bits of the values of a bin
     } bins;
     uint32_t k_bins[kKBins];
+    unsigned long long part[kParts];        // sums of parts of the list
   };
   uint64_t list[kList];
 };
@@ -378,6 +380,91 @@ __device__ void sort_list(uint64_t* list, uint32_t n, uint32_t tid) {
   }
 }
 
+// What the drawn number asks for, below the total.
+__device__ __forceinline__ uint64_t target(float u, uint64_t total) {
+  if (!(u < 1.f)) return u >= 1.f ? total - 1u : 0ull;
+  bool more;
+  return u > 0.f ? times(u, total, more) : 0ull;
+}
+// Sums over the threads of a CTA, and what is of the threads before.
+__device__ __forceinline__ uint64_t scan_cta(Shared& sh, uint64_t sum, uint64_t& total) {
+  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+  const uint64_t upto = warp_upto(sum, lane);
+  __syncthreads();
+  if (lane == 31) sh.warps[warp] = upto;
+  __syncthreads();
+  const uint64_t w = lane < kWarps ? sh.warps[lane] : 0ull;
+  total = warp_sum(w);
+  return warp_sum(lane < warp ? w : 0ull) + upto - sum;
+}
+// The token among the list's m entries: the last of top-k, the last of top-p, then the one that the drawn number asks for (by sorting twice, 1200
+// entries take 20 us longer).  Each is the entry with which a sum reaches a bound, found by the sums of kParts parts and then each with each of the
+// part that has it; ~0 where those are more than kNear.  What is summed: 0: numbers, from the largest logit down; 1: weights of those that
+// are left, likewise; 2: these in the order of the vocabulary.  told[1] is the sum of what is kept.  (As a call it costs the other ways up to 8 %,
+// inlined 2 to 4.)
+__device__ __forceinline__ uint64_t token_of_list(Shared& sh, const Weights weight, uint32_t m, uint32_t k, float top_p, uint64_t keep, float u, float fall,
+                                               uint32_t vocab) {
+  const uint32_t tid = threadIdx.x;
+  uint64_t edge = 0;
+#pragma unroll 1
+  for (uint32_t what = 0; what < 3u; ++what) {
+    if (what == 0u ? k >= m : what == 1u && !(top_p < 1.f)) continue;
+    if (what == 2u) edge = max(edge, keep);
+    const float scale = what == 2u ? (float)kParts / (float)vocab : fall;
+    auto measure = [&](uint64_t e) { return what == 0u ? 1ull : e >= edge ? weight(logit_of(e)) : 0ull; };
+    auto part = [&](uint64_t e) { return (uint32_t)fminf((what == 2u ? (float)index_of(e) : weight.top - logit_of(e)) * scale, (float)(kParts - 1u)); };
+    auto key = [&](uint64_t e) { return what == 2u ? e & kIndexMask : e; };  // falls along the order
+    for (uint32_t i = tid; i < kParts; i += kThreads) sh.part[i] = 0ull;
+    if (tid == 0) sh.near = 0u;
+    __syncthreads();
+    for (uint32_t i = tid; i < m; i += kThreads) {
+      const uint64_t entry = sh.list[i], w = measure(entry);
+      if (w != 0ull) atomicAdd(&sh.part[part(entry)], (unsigned long long)w);
+    }
+    __syncthreads();
+    uint64_t mass[2], total;
+#pragma unroll
+    for (uint32_t z = 0; z < 2u; ++z) mass[z] = 2u * tid + z < kParts ? sh.part[2u * tid + z] : 0ull;
+    uint64_t prev = scan_cta(sh, mass[0] + mass[1], total);
+    const uint64_t bound = what == 0u ? (uint64_t)k : what == 1u ? bound_of(top_p, total) : target(u, total) + 1ull;
+#pragma unroll
+    for (uint32_t z = 0; z < 2u; ++z) {
+      if (prev < bound && prev + mass[z] >= bound) {
+        sh.told[0] = 2u * tid + z;
+        sh.told[1] = prev;
+      }
+      prev += mass[z];
+    }
+    __syncthreads();
+    const uint32_t chosen = (uint32_t)sh.told[0];
+    const uint64_t ahead = sh.told[1];
+    for (uint32_t i = tid; i < m; i += kThreads) {
+      const uint64_t entry = sh.list[i];
+      if (part(entry) != chosen) continue;
+      const uint64_t w = measure(entry);
+      if (w == 0ull) continue;
+      const uint32_t at = atomicAdd(&sh.near, 1u);
+      if (at >= kNear) continue;
+      sh.close[at] = entry;
+      sh.close_w[at] = w;
+    }
+    __syncthreads();
+    const uint32_t near = sh.near, j = tid / 4u;
+    if (near > kNear) return ~0ull;
+    const uint64_t entry = j < near ? sh.close[j] : 0ull, mine = key(entry);
+    uint64_t at = 0;
+    for (uint32_t i = tid % 4u; i < near; i += 4u) at += key(sh.close[i]) > mine ? sh.close_w[i] : 0ull;
+    at += __shfl_xor_sync(kFull, at, 1);
+    at += __shfl_xor_sync(kFull, at, 2);
+    at += ahead;
+    if (j < near && tid % 4u == 0u && at < bound && at + sh.close_w[j] >= bound) sh.told[0] = entry;
+    if (tid == 0) sh.told[1] = total;
+    __syncthreads();
+    edge = sh.told[0];
+  }
+  return edge;
+}
+
 template <int TYPE>
 __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams p) {
   extern __shared__ __align__(16) uint8_t smem[];
@@ -592,11 +679,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     keep = sh.told[1] << kIndexBits;
     __syncthreads();
   }
-  auto target_of = [&](uint64_t total) {
-    if (!(u < 1.f)) return u >= 1.f ? total - 1u : 0ull;
-    bool more;
-    return u > 0.f ? times(u, total, more) : 0ull;  // below the total
-  };
+  auto target_of = [&](uint64_t total) { return target(u, total); };
   auto answer = [&](uint64_t order, uint64_t total) {
     p.token[row] = (int32_t)index_of(order);
     if (p.logprob) {  // ln 2 (t - log2(total / 2^45))
@@ -630,16 +713,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     __syncwarp();
   };
   constexpr uint32_t kEach = kList / kThreads;  // consecutive entries of the list to a thread
-  // Sums over the threads of a CTA, and what is of the threads before.
-  auto scan = [&](uint64_t sum, uint64_t& total) {
-    const uint64_t upto = warp_upto(sum, lane);
-    __syncthreads();
-    if (lane == 31) sh.warps[warp] = upto;
-    __syncthreads();
-    const uint64_t w = lane < kWarps ? sh.warps[lane] : 0ull;
-    total = warp_sum(w);
-    return warp_sum(lane < warp ? w : 0ull) + upto - sum;
-  };
+  auto scan = [&](uint64_t sum, uint64_t& total) { return scan_cta(sh, sum, total); };
 
   // Bisection of the order: the last place before which less than `bound` (a weight, or a number) lies.
   auto before = [&](uint64_t order, bool count) {
@@ -743,7 +817,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     }
   };
   // The filters and the token of at most kNear listed ones by comparing each with each, four threads to a token: three steps of the CTA,
-  // where sorting by order and by place takes some thirty (one row 10.1 us with that, 8.5 with this).
+  // where sorting by order and by place takes some thirty (one row 10.1 us with that, 8.7 with this).
   auto few_in_list = [&](uint32_t m, uint32_t k, uint64_t keep) {
     const uint32_t j = tid / 4u, part = tid % 4u;
     const uint64_t order = j < m ? sh.list[j] : 0ull, own = j < m ? weight(logit_of(order)) : 0ull;
@@ -837,6 +911,12 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
       if (rank != 0) return;
       if (m <= kNear) {
         few_in_list(m, k, keep);
+        cluster_wait();
+        return;
+      }
+      const uint64_t found = token_of_list(sh, weight, m, k, top_p, keep, u, scale * ((float)kParts / fminf(end, 2.f * (float)kKBins)), p.vocab);
+      if (found != ~0ull) {
+        if (tid == 0) answer(found, sh.told[1]);
         cluster_wait();
         return;
       }

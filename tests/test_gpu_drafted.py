@@ -566,6 +566,22 @@ def test_sample_where_the_border_is_crowded(tq, vocab, scale):
     sample_case(tq, x, u, top_p=p)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("scale", [0.5, 3.0])
+def test_sample_of_the_first_hundreds(tq, dtype, scale):
+    """Lists of more than 128 tokens: distinct logits, and (16 bits) groups of equals that no part of the list holds."""
+    g, R = gen(int(scale * 10)), 12
+    x, u = randn(g, R, 60000, dtype=dtype, scale=scale), torch.rand(R, generator=g, device="cuda")
+    k, last = i32([129, 200, 300, 500, 700, 900, 1000, 1023, 1024, 150, 400, 600]), torch.full((R,), 1.0 - 2.0 ** -24, device="cuda")
+    p, t = f32([0.1, 0.3, 0.5, 0.7, 0.9, 0.95, 0.99, 0.999, 1.0, 0.9, 0.9, 0.9]), f32([0.3, 1.0, 2.0] * 4)
+    for v in (u, last, u * 0):
+        sample_case(tq, x, v, top_k=k, temperature=t)
+        sample_case(tq, x, v, top_k=k, top_p=p)
+        sample_case(tq, x, v, top_k=k, top_p=p, min_p=f32([0.0, 0.01, 0.3] * 4), temperature=t)
+    x[:, ::60] = x.amax() + 1  # a thousand equals at the head
+    sample_case(tq, x, u, top_k=k, top_p=p)
+
+
 def test_sample_of_what_is_not_finite(tq):
     g, V = gen(31), 20000
     x = logits(g, 12, V)
