@@ -66,6 +66,7 @@ constexpr int kTreeThreads = 512;
 // checks the kernel's own count: a split above it would wait for ever.
 constexpr int kSoftRegs = 192, kOtherRegs = 64;
 constexpr uint32_t kTmemCols = 512;
+constexpr uint32_t kMlSets = 2;    // sets of the rows' maxima and sums that the two halves exchange at a group's end, used in turn
 constexpr uint32_t kThere = 16;    // tiles whose words of present states are kept: more than loads run ahead of the softmax
 constexpr uint32_t kWideRows = 129;  // rows of a sequence, on average, from which on tiles have 256
 constexpr float kRescale = 8.0f;   // log2 of how far p may exceed 1
@@ -114,7 +115,7 @@ struct TreeSmem {
   static constexpr uint32_t kOffPlan = (kBarMl + 8 + 15) / 16 * 16;
   static constexpr uint32_t kOffThere = kOffPlan + 96;
   static constexpr uint32_t kOffMl = kOffThere + kThere * 16;
-  static constexpr uint32_t kTotal = kOffMisc + kOffMl + 2 * kRows * 8;
+  static constexpr uint32_t kTotal = kOffMisc + kOffMl + (WIDE ? 0 : kMlSets * 2 * kRows * 8);
   static_assert(kTotal <= 232448, "shared memory of one CTA");
 };
 // a part of a cut group: [D / 4][128] float4 of output, then the rows' maxima and sums; two of them in a row where tiles have 256 rows
@@ -908,7 +909,11 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         }
         if (!ok) break;
         // ---- end of the group, or of this CTA's part of it: the two halves of the states become one ---------------
-        s_ml[w * kRows + row_in] = make_float2(m, l);
+        // Two sets, in turn.  A warp is a group ahead of its partner at most: the next tile's scores wait for the product before the last, not for the
+        // partner's reading of this group, so where the next group has one or two tiles here it may write its entries while the partner still reads
+        // these.  Two groups ahead it cannot be: the wait below, of the group between, is for the partner's arrival, which follows its reading.
+        float2* const ml = s_ml + groups % kMlSets * 2u * kRows;
+        ml[w * kRows + row_in] = make_float2(m, l);
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(L::kBarMl, 0));
         wait(bar(L::kBarODone, (count - 1u) & 1u), ((count - 1u) >> 1) & 1u);
@@ -919,7 +924,8 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
       tmem_fence_after();
       float M = m, fa = 1.f, fb = 0.f, sum = l;
       if constexpr (!WIDE) {
-        const float2 a = s_ml[row_in], b = s_ml[kRows + row_in];
+        const float2* const ml = s_ml + groups % kMlSets * 2u * kRows;
+        const float2 a = ml[row_in], b = ml[kRows + row_in];
         M = fmaxf(a.x, b.x);
         const float ref = M == -INFINITY ? 0.f : M;
         fa = exp2_fast(a.x - ref), fb = exp2_fast(b.x - ref), sum = a.y * fa + b.y * fb;
