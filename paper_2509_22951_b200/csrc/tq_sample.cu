@@ -238,9 +238,12 @@ struct Weights {
     const float t = d.hi * c;
     return Pair{t, fmaf(d.lo, c, fmaf(d.hi, c_low, fmaf(d.hi, c, -t)))};
   }
-  // 32 t rounded, of a sum s of t with 1.5 * 2^18, which is rounded to 1/32; from some octaves below the histogram's on, something as low.
-  static constexpr float kRound = 393216.0f;
-  __device__ __forceinline__ static int place_in(float s) { return __float_as_int(s) - 0x48C00000; }
+  // A sum s of t with 1.5 * 2^18 is rounded to 1/32.  Below the histogram's octaves a weight is small, and that is told from s itself: below 2^18
+  // (t < -131072: a mask of -65504 at a temperature of 0.2) its bits say nothing of t, and taken for a place they could be any.
+  static constexpr float kRound = 393216.0f, kLeastSum = kRound - (float)kOctaves;
+  __device__ __forceinline__ static bool is_small(float s) { return s < kLeastSum; }
+  // 32 t rounded, of the sum of a weight that is not small.
+  __device__ __forceinline__ static int place_in(float s) { return (int)(__float_as_uint(s) - 0x48C00000u); }
   // 2^t = 2^(place / 32) (1 + q 2^-26), of s = base(x) + kRound.
   static constexpr float kA2 = 0.24022651f, kA3 = 0.055504109f, kA4 = 0.0096181291f;  // (ln 2)^k / k!
   static constexpr float kQUnit = 67108864.0f, kQRound = 12582912.0f;                 // 2^26, 1.5 * 2^23
@@ -270,12 +273,10 @@ struct Weights {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(w) : "f"(base + to_small));
     return __float_as_uint(w + 8388608.0f) - 0x4B000000u;  // rounded
   }
-  // Below the octaves of the histogram a weight is small.
-  static constexpr int kLeastPlace = -32 * kOctaves;
   __device__ __forceinline__ uint64_t operator()(float x) const {
     const float t = base(x), s = t + kRound;
+    if (is_small(s)) return small(t);
     const int place = place_in(s);
-    if (place < kLeastPlace) return small(t);
     return (uint64_t)value(place, fine(x, s)) << shift(place);
   }
   // Four at once, for a whole warp: the chains of fine() side by side, or none of them where all weights are small.  use(j, is fine, place, q)
@@ -285,12 +286,13 @@ struct Weights {
     float t[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) t[j] = base(x[j]);
-    if (!__any_sync(kFull, place_in(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) + kRound) >= kLeastPlace)) {
+    if (!__any_sync(kFull, !is_small(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) + kRound))) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) use(j, false, 0, (int)small(t[j]));
       return;
     }
-    int q[4], place[4];  // (of a small one q is not used)
+    int q[4];  // (of a small one it is not used)
+    float sums[4];
     if (plain) {  // the operations of fine(), two weights to an instruction
       using namespace tq_attn;
       const float k = kRound - a;
@@ -303,21 +305,19 @@ struct Weights {
         float u, v;
         unpair(fma2(fma2(r, h, pair(-0.f, -0.f)), pair(kQUnit, kQUnit), pair(kQRound, kQRound)), u, v);
         q[j] = __float_as_int(u) - kQBits, q[j + 1] = __float_as_int(v) - kQBits;
-        unpair(s, u, v);
-        place[j] = place_in(u), place[j + 1] = place_in(v);
+        unpair(s, sums[j], sums[j + 1]);
       }
     } else {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float s = t[j] + kRound;
-        q[j] = fine(x[j], s);
-        place[j] = place_in(s);
+        sums[j] = t[j] + kRound;
+        q[j] = fine(x[j], sums[j]);
       }
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const bool is_small = place[j] < kLeastPlace;
-      use(j, !is_small, place[j], is_small ? (int)small(t[j]) : q[j]);
+      const bool low = is_small(sums[j]);
+      use(j, !low, place_in(sums[j]), low ? (int)small(t[j]) : q[j]);
     }
   }
 };
@@ -1100,11 +1100,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     keep_place = (int)border_bin;
   } else if (coded) {
     const float s = weight.base(keep_x) + Weights::kRound;
-    const int place = Weights::place_in(s);
     keep_place = (int)kSmallPlace;
     edge_near = 1 << 24;  // small ones: always by the logit
-    if (keep_x > -INFINITY && place >= Weights::kLeastPlace) {
-      keep_place = kTopPlace - place;
+    if (keep_x > -INFINITY && !Weights::is_small(s)) {
+      keep_place = kTopPlace - Weights::place_in(s);
       edge_q = weight.fine(keep_x, s);
       edge_near = 2;
     }
