@@ -870,8 +870,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
 
   if (k != 0u && k <= kListK) {
     // ---- top-k: a bound from the threads' maxima, and a list -----------------------------------------------
-    // bins that fall with x from the largest logit to the least of the maxima; what is below is in the last
-    const float span = top - least, scale = span > 0.f && span < INFINITY ? (float)(kKBins - 1u) / span : 0.f;
+    // bins that fall with x from the largest logit to the least of the maxima; what is below is in the last.  One bin where a bin's width would be
+    // 0, infinite, or so small that bins to a unit are (a span below 7.5e-37).
+    const float span = top - least, per = (float)(kKBins - 1u) / span, scale = span > 0.f && per < INFINITY ? per : 0.f;
     auto bin_at = [&](float x) { return min((uint32_t)((top - x) * scale), kKBins - 1u); };
     if (mine > -INFINITY) atomicAdd(&sh.k_bins[bin_at(mine)], 1u);
     cluster_sync();
@@ -890,8 +891,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     if (ahead < k && ahead + in_bin >= k) sh.told[0] = tid;
     cluster_sync();
     const uint32_t cut = (uint32_t)sh.told[0];
-    // the products of bin_at, compared with the bin's end; where all are alike, or in the last bin, everything is listed
-    const float end = cut == kKBins - 1u || scale == 0.f ? INFINITY : (float)(cut + 1u);
+    // the products of bin_at, compared with the bin's end; where all are alike, or in the last bin, everything is listed, whatever its product
+    // (infinite, or 0 times that)
+    const bool everything = cut == kKBins - 1u || scale == 0.f;
+    const float end = everything ? INFINITY : (float)(cut + 1u);
 #pragma unroll
     for (uint32_t b = 0; b < kBlocks; ++b) {
       for (uint32_t s = 0; s < 8u && w0 + b * 1024u + s * 128u < w1; ++s) {
@@ -899,7 +902,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
         read4(w0 + b * 1024u + s * 128u + 4u * lane, w1, x);
         uint32_t mask = 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) mask |= x[j] > -INFINITY && (top - x[j]) * scale < end ? 1u << j : 0u;
+        for (int j = 0; j < 4; ++j) mask |= x[j] > -INFINITY && (everything || (top - x[j]) * scale < end) ? 1u << j : 0u;
         hits[b] |= mask << (4u * s);
       }
     }
