@@ -386,11 +386,8 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
     while (f_any && ok) {
       const uint32_t kvh = f_kvh, slot = f_slot, valid = f_valid;
       const int32_t page = f_page;
-      bool live = f_live;
-      if (live && (uint32_t)page >= p.n_pages) {
-        live = false;
-        bad = true;
-      }
+      const bool live = f_live && (uint32_t)page < p.n_pages, absent = f_live && !live;
+      bad = bad || absent;
       fetch();
       const uint32_t there = __ballot_sync(kFull, live);
       if (warp == kLoadWarp && lane < 4u) {  // states that are there, 32 to a word
@@ -409,6 +406,15 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
       const uint32_t slab = L::kSlabs == 2u ? part : 0u;
       const uint32_t full = bar(bar_full, st), dst = smem0 + offset + st * L::kTileBytes + slab * kStates * 128u + lane * p.box * 128u;
       const uint32_t bytes = (uint32_t)__popc(__ballot_sync(kFull, mine)) * p.box * 128u;
+      // a box on a page outside the pool: zeros, for values (0 x what the stage held before may be NaN; scores are hidden whatever they are)
+      uint32_t gone = values ? __ballot_sync(kFull, L::kSlabs == 2u ? absent : absent && (lane & 1u) == part) : 0u;
+      if (gone) {
+        for (; gone; gone &= gone - 1u) {
+          uint8_t* const box = smem + offset + st * L::kTileBytes + slab * kStates * 128u + (__ffs(gone) - 1u) * p.box * 128u;
+          for (uint32_t i = lane; i < p.box * 8u; i += 32u) reinterpret_cast<uint4*>(box)[i] = make_uint4(0u, 0u, 0u, 0u);
+        }
+        copies_fence();
+      }
       __syncwarp();  // the words of present states are written
       if (lane == 0) mbar_expect_tx(full, bytes);
       __syncwarp();

@@ -1,17 +1,27 @@
 """The operators of a decode step with drafted tokens where their inputs are unusual.  References, helpers and what is not said here of
 bounds are those of test_gpu_drafted.py."""
+import math
+
 import pytest
 import torch
 
-from test_gpu_drafted import f32, gen, i32, logits, randn, sample_case
+from test_gpu_drafted import BF, attend_ref, f32, gen, i32, logits, randn, sample_case, within
 
 pytestmark = pytest.mark.gpu
+INF, NAN = math.inf, math.nan
 
 
 @pytest.fixture(scope="module")
 def tq():
     from paper_2509_22951_b200 import binding
     return binding
+
+
+@pytest.fixture(scope="module")
+def ws(tq):
+    w = tq.tq_attn_workspace()
+    yield w
+    assert tq.tq_attn_status(w) == 0
 
 
 # ------------------------------------------------------------------------------------------------ sampling
@@ -57,3 +67,34 @@ def test_top_k_of_logits_next_to_one_another(tq):
         v = f32([0.1, 0.5, 0.9, 1.0 - 2.0 ** -24])
         sample_case(tq, y, v, top_k=i32([V // 4 + 50] * 4), temperature=f32([1e30] * 4))
         sample_case(tq, y, v, top_k=i32([V - 1] * 4), temperature=f32([1e30] * 4))
+
+
+# ------------------------------------------------------------------------------------------------ attention
+@pytest.mark.parametrize("D,H,n", [(64, 4, 5), (128, 4, 5), (64, 16, 40), (128, 16, 40)])  # tiles of 128 rows and of 256
+@pytest.mark.parametrize("page", [16, 20])  # tensor copies, copies row by row
+def test_pages_outside_the_pool_are_zeros(tq, ws, D, H, n, page):
+    """What is multiplied with p = 0 in their place does not come from what the multiprocessor had before: the same bits after values of all kinds."""
+    g, K = gen(D + n + page), 2
+    P = 320 // page
+    kp, vp = randn(g, P, K, page, D, dtype=BF), randn(g, P, K, page, D, dtype=BF)
+    cache, q = tq.tq_kv_cache(kp, vp), randn(g, n, H, D, dtype=BF)
+    table = torch.arange(P, device="cuda", dtype=torch.int32)[None].contiguous()
+    table[0, [1, 7, 9]] = i32([-1, P, 2 ** 31 - 1])
+    args = (q, cache, table, i32([0, n]), i32([300]), ws)
+    # every stage of every multiprocessor
+    B = 400
+    dirty = [tq.tq_kv_cache(torch.zeros_like(kp), torch.full_like(vp, v)) for v in (0.0, INF, NAN)]
+    many = torch.arange(P, device="cuda", dtype=torch.int32).expand(B, -1).contiguous()
+    got = []
+    for d in dirty:
+        tq.tq_tree_attention(torch.zeros(B * n, H, D, dtype=BF, device="cuda"), d, many, i32([n * b for b in range(B + 1)]), i32([320] * B), ws)
+        got.append(tq.tq_tree_attention(*args))
+    assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
+    assert tq.tq_kv_cache_status(cache) == tq.TQ_STATUS_BAD_PAGE
+    there = torch.ones(P, page, dtype=torch.bool, device="cuda")
+    there[[1, 7, 9]] = False
+    seen = (there.flatten()[:300] & torch.ones(n, 300, dtype=torch.bool, device="cuda").tril(300 - n))
+    for h in range(H):
+        k, v = (x[:, h // (H // K)].reshape(-1, D)[:300] for x in (kp, vp))
+        want, _, bound = attend_ref(q[:, h], k, v, seen, D ** -0.5)
+        within(got[0][:, h], want, bound)
