@@ -891,10 +891,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     if (ahead < k && ahead + in_bin >= k) sh.told[0] = tid;
     cluster_sync();
     const uint32_t cut = (uint32_t)sh.told[0];
-    // the products of bin_at, compared with the bin's end; where all are alike, or in the last bin, everything is listed, whatever its product
-    // (infinite, or 0 times that)
-    const bool everything = cut == kKBins - 1u || scale == 0.f;
-    const float end = everything ? INFINITY : (float)(cut + 1u);
+    // the products of bin_at, compared with the bin's end; where all are alike, or in the last bin, everything is listed: the products are then with 0,
+    // which is not beyond the end even where the distance is infinite (a choice beside the comparison: one row 11.3 us, so 10.3, in a graph)
+    const float end = cut == kKBins - 1u || scale == 0.f ? INFINITY : (float)(cut + 1u), by = end < INFINITY ? scale : 0.f;
 #pragma unroll
     for (uint32_t b = 0; b < kBlocks; ++b) {
       for (uint32_t s = 0; s < 8u && w0 + b * 1024u + s * 128u < w1; ++s) {
@@ -902,7 +901,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
         read4(w0 + b * 1024u + s * 128u + 4u * lane, w1, x);
         uint32_t mask = 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) mask |= x[j] > -INFINITY && (everything || (top - x[j]) * scale < end) ? 1u << j : 0u;
+        for (int j = 0; j < 4; ++j) mask |= x[j] > -INFINITY && !((top - x[j]) * by >= end) ? 1u << j : 0u;
         hits[b] |= mask << (4u * s);
       }
     }
