@@ -908,7 +908,7 @@ def tq_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, table: tor
 
 
 class AttnWorkspace:
-    """Workspace of tq_paged_attention and tq_cross_attention: one for each stream that makes such calls."""
+    """Workspace of tq_paged_attention, tq_cross_attention and tq_tree_attention: one for each stream that makes such calls."""
 
     def __init__(self, buf: torch.Tensor):
         self.buf = buf

@@ -548,8 +548,8 @@ extern "C" {
 int tq_attn_workspace_size(uint64_t* device_bytes) {
   if (!device_bytes) return TQ_ERR_INVALID_ARG;
   const uint64_t ctas = min((uint32_t)sm_count(), kAttnMaxCtas);
-  const uint64_t split = ctas * 2u * kPartFloats * sizeof(float), cross = tq_cross_workspace_bytes();
-  *device_bytes = kAttnWsHeader + (split > cross ? split : cross);
+  const uint64_t split = ctas * 2u * kPartFloats * sizeof(float), cross = tq_cross_workspace_bytes(), tree = tq_tree_workspace_bytes();
+  *device_bytes = kAttnWsHeader + max(max(split, cross), tree);
   return TQ_OK;
 }
 

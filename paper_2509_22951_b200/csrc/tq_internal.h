@@ -248,6 +248,8 @@ struct tq_attn_ws {
 constexpr uint64_t kAttnWsOpen = kAttnMaxCtas * 4 + 256, kAttnWsHeader = kAttnWsOpen + kAttnMaxCtas * 16;
 // nullptr counters: d_ws is not usable as a workspace of ws_bytes bytes
 tq_attn_ws tq_attn_ws_plan(void* d_ws, uint64_t ws_bytes);
+// What the parts of tq_tree_attention (tq_tree.cu) want of it.
+uint64_t tq_tree_workspace_bytes();
 
 // The tensor-core form of tq_cross_attention (tq_cross.cu): *served is false, and nothing was launched, if the states
 // cannot be described by a tensor map (strides of 2^40 bytes and more, no states) or there are 2^32 and more pieces of work.

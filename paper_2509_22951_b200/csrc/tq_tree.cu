@@ -1158,6 +1158,9 @@ bool misaligned(const void* ptr, uintptr_t align) { return ptr == nullptr || ((u
 
 }  // namespace
 
+// two parts a CTA, of 256 rows
+uint64_t tq_tree_workspace_bytes() { return (uint64_t)min((uint32_t)sm_count(), kAttnMaxCtas) * 2u * 2u * kTreePartFloats * sizeof(float); }
+
 extern "C" int tq_tree_attention(const tq_kv_cache* cache, const void* d_q, int64_t q_stride, uint32_t n_tokens, uint32_t n_seqs,
                                  uint32_t n_q_heads, const int32_t* d_first, const int32_t* d_page_table, uint32_t max_pages,
                                  const int32_t* d_lens, const uint32_t* d_mask, uint32_t mask_words, float scale, void* d_out,

@@ -1,0 +1,14 @@
+"""What the calls of a decode step with drafted tokens say without a GPU."""
+import re
+from pathlib import Path
+
+CSRC = Path(__file__).resolve().parent.parent / "paper_2509_22951_b200" / "csrc"
+
+
+def test_the_workspace_knows_its_callers():
+    """Every kernel that leaves parts in the workspace has its need in tq_attn_workspace_size."""
+    size = re.search(r"int tq_attn_workspace_size\(.*?\n}", (CSRC / "tq_attn.cu").read_text(), re.S).group(0)
+    users = [f for f in CSRC.glob("*.cu") if "ws.parts +" in f.read_text()]
+    assert len(users) == 3
+    for f in users:
+        assert f.name == "tq_attn.cu" or f"{f.stem}_workspace_bytes()" in size, f.name

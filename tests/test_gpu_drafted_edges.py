@@ -98,3 +98,19 @@ def test_pages_outside_the_pool_are_zeros(tq, ws, D, H, n, page):
         k, v = (x[:, h // (H // K)].reshape(-1, D)[:300] for x in (kp, vp))
         want, _, bound = attend_ref(q[:, h], k, v, seen, D ** -0.5)
         within(got[0][:, h], want, bound)
+
+
+@pytest.mark.parametrize("D,H,n,length", [(128, 32, 40, 9000), (64, 32, 40, 9000), (128, 8, 3, 20000)])
+def test_a_workspace_of_the_stated_size_is_enough(tq, D, H, n, length):
+    """Parts of cut groups of both forms: nothing behind the workspace's stated size is written."""
+    g, K, page = gen(length), 8, 32
+    P = -(-length // page)
+    cache = tq.tq_kv_cache(randn(g, P, K, page, D, dtype=BF), randn(g, P, K, page, D, dtype=BF))
+    w = tq.tq_attn_workspace()
+    room = torch.full((w.bytes + (1 << 20),), 0x5A, dtype=torch.uint8, device="cuda")
+    room[:w.bytes] = 0
+    assert room.data_ptr() % 256 == 0
+    w.ptr = room.data_ptr()
+    q, table = randn(g, n, H, D, dtype=BF), torch.arange(P, device="cuda", dtype=torch.int32)[None].contiguous()
+    out = tq.tq_tree_attention(q, cache, table, i32([0, n]), i32([length]), w)
+    assert bool(out.isfinite().all()) and bool((room[w.bytes:] == 0x5A).all())
