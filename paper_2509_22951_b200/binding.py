@@ -1023,6 +1023,12 @@ def _like(x: torch.Tensor, device: int, dtype, *shape) -> int:
     return x.data_ptr()
 
 
+def _count(x: torch.Tensor, device: int, dtype, n: int) -> int:
+    """Likewise, of a contiguous tensor of n elements, whatever its shape."""
+    assert x.get_device() == device and x.dtype == dtype and x.is_contiguous() and x.numel() == n, f"{n} elements of {dtype} on device {device} are wanted"
+    return x.data_ptr()
+
+
 def tq_qk_norm_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_weight: torch.Tensor, k_weight: torch.Tensor,
                            table: torch.Tensor, positions: torch.Tensor, slots: torch.Tensor, cache: KvCache, eps: float = 1e-5,
                            sections=None, interleaved: bool = False, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
@@ -1079,7 +1085,7 @@ def tq_sample(logits: torch.Tensor, uniform: torch.Tensor, temperature: torch.Te
               top_p: torch.Tensor | None = None, min_p: torch.Tensor | None = None, out: torch.Tensor | None = None,
               logprob: torch.Tensor | bool | None = None, stream=None):
     """logits: CUDA bf16 or fp32 [rows][vocab] (rows may be strided); uniform: fp32 [rows] in [0, 1); temperature, top_p, min_p: fp32
-    [rows]; top_k: int32 [rows].  -> int32 [rows] tokens; with logprob (True, or the fp32 [rows] tensor to fill) also their logarithms."""
+    [rows] or of another shape with as many elements; top_k: int32, likewise.  -> int32 [rows] tokens; with logprob (True, or the fp32 [rows] tensor to fill) also their logarithms."""
     if stream is None and out is None and (logprob is None or isinstance(logprob, bool)) and _fast is not None:
         r = _fast.sample(logits, uniform, temperature, top_k, top_p, min_p, logprob is True)
         if r is not None:
@@ -1092,7 +1098,7 @@ def tq_sample(logits: torch.Tensor, uniform: torch.Tensor, temperature: torch.Te
     (R, V), stride = logits.shape, logits.stride()
     assert logits.dtype in _TYPES and (stride[1] == 1 or V == 1)
     u = _like(uniform, device, torch.float32, R)
-    t, k, p, m = (None if x is None else _like(x, device, dt, R) for x, dt in
+    t, k, p, m = (None if x is None else _count(x, device, dt, R) for x, dt in
                   ((temperature, torch.float32), (top_k, torch.int32), (top_p, torch.float32), (min_p, torch.float32)))
     if out is None:
         out = torch.empty(R, dtype=torch.int32, device=logits.device)
@@ -1144,7 +1150,7 @@ def tq_tree_accept(caches: KvCaches | None, page_table: torch.Tensor | None, fir
     B, T = first.numel() - 1, tokens.numel()
     assert max_path >= 1
     f, length = _like(first, device, torch.int32, B + 1), _like(lens, device, torch.int32, B)
-    rows = [_like(x, device, torch.int32, T) for x in (tokens, parents, sampled)]
+    rows = [_like(tokens, device, torch.int32, T), *(_count(x, device, torch.int32, T) for x in (parents, sampled))]
     max_pages = page_table.shape[1] if n else 0
     table = _like(page_table, device, torch.int32, B, max_pages) if n else None
     both = torch.empty((2, B, max_path), dtype=torch.int32, device=first.device)

@@ -114,3 +114,25 @@ def test_a_workspace_of_the_stated_size_is_enough(tq, D, H, n, length):
     q, table = randn(g, n, H, D, dtype=BF), torch.arange(P, device="cuda", dtype=torch.int32)[None].contiguous()
     out = tq.tq_tree_attention(q, cache, table, i32([0, n]), i32([length]), w)
     assert bool(out.isfinite().all()) and bool((room[w.bytes:] == 0x5A).all())
+
+
+# ------------------------------------------------------------------------------------------------ the binding
+def test_settings_of_any_shape(tq, monkeypatch):
+    """A setting is `rows` numbers one behind the other, in whatever shape, for both forms of a call."""
+    g, R, V = gen(72), 6, 3000
+    x, u = randn(g, R, V, scale=3), torch.rand(R, generator=g, device="cuda")
+    kw = dict(temperature=f32([0.7] * R), top_k=i32([40] * R), top_p=f32([0.9] * R), min_p=f32([0.01] * R))
+    first, lens, tokens, parents, sampled = i32([0, 4, 6]), i32([40, 20]), i32([1, 2, 3, 4, 5, 6]), i32([-1, 0, 1, 0, -1, 0]), i32([2, 3, 4, 4, 6, 6])
+    want, path = tq.tq_sample(x, u, **kw), tq.tq_tree_accept(None, None, first, lens, tokens, parents, sampled, 3)
+    for form in (tq._fast, None):
+        monkeypatch.setattr(tq, "_fast", form)
+        for shape in ((R, 1), (1, R), (2, 3)):
+            other = {n: v.view(shape) for n, v in kw.items()}
+            assert torch.equal(tq.tq_sample(x, u, **other), want)
+            assert torch.equal(tq.tq_sample(x, u, out=torch.empty_like(want), **other), want)
+            assert torch.equal(tq.tq_sample(x, u, logprob=torch.empty(R, device="cuda"), **other)[0], want)
+        got = tq.tq_tree_accept(None, None, first, lens, tokens, parents.view(6, 1), sampled.view(2, 3), 3)
+        assert all(torch.equal(a, b) for a, b in zip(got, path))
+        for bad in (u[:5], x[0, :12].view(6, 2), u.view(R, 1).expand(R, 2)):
+            with pytest.raises(AssertionError):
+                tq.tq_sample(x, u, temperature=bad)
