@@ -551,7 +551,7 @@ int tq_qk_norm_rope_append(const void* d_q, const void* d_k, const void* d_v, in
  * d_q: DEVICE bf16, n_tokens rows of [n_q_heads][head_dim], q_stride elements from row to row (multiple of 8), 16-byte aligned.
  * Page table, lengths, workspace and status are those of tq_paged_attention, d_out bf16 [n_tokens][n_q_heads][head_dim],
  * d_lse fp32 [n_tokens][n_q_heads] or NULL.  Fewer states than new tokens (lens[b] < n): the first ones have none.
- * TQ_ERR_UNSUPPORTED_SHAPE where n_tokens x n_q_heads reaches 2^31 or tiles of 128 rows x key-value heads x tiles of 128 states 2^32. */
+ * TQ_ERR_UNSUPPORTED_SHAPE where n_tokens x n_q_heads reaches 2^31 or tiles of 128 rows x key-value heads x (tiles of 128 states + 4) 2^32. */
 int tq_tree_attention(const tq_kv_cache* cache, const void* d_q, int64_t q_stride, uint32_t n_tokens, uint32_t n_seqs,
                       uint32_t n_q_heads, const int32_t* d_first, const int32_t* d_page_table, uint32_t max_pages,
                       const int32_t* d_lens, const uint32_t* d_mask, uint32_t mask_words, float scale, void* d_out,

@@ -264,6 +264,7 @@ __device__ __forceinline__ Plan make_plan(const TreeParams& p, uint32_t lane) {
   u = __shfl_sync(kFull, u, owner);
   if (u == 0u || w.b >= p.n_seqs) return r;  // only rows that overlap (first not rising) get here
   w.kvh = (r.u0 - at) / u;
+  if (w.kvh >= p.n_kv_heads) return r;  // likewise: their units may have passed 32 bits
   w.unit = at + w.kvh * u;
   w.rt = 0;
   w.enter(p);
@@ -1169,8 +1170,10 @@ extern "C" int tq_tree_attention(const tq_kv_cache* cache, const void* d_q, int6
   if (n_q_heads == 0 || n_q_heads % cache->n_kv_heads || q_stride % 8 || max_pages == 0 || !(scale > 0.f && scale < INFINITY) || (d_mask && mask_words == 0)) return TQ_ERR_INVALID_ARG;
   if (n_q_heads > 65536u || n_tokens > 0x7FFFFFFFu || n_seqs > 0x7FFFFFFEu || (uint64_t)n_tokens * n_q_heads > 0x7FFFFFFFull) return TQ_ERR_UNSUPPORTED_SHAPE;
   const uint64_t group = n_q_heads / cache->n_kv_heads, states = (uint64_t)max_pages * cache->page_size;
-  const uint64_t tiles = (states < 0x7FFFFFFFull ? states : 0x7FFFFFFFull) / 128u + 1u, row_tiles = ((uint64_t)n_tokens * group + 127u) / 128u + n_seqs;
-  if (row_tiles > 0xFFFFFFFFull / cache->n_kv_heads / tiles) return TQ_ERR_UNSUPPORTED_SHAPE;
+  // units of work are counted in 32 bits: those of a group are its tiles of states and kGroupUnits; a sequence without rows has no group
+  const uint64_t units = (states < 0x7FFFFFFFull ? states : 0x7FFFFFFFull) / 128u + 1u + kGroupUnits;
+  const uint64_t row_tiles = ((uint64_t)n_tokens * group + 127u) / 128u + min(n_seqs, n_tokens);
+  if (row_tiles > 0xFFFFFFFFull / cache->n_kv_heads / units) return TQ_ERR_UNSUPPORTED_SHAPE;
   if (n_seqs == 0 || n_tokens == 0) return TQ_OK;
   if (misaligned(d_q, 16) || misaligned(d_first, 4) || misaligned(d_page_table, 4) || misaligned(d_lens, 4) || ((uintptr_t)d_mask & 3u) || misaligned(d_out, 16) ||
       ((uintptr_t)d_lse & 3u) || misaligned(d_ws, 256))

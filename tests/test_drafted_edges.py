@@ -2,6 +2,8 @@
 import re
 from pathlib import Path
 
+from test_drafted_args import _cache, _tree
+
 CSRC = Path(__file__).resolve().parent.parent / "paper_2509_22951_b200" / "csrc"
 
 
@@ -12,3 +14,9 @@ def test_the_workspace_knows_its_callers():
     assert len(users) == 3
     for f in users:
         assert f.name == "tq_attn.cu" or f"{f.stem}_workspace_bytes()" in size, f.name
+
+
+def test_tree_attention_counts_its_units_in_32_bits():
+    """Half a billion sequences of one token and one tile: four units each over two key-value heads are more than 2^32."""
+    assert _tree(_cache(), T=(1 << 29) - 1, B=1 << 30, max_pages=1) == -4
+    assert _tree(_cache(), T=0, B=1 << 30, max_pages=1) == 0
