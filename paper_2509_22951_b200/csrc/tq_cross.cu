@@ -867,10 +867,13 @@ int launch(const CrossParams& p, const CUtensorMap& k_map, const CUtensorMap& v_
   constexpr size_t smem = CrossSmem<D>::kTotal + 1024;
   const char* what = "cross attention (tensor core) launch";
   if (int rc = tq_ensure_dynamic_smem((const void*)kern, smem, what)) return rc;
-  static const int regs = [&] {
+  static std::atomic<int> known{0};  // registers a thread; a query that has failed is made again
+  int regs = known.load(std::memory_order_relaxed);
+  if (regs == 0) {
     cudaFuncAttributes a{};
-    return cudaFuncGetAttributes(&a, (const void*)kern) == cudaSuccess ? a.numRegs : 0;
-  }();
+    if (int rc = tq_cuda_status((int)cudaFuncGetAttributes(&a, (const void*)kern), what)) return rc;
+    known.store(regs = a.numRegs, std::memory_order_relaxed);
+  }
   if (256 * kSoftRegs + 128 * kOtherRegs > kCrossThreads * regs) return tq_cuda_status((int)cudaErrorInvalidConfiguration, what);
   const uint32_t grid = min((uint32_t)sm_count(), kAttnMaxCtas);
   if (int rc = launch_pdl(kern, dim3(grid), kCrossThreads, smem, st, what, p, k_map, v_map)) return rc;

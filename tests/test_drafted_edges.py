@@ -20,3 +20,10 @@ def test_tree_attention_counts_its_units_in_32_bits():
     """Half a billion sequences of one token and one tile: four units each over two key-value heads are more than 2^32."""
     assert _tree(_cache(), T=(1 << 29) - 1, B=1 << 30, max_pages=1) == -4
     assert _tree(_cache(), T=0, B=1 << 30, max_pages=1) == 0
+
+
+def test_a_failed_query_of_a_kernel_is_not_kept():
+    """The register counts that a launch checks: what is kept between calls is a count, not that there was none."""
+    for name in ("tq_tree.cu", "tq_cross.cu"):
+        text = (CSRC / name).read_text()
+        assert "static const int regs" not in text and re.search(r"cudaFuncGetAttributes\(&a, \(const void\*\)kern\), what\)\) return rc;\s+known.store", text)
