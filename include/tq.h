@@ -547,7 +547,8 @@ int tq_qk_norm_rope_append(const void* d_q, const void* d_k, const void* d_v, in
  *   out[row][h] = sum_s softmax_s(scale * q[row][h] . k_s) v_s,  lse[row][h] the natural logarithm of the denominator;
  * a token that sees nothing gives zeros and lse -inf.  States that a token does not see may hold anything, Inf and NaN included (a token
  * is slow where another token of its sequence sees such a state: its output is computed again, which over more than 300000 states may
- * end in TQ_STATUS_WAIT_EXPIRED).  The same call gives the same bits.
+ * end in TQ_STATUS_WAIT_EXPIRED).  The same call gives the same bits.  p is rounded to bf16 for the product with v, its sum is not: beside the scores' fp32 errors
+ * out is within 2^-8 of sum p |v| / sum p before its own rounding (tq_paged_attention, for one token, keeps 16 bits of p).
  * d_q: DEVICE bf16, n_tokens rows of [n_q_heads][head_dim], q_stride elements from row to row (multiple of 8), 16-byte aligned.
  * Page table, lengths, workspace and status are those of tq_paged_attention, d_out bf16 [n_tokens][n_q_heads][head_dim],
  * d_lse fp32 [n_tokens][n_q_heads] or NULL.  Fewer states than new tokens (lens[b] < n): the first ones have none.

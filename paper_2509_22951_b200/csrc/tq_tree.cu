@@ -29,6 +29,13 @@
 //   512 tokens 28.0 | 27.5, 33 tokens over 1000 states 18.2 | 16.9.
 //   Of 256 rows x 128 states some 3200 cycles are left beside the 2048 of the tensor core at its full rate: a half's softmax takes 2100 (exponentials
 //   1450, 1024 at the special function unit's rate; maxima 450), its next scores come some 1300 after its p.
+// Bits of p: rounded to one bf16 number for the product with V (the sum of p is fp32 and takes it unrounded).  The error against 64 bits is then 2.1 -
+// 2.3e-3 of the result's norm, where the rounding of the result alone makes 1.64 - 1.67e-3.  Two numbers, which hold 16 of p's bits, as in tq_paged_attention
+// for one token, leave the result's rounding alone, but want a second product: the kernel is not bound by the tensor core, but a tile's chain
+// gets longer by it, and at the power limit the clock lower.  One | two (us, in a graph): 8 ragged 37.3 | 39.1, 131071 states 110.5 | 117.8, 64 chains 398 -
+// 403 | 441 - 494, pieces of prompts 191 - 213 | 249 - 265; only calls of a few tiles lose nothing (197 states 12.36 | 12.36).  (The lower parts in lanes 64 - 127 of
+// tiles with up to 64 rows, beside a copy of the queries, without a second product: twice the exponentials, 8 ragged 49.)  So it is one.
+//
 // The output is rescaled only when a row's maximum has grown by more than 2^8 since the last rescaling (online softmax with the rescaling
 // delayed up to a threshold, as in the kernel of cross attention): p stays below 2^8, which costs no precision in bf16 or the fp32 sum.
 //

@@ -100,6 +100,24 @@ def test_pages_outside_the_pool_are_zeros(tq, ws, D, H, n, page):
         within(got[0][:, h], want, bound)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("H,n", [(4, 7), (16, 9), (16, 40)])  # the last with 256 rows a tile
+@pytest.mark.parametrize("length", [1, 70, 900])
+def test_an_infinite_value_makes_its_column_infinite(tq, ws, D, H, n, length):
+    """Seen by all, with every p above 0: its own column and no other."""
+    g, K, page = gen(D + n + length), 2, 16
+    P = 60
+    kp, vp = randn(g, P, K, page, D, dtype=BF, scale=0.2), randn(g, P, K, page, D, dtype=BF)
+    vp[0, :, 0, 5], vp[0, :, 0, 9] = INF, -INF
+    kp[0, 0, 0] = kp[0, 0, 0] * 30
+    table = torch.arange(P, device="cuda", dtype=torch.int32)[None].contiguous()
+    q = randn(g, n, H, D, dtype=BF)
+    out = tq.tq_tree_attention(q, tq.tq_kv_cache(kp, vp), table, i32([0, n]), i32([length + n - 1]), ws)
+    assert bool((out[..., 5] == INF).all()) and bool((out[..., 9] == -INF).all())
+    others = [c for c in range(D) if c not in (5, 9)]
+    assert bool(out[..., others].isfinite().all())
+
+
 @pytest.mark.parametrize("D,H,n,length", [(128, 32, 40, 9000), (64, 32, 40, 9000), (128, 8, 3, 20000)])
 def test_a_workspace_of_the_stated_size_is_enough(tq, D, H, n, length):
     """Parts of cut groups of both forms: nothing behind the workspace's stated size is written."""
