@@ -6,7 +6,8 @@
 // order, so that neither the split of a row nor the order of atomics can change a token.  With A a multiple of 1/32 next to max log2(e) / temperature,
 // one fused multiply-add rounds t to 1/32 and another, which takes that from the exact product again, leaves the rest to 2^-31: the first is a
 // place in a table of 2^(i/32) (a bank of shared memory for each entry) and an octave, the second goes into a polynomial: 26 bits and more in some
-// 25 instructions, none of them a conversion.  W below 2^21 (t < -24) is the fp32 exponential, to some units.
+// 25 instructions, none of them a conversion; W is then a whole number (within 2^-26 of itself and half a unit).  W below 2^21 (t < -24) is the fp32
+// exponential of an fp32 exponent: within five units (its three roundings, and c_low left out: 2^-20 of t each at most; ex2's 2^-22; a rounding).
 //
 // Order.  Tokens fall by (x, lower index first): as one integer, the logit's bits made to rise with it above the index turned
 // round.  What is kept is all that is not below a border in that order, so every filter is a search for its border.
@@ -44,7 +45,7 @@ constexpr uint32_t kIndexBits = 18;
 static_assert((1u << kIndexBits) == TQ_SAMPLE_MAX_VOCAB, "a token's index fits its place in the order");
 constexpr uint32_t kIndexMask = (1u << kIndexBits) - 1u;
 constexpr int kOne = 45;      // W of the largest logit is 2^45
-constexpr int kOctaves = 24;  // of the histogram, and of the weights that are computed to 29 bits
+constexpr int kOctaves = 24;  // of the histogram, and of the weights that are computed to 26 bits; rounded to whole units, the least of them keep 22
 constexpr int kTopPlace = 1;  // place of the largest logit at most (a is off by up to 1/64 and a little)
 constexpr uint32_t kBins = kOctaves * 32u + kTopPlace + 1u;  // a place each
 constexpr uint32_t kList = 2048;   // tokens that one CTA sorts
