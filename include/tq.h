@@ -571,7 +571,8 @@ int tq_tree_attention(const tq_kv_cache* cache, const void* d_q, int64_t q_strid
  * A NaN counts as -inf.  Where some x_i are +inf they alone are kept, as equals.  A row without anything above -inf gives token -1 and
  * logprob -inf.  vocab: 1..TQ_SAMPLE_MAX_VOCAB.
  * Weights are held as integers, the largest as 2^45 and each within 2^-26 of itself and half a unit (below 2^21, five units), and their sums are exact: a
- * row's token depends on nothing but the row.  Temperatures below 2^-120 and above 2^100 are taken as
+ * row's token depends on nothing but the row.  (A row with k above 1024, or with thousands of tokens next to top_p's border, takes seven to thirty times as
+ * long as others.)  Temperatures below 2^-120 and above 2^100 are taken as
  * those, settings that are NaN as not given. */
 #define TQ_SAMPLE_MAX_VOCAB 262144u
 int tq_sample(const void* d_logits, int x_type, int64_t row_stride, uint32_t rows, uint32_t vocab,

@@ -239,8 +239,8 @@ struct Weights {
     const float t = d.hi * c;
     return Pair{t, fmaf(d.lo, c, fmaf(d.hi, c_low, fmaf(d.hi, c, -t)))};
   }
-  // A sum s of t with 1.5 * 2^18 is rounded to 1/32.  Below the histogram's octaves a weight is small, and that is told from s itself: below 2^18
-  // (t < -131072: a mask of -65504 at a temperature of 0.2) its bits say nothing of t, and taken for a place they could be any.
+  // A sum s of t with 1.5 * 2^18 is rounded to 1/32.  Below the histogram's octaves a weight is small, and that is told from s itself: below 0
+  // (t < -393216: a mask of -65504 at a temperature of 0.2) its bits fall with t, and a place taken from them could be any.
   static constexpr float kRound = 393216.0f, kLeastSum = kRound - (float)kOctaves;
   __device__ __forceinline__ static bool is_small(float s) { return s < kLeastSum; }
   // 32 t rounded, of the sum of a weight that is not small.

@@ -26,7 +26,8 @@
 //          run during the other's softmax; the product with V begins when the first 64 states have their p.
 //   256 rows are taken where the sequences have more than 128 on average.  us, 256 rows | 128 rows, 32 heads on 8 of 128: 4096 tokens of a prompt
 //   194 | 246, 40 tokens over 131071 states 139 | 173, 64 sequences of up to 64 tokens and 4096 states 180 | 204; where it does not matter:
-//   512 tokens 28.0 | 27.5, 33 tokens over 1000 states 18.2 | 16.9.
+//   512 tokens 28.0 | 27.5, 33 tokens over 1000 states 18.2 | 16.9.  The average says little of a mix: a piece of 1024 tokens of 9001 with 63 sequences of one
+//   token and 4096 states goes by tiles of 128, 321 us, where the two by themselves take 161 and 178.
 //   Of 256 rows x 128 states some 3200 cycles are left beside the 2048 of the tensor core at its full rate: a half's softmax takes 2100 (exponentials
 //   1450, 1024 at the special function unit's rate; maxima 450), its next scores come some 1300 after its p.
 // Bits of p: rounded to one bf16 number for the product with V (the sum of p is fp32 and takes it unrounded).  The error against 64 bits is then 2.1 -
@@ -43,7 +44,7 @@
 // bytes: 19); 31 tokens over 131071 states, 32 heads 104 (82); 64 chains of 5 tokens over up to 16384 states, 64 heads 392 (386), 453 under the
 // power limit; pieces of 1024 tokens of two prompts up to 9001 long, 32 heads 184, 207 under the limit (operations at the rate of a library product: 106).
 //
-// States that are not there (past the end, on a page outside the pool) are zeros in shared memory and hidden from all rows.  A state that only
+// States that are not there (past the end, on a page outside the pool) are hidden from all rows, and their values zeros in shared memory.  A state that only
 // some rows see enters the others' sums with p = 0; if its value is Inf or NaN that product is NaN, so a row whose sum of p is finite but whose
 // output has a NaN is computed again from the states it sees (slow).
 //
@@ -210,7 +211,8 @@ static_assert(sizeof(Plan) <= 96 && alignof(Plan) <= 16, "room for the plan");
 constexpr uint32_t kWholeTiles = 3;
 // Where the page table has no room for longer sequences than this, none is cut and the joining kernel is not launched.  us, never cut | cut as the
 // lengths have it, 32 / 8 heads of 128, 8 new tokens: 1 sequence of 100 states 9.2 | 10.8, 16 of 500 15.5 | 18.7, 64 of 250 31.6 | 34.5; 512 tokens
-// of a prompt 24 | 28; but 1 sequence of 1000 states 17.2 | 14.7, of 760 14.9 | 13.8.
+// of a prompt 24 | 28; but 1 sequence of 1000 states 17.2 | 14.7, of 760 14.9 | 13.8.  (The lengths are known on the device only: a table wider than its
+// sequences, as a program that serves has it, is on the right-hand side of these.)
 constexpr uint32_t kNeverCutTiles = 4;
 
 __device__ __forceinline__ Plan make_plan(const TreeParams& p, uint32_t lane) {
